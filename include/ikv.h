@@ -213,9 +213,13 @@ int64_t ikv_launch_count(void);
  * the device).  0 = no error.  Bit 0: a bounded wait inside the tensor-core
  * attention kernel ran out (the kernel abandoned its work and returned);
  * bit 1: a split longer than the kernel's TMEM budget reached the device;
- * bit 2: an append found no free slot (start + len = cap) and was dropped;
+ * bit 2: an append found no free slot (start + len = cap) and was dropped, or
+ * ikv_pages_writable was asked for slots past a sequence's slot space;
  * bit 3: per-layer eviction, a sequence's next_pos reached cache->pos_cap (the token
- * was dropped); bit 4: a rank-trace set exceeded 16384 tokens (not traced). */
+ * was dropped); bit 4: a rank-trace set exceeded 16384 tokens (not traced);
+ * bit 5: rows of ikv_q4_store or ikv_q4_load lay outside a sequence's slot space (left alone);
+ * bit 6: ikv_pages_writable or ikv_pages_compact needed more pages than were free (nothing was
+ * done); bit 7: a sequence number or a block table entry that a page call met was out of range. */
 ikv_status ikv_device_status(uint32_t *flags);
 
 /* Test of the bounded waits (no counterpart in the paper): the next tensor-core attention
@@ -442,6 +446,134 @@ ikv_status ikv_step_layer(const ikv_shape *shape, const ikv_params *params, ikv_
                           size_t ws_bytes, cudaStream_t stream);
 ikv_status ikv_step_end(const ikv_shape *shape, const ikv_params *params, ikv_cache *cache, float *ema, int32_t t,
                         void *ws, size_t ws_bytes, cudaStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Caches held in 4 bits
+ *
+ * A quarter of a bf16 cache's bytes: decode attention, which is bound by reading the cache,
+ * reads 4.5 bits a value.  cache->k and cache->v then are code pools
+ * [layers][num_pages][kv_heads][page_size][head_dim / 2] (bytes), and ikv_q4 adds the scale
+ * pools [layers][num_pages][kv_heads][page_size][head_dim / 32] (bf16).  page_size must be a
+ * multiple of 16.  Everything else of ikv_cache keeps its meaning (block table, start, len,
+ * pos, dead slots), so ikv_select_budget, ikv_ema_update and the ikv_pages_* calls serve such a
+ * cache as they are; shape->dtype is the type of q, out and of the dense rows.  cache->vnorm
+ * is not used.
+ *
+ * Each row is cut into groups of 32 channels.  With a the largest magnitude of a group:
+ *   scale s = the smallest bf16 number with 6 s >= a; 0 if a < 2^-120 (the group reads as
+ *     zeros); NaN if a > 2^127 or any value is infinite or NaN (the group reads as NaN)
+ *   code    = a sign and the magnitude of {0, 0.5, 1, 1.5, 2, 3, 4, 6} nearest |x| / s, the
+ *     larger of two as near: bit for bit defined by the row alone
+ *   value   = magnitude * s with the sign, rounded once to the dense type where that is bf16.
+ * In a row of D = head_dim channels, byte u * (D / 16) + 2 y + h (u < 8, y < D / 32, h < 2)
+ * holds the codes of channels 32 y + 4 u + 2 h (low half) and the one after it; bit 3 of a code
+ * is the sign, bits 0..2 number the magnitudes in ascending order.  Slots outside a sequence
+ * may hold anything.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    void *k_scale, *v_scale;     /* scale pools (device), 16-byte aligned */
+} ikv_q4;
+
+/* Where dense K / V rows lie, in elements: element e of row i of sequence b, layer li (of the
+ * call's layers), KV head g is at li * layer + off(b) + i * token + g * head + e, with
+ * off(b) = row0 ? row0[b] * token : b * seq.  Multiples of 8 (bf16) or 4 (fp32). */
+typedef struct {
+    int64_t layer, seq, token, head;
+    const int32_t *row0;         /* [batch] (device) first row of each sequence in packed rows, or NULL */
+} ikv_rows;
+
+/* ikv_q4_store quantises count[b] rows of K and of V into slots first[b] .. of layers
+ * [layer0, layer0 + n_layers); ikv_q4_load turns those slots' rows back into dense ones.
+ *  k, v: dense rows (dtype, 16-byte aligned), laid out as `rows` says.
+ *  first: [batch] (device) first slot; a sequence with first[b] < 0 is left out.  NULL: the
+ *    newest slots, len[b] - n .. len[b] - 1 with n = min(count[b], len[b]).
+ *  count: [batch] (device) rows of each sequence, cut to max_count; NULL: max_count each.
+ * A sequence whose rows would reach past its slot space is left alone and sets bit 5 of the
+ * device error word.  The pages of the slots are written in place: a page that several
+ * sequences share is made the writer's own first (ikv_pages_writable). */
+ikv_status ikv_q4_store(const ikv_shape *shape, const ikv_cache *cache, const ikv_q4 *q4, int32_t layer0,
+                        int32_t n_layers, const void *k, const void *v, const ikv_rows *rows, const int32_t *first,
+                        const int32_t *count, int32_t max_count, cudaStream_t stream);
+ikv_status ikv_q4_load(const ikv_shape *shape, const ikv_cache *cache, const ikv_q4 *q4, int32_t layer0,
+                       int32_t n_layers, void *k, void *v, const ikv_rows *rows, const int32_t *first,
+                       const int32_t *count, int32_t max_count, cudaStream_t stream);
+
+/* ikv_append_token for a 4-bit cache: the same books (position, utility, len, next_pos), and
+ * slot[b] (device [batch], written) receives the new token's slot, -1 where there was no room.
+ * k_new / v_new ([layers][batch][kv_heads][head_dim], dtype) are stored there in every layer; both
+ * may be NULL for a model that has a layer's rows only when it gets there: it then calls
+ * ikv_q4_store(layer0 = l, n_layers = 1, first = slot, count = NULL, max_count = 1) in each layer. */
+ikv_status ikv_q4_append_token(const ikv_shape *shape, ikv_cache *cache, const ikv_q4 *q4, const void *k_new,
+                               const void *v_new, float *ema, int32_t init_mean, int32_t *slot, cudaStream_t stream);
+
+/* ikv_decode_attend_score over a 4-bit cache: out = softmax(q K^T / sqrt(d)) V over the values
+ * that the codes stand for, score and ema as there, ws of ikv_attend_workspace_size() bytes.  A
+ * sequence without a live slot gets out = 0.  Slots outside [0, len[b]) are never used, whatever
+ * they hold. */
+ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, const ikv_q4 *q4, int32_t layer,
+                               const void *q, void *out, float *score, float *ema, float alpha, void *ws,
+                               size_t ws_bytes, cudaStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Page pools: sequences that share, take and give back pages
+ *
+ * For a cache whose pages are handed out as sequences grow.  A block table entry of 0 means "no
+ * page": page 0 belongs to nobody, is never handed out and must hold finite values (it is what
+ * reads past a sequence's end may touch).  refs[p] counts the entries that hold page p; a page
+ * with refs 0 is free.  The caller starts with every entry 0, refs[0] = 1 and the others 0, and
+ * changes them only through these calls, which hand out the lowest free pages first, in the
+ * order of sequences and slots.  All are asynchronous and may be captured in a graph.
+ * The planes are the arrays paged alike: K and V, and for a 4-bit cache both scale pools.
+ * Writes into a page that several sequences hold reach them all: call ikv_pages_writable for the
+ * slots that ikv_q4_store, ikv_append_token, ikv_step or ikv_compact_kv are about to write.
+ * ------------------------------------------------------------------------- */
+enum { IKV_MAX_PLANES = 4 };
+typedef struct {
+    int32_t *refs;               /* [num_pages] (device) */
+    int32_t n_planes;            /* 1 .. IKV_MAX_PLANES */
+    void *plane[IKV_MAX_PLANES]; /* [layers][num_pages][kv_heads][page_size][row_bytes] (device), 16-byte
+                                    aligned */
+    int32_t row_bytes[IKV_MAX_PLANES]; /* bytes of a plane's row, a multiple of 4 */
+} ikv_pages;
+
+ikv_status ikv_pages_workspace_size(const ikv_shape *shape, const ikv_cache *cache, const ikv_pages *pages,
+                                    size_t *bytes);
+
+/* Gives back every page that holds none of a sequence's slots 0 .. len[b] + extra - 1 (len[b] = 0: all
+ * of its pages): its entries become 0 and the pages' refs drop. */
+ikv_status ikv_pages_release(const ikv_shape *shape, ikv_cache *cache, const ikv_pages *pages, int32_t extra,
+                             cudaStream_t stream);
+
+/* Sequence dst[i] continues from sequence src[i], i < n (both device [n]): it shares every page of
+ * src[i], whose refs grow, and takes over len, next_pos, start, its rows of pos, of ema (or NULL) and of
+ * vnorm.  No page is copied: ikv_pages_writable does that where a sequence first writes.  Each
+ * dst[i] holds no page (ikv_pages_release at len 0), appears once and is no src. */
+ikv_status ikv_pages_fork(const ikv_shape *shape, ikv_cache *cache, const ikv_pages *pages, int32_t n,
+                          const int32_t *src, const int32_t *dst, float *ema, cudaStream_t stream);
+
+/* Makes slots first[b] .. first[b] + count[b] - 1 of every sequence its own to write: a slot without a
+ * page gets a free one, a page that others hold too is copied (the rows of slots 0 .. len[b] - 1 that
+ * lie in it, in every layer, plane and KV head).  Of the sequences of one call that would write a
+ * shared page which nobody else holds, the last keeps it.
+ *  first: [batch] (device), < 0: sequence left out; NULL: len[b], the slots behind the last.
+ *  count: [batch] (device), cut to max_count; NULL: max_count each.
+ *  lacking: (device, or NULL) receives 0, or how many more free pages the call would have needed:
+ *    then bit 6 of the device error word is set and nothing is changed.
+ * A sequence whose slots would pass its slot space is left out and sets bit 2. */
+ikv_status ikv_pages_writable(const ikv_shape *shape, ikv_cache *cache, const ikv_pages *pages, const int32_t *first,
+                              const int32_t *count, int32_t max_count, int32_t *lacking, void *ws, size_t ws_bytes,
+                              cudaStream_t stream);
+
+/* The stable compaction of ikv_compact_kv into pages of the sequence's own: slot j holds what slot
+ * keep[r][j] held, j < keep_len[r], pos, ema (or NULL) and vnorm with it, len[b] = keep_len[r].  Pages in
+ * front of the first slot that moves stay as they are, shared or not; the survivors behind it are
+ * gathered into free pages, and the old pages are given back (also when only the end was cut off,
+ * which copies nothing).  start stays.  A sequence with keep_len < 0 is left alone.  keep and keep_len
+ * as ikv_select_budget produces them; the rows of one sequence keep the same number.
+ *  lacking as in ikv_pages_writable: too few free pages leave everything as it was. */
+ikv_status ikv_pages_compact(const ikv_shape *shape, ikv_cache *cache, const ikv_pages *pages, const int32_t *keep,
+                             const int32_t *keep_len, float *ema, int32_t *lacking, void *ws, size_t ws_bytes,
+                             cudaStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -14,7 +14,7 @@ import torch
 
 from . import ikv
 
-__all__ = ["ikv", "DecodeCache", "RankTrace", "step_lengths", "auto_max_holes"]
+__all__ = ["ikv", "DecodeCache", "Q4Cache", "RankTrace", "step_lengths", "auto_max_holes"]
 
 
 def auto_max_holes(budgets: Sequence[int]) -> int:
@@ -65,22 +65,29 @@ class DecodeCache:
     def __init__(self, batch: int, layers: int, q_heads: int, kv_heads: int, head_dim: int, cap_tokens: int,
                  dtype: int = ikv.IKV_BF16, page_size: int = 64, granularity: int = ikv.IKV_GRAN_SEQ,
                  device: str = "cuda", page_perm_seed: Optional[int] = None, value_norms: bool = False,
-                 pos_cap: int = 0):
+                 pos_cap: int = 0, pool_pages: Optional[int] = None):
         self.batch, self.layers, self.q_heads, self.kv_heads, self.head_dim = batch, layers, q_heads, kv_heads, head_dim
         self.dtype, self.granularity, self.page_size = dtype, granularity, page_size
         self.max_pages = (cap_tokens + page_size - 1) // page_size
         self.cap = self.max_pages * page_size
-        self.num_pages = batch * self.max_pages
+        self.num_pages = batch * self.max_pages if pool_pages is None else pool_pages + 1
         tdt = torch.bfloat16 if dtype == ikv.IKV_BF16 else torch.float32
         self.torch_dtype = tdt
-        shp = (layers, self.num_pages, kv_heads, page_size, head_dim)
-        self.k = torch.zeros(shp, dtype=tdt, device=device)
-        self.v = torch.zeros(shp, dtype=tdt, device=device)
+        self._alloc_pools((layers, self.num_pages, kv_heads, page_size), device)
+        # pages handed out as sequences grow (ikv_pages_*): no sequence holds one yet, and page 0
+        # stands for none; otherwise every sequence owns max_pages pages for good
+        self.refs = None
+        if pool_pages is not None:
+            self.refs = torch.zeros(self.num_pages, dtype=torch.int32, device=device)
+            self.refs[0] = 1
         pages = torch.arange(self.num_pages, dtype=torch.int32)
         if page_perm_seed is not None:
             g = torch.Generator().manual_seed(page_perm_seed)
             pages = pages[torch.randperm(self.num_pages, generator=g)]
-        self.block_table = pages.view(batch, self.max_pages).to(device)
+        if pool_pages is None:
+            self.block_table = pages.view(batch, self.max_pages).to(device)
+        else:
+            self.block_table = torch.zeros((batch, self.max_pages), dtype=torch.int32, device=device)
         self.rows = batch if granularity == ikv.IKV_GRAN_SEQ else batch * kv_heads
         self.len = torch.zeros(batch, dtype=torch.int32, device=device)
         self.next_pos = torch.zeros(batch, dtype=torch.int32, device=device)
@@ -100,7 +107,22 @@ class DecodeCache:
                       if value_norms else None)
         self.max_len = 0
 
+    def _alloc_pools(self, shp, device) -> None:
+        self.k = torch.zeros(shp + (self.head_dim,), dtype=self.torch_dtype, device=device)
+        self.v = torch.zeros(shp + (self.head_dim,), dtype=self.torch_dtype, device=device)
+
+    def planes(self):
+        """The arrays paged alike, for the ikv_pages_* calls."""
+        return [self.k, self.v]
+
     # ---- ABI structs ------------------------------------------------------
+    def pages(self) -> ikv.ikv_pages:
+        return ikv.ikv_pages_of(self.refs, self.planes())
+
+    def pages_workspace(self) -> torch.Tensor:
+        n = ikv.ikv_pages_workspace_size(self.shape(), self.cache(), self.pages())
+        return torch.empty(n, dtype=torch.uint8, device=self.k.device)
+
     def shape(self) -> ikv.ikv_shape:
         return ikv.ikv_shape(self.batch, self.layers, self.q_heads, self.kv_heads, self.head_dim, self.dtype,
                              self.granularity)
@@ -182,6 +204,37 @@ class DecodeCache:
             p.trace = _ct.pointer(trace.struct)
             self._trace = trace
         return p
+
+
+class Q4Cache(DecodeCache):
+    """A DecodeCache held in 4 bits (include/ikv.h, "Caches held in 4 bits"): k and v are code pools
+    [layers][num_pages][kv_heads][page_size][head_dim / 2], k_scale and v_scale their scales; dtype is
+    the type of q, out and of the rows that ikv_q4_store takes."""
+
+    def _alloc_pools(self, shp, device) -> None:
+        self.k = torch.zeros(shp + (self.head_dim // 2,), dtype=torch.uint8, device=device)
+        self.v = torch.zeros(shp + (self.head_dim // 2,), dtype=torch.uint8, device=device)
+        self.k_scale = torch.zeros(shp + (self.head_dim // 32,), dtype=torch.bfloat16, device=device)
+        self.v_scale = torch.zeros(shp + (self.head_dim // 32,), dtype=torch.bfloat16, device=device)
+
+    def planes(self):
+        return [self.k, self.v, self.k_scale, self.v_scale]
+
+    def q4(self) -> ikv.ikv_q4:
+        return ikv.ikv_q4(self.k_scale.data_ptr(), self.v_scale.data_ptr())
+
+    def dense_rows(self, k: torch.Tensor, row0: Optional[torch.Tensor] = None) -> ikv.ikv_rows:
+        """How dense rows lie: [layers][batch][tokens][kv_heads][head_dim], or packed
+        [layers][tokens][kv_heads][head_dim] with the first row of every sequence in row0; any
+        strides but the last."""
+        st = k.stride()
+        if row0 is not None:
+            return ikv.ikv_rows(st[0], 0, st[1], st[2], row0.data_ptr())
+        return ikv.ikv_rows(st[0], st[1], st[2], st[3], None)
+
+    def attend_workspace(self) -> torch.Tensor:
+        n = ikv.ikv_attend_workspace_size(self.shape(), self.cache())
+        return torch.empty(n, dtype=torch.uint8, device=self.k.device)
 
 
 import ctypes as _ct  # noqa: E402

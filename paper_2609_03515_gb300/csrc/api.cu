@@ -30,15 +30,9 @@ ikv_status fail(ikv_status s, const char *fmt, ...) {
     return s;
 }
 
-ikv_status cuda_fail(cudaError_t e, const char *what) {
-    return fail(IKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
-}
+}  // namespace
 
-#define IKV_TRY_CUDA(expr, what)                         \
-    do {                                                 \
-        cudaError_t _e = (expr);                         \
-        if (_e != cudaSuccess) return cuda_fail(_e, what); \
-    } while (0)
+void clear_error() { g_err[0] = 0; }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -108,10 +102,6 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 int32_t logit_stride(int32_t cap) { return (cap + 127) / 128 * 128; }
 
-struct AttendWs {
-    size_t part_ml, part_o, lse2, arrivals, logits, end;
-};
-
 AttendWs attend_ws(const ikv_shape *s, int32_t cap, int n_layers, bool logits) {
     AttendWs w;
     size_t off = 0;
@@ -129,6 +119,8 @@ AttendWs attend_ws(const ikv_shape *s, int32_t cap, int n_layers, bool logits) {
     w.end = off;
     return w;
 }
+
+namespace {
 
 struct StepWs {
     AttendWs at;
@@ -193,11 +185,6 @@ StepWs step_ws(const ikv_shape *s, int32_t cap, int32_t pos_cap) {
     off = align256(off + (size_t)s->batch * sizeof(int32_t));
     w.end = off;
     return w;
-}
-
-template <typename T>
-T *at(void *ws, size_t off) {
-    return reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(ws) + off);
 }
 
 // split-K partition of the kernels of attend.cu for lengths up to max_len: at most kMaxSplits

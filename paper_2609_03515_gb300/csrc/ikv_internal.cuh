@@ -29,6 +29,13 @@ void note_launch(int n = 1);
 // Set the thread's ikv_last_error() message and return `s` (host).
 ikv_status report(ikv_status s, const char *fmt, ...);
 
+void clear_error();
+#define IKV_TRY_CUDA(expr, what)                                                                          \
+    do {                                                                                                  \
+        cudaError_t _e = (expr);                                                                          \
+        if (_e != cudaSuccess) return ikv::report(IKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(_e)); \
+    } while (0)
+
 // Programmatic dependent launch.  While a PdlScope is alive on the issuing thread
 // (ikv_step, for the kernels after its first), kernels are launched with programmatic
 // stream serialisation: each may be scheduled while its predecessor drains.  Every
@@ -89,6 +96,26 @@ struct PagedView {
         return (((int64_t)l * num_pages + page) * kv_heads + g) * page_size + (phys - lp * page_size);
     }
 };
+
+// Host side of the entry points: argument checks, the cache as the kernels see it, and the
+// workspace of one attention (api.cu)
+bool aligned16(const void *p);
+int sm_count();
+ikv_status check_shape(const ikv_shape *s);
+ikv_status check_cache(const ikv_shape *s, const ikv_cache *c, bool need_pos);
+int rows_per_seq(const ikv_shape *s);
+int32_t cap_of(const ikv_cache *c);
+PagedView view_of(const ikv_shape *s, const ikv_cache *c);
+size_t align256(size_t x);
+int32_t logit_stride(int32_t cap);
+struct AttendWs {
+    size_t part_ml, part_o, lse2, arrivals, logits, end;
+};
+AttendWs attend_ws(const ikv_shape *s, int32_t cap, int n_layers, bool logits);
+template <typename T>
+T *at(void *ws, size_t off) {
+    return reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(ws) + off);
+}
 
 // Deferred compaction inside selection: when a row has exactly one slot too many and
 // the sequence may defer (len - budget <= max_holes and start + len < cap), select
@@ -348,6 +375,9 @@ cudaError_t launch_trace(const TraceArgs &a, cudaStream_t st);
 cudaError_t read_clear_trace_error(unsigned int *v);
 // reads and clears the append kernel's device error word (bit 0: no free slot)
 cudaError_t read_clear_append_error(unsigned int *v);
+// the same of the 4-bit stores and loads (bit 5) and of the page calls (bits 2, 6, 7)
+cudaError_t read_clear_q4_error(unsigned int *v);
+cudaError_t read_clear_pages_error(unsigned int *v);
 // the same of the kernels of attend.cu (bit 2)
 cudaError_t read_clear_attend_error(unsigned int *v);
 

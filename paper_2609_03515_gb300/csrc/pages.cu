@@ -1,0 +1,505 @@
+// Pages that sequences share, take and give back.
+//
+// Page 0 is nobody's: a block table entry of 0 means "no page", so that every entry names a valid
+// page whatever it is.  refs counts the entries that hold a page; a page with none is free.  Pages
+// are handed out lowest first, in the order of the sequences and their slots, so that a run can
+// be repeated.
+#include "q4.cuh"
+
+namespace ikv {
+
+__device__ unsigned int g_pages_error = 0;  // bit 2: slots past the slot space; bit 6: too few free pages; bit 7: bad index
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kCopyThreads = 256;
+constexpr int kRowThreads = 256;
+
+__device__ __forceinline__ int start_of(const PagesArgs &a, int b) { return a.start ? a.start[b] : 0; }
+
+// Exclusive prefix sum of x over the CTA (kPlanThreads threads), and the total.
+__device__ __forceinline__ int block_scan(int x, int *total) {
+    __shared__ int sums[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int y = x;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int z = __shfl_up_sync(0xffffffffu, y, d);
+        if (lane >= d) y += z;
+    }
+    __syncthreads();  // (the sums of a scan before)
+    if (lane == 31) sums[warp] = y;
+    __syncthreads();
+    if (warp == 0) {
+        int s = sums[lane];
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int z = __shfl_up_sync(0xffffffffu, s, d);
+            if (lane >= d) s += z;
+        }
+        sums[lane] = s;
+    }
+    __syncthreads();
+    *total = sums[31];
+    return y - x + (warp ? sums[warp - 1] : 0);
+}
+
+// The lowest `want` free pages into ids, by one CTA; how many there are, at most `want`.
+__device__ int find_free(const int32_t *refs, int pages, int want, int32_t *ids) {
+    constexpr int U = 8;
+    int found = 0;
+    for (int p0 = 1; p0 < pages && found < want; p0 += kPlanThreads * U) {
+        const int p = p0 + threadIdx.x * U;
+        uint32_t free = 0u;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u < pages && __ldcg(refs + p + u) == 0) free |= 1u << u;
+        int n;
+        int at = found + block_scan(__popc(free), &n);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (free >> u & 1u) {
+                if (at < want) ids[at] = p + u;
+                ++at;
+            }
+        found += n;
+    }
+    __syncthreads();
+    return min(found, want);
+}
+
+__global__ void __launch_bounds__(kRowThreads) release_kernel(const PagesArgs a, int extra) {
+    pdl_wait();
+    const int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
+    if (i >= (int64_t)a.batch * a.max_pages) return;
+    const int e = a.table[i];
+    if (e <= 0 || e >= a.num_pages) return;
+    const int b = (int)(i / a.max_pages), lp = (int)(i % a.max_pages);
+    const int64_t S = start_of(a, b), L = a.len[b], p0 = (int64_t)lp * a.page_size;
+    if (L > 0 && p0 + a.page_size > S && p0 < S + L + extra) return;
+    a.table[i] = 0;
+    atomicSub(a.refs + e, 1);
+}
+
+// CTAs (part, fork): the parent's table entries and counts, then its rows of pos, ema and vnorm.
+__global__ void __launch_bounds__(kRowThreads) fork_kernel(const PagesArgs a, const int32_t *src, const int32_t *dst) {
+    pdl_wait();
+    const int i = blockIdx.y, s = src[i], d = dst[i];
+    if (s < 0 || s >= a.batch || d < 0 || d >= a.batch || s == d) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(&g_pages_error, 128u);
+        return;
+    }
+    const int64_t at = (int64_t)blockIdx.x * kRowThreads + threadIdx.x, step = (int64_t)gridDim.x * kRowThreads;
+    for (int64_t p = at; p < a.max_pages; p += step) {
+        const int e = a.table[(int64_t)s * a.max_pages + p];
+        a.table[(int64_t)d * a.max_pages + p] = e;
+        if (e > 0 && e < a.num_pages) atomicAdd(a.refs + e, 1);
+    }
+    if (at == 0) {
+        a.len[d] = a.len[s];
+        if (a.next_pos) a.next_pos[d] = a.next_pos[s];
+        if (a.start) a.start[d] = a.start[s];
+    }
+    const int64_t n = (int64_t)a.rows_per_seq * a.cap;
+    for (int64_t j = at; j < n; j += step) {
+        if (a.pos) a.pos[d * n + j] = a.pos[s * n + j];
+        if (a.ema) a.ema[d * n + j] = a.ema[s * n + j];
+    }
+    if (a.vnorm) {
+        const int64_t m = (int64_t)a.kv_heads * a.cap;
+        for (int64_t j = at; j < m * a.layers; j += step) {
+            const int64_t l = j / m, x = j % m;
+            a.vnorm[(l * a.batch + d) * m + x] = a.vnorm[(l * a.batch + s) * m + x];
+        }
+    }
+}
+
+// One CTA decides which pages of the slots to be written are missing or shared, takes free ones for
+// them and lists the copies to make: {page, copy, first row, rows}.  Of the sequences of this call
+// that would write a shared page which nobody else holds, the last keeps it.
+__global__ void __launch_bounds__(kPlanThreads)
+writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, const int32_t *count, int max_count,
+                     int span, int32_t *lacking) {
+    pdl_wait();
+    const int64_t R = (int64_t)a.batch * span;
+    // the entry of request i, or -1: page lp of sequence b
+    auto request = [&](int64_t i, int *b, int *lp) -> int {
+        *b = (int)(i / span);
+        const int n = min(count ? count[*b] : max_count, max_count);
+        const int64_t f = (int64_t)start_of(a, *b) + (first ? first[*b] : a.len[*b]);
+        if (n <= 0 || (first && first[*b] < 0)) return -1;
+        if (f + n > a.cap) {
+            if (i % span == 0) atomicOr(&g_pages_error, 4u);
+            return -1;
+        }
+        const int64_t p = f / a.page_size + i % span;
+        if (p > (f + n - 1) / a.page_size) return -1;
+        *lp = (int)p;
+        const int e = a.table[(int64_t)*b * a.max_pages + p];
+        if (e >= 0 && e < a.num_pages) return e;
+        atomicOr(&g_pages_error, 128u);
+        return -1;
+    };
+    int b, lp;
+    for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
+        const int e = request(i, &b, &lp);
+        if (e > 0) {
+            w.count[e] = 0;
+            w.last[e] = -1;
+        }
+    }
+    __syncthreads();
+    for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
+        const int e = request(i, &b, &lp);
+        if (e > 0 && a.refs[e] > 1) {
+            atomicAdd(w.count + e, 1);
+            atomicMax(w.last + e, b);
+        }
+    }
+    __syncthreads();
+    auto needs = [&](int64_t i, int *b, int *lp, int *e) {
+        *e = i < R ? request(i, b, lp) : -1;
+        if (*e <= 0) return *e == 0;
+        const int r = __ldcg(a.refs + *e);
+        return r > 1 && !(__ldcg(w.count + *e) == r && __ldcg(w.last + *e) == *b);
+    };
+    int total = 0, e;
+    for (int64_t i0 = 0; i0 < R; i0 += kPlanThreads) {
+        int n;
+        block_scan(needs(i0 + threadIdx.x, &b, &lp, &e) ? 1 : 0, &n);
+        total += n;
+    }
+    const int have = find_free(a.refs, a.num_pages, total, w.free_ids);
+    if (threadIdx.x == 0) {
+        w.total[0] = have == total ? total : 0;
+        if (lacking) *lacking = total - have;
+        if (have < total) atomicOr(&g_pages_error, 64u);
+    }
+    if (have < total) return;
+    int done = 0;
+    for (int64_t i0 = 0; i0 < R; i0 += kPlanThreads) {
+        const int64_t i = i0 + threadIdx.x;
+        const bool need = needs(i, &b, &lp, &e);
+        int n;
+        const int at = done + block_scan(need ? 1 : 0, &n);  // (its barriers: everybody has read the counts)
+        done += n;
+        if (need) {
+            const int to = w.free_ids[at];
+            a.table[(int64_t)b * a.max_pages + lp] = to;
+            a.refs[to] = 1;
+            int32_t *job = w.jobs + 4 * (int64_t)at;
+            // rows of the page that hold slots in use
+            const int64_t S = start_of(a, b), p0 = (int64_t)lp * a.page_size;
+            const int r0 = (int)min(max(S - p0, (int64_t)0), (int64_t)a.page_size);
+            const int r1 = (int)min(max(S + a.len[b] - p0, (int64_t)0), (int64_t)a.page_size);
+            job[0] = e;
+            job[1] = to;
+            job[2] = r0;
+            job[3] = e > 0 ? max(r1 - r0, 0) : 0;
+        }
+    }
+    __syncthreads();
+    // the copied pages' holders go once no count is read any more
+    for (int64_t i = threadIdx.x; i < total; i += kPlanThreads) {
+        const int e = w.jobs[4 * i];
+        if (e > 0) atomicSub(a.refs + e, 1);
+    }
+}
+
+// Copies of jobs x layers x planes x KV heads: a run of rows each.
+template <typename V>
+__device__ __forceinline__ void copy_run(unsigned char *dst, const unsigned char *src, int n) {
+    constexpr int U = 4;
+    const V *s = reinterpret_cast<const V *>(src);
+    V *d = reinterpret_cast<V *>(dst);
+    n /= (int)sizeof(V);
+    for (int i0 = threadIdx.x; i0 < n; i0 += kCopyThreads * U) {
+        V x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + u * kCopyThreads < n) x[u] = s[i0 + u * kCopyThreads];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + u * kCopyThreads < n) d[i0 + u * kCopyThreads] = x[u];
+    }
+}
+__global__ void __launch_bounds__(kCopyThreads) writable_copy_kernel(const PagesArgs a, const PagesWs w) {
+    pdl_wait();
+    const int64_t per = (int64_t)a.layers * a.n_planes * a.kv_heads, items = (int64_t)w.total[0] * per;
+    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
+        const int4 job = *reinterpret_cast<const int4 *>(w.jobs + 4 * (i / per));
+        if (job.w <= 0) continue;
+        const int x = (int)(i % per), g = x % a.kv_heads, y = x / a.kv_heads, pl = y % a.n_planes, l = y / a.n_planes;
+        const int64_t rb = a.row_bytes[pl];
+        auto row = [&](int page) { return ((((int64_t)l * a.num_pages + page) * a.kv_heads + g) * a.page_size + job.z) * rb; };
+        unsigned char *d = a.plane[pl] + row(job.y);
+        const unsigned char *s = a.plane[pl] + row(job.x);
+        const int n = job.w * (int)rb;
+        if (rb % 16 == 0) copy_run<uint4>(d, s, n);
+        else copy_run<uint32_t>(d, s, n);
+    }
+}
+
+// One CTA: where each sequence's first moved slot lies, the pages it makes anew, the free pages for
+// them.  keep[j] >= j rises with j, so the slots that stay are a prefix, found by bisection.
+__global__ void __launch_bounds__(kPlanThreads)
+compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int32_t *lacking) {
+    pdl_wait();
+    int total = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {
+        const int b = b0 + threadIdx.x;
+        int need = 0;
+        if (b < a.batch) {
+            const int64_t r0 = (int64_t)b * a.rows_per_seq;
+            const int n = min(keep_len[r0], a.cap);
+            int begin = a.max_pages;  // a sequence that is left alone
+            if (n >= 0) {
+                int f = n;
+                for (int r = 0; r < a.rows_per_seq; ++r) {
+                    const int32_t *k = keep + (r0 + r) * a.cap;
+                    int lo = 0, hi = f;
+                    while (lo < hi) {
+                        const int mid = (lo + hi) >> 1;
+                        if (k[mid] == mid) lo = mid + 1;
+                        else hi = mid;
+                    }
+                    f = lo;
+                }
+                const int S = start_of(a, b), end = (S + n + a.page_size - 1) / a.page_size;
+                begin = f == n ? end : (S + f) / a.page_size;
+                need = end - begin;
+            }
+            w.begin[b] = begin;
+        }
+        int n;
+        const int at = total + block_scan(need, &n);
+        if (b < a.batch) w.base[b] = at;
+        total += n;
+    }
+    if (threadIdx.x == 0) w.base[a.batch] = total;
+    const int have = find_free(a.refs, a.num_pages, total, w.free_ids);
+    if (threadIdx.x == 0) {
+        w.total[0] = have == total ? total : 0;
+        w.total[1] = have == total;
+        if (lacking) *lacking = total - have;
+        if (have < total) atomicOr(&g_pages_error, 64u);
+    }
+}
+
+// Rows of a new page: slot j comes from slot keep[j] of the old pages.  CTAs take (new page, layer)
+// items; the rows' sources are looked up once for all planes and heads.
+template <typename V>
+__device__ __forceinline__ void gather_rows(unsigned char *dst, const unsigned char *base, const int64_t *src, int rows,
+                                            int row_bytes) {
+    constexpr int U = 4;
+    const int per = row_bytes / (int)sizeof(V), n = rows * per;
+    for (int i0 = threadIdx.x; i0 < n; i0 += kCopyThreads * U) {
+        V x[U];
+        bool ok[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * kCopyThreads;
+            ok[u] = i < n;
+            if (ok[u]) {
+                const int64_t s = src[i / per];
+                ok[u] = s >= 0;
+                if (ok[u]) x[u] = reinterpret_cast<const V *>(base + s * row_bytes)[i % per];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (ok[u]) reinterpret_cast<V *>(dst)[i0 + u * kCopyThreads] = x[u];
+    }
+}
+constexpr int kRowsAtOnce = 256;
+__global__ void __launch_bounds__(kCopyThreads)
+compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len) {
+    pdl_wait();
+    __shared__ int64_t src[kRowsAtOnce];  // rows of a plane, head 0; -1: not moved
+    const int64_t items = (int64_t)w.total[0] * a.layers;
+    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+        const int job = (int)(it / a.layers), l = (int)(it % a.layers);
+        int lo = 0, hi = a.batch;  // the sequence whose job it is: base[b] <= job < base[b + 1]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (w.base[mid] <= job) lo = mid;
+            else hi = mid;
+        }
+        const int b = lo, lp = w.begin[b] + job - w.base[b], to = w.free_ids[job];
+        const int S = start_of(a, b);
+        for (int rr = 0; rr < a.rows_per_seq; ++rr) {
+            const int64_t r = (int64_t)b * a.rows_per_seq + rr;
+            const int n = min(keep_len[r], a.cap);
+            for (int q0 = 0; q0 < a.page_size; q0 += kRowsAtOnce) {
+                const int rows = min(kRowsAtOnce, a.page_size - q0);
+                __syncthreads();
+                for (int q = threadIdx.x; q < rows; q += kCopyThreads) {
+                    const int64_t j = (int64_t)lp * a.page_size + q0 + q - S;
+                    int64_t row = -1;
+                    if (j >= 0 && j < n) {
+                        const int64_t from = (int64_t)S + keep[r * a.cap + j];
+                        const int fp = (int)(from / a.page_size);
+                        const int page = from >= 0 && fp < a.max_pages ? a.table[(int64_t)b * a.max_pages + fp] : -1;
+                        if (page >= 0 && page < a.num_pages)
+                            row = (((int64_t)l * a.num_pages + page) * a.kv_heads) * a.page_size + from % a.page_size;
+                        else
+                            atomicOr(&g_pages_error, 128u);
+                    }
+                    src[q] = row;
+                }
+                __syncthreads();
+                const int g0 = a.rows_per_seq == 1 ? 0 : rr, g1 = a.rows_per_seq == 1 ? a.kv_heads : rr + 1;
+                for (int pl = 0; pl < a.n_planes; ++pl) {
+                    const int rb = a.row_bytes[pl];
+                    for (int g = g0; g < g1; ++g) {
+                        const int64_t head = (int64_t)g * a.page_size;
+                        unsigned char *d =
+                            a.plane[pl] + ((((int64_t)l * a.num_pages + to) * a.kv_heads) * a.page_size + head + q0) * rb;
+                        const unsigned char *base = a.plane[pl] + head * rb;
+                        if (rb % 16 == 0) gather_rows<uint4>(d, base, src, rows, rb);
+                        else gather_rows<uint32_t>(d, base, src, rows, rb);
+                    }
+                }
+            }
+        }
+    }
+}
+
+// After the copies.  CTAs [0, batch): the sequence's table, its pages' counts and its length; the
+// others gather a row of pos, ema or vnorm in place: keep[j] >= j, so a run of slots is read
+// before it is written, and no later run is read from it.
+__global__ void __launch_bounds__(kRowThreads)
+compact_commit_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len) {
+    pdl_wait();
+    if (!w.total[1]) return;
+    if ((int)blockIdx.x < a.batch) {
+        const int b = blockIdx.x, begin = w.begin[b], base = w.base[b], made = w.base[b + 1] - base;
+        if (begin >= a.max_pages && keep_len[(int64_t)b * a.rows_per_seq] < 0) return;
+        for (int lp = begin + threadIdx.x; lp < a.max_pages; lp += kRowThreads) {
+            int32_t *entry = a.table + (int64_t)b * a.max_pages + lp;
+            const int e = *entry;
+            if (e > 0 && e < a.num_pages) atomicSub(a.refs + e, 1);
+            const int to = lp - begin < made ? w.free_ids[base + lp - begin] : 0;
+            if (to) a.refs[to] = 1;
+            *entry = to;
+        }
+        if (threadIdx.x == 0) a.len[b] = min(keep_len[(int64_t)b * a.rows_per_seq], a.cap);
+        return;
+    }
+    constexpr int U = 8;
+    int64_t x = blockIdx.x - a.batch;
+    const int64_t R = (int64_t)a.batch * a.rows_per_seq;
+    int64_t r = x;
+    uint32_t *row;  // 4-byte values whatever they are
+    if (x < R) {
+        if (!a.pos) return;
+        row = reinterpret_cast<uint32_t *>(a.pos) + r * a.cap;
+    } else if (x < 2 * R) {
+        r = x - R;
+        if (!a.ema) return;
+        row = reinterpret_cast<uint32_t *>(a.ema) + r * a.cap;
+    } else {  // vnorm [layers][batch][kv_heads][cap]
+        x -= 2 * R;
+        const int b = (int)(x / a.kv_heads % a.batch), g = (int)(x % a.kv_heads);
+        r = a.rows_per_seq == 1 ? b : (int64_t)b * a.rows_per_seq + g;
+        row = reinterpret_cast<uint32_t *>(a.vnorm) + x * a.cap;
+    }
+    const int n = min(keep_len[r], a.cap);
+    const int32_t *k = keep + r * a.cap;
+    for (int j0 = 0; j0 < n; j0 += kRowThreads * U) {
+        uint32_t v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * kRowThreads + threadIdx.x;
+            const int from = j < n ? k[j] : 0;
+            v[u] = from >= 0 && from < a.cap ? row[from] : 0u;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * kRowThreads + threadIdx.x;
+            if (j < n) row[j] = v[u];
+        }
+    }
+}
+
+}  // namespace
+
+size_t pages_ws(int32_t batch, int32_t max_pages, int32_t num_pages, void *ws, PagesWs *w) {
+    size_t off = 0;
+    auto take = [&](size_t n) {
+        int32_t *p = ws ? at<int32_t>(ws, off) : nullptr;
+        off = align256(off + n * sizeof(int32_t));
+        return p;
+    };
+    PagesWs x;
+    const size_t R = (size_t)batch * max_pages;
+    x.total = take(4);
+    x.free_ids = take(R);
+    x.count = take(num_pages);
+    x.last = take(num_pages);
+    x.jobs = take(4 * R);
+    x.begin = take(batch);
+    x.base = take((size_t)batch + 1);
+    if (w) *w = x;
+    return off;
+}
+
+cudaError_t launch_pages_release(const PagesArgs &a, int32_t extra, cudaStream_t st) {
+    const int64_t n = ((int64_t)a.batch * a.max_pages + kRowThreads - 1) / kRowThreads;
+    const cudaError_t e = launch_k(release_kernel, dim3((unsigned)n), dim3(kRowThreads), 0, st, a, (int)extra);
+    note_launch();
+    return e;
+}
+
+cudaError_t launch_pages_fork(const PagesArgs &a, int32_t n, const int32_t *src, const int32_t *dst, cudaStream_t st) {
+    const int64_t words = (int64_t)a.rows_per_seq * a.cap;
+    const int64_t parts = (words + 8 * kRowThreads - 1) / (8 * kRowThreads);
+    const cudaError_t e = launch_k(fork_kernel, dim3((unsigned)(parts < 64 ? parts : 64), (unsigned)n), dim3(kRowThreads), 0,
+                                   st, a, src, dst);
+    note_launch();
+    return e;
+}
+
+cudaError_t launch_pages_writable(const PagesArgs &a, const PagesWs &w, const int32_t *first, const int32_t *count,
+                                  int32_t max_count, int32_t *lacking, int sms, cudaStream_t st) {
+    // pages that max_count slots from anywhere in a page may touch
+    const int64_t most = ((int64_t)max_count + a.page_size - 2) / a.page_size + 1;
+    const int span = (int)(most < a.max_pages ? most : a.max_pages);
+    cudaError_t e = launch_k(writable_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, w, first, count, (int)max_count,
+                             span, lacking);
+    note_launch();
+    if (e != cudaSuccess) return e;
+    const int64_t items = (int64_t)a.batch * span * a.layers * a.n_planes * a.kv_heads;
+    const int64_t ctas = items < 8 * (int64_t)sms ? items : 8 * (int64_t)sms;
+    e = launch_k(writable_copy_kernel, dim3((unsigned)ctas), dim3(kCopyThreads), 0, st, a, w);
+    note_launch();
+    return e;
+}
+
+cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int32_t *keep, const int32_t *keep_len,
+                                 int32_t *lacking, int sms, cudaStream_t st) {
+    cudaError_t e = launch_k(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, w, keep, keep_len, lacking);
+    note_launch();
+    if (e != cudaSuccess) return e;
+    const int64_t items = (int64_t)a.batch * a.max_pages * a.layers;
+    const int64_t ctas = items < 8 * (int64_t)sms ? items : 8 * (int64_t)sms;
+    e = launch_k(compact_copy_kernel, dim3((unsigned)ctas), dim3(kCopyThreads), 0, st, a, w, keep, keep_len);
+    note_launch();
+    if (e != cudaSuccess) return e;
+    const int64_t rows = (int64_t)a.batch * a.rows_per_seq;
+    const int64_t all = a.batch + 2 * rows + (a.vnorm ? (int64_t)a.layers * a.batch * a.kv_heads : 0);
+    e = launch_k(compact_commit_kernel, dim3((unsigned)all), dim3(kRowThreads), 0, st, a, w, keep, keep_len);
+    note_launch();
+    return e;
+}
+
+cudaError_t read_clear_pages_error(unsigned int *v) {
+    unsigned int z = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(v, g_pages_error, sizeof(*v));
+    if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_pages_error, &z, sizeof(z));
+    return e;
+}
+
+}  // namespace ikv

@@ -57,6 +57,22 @@ class ikv_params(ctypes.Structure):
                 ("scorer", I32), ("evict_mode", I32), ("trace", ctypes.POINTER(ikv_trace)), ("ws_zeroed", I32)]
 
 
+class ikv_q4(ctypes.Structure):
+    _fields_ = [("k_scale", P), ("v_scale", P)]
+
+
+class ikv_rows(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_int64), ("seq", ctypes.c_int64), ("token", ctypes.c_int64),
+                ("head", ctypes.c_int64), ("row0", P)]
+
+
+IKV_MAX_PLANES = 4
+
+
+class ikv_pages(ctypes.Structure):
+    _fields_ = [("refs", P), ("n_planes", I32), ("plane", P * IKV_MAX_PLANES), ("row_bytes", I32 * IKV_MAX_PLANES)]
+
+
 class IKVError(RuntimeError):
     def __init__(self, status: int, where: str, msg: str):
         super().__init__(f"{where} failed with status {status}: {msg}")
@@ -68,6 +84,7 @@ def _load():
         raise ImportError(f"libikv.so not built ({LIB_PATH}); run __graft_entry__.build()")
     lib = ctypes.CDLL(LIB_PATH)
     SP, CP, PP = ctypes.POINTER(ikv_shape), ctypes.POINTER(ikv_cache), ctypes.POINTER(ikv_params)
+    QP, RP, GP = ctypes.POINTER(ikv_q4), ctypes.POINTER(ikv_rows), ctypes.POINTER(ikv_pages)
     sigs = {
         "ikv_last_error": ([], ctypes.c_char_p),
         "ikv_launch_count": ([], ctypes.c_int64),
@@ -91,6 +108,15 @@ def _load():
         "ikv_step_begin": ([SP, PP, CP, P, I32, P, SZ, P], I32),
         "ikv_step_layer": ([SP, PP, CP, P, I32, I32, P, P, P, P, P, SZ, P], I32),
         "ikv_step_end": ([SP, PP, CP, P, I32, P, SZ, P], I32),
+        "ikv_q4_store": ([SP, CP, QP, I32, I32, P, P, RP, P, P, I32, P], I32),
+        "ikv_q4_load": ([SP, CP, QP, I32, I32, P, P, RP, P, P, I32, P], I32),
+        "ikv_q4_append_token": ([SP, CP, QP, P, P, P, I32, P, P], I32),
+        "ikv_q4_attend_score": ([SP, CP, QP, I32, P, P, P, P, F32, P, SZ, P], I32),
+        "ikv_pages_workspace_size": ([SP, CP, GP, ctypes.POINTER(SZ)], I32),
+        "ikv_pages_release": ([SP, CP, GP, I32, P], I32),
+        "ikv_pages_fork": ([SP, CP, GP, I32, P, P, P, P], I32),
+        "ikv_pages_writable": ([SP, CP, GP, P, P, I32, P, P, SZ, P], I32),
+        "ikv_pages_compact": ([SP, CP, GP, P, P, P, P, P, SZ, P], I32),
     }
     for name, (args, res) in sigs.items():
         f = getattr(lib, name)
@@ -242,6 +268,66 @@ def ikv_step_layer(shape, params, cache, ema, t, layer, q, k_new, v_new, out, ws
 def ikv_step_end(shape, params, cache, ema, t, ws, ws_bytes, stream=None) -> None:
     _check(_lib.ikv_step_end(ctypes.byref(shape), ctypes.byref(params), ctypes.byref(cache), _p(ema), t, _p(ws),
                              ws_bytes, _stream(stream)), "ikv_step_end")
+
+
+def ikv_q4_store(shape, cache, q4, layer0, n_layers, k, v, rows, first, count, max_count, stream=None) -> None:
+    _check(_lib.ikv_q4_store(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(q4), layer0, n_layers, _p(k),
+                             _p(v), ctypes.byref(rows), _p(first), _p(count), max_count, _stream(stream)),
+           "ikv_q4_store")
+
+
+def ikv_q4_load(shape, cache, q4, layer0, n_layers, k, v, rows, first, count, max_count, stream=None) -> None:
+    _check(_lib.ikv_q4_load(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(q4), layer0, n_layers, _p(k),
+                            _p(v), ctypes.byref(rows), _p(first), _p(count), max_count, _stream(stream)),
+           "ikv_q4_load")
+
+
+def ikv_q4_append_token(shape, cache, q4, k_new, v_new, ema, init_mean, slot, stream=None) -> None:
+    _check(_lib.ikv_q4_append_token(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(q4), _p(k_new), _p(v_new),
+                                    _p(ema), init_mean, _p(slot), _stream(stream)), "ikv_q4_append_token")
+
+
+def ikv_q4_attend_score(shape, cache, q4, layer, q, out, score, ema, alpha, ws, ws_bytes, stream=None) -> None:
+    _check(_lib.ikv_q4_attend_score(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(q4), layer, _p(q), _p(out),
+                                    _p(score), _p(ema), alpha, _p(ws), ws_bytes, _stream(stream)),
+           "ikv_q4_attend_score")
+
+
+def ikv_pages_of(refs, planes) -> ikv_pages:
+    """The ikv_pages of paged tensors [layers][num_pages][kv_heads][page_size][row]."""
+    p = ikv_pages()
+    p.refs, p.n_planes = _p(refs), len(planes)
+    for i, t in enumerate(planes):
+        p.plane[i], p.row_bytes[i] = t.data_ptr(), t.shape[-1] * t.element_size()
+    return p
+
+
+def ikv_pages_workspace_size(shape, cache, pages) -> int:
+    n = SZ(0)
+    _check(_lib.ikv_pages_workspace_size(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(pages),
+                                         ctypes.byref(n)), "ikv_pages_workspace_size")
+    return n.value
+
+
+def ikv_pages_release(shape, cache, pages, extra, stream=None) -> None:
+    _check(_lib.ikv_pages_release(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(pages), extra,
+                                  _stream(stream)), "ikv_pages_release")
+
+
+def ikv_pages_fork(shape, cache, pages, n, src, dst, ema, stream=None) -> None:
+    _check(_lib.ikv_pages_fork(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(pages), n, _p(src), _p(dst),
+                               _p(ema), _stream(stream)), "ikv_pages_fork")
+
+
+def ikv_pages_writable(shape, cache, pages, first, count, max_count, lacking, ws, ws_bytes, stream=None) -> None:
+    _check(_lib.ikv_pages_writable(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(pages), _p(first), _p(count),
+                                   max_count, _p(lacking), _p(ws), ws_bytes, _stream(stream)), "ikv_pages_writable")
+
+
+def ikv_pages_compact(shape, cache, pages, keep, keep_len, ema, lacking, ws, ws_bytes, stream=None) -> None:
+    _check(_lib.ikv_pages_compact(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(pages), _p(keep),
+                                  _p(keep_len), _p(ema), _p(lacking), _p(ws), ws_bytes, _stream(stream)),
+           "ikv_pages_compact")
 
 
 def raw_status(fn_name: str, *args) -> int:
