@@ -170,7 +170,6 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     a.layer = layer;
     a.rows_per_seq = rows_per_seq(shape);
     a.cap = cap_of(cache);
-    q4_attend_plan(shape, cache->max_len, sm_count(), &a.chunk_tiles, &a.n_chunks);
     a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)shape->head_dim));
     a.logits = want_score ? at<float>(ws, w.logits) : nullptr;
     a.lstride = logit_stride(a.cap);
@@ -178,33 +177,29 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     a.part_o = at<float>(ws, w.part_o);
     a.lse2 = at<float>(ws, w.lse2);
     PdlScope pdl;
-    IKV_TRY_CUDA(launch_q4_attend(a, shape->dtype, shape->head_dim, stream), "4-bit attend launch");
-    // the chunks' merge, and the scores
-    ScoreOneArgs sa{};
-    sa.len = cache->len;
-    sa.start = cache->start;
-    sa.batch = shape->batch;
-    sa.q_heads = shape->q_heads;
-    sa.kv_heads = shape->kv_heads;
-    sa.rows_per_seq = a.rows_per_seq;
-    sa.cap = a.cap;
-    sa.head_dim = shape->head_dim;
-    sa.bf16 = shape->dtype == IKV_BF16;
-    sa.logits = a.logits;
-    sa.lstride = a.lstride;
-    sa.lse2 = a.lse2;
-    sa.tile = kQ4Tile;
-    sa.split_tokens = a.chunk_tiles * kQ4Tile;
-    sa.passes = 1;
-    sa.n_splits = a.n_chunks;
-    sa.part_ml = a.part_ml;
-    sa.part_o = a.part_o;
-    sa.out = out;
-    sa.alpha = alpha;
-    sa.score = score;
-    sa.ema = ema;
-    sa.vec = sa.cap % 4 == 0 && aligned16(score) && aligned16(ema);
-    IKV_TRY_CUDA(launch_score_one(sa, cache->max_len, sm_count(), stream), "score launch");
+    const int32_t ctas = q4_attend_ctas(shape, cache->max_len, sm_count());
+    IKV_TRY_CUDA(launch_q4_attend(a, shape->dtype, shape->head_dim, ctas, stream), "4-bit attend launch");
+    Q4FinishArgs f{};
+    f.len = cache->len;
+    f.start = cache->start;
+    f.batch = shape->batch;
+    f.q_heads = shape->q_heads;
+    f.kv_heads = shape->kv_heads;
+    f.rows_per_seq = a.rows_per_seq;
+    f.cap = a.cap;
+    f.head_dim = shape->head_dim;
+    f.bf16 = shape->dtype == IKV_BF16;
+    f.attend_ctas = ctas;
+    f.logits = a.logits;
+    f.lstride = a.lstride;
+    f.lse2 = a.lse2;
+    f.part_ml = a.part_ml;
+    f.part_o = a.part_o;
+    f.out = out;
+    f.alpha = alpha;
+    f.score = score;
+    f.ema = ema;
+    IKV_TRY_CUDA(launch_q4_finish(f, cache->max_len, sm_count(), stream), "4-bit score launch");
     return IKV_OK;
 }
 

@@ -57,15 +57,29 @@ struct Q4AttendArgs {
     const void *q;                    // [batch][q_heads][D] (dtype)
     void *out;                        // the same
     int32_t batch, q_heads, layer, rows_per_seq, cap;
-    int32_t chunk_tiles, n_chunks;    // tiles of kQ4Tile slots a CTA takes, chunks of the longest sequence
     float scale_log2;
     float *logits;                    // [batch][q_heads][lstride] log2-domain logits, or null
     int32_t lstride;
-    float *part_ml, *part_o;          // [batch][q_heads][n_chunks][2], [..][D]: sequences of several chunks
-    float *lse2;                      // [batch][q_heads]: sequences of one chunk
+    float *part_ml, *part_o;          // [batch][q_heads][kMaxSplits][2], [..][D]: units of several segments
+    float *lse2;                      // [batch][q_heads]: units of one segment
 };
-void q4_attend_plan(const ikv_shape *s, int32_t max_len, int sms, int32_t *chunk_tiles, int32_t *n_chunks);
-cudaError_t launch_q4_attend(const Q4AttendArgs &a, int dtype, int head_dim, cudaStream_t st);
+// CTAs of an attention launch at lengths up to max_len
+int32_t q4_attend_ctas(const ikv_shape *s, int32_t max_len, int sms);
+cudaError_t launch_q4_attend(const Q4AttendArgs &a, int dtype, int head_dim, int32_t ctas, cudaStream_t st);
+
+struct Q4FinishArgs {
+    const int32_t *len, *start;
+    int32_t batch, q_heads, kv_heads, rows_per_seq, cap, head_dim, bf16;
+    int32_t attend_ctas;              // of the attention launch before
+    const float *logits;
+    int32_t lstride;
+    const float *lse2, *part_ml, *part_o;
+    void *out;
+    float alpha;
+    float *score, *ema;               // [rows][cap] or null
+    int32_t token_ctas, merge_ctas;   // CTAs of all rows' tokens, of a sequence's merges; set by the launcher
+};
+cudaError_t launch_q4_finish(const Q4FinishArgs &a, int32_t max_len, int sms, cudaStream_t st);
 
 // ---- page pools (pages.cu)
 constexpr int kMaxPlanes = IKV_MAX_PLANES;
