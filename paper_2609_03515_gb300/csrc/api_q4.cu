@@ -176,6 +176,10 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     a.part_ml = at<float>(ws, w.part_ml);
     a.part_o = at<float>(ws, w.part_o);
     a.lse2 = at<float>(ws, w.lse2);
+    a.segs = at<int32_t>(ws, w.arrivals);
+    // (the kernels count the sequences' pairs of tiles in 32 bits)
+    if ((int64_t)shape->batch * shape->kv_heads * (a.cap / 32 + 1) > 0x7fffffff)
+        return report(IKV_ERR_SHAPE, "batch * kv_heads * cap too large");
     PdlScope pdl;
     const int32_t ctas = q4_attend_ctas(shape, cache->max_len, sm_count());
     IKV_TRY_CUDA(launch_q4_attend(a, shape->dtype, shape->head_dim, ctas, stream), "4-bit attend launch");
@@ -189,7 +193,7 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     f.cap = a.cap;
     f.head_dim = shape->head_dim;
     f.bf16 = shape->dtype == IKV_BF16;
-    f.attend_ctas = ctas;
+    f.segs = a.segs;
     f.logits = a.logits;
     f.lstride = a.lstride;
     f.lse2 = a.lse2;
@@ -199,7 +203,7 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     f.alpha = alpha;
     f.score = score;
     f.ema = ema;
-    IKV_TRY_CUDA(launch_q4_finish(f, cache->max_len, sm_count(), stream), "4-bit score launch");
+    IKV_TRY_CUDA(launch_q4_finish(f, ctas, cache->max_len, sm_count(), stream), "4-bit score launch");
     return IKV_OK;
 }
 

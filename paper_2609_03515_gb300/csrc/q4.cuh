@@ -62,6 +62,7 @@ struct Q4AttendArgs {
     int32_t lstride;
     float *part_ml, *part_o;          // [batch][q_heads][kMaxSplits][2], [..][D]: units of several segments
     float *lse2;                      // [batch][q_heads]: units of one segment
+    int32_t *segs;                    // [batch][kv_heads] segments of a unit (of sequences that have a slot)
 };
 // CTAs of an attention launch at lengths up to max_len
 int32_t q4_attend_ctas(const ikv_shape *s, int32_t max_len, int sms);
@@ -70,16 +71,17 @@ cudaError_t launch_q4_attend(const Q4AttendArgs &a, int dtype, int head_dim, int
 struct Q4FinishArgs {
     const int32_t *len, *start;
     int32_t batch, q_heads, kv_heads, rows_per_seq, cap, head_dim, bf16;
-    int32_t attend_ctas;              // of the attention launch before
     const float *logits;
     int32_t lstride;
     const float *lse2, *part_ml, *part_o;
+    const int32_t *segs;
     void *out;
     float alpha;
     float *score, *ema;               // [rows][cap] or null
-    int32_t token_ctas, merge_ctas;   // CTAs of all rows' tokens, of a sequence's merges; set by the launcher
+    int32_t token_ctas, row_ctas;     // CTAs of all rows' tokens, of a row's; set by the launcher
 };
-cudaError_t launch_q4_finish(const Q4FinishArgs &a, int32_t max_len, int sms, cudaStream_t st);
+// ctas: of the attention launch before
+cudaError_t launch_q4_finish(const Q4FinishArgs &a, int32_t ctas, int32_t max_len, int sms, cudaStream_t st);
 
 // ---- page pools (pages.cu)
 constexpr int kMaxPlanes = IKV_MAX_PLANES;

@@ -1,5 +1,6 @@
 // Decode attention over a cache held in 4 bits.
 #include <cfloat>
+#include <climits>
 #include <cstddef>
 #include <type_traits>
 
@@ -13,6 +14,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kPair = 2;              // tiles of an iteration
 constexpr int kStages = 3;            // pairs of tiles a warp has in flight or in use
 constexpr int kCtasPerSm = 3;
+constexpr int kSwitch = 6;             // what going from one unit to the next costs a CTA, in pairs of tiles
 constexpr float kMaxSlack = 6.f;      // log2: how far a logit may lie above the running reference
 constexpr float kScaleRoom = 256.f;   // how far a V scale may grow, normalised, before it is renormalised
 
@@ -78,85 +80,117 @@ struct Tile {
     int32_t pos[kQ4Tile];
 };
 
+template <int D>
+constexpr size_t kJoinBytes = kWarps * 8 * (sizeof(float2) + D * sizeof(float));  // shared memory in front of the rings
+
 // A tile's row r stands for token perm(r): lane (g, t) of the second product then finds its
 // four tokens t, 4 + t, 8 + t, 12 + t, whose 8-byte units lie in different banks.
 __device__ __forceinline__ int perm_of_row(int r) { return ((r >> 1) & 3) + 4 * (r & 1) + 8 * (r >> 3); }
 __device__ __forceinline__ int row_of_token(int t) { return 2 * (t & 3) + ((t >> 2) & 1) + 8 * (t >> 3); }
 
-// How the work is cut.  A unit (sequence, KV head) is rounds of kRound slots, counted from the tile
-// that holds its first slot; the units' rounds, one unit behind another, are dealt to the CTAs in
-// equal runs of `per`, so a batch of uneven lengths loads them evenly, and a CTA's run is one or
-// more segments, each of one unit.  A unit's n segments leave partials 0 .. n - 1.  Everything
-// follows from the lengths on the device; each kernel works it out for itself.
-constexpr int kRoundTiles = kWarps * kPair, kRound = kRoundTiles * kQ4Tile;
+// How the work is cut.  A unit (sequence, KV head) is pairs of tiles, counted from the tile that
+// holds its first slot.  The units are laid one behind another, each a little longer than its pairs,
+// and that length is dealt to one wave of CTAs in equal runs: a batch of uneven lengths loads them
+// evenly, and a CTA's run is one or more segments, each of one unit.  A unit's n segments leave
+// partials 0 .. n - 1 and n in segs.
 struct Span {  // of a sequence
-    int tile0, tiles, rounds;
+    int L, S, tile0, tiles, pairs;
 };
-__device__ __forceinline__ Span span_of(int L, int S) {
+__device__ __forceinline__ Span span_of(const Q4AttendArgs &a, int b) {
     Span s;
-    s.tile0 = S / kQ4Tile;
-    s.tiles = L > 0 ? (S + L + kQ4Tile - 1) / kQ4Tile - s.tile0 : 0;
-    s.rounds = (s.tiles + kRoundTiles - 1) / kRoundTiles;
+    s.L = a.len[b];
+    s.S = a.pv.start_of(b);
+    s.tile0 = s.S / kQ4Tile;
+    s.tiles = s.L > 0 ? (s.S + s.L + kQ4Tile - 1) / kQ4Tile - s.tile0 : 0;
+    s.pairs = (s.tiles + kPair - 1) / kPair;
     return s;
 }
-struct Deal {
-    int64_t per;     // rounds of a CTA
-    int64_t before;  // rounds (of one KV head) of the sequences in front of one
+struct Segment {
+    int b, kv;          // its unit
+    int pairs;          // the unit's pairs that are the CTA's
+    int seg0, segs;     // the CTA of the unit's first segment, the unit's segments
 };
-// The deal to `ctas` CTAs, and for the sequence that `pick` finds, given the rounds in front of a
-// sequence, its own and per (true for one sequence at most): its number, through *found (-1: none).
-// All threads of the CTA; each takes a run of sequences.
-template <int NT, typename Pick>
-__device__ __forceinline__ Deal deal_rounds(const int32_t *len, const int32_t *start, int batch, int kv_heads, int ctas,
-                                            Pick pick, int *found) {
-    __shared__ int64_t sums[NT / 32];
-    __shared__ int tops[NT / 32];
-    __shared__ int64_t s_before;
-    __shared__ int s_found;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int run = (batch + NT - 1) / NT, b0 = threadIdx.x * run, b1 = min(b0 + run, batch);
-    int64_t mine = 0;
-    int top = 0;
-    for (int b = b0; b < b1; ++b) {
-        const int r = span_of(len[b], start ? start[b] : 0).rounds;
-        mine += r;
-        top = max(top, r);
+// Where a CTA's run starts and how long it is; every thread of the CTA, each takes some sequences.
+struct Run {
+    int b, before;      // its first sequence, and the length (of one KV head) in front of that; b < 0: none
+    int per;            // length of a run
+    int whole;          // > 0: every unit is as long as its pairs rounded up to runs; 0: kSwitch longer than its pairs
+    __device__ __forceinline__ int length(int pairs) const {
+        return pairs == 0 ? 0 : whole ? whole : pairs + kSwitch;
     }
-    int64_t scan = mine;
+};
+__device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
+    __shared__ int sums[kWarps], counts[kWarps], tops[kWarps], lows[kWarps], found[2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int each = (a.batch + kThreads - 1) / kThreads, b0 = threadIdx.x * each, b1 = min(b0 + each, a.batch);
+    int mine = 0, n_mine = 0, top = 0, low = INT_MAX;
+    for (int b = b0; b < b1; ++b) {
+        const int n = span_of(a, b).pairs;
+        mine += n;
+        n_mine += n > 0;
+        top = max(top, n);
+        if (n > 0) low = min(low, n);
+    }
+    int scan = mine, n_scan = n_mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, scan, d);
-        if (lane >= d) scan += y;
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const int y = __shfl_up_sync(0xffffffffu, scan, d), z = __shfl_up_sync(0xffffffffu, n_scan, d);
+        if (lane >= d) {
+            scan += y;
+            n_scan += z;
+        }
     }
-    if (threadIdx.x == 0) s_found = -1;
+    top = __reduce_max_sync(0xffffffffu, top);
+    low = __reduce_min_sync(0xffffffffu, low);
+    if (threadIdx.x == 0) found[0] = -1;
     if (lane == 31) {
         sums[warp] = scan;
+        counts[warp] = n_scan;
         tops[warp] = top;
+        lows[warp] = low;
     }
     __syncthreads();
-    int64_t total = 0, base = scan - mine;
+    int total = 0, n = 0, base = scan - mine, n_base = n_scan - n_mine;
 #pragma unroll
-    for (int w = 0; w < NT / 32; ++w) {
-        if (w < warp) base += sums[w];
-        total += sums[w];
-        top = max(top, tops[w]);
-    }
-    Deal deal;
-    // (a unit is cut into kMaxSplits segments at most: two of them may be parts of a run)
-    deal.per = max(max((total * kv_heads + ctas - 1) / ctas, ((int64_t)top + kMaxSplits - 3) / (kMaxSplits - 2)), (int64_t)1);
-    for (int b = b0; b < b1; ++b) {
-        const int r = span_of(len[b], start ? start[b] : 0).rounds;
-        if (pick(b, base, r, deal.per)) {
-            s_before = base;
-            s_found = b;
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) {
+            base += sums[w];
+            n_base += counts[w];
         }
-        base += r;
+        total += sums[w];
+        n += counts[w];
+        top = max(top, tops[w]);
+        low = min(low, lows[w]);
+    }
+    const int kvh = a.pv.kv_heads, ctas = (int)gridDim.x, units = n * kvh;
+    // (a unit of kMaxSplits - 2 whole runs at most: it may begin and end inside two more)
+    const int least = (top + kMaxSplits - 3) / (kMaxSplits - 2);
+    Run run;
+    run.per = max(max((int)(((int64_t)total * kvh + (int64_t)units * kSwitch + ctas - 1) / ctas), least), 1);
+    run.whole = 0;
+    if (top == low && units <= ctas) {
+        // units of one length, cut evenly, each into runs of its own, if that makes them no longer
+        const int cut = max((top + ctas / units - 1) / (ctas / units), least);
+        const int even = (cut + kWarps - 1) / kWarps * kWarps;
+        if (even <= run.per + kSwitch) {
+            run.per = even;
+            run.whole = (top + even - 1) / even * even;
+        }
+    }
+    base = run.whole ? n_base * run.whole : base + n_base * kSwitch;
+    const int64_t x = (int64_t)blockIdx.x * run.per;
+    for (int b = b0; b < b1; ++b) {
+        const int len = run.length(span_of(a, b).pairs);
+        if (x >= (int64_t)base * kvh && x < (int64_t)(base + len) * kvh) {
+            found[0] = b;
+            found[1] = base;
+        }
+        base += len;
     }
     __syncthreads();
-    *found = s_found;
-    deal.before = s_before;
-    return deal;
+    run.b = found[0];
+    run.before = found[1];
+    return run;
 }
 
 // softmax(q K^T / sqrt d) V for a CTA's segments, and the log2-domain logits of their slots.
@@ -178,32 +212,119 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
     constexpr int NP = sizeof(T) == 4 ? 2 : 1;  // fp16 terms of q and of the probabilities
     constexpr int kPieces = D / 32;        // 16-byte pieces of a row of codes
     extern __shared__ __align__(128) unsigned char smem[];
-    Tile<D> *ring = reinterpret_cast<Tile<D> *>(smem) + (threadIdx.x >> 5) * (kStages * kPair);
-    pdl_wait();
+    float2 *ml = reinterpret_cast<float2 *>(smem);                              // [kWarps][8]
+    float *po = reinterpret_cast<float *>(smem + kWarps * 8 * sizeof(float2));  // [kWarps][8][D]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int g = lane >> 2, t = lane & 3;
-    const int kvh = a.pv.kv_heads;
-    const int G = a.q_heads / kvh;
-    int b;
-    int64_t at = 0;  // the run starts at this round
-    const Deal deal = deal_rounds<kThreads>(a.len, a.pv.start, a.batch, kvh, (int)gridDim.x,
-        [&](int, int64_t before, int rounds, int64_t per) {
-            const int64_t x = blockIdx.x * per;
-            return x >= before * kvh && x < (before + rounds) * kvh;
-        }, &b);
-    if (b < 0) return;  // past the last round
-    at = blockIdx.x * deal.per - deal.before * kvh;  // within the sequence's units
-    int64_t before = deal.before, left = deal.per;
-    Span sp = span_of(a.len[b], a.pv.start_of(b));
-    int kv = (int)(at / sp.rounds), round = (int)(at % sp.rounds);
-    while (left > 0) {
-    const int L = a.len[b], S = a.pv.start_of(b);
-    const int64_t head0 = (int64_t)b * a.q_heads + (int64_t)kv * G;
-    const int tile0 = sp.tile0, take = (int)min((int64_t)(sp.rounds - round), left);
-    const int first = round * kRoundTiles, last = min(first + take * kRoundTiles, sp.tiles);  // tiles of the sequence
-    // the unit's segments: the runs that its rounds lie in
-    const int64_t unit0 = before * kvh + (int64_t)kv * sp.rounds;
-    const int seg0 = (int)(unit0 / deal.per), segs = (int)((unit0 + sp.rounds - 1) / deal.per) - seg0 + 1;
+    const Tile<D> *ring = reinterpret_cast<const Tile<D> *>(smem + kJoinBytes<D>) + warp * (kStages * kPair);
+    pdl_wait();
+    const int kvh = a.pv.kv_heads, G = a.q_heads / kvh;
+    const Run run = run_of(a);
+    if (run.b < 0) return;  // past the last round
+
+    // where a lane's pieces of a tile go: K's rows permuted, V's pieces swizzled
+    constexpr int kCopies = kQ4Tile * kPieces / 32;
+    constexpr int kScalePieces = kQ4Tile * Tile<D>::kScaleRow / 16;  // 8 or 4
+    constexpr uint32_t kStageBytes = kPair * sizeof(Tile<D>);
+    const uint32_t ring_at = smem_u32(ring);
+    uint32_t to_k[kCopies], to_v[kCopies];
+#pragma unroll
+    for (int j = 0; j < kCopies; ++j) {
+        const int c = lane + 32 * j, tok = c / kPieces, piece = c % kPieces;
+        to_k[j] = offsetof(Tile<D>, k) + row_of_token(tok) * Tile<D>::kRow + piece * 16;
+        to_v[j] = offsetof(Tile<D>, v) + tok * Tile<D>::kRow + (D == 128 ? piece ^ (tok & 2) : piece) * 16;
+    }
+    const unsigned char *scales = reinterpret_cast<const unsigned char *>(lane < 8 ? a.ks : a.vs) + (lane & 7) * 16;
+    const uint32_t to_s = (lane < 8 ? offsetof(Tile<D>, ks) : offsetof(Tile<D>, vs)) + (lane & 7) * 16;
+
+    // the segment at hand
+    int before = run.before, left = run.per;
+    Span sp = span_of(a, run.b);
+    Segment sg;
+    const int32_t *pos = nullptr;
+    int first = 0, last = 0, mine = 0;  // its tiles [first, last) of the sequence, this warp's pairs of them
+    auto enter = [&](int b, int kv, int pair) {
+        sg.b = b;
+        sg.kv = kv;
+        sg.pairs = min(sp.pairs - pair, left);
+        const int64_t unit0 = (int64_t)before * kvh + (int64_t)kv * run.length(sp.pairs);
+        sg.seg0 = (int)(unit0 / run.per);
+        sg.segs = (int)((unit0 + sp.pairs - 1) / run.per) - sg.seg0 + 1;
+        left -= run.length(sp.pairs) - pair;
+        if (threadIdx.x == 0 && pair == 0) a.segs[b * kvh + kv] = sg.segs;
+        pos = a.pos ? a.pos + (int64_t)(a.rows_per_seq == 1 ? b : b * a.rows_per_seq + kv) * a.cap : nullptr;
+        first = pair * kPair;
+        last = min(first + sg.pairs * kPair, sp.tiles);
+        mine = sg.pairs > warp ? (sg.pairs - warp + kWarps - 1) / kWarps : 0;
+    };
+    // the unit behind (b, kv), if the run reaches it
+    auto enter_next = [&](int b, int kv) -> bool {
+        if (left <= 0) return false;
+        if (++kv == kvh) {
+            kv = 0;
+            before += run.length(sp.pairs);
+            do {
+                if (++b >= a.batch) return false;
+                sp = span_of(a, b);
+            } while (sp.pairs == 0);
+        }
+        enter(b, kv, 0);
+        return true;
+    };
+    // the warp's pairs of tiles: first / 2 + warp, + kWarps, ...; lane i knows where the i-th of
+    // the 32 tiles from a multiple of 32 on starts
+    auto tile_of = [&](int i) { return first + ((i >> 1) * kWarps + warp) * kPair + (i & 1); };  // my i-th tile
+    auto row_of = [&](int i) -> int64_t {  // row of the paged arrays where it starts
+        const int x = tile_of(i);
+        return x < last ? a.pv.row_phys(sg.b, a.layer, sg.kv, (sp.tile0 + x) * kQ4Tile) : 0;
+    };
+    int64_t my_row = 0;
+    auto issue = [&](int i, uint32_t stage) {
+        if (i < mine) {
+            if ((i & 15) == 0) my_row = row_of(2 * i + lane);
+#pragma unroll
+            for (int u = 0; u < kPair; ++u) {
+                const int64_t row = __shfl_sync(0xffffffffu, my_row, (2 * i + u) & 31);
+                const uint32_t dst = stage + u * sizeof(Tile<D>);
+                if (u > 0 && tile_of(2 * i + u) >= last) break;
+                const unsigned char *ks = a.k + row * Tile<D>::kRow + lane * 16, *vs = a.v + row * Tile<D>::kRow + lane * 16;
+#pragma unroll
+                for (int j = 0; j < kCopies; ++j) {
+                    copy16(dst + to_k[j], ks + j * 512);
+                    copy16(dst + to_v[j], vs + j * 512);
+                }
+                if ((lane & 7) < kScalePieces && lane < 16) copy16(dst + to_s, scales + row * Tile<D>::kScaleRow);
+                else if (lane >= 16 && pos) {
+                    const int j = (sp.tile0 + tile_of(2 * i + u)) * kQ4Tile + lane - 16 - sp.S;
+                    if (j >= 0 && j < sp.L) copy4(dst + offsetof(Tile<D>, pos) + (lane - 16) * 4, pos + j);
+                }
+            }
+        }
+        copy_commit();
+    };
+    uint32_t use = 0;  // the stage of the next pair, as an offset
+    auto stage_after = [&](uint32_t x, int n) {  // n < kStages
+        x += n * kStageBytes;
+        return x >= kStages * kStageBytes ? x - kStages * kStageBytes : x;
+    };
+    auto prologue = [&]() {
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) issue(i, ring_at + stage_after(use, i));
+    };
+    {
+        const int at = (int)((int64_t)blockIdx.x * run.per - (int64_t)run.before * kvh);  // within the sequence's units
+        const int length = run.length(sp.pairs), kv = at / length, pair = at % length;
+        if (pair < sp.pairs) {
+            enter(run.b, kv, pair);
+        } else {  // behind the unit's last pair
+            left -= length - pair;
+            if (!enter_next(run.b, kv)) return;
+        }
+    }
+    prologue();
+    while (true) {
+    const int L = sp.L, S = sp.S, tile0 = sp.tile0;
+    const int64_t head0 = (int64_t)sg.b * a.q_heads + (int64_t)sg.kv * G;
 
     // q: lane (g, t) holds head g's channels 32 y + 8 t .. + 7
     uint32_t q[NP][Y][4];
@@ -267,57 +388,6 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
     float ref[2] = {-FLT_MAX, -FLT_MAX}, sum[2] = {0.f, 0.f};
     float norm = 1.f, room = -1.f;  // V scales times norm stay within kScaleRoom while they are <= room
     int norm_e = 0;                 // norm = 2^norm_e
-
-    const int32_t *pos = a.pos ? a.pos + (int64_t)(a.rows_per_seq == 1 ? b : b * a.rows_per_seq + kv) * a.cap : nullptr;
-    // this warp's pairs of tiles: first / 2 + warp, + kWarps, ...; lane i knows where the i-th of
-    // the 32 tiles from base on start
-    const int pairs = (last - first + kPair - 1) / kPair;
-    const int mine = pairs > warp ? (pairs - warp + kWarps - 1) / kWarps : 0;
-    auto tile_of = [&](int i) { return first + ((i >> 1) * kWarps + warp) * kPair + (i & 1); };  // my i-th tile
-    auto row_of = [&](int i) -> int64_t {  // row of the paged arrays where it starts
-        const int x = tile_of(i);
-        return x < last ? a.pv.row_phys(b, a.layer, kv, (tile0 + x) * kQ4Tile) : 0;
-    };
-    int64_t my_row = row_of(lane);
-    // where a lane's pieces of a tile go: K's rows permuted, V's pieces swizzled
-    constexpr int kCopies = kQ4Tile * kPieces / 32;
-    constexpr int kScalePieces = kQ4Tile * Tile<D>::kScaleRow / 16;  // 8 or 4
-    const uint32_t ring_at = smem_u32(ring);
-    uint32_t to_k[kCopies], to_v[kCopies];
-#pragma unroll
-    for (int j = 0; j < kCopies; ++j) {
-        const int c = lane + 32 * j, tok = c / kPieces, piece = c % kPieces;
-        to_k[j] = offsetof(Tile<D>, k) + row_of_token(tok) * Tile<D>::kRow + piece * 16;
-        to_v[j] = offsetof(Tile<D>, v) + tok * Tile<D>::kRow + (D == 128 ? piece ^ (tok & 2) : piece) * 16;
-    }
-    const unsigned char *scales = reinterpret_cast<const unsigned char *>(lane < 8 ? a.ks : a.vs) + (lane & 7) * 16;
-    const uint32_t to_s = (lane < 8 ? offsetof(Tile<D>, ks) : offsetof(Tile<D>, vs)) + (lane & 7) * 16;
-    auto issue = [&](int i, uint32_t stage) {
-        if (i < mine) {
-            if (i > 0 && (i & 15) == 0) my_row = row_of(2 * i + lane);
-#pragma unroll
-            for (int u = 0; u < kPair; ++u) {
-                const int64_t row = __shfl_sync(0xffffffffu, my_row, (2 * i + u) & 31);
-                const uint32_t dst = stage + u * sizeof(Tile<D>);
-                if (u > 0 && tile_of(2 * i + u) >= last) break;
-                const unsigned char *ks = a.k + row * Tile<D>::kRow + lane * 16, *vs = a.v + row * Tile<D>::kRow + lane * 16;
-#pragma unroll
-                for (int j = 0; j < kCopies; ++j) {
-                    copy16(dst + to_k[j], ks + j * 512);
-                    copy16(dst + to_v[j], vs + j * 512);
-                }
-                if ((lane & 7) < kScalePieces && lane < 16) copy16(dst + to_s, scales + row * Tile<D>::kScaleRow);
-                else if (lane >= 16 && pos) {
-                    const int j = (tile0 + tile_of(2 * i + u)) * kQ4Tile + lane - 16 - S;
-                    if (j >= 0 && j < L) copy4(dst + offsetof(Tile<D>, pos) + (lane - 16) * 4, pos + j);
-                }
-            }
-        }
-        copy_commit();
-    };
-    constexpr uint32_t kStageBytes = kPair * sizeof(Tile<D>);
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) issue(i, ring_at + i * kStageBytes);
 
     const int tok0 = perm_of_row(g);  // tokens of rows g and g + 8: tok0, tok0 + 8
     // One pair of tiles; MASK: some of its slots are not the sequence's, or dead
@@ -484,31 +554,33 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
             }
         }
     };
-    uint32_t use = 0, fill = (kStages - 1) * kStageBytes;  // stages, as offsets
     for (int i = 0; i < mine; ++i) {
         copy_wait<kStages - 2>();
         __syncwarp();
-        issue(i + kStages - 1, ring_at + fill);  // into the stage that the previous iteration left
+        issue(i + kStages - 1, ring_at + stage_after(use, kStages - 1));  // into the stage that the previous iteration left
         const Tile<D> *tiles = reinterpret_cast<const Tile<D> *>(reinterpret_cast<const unsigned char *>(ring) + use);
         const int slot0 = (tile0 + tile_of(2 * i)) * kQ4Tile - S;  // cache slot of the pair's first token
         if (!pos && slot0 >= 0 && slot0 + kPair * kQ4Tile <= L) pair_step(tiles, slot0, std::false_type{});
         else pair_step(tiles, slot0, std::true_type{});
-        fill = use;
-        use = use + kStageBytes == kStages * kStageBytes ? 0u : use + kStageBytes;
+        use = stage_after(use, 1);
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c)
         if (ref[c] == -FLT_MAX) ref[c] = -INFINITY;  // no live slot
-    copy_wait<0>();
+    // ---- the run goes on in the next unit: its first copies are under way while this one is joined
+    const Segment done = sg;
+    const bool more = enter_next(sg.b, sg.kv);
+    if (more) {
+        __syncwarp();  // the last stage is read
+        prologue();
+    }
 
     // ---- the warps' results joined: (reference, sum) and outputs through shared memory
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], d);
-    __syncthreads();  // every ring is done with
-    float2 *ml = reinterpret_cast<float2 *>(smem);                          // [kWarps][8]
-    float *po = reinterpret_cast<float *>(smem + kWarps * 8 * sizeof(float2));  // [kWarps][8][D]
+    __syncthreads();  // the join before is read
     const float back = ldexpf(1.f, -norm_e);
     if (g == 0) {
         ml[warp * 8 + 2 * t] = make_float2(ref[0], sum[0]);
@@ -543,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
             x.w += f * v.w;
         }
         const int64_t head = head0 + h;
-        if (segs == 1) {
+        if (done.segs == 1) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
             T *dst = static_cast<T *>(a.out) + head * D + e;
             store_as(dst, x.x * inv);
@@ -552,120 +624,191 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
             store_as(dst + 3, x.w * inv);
             if (e == 0) a.lse2[head] = l == 0.f ? -INFINITY : m + log2f(l);
         } else {
-            const int64_t to = head * kMaxSplits + ((int)blockIdx.x - seg0);
+            const int64_t to = head * kMaxSplits + ((int)blockIdx.x - done.seg0);
             *reinterpret_cast<float4 *>(a.part_o + to * D + e) = x;
             if (e == 0) reinterpret_cast<float2 *>(a.part_ml)[to] = make_float2(m, l);
         }
     }
-    // ---- the run goes on in the next unit
-    left -= take;
-    round = 0;
-    if (++kv == kvh) {
-        kv = 0;
-        before += sp.rounds;
-        do {
-            if (++b >= a.batch) return;
-            sp = span_of(a.len[b], a.pv.start_of(b));
-        } while (sp.rounds == 0);
-    }
-    __syncthreads();  // the shared memory is read
+    if (!more) return;
     }
 }
 
 // The rest of a call: outputs of units of several segments (or of none: 0), Eq. 1's scores and Eq. 4.
 //
 // The first CTAs take a utility row's tokens, kFinishThreads / HS of them each, HS threads a token
-// that share the row's heads; the others merge eight heads' outputs.  A head's log-sum-exp comes from
+// that share the row's heads; the others merge a head's outputs.  A head's log-sum-exp comes from
 // its segments' (reference, sum) pairs, so no pass of its own has to gather it.
 constexpr int kFinishThreads = 256;
-template <int HS>
-__global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4FinishArgs a) {
-    constexpr int kTok = kFinishThreads / HS, kAhead = 8;
-    extern __shared__ float lse[];  // [heads of a row]
+
+// One CTA merges one head's segments: every warp sums some of them, 32 E channels wide.
+template <int E, typename T>
+__device__ __forceinline__ void merge_segments(const Q4FinishArgs &a, int hh) {
+    constexpr int kW = kFinishThreads / 32, D = 32 * E, kLoads = 4;
+    __shared__ __align__(16) float sum[kW][D];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (int64_t)hh * kMaxSplits;
+    const float *po = a.part_o + (int64_t)hh * kMaxSplits * D + lane * E;
+    // the loads go out with the count of segments: those that are none are read and dropped
+    float2 y[kMaxSplits / 32];
+    y[0] = __ldcg(ml + lane);
+    float v[kLoads][E];
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const float *p = po + (int64_t)(k0 + j * kW) * D;
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                const float2 x = k0 + j * kW < kMaxSplits ? __ldcg(reinterpret_cast<const float2 *>(p + e)) : make_float2(0.f, 0.f);
+                v[j][e] = x.x;
+                v[j][e + 1] = x.y;
+            }
+        }
+    };
+    load(warp);
+    const int n = a.len[hh / a.q_heads] > 0 ? __ldcg(a.segs + hh / (a.q_heads / a.kv_heads)) : 0;
+    if (n == 1) return;
+    float m = -INFINITY, w = 0.f;
+#pragma unroll
+    for (int k = 0; k < kMaxSplits / 32; ++k) {
+        if (k > 0 && 32 * k < n) y[k] = __ldcg(ml + lane + 32 * k);
+        if (lane + 32 * k >= n) y[k] = make_float2(-INFINITY, 0.f);
+        m = fmaxf(m, y[k].x);
+    }
+    m = warp_max(m);
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int k = 0; k < kMaxSplits / 32; ++k) {
+        y[k].x = exp2f(y[k].x - base);
+        w += y[k].y * y[k].x;
+    }
+    w = warp_sum(w);
+    float acc[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    for (int k0 = warp; k0 < n; k0 += kLoads * kW) {
+        if (k0 != warp) load(k0);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int k = k0 + j * kW;
+            float mine = y[0].x;
+#pragma unroll
+            for (int i = 1; i < kMaxSplits / 32; ++i)
+                if (k >> 5 == i) mine = y[i].x;
+            const float f = __shfl_sync(0xffffffffu, mine, k & 31);
+            if (k < n) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] += f * v[j][e];
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[warp][lane * E + e] = acc[e];
+    __syncthreads();
+    if (threadIdx.x < D) {
+        float x = 0.f;
+#pragma unroll
+        for (int k = 0; k < kW; ++k) x += sum[k][threadIdx.x];
+        store_as(static_cast<T *>(a.out) + (int64_t)hh * D + threadIdx.x, w == 0.f ? 0.f : x / w);
+    }
+}
+
+// CTA x of those that merge: of one head (MANY), or of a head a warp.
+template <bool MANY, int E, typename T>
+__device__ __forceinline__ void merge_any(const Q4FinishArgs &a, int x) {
+    if (MANY) {
+        merge_segments<E, T>(a, x);
+        return;
+    }
     __shared__ float wq[kFinishThreads / 32][kMaxSplits];
+    const int warp = threadIdx.x >> 5, hh = x * (kFinishThreads / 32) + warp;
+    if (hh >= a.batch * a.q_heads) return;
+    const int n = a.len[hh / a.q_heads] > 0 ? __ldcg(a.segs + hh / (a.q_heads / a.kv_heads)) : 0;
+    if (n != 1)
+        merge_head<E>(reinterpret_cast<const float2 *>(a.part_ml) + (int64_t)hh * kMaxSplits,
+                      a.part_o + (int64_t)hh * kMaxSplits * 32 * E, n, wq[warp],
+                      static_cast<T *>(a.out) + (int64_t)hh * 32 * E, (float *)nullptr);
+}
+
+template <int HS, bool MANY>
+__global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4FinishArgs a) {
+    constexpr int kTok = kFinishThreads / HS, kAhead = 8, kWarpsF = kFinishThreads / 32, kHeads = 4;
+    extern __shared__ float lse[];  // [heads of a row]
     __shared__ float part[HS > 1 ? kFinishThreads : 1];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int G = a.q_heads / a.kv_heads;
-    const bool merge = (int)blockIdx.x >= a.token_ctas;
-    const int blocks = a.token_ctas > 0 ? a.token_ctas / (a.batch * a.rows_per_seq) : 1;
-    int b, r = 0, token = 0;
-    if (merge) {
-        b = ((int)blockIdx.x - a.token_ctas) / a.merge_ctas;
-    } else {
-        r = blockIdx.x / blocks;
-        b = r / a.rows_per_seq;
-        token = blockIdx.x % blocks * kTok + (threadIdx.x & (kTok - 1));
-        if (blockIdx.x % blocks * kTok >= a.len[b]) return;
+    if ((int)blockIdx.x >= a.token_ctas) {
+        const int x = (int)blockIdx.x - a.token_ctas;
+        if (a.bf16) {
+            if (a.head_dim == 128) merge_any<MANY, 4, __nv_bfloat16>(a, x);
+            else merge_any<MANY, 2, __nv_bfloat16>(a, x);
+        } else {
+            if (a.head_dim == 128) merge_any<MANY, 4, float>(a, x);
+            else merge_any<MANY, 2, float>(a, x);
+        }
+        return;
     }
+    const int r = blockIdx.x / a.row_ctas, b = r / a.rows_per_seq, block = blockIdx.x % a.row_ctas;
+    const int token = block * kTok + (threadIdx.x & (kTok - 1)), hs = threadIdx.x / kTok;
+    const int h0 = a.rows_per_seq == 1 ? 0 : r % a.rows_per_seq * G;
+    const int nh = a.rows_per_seq == 1 ? a.q_heads : G;
+    const int64_t head0 = (int64_t)b * a.q_heads + h0;
+    // whatever has an address goes out before anything is waited for
     const int L = a.len[b];
-    const int rounds = span_of(L, a.start ? a.start[b] : 0).rounds;
-    const int h0 = merge || a.rows_per_seq == 1 ? 0 : r % a.rows_per_seq * G;
-    const int nh = merge || a.rows_per_seq == 1 ? a.q_heads : G;
-    // the first of the thread's logits, before anything that they wait for
-    const int hs = threadIdx.x / kTok;
-    const float *zp = a.logits + ((int64_t)b * a.q_heads + h0) * a.lstride + token;
+    const float *zp = a.logits + head0 * a.lstride + token;
     float z[kAhead], was = 0.f;
     auto load = [&](int j0) {
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             const int h = (j0 + j) * HS + hs;
-            z[j] = h < nh && token < L ? __ldcg(zp + (int64_t)h * a.lstride) : -INFINITY;
+            z[j] = h < nh && token < a.lstride ? __ldcg(zp + (int64_t)h * a.lstride) : 0.f;
         }
     };
-    if (!merge) {
-        load(0);
-        if (a.ema && hs == 0 && token < L) was = a.ema[(int64_t)r * a.cap + token];
-    }
-    int found;
-    const Deal deal = deal_rounds<kFinishThreads>(a.len, a.start, a.batch, a.kv_heads, a.attend_ctas,
-                                                  [&](int x, int64_t, int, int64_t) { return x == b; }, &found);
-    auto segments = [&](int h) {  // of the unit that head h of sequence b belongs to
-        const int64_t unit0 = deal.before * a.kv_heads + (int64_t)(h / G) * rounds;
-        return rounds > 0 ? (int)((unit0 + rounds - 1) / deal.per - unit0 / deal.per) + 1 : 0;
-    };
-    if (merge) {
-        const int h = ((int)blockIdx.x - a.token_ctas) % a.merge_ctas * (kFinishThreads / 32) + warp;
-        if (h >= a.q_heads) return;
-        const int n = segments(h);
-        if (n == 1) return;
-        const int64_t hh = (int64_t)b * a.q_heads + h;
-        const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + hh * kMaxSplits;
-        const float *po = a.part_o + hh * kMaxSplits * a.head_dim;
-        if (a.bf16) {
-            __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(a.out) + hh * a.head_dim;
-            if (a.head_dim == 128) merge_head<4>(ml, po, n, wq[warp], o, (float *)nullptr);
-            else merge_head<2>(ml, po, n, wq[warp], o, (float *)nullptr);
-        } else {
-            float *o = static_cast<float *>(a.out) + hh * a.head_dim;
-            if (a.head_dim == 128) merge_head<4>(ml, po, n, wq[warp], o, (float *)nullptr);
-            else merge_head<2>(ml, po, n, wq[warp], o, (float *)nullptr);
-        }
-        return;
-    }
-    for (int h = warp; h < nh; h += kFinishThreads / 32) {
-        const int n = segments(h0 + h);
-        const int64_t hh = (int64_t)b * a.q_heads + h0 + h;
-        float x;
-        if (n == 1) {
-            x = __ldcg(a.lse2 + hh);
-        } else {
-            const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + hh * kMaxSplits;
-            float2 y[kMaxSplits / 32];
-            float m = -INFINITY, w = 0.f;
+    load(0);
+    if (a.ema && hs == 0 && token < a.cap) was = a.ema[(int64_t)r * a.cap + token];
+    if (block * kTok >= L) return;  // (a sequence without slots has no segment count either)
+    for (int hb = warp; hb < nh; hb += kHeads * kWarpsF) {
+        int n[kHeads];
+        float one[kHeads];
+        constexpr int PL = MANY ? 2 : 1;  // pairs a lane loads before it knows how many there are
+        float2 y[kHeads][PL];
 #pragma unroll
-            for (int k = 0; k < kMaxSplits / 32; ++k) {
-                y[k] = lane + 32 * k < n ? __ldcg(ml + lane + 32 * k) : make_float2(-INFINITY, 0.f);
-                m = fmaxf(m, y[k].x);
+        for (int j = 0; j < kHeads; ++j) {
+            const int h = hb + j * kWarpsF;
+            const bool have = h < nh;
+            n[j] = have ? __ldcg(a.segs + (head0 + h) / G) : 0;
+            one[j] = have ? __ldcg(a.lse2 + head0 + h) : 0.f;
+#pragma unroll
+            for (int k = 0; k < PL; ++k)
+                y[j][k] = have ? __ldcg(reinterpret_cast<const float2 *>(a.part_ml) + (head0 + h) * kMaxSplits + lane + 32 * k)
+                               : make_float2(0.f, 0.f);
+        }
+#pragma unroll
+        for (int j = 0; j < kHeads; ++j) {
+            const int h = hb + j * kWarpsF;
+            if (h >= nh) break;
+            const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (head0 + h) * kMaxSplits;
+            float x = one[j];
+            if (n[j] != 1) {
+                float m = -INFINITY, w = 0.f;
+#pragma unroll
+                for (int k = 0; k < PL; ++k)
+                    if (lane + 32 * k < n[j]) m = fmaxf(m, y[j][k].x);
+                for (int k = 32 * PL + lane; k < n[j]; k += 32) m = fmaxf(m, __ldcg(&ml[k].x));
+                m = warp_max(m);
+                const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int k = 0; k < PL; ++k)
+                    if (lane + 32 * k < n[j]) w += y[j][k].y * exp2f(y[j][k].x - base);
+                for (int k = 32 * PL + lane; k < n[j]; k += 32) {
+                    const float2 v = __ldcg(ml + k);
+                    w += v.y * exp2f(v.x - base);
+                }
+                w = warp_sum(w);
+                x = w == 0.f ? -INFINITY : m + log2f(w);
             }
-            m = warp_max(m);
-            const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-            for (int k = 0; k < kMaxSplits / 32; ++k) w += y[k].y * exp2f(y[k].x - base);
-            w = warp_sum(w);
-            x = w == 0.f ? -INFINITY : m + log2f(w);
+            if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;  // no live slot: probabilities 0
         }
-        if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;  // no live slot: probabilities 0
     }
     __syncthreads();
     float acc = 0.f;
@@ -693,9 +836,7 @@ __global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4Finis
 
 template <int D, typename T>
 cudaError_t launch_t(const Q4AttendArgs &a, int ctas, cudaStream_t st) {
-    constexpr size_t ring = sizeof(Tile<D>) * kPair * kStages * kWarps;
-    constexpr size_t join = kWarps * 8 * (sizeof(float2) + D * sizeof(float));
-    constexpr size_t smem = ring > join ? ring : join;
+    constexpr size_t smem = kJoinBytes<D> + sizeof(Tile<D>) * kPair * kStages * kWarps;
     auto kernel = a.logits ? q4_attend_kernel<D, T, true> : q4_attend_kernel<D, T, false>;
     if (smem > 48 << 10) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -706,27 +847,38 @@ cudaError_t launch_t(const Q4AttendArgs &a, int ctas, cudaStream_t st) {
     return e;
 }
 
-template <int HS>
+template <int HS, bool MANY>
 cudaError_t launch_finish_t(Q4FinishArgs a, int64_t rows, int32_t max_len, cudaStream_t st) {
-    constexpr int tok = kFinishThreads / HS;
-    const int64_t tokens = rows * ((max_len + tok - 1) / tok), merges = (int64_t)a.batch * a.merge_ctas;
+    constexpr int tok = kFinishThreads / HS, heads = MANY ? 1 : kFinishThreads / 32;
+    a.row_ctas = (max_len + tok - 1) / tok;
+    const int64_t tokens = rows * a.row_ctas, merges = ((int64_t)a.batch * a.q_heads + heads - 1) / heads;
     if (tokens + merges > 0x7fffffff) return cudaErrorInvalidConfiguration;
     a.token_ctas = (int32_t)tokens;
     const int nh = a.rows_per_seq > 1 ? a.q_heads / a.kv_heads : a.q_heads;
-    const cudaError_t e = launch_k(q4_finish_kernel<HS>, dim3((unsigned)(tokens + merges)), dim3(kFinishThreads),
+    const cudaError_t e = launch_k(q4_finish_kernel<HS, MANY>, dim3((unsigned)(tokens + merges)), dim3(kFinishThreads),
                                    sizeof(float) * nh, st, a);
     note_launch();
     return e;
 }
+template <bool MANY>
+cudaError_t launch_finish(const Q4FinishArgs &a, int32_t max_len, int sms, cudaStream_t st) {
+    const int64_t rows = a.score || a.ema ? (int64_t)a.batch * a.rows_per_seq : 0;
+    // as many threads a token as it takes to give every SM a CTA
+    if (rows * ((max_len + kFinishThreads - 1) / kFinishThreads) >= sms) return launch_finish_t<1, MANY>(a, rows, max_len, st);
+    if (rows * ((max_len + kFinishThreads / 4 - 1) / (kFinishThreads / 4)) >= sms)
+        return launch_finish_t<4, MANY>(a, rows, max_len, st);
+    return launch_finish_t<8, MANY>(a, rows, max_len, st);
+}
 
 }  // namespace
 
-// One wave of CTAs at most, one round each at least.
+// One wave of CTAs at most, a pair for each warp at least.
 int32_t q4_attend_ctas(const ikv_shape *s, int32_t max_len, int sms) {
     // a start offset may put the first slot anywhere in its tile
-    const int64_t rounds = max_len > 0 ? ((int64_t)max_len + kQ4Tile - 1 + kRound - 1) / kRound : 1;
-    const int64_t units = (int64_t)s->batch * s->kv_heads, wave = (int64_t)sms * kCtasPerSm;
-    return (int32_t)(rounds * units < wave ? rounds * units : wave);
+    constexpr int kSlots = kPair * kQ4Tile;
+    const int64_t pairs = max_len > 0 ? ((int64_t)max_len + kQ4Tile - 1 + kSlots - 1) / kSlots : 1;
+    const int64_t ctas = (int64_t)s->batch * s->kv_heads * ((pairs + kWarps - 1) / kWarps), wave = (int64_t)sms * kCtasPerSm;
+    return (int32_t)(ctas < wave ? ctas : wave);
 }
 
 cudaError_t launch_q4_attend(const Q4AttendArgs &a, int dtype, int head_dim, int32_t ctas, cudaStream_t st) {
@@ -735,15 +887,10 @@ cudaError_t launch_q4_attend(const Q4AttendArgs &a, int dtype, int head_dim, int
     return head_dim == 128 ? launch_t<128, float>(a, ctas, st) : launch_t<64, float>(a, ctas, st);
 }
 
-cudaError_t launch_q4_finish(const Q4FinishArgs &args, int32_t max_len, int sms, cudaStream_t st) {
-    Q4FinishArgs a = args;
-    a.merge_ctas = (a.q_heads + kFinishThreads / 32 - 1) / (kFinishThreads / 32);
-    const int64_t rows = a.score || a.ema ? (int64_t)a.batch * a.rows_per_seq : 0;
-    // as many threads a token as it takes to give every SM a CTA
-    if (rows * ((max_len + kFinishThreads - 1) / kFinishThreads) >= sms) return launch_finish_t<1>(a, rows, max_len, st);
-    if (rows * ((max_len + kFinishThreads / 4 - 1) / (kFinishThreads / 4)) >= sms)
-        return launch_finish_t<4>(a, rows, max_len, st);
-    return launch_finish_t<8>(a, rows, max_len, st);
+cudaError_t launch_q4_finish(const Q4FinishArgs &a, int32_t ctas, int32_t max_len, int sms, cudaStream_t st) {
+    // segments of a unit, if all are alike
+    return ctas > 8 * (int64_t)a.batch * a.kv_heads ? launch_finish<true>(a, max_len, sms, st)
+                                                     : launch_finish<false>(a, max_len, sms, st);
 }
 
 }  // namespace ikv
