@@ -47,22 +47,32 @@ __device__ __forceinline__ int block_scan(int x, int *total) {
 
 // The lowest `want` free pages into ids, by one CTA; how many there are, at most `want`.
 __device__ int find_free(const int32_t *refs, int pages, int want, int32_t *ids) {
-    constexpr int U = 8;
+    constexpr int U = 16;
+    const int lane = threadIdx.x & 31;
     int found = 0;
-    for (int p0 = 1; p0 < pages && found < want; p0 += kPlanThreads * U) {
-        const int p = p0 + threadIdx.x * U;
-        uint32_t free = 0u;
+    for (int p0 = (threadIdx.x >> 5) * 32 * U; p0 - (int)(threadIdx.x >> 5) * 32 * U < pages && found < want;
+         p0 += kPlanThreads * U) {  // a warp takes 32 U pages behind one another
+        int32_t r[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p + u < pages && __ldcg(refs + p + u) == 0) free |= 1u << u;
-        int n;
-        int at = found + block_scan(__popc(free), &n);
+        for (int u = 0; u < U; ++u) {
+            const int p = p0 + 32 * u + lane;
+            r[u] = p > 0 && p < pages ? __ldcg(refs + p) : 1;
+        }
+        uint32_t free[U];
+        int mine = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (free >> u & 1u) {
-                if (at < want) ids[at] = p + u;
-                ++at;
-            }
+        for (int u = 0; u < U; ++u) {
+            free[u] = __ballot_sync(0xffffffffu, r[u] == 0);
+            mine += __popc(free[u]);
+        }
+        int n, at = block_scan(lane == 0 ? mine : 0, &n);
+        at = found + __shfl_sync(0xffffffffu, at, 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int to = at + __popc(free[u] & ((1u << lane) - 1));
+            if ((free[u] >> lane & 1u) && to < want) ids[to] = p0 + 32 * u + lane;
+            at += __popc(free[u]);
+        }
         found += n;
     }
     __syncthreads();
@@ -80,6 +90,20 @@ __global__ void __launch_bounds__(kRowThreads) release_kernel(const PagesArgs a,
     if (L > 0 && p0 + a.page_size > S && p0 < S + L + extra) return;
     a.table[i] = 0;
     atomicSub(a.refs + e, 1);
+}
+
+template <typename T>
+__device__ __forceinline__ void copy_words(T *dst, const T *src, int64_t n, int64_t at, int64_t step) {
+    constexpr int U = 8;
+    for (int64_t j0 = at; j0 < n; j0 += U * step) {
+        T x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (j0 + u * step < n) x[u] = src[j0 + u * step];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (j0 + u * step < n) dst[j0 + u * step] = x[u];
+    }
 }
 
 // CTAs (part, fork): the parent's table entries and counts, then its rows of pos, ema and vnorm.
@@ -102,16 +126,12 @@ __global__ void __launch_bounds__(kRowThreads) fork_kernel(const PagesArgs a, co
         if (a.start) a.start[d] = a.start[s];
     }
     const int64_t n = (int64_t)a.rows_per_seq * a.cap;
-    for (int64_t j = at; j < n; j += step) {
-        if (a.pos) a.pos[d * n + j] = a.pos[s * n + j];
-        if (a.ema) a.ema[d * n + j] = a.ema[s * n + j];
-    }
+    if (a.pos) copy_words(a.pos + d * n, a.pos + s * n, n, at, step);
+    if (a.ema) copy_words(a.ema + d * n, a.ema + s * n, n, at, step);
     if (a.vnorm) {
         const int64_t m = (int64_t)a.kv_heads * a.cap;
-        for (int64_t j = at; j < m * a.layers; j += step) {
-            const int64_t l = j / m, x = j % m;
-            a.vnorm[(l * a.batch + d) * m + x] = a.vnorm[(l * a.batch + s) * m + x];
-        }
+        for (int l = 0; l < a.layers; ++l)
+            copy_words(a.vnorm + ((int64_t)l * a.batch + d) * m, a.vnorm + ((int64_t)l * a.batch + s) * m, m, at, step);
     }
 }
 
@@ -141,9 +161,19 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
         atomicOr(&g_pages_error, 128u);
         return -1;
     };
+    // what a thread's request asks for is looked up once if there is one a thread (single tokens)
+    const bool once = R <= kPlanThreads;
+    int kb = 0, klp = 0;
+    const int ke = once && threadIdx.x < R ? request(threadIdx.x, &kb, &klp) : -1;
+    auto get = [&](int64_t i, int *b, int *lp) -> int {
+        if (!once) return i < R ? request(i, b, lp) : -1;
+        *b = kb;
+        *lp = klp;
+        return ke;
+    };
     int b, lp;
     for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
-        const int e = request(i, &b, &lp);
+        const int e = get(i, &b, &lp);
         if (e > 0) {
             w.count[e] = 0;
             w.last[e] = -1;
@@ -151,23 +181,25 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
     }
     __syncthreads();
     for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
-        const int e = request(i, &b, &lp);
-        if (e > 0 && a.refs[e] > 1) {
+        const int e = get(i, &b, &lp);
+        if (e > 0 && __ldcg(a.refs + e) > 1) {
             atomicAdd(w.count + e, 1);
             atomicMax(w.last + e, b);
         }
     }
     __syncthreads();
     auto needs = [&](int64_t i, int *b, int *lp, int *e) {
-        *e = i < R ? request(i, b, lp) : -1;
+        *e = get(i, b, lp);
         if (*e <= 0) return *e == 0;
-        const int r = __ldcg(a.refs + *e);
-        return r > 1 && !(__ldcg(w.count + *e) == r && __ldcg(w.last + *e) == *b);
+        const int r = __ldcg(a.refs + *e), c = __ldcg(w.count + *e), last = __ldcg(w.last + *e);
+        return r > 1 && !(c == r && last == *b);
     };
-    int total = 0, e;
+    int total = 0, e, rank = 0;
+    bool need = false;
     for (int64_t i0 = 0; i0 < R; i0 += kPlanThreads) {
         int n;
-        block_scan(needs(i0 + threadIdx.x, &b, &lp, &e) ? 1 : 0, &n);
+        need = needs(i0 + threadIdx.x, &b, &lp, &e);
+        rank = block_scan(need ? 1 : 0, &n);
         total += n;
     }
     const int have = find_free(a.refs, a.num_pages, total, w.free_ids);
@@ -179,24 +211,22 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
     if (have < total) return;
     int done = 0;
     for (int64_t i0 = 0; i0 < R; i0 += kPlanThreads) {
-        const int64_t i = i0 + threadIdx.x;
-        const bool need = needs(i, &b, &lp, &e);
-        int n;
-        const int at = done + block_scan(need ? 1 : 0, &n);  // (its barriers: everybody has read the counts)
-        done += n;
+        if (!once) {
+            int n;
+            need = needs(i0 + threadIdx.x, &b, &lp, &e);
+            rank = done + block_scan(need ? 1 : 0, &n);  // (its barriers: everybody has read the counts)
+            done += n;
+        }
         if (need) {
-            const int to = w.free_ids[at];
+            const int to = __ldcg(w.free_ids + rank);
             a.table[(int64_t)b * a.max_pages + lp] = to;
             a.refs[to] = 1;
-            int32_t *job = w.jobs + 4 * (int64_t)at;
+            int32_t *job = w.jobs + 4 * (int64_t)rank;
             // rows of the page that hold slots in use
             const int64_t S = start_of(a, b), p0 = (int64_t)lp * a.page_size;
             const int r0 = (int)min(max(S - p0, (int64_t)0), (int64_t)a.page_size);
             const int r1 = (int)min(max(S + a.len[b] - p0, (int64_t)0), (int64_t)a.page_size);
-            job[0] = e;
-            job[1] = to;
-            job[2] = r0;
-            job[3] = e > 0 ? max(r1 - r0, 0) : 0;
+            *reinterpret_cast<int4 *>(job) = make_int4(e, to, r0, e > 0 ? max(r1 - r0, 0) : 0);
         }
     }
     __syncthreads();
@@ -242,36 +272,42 @@ __global__ void __launch_bounds__(kCopyThreads) writable_copy_kernel(const Pages
 }
 
 // One CTA: where each sequence's first moved slot lies, the pages it makes anew, the free pages for
-// them.  keep[j] >= j rises with j, so the slots that stay are a prefix, found by bisection.
+// them.  keep[j] >= j rises with j, so the slots that stay are a prefix: a warp looks for its end.
 __global__ void __launch_bounds__(kPlanThreads)
 compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int32_t *lacking) {
     pdl_wait();
+    const int lane = threadIdx.x & 31;
+    for (int b = threadIdx.x >> 5; b < a.batch; b += kPlanThreads / 32) {
+        const int64_t r0 = (int64_t)b * a.rows_per_seq;
+        const int n = min(keep_len[r0], a.cap);
+        int begin = a.max_pages;  // a sequence that is left alone
+        if (n >= 0) {
+            int f = n;
+            for (int r = 0; r < a.rows_per_seq; ++r) {
+                const int32_t *k = keep + (r0 + r) * a.cap;
+                int lo = 0, hi = f;  // slots below lo stay, slot hi does not (or is f)
+                while (lo < hi) {
+                    const int step = (hi - lo + 31) / 32, x = lo + lane * step;
+                    const uint32_t stay = __ballot_sync(0xffffffffu, x < hi && k[x] == x);
+                    // the lanes that stay are the first ones
+                    const int c = __popc(stay);
+                    if (c < 32) hi = min(hi, lo + c * step);
+                    if (c > 0) lo += (c - 1) * step + 1;
+                }
+                f = lo;
+            }
+            const int S = start_of(a, b), end = (S + n + a.page_size - 1) / a.page_size;
+            begin = f == n ? end : (S + f) / a.page_size;
+            if (lane == 0) w.base[b] = end - begin;
+        } else if (lane == 0) {
+            w.base[b] = 0;
+        }
+        if (lane == 0) w.begin[b] = begin;
+    }
+    __syncthreads();
     int total = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {
-        const int b = b0 + threadIdx.x;
-        int need = 0;
-        if (b < a.batch) {
-            const int64_t r0 = (int64_t)b * a.rows_per_seq;
-            const int n = min(keep_len[r0], a.cap);
-            int begin = a.max_pages;  // a sequence that is left alone
-            if (n >= 0) {
-                int f = n;
-                for (int r = 0; r < a.rows_per_seq; ++r) {
-                    const int32_t *k = keep + (r0 + r) * a.cap;
-                    int lo = 0, hi = f;
-                    while (lo < hi) {
-                        const int mid = (lo + hi) >> 1;
-                        if (k[mid] == mid) lo = mid + 1;
-                        else hi = mid;
-                    }
-                    f = lo;
-                }
-                const int S = start_of(a, b), end = (S + n + a.page_size - 1) / a.page_size;
-                begin = f == n ? end : (S + f) / a.page_size;
-                need = end - begin;
-            }
-            w.begin[b] = begin;
-        }
+        const int b = b0 + threadIdx.x, need = b < a.batch ? __ldcg(w.base + b) : 0;
         int n;
         const int at = total + block_scan(need, &n);
         if (b < a.batch) w.base[b] = at;
@@ -287,80 +323,84 @@ compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
     }
 }
 
-// Rows of a new page: slot j comes from slot keep[j] of the old pages.  CTAs take (new page, layer)
-// items; the rows' sources are looked up once for all planes and heads.
+// Rows of new pages: slot j comes from slot keep[j] of the old pages.  CTAs take items of one layer
+// and as many new pages as make about kRowsAtOnce rows (small pages would leave most threads
+// idle); where a row comes from and goes to is looked up once for all planes and heads.  Bound by
+// memory: a thread has kAhead vectors in flight.
+constexpr int kRowsAtOnce = 128, kHeadRows = 1024;  // rows, rows x heads of an item
+struct RowMove {
+    int64_t src, dst;  // rows of a plane; src < 0: not moved
+};
 template <typename V>
-__device__ __forceinline__ void gather_rows(unsigned char *dst, const unsigned char *base, const int64_t *src, int rows,
-                                            int row_bytes) {
-    constexpr int U = 4;
-    const int per = row_bytes / (int)sizeof(V), n = rows * per;
-    for (int i0 = threadIdx.x; i0 < n; i0 += kCopyThreads * U) {
-        V x[U];
-        bool ok[U];
+__device__ __forceinline__ void gather_plane(unsigned char *plane, int rb, const RowMove *moves, int n_moves) {
+    constexpr int kAhead = 8;
+    const int per = rb / (int)sizeof(V), n = n_moves * per;
+    const int shift = (per & (per - 1)) == 0 ? __ffs(per) - 1 : -1;
+    for (int i0 = threadIdx.x; i0 < n; i0 += kCopyThreads * kAhead) {
+        V x[kAhead];
+        V *to[kAhead];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * kCopyThreads;
-            ok[u] = i < n;
-            if (ok[u]) {
-                const int64_t s = src[i / per];
-                ok[u] = s >= 0;
-                if (ok[u]) x[u] = reinterpret_cast<const V *>(base + s * row_bytes)[i % per];
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = i0 + u * kCopyThreads, m = shift >= 0 ? i >> shift : i / per;
+            to[u] = nullptr;
+            if (i < n && moves[m].src >= 0) {
+                const int64_t piece = (int64_t)(i - m * per) * sizeof(V);
+                to[u] = reinterpret_cast<V *>(plane + moves[m].dst * rb + piece);
+                x[u] = *reinterpret_cast<const V *>(plane + moves[m].src * rb + piece);
             }
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (ok[u]) reinterpret_cast<V *>(dst)[i0 + u * kCopyThreads] = x[u];
+        for (int u = 0; u < kAhead; ++u)
+            if (to[u]) *to[u] = x[u];
     }
 }
-constexpr int kRowsAtOnce = 256;
 __global__ void __launch_bounds__(kCopyThreads)
-compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len) {
+compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int pages_at_once,
+                    int heads_at_once) {
     pdl_wait();
-    __shared__ int64_t src[kRowsAtOnce];  // rows of a plane, head 0; -1: not moved
-    const int64_t items = (int64_t)w.total[0] * a.layers;
+    __shared__ RowMove moves[kHeadRows];
+    const int jobs = w.total[0];
+    const int groups = (jobs + pages_at_once - 1) / pages_at_once, parts = (a.kv_heads + heads_at_once - 1) / heads_at_once;
+    const int64_t items = (int64_t)groups * a.layers * parts;
     for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-        const int job = (int)(it / a.layers), l = (int)(it % a.layers);
-        int lo = 0, hi = a.batch;  // the sequence whose job it is: base[b] <= job < base[b + 1]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (w.base[mid] <= job) lo = mid;
-            else hi = mid;
-        }
-        const int b = lo, lp = w.begin[b] + job - w.base[b], to = w.free_ids[job];
-        const int S = start_of(a, b);
-        for (int rr = 0; rr < a.rows_per_seq; ++rr) {
-            const int64_t r = (int64_t)b * a.rows_per_seq + rr;
-            const int n = min(keep_len[r], a.cap);
-            for (int q0 = 0; q0 < a.page_size; q0 += kRowsAtOnce) {
-                const int rows = min(kRowsAtOnce, a.page_size - q0);
-                __syncthreads();
-                for (int q = threadIdx.x; q < rows; q += kCopyThreads) {
-                    const int64_t j = (int64_t)lp * a.page_size + q0 + q - S;
-                    int64_t row = -1;
-                    if (j >= 0 && j < n) {
-                        const int64_t from = (int64_t)S + keep[r * a.cap + j];
-                        const int fp = (int)(from / a.page_size);
-                        const int page = from >= 0 && fp < a.max_pages ? a.table[(int64_t)b * a.max_pages + fp] : -1;
-                        if (page >= 0 && page < a.num_pages)
-                            row = (((int64_t)l * a.num_pages + page) * a.kv_heads) * a.page_size + from % a.page_size;
-                        else
-                            atomicOr(&g_pages_error, 128u);
-                    }
-                    src[q] = row;
+        const int g0 = (int)(it % parts) * heads_at_once, heads = min(heads_at_once, a.kv_heads - g0);
+        const int l = (int)(it / parts % a.layers), job0 = (int)(it / parts / a.layers) * pages_at_once;
+        const int pages = min(pages_at_once, jobs - job0);
+        for (int q0 = 0; q0 < a.page_size; q0 += kRowsAtOnce) {  // (pages longer than that: one of them, in parts)
+            const int rows = min(a.page_size - q0, kRowsAtOnce), n = pages * rows * heads;
+            __syncthreads();
+            for (int i = threadIdx.x; i < n; i += kCopyThreads) {
+                // rows of one head behind one another, as they lie in a page
+                const int q = i % rows, g = g0 + i / rows % heads, job = job0 + i / (rows * heads);
+                int lo = 0, hi = a.batch;  // the sequence whose job it is: base[b] <= job < base[b + 1]
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (w.base[mid] <= job) lo = mid;
+                    else hi = mid;
                 }
-                __syncthreads();
-                const int g0 = a.rows_per_seq == 1 ? 0 : rr, g1 = a.rows_per_seq == 1 ? a.kv_heads : rr + 1;
-                for (int pl = 0; pl < a.n_planes; ++pl) {
-                    const int rb = a.row_bytes[pl];
-                    for (int g = g0; g < g1; ++g) {
-                        const int64_t head = (int64_t)g * a.page_size;
-                        unsigned char *d =
-                            a.plane[pl] + ((((int64_t)l * a.num_pages + to) * a.kv_heads) * a.page_size + head + q0) * rb;
-                        const unsigned char *base = a.plane[pl] + head * rb;
-                        if (rb % 16 == 0) gather_rows<uint4>(d, base, src, rows, rb);
-                        else gather_rows<uint32_t>(d, base, src, rows, rb);
+                const int b = lo, S = start_of(a, b);
+                const int64_t r = a.rows_per_seq == 1 ? b : (int64_t)b * a.rows_per_seq + g;
+                const int64_t j = (int64_t)(w.begin[b] + job - w.base[b]) * a.page_size + q0 + q - S;
+                RowMove m{-1, 0};
+                if (j >= 0 && j < min(keep_len[r], a.cap)) {
+                    const int64_t from = (int64_t)S + keep[r * a.cap + j];
+                    const int fp = (int)(from / a.page_size);
+                    const int page = from >= 0 && fp < a.max_pages ? a.table[(int64_t)b * a.max_pages + fp] : -1;
+                    if (page >= 0 && page < a.num_pages) {
+                        m.src = (((int64_t)l * a.num_pages + page) * a.kv_heads + g) * a.page_size + from % a.page_size;
+                        m.dst = (((int64_t)l * a.num_pages + w.free_ids[job]) * a.kv_heads + g) * a.page_size + q0 + q;
+                    } else {
+                        atomicOr(&g_pages_error, 128u);
                     }
                 }
+                moves[i] = m;
+            }
+            __syncthreads();
+            for (int pl = 0; pl < a.n_planes; ++pl) {
+                const int rb = a.row_bytes[pl];
+                if (rb % 16 == 0) gather_plane<uint4>(a.plane[pl], rb, moves, n);
+                else if (rb % 8 == 0) gather_plane<uint2>(a.plane[pl], rb, moves, n);
+                else gather_plane<uint32_t>(a.plane[pl], rb, moves, n);
             }
         }
     }
@@ -483,9 +523,12 @@ cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int
     cudaError_t e = launch_k(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, w, keep, keep_len, lacking);
     note_launch();
     if (e != cudaSuccess) return e;
+    const int part = a.page_size < kRowsAtOnce ? a.page_size : kRowsAtOnce;
+    const int heads = a.kv_heads < kHeadRows / part ? a.kv_heads : kHeadRows / part;
+    const int at_once = kRowsAtOnce / part < kHeadRows / (part * heads) ? kRowsAtOnce / part : kHeadRows / (part * heads);
     const int64_t items = (int64_t)a.batch * a.max_pages * a.layers;
     const int64_t ctas = items < 8 * (int64_t)sms ? items : 8 * (int64_t)sms;
-    e = launch_k(compact_copy_kernel, dim3((unsigned)ctas), dim3(kCopyThreads), 0, st, a, w, keep, keep_len);
+    e = launch_k(compact_copy_kernel, dim3((unsigned)ctas), dim3(kCopyThreads), 0, st, a, w, keep, keep_len, at_once, heads);
     note_launch();
     if (e != cudaSuccess) return e;
     const int64_t rows = (int64_t)a.batch * a.rows_per_seq;

@@ -137,12 +137,14 @@ template <> struct Chunk<float> {
     }
 };
 
-// The rows of a CTA: D / 8 threads a row, K and V alike; row r of a sequence is KV head
-// r % kv_heads of its token r / kv_heads, so a CTA's dense side is one run of memory.
-template <typename T, int D, bool STORE>
-__global__ void __launch_bounds__(kMoveThreads) q4_move_kernel(const Q4MoveArgs a) {
+// The rows of a CTA: D / 8 threads a row, K and V alike, ROWS rows a thread; row r of a sequence is KV
+// head r % kv_heads of its token r / kv_heads, so a CTA's dense side is one run of memory.  Bound by
+// memory: all of a thread's loads, K's and V's, go out before the first is used.
+template <typename T, int D, bool STORE, int ROWS>
+__global__ void __launch_bounds__(kMoveThreads, 3) q4_move_kernel(const Q4MoveArgs a) {
     pdl_wait();
-    constexpr int TPR = D / 8, RPP = kMoveThreads / TPR;
+    constexpr int TPR = D / 8, Y = D / kQ4Group;
+    const int RPP = blockDim.x / TPR;  // rows of a pass
     const int blk = blockIdx.x % a.blocks, lb = blockIdx.x / a.blocks;
     const int b = lb % a.batch, li = lb / a.batch;
     const int G = a.pv.kv_heads;
@@ -161,94 +163,96 @@ __global__ void __launch_bounds__(kMoveThreads) q4_move_kernel(const Q4MoveArgs 
         if (threadIdx.x == 0) atomicOr(&g_q4_error, 32u);
         return;
     }
-    const int p = threadIdx.x & (TPR - 1);
     const int rows = n * G;
-    const int64_t dense0 = (int64_t)li * a.rows.layer + (a.rows.row0 ? a.rows.row0[b] * a.rows.token : b * a.rows.seq);
+    if (blk * RPP * ROWS >= rows) return;
+    const int p = threadIdx.x & (TPR - 1), r0 = blk * RPP * ROWS + threadIdx.x / TPR;
+    const int64_t dense0 = (int64_t)li * a.rows.layer + (a.rows.row0 ? a.rows.row0[b] * a.rows.token : b * a.rows.seq) + p * 8;
     T *dk = static_cast<T *>(a.rows.k) + dense0, *dv = static_cast<T *>(a.rows.v) + dense0;
-    const int r0 = blk * (RPP * kMoveRows) + threadIdx.x / TPR;
-    if (r0 - (int)threadIdx.x / TPR >= rows) return;
-    int64_t dense[kMoveRows], paged[kMoveRows];
-    bool in[kMoveRows];
+    int64_t dense[ROWS], paged[ROWS];
+    bool in[ROWS];
 #pragma unroll
-    for (int j = 0; j < kMoveRows; ++j) {
+    for (int j = 0; j < ROWS; ++j) {
         const int r = r0 + j * RPP;
         in[j] = r < rows;
         const int i = in[j] ? (a.head_shift >= 0 ? r >> a.head_shift : r / G) : 0, g = in[j] ? r - i * G : 0;
-        dense[j] = i * a.rows.token + g * a.rows.head + p * 8;
+        dense[j] = i * a.rows.token + g * a.rows.head;
         paged[j] = a.pv.row_phys(b, a.layer0 + li, g, S + first + i);
     }
     if (STORE) {
+        Chunk<T> x[2][ROWS];
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+            for (int j = 0; j < ROWS; ++j)
+                if (in[j]) x[kv][j].load((kv ? dv : dk) + dense[j]);
+                else x[kv][j].zero();
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-            const T *src = kv ? dv : dk;
             unsigned char *codes = kv ? a.v : a.k;
             uint16_t *scales = kv ? a.vs : a.ks;
-            Chunk<T> x[kMoveRows];
 #pragma unroll
-            for (int j = 0; j < kMoveRows; ++j)
-                if (in[j]) x[j].load(src + dense[j]);
-                else x[j].zero();
-#pragma unroll
-            for (int j = 0; j < kMoveRows; ++j) {
-                uint32_t m = x[j].amax();
+            for (int j = 0; j < ROWS; ++j) {
+                uint32_t m = x[kv][j].amax();
                 m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
                 m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
                 const uint32_t s = group_scale(__uint_as_float(m));
-                const uint32_t w = to_units<D>(x[j].codes(__uint_as_float(s)));
+                const uint32_t w = to_units<D>(x[kv][j].codes(__uint_as_float(s)));
                 if (!in[j]) continue;
                 *reinterpret_cast<uint32_t *>(codes + paged[j] * (D / 2) + p * 4) = w;
-                if ((p & 3) == 0) scales[paged[j] * (D / kQ4Group) + (p >> 2)] = (uint16_t)(s >> 16);
+                if ((p & 3) == 0) scales[paged[j] * Y + (p >> 2)] = (uint16_t)(s >> 16);
             }
         }
     } else {
+        uint32_t w[2][ROWS], s[2][ROWS];
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            T *dst = kv ? dv : dk;
-            const unsigned char *codes = kv ? a.v : a.k;
-            const uint16_t *scales = kv ? a.vs : a.ks;
-            uint32_t w[kMoveRows];
-            float s[kMoveRows];
+        for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-            for (int j = 0; j < kMoveRows; ++j) {
-                w[j] = in[j] ? __ldg(reinterpret_cast<const uint32_t *>(codes + paged[j] * (D / 2) + p * 4)) : 0u;
-                s[j] = in[j] ? __uint_as_float((uint32_t)__ldg(scales + paged[j] * (D / kQ4Group) + (p >> 2)) << 16) : 0.f;
+            for (int j = 0; j < ROWS; ++j) {
+                w[kv][j] = in[j] ? __ldg(reinterpret_cast<const uint32_t *>((kv ? a.v : a.k) + paged[j] * (D / 2) + p * 4)) : 0u;
+                s[kv][j] = in[j] ? __ldg((kv ? a.vs : a.ks) + paged[j] * Y + (p >> 2)) : 0u;
             }
 #pragma unroll
-            for (int j = 0; j < kMoveRows; ++j) {
-                const uint32_t c = from_units<D>(w[j]);
+        for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+            for (int j = 0; j < ROWS; ++j) {
+                const uint32_t c = from_units<D>(w[kv][j]);
+                const float f = __uint_as_float(s[kv][j] << 16);
                 float y[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float2 f = __half22float2(e2m1_pair(c, i));
-                    y[2 * i] = f.x * s[j];
-                    y[2 * i + 1] = f.y * s[j];
+                    const float2 v = __half22float2(e2m1_pair(c, i));
+                    y[2 * i] = v.x * f;
+                    y[2 * i + 1] = v.y * f;
                 }
                 Chunk<T> x;
                 x.set(y);
-                if (in[j]) x.store(dst + dense[j]);
+                if (in[j]) x.store((kv ? dv : dk) + dense[j]);
             }
-        }
     }
 }
 
-template <bool STORE>
-cudaError_t launch_move(Q4MoveArgs a, int dtype, cudaStream_t st) {
-    const int D = a.pv.head_dim;
-    const int per = kMoveThreads / (D / 8) * kMoveRows;
-    a.blocks = (int)(((int64_t)a.max_count * a.pv.kv_heads + per - 1) / per);
+template <typename T, int D, bool STORE>
+cudaError_t launch_move_t(Q4MoveArgs a, cudaStream_t st) {
+    // single tokens: a row a thread, in CTAs no larger than a sequence's rows need
+    const int64_t rows = (int64_t)a.max_count * a.pv.kv_heads;
+    const bool few = rows * (D / 8) <= kMoveThreads;
+    const int threads = few ? (int)((rows * (D / 8) + 31) / 32 * 32) : kMoveThreads;
+    const int per = threads / (D / 8) * (few ? 1 : kMoveRows);
+    a.blocks = (int)((rows + per - 1) / per);
     const int64_t ctas = (int64_t)a.blocks * a.batch * a.n_layers;
     if (ctas == 0) return cudaSuccess;
     if (ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    const dim3 grid((unsigned)ctas), block(kMoveThreads);
-    cudaError_t e;
-    if (dtype == IKV_BF16)
-        e = D == 128 ? launch_k(q4_move_kernel<__nv_bfloat16, 128, STORE>, grid, block, 0, st, a)
-                     : launch_k(q4_move_kernel<__nv_bfloat16, 64, STORE>, grid, block, 0, st, a);
-    else
-        e = D == 128 ? launch_k(q4_move_kernel<float, 128, STORE>, grid, block, 0, st, a)
-                     : launch_k(q4_move_kernel<float, 64, STORE>, grid, block, 0, st, a);
+    const cudaError_t e = launch_k(few ? q4_move_kernel<T, D, STORE, 1> : q4_move_kernel<T, D, STORE, kMoveRows>,
+                                   dim3((unsigned)ctas), dim3(threads), 0, st, a);
     note_launch();
     return e;
+}
+template <bool STORE>
+cudaError_t launch_move(const Q4MoveArgs &a, int dtype, cudaStream_t st) {
+    const bool wide = a.pv.head_dim == 128;
+    if (dtype == IKV_BF16)
+        return wide ? launch_move_t<__nv_bfloat16, 128, STORE>(a, st) : launch_move_t<__nv_bfloat16, 64, STORE>(a, st);
+    return wide ? launch_move_t<float, 128, STORE>(a, st) : launch_move_t<float, 64, STORE>(a, st);
 }
 
 }  // namespace
