@@ -325,28 +325,35 @@ compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
 
 // Rows of new pages: slot j comes from slot keep[j] of the old pages.  CTAs take items of one layer
 // and as many new pages as make about kRowsAtOnce rows (small pages would leave most threads
-// idle); where a row comes from and goes to is looked up once for all planes and heads.  Bound by
+// idle); where a row comes from and goes to is looked up once for all planes, and heads that keep the
+// same.  Bound by
 // memory: a thread has kAhead vectors in flight.
-constexpr int kRowsAtOnce = 128, kHeadRows = 1024;  // rows, rows x heads of an item
+constexpr int kRowsAtOnce = 128;
 struct RowMove {
-    int64_t src, dst;  // rows of a plane; src < 0: not moved
+    int64_t src, dst;  // rows of a plane, of the item's first head; src < 0: not moved
 };
+__device__ __forceinline__ int log2_or(int n) { return (n & (n - 1)) == 0 ? __ffs(n) - 1 : -1; }
+// heads x n_moves rows of a plane: head g's lie g * step rows behind the first head's
 template <typename V>
-__device__ __forceinline__ void gather_plane(unsigned char *plane, int rb, const RowMove *moves, int n_moves) {
+__device__ __forceinline__ void gather_plane(unsigned char *plane, int rb, const RowMove *moves, int n_moves, int heads, int step) {
     constexpr int kAhead = 8;
-    const int per = rb / (int)sizeof(V), n = n_moves * per;
-    const int shift = (per & (per - 1)) == 0 ? __ffs(per) - 1 : -1;
+    const int per = rb / (int)sizeof(V), n = heads * n_moves * per;
+    const int per_shift = log2_or(per), move_shift = log2_or(n_moves);
     for (int i0 = threadIdx.x; i0 < n; i0 += kCopyThreads * kAhead) {
         V x[kAhead];
         V *to[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int i = i0 + u * kCopyThreads, m = shift >= 0 ? i >> shift : i / per;
+            const int i = i0 + u * kCopyThreads, row = per_shift >= 0 ? i >> per_shift : i / per;
+            const int g = move_shift >= 0 ? row >> move_shift : row / n_moves;
             to[u] = nullptr;
-            if (i < n && moves[m].src >= 0) {
-                const int64_t piece = (int64_t)(i - m * per) * sizeof(V);
-                to[u] = reinterpret_cast<V *>(plane + moves[m].dst * rb + piece);
-                x[u] = *reinterpret_cast<const V *>(plane + moves[m].src * rb + piece);
+            if (i < n) {
+                const RowMove m = moves[row - g * n_moves];
+                if (m.src >= 0) {
+                    const int64_t piece = (int64_t)(i - row * per) * sizeof(V), head = (int64_t)g * step;
+                    to[u] = reinterpret_cast<V *>(plane + (m.dst + head) * rb + piece);
+                    x[u] = *reinterpret_cast<const V *>(plane + (m.src + head) * rb + piece);
+                }
             }
         }
 #pragma unroll
@@ -355,23 +362,23 @@ __device__ __forceinline__ void gather_plane(unsigned char *plane, int rb, const
     }
 }
 __global__ void __launch_bounds__(kCopyThreads)
-compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int pages_at_once,
-                    int heads_at_once) {
+compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int pages_at_once) {
     pdl_wait();
-    __shared__ RowMove moves[kHeadRows];
+    __shared__ RowMove moves[kRowsAtOnce];
     const int jobs = w.total[0];
-    const int groups = (jobs + pages_at_once - 1) / pages_at_once, parts = (a.kv_heads + heads_at_once - 1) / heads_at_once;
+    // heads that share their moves: all, or with a keep row for each KV head one
+    const int heads = a.rows_per_seq == 1 ? a.kv_heads : 1;
+    const int groups = (jobs + pages_at_once - 1) / pages_at_once, parts = a.kv_heads / heads;
     const int64_t items = (int64_t)groups * a.layers * parts;
     for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-        const int g0 = (int)(it % parts) * heads_at_once, heads = min(heads_at_once, a.kv_heads - g0);
+        const int g0 = (int)(it % parts);
         const int l = (int)(it / parts % a.layers), job0 = (int)(it / parts / a.layers) * pages_at_once;
         const int pages = min(pages_at_once, jobs - job0);
         for (int q0 = 0; q0 < a.page_size; q0 += kRowsAtOnce) {  // (pages longer than that: one of them, in parts)
-            const int rows = min(a.page_size - q0, kRowsAtOnce), n = pages * rows * heads;
+            const int rows = min(a.page_size - q0, kRowsAtOnce), n = pages * rows;
             __syncthreads();
             for (int i = threadIdx.x; i < n; i += kCopyThreads) {
-                // rows of one head behind one another, as they lie in a page
-                const int q = i % rows, g = g0 + i / rows % heads, job = job0 + i / (rows * heads);
+                const int q = i % rows, job = job0 + i / rows;
                 int lo = 0, hi = a.batch;  // the sequence whose job it is: base[b] <= job < base[b + 1]
                 while (hi - lo > 1) {
                     const int mid = (lo + hi) >> 1;
@@ -379,7 +386,7 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
                     else hi = mid;
                 }
                 const int b = lo, S = start_of(a, b);
-                const int64_t r = a.rows_per_seq == 1 ? b : (int64_t)b * a.rows_per_seq + g;
+                const int64_t r = a.rows_per_seq == 1 ? b : (int64_t)b * a.rows_per_seq + g0;
                 const int64_t j = (int64_t)(w.begin[b] + job - w.base[b]) * a.page_size + q0 + q - S;
                 RowMove m{-1, 0};
                 if (j >= 0 && j < min(keep_len[r], a.cap)) {
@@ -387,8 +394,8 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
                     const int fp = (int)(from / a.page_size);
                     const int page = from >= 0 && fp < a.max_pages ? a.table[(int64_t)b * a.max_pages + fp] : -1;
                     if (page >= 0 && page < a.num_pages) {
-                        m.src = (((int64_t)l * a.num_pages + page) * a.kv_heads + g) * a.page_size + from % a.page_size;
-                        m.dst = (((int64_t)l * a.num_pages + w.free_ids[job]) * a.kv_heads + g) * a.page_size + q0 + q;
+                        m.src = (((int64_t)l * a.num_pages + page) * a.kv_heads + g0) * a.page_size + from % a.page_size;
+                        m.dst = (((int64_t)l * a.num_pages + w.free_ids[job]) * a.kv_heads + g0) * a.page_size + q0 + q;
                     } else {
                         atomicOr(&g_pages_error, 128u);
                     }
@@ -398,9 +405,9 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
             __syncthreads();
             for (int pl = 0; pl < a.n_planes; ++pl) {
                 const int rb = a.row_bytes[pl];
-                if (rb % 16 == 0) gather_plane<uint4>(a.plane[pl], rb, moves, n);
-                else if (rb % 8 == 0) gather_plane<uint2>(a.plane[pl], rb, moves, n);
-                else gather_plane<uint32_t>(a.plane[pl], rb, moves, n);
+                if (rb % 16 == 0) gather_plane<uint4>(a.plane[pl], rb, moves, n, heads, a.page_size);
+                else if (rb % 8 == 0) gather_plane<uint2>(a.plane[pl], rb, moves, n, heads, a.page_size);
+                else gather_plane<uint32_t>(a.plane[pl], rb, moves, n, heads, a.page_size);
             }
         }
     }
@@ -523,12 +530,10 @@ cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int
     cudaError_t e = launch_k(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, w, keep, keep_len, lacking);
     note_launch();
     if (e != cudaSuccess) return e;
-    const int part = a.page_size < kRowsAtOnce ? a.page_size : kRowsAtOnce;
-    const int heads = a.kv_heads < kHeadRows / part ? a.kv_heads : kHeadRows / part;
-    const int at_once = kRowsAtOnce / part < kHeadRows / (part * heads) ? kRowsAtOnce / part : kHeadRows / (part * heads);
-    const int64_t items = (int64_t)a.batch * a.max_pages * a.layers;
+    const int at_once = a.page_size < kRowsAtOnce ? kRowsAtOnce / a.page_size : 1;
+    const int64_t items = (int64_t)a.batch * a.max_pages * a.layers * (a.rows_per_seq == 1 ? 1 : a.kv_heads);
     const int64_t ctas = items < 8 * (int64_t)sms ? items : 8 * (int64_t)sms;
-    e = launch_k(compact_copy_kernel, dim3((unsigned)ctas), dim3(kCopyThreads), 0, st, a, w, keep, keep_len, at_once, heads);
+    e = launch_k(compact_copy_kernel, dim3((unsigned)ctas), dim3(kCopyThreads), 0, st, a, w, keep, keep_len, at_once);
     note_launch();
     if (e != cudaSuccess) return e;
     const int64_t rows = (int64_t)a.batch * a.rows_per_seq;
