@@ -336,7 +336,7 @@ __device__ __forceinline__ int log2_or(int n) { return (n & (n - 1)) == 0 ? __ff
 // heads x n_moves rows of a plane: head g's lie g * step rows behind the first head's
 template <typename V>
 __device__ __forceinline__ void gather_plane(unsigned char *plane, int rb, const RowMove *moves, int n_moves, int heads, int step) {
-    constexpr int kAhead = 8;
+    constexpr int kAhead = 4;
     const int per = rb / (int)sizeof(V), n = heads * n_moves * per;
     const int per_shift = log2_or(per), move_shift = log2_or(n_moves);
     for (int i0 = threadIdx.x; i0 < n; i0 += kCopyThreads * kAhead) {
@@ -361,7 +361,7 @@ __device__ __forceinline__ void gather_plane(unsigned char *plane, int rb, const
             if (to[u]) *to[u] = x[u];
     }
 }
-__global__ void __launch_bounds__(kCopyThreads)
+__global__ void __launch_bounds__(kCopyThreads, 4)
 compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int pages_at_once) {
     pdl_wait();
     __shared__ RowMove moves[kRowsAtOnce];

@@ -27,27 +27,57 @@ __device__ __forceinline__ uint32_t group_scale(float a) {
     return a <= 0x1p127f ? bits : 0x7fc00000u;  // (false for NaN)
 }
 
-__device__ __forceinline__ uint32_t to_codes(float lo, float hi) {  // two codes in the low byte
+// Eight codes, the first in the lowest bits.
+__device__ __forceinline__ uint32_t to_codes(const float2 (&y)[4]) {
     uint32_t r;
-    asm("{\n\t.reg .b8 b;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %1, %2;\n\tcvt.u32.u8 %0, b;\n\t}" : "=r"(r) : "f"(hi), "f"(lo));
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r) : "f"(y[0].x), "f"(y[0].y), "f"(y[1].x), "f"(y[1].y), "f"(y[2].x), "f"(y[2].y), "f"(y[3].x), "f"(y[3].y));
     return r;
 }
+__device__ __forceinline__ float2 mul2(float2 a, float f) {  // both at once
+    uint64_t r;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%1, %2};\n\tmov.b64 y, {%3, %3};\n\tmul.rn.f32x2 %0, x, y;\n\t}"
+        : "=l"(r) : "f"(a.x), "f"(a.y), "f"(f));
+    return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
+}
+// 1 / s to an ulp or two
+__device__ __forceinline__ float inverse(float s) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    return s > 0.f ? r : 0.f;
+}
 
-template <typename T> struct Quad;  // 4 channels
+// 4 channels of a row; two of them (groups y and y + 1) make a word of codes.
+template <typename T> struct Quad;
 template <> struct Quad<__nv_bfloat16> {
     uint2 w;
     __device__ __forceinline__ void load(const __nv_bfloat16 *p) { w = __ldcs(reinterpret_cast<const uint2 *>(p)); }
     __device__ __forceinline__ void zero() { w = make_uint2(0u, 0u); }
-    __device__ __forceinline__ uint32_t amax() const {  // upper half: bits of the largest magnitude, NaN above all
-        const uint32_t m = 0x7fff7fffu, x = __vmaxu2(w.x & m, w.y & m);
-        return max(x << 16, x & 0xffff0000u);
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {  // of two pairs of magnitudes, or NaN
+        const __nv_bfloat162 r = __hmax2_nan(__habs2(*reinterpret_cast<const __nv_bfloat162 *>(&a)),
+                                             __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&b)));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    }
+    // the largest magnitudes of two groups over the row's threads (bits of a float; NaN above all)
+    static __device__ __forceinline__ void amax2(const Quad &a, const Quad &b, uint32_t &m0, uint32_t &m1) {
+        const uint32_t x = larger(a.w.x, a.w.y), y = larger(b.w.x, b.w.y);
+        uint32_t two = larger(__byte_perm(x, y, 0x5410), __byte_perm(x, y, 0x7632));
+#pragma unroll
+        for (int d = 1; d < kUnits; d <<= 1) two = larger(two, __shfl_xor_sync(0xffffffffu, two, d));
+        m0 = two << 16;
+        m1 = two & 0xffff0000u;
     }
     // |x| / s against a midpoint m: both x and m s have at most 11 bits, so they are equal or
     // 2^-11 apart, and a factor 1 + 2^-14 puts ties on the upper side and moves nothing else
-    static __device__ __forceinline__ float inverse(float s) { return s > 0.f ? __frcp_rn(s) * (1.f + 0x1p-14f) : 0.f; }
-    __device__ __forceinline__ uint32_t codes(float, float r) const {
-        return to_codes(__uint_as_float(w.x << 16) * r, __uint_as_float(w.x & 0xffff0000u) * r) |
-               to_codes(__uint_as_float(w.y << 16) * r, __uint_as_float(w.y & 0xffff0000u) * r) << 8;
+    static __device__ __forceinline__ uint32_t codes2(const Quad &a, const Quad &b, float, float, float r0, float r1) {
+        r0 *= 1.f + 0x1p-14f;
+        r1 *= 1.f + 0x1p-14f;
+        auto both = [](uint32_t x) { return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); };
+        const float2 y[4] = {mul2(both(a.w.x), r0), mul2(both(a.w.y), r0), mul2(both(b.w.x), r1), mul2(both(b.w.y), r1)};
+        return to_codes(y);
     }
     static __device__ __forceinline__ void store(__nv_bfloat16 *p, float2 a, float2 b) {
         const __nv_bfloat162 x = __floats2bfloat162_rn(a.x, a.y), y = __floats2bfloat162_rn(b.x, b.y);
@@ -63,21 +93,34 @@ template <> struct Quad<float> {
         const uint32_t m = 0x7fffffffu;
         return max(max(__float_as_uint(w.x) & m, __float_as_uint(w.y) & m), max(__float_as_uint(w.z) & m, __float_as_uint(w.w) & m));
     }
+    static __device__ __forceinline__ void amax2(const Quad &a, const Quad &b, uint32_t &m0, uint32_t &m1) {
+        m0 = a.amax();
+        m1 = b.amax();
+#pragma unroll
+        for (int d = 1; d < kUnits; d <<= 1) {
+            m0 = max(m0, __shfl_xor_sync(0xffffffffu, m0, d));
+            m1 = max(m1, __shfl_xor_sync(0xffffffffu, m1, d));
+        }
+    }
     // x may lie an ulp from a midpoint: where a factor of 1 +- 2^-20, which covers the errors of
     // the reciprocal and the product, makes a difference, m s decides, which is exact
-    static __device__ __forceinline__ float inverse(float s) { return s > 0.f ? __frcp_rn(s) : 0.f; }
-    __device__ __forceinline__ uint32_t codes(float s, float r) const {
-        const float ru = r * (1.f + 0x1p-20f), rd = r * (1.f - 0x1p-20f);
-        uint32_t c = to_codes(w.x * ru, w.y * ru) | to_codes(w.z * ru, w.w * ru) << 8;
-        if (c != (to_codes(w.x * rd, w.y * rd) | to_codes(w.z * rd, w.w * rd) << 8) && s > 0.f) {
-            const float x[4] = {w.x, w.y, w.z, w.w};
-            c = 0u;
+    static __device__ __forceinline__ uint32_t codes2(const Quad &a, const Quad &b, float s0, float s1, float r0, float r1) {
+        const float4 p = a.w, q = b.w;
+        auto all = [&](float f) {
+            const float2 y[4] = {mul2(make_float2(p.x, p.y), r0 * f), mul2(make_float2(p.z, p.w), r0 * f),
+                                 mul2(make_float2(q.x, q.y), r1 * f), mul2(make_float2(q.z, q.w), r1 * f)};
+            return to_codes(y);
+        };
+        uint32_t c = all(1.f + 0x1p-20f);
+        const uint32_t differ = c ^ all(1.f - 0x1p-20f);
+        if (differ) {
+            const float x[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = fabsf(x[i]);
-                const uint32_t n = (a >= 0.25f * s) + (a >= 0.75f * s) + (a >= 1.25f * s) + (a >= 1.75f * s) +
-                                   (a >= 2.5f * s) + (a >= 3.5f * s) + (a >= 5.f * s);
-                c |= (n | (x[i] < 0.f ? 8u : 0u)) << (4 * i);
+            for (int i = 0; i < 8; ++i) {
+                const float v = fabsf(x[i]), s = i < 4 ? s0 : s1;
+                const uint32_t n = (v >= 0.25f * s) + (v >= 0.75f * s) + (v >= 1.25f * s) + (v >= 1.75f * s) +
+                                   (v >= 2.5f * s) + (v >= 3.5f * s) + (v >= 5.f * s);
+                if (differ >> (4 * i) & 15u) c = (c & ~(15u << (4 * i))) | (n | (x[i] < 0.f ? 8u : 0u)) << (4 * i);
             }
         }
         return c;
@@ -144,42 +187,31 @@ __global__ void __launch_bounds__(kMoveThreads, 3) q4_move_kernel(const Q4MoveAr
             uint16_t *scales = kv ? a.vs : a.ks;
 #pragma unroll
             for (int j = 0; j < ROWS; ++j) {
-                // the groups' maxima over the row's threads: bf16's in halves of a word
                 uint32_t m[Y];
 #pragma unroll
-                for (int y = 0; y < Y; ++y) m[y] = x[kv][j][y].amax();
-                if (sizeof(T) == 2) {
-#pragma unroll
-                    for (int y = 0; y < Y; y += 2) {
-                        uint32_t two = __byte_perm(m[y], m[y + 1], 0x7632);
-#pragma unroll
-                        for (int d = 1; d < kUnits; d <<= 1) two = __vmaxu2(two, __shfl_xor_sync(0xffffffffu, two, d));
-                        m[y] = two << 16;
-                        m[y + 1] = two & 0xffff0000u;
-                    }
-                } else {
-#pragma unroll
-                    for (int y = 0; y < Y; ++y)
-#pragma unroll
-                        for (int d = 1; d < kUnits; d <<= 1) m[y] = max(m[y], __shfl_xor_sync(0xffffffffu, m[y], d));
-                }
+                for (int y = 0; y < Y; y += 2) Quad<T>::amax2(x[kv][j][y], x[kv][j][y + 1], m[y], m[y + 1]);
                 // thread u works out group u % Y's scale for all
                 uint32_t mine = m[0];
 #pragma unroll
                 for (int y = 1; y < Y; ++y)
                     if (u % Y == y) mine = m[y];
                 const uint32_t s_mine = group_scale(__uint_as_float(mine));
-                const float r_mine = Quad<T>::inverse(__uint_as_float(s_mine));
-                uint32_t c[Y];
+                const float r_mine = inverse(__uint_as_float(s_mine));
+                uint32_t c[Y / 2];
 #pragma unroll
-                for (int y = 0; y < Y; ++y) {
-                    const float s = sizeof(T) == 2 ? 0.f : __uint_as_float(__shfl_sync(0xffffffffu, s_mine, y, kUnits));
-                    c[y] = x[kv][j][y].codes(s, __shfl_sync(0xffffffffu, r_mine, y, kUnits));
+                for (int y = 0; y < Y; y += 2) {
+                    float s[2] = {0.f, 0.f}, r[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (sizeof(T) == 4) s[i] = __uint_as_float(__shfl_sync(0xffffffffu, s_mine, y + i, kUnits));
+                        r[i] = __shfl_sync(0xffffffffu, r_mine, y + i, kUnits);
+                    }
+                    c[y / 2] = Quad<T>::codes2(x[kv][j][y], x[kv][j][y + 1], s[0], s[1], r[0], r[1]);
                 }
                 if (!in[j]) continue;
                 unsigned char *to = codes + paged[j] * (D / 2) + u * (D / 16);
-                if (Y == 4) *reinterpret_cast<uint2 *>(to) = make_uint2(c[0] | c[1] << 16, c[2 % Y] | c[3 % Y] << 16);
-                else *reinterpret_cast<uint32_t *>(to) = c[0] | c[1] << 16;
+                if (Y == 4) *reinterpret_cast<uint2 *>(to) = make_uint2(c[0], c[Y / 2 - 1]);
+                else *reinterpret_cast<uint32_t *>(to) = c[0];
                 if (u < Y) scales[paged[j] * Y + u] = (uint16_t)(s_mine >> 16);
             }
         }
