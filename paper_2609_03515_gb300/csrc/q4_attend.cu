@@ -380,6 +380,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
         post[1] = __shfl_sync(0xffffffffu, mine, 8 * t + 4);
     }
 
+    // where the logits of heads 2 t and 2 t + 1 go, by cache slot
+    float *const lg = SCORE ? a.logits + (head0 + 2 * t) * a.lstride : nullptr;
+    const bool lg0 = 2 * t < G, lg1 = 2 * t + 1 < G;
+
     float o[2 * Y][4];  // O^T of channels 32 y + 4 g + 2 h (+ 1), heads 2 t, 2 t + 1
 #pragma unroll
     for (int i = 0; i < 2 * Y; ++i)
@@ -438,9 +442,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
                 const bool have = !MASK || (j >= 0 && j < L);
                 in[u][r] = have && (!MASK || !pos || s.pos[tok0 + 8 * r] >= 0);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    z[u][2 * r + c] = in[u][r] ? z[u][2 * r + c] * post[c] : -INFINITY;
-                    if (SCORE && have && 2 * t + c < G) a.logits[(head0 + 2 * t + c) * a.lstride + j] = z[u][2 * r + c];
+                for (int c = 0; c < 2; ++c) z[u][2 * r + c] = in[u][r] ? z[u][2 * r + c] * post[c] : -INFINITY;
+                if (SCORE && have) {
+                    if (lg0) lg[j] = z[u][2 * r];
+                    if (lg1) lg[j + a.lstride] = z[u][2 * r + 1];
                 }
             }
         }
@@ -638,13 +643,12 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
 // The first CTAs take a utility row's tokens, kFinishThreads / HS of them each, HS threads a token
 // that share the row's heads; the others merge a head's outputs.  A head's log-sum-exp comes from
 // its segments' (reference, sum) pairs, so no pass of its own has to gather it.
-constexpr int kFinishThreads = 256;
+constexpr int kFinishThreads = 512;
 
 // One CTA merges one head's segments: every warp sums some of them, 32 E channels wide.
 template <int E, typename T>
-__device__ __forceinline__ void merge_segments(const Q4FinishArgs &a, int hh) {
-    constexpr int kW = kFinishThreads / 32, D = 32 * E, kLoads = 4;
-    __shared__ __align__(16) float sum[kW][D];
+__device__ __forceinline__ void merge_segments(const Q4FinishArgs &a, int hh, float *sum) {
+    constexpr int kW = kFinishThreads / 32, D = 32 * E, kLoads = 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (int64_t)hh * kMaxSplits;
     const float *po = a.part_o + (int64_t)hh * kMaxSplits * D + lane * E;
@@ -702,49 +706,50 @@ __device__ __forceinline__ void merge_segments(const Q4FinishArgs &a, int hh) {
         }
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[warp][lane * E + e] = acc[e];
+    for (int e = 0; e < E; ++e) sum[warp * D + lane * E + e] = acc[e];
     __syncthreads();
     if (threadIdx.x < D) {
         float x = 0.f;
 #pragma unroll
-        for (int k = 0; k < kW; ++k) x += sum[k][threadIdx.x];
+        for (int k = 0; k < kW; ++k) x += sum[k * D + threadIdx.x];
         store_as(static_cast<T *>(a.out) + (int64_t)hh * D + threadIdx.x, w == 0.f ? 0.f : x / w);
     }
 }
 
 // CTA x of those that merge: of one head (MANY), or of a head a warp.
 template <bool MANY, int E, typename T>
-__device__ __forceinline__ void merge_any(const Q4FinishArgs &a, int x) {
+__device__ __forceinline__ void merge_any(const Q4FinishArgs &a, int x, float *room) {
     if (MANY) {
-        merge_segments<E, T>(a, x);
+        merge_segments<E, T>(a, x, room);
         return;
     }
-    __shared__ float wq[kFinishThreads / 32][kMaxSplits];
     const int warp = threadIdx.x >> 5, hh = x * (kFinishThreads / 32) + warp;
     if (hh >= a.batch * a.q_heads) return;
     const int n = a.len[hh / a.q_heads] > 0 ? __ldcg(a.segs + hh / (a.q_heads / a.kv_heads)) : 0;
     if (n != 1)
         merge_head<E>(reinterpret_cast<const float2 *>(a.part_ml) + (int64_t)hh * kMaxSplits,
-                      a.part_o + (int64_t)hh * kMaxSplits * 32 * E, n, wq[warp],
+                      a.part_o + (int64_t)hh * kMaxSplits * 32 * E, n, room + warp * kMaxSplits,
                       static_cast<T *>(a.out) + (int64_t)hh * 32 * E, (float *)nullptr);
 }
 
 template <int HS, bool MANY>
 __global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4FinishArgs a) {
-    constexpr int kTok = kFinishThreads / HS, kAhead = 8, kWarpsF = kFinishThreads / 32, kHeads = 4;
+    constexpr int kTok = kFinishThreads / HS, kAhead = 8, kWarpsF = kFinishThreads / 32, kHeads = 2;
     extern __shared__ float lse[];  // [heads of a row]
     __shared__ float part[HS > 1 ? kFinishThreads : 1];
+    __shared__ float room[kWarpsF * 128];  // of those that merge
+    static_assert(kMaxSplits <= 128, "a warp's weights");
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int G = a.q_heads / a.kv_heads;
     if ((int)blockIdx.x >= a.token_ctas) {
         const int x = (int)blockIdx.x - a.token_ctas;
         if (a.bf16) {
-            if (a.head_dim == 128) merge_any<MANY, 4, __nv_bfloat16>(a, x);
-            else merge_any<MANY, 2, __nv_bfloat16>(a, x);
+            if (a.head_dim == 128) merge_any<MANY, 4, __nv_bfloat16>(a, x, room);
+            else merge_any<MANY, 2, __nv_bfloat16>(a, x, room);
         } else {
-            if (a.head_dim == 128) merge_any<MANY, 4, float>(a, x);
-            else merge_any<MANY, 2, float>(a, x);
+            if (a.head_dim == 128) merge_any<MANY, 4, float>(a, x, room);
+            else merge_any<MANY, 2, float>(a, x, room);
         }
         return;
     }
@@ -755,22 +760,48 @@ __global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4Finis
     const int64_t head0 = (int64_t)b * a.q_heads + h0;
     // whatever has an address goes out before anything is waited for
     const int L = a.len[b];
-    const float *zp = a.logits + head0 * a.lstride + token;
     float z[kAhead], was = 0.f;
+    const int64_t next = (int64_t)HS * a.lstride;  // from one of the thread's heads to its next
+    const float *zp = a.logits + (head0 + hs) * a.lstride + min(token, a.lstride - 1);
+    const int mine = (nh - hs + HS - 1) / HS;      // the thread's heads: hs, hs + HS, ...
     auto load = [&](int j0) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int h = (j0 + j) * HS + hs;
-            z[j] = h < nh && token < a.lstride ? __ldcg(zp + (int64_t)h * a.lstride) : 0.f;
-        }
+        for (int j = 0; j < kAhead; ++j) z[j] = j0 + j < mine ? __ldcg(zp + (j0 + j) * next) : -INFINITY;
     };
     load(0);
     if (a.ema && hs == 0 && token < a.cap) was = a.ema[(int64_t)r * a.cap + token];
     if (block * kTok >= L) return;  // (a sequence without slots has no segment count either)
-    for (int hb = warp; hb < nh; hb += kHeads * kWarpsF) {
+    if (!MANY) {  // few segments: a head a thread
+        for (int h = threadIdx.x; h < nh; h += kFinishThreads) {
+            constexpr int kFew = 4;
+            const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (head0 + h) * kMaxSplits;
+            const int n = __ldcg(a.segs + (head0 + h) / G);
+            const float one = __ldcg(a.lse2 + head0 + h);
+            float2 y[kFew];
+#pragma unroll
+            for (int k = 0; k < kFew; ++k) y[k] = __ldcg(ml + k);
+            float x = one;
+            if (n != 1) {
+                float m = -INFINITY, w = 0.f;
+#pragma unroll
+                for (int k = 0; k < kFew; ++k) m = k < n ? fmaxf(m, y[k].x) : m;
+                for (int k = kFew; k < n; ++k) m = fmaxf(m, __ldcg(&ml[k].x));
+                const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int k = 0; k < kFew; ++k) w += k < n ? y[k].y * exp2f(y[k].x - base) : 0.f;
+                for (int k = kFew; k < n; ++k) {
+                    const float2 v = __ldcg(ml + k);
+                    w += v.y * exp2f(v.x - base);
+                }
+                x = w == 0.f ? -INFINITY : m + log2f(w);
+            }
+            lse[h] = x == -INFINITY ? INFINITY : x;  // no live slot: probabilities 0
+        }
+    }
+    for (int hb = warp; MANY && hb < nh; hb += kHeads * kWarpsF) {
         int n[kHeads];
         float one[kHeads];
-        constexpr int PL = MANY ? 2 : 1;  // pairs a lane loads before it knows how many there are
+        constexpr int PL = 2;  // pairs a lane loads before it knows how many there are
         float2 y[kHeads][PL];
 #pragma unroll
         for (int j = 0; j < kHeads; ++j) {
@@ -807,18 +838,15 @@ __global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4Finis
                 w = warp_sum(w);
                 x = w == 0.f ? -INFINITY : m + log2f(w);
             }
-            if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;  // no live slot: probabilities 0
+            if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;
         }
     }
     __syncthreads();
     float acc = 0.f;
-    for (int j0 = 0; j0 * HS < nh; j0 += kAhead) {
+    for (int j0 = 0; j0 < mine; j0 += kAhead) {
         if (j0) load(j0);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int h = (j0 + j) * HS + hs;
-            if (h < nh) acc += exp2f(z[j] - lse[h]);
-        }
+        for (int j = 0; j < kAhead; ++j) acc += exp2_fast(z[j] - lse[min((j0 + j) * HS + hs, nh - 1)]);  // (past the last: 0)
     }
     if (HS > 1) {
         part[threadIdx.x] = acc;
