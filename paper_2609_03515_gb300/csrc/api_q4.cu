@@ -180,6 +180,9 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     // (the kernels count the sequences' pairs of tiles in 32 bits)
     if ((int64_t)shape->batch * shape->kv_heads * (a.cap / 32 + 1) > 0x7fffffff)
         return report(IKV_ERR_SHAPE, "batch * kv_heads * cap too large");
+    // (and name a pool's tiles in 32 bits)
+    if ((uint64_t)shape->layers * shape->kv_heads * cache->num_pages * (cache->page_size / kQ4Tile) > 0xffffffffu)
+        return report(IKV_ERR_SHAPE, "pool too large");
     PdlScope pdl;
     const int32_t ctas = q4_attend_ctas(shape, cache->max_len, sm_count());
     IKV_TRY_CUDA(launch_q4_attend(a, shape->dtype, shape->head_dim, ctas, stream), "4-bit attend launch");

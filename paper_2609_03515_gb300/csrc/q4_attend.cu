@@ -14,7 +14,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kPair = 2;              // tiles of an iteration
 constexpr int kStages = 3;            // pairs of tiles a warp has in flight or in use
 constexpr int kCtasPerSm = 3;
-constexpr int kSwitch = 6;             // what going from one unit to the next costs a CTA, in pairs of tiles
+constexpr int kSwitch = 12;            // what going from one unit to the next costs a CTA, in pairs of tiles
 constexpr float kMaxSlack = 6.f;      // log2: how far a logit may lie above the running reference
 constexpr float kScaleRoom = 256.f;   // how far a V scale may grow, normalised, before it is renormalised
 
@@ -274,26 +274,29 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
     // the warp's pairs of tiles: first / 2 + warp, + kWarps, ...; lane i knows where the i-th of
     // the 32 tiles from a multiple of 32 on starts
     auto tile_of = [&](int i) { return first + ((i >> 1) * kWarps + warp) * kPair + (i & 1); };  // my i-th tile
-    auto row_of = [&](int i) -> int64_t {  // row of the paged arrays where it starts
+    auto place_of = [&](int i) -> uint32_t {  // the tile of the paged arrays (its row / kQ4Tile)
         const int x = tile_of(i);
-        return x < last ? a.pv.row_phys(sg.b, a.layer, sg.kv, (sp.tile0 + x) * kQ4Tile) : 0;
+        return x < last ? (uint32_t)(a.pv.row_phys(sg.b, a.layer, sg.kv, (sp.tile0 + x) * kQ4Tile) / kQ4Tile) : 0u;
     };
-    int64_t my_row = 0;
+    uint32_t places = 0;
+    const unsigned char *const from_k = a.k + lane * 16, *const from_v = a.v + lane * 16;
     auto issue = [&](int i, uint32_t stage) {
         if (i < mine) {
-            if ((i & 15) == 0) my_row = row_of(2 * i + lane);
+            if ((i & 15) == 0) places = place_of(2 * i + lane);
 #pragma unroll
             for (int u = 0; u < kPair; ++u) {
-                const int64_t row = __shfl_sync(0xffffffffu, my_row, (2 * i + u) & 31);
+                const uint32_t place = __shfl_sync(0xffffffffu, places, (2 * i + u) & 31);
                 const uint32_t dst = stage + u * sizeof(Tile<D>);
                 if (u > 0 && tile_of(2 * i + u) >= last) break;
-                const unsigned char *ks = a.k + row * Tile<D>::kRow + lane * 16, *vs = a.v + row * Tile<D>::kRow + lane * 16;
+                const unsigned char *k = from_k + (uint64_t)place * (kQ4Tile * Tile<D>::kRow);
+                const unsigned char *v = from_v + (uint64_t)place * (kQ4Tile * Tile<D>::kRow);
 #pragma unroll
                 for (int j = 0; j < kCopies; ++j) {
-                    copy16(dst + to_k[j], ks + j * 512);
-                    copy16(dst + to_v[j], vs + j * 512);
+                    copy16(dst + to_k[j], k + j * 512);
+                    copy16(dst + to_v[j], v + j * 512);
                 }
-                if ((lane & 7) < kScalePieces && lane < 16) copy16(dst + to_s, scales + row * Tile<D>::kScaleRow);
+                if ((lane & 7) < kScalePieces && lane < 16)
+                    copy16(dst + to_s, scales + (uint64_t)place * (kQ4Tile * Tile<D>::kScaleRow));
                 else if (lane >= 16 && pos) {
                     const int j = (sp.tile0 + tile_of(2 * i + u)) * kQ4Tile + lane - 16 - sp.S;
                     if (j >= 0 && j < sp.L) copy4(dst + offsetof(Tile<D>, pos) + (lane - 16) * 4, pos + j);
@@ -390,8 +393,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
     float ref[2] = {-FLT_MAX, -FLT_MAX}, sum[2] = {0.f, 0.f};
-    float norm = 1.f, room = -1.f;  // V scales times norm stay within kScaleRoom while they are <= room
-    int norm_e = 0;                 // norm = 2^norm_e
+    // weights carry 2^norm_e, so that V scales times it stay within kScaleRoom while they are <= room
+    float norm_e = 0.f, room = -1.f;
 
     const int tok0 = perm_of_row(g);  // tokens of rows g and g + 8: tok0, tok0 + 8
     // One pair of tiles; MASK: some of its slots are not the sequence's, or dead
@@ -442,10 +445,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
                 const bool have = !MASK || (j >= 0 && j < L);
                 in[u][r] = have && (!MASK || !pos || s.pos[tok0 + 8 * r] >= 0);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) z[u][2 * r + c] = in[u][r] ? z[u][2 * r + c] * post[c] : -INFINITY;
+                for (int c = 0; c < 2; ++c)
+                    if (!in[u][r]) z[u][2 * r + c] = -INFINITY;
                 if (SCORE && have) {
-                    if (lg0) lg[j] = z[u][2 * r];
-                    if (lg1) lg[j + a.lstride] = z[u][2 * r + 1];
+                    if (lg0) lg[j] = z[u][2 * r] * post[0];
+                    if (lg1) lg[j + a.lstride] = z[u][2 * r + 1] * post[1];
                 }
             }
         }
@@ -462,54 +466,63 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
                     sv[u][r][y] = in[u][r] ? w : 0u;
                     big = max3(big, bf16_lo(sv[u][r][y]), bf16_hi(sv[u][r][y]));
                 }
-        // ---- running reference of the logits, norm of the scales
-        float over = -FLT_MAX;
+        // ---- running reference of the logits, norm of the scales; a weight is 2^(logit - less)
+        float less[2] = {ref[0] - norm_e, ref[1] - norm_e}, d[kPair][4], over = -FLT_MAX;
+        auto weigh = [&]() {
+#pragma unroll
+            for (int u = 0; u < kPair; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[u][e] = fmaf(z[u][e], post[e & 1], -less[e & 1]);
+        };
+        weigh();
 #pragma unroll
         for (int u = 0; u < kPair; ++u)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) over = max3(over, z[u][c] - ref[c], z[u][2 + c] - ref[c]);
-        if (__any_sync(0xffffffffu, over > kMaxSlack || big > room)) {
+            for (int c = 0; c < 2; ++c) over = max3(over, d[u][c], d[u][2 + c]);
+        if (__any_sync(0xffffffffu, over > kMaxSlack + norm_e || big > room)) {
+            float f[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                float m = ref[c];
+                float m = -INFINITY;
 #pragma unroll
                 for (int u = 0; u < kPair; ++u) m = max3(m, z[u][c], z[u][2 + c]);
 #pragma unroll
-                for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-                const float f = exp2_fast(ref[c] - m);
+                for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+                m = fmaxf(ref[c], m * post[c]);
+                f[c] = exp2_fast(ref[c] - m);
                 ref[c] = m;
-                sum[c] *= f;
+            }
+#pragma unroll
+            for (int x = 1; x < 32; x <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, x));
+            if (big > room) {
+                // (2^104: a weight of 2^6 and a sum of 2^16 of them stay finite)
+                const float e = big > 0.f ? (float)(4 - max(ilogbf(big), -100)) : norm_e;
+                // (nothing summed before the first)
+                const float up = room < 0.f ? 1.f : ldexpf(1.f, (int)(e - norm_e));
+                f[0] *= up;
+                f[1] *= up;
+                norm_e = e;
+                room = big > 0.f ? kScaleRoom * ldexpf(1.f, -(int)e) : 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                sum[c] *= f[c];
+                less[c] = ref[c] - norm_e;
 #pragma unroll
                 for (int j = 0; j < 2 * Y; ++j) {
-                    o[j][c] *= f;
-                    o[j][2 + c] *= f;
+                    o[j][c] *= f[c];
+                    o[j][2 + c] *= f[c];
                 }
             }
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
-            if (big > room) {
-                const int e = big > 0.f ? 4 - max(ilogbf(big), -114) : norm_e;
-                const float f = room < 0.f ? 1.f : ldexpf(1.f, e - norm_e);  // (nothing summed before the first)
-                norm_e = e;
-                norm = ldexpf(1.f, e);
-                room = big > 0.f ? kScaleRoom * ldexpf(1.f, -e) : 0.f;
-#pragma unroll
-                for (int j = 0; j < 2 * Y; ++j)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) o[j][c] *= f;
-            }
+            weigh();
         }
 #pragma unroll
         for (int u = 0; u < kPair; ++u) {
             float p[4];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                p[c] = exp2_fast(z[u][c] - ref[c]);
-                p[2 + c] = exp2_fast(z[u][2 + c] - ref[c]);
-                sum[c] += p[c] + p[2 + c];
-            }
+            for (int e = 0; e < 4; ++e) p[e] = exp2_fast(d[u][e]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] *= norm;
+            for (int c = 0; c < 2; ++c) sum[c] += p[c] + p[2 + c];
             // ---- outputs
             uint32_t vw[4][Y / 2];  // unit g of tokens t, 4 + t, 8 + t, 12 + t
 #pragma unroll
@@ -586,10 +599,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], d);
     __syncthreads();  // the join before is read
-    const float back = ldexpf(1.f, -norm_e);
+    const float back = ldexpf(1.f, -(int)norm_e);
     if (g == 0) {
-        ml[warp * 8 + 2 * t] = make_float2(ref[0], sum[0]);
-        ml[warp * 8 + 2 * t + 1] = make_float2(ref[1], sum[1]);
+        ml[warp * 8 + 2 * t] = make_float2(ref[0], sum[0] * back);
+        ml[warp * 8 + 2 * t + 1] = make_float2(ref[1], sum[1] * back);
     }
 #pragma unroll
     for (int y = 0; y < Y; ++y)
