@@ -361,16 +361,59 @@ __device__ __forceinline__ void gather_plane(unsigned char *plane, int rb, const
             if (to[u]) *to[u] = x[u];
     }
 }
+// Row x of pos, then of ema, then of vnorm, gathered in place: keep[j] >= j, so a run of slots is read
+// before it is written, and no later run is read from it.
+__device__ __forceinline__ void gather_in_place(const PagesArgs &a, const int32_t *keep, const int32_t *keep_len, int64_t x) {
+    constexpr int U = 8;
+    const int64_t R = (int64_t)a.batch * a.rows_per_seq;
+    int64_t r = x;
+    uint32_t *row;  // 4-byte values whatever they are
+    if (x < R) {
+        if (!a.pos) return;
+        row = reinterpret_cast<uint32_t *>(a.pos) + r * a.cap;
+    } else if (x < 2 * R) {
+        r = x - R;
+        if (!a.ema) return;
+        row = reinterpret_cast<uint32_t *>(a.ema) + r * a.cap;
+    } else {  // vnorm [layers][batch][kv_heads][cap]
+        x -= 2 * R;
+        const int b = (int)(x / a.kv_heads % a.batch), g = (int)(x % a.kv_heads);
+        r = a.rows_per_seq == 1 ? b : (int64_t)b * a.rows_per_seq + g;
+        row = reinterpret_cast<uint32_t *>(a.vnorm) + x * a.cap;
+    }
+    const int n = min(keep_len[r], a.cap);
+    const int32_t *k = keep + r * a.cap;
+    for (int j0 = 0; j0 < n; j0 += kCopyThreads * U) {
+        uint32_t v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * kCopyThreads + threadIdx.x;
+            const int from = j < n ? k[j] : 0;
+            v[u] = from >= 0 && from < a.cap ? row[from] : 0u;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * kCopyThreads + threadIdx.x;
+            if (j < n) row[j] = v[u];
+        }
+    }
+}
 __global__ void __launch_bounds__(kCopyThreads, 4)
-compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int pages_at_once) {
+compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int pages_at_once,
+                    int n_rows) {
     pdl_wait();
     __shared__ RowMove moves[kRowsAtOnce];
+    if ((int)blockIdx.x < n_rows) {  // beside the copies
+        if (w.total[1]) gather_in_place(a, keep, keep_len, blockIdx.x);
+        return;
+    }
     const int jobs = w.total[0];
     // heads that share their moves: all, or with a keep row for each KV head one
     const int heads = a.rows_per_seq == 1 ? a.kv_heads : 1;
     const int groups = (jobs + pages_at_once - 1) / pages_at_once, parts = a.kv_heads / heads;
     const int64_t items = (int64_t)groups * a.layers * parts;
-    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    for (int64_t it = (int)blockIdx.x - n_rows; it < items; it += (int)gridDim.x - n_rows) {
         const int g0 = (int)(it % parts);
         const int l = (int)(it / parts % a.layers), job0 = (int)(it / parts / a.layers) * pages_at_once;
         const int pages = min(pages_at_once, jobs - job0);
@@ -413,62 +456,21 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
     }
 }
 
-// After the copies.  CTAs [0, batch): the sequence's table, its pages' counts and its length; the
-// others gather a row of pos, ema or vnorm in place: keep[j] >= j, so a run of slots is read
-// before it is written, and no later run is read from it.
-__global__ void __launch_bounds__(kRowThreads)
-compact_commit_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len) {
+// After the copies: a CTA a sequence, its table, its pages' counts and its length.
+__global__ void __launch_bounds__(kRowThreads) compact_commit_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep_len) {
     pdl_wait();
-    if (!w.total[1]) return;
-    if ((int)blockIdx.x < a.batch) {
-        const int b = blockIdx.x, begin = w.begin[b], base = w.base[b], made = w.base[b + 1] - base;
-        if (begin >= a.max_pages && keep_len[(int64_t)b * a.rows_per_seq] < 0) return;
-        for (int lp = begin + threadIdx.x; lp < a.max_pages; lp += kRowThreads) {
-            int32_t *entry = a.table + (int64_t)b * a.max_pages + lp;
-            const int e = *entry;
-            if (e > 0 && e < a.num_pages) atomicSub(a.refs + e, 1);
-            const int to = lp - begin < made ? w.free_ids[base + lp - begin] : 0;
-            if (to) a.refs[to] = 1;
-            *entry = to;
-        }
-        if (threadIdx.x == 0) a.len[b] = min(keep_len[(int64_t)b * a.rows_per_seq], a.cap);
-        return;
+    const int b = blockIdx.x, n = keep_len[(int64_t)b * a.rows_per_seq];
+    const int begin = w.begin[b], base = w.base[b], made = w.base[b + 1] - base;
+    if (!w.total[1] || n < 0) return;
+    for (int lp = begin + threadIdx.x; lp < a.max_pages; lp += kRowThreads) {
+        int32_t *entry = a.table + (int64_t)b * a.max_pages + lp;
+        const int e = *entry;
+        if (e > 0 && e < a.num_pages) atomicSub(a.refs + e, 1);
+        const int to = lp - begin < made ? w.free_ids[base + lp - begin] : 0;
+        if (to) a.refs[to] = 1;
+        *entry = to;
     }
-    constexpr int U = 8;
-    int64_t x = blockIdx.x - a.batch;
-    const int64_t R = (int64_t)a.batch * a.rows_per_seq;
-    int64_t r = x;
-    uint32_t *row;  // 4-byte values whatever they are
-    if (x < R) {
-        if (!a.pos) return;
-        row = reinterpret_cast<uint32_t *>(a.pos) + r * a.cap;
-    } else if (x < 2 * R) {
-        r = x - R;
-        if (!a.ema) return;
-        row = reinterpret_cast<uint32_t *>(a.ema) + r * a.cap;
-    } else {  // vnorm [layers][batch][kv_heads][cap]
-        x -= 2 * R;
-        const int b = (int)(x / a.kv_heads % a.batch), g = (int)(x % a.kv_heads);
-        r = a.rows_per_seq == 1 ? b : (int64_t)b * a.rows_per_seq + g;
-        row = reinterpret_cast<uint32_t *>(a.vnorm) + x * a.cap;
-    }
-    const int n = min(keep_len[r], a.cap);
-    const int32_t *k = keep + r * a.cap;
-    for (int j0 = 0; j0 < n; j0 += kRowThreads * U) {
-        uint32_t v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = j0 + u * kRowThreads + threadIdx.x;
-            const int from = j < n ? k[j] : 0;
-            v[u] = from >= 0 && from < a.cap ? row[from] : 0u;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = j0 + u * kRowThreads + threadIdx.x;
-            if (j < n) row[j] = v[u];
-        }
-    }
+    if (threadIdx.x == 0) a.len[b] = min(n, a.cap);
 }
 
 }  // namespace
@@ -533,12 +535,13 @@ cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int
     const int at_once = a.page_size < kRowsAtOnce ? kRowsAtOnce / a.page_size : 1;
     const int64_t items = (int64_t)a.batch * a.max_pages * a.layers * (a.rows_per_seq == 1 ? 1 : a.kv_heads);
     const int64_t ctas = items < 8 * (int64_t)sms ? items : 8 * (int64_t)sms;
-    e = launch_k(compact_copy_kernel, dim3((unsigned)ctas), dim3(kCopyThreads), 0, st, a, w, keep, keep_len, at_once);
+    const int64_t rows = 2 * (int64_t)a.batch * a.rows_per_seq + (a.vnorm ? (int64_t)a.layers * a.batch * a.kv_heads : 0);
+    if (rows + ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    e = launch_k(compact_copy_kernel, dim3((unsigned)(rows + ctas)), dim3(kCopyThreads), 0, st, a, w, keep, keep_len, at_once,
+                 (int)rows);
     note_launch();
     if (e != cudaSuccess) return e;
-    const int64_t rows = (int64_t)a.batch * a.rows_per_seq;
-    const int64_t all = a.batch + 2 * rows + (a.vnorm ? (int64_t)a.layers * a.batch * a.kv_heads : 0);
-    e = launch_k(compact_commit_kernel, dim3((unsigned)all), dim3(kRowThreads), 0, st, a, w, keep, keep_len);
+    e = launch_k(compact_commit_kernel, dim3((unsigned)a.batch), dim3(kRowThreads), 0, st, a, w, keep_len);
     note_launch();
     return e;
 }
