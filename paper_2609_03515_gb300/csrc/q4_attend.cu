@@ -206,7 +206,7 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
 // that follows the largest scale seen, they stay within fp16's range.
 // The softmax runs on a reference that is at most 2^6 below the largest logit, so the sums are
 // rescaled a few times a sequence and no tile waits for a maximum across lanes.
-template <int D, typename T, bool SCORE>
+template <int D, typename T, bool SCORE, bool DUAL>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q4AttendArgs a) {
     constexpr int Y = D / kQ4Group;        // groups of a row
     constexpr int NP = sizeof(T) == 4 ? 2 : 1;  // fp16 terms of q and of the probabilities
@@ -329,17 +329,19 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
     const int L = sp.L, S = sp.S, tile0 = sp.tile0;
     const int64_t head0 = (int64_t)sg.b * a.q_heads + (int64_t)sg.kv * G;
 
-    // q: lane (g, t) holds head g's channels 32 y + 8 t .. + 7
-    uint32_t q[NP][Y][4];
-    float post[2];  // what turns the mma's sums into log2-domain logits, heads 2 t and 2 t + 1
+    // q: lane (g, t) holds channels 32 y + 8 t .. + 7 of its column's head; DUAL: the first tile's
+    // operand, with columns 4 to 7 zero, and the second's
+    uint32_t q[DUAL ? 2 : 1][NP][Y][4];
+    float post[2];  // what turns the mma's sums into log2-domain logits, columns 2 t and 2 t + 1
     {
         float x[Y][8], m = 0.f;
-        const T *src = static_cast<const T *>(a.q) + (head0 + g) * D + 8 * t;
+        const int head = DUAL ? g & 3 : g;
+        const T *src = static_cast<const T *>(a.q) + (head0 + head) * D + 8 * t;
 #pragma unroll
         for (int y = 0; y < Y; ++y) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[y][e] = 0.f;
-            if (g < G) {
+            if (head < G) {
                 if (NP == 1) {
                     const uint4 w = *reinterpret_cast<const uint4 *>(src + 32 * y);
                     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -372,10 +374,17 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float lo = x[y][2 * i] * up, hi = x[y][2 * i + 1] * up;
-                q[0][y][i] = pack_half(lo, hi);
+                q[0][0][y][i] = pack_half(lo, hi);
                 if (NP == 2) {
-                    const float2 f = unpack_half(q[0][y][i]);
-                    q[NP - 1][y][i] = pack_half(lo - f.x, hi - f.y);
+                    const float2 f = unpack_half(q[0][0][y][i]);
+                    q[0][NP - 1][y][i] = pack_half(lo - f.x, hi - f.y);
+                }
+                if constexpr (DUAL) {
+#pragma unroll
+                    for (int n = 0; n < NP; ++n) {
+                        q[1][n][y][i] = g < 4 ? 0u : q[0][n][y][i];
+                        q[0][n][y][i] = g < 4 ? q[0][n][y][i] : 0u;
+                    }
                 }
             }
         const float mine = a.scale_log2 * ldexpf(1.f, e - 7);
@@ -383,11 +392,12 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
         post[1] = __shfl_sync(0xffffffffu, mine, 8 * t + 4);
     }
 
-    // where the logits of heads 2 t and 2 t + 1 go, by cache slot
-    float *const lg = SCORE ? a.logits + (head0 + 2 * t) * a.lstride : nullptr;
-    const bool lg0 = 2 * t < G, lg1 = 2 * t + 1 < G;
+    // where the logits of columns 2 t and 2 t + 1 go, by cache slot
+    const int col = DUAL ? 2 * (t & 1) : 2 * t;  // their heads: col, col + 1
+    float *const lg = SCORE ? a.logits + (head0 + col) * a.lstride : nullptr;
+    const bool lg0 = col < G, lg1 = col + 1 < G;
 
-    float o[2 * Y][4];  // O^T of channels 32 y + 4 g + 2 h (+ 1), heads 2 t, 2 t + 1
+    float o[2 * Y][4];  // O^T of channels 32 y + 4 g + 2 h (+ 1), columns 2 t, 2 t + 1
 #pragma unroll
     for (int i = 0; i < 2 * Y; ++i)
 #pragma unroll
@@ -397,95 +407,108 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
     float norm_e = 0.f, room = -1.f;
 
     const int tok0 = perm_of_row(g);  // tokens of rows g and g + 8: tok0, tok0 + 8
-    // One pair of tiles; MASK: some of its slots are not the sequence's, or dead
+    // One pair of tiles; MASK: some of its slots are not the sequence's, or dead.  A lane's columns
+    // belong to both tiles one after the other (NZ = 2 sets of logits), or DUAL to one of them.
+    constexpr int NZ = DUAL ? 1 : kPair;
+    const int my_tile = DUAL ? t >> 1 : 0;
     auto pair_step = [&](const Tile<D> *tiles, int slot0, auto mask_tag) {
         constexpr bool MASK = decltype(mask_tag)::value;
         // ---- logits
-        float z[kPair][4];
-        bool in[kPair][2];
+        float z[NZ][4];
+        bool in[NZ][2];
+        uint32_t kw[kPair][2][D / 32];  // rows g, g + 8: two units
 #pragma unroll
-        for (int u = 0; u < kPair; ++u) {
-            const Tile<D> &s = tiles[u];
-            uint32_t kw[2][D / 32];  // rows g, g + 8: two units
-            if (D == 128) {
-                *reinterpret_cast<uint4 *>(kw[0]) = *reinterpret_cast<const uint4 *>(s.k + g * Tile<D>::kRow + t * 16);
-                *reinterpret_cast<uint4 *>(kw[1]) = *reinterpret_cast<const uint4 *>(s.k + (g + 8) * Tile<D>::kRow + t * 16);
-            } else {
-                *reinterpret_cast<uint2 *>(kw[0]) = *reinterpret_cast<const uint2 *>(s.k + g * Tile<D>::kRow + t * 8);
-                *reinterpret_cast<uint2 *>(kw[1]) = *reinterpret_cast<const uint2 *>(s.k + (g + 8) * Tile<D>::kRow + t * 8);
+        for (int u = 0; u < kPair; ++u)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const unsigned char *row = tiles[u].k + (g + 8 * r) * Tile<D>::kRow + t * (D / 8);
+                if (D == 128) *reinterpret_cast<uint4 *>(kw[u][r]) = *reinterpret_cast<const uint4 *>(row);
+                else *reinterpret_cast<uint2 *>(kw[u][r]) = *reinterpret_cast<const uint2 *>(row);
             }
-            uint32_t sc[2][Y / 2];
+        uint32_t sc[NZ][2][Y / 2];
+#pragma unroll
+        for (int v = 0; v < NZ; ++v)
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
                 for (int y = 0; y < Y / 2; ++y)
-                    sc[r][y] = reinterpret_cast<const uint32_t *>(s.ks + (tok0 + 8 * r) * Tile<D>::kScaleRow)[y];
+                    sc[v][r][y] = reinterpret_cast<const uint32_t *>(tiles[v + my_tile].ks + (tok0 + 8 * r) * Tile<D>::kScaleRow)[y];
 #pragma unroll
-            for (int y = 0; y < Y; ++y) {
-                float c[4];
+        for (int y = 0; y < Y; ++y) {
+            float c[NZ][4];
+#pragma unroll
+            for (int u = 0; u < kPair; ++u)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     // unit 2 t + h: words h * Y / 2 ..; group y's two bytes
                     const int w = h * (Y / 2) + (y >> 1), byte = 2 * (y & 1);
-                    const uint32_t f[4] = {e2m1_bits(kw[0][w], byte), e2m1_bits(kw[1][w], byte),
-                                           e2m1_bits(kw[0][w], byte + 1), e2m1_bits(kw[1][w], byte + 1)};
+                    const uint32_t f[4] = {e2m1_bits(kw[u][0][w], byte), e2m1_bits(kw[u][1][w], byte),
+                                           e2m1_bits(kw[u][0][w], byte + 1), e2m1_bits(kw[u][1][w], byte + 1)};
+                    const auto &qu = q[DUAL ? u : 0];
+                    float(&cu)[4] = c[DUAL ? 0 : u];
 #pragma unroll
                     for (int n = 0; n < NP; ++n)
-                        if (h == 0 && n == 0) mma16816_first(c, f, q[n][y][2 * h], q[n][y][2 * h + 1]);
-                        else mma16816(c, f, q[n][y][2 * h], q[n][y][2 * h + 1]);
+                        if (h == 0 && n == 0 && !(DUAL && u > 0)) mma16816_first(cu, f, qu[n][y][2 * h], qu[n][y][2 * h + 1]);
+                        else mma16816(cu, f, qu[n][y][2 * h], qu[n][y][2 * h + 1]);
                 }
-                const float s0 = (y & 1) ? bf16_hi(sc[0][y >> 1]) : bf16_lo(sc[0][y >> 1]);
-                const float s1 = (y & 1) ? bf16_hi(sc[1][y >> 1]) : bf16_lo(sc[1][y >> 1]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) z[u][e] = y == 0 ? (e < 2 ? s0 : s1) * c[e] : z[u][e] + (e < 2 ? s0 : s1) * c[e];
-            }
+            for (int v = 0; v < NZ; ++v) {
+                const float s0 = (y & 1) ? bf16_hi(sc[v][0][y >> 1]) : bf16_lo(sc[v][0][y >> 1]);
+                const float s1 = (y & 1) ? bf16_hi(sc[v][1][y >> 1]) : bf16_lo(sc[v][1][y >> 1]);
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int j = slot0 + u * kQ4Tile + 8 * r + tok0;  // cache slot of row g + 8 r
-                const bool have = !MASK || (j >= 0 && j < L);
-                in[u][r] = have && (!MASK || !pos || s.pos[tok0 + 8 * r] >= 0);
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (!in[u][r]) z[u][2 * r + c] = -INFINITY;
-                if (SCORE && have) {
-                    if (lg0) lg[j] = z[u][2 * r] * post[0];
-                    if (lg1) lg[j + a.lstride] = z[u][2 * r + 1] * post[1];
-                }
+                for (int e = 0; e < 4; ++e)
+                    z[v][e] = y == 0 ? (e < 2 ? s0 : s1) * c[v][e] : z[v][e] + (e < 2 ? s0 : s1) * c[v][e];
             }
         }
+#pragma unroll
+        for (int v = 0; v < NZ; ++v)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int j = slot0 + (v + my_tile) * kQ4Tile + 8 * r + tok0;  // cache slot of row g + 8 r
+                const bool have = !MASK || (j >= 0 && j < L);
+                in[v][r] = have && (!MASK || !pos || tiles[v + my_tile].pos[tok0 + 8 * r] >= 0);
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (!in[v][r]) z[v][2 * r + c] = -INFINITY;
+                if (SCORE && have) {
+                    if (lg0) lg[j] = z[v][2 * r] * post[0];
+                    if (lg1) lg[j + a.lstride] = z[v][2 * r + 1] * post[1];
+                }
+            }
         // ---- V scales of rows g and g + 8 (0 where the slot is none of the sequence's, whatever it holds)
-        uint32_t sv[kPair][2][Y / 2];
+        uint32_t sv[NZ][2][Y / 2];
         float big = 0.f;
 #pragma unroll
-        for (int u = 0; u < kPair; ++u)
+        for (int v = 0; v < NZ; ++v)
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
                 for (int y = 0; y < Y / 2; ++y) {
-                    const uint32_t w = reinterpret_cast<const uint32_t *>(tiles[u].vs + (tok0 + 8 * r) * Tile<D>::kScaleRow)[y];
-                    sv[u][r][y] = in[u][r] ? w : 0u;
-                    big = max3(big, bf16_lo(sv[u][r][y]), bf16_hi(sv[u][r][y]));
+                    const uint32_t w =
+                        reinterpret_cast<const uint32_t *>(tiles[v + my_tile].vs + (tok0 + 8 * r) * Tile<D>::kScaleRow)[y];
+                    sv[v][r][y] = in[v][r] ? w : 0u;
+                    big = max3(big, bf16_lo(sv[v][r][y]), bf16_hi(sv[v][r][y]));
                 }
         // ---- running reference of the logits, norm of the scales; a weight is 2^(logit - less)
-        float less[2] = {ref[0] - norm_e, ref[1] - norm_e}, d[kPair][4], over = -FLT_MAX;
+        float less[2] = {ref[0] - norm_e, ref[1] - norm_e}, d[NZ][4], over = -FLT_MAX;
         auto weigh = [&]() {
 #pragma unroll
-            for (int u = 0; u < kPair; ++u)
+            for (int v = 0; v < NZ; ++v)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) d[u][e] = fmaf(z[u][e], post[e & 1], -less[e & 1]);
+                for (int e = 0; e < 4; ++e) d[v][e] = fmaf(z[v][e], post[e & 1], -less[e & 1]);
         };
         weigh();
 #pragma unroll
-        for (int u = 0; u < kPair; ++u)
+        for (int v = 0; v < NZ; ++v)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) over = max3(over, d[u][c], d[u][2 + c]);
+            for (int c = 0; c < 2; ++c) over = max3(over, d[v][c], d[v][2 + c]);
         if (__any_sync(0xffffffffu, over > kMaxSlack + norm_e || big > room)) {
             float f[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 float m = -INFINITY;
 #pragma unroll
-                for (int u = 0; u < kPair; ++u) m = max3(m, z[u][c], z[u][2 + c]);
+                for (int v = 0; v < NZ; ++v) m = max3(m, z[v][c], z[v][2 + c]);
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
                 m = fmaxf(ref[c], m * post[c]);
@@ -516,15 +539,18 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
             }
             weigh();
         }
+        float p[NZ][4];
 #pragma unroll
-        for (int u = 0; u < kPair; ++u) {
-            float p[4];
+        for (int v = 0; v < NZ; ++v) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = exp2_fast(d[u][e]);
+            for (int e = 0; e < 4; ++e) p[v][e] = exp2_fast(d[v][e]);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) sum[c] += p[c] + p[2 + c];
-            // ---- outputs
-            uint32_t vw[4][Y / 2];  // unit g of tokens t, 4 + t, 8 + t, 12 + t
+            for (int c = 0; c < 2; ++c) sum[c] += p[v][c] + p[v][2 + c];
+        }
+        // ---- outputs
+        // unit g of tokens t, 4 + t, 8 + t, 12 + t: bytes with a channel's codes of two tokens, the
+        // even channels in x[0], the odd ones in x[1]
+        auto load_v = [&](int u, uint32_t(&vw)[4][Y / 2]) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const unsigned char *row = tiles[u].v + (4 * j + t) * Tile<D>::kRow;
@@ -533,40 +559,82 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
                 else
                     vw[j][0] = *reinterpret_cast<const uint32_t *>(row + g * 4);
             }
+        };
+        auto mix_v = [&](const uint32_t(&vw)[4][Y / 2], int y2, uint32_t(&x)[2][2]) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t lo = vw[2 * j][y2], hi = vw[2 * j + 1][y2];
+                x[j][0] = (lo & 0x0f0f0f0fu) | ((hi << 4) & 0xf0f0f0f0u);
+                x[j][1] = ((lo >> 4) & 0x0f0f0f0fu) | (hi & 0xf0f0f0f0u);
+            }
+        };
+        // P^T times the scales of group 2 y2 + yy, as an mma's second operand
+        auto weights = [&](int v, int y2, int yy, uint32_t(&bf)[NP][2]) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float f = yy ? bf16_hi(sv[v][r][y2]) : bf16_lo(sv[v][r][y2]);
+                const float w0 = p[v][2 * r] * f, w1 = p[v][2 * r + 1] * f;
+                const uint32_t w = pack_half(w0, w1);
+                bf[0][r] = transpose8x8(w);
+                if (NP == 2) {
+                    const float2 back = unpack_half(w);
+                    bf[NP - 1][r] = transpose8x8(pack_half((w0 - back.x) * kLowUp, (w1 - back.y) * kLowUp));
+                }
+            }
+        };
+        auto add_v = [&](const uint32_t(&x)[2][2], int y2, int yy, int h, const uint32_t(&bf)[NP][2]) {
+            float(&to)[4] = o[2 * (2 * y2 + yy) + h];
+            const int byte = 2 * yy + h;
+            const uint32_t f[4] = {e2m1_bits(x[0][0], byte), e2m1_bits(x[0][1], byte), e2m1_bits(x[1][0], byte),
+                                   e2m1_bits(x[1][1], byte)};
+            mma16816(to, f, bf[0][0], bf[0][1]);
+            if (NP == 2) {
+                const uint32_t low[4] = {shrink(f[0]), shrink(f[1]), shrink(f[2]), shrink(f[3])};
+                mma16816(to, low, bf[NP - 1][0], bf[NP - 1][1]);
+            }
+        };
+        if constexpr (DUAL) {
+            uint32_t vw[kPair][4][Y / 2];
+#pragma unroll
+            for (int u = 0; u < kPair; ++u) load_v(u, vw[u]);
+            const uint32_t keep = g < 4 ? 0xffffffffu : 0u;  // columns of the first tile
 #pragma unroll
             for (int y2 = 0; y2 < Y / 2; ++y2) {
-                // bytes with a channel's codes of two tokens: the even channels, the odd ones
-                uint32_t x[2][2];
+                uint32_t x[kPair][2][2];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t lo = vw[2 * j][y2], hi = vw[2 * j + 1][y2];
-                    x[j][0] = (lo & 0x0f0f0f0fu) | ((hi << 4) & 0xf0f0f0f0u);
-                    x[j][1] = ((lo >> 4) & 0x0f0f0f0fu) | (hi & 0xf0f0f0f0u);
-                }
+                for (int u = 0; u < kPair; ++u) mix_v(vw[u], y2, x[u]);
 #pragma unroll
                 for (int yy = 0; yy < 2; ++yy) {
-                    uint32_t bf[NP][2];
+                    uint32_t bf[kPair][NP][2];
+                    weights(0, y2, yy, bf[0]);
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const float f = yy ? bf16_hi(sv[u][r][y2]) : bf16_lo(sv[u][r][y2]);
-                        const float w0 = p[2 * r] * f, w1 = p[2 * r + 1] * f;
-                        const uint32_t w = pack_half(w0, w1);
-                        bf[0][r] = transpose8x8(w);
-                        if (NP == 2) {
-                            const float2 back = unpack_half(w);
-                            bf[NP - 1][r] = transpose8x8(pack_half((w0 - back.x) * kLowUp, (w1 - back.y) * kLowUp));
-                        }
-                    }
+                    for (int n = 0; n < NP; ++n)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int y = 2 * y2 + yy, byte = 2 * yy + h;
-                        const uint32_t f[4] = {e2m1_bits(x[0][0], byte), e2m1_bits(x[0][1], byte), e2m1_bits(x[1][0], byte),
-                                               e2m1_bits(x[1][1], byte)};
-                        mma16816(o[2 * y + h], f, bf[0][0], bf[0][1]);
-                        if (NP == 2) {
-                            const uint32_t low[4] = {shrink(f[0]), shrink(f[1]), shrink(f[2]), shrink(f[3])};
-                            mma16816(o[2 * y + h], low, bf[NP - 1][0], bf[NP - 1][1]);
+                        for (int r = 0; r < 2; ++r) {
+                            bf[1][n][r] = bf[0][n][r] & ~keep;
+                            bf[0][n][r] &= keep;
                         }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int u = 0; u < kPair; ++u) add_v(x[u], y2, yy, h, bf[u]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < kPair; ++u) {
+                uint32_t vw[4][Y / 2];
+                load_v(u, vw);
+#pragma unroll
+                for (int y2 = 0; y2 < Y / 2; ++y2) {
+                    uint32_t x[2][2];
+                    mix_v(vw, y2, x);
+#pragma unroll
+                    for (int yy = 0; yy < 2; ++yy) {
+                        uint32_t bf[NP][2];
+                        weights(u, y2, yy, bf);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) add_v(x, y2, yy, h, bf);
                     }
                 }
             }
@@ -615,17 +683,20 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
     __syncthreads();
     for (int i = threadIdx.x; i < G * (D / 4); i += kThreads) {
         const int h = i / (D / 4), e = i % (D / 4) * 4;
+        // its columns: one a warp, or two that took turns
+        constexpr int kParts = DUAL ? 2 * kWarps : kWarps;
+        auto part = [&](int w) { return DUAL ? (w >> 1) * 8 + 4 * (w & 1) + h : w * 8 + h; };
         float m = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) m = fmaxf(m, ml[w * 8 + h].x);
+        for (int w = 0; w < kParts; ++w) m = fmaxf(m, ml[part(w)].x);
         const float base = m == -INFINITY ? 0.f : m;
         float l = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float2 y = ml[w * 8 + h];
+        for (int w = 0; w < kParts; ++w) {
+            const float2 y = ml[part(w)];
             const float f = exp2f(y.x - base);
-            const float4 v = *reinterpret_cast<const float4 *>(po + (w * 8 + h) * D + e);
+            const float4 v = *reinterpret_cast<const float4 *>(po + part(w) * D + e);
             l += f * y.y;
             x.x += f * v.x;
             x.y += f * v.y;
@@ -878,7 +949,11 @@ __global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4Finis
 template <int D, typename T>
 cudaError_t launch_t(const Q4AttendArgs &a, int ctas, cudaStream_t st) {
     constexpr size_t smem = kJoinBytes<D> + sizeof(Tile<D>) * kPair * kStages * kWarps;
-    auto kernel = a.logits ? q4_attend_kernel<D, T, true> : q4_attend_kernel<D, T, false>;
+    // two tiles share the columns of a group of 4 or fewer, where the registers hold q for both
+    constexpr bool kDual = sizeof(T) * D <= 256;
+    const bool dual = kDual && a.q_heads <= 4 * a.pv.kv_heads;
+    auto kernel = dual ? (a.logits ? q4_attend_kernel<D, T, true, kDual> : q4_attend_kernel<D, T, false, kDual>)
+                       : (a.logits ? q4_attend_kernel<D, T, true, false> : q4_attend_kernel<D, T, false, false>);
     if (smem > 48 << 10) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
