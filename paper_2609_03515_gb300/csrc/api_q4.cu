@@ -177,8 +177,8 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     a.part_o = at<float>(ws, w.part_o);
     a.lse2 = at<float>(ws, w.lse2);
     a.segs = at<int32_t>(ws, w.arrivals);
-    // (the kernels count the sequences' pairs of tiles in 32 bits)
-    if ((int64_t)shape->batch * shape->kv_heads * (a.cap / 32 + 1) > 0x7fffffff)
+    // (the kernels count the sequences' pairs of tiles in 32 bits, with some to spare for each unit)
+    if ((int64_t)shape->batch * shape->kv_heads * (a.cap / 32 + 64) > 0x30000000)
         return report(IKV_ERR_SHAPE, "batch * kv_heads * cap too large");
     // (and name a pool's tiles in 32 bits)
     if ((uint64_t)shape->layers * shape->kv_heads * cache->num_pages * (cache->page_size / kQ4Tile) > 0xffffffffu)

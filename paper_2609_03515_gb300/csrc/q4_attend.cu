@@ -123,13 +123,13 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
     __shared__ int sums[kWarps], counts[kWarps], tops[kWarps], lows[kWarps], found[2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int each = (a.batch + kThreads - 1) / kThreads, b0 = threadIdx.x * each, b1 = min(b0 + each, a.batch);
-    int mine = 0, n_mine = 0, top = 0, low = INT_MAX;
+    int mine = 0, n_mine = 0, top = 0, low = INT_MAX, pairs = 0;
     for (int b = b0; b < b1; ++b) {
-        const int n = span_of(a, b).pairs;
-        mine += n;
-        n_mine += n > 0;
-        top = max(top, n);
-        if (n > 0) low = min(low, n);
+        pairs = span_of(a, b).pairs;
+        mine += pairs;
+        n_mine += pairs > 0;
+        top = max(top, pairs);
+        if (pairs > 0) low = min(low, pairs);
     }
     int scan = mine, n_scan = n_mine;
 #pragma unroll
@@ -166,12 +166,13 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
     // (a unit of kMaxSplits - 2 whole runs at most: it may begin and end inside two more)
     const int least = (top + kMaxSplits - 3) / (kMaxSplits - 2);
     Run run;
-    run.per = max(max((int)(((int64_t)total * kvh + (int64_t)units * kSwitch + ctas - 1) / ctas), least), 1);
+    run.per = max(max((total * kvh + units * kSwitch + ctas - 1) / ctas, least), 1);
     run.whole = 0;
     if (top == low && units <= ctas) {
         // units of one length, cut evenly, each into runs of its own, if that makes them no longer
-        const int cut = max((top + ctas / units - 1) / (ctas / units), least);
-        const int even = (cut + kWarps - 1) / kWarps * kWarps;
+        const int each_unit = ctas / units, cut = max((top + each_unit - 1) / each_unit, least);
+        // (a few pairs: as many for every warp)
+        const int even = cut > 2 * kWarps ? cut : (cut + kWarps - 1) / kWarps * kWarps;
         if (even <= run.per + kSwitch) {
             run.per = even;
             run.whole = (top + even - 1) / even * even;
@@ -180,8 +181,8 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
     base = run.whole ? n_base * run.whole : base + n_base * kSwitch;
     const int64_t x = (int64_t)blockIdx.x * run.per;
     for (int b = b0; b < b1; ++b) {
-        const int len = run.length(span_of(a, b).pairs);
-        if (x >= (int64_t)base * kvh && x < (int64_t)(base + len) * kvh) {
+        const int len = run.length(each == 1 ? pairs : span_of(a, b).pairs);
+        if (x >= base * kvh && x < (base + len) * kvh) {
             found[0] = b;
             found[1] = base;
         }
@@ -227,13 +228,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
     constexpr int kScalePieces = kQ4Tile * Tile<D>::kScaleRow / 16;  // 8 or 4
     constexpr uint32_t kStageBytes = kPair * sizeof(Tile<D>);
     const uint32_t ring_at = smem_u32(ring);
-    uint32_t to_k[kCopies], to_v[kCopies];
-#pragma unroll
-    for (int j = 0; j < kCopies; ++j) {
-        const int c = lane + 32 * j, tok = c / kPieces, piece = c % kPieces;
-        to_k[j] = offsetof(Tile<D>, k) + row_of_token(tok) * Tile<D>::kRow + piece * 16;
-        to_v[j] = offsetof(Tile<D>, v) + tok * Tile<D>::kRow + (D == 128 ? piece ^ (tok & 2) : piece) * 16;
-    }
+    // (its second piece of each lies 8 tokens on: the same distance in memory and in the ring)
+    const int c_tok = lane / kPieces, c_piece = lane % kPieces;
+    const uint32_t to_k = offsetof(Tile<D>, k) + row_of_token(c_tok) * Tile<D>::kRow + c_piece * 16;
+    const uint32_t to_v = offsetof(Tile<D>, v) + c_tok * Tile<D>::kRow + (D == 128 ? c_piece ^ (c_tok & 2) : c_piece) * 16;
+    const bool has_scale = lane < 16 && (lane & 7) < kScalePieces;
     const unsigned char *scales = reinterpret_cast<const unsigned char *>(lane < 8 ? a.ks : a.vs) + (lane & 7) * 16;
     const uint32_t to_s = (lane < 8 ? offsetof(Tile<D>, ks) : offsetof(Tile<D>, vs)) + (lane & 7) * 16;
 
@@ -247,9 +246,9 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
         sg.b = b;
         sg.kv = kv;
         sg.pairs = min(sp.pairs - pair, left);
-        const int64_t unit0 = (int64_t)before * kvh + (int64_t)kv * run.length(sp.pairs);
-        sg.seg0 = (int)(unit0 / run.per);
-        sg.segs = (int)((unit0 + sp.pairs - 1) / run.per) - sg.seg0 + 1;
+        const int unit0 = before * kvh + kv * run.length(sp.pairs);
+        sg.seg0 = unit0 / run.per;
+        sg.segs = (unit0 + sp.pairs - 1) / run.per - sg.seg0 + 1;
         left -= run.length(sp.pairs) - pair;
         if (threadIdx.x == 0 && pair == 0) a.segs[b * kvh + kv] = sg.segs;
         pos = a.pos ? a.pos + (int64_t)(a.rows_per_seq == 1 ? b : b * a.rows_per_seq + kv) * a.cap : nullptr;
@@ -283,23 +282,23 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
     auto issue = [&](int i, uint32_t stage) {
         if (i < mine) {
             if ((i & 15) == 0) places = place_of(2 * i + lane);
+            const uint32_t at_k = stage + to_k, at_v = stage + to_v, at_s = stage + to_s;
+            const bool both = tile_of(2 * i + 1) < last;
 #pragma unroll
             for (int u = 0; u < kPair; ++u) {
                 const uint32_t place = __shfl_sync(0xffffffffu, places, (2 * i + u) & 31);
-                const uint32_t dst = stage + u * sizeof(Tile<D>);
-                if (u > 0 && tile_of(2 * i + u) >= last) break;
+                if (u > 0 && !both) break;
                 const unsigned char *k = from_k + (uint64_t)place * (kQ4Tile * Tile<D>::kRow);
                 const unsigned char *v = from_v + (uint64_t)place * (kQ4Tile * Tile<D>::kRow);
 #pragma unroll
                 for (int j = 0; j < kCopies; ++j) {
-                    copy16(dst + to_k[j], k + j * 512);
-                    copy16(dst + to_v[j], v + j * 512);
+                    copy16(at_k + u * sizeof(Tile<D>) + j * 512, k + j * 512);
+                    copy16(at_v + u * sizeof(Tile<D>) + j * 512, v + j * 512);
                 }
-                if ((lane & 7) < kScalePieces && lane < 16)
-                    copy16(dst + to_s, scales + (uint64_t)place * (kQ4Tile * Tile<D>::kScaleRow));
-                else if (lane >= 16 && pos) {
+                if (has_scale) copy16(at_s + u * sizeof(Tile<D>), scales + (uint64_t)place * (kQ4Tile * Tile<D>::kScaleRow));
+                if (pos && lane >= 16) {
                     const int j = (sp.tile0 + tile_of(2 * i + u)) * kQ4Tile + lane - 16 - sp.S;
-                    if (j >= 0 && j < sp.L) copy4(dst + offsetof(Tile<D>, pos) + (lane - 16) * 4, pos + j);
+                    if (j >= 0 && j < sp.L) copy4(stage + u * sizeof(Tile<D>) + offsetof(Tile<D>, pos) + (lane - 16) * 4, pos + j);
                 }
             }
         }
