@@ -12,15 +12,21 @@ namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kPair = 2;              // tiles of an iteration
-constexpr int kStages = 3;            // pairs of tiles a warp has in flight or in use
+constexpr int kStages = 2;            // pairs of tiles a warp has in flight or in use
 constexpr int kCtasPerSm = 3;
 constexpr int kSwitch = 12;            // what going from one unit to the next costs a CTA, in pairs of tiles
 constexpr float kMaxSlack = 6.f;      // log2: how far a logit may lie above the running reference
 constexpr float kScaleRoom = 256.f;   // how far a V scale may grow, normalised, before it is renormalised
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// The cache is read once: it goes out of L2 before the logits and partials, which are read again.
+__device__ __forceinline__ uint64_t read_once_policy() {
+    uint64_t p;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t dst, const void *src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
@@ -278,6 +284,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
         return x < last ? (uint32_t)(a.pv.row_phys(sg.b, a.layer, sg.kv, (sp.tile0 + x) * kQ4Tile) / kQ4Tile) : 0u;
     };
     uint32_t places = 0;
+    const uint64_t policy = read_once_policy();
     const unsigned char *const from_k = a.k + lane * 16, *const from_v = a.v + lane * 16;
     auto issue = [&](int i, uint32_t stage) {
         if (i < mine) {
@@ -292,10 +299,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q
                 const unsigned char *v = from_v + (uint64_t)place * (kQ4Tile * Tile<D>::kRow);
 #pragma unroll
                 for (int j = 0; j < kCopies; ++j) {
-                    copy16(at_k + u * sizeof(Tile<D>) + j * 512, k + j * 512);
-                    copy16(at_v + u * sizeof(Tile<D>) + j * 512, v + j * 512);
+                    copy16(at_k + u * sizeof(Tile<D>) + j * 512, k + j * 512, policy);
+                    copy16(at_v + u * sizeof(Tile<D>) + j * 512, v + j * 512, policy);
                 }
-                if (has_scale) copy16(at_s + u * sizeof(Tile<D>), scales + (uint64_t)place * (kQ4Tile * Tile<D>::kScaleRow));
+                if (has_scale) copy16(at_s + u * sizeof(Tile<D>), scales + (uint64_t)place * (kQ4Tile * Tile<D>::kScaleRow), policy);
                 if (pos && lane >= 16) {
                     const int j = (sp.tile0 + tile_of(2 * i + u)) * kQ4Tile + lane - 16 - sp.S;
                     if (j >= 0 && j < sp.L) copy4(stage + u * sizeof(Tile<D>) + offsetof(Tile<D>, pos) + (lane - 16) * 4, pos + j);
