@@ -45,39 +45,47 @@ __device__ __forceinline__ int block_scan(int x, int *total) {
     return y - x + (warp ? sums[warp - 1] : 0);
 }
 
-// The lowest `want` free pages into ids, by one CTA; how many there are, at most `want`.
-__device__ int find_free(const int32_t *refs, int pages, int want, int32_t *ids) {
-    constexpr int U = 16;
-    const int lane = threadIdx.x & 31;
-    int found = 0;
-    for (int p0 = (threadIdx.x >> 5) * 32 * U; p0 - (int)(threadIdx.x >> 5) * 32 * U < pages && found < want;
-         p0 += kPlanThreads * U) {  // a warp takes 32 U pages behind one another
-        int32_t r[U];
+// The lowest free pages, by one CTA.  A pass looks at kPlanThreads x kPass pages, a warp at
+// 32 kPass behind one another; the first pass is loaded ahead of what says how many are wanted.
+struct FreePages {
+    static constexpr int kPass = 16;
+    const int32_t *refs;
+    int pages;
+    int32_t r[kPass];
+    __device__ __forceinline__ void load(int p0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int p = p0 + 32 * u + lane;
+        for (int u = 0; u < kPass; ++u) {
+            const int p = p0 + (threadIdx.x >> 5) * 32 * kPass + 32 * u + (threadIdx.x & 31);
             r[u] = p > 0 && p < pages ? __ldcg(refs + p) : 1;
         }
-        uint32_t free[U];
-        int mine = 0;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            free[u] = __ballot_sync(0xffffffffu, r[u] == 0);
-            mine += __popc(free[u]);
-        }
-        int n, at = block_scan(lane == 0 ? mine : 0, &n);
-        at = found + __shfl_sync(0xffffffffu, at, 0);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int to = at + __popc(free[u] & ((1u << lane) - 1));
-            if ((free[u] >> lane & 1u) && to < want) ids[to] = p0 + 32 * u + lane;
-            at += __popc(free[u]);
-        }
-        found += n;
     }
-    __syncthreads();
-    return min(found, want);
-}
+    // `want` of them into ids (which all threads may read then), after load(0); how many there are, at most `want`
+    __device__ __forceinline__ int find(int want, int32_t *ids) {
+        const int lane = threadIdx.x & 31, mine0 = (threadIdx.x >> 5) * 32 * kPass;
+        int found = 0;
+        for (int p0 = 0; p0 < pages && found < want; p0 += kPlanThreads * kPass) {
+            if (p0 > 0) load(p0);
+            uint32_t free[kPass];
+            int mine = 0;
+#pragma unroll
+            for (int u = 0; u < kPass; ++u) {
+                free[u] = __ballot_sync(0xffffffffu, r[u] == 0);
+                mine += __popc(free[u]);
+            }
+            int n, at = block_scan(lane == 0 ? mine : 0, &n);
+            at = found + __shfl_sync(0xffffffffu, at, 0);
+#pragma unroll
+            for (int u = 0; u < kPass; ++u) {
+                const int to = at + __popc(free[u] & ((1u << lane) - 1));
+                if ((free[u] >> lane & 1u) && to < want) ids[to] = p0 + mine0 + 32 * u + lane;
+                at += __popc(free[u]);
+            }
+            found += n;
+        }
+        __syncthreads();
+        return min(found, want);
+    }
+};
 
 __global__ void __launch_bounds__(kRowThreads) release_kernel(const PagesArgs a, int extra) {
     pdl_wait();
@@ -137,103 +145,125 @@ __global__ void __launch_bounds__(kRowThreads) fork_kernel(const PagesArgs a, co
 
 // One CTA decides which pages of the slots to be written are missing or shared, takes free ones for
 // them and lists the copies to make: {page, copy, first row, rows}.  Of the sequences of this call
-// that would write a shared page which nobody else holds, the last keeps it.
+// that would write a shared page which nobody else holds, the last keeps it.  A chain of round
+// trips to memory, and FEW (kFewRequests at most: single tokens) has the fewest: lengths, entries,
+// counts; the writers are counted in shared memory, and the free pages are looked for meanwhile.
+constexpr int kFewRequests = 256;
+template <bool FEW>
 __global__ void __launch_bounds__(kPlanThreads)
 writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, const int32_t *count, int max_count,
                      int span, int32_t *lacking) {
     pdl_wait();
+    __shared__ int32_t shared_pages[FEW ? kFewRequests : 1], ids_s[FEW ? kFewRequests : 1];
     const int64_t R = (int64_t)a.batch * span;
+    FreePages pages{a.refs, a.num_pages};
+    pages.load(0);
     // the entry of request i, or -1: page lp of sequence b
     auto request = [&](int64_t i, int *b, int *lp) -> int {
-        *b = (int)(i / span);
+        if (i >= R) return -1;
+        *b = FEW ? (int)i / span : (int)(i / span);
+        const int x = (int)(i - (int64_t)*b * span);
         const int n = min(count ? count[*b] : max_count, max_count);
-        const int64_t f = (int64_t)start_of(a, *b) + (first ? first[*b] : a.len[*b]);
-        if (n <= 0 || (first && first[*b] < 0)) return -1;
-        if (f + n > a.cap) {
-            if (i % span == 0) atomicOr(&g_pages_error, 4u);
+        const int from = first ? first[*b] : a.len[*b], S = start_of(a, *b);
+        if (n <= 0 || from < 0) return -1;
+        if ((int64_t)S + from + n > a.cap) {
+            if (x == 0) atomicOr(&g_pages_error, 4u);
             return -1;
         }
-        const int64_t p = f / a.page_size + i % span;
+        const int f = S + from, p = f / a.page_size + x;
         if (p > (f + n - 1) / a.page_size) return -1;
-        *lp = (int)p;
+        *lp = p;
         const int e = a.table[(int64_t)*b * a.max_pages + p];
         if (e >= 0 && e < a.num_pages) return e;
         atomicOr(&g_pages_error, 128u);
         return -1;
     };
-    // what a thread's request asks for is looked up once if there is one a thread (single tokens)
-    const bool once = R <= kPlanThreads;
-    int kb = 0, klp = 0;
-    const int ke = once && threadIdx.x < R ? request(threadIdx.x, &kb, &klp) : -1;
-    auto get = [&](int64_t i, int *b, int *lp) -> int {
-        if (!once) return i < R ? request(i, b, lp) : -1;
-        *b = kb;
-        *lp = klp;
-        return ke;
+    auto assign = [&](int b, int lp, int e, int to, int rank) {
+        a.table[(int64_t)b * a.max_pages + lp] = to;
+        a.refs[to] = 1;
+        // rows of the page that hold slots in use
+        const int64_t S = start_of(a, b), p0 = (int64_t)lp * a.page_size;
+        const int r0 = (int)min(max(S - p0, (int64_t)0), (int64_t)a.page_size);
+        const int r1 = (int)min(max(S + a.len[b] - p0, (int64_t)0), (int64_t)a.page_size);
+        *reinterpret_cast<int4 *>(w.jobs + 4 * (int64_t)rank) = make_int4(e, to, r0, e > 0 ? max(r1 - r0, 0) : 0);
     };
-    int b, lp;
-    for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
-        const int e = get(i, &b, &lp);
-        if (e > 0) {
-            w.count[e] = 0;
-            w.last[e] = -1;
+    auto report_total = [&](int total, int have) {
+        if (threadIdx.x == 0) {
+            w.total[0] = have == total ? total : 0;
+            if (lacking) *lacking = total - have;
+            if (have < total) atomicOr(&g_pages_error, 64u);
         }
-    }
-    __syncthreads();
-    for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
-        const int e = get(i, &b, &lp);
-        if (e > 0 && __ldcg(a.refs + e) > 1) {
-            atomicAdd(w.count + e, 1);
-            atomicMax(w.last + e, b);
-        }
-    }
-    __syncthreads();
-    auto needs = [&](int64_t i, int *b, int *lp, int *e) {
-        *e = get(i, b, lp);
-        if (*e <= 0) return *e == 0;
-        const int r = __ldcg(a.refs + *e), c = __ldcg(w.count + *e), last = __ldcg(w.last + *e);
-        return r > 1 && !(c == r && last == *b);
     };
-    int total = 0, e, rank = 0;
-    bool need = false;
-    for (int64_t i0 = 0; i0 < R; i0 += kPlanThreads) {
-        int n;
-        need = needs(i0 + threadIdx.x, &b, &lp, &e);
-        rank = block_scan(need ? 1 : 0, &n);
-        total += n;
-    }
-    const int have = find_free(a.refs, a.num_pages, total, w.free_ids);
-    if (threadIdx.x == 0) {
-        w.total[0] = have == total ? total : 0;
-        if (lacking) *lacking = total - have;
-        if (have < total) atomicOr(&g_pages_error, 64u);
-    }
-    if (have < total) return;
-    int done = 0;
-    for (int64_t i0 = 0; i0 < R; i0 += kPlanThreads) {
-        if (!once) {
+    int b = 0, lp = 0;
+    if constexpr (FEW) {
+        const int i = threadIdx.x, e = request(i, &b, &lp);
+        const int r = e > 0 ? __ldcg(a.refs + e) : 0;
+        if (i < kFewRequests) shared_pages[i] = r > 1 ? e : 0;
+        __syncthreads();
+        bool need = e == 0;
+        if (r > 1) {  // requests are in the order of the sequences
+            int writers = 0;
+            bool later = false;
+            for (int j = 0; j < (int)R; ++j)
+                if (shared_pages[j] == e) {
+                    ++writers;
+                    later |= j > i;
+                }
+            need = writers < r || later;
+        }
+        int total;
+        const int rank = block_scan(need ? 1 : 0, &total);
+        const int have = pages.find(total, ids_s);
+        report_total(total, have);
+        if (have < total || !need) return;
+        assign(b, lp, e, ids_s[rank], rank);
+        if (e > 0) atomicSub(a.refs + e, 1);  // (every count is read)
+    } else {
+        for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
+            const int e = request(i, &b, &lp);
+            if (e > 0) {
+                w.count[e] = 0;
+                w.last[e] = -1;
+            }
+        }
+        __syncthreads();
+        for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
+            const int e = request(i, &b, &lp);
+            if (e > 0 && __ldcg(a.refs + e) > 1) {
+                atomicAdd(w.count + e, 1);
+                atomicMax(w.last + e, b);
+            }
+        }
+        __syncthreads();
+        auto needs = [&](int64_t i, int *b, int *lp, int *e) {
+            *e = request(i, b, lp);
+            if (*e <= 0) return *e == 0;
+            const int r = __ldcg(a.refs + *e), c = __ldcg(w.count + *e), last = __ldcg(w.last + *e);
+            return r > 1 && !(c == r && last == *b);
+        };
+        int total = 0, e;
+        for (int64_t i0 = 0; i0 < R; i0 += kPlanThreads) {
             int n;
-            need = needs(i0 + threadIdx.x, &b, &lp, &e);
-            rank = done + block_scan(need ? 1 : 0, &n);  // (its barriers: everybody has read the counts)
+            block_scan(needs(i0 + threadIdx.x, &b, &lp, &e) ? 1 : 0, &n);
+            total += n;
+        }
+        const int have = pages.find(total, w.free_ids);
+        report_total(total, have);
+        if (have < total) return;
+        int done = 0;
+        for (int64_t i0 = 0; i0 < R; i0 += kPlanThreads) {
+            const bool need = needs(i0 + threadIdx.x, &b, &lp, &e);
+            int n;
+            const int rank = done + block_scan(need ? 1 : 0, &n);  // (its barriers: everybody has read the counts)
             done += n;
+            if (need) assign(b, lp, e, __ldcg(w.free_ids + rank), rank);
         }
-        if (need) {
-            const int to = __ldcg(w.free_ids + rank);
-            a.table[(int64_t)b * a.max_pages + lp] = to;
-            a.refs[to] = 1;
-            int32_t *job = w.jobs + 4 * (int64_t)rank;
-            // rows of the page that hold slots in use
-            const int64_t S = start_of(a, b), p0 = (int64_t)lp * a.page_size;
-            const int r0 = (int)min(max(S - p0, (int64_t)0), (int64_t)a.page_size);
-            const int r1 = (int)min(max(S + a.len[b] - p0, (int64_t)0), (int64_t)a.page_size);
-            *reinterpret_cast<int4 *>(job) = make_int4(e, to, r0, e > 0 ? max(r1 - r0, 0) : 0);
+        __syncthreads();
+        // the copied pages' holders go once no count is read any more
+        for (int64_t i = threadIdx.x; i < total; i += kPlanThreads) {
+            const int e = w.jobs[4 * i];
+            if (e > 0) atomicSub(a.refs + e, 1);
         }
-    }
-    __syncthreads();
-    // the copied pages' holders go once no count is read any more
-    for (int64_t i = threadIdx.x; i < total; i += kPlanThreads) {
-        const int e = w.jobs[4 * i];
-        if (e > 0) atomicSub(a.refs + e, 1);
     }
 }
 
@@ -276,6 +306,10 @@ __global__ void __launch_bounds__(kCopyThreads) writable_copy_kernel(const Pages
 __global__ void __launch_bounds__(kPlanThreads)
 compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int32_t *lacking) {
     pdl_wait();
+    __shared__ int32_t need_s[kPlanThreads];
+    int32_t *needs = a.batch <= kPlanThreads ? need_s : w.base;  // pages that a sequence makes anew
+    FreePages pages{a.refs, a.num_pages};
+    pages.load(0);
     const int lane = threadIdx.x & 31;
     for (int b = threadIdx.x >> 5; b < a.batch; b += kPlanThreads / 32) {
         const int64_t r0 = (int64_t)b * a.rows_per_seq;
@@ -298,23 +332,23 @@ compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
             }
             const int S = start_of(a, b), end = (S + n + a.page_size - 1) / a.page_size;
             begin = f == n ? end : (S + f) / a.page_size;
-            if (lane == 0) w.base[b] = end - begin;
+            if (lane == 0) needs[b] = end - begin;
         } else if (lane == 0) {
-            w.base[b] = 0;
+            needs[b] = 0;
         }
         if (lane == 0) w.begin[b] = begin;
     }
     __syncthreads();
     int total = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {
-        const int b = b0 + threadIdx.x, need = b < a.batch ? __ldcg(w.base + b) : 0;
+        const int b = b0 + threadIdx.x, need = b < a.batch ? needs[b] : 0;
         int n;
         const int at = total + block_scan(need, &n);
         if (b < a.batch) w.base[b] = at;
         total += n;
     }
     if (threadIdx.x == 0) w.base[a.batch] = total;
-    const int have = find_free(a.refs, a.num_pages, total, w.free_ids);
+    const int have = pages.find(total, w.free_ids);
     if (threadIdx.x == 0) {
         w.total[0] = have == total ? total : 0;
         w.total[1] = have == total;
@@ -516,8 +550,9 @@ cudaError_t launch_pages_writable(const PagesArgs &a, const PagesWs &w, const in
     // pages that max_count slots from anywhere in a page may touch
     const int64_t most = ((int64_t)max_count + a.page_size - 2) / a.page_size + 1;
     const int span = (int)(most < a.max_pages ? most : a.max_pages);
-    cudaError_t e = launch_k(writable_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, w, first, count, (int)max_count,
-                             span, lacking);
+    const bool few = (int64_t)a.batch * span <= kFewRequests;
+    cudaError_t e = launch_k(few ? writable_plan_kernel<true> : writable_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0,
+                             st, a, w, first, count, (int)max_count, span, lacking);
     note_launch();
     if (e != cudaSuccess) return e;
     const int64_t items = (int64_t)a.batch * span * a.layers * a.n_planes * a.kv_heads;
