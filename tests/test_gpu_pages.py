@@ -331,3 +331,38 @@ def test_free_pages_of_a_large_pool(pool):
     assert ikv.ikv_device_status() == 0
     assert c.block_table[0, :300].tolist() == free[:300] and int(c.block_table[1, 0]) == free[300]
     assert c.block_table[2, :250].tolist() == free[301:551] and int(c.refs.sum()) == pool + 1 - len(free) + 551
+
+
+@pytest.mark.parametrize("nb,idle", [(250, 0), (300, 0), (300, 3), (1100, 0)])
+def test_many_sequences_share_and_leave_a_page(nb, idle):
+    """More requests than one CTA plans in shared memory, and more sequences than it has threads: all
+    write a shared page (the last keeps it, or nobody while some are idle), then all are compacted."""
+    c = make("bf16", nb, 16, 64, 1, 0, [0] * nb, pool=3 * nb, cap=48, layers=1)
+    m, rng = Model(c), random.Random(nb)
+    ws = c.pages_workspace()
+    shape, cache, pages = c.shape(), c.cache(c.cap), c.pages()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    m.writable({0: (0, 20)})
+    ikv.ikv_pages_writable(shape, cache, pages, None, i32([20] + [0] * (nb - 1)), 20, None, ws, ws.numel())
+    m.compare()
+    m.write({0: (0, 20)}, rng)
+    m.fork([(0, b) for b in range(1, nb)])
+    ikv.ikv_pages_fork(shape, cache, pages, nb - 1, i32([0] * (nb - 1)), i32(list(range(1, nb))), c.ema)
+    m.compare()
+    who = {b: (20, 2) for b in range(nb - idle)}
+    m.writable(who)
+    ikv.ikv_pages_writable(shape, cache, pages, None, i32([2 if b in who else 0 for b in range(nb)]), 2, None, ws, ws.numel())
+    m.compare()
+    kept = c.block_table[:, 1].tolist().count(2)
+    assert kept == (1 if idle == 0 else idle) and c.block_table[0, 0] == 1 and int(c.refs[1]) == nb
+    m.write(who, rng)
+    keep, kp, kl = {}, torch.zeros(nb, c.cap, dtype=torch.int32), []
+    for b in range(nb):
+        n = rng.choice([17, 5, m.len[b]])
+        keep[b] = [sorted(rng.sample(range(m.len[b]), n))]
+        kp[b, :n] = torch.tensor(keep[b][0], dtype=torch.int32)
+        kl.append(n)
+    assert m.compact(keep) == 0
+    ikv.ikv_pages_compact(shape, cache, pages, kp.cuda(), i32(kl), c.ema, None, ws, ws.numel())
+    m.compare()
+    assert ikv.ikv_device_status() == 0

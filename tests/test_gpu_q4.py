@@ -390,3 +390,28 @@ def test_rows_past_four_gigabytes():
     assert ikv.ikv_device_status() == 0
     c.pos = torch.zeros(1, c.cap, dtype=torch.int32, device="cuda")
     check(c, 0, q, out, score, False, torch.ones(1, c.cap, dtype=torch.bool, device="cuda"))
+
+
+@pytest.mark.parametrize("lens,kvh,G,gran", [
+    ([(7 * i) % 41 for i in range(300)], 8, 4, 0),             # far more units than CTAs, some empty
+    ([33] * 200, 4, 7, 1),                                     # as many, of one length
+    ([600] * 9, 2, 2, 0),                                      # one length, cut evenly
+    ([3000] + [5 + i % 3 for i in range(140)], 2, 8, 0),       # one long among short, two a thread
+    ([0] * 130 + [1], 1, 1, 0)])
+def test_many_sequences(lens, kvh, G, gran):
+    """The deal of the work to the CTAs: batches larger than a CTA, units cut evenly and not."""
+    gen = torch.Generator(device="cuda").manual_seed(len(lens))
+    d, nb = 64, len(lens)
+    c = make(lens, kvh, G, d, 16, ikv.IKV_BF16, starts=[(3 * i) % 19 for i in range(nb)], layers=1, gran=gran, room=20)
+    noise(c, gen)
+    x = torch.randn(1, nb, max(lens), kvh, d, generator=gen, device="cuda").to(torch.bfloat16)
+    ikv.ikv_q4_store(c.shape(), c.cache(max(lens)), c.q4(), 0, 1, x, x.flip(2), c.dense_rows(x), torch.zeros_like(c.len), c.len,
+                     max(lens))
+    q = (2.0 * torch.randn(nb, G * kvh, d, generator=gen, device="cuda")).to(torch.bfloat16)
+    cch = c.cache(max(lens))
+    n = ikv.ikv_attend_workspace_size(c.shape(), cch)
+    ws = torch.full((n,), 0xAB, dtype=torch.uint8, device="cuda")
+    out, score = torch.full_like(q, 9.0), torch.full((c.rows, c.cap), -7.0, device="cuda")
+    ikv.ikv_q4_attend_score(c.shape(), cch, c.q4(), 0, q, out, score, None, 0.0, ws, n)
+    assert ikv.ikv_device_status() == 0
+    check(c, 0, q, out, score, False, torch.ones_like(c.pos, dtype=torch.bool))
