@@ -13,8 +13,10 @@ namespace {
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kPair = 2;              // tiles of an iteration
 constexpr int kStages = 2;            // pairs of tiles a warp has in flight or in use
-constexpr int kCtasPerSm = 3;
-constexpr int kSwitch = 12;            // what going from one unit to the next costs a CTA, in pairs of tiles
+// CTAs an SM holds: at 4, 128 channels have neither the registers nor the L1 that 3 leave (qwen-like
+// 32 x 16k: 56.9 us against 52.6), 64 channels of bf16 queries have both (groups of 4: 33.7 against 35.5)
+constexpr int ctas_per_sm(int head_dim, int elem_bytes) { return head_dim == 64 && elem_bytes == 2 ? 4 : 3; }
+constexpr int kSwitch = 12;           // what going from one unit to the next costs a CTA, in pairs of tiles
 constexpr float kMaxSlack = 6.f;      // log2: how far a logit may lie above the running reference
 constexpr float kScaleRoom = 256.f;   // how far a V scale may grow, normalised, before it is renormalised
 
@@ -214,7 +216,7 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
 // The softmax runs on a reference that is at most 2^6 below the largest logit, so the sums are
 // rescaled a few times a sequence and no tile waits for a maximum across lanes.
 template <int D, typename T, bool SCORE, bool DUAL>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) q4_attend_kernel(const Q4AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend_kernel(const Q4AttendArgs a) {
     constexpr int Y = D / kQ4Group;        // groups of a row
     constexpr int NP = sizeof(T) == 4 ? 2 : 1;  // fp16 terms of q and of the probabilities
     constexpr int kPieces = D / 32;        // 16-byte pieces of a row of codes
@@ -999,7 +1001,7 @@ int32_t q4_attend_ctas(const ikv_shape *s, int32_t max_len, int sms) {
     // a start offset may put the first slot anywhere in its tile
     constexpr int kSlots = kPair * kQ4Tile;
     const int64_t pairs = max_len > 0 ? ((int64_t)max_len + kQ4Tile - 1 + kSlots - 1) / kSlots : 1;
-    const int64_t ctas = (int64_t)s->batch * s->kv_heads * ((pairs + kWarps - 1) / kWarps), wave = (int64_t)sms * kCtasPerSm;
+    const int64_t ctas = (int64_t)s->batch * s->kv_heads * ((pairs + kWarps - 1) / kWarps), wave = (int64_t)sms * ctas_per_sm(s->head_dim, s->dtype == IKV_BF16 ? 2 : 4);
     return (int32_t)(ctas < wave ? ctas : wave);
 }
 
