@@ -509,7 +509,9 @@ ikv_status ikv_q4_append_token(const ikv_shape *shape, ikv_cache *cache, const i
 /* ikv_decode_attend_score over a 4-bit cache: out = softmax(q K^T / sqrt(d)) V over the values
  * that the codes stand for, score and ema as there, ws of ikv_attend_workspace_size() bytes.  A
  * sequence without a live slot gets out = 0.  Slots outside [0, len[b]) are never used, whatever
- * they hold. */
+ * they hold.  A NaN group of a live V row makes its 32 channels NaN for that KV head's queries, one
+ * of a live K row every channel.  Fails with IKV_ERR_SHAPE where batch * kv_heads * cap passes
+ * 2.5e10 slots or the pool 6.8e10 rows, and above 8192 query heads. */
 ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, const ikv_q4 *q4, int32_t layer,
                                const void *q, void *out, float *score, float *ema, float alpha, void *ws,
                                size_t ws_bytes, cudaStream_t stream);
@@ -522,7 +524,8 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
  * reads past a sequence's end may touch).  refs[p] counts the entries that hold page p; a page
  * with refs 0 is free.  The caller starts with every entry 0, refs[0] = 1 and the others 0, and
  * changes them only through these calls, which hand out the lowest free pages first, in the
- * order of sequences and slots.  All are asynchronous and may be captured in a graph.
+ * order of sequences and slots.  They write cache->block_table.  All are asynchronous and may be
+ * captured in a graph.
  * The planes are the arrays paged alike: K and V, and for a 4-bit cache both scale pools.
  * Writes into a page that several sequences hold reach them all: call ikv_pages_writable for the
  * slots that ikv_q4_store, ikv_append_token, ikv_step or ikv_compact_kv are about to write.
@@ -533,7 +536,8 @@ typedef struct {
     int32_t n_planes;            /* 1 .. IKV_MAX_PLANES */
     void *plane[IKV_MAX_PLANES]; /* [layers][num_pages][kv_heads][page_size][row_bytes] (device), 16-byte
                                     aligned */
-    int32_t row_bytes[IKV_MAX_PLANES]; /* bytes of a plane's row, a multiple of 4 */
+    int32_t row_bytes[IKV_MAX_PLANES]; /* bytes of a plane's row, a multiple of 4; a page of one KV head
+                                    holds at most 16 MB */
 } ikv_pages;
 
 ikv_status ikv_pages_workspace_size(const ikv_shape *shape, const ikv_cache *cache, const ikv_pages *pages,

@@ -60,6 +60,8 @@ class DecodeCache:
                  eviction): pos has batch * layers rows (row b * layers + l: layer l's positions)
                  and pos_state [batch][pos_cap] is the utility by token position
     budget:      [batch] int32
+    With pool_pages, sequences own no page at first: pool_pages pages (numbers 1 ..) are handed out by
+    the ikv_pages_* calls, refs [num_pages] counts their holders, and block_table entries of 0 mean none.
     """
 
     def __init__(self, batch: int, layers: int, q_heads: int, kv_heads: int, head_dim: int, cap_tokens: int,

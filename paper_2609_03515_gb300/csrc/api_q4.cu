@@ -63,7 +63,7 @@ ikv_status check_pages(const ikv_shape *s, const ikv_cache *c, const ikv_pages *
         if (!aligned16(p->plane[i])) return report(IKV_ERR_ALIGN, "planes must be 16-byte aligned");
         if (p->row_bytes[i] <= 0 || p->row_bytes[i] % 4)
             return report(IKV_ERR_SHAPE, "row_bytes must be positive multiples of 4");
-        if ((int64_t)p->row_bytes[i] * c->page_size > (int64_t)1 << 30) return report(IKV_ERR_SHAPE, "page too large");
+        if ((int64_t)p->row_bytes[i] * c->page_size > (int64_t)1 << 24) return report(IKV_ERR_SHAPE, "page too large");
         a->plane[i] = static_cast<unsigned char *>(p->plane[i]);
         a->row_bytes[i] = p->row_bytes[i];
     }
@@ -151,6 +151,7 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     if (!q || !out) return report(IKV_ERR_ARG, "q/out is NULL");
     if (!aligned16(q) || !aligned16(out)) return report(IKV_ERR_ALIGN, "q/out must be 16-byte aligned");
     if (ema && !(alpha >= 0.f && alpha <= 1.f)) return report(IKV_ERR_ARG, "alpha must be in [0, 1]");
+    if (shape->q_heads > 8192) return report(IKV_ERR_UNSUPPORTED, "more than 8192 query heads");
     const bool want_score = score || ema;
     const AttendWs w = attend_ws(shape, cap_of(cache), 1, want_score);
     if (!ws || ws_bytes < w.end) return report(IKV_ERR_WORKSPACE, "workspace needs %zu bytes", w.end);

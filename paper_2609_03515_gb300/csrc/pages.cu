@@ -548,7 +548,7 @@ cudaError_t launch_pages_fork(const PagesArgs &a, int32_t n, const int32_t *src,
 cudaError_t launch_pages_writable(const PagesArgs &a, const PagesWs &w, const int32_t *first, const int32_t *count,
                                   int32_t max_count, int32_t *lacking, int sms, cudaStream_t st) {
     // pages that max_count slots from anywhere in a page may touch
-    const int64_t most = ((int64_t)max_count + a.page_size - 2) / a.page_size + 1;
+    const int64_t most = max_count > 0 ? ((int64_t)max_count + a.page_size - 2) / a.page_size + 1 : 1;
     const int span = (int)(most < a.max_pages ? most : a.max_pages);
     const bool few = (int64_t)a.batch * span <= kFewRequests;
     cudaError_t e = launch_k(few ? writable_plan_kernel<true> : writable_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0,

@@ -366,3 +366,20 @@ def test_many_sequences_share_and_leave_a_page(nb, idle):
     ikv.ikv_pages_compact(shape, cache, pages, kp.cuda(), i32(kl), c.ema, None, ws, ws.numel())
     m.compare()
     assert ikv.ikv_device_status() == 0
+
+
+def test_nothing_to_do():
+    """No slots asked for, no forks, empty sequences: nothing changes, and lacking says 0."""
+    c = make("q4", 3, 16, 64, 1, 0, [0] * 3, pool=5)
+    ws = c.pages_workspace()
+    shape, cache, pages = c.shape(), c.cache(0), c.pages()
+    lacking = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    ikv.ikv_pages_writable(shape, cache, pages, None, None, 0, lacking, ws, ws.numel())
+    assert int(lacking) == 0
+    lacking.fill_(9)
+    ikv.ikv_pages_fork(shape, cache, pages, 0, None, None, None)
+    ikv.ikv_pages_release(shape, cache, pages, 3)
+    keep, kl = torch.zeros(3, c.cap, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    ikv.ikv_pages_compact(shape, cache, pages, keep, kl, None, lacking, ws, ws.numel())
+    assert int(lacking) == 0 and ikv.ikv_device_status() == 0
+    assert not c.block_table.any() and c.refs.tolist() == [1, 0, 0, 0, 0, 0] and not c.len.any()
