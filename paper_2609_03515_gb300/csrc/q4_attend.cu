@@ -215,6 +215,18 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
 // that follows the largest scale seen, they stay within fp16's range.
 // The softmax runs on a reference that is at most 2^6 below the largest logit, so the sums are
 // rescaled a few times a sequence and no tile waits for a maximum across lanes.
+// DUAL (groups of four heads or fewer): a pair of tiles shares the columns, the first's logits in
+// columns 0 to 3 and the second's in 4 to 7, each with an operand that is zero in the other's
+// columns; logits, weights and scales then take half the instructions, and a head's two columns
+// are joined like two warps (16 ragged sequences of 4k to 8k, 32 / 8 heads: 39.0 -> 36.7 us).
+//
+// Memory allows a tile of 128 channels 99 cycles of an SM.  It takes about 250 instructions (224
+// DUAL), 64 of them conversions of codes that fill the ALU pipe for 32 cycles, and 12 warps issue
+// some 2.3 a cycle: close behind memory, so what was cut was instructions.  32 sequences of 12k to
+// 16k, 28 / 4 heads: 264 MB in 52.6 us with the merge (5.0 TB/s; 5.8 while tiles stream); one of
+// 32k, 32 / 8 heads, 38 MB in 12 us before its scores: lengths, table and first tiles are 4 of
+// them, the join 1.5.  Two stages a warp: a third costs L1 that the rest of the launch uses
+// (54.5 us against 52.6).
 template <int D, typename T, bool SCORE, bool DUAL>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend_kernel(const Q4AttendArgs a) {
     constexpr int Y = D / kQ4Group;        // groups of a row
@@ -229,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
     pdl_wait();
     const int kvh = a.pv.kv_heads, G = a.q_heads / kvh;
     const Run run = run_of(a);
-    if (run.b < 0) return;  // past the last round
+    if (run.b < 0) return;  // past the last run
 
     // where a lane's pieces of a tile go: K's rows permuted, V's pieces swizzled
     constexpr int kCopies = kQ4Tile * kPieces / 32;
@@ -733,7 +745,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
 // The rest of a call: outputs of units of several segments (or of none: 0), Eq. 1's scores and Eq. 4.
 //
 // The first CTAs take a utility row's tokens, kFinishThreads / HS of them each, HS threads a token
-// that share the row's heads; the others merge a head's outputs.  A head's log-sum-exp comes from
+// that share the row's heads; the others merge a head's outputs (MANY: each a CTA, its warps a part of
+// the segments each; else a head a warp).  A head's log-sum-exp comes from
 // its segments' (reference, sum) pairs, so no pass of its own has to gather it.
 constexpr int kFinishThreads = 512;
 
