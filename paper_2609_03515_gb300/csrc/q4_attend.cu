@@ -13,8 +13,8 @@ namespace {
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kPair = 2;              // tiles of an iteration
 constexpr int kStages = 2;            // pairs of tiles a warp has in flight or in use
-// CTAs an SM holds: at 4, 128 channels have neither the registers nor the L1 that 3 leave (qwen-like
-// 32 x 16k: 56.9 us against 52.6), 64 channels of bf16 queries have both (groups of 4: 33.7 against 35.5)
+// CTAs an SM holds: at 4, 128 channels lack the registers that 3 leave (32 x 16k, 28 / 4 heads: 56.3 us
+// against 52.6); 64 channels of bf16 queries have them (16 / 4 heads: 33.7 against 35.5)
 constexpr int ctas_per_sm(int head_dim, int elem_bytes) { return head_dim == 64 && elem_bytes == 2 ? 4 : 3; }
 constexpr int kSwitch = 12;           // what going from one unit to the next costs a CTA, in pairs of tiles
 constexpr float kMaxSlack = 6.f;      // log2: how far a logit may lie above the running reference
@@ -221,12 +221,11 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
 // are joined like two warps (16 ragged sequences of 4k to 8k, 32 / 8 heads: 39.0 -> 36.7 us).
 //
 // Memory allows a tile of 128 channels 99 cycles of an SM.  It takes about 250 instructions (224
-// DUAL), 64 of them conversions of codes that fill the ALU pipe for 32 cycles, and 12 warps issue
-// some 2.3 a cycle: close behind memory, so what was cut was instructions.  32 sequences of 12k to
-// 16k, 28 / 4 heads: 264 MB in 52.6 us with the merge (5.0 TB/s; 5.8 while tiles stream); one of
-// 32k, 32 / 8 heads, 38 MB in 12 us before its scores: lengths, table and first tiles are 4 of
-// them, the join 1.5.  Two stages a warp: a third costs L1 that the rest of the launch uses
-// (54.5 us against 52.6).
+// DUAL), 64 of them conversions of codes that fill the ALU pipe for 32 cycles; 12 warps issue some
+// 2.3 a cycle, which hides most of them.  32 sequences of 12k to 16k, 28 / 4 heads: 264 MB in
+// 52.6 us with the merge (5.0 TB/s), of which waiting for the tiles alone takes 47.8; one of 32k,
+// 32 / 8 heads, 38 MB in 12 us before its scores: lengths, table and first tiles are 4 of them,
+// the join 1.5.  A third stage is slower (54.5 us), a fourth CTA of 128 registers too (56.3).
 template <int D, typename T, bool SCORE, bool DUAL>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend_kernel(const Q4AttendArgs a) {
     constexpr int Y = D / kQ4Group;        // groups of a row
