@@ -353,6 +353,7 @@ compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
     if (threadIdx.x == 0) {
         w.total[0] = have == total ? total : 0;
         w.total[1] = have == total;
+        w.total[2] = 0;  // arrivals of the copies
         if (lacking) *lacking = total - have;
         if (have < total) atomicOr(&g_pages_error, 64u);
     }
@@ -397,6 +398,32 @@ __device__ __forceinline__ void gather_plane(unsigned char *plane, int rb, const
             if (to[u]) *to[u] = x[u];
     }
 }
+// A sequence's table, its pages' counts and its length, once its rows are copied.
+__device__ __forceinline__ void commit_sequence(const PagesArgs &a, const PagesWs &w, const int32_t *keep_len, int b) {
+    constexpr int U = 4;
+    const int n = keep_len[(int64_t)b * a.rows_per_seq];
+    if (n < 0) return;
+    const int begin = w.begin[b], base = w.base[b], made = w.base[b + 1] - base;
+    int32_t *table = a.table + (int64_t)b * a.max_pages;
+    for (int lp0 = begin + threadIdx.x; lp0 < a.max_pages; lp0 += U * kCopyThreads) {
+        int e[U], to[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int lp = lp0 + u * kCopyThreads;
+            e[u] = lp < a.max_pages ? table[lp] : 0;
+            to[u] = lp < a.max_pages && lp - begin < made ? w.free_ids[base + lp - begin] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int lp = lp0 + u * kCopyThreads;
+            if (e[u] > 0 && e[u] < a.num_pages) atomicSub(a.refs + e[u], 1);
+            if (to[u]) a.refs[to[u]] = 1;
+            if (lp < a.max_pages && e[u] != to[u]) table[lp] = to[u];
+        }
+    }
+    if (threadIdx.x == 0) a.len[b] = min(n, a.cap);
+}
+
 // Row x of pos, then of ema, then of vnorm, gathered in place: keep[j] >= j, so a run of slots is read
 // before it is written, and no later run is read from it.
 __device__ __forceinline__ void gather_in_place(const PagesArgs &a, const int32_t *keep, const int32_t *keep_len, int64_t x) {
@@ -435,21 +462,24 @@ __device__ __forceinline__ void gather_in_place(const PagesArgs &a, const int32_
         }
     }
 }
+template <bool COMMIT>
 __global__ void __launch_bounds__(kCopyThreads, 4)
 compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int pages_at_once,
                     int n_rows) {
     pdl_wait();
     __shared__ RowMove moves[kRowsAtOnce];
-    if ((int)blockIdx.x < n_rows) {  // beside the copies
-        if (w.total[1]) gather_in_place(a, keep, keep_len, blockIdx.x);
-        return;
+    if (!w.total[1]) return;  // too few pages
+    const bool gathers = (int)blockIdx.x < n_rows;  // beside the copies
+    if (gathers) {
+        gather_in_place(a, keep, keep_len, blockIdx.x);
+        if (!COMMIT) return;
     }
     const int jobs = w.total[0];
     // heads that share their moves: all, or with a keep row for each KV head one
     const int heads = a.rows_per_seq == 1 ? a.kv_heads : 1;
     const int groups = (jobs + pages_at_once - 1) / pages_at_once, parts = a.kv_heads / heads;
     const int64_t items = (int64_t)groups * a.layers * parts;
-    for (int64_t it = (int)blockIdx.x - n_rows; it < items; it += (int)gridDim.x - n_rows) {
+    for (int64_t it = gathers ? items : (int)blockIdx.x - n_rows; it < items; it += (int)gridDim.x - n_rows) {
         const int g0 = (int)(it % parts);
         const int l = (int)(it / parts % a.layers), job0 = (int)(it / parts / a.layers) * pages_at_once;
         const int pages = min(pages_at_once, jobs - job0);
@@ -490,23 +520,20 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
             }
         }
     }
+    if constexpr (COMMIT) {
+        __shared__ int last;
+        __syncthreads();
+        if (threadIdx.x == 0) last = arrive_acq_rel(w.total + 2) == (int)gridDim.x - 1;
+        __syncthreads();
+        if (last)
+            for (int b = 0; b < a.batch; ++b) commit_sequence(a, w, keep_len, b);
+    }
 }
 
-// After the copies: a CTA a sequence, its table, its pages' counts and its length.
-__global__ void __launch_bounds__(kRowThreads) compact_commit_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep_len) {
+// After the copies of many sequences: a CTA a sequence.
+__global__ void __launch_bounds__(kCopyThreads) compact_commit_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep_len) {
     pdl_wait();
-    const int b = blockIdx.x, n = keep_len[(int64_t)b * a.rows_per_seq];
-    const int begin = w.begin[b], base = w.base[b], made = w.base[b + 1] - base;
-    if (!w.total[1] || n < 0) return;
-    for (int lp = begin + threadIdx.x; lp < a.max_pages; lp += kRowThreads) {
-        int32_t *entry = a.table + (int64_t)b * a.max_pages + lp;
-        const int e = *entry;
-        if (e > 0 && e < a.num_pages) atomicSub(a.refs + e, 1);
-        const int to = lp - begin < made ? w.free_ids[base + lp - begin] : 0;
-        if (to) a.refs[to] = 1;
-        *entry = to;
-    }
-    if (threadIdx.x == 0) a.len[b] = min(n, a.cap);
+    if (w.total[1]) commit_sequence(a, w, keep_len, blockIdx.x);
 }
 
 }  // namespace
@@ -574,11 +601,20 @@ cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int
     const int64_t ctas = items < 8 * (int64_t)sms ? items : 8 * (int64_t)sms;
     const int64_t rows = 2 * (int64_t)a.batch * a.rows_per_seq + (a.vnorm ? (int64_t)a.layers * a.batch * a.kv_heads : 0);
     if (rows + ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    e = launch_k(compact_copy_kernel, dim3((unsigned)(rows + ctas)), dim3(kCopyThreads), 0, st, a, w, keep, keep_len, at_once,
-                 (int)rows);
+    // Little to move: the last CTA of the copies writes the tables.  It saves a launch (3 us of a case of
+    // a few sequences), but costs registers that the copies of a large cache want (first eviction
+    // of a 32k prompt: 160 us against 153).
+    int64_t most = (int64_t)a.batch * a.max_pages;
+    const bool few_entries = most <= 2048;
+    most *= (int64_t)a.page_size * a.kv_heads * a.layers;
+    int64_t bytes = 0;
+    for (int i = 0; i < a.n_planes; ++i) bytes += most * a.row_bytes[i];
+    const bool commit = few_entries && bytes <= (int64_t)128 << 20;
+    e = launch_k(commit ? compact_copy_kernel<true> : compact_copy_kernel<false>, dim3((unsigned)(rows + ctas)), dim3(kCopyThreads),
+                 0, st, a, w, keep, keep_len, at_once, (int)rows);
     note_launch();
-    if (e != cudaSuccess) return e;
-    e = launch_k(compact_commit_kernel, dim3((unsigned)a.batch), dim3(kRowThreads), 0, st, a, w, keep_len);
+    if (e != cudaSuccess || commit) return e;
+    e = launch_k(compact_commit_kernel, dim3((unsigned)a.batch), dim3(kCopyThreads), 0, st, a, w, keep_len);
     note_launch();
     return e;
 }

@@ -97,7 +97,7 @@ struct PagesArgs {
 };
 // scratch of one call: what its kernels hand to one another
 struct PagesWs {
-    int32_t *total;                   // [4]: jobs, 0 / 1 done, -, -
+    int32_t *total;                   // [4]: jobs, whether there were pages enough, arrivals, -
     int32_t *free_ids;                // [batch * max_pages] the free pages that the call takes, ascending
     int32_t *count, *last;            // [num_pages] writers of a shared page, the last of them
     int32_t *jobs;                    // [batch * max_pages][4]

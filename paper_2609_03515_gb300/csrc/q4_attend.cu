@@ -89,7 +89,7 @@ struct Tile {
 };
 
 template <int D>
-constexpr size_t kJoinBytes = kWarps * 8 * (sizeof(float2) + D * sizeof(float));  // shared memory in front of the rings
+constexpr size_t kJoinBytes = kWarps * 8 * (sizeof(float2) + D * sizeof(float));  // in place of the rings
 
 // A tile's row r stands for token perm(r): lane (g, t) of the second product then finds its
 // four tokens t, 4 + t, 8 + t, 12 + t, whose 8-byte units lie in different banks.
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
     float *po = reinterpret_cast<float *>(smem + kWarps * 8 * sizeof(float2));  // [kWarps][8][D]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int g = lane >> 2, t = lane & 3;
-    const Tile<D> *ring = reinterpret_cast<const Tile<D> *>(smem + kJoinBytes<D>) + warp * (kStages * kPair);
+    const Tile<D> *ring = reinterpret_cast<const Tile<D> *>(smem) + warp * (kStages * kPair);
     pdl_wait();
     const int kvh = a.pv.kv_heads, G = a.q_heads / kvh;
     const Run run = run_of(a);
@@ -672,20 +672,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
 #pragma unroll
     for (int c = 0; c < 2; ++c)
         if (ref[c] == -FLT_MAX) ref[c] = -INFINITY;  // no live slot
-    // ---- the run goes on in the next unit: its first copies are under way while this one is joined
-    const Segment done = sg;
-    const bool more = enter_next(sg.b, sg.kv);
-    if (more) {
-        __syncwarp();  // the last stage is read
-        prologue();
-    }
-
     // ---- the warps' results joined: (reference, sum) and outputs through shared memory
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], d);
-    __syncthreads();  // the join before is read
+    __syncthreads();  // every ring is done with
     const float back = ldexpf(1.f, -(int)norm_e);
     if (g == 0) {
         ml[warp * 8 + 2 * t] = make_float2(ref[0], sum[0] * back);
@@ -723,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
             x.w += f * v.w;
         }
         const int64_t head = head0 + h;
-        if (done.segs == 1) {
+        if (sg.segs == 1) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
             T *dst = static_cast<T *>(a.out) + head * D + e;
             store_as(dst, x.x * inv);
@@ -732,12 +724,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
             store_as(dst + 3, x.w * inv);
             if (e == 0) a.lse2[head] = l == 0.f ? -INFINITY : m + log2f(l);
         } else {
-            const int64_t to = head * kMaxSplits + ((int)blockIdx.x - done.seg0);
+            const int64_t to = head * kMaxSplits + ((int)blockIdx.x - sg.seg0);
             *reinterpret_cast<float4 *>(a.part_o + to * D + e) = x;
             if (e == 0) reinterpret_cast<float2 *>(a.part_ml)[to] = make_float2(m, l);
         }
     }
-    if (!more) return;
+    // ---- the run goes on in the next unit
+    if (!enter_next(sg.b, sg.kv)) return;
+    __syncthreads();  // the join is read
+    prologue();
     }
 }
 
@@ -968,16 +963,13 @@ __global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4Finis
 
 template <int D, typename T>
 cudaError_t launch_t(const Q4AttendArgs &a, int ctas, cudaStream_t st) {
-    constexpr size_t smem = kJoinBytes<D> + sizeof(Tile<D>) * kPair * kStages * kWarps;
+    constexpr size_t ring = sizeof(Tile<D>) * kPair * kStages * kWarps, smem = ring > kJoinBytes<D> ? ring : kJoinBytes<D>;
+    static_assert(smem <= 48 << 10, "more shared memory needs an attribute of the kernel");
     // two tiles share the columns of a group of 4 or fewer, where the registers hold q for both
     constexpr bool kDual = sizeof(T) * D <= 256;
     const bool dual = kDual && a.q_heads <= 4 * a.pv.kv_heads;
     auto kernel = dual ? (a.logits ? q4_attend_kernel<D, T, true, kDual> : q4_attend_kernel<D, T, false, kDual>)
                        : (a.logits ? q4_attend_kernel<D, T, true, false> : q4_attend_kernel<D, T, false, false>);
-    if (smem > 48 << 10) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
     const cudaError_t e = launch_k(kernel, dim3((unsigned)ctas), dim3(kThreads), smem, st, a);
     note_launch();
     return e;

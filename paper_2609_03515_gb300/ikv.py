@@ -270,27 +270,25 @@ def ikv_step_end(shape, params, cache, ema, t, ws, ws_bytes, stream=None) -> Non
                              ws_bytes, _stream(stream)), "ikv_step_end")
 
 
+# (structs go by reference of themselves: ctypes does it faster than an explicit byref)
 def ikv_q4_store(shape, cache, q4, layer0, n_layers, k, v, rows, first, count, max_count, stream=None) -> None:
-    _check(_lib.ikv_q4_store(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(q4), layer0, n_layers, _p(k),
-                             _p(v), ctypes.byref(rows), _p(first), _p(count), max_count, _stream(stream)),
-           "ikv_q4_store")
+    _check(_lib.ikv_q4_store(shape, cache, q4, layer0, n_layers, _p(k), _p(v), rows, _p(first), _p(count), max_count,
+                             _stream(stream)), "ikv_q4_store")
 
 
 def ikv_q4_load(shape, cache, q4, layer0, n_layers, k, v, rows, first, count, max_count, stream=None) -> None:
-    _check(_lib.ikv_q4_load(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(q4), layer0, n_layers, _p(k),
-                            _p(v), ctypes.byref(rows), _p(first), _p(count), max_count, _stream(stream)),
-           "ikv_q4_load")
+    _check(_lib.ikv_q4_load(shape, cache, q4, layer0, n_layers, _p(k), _p(v), rows, _p(first), _p(count), max_count,
+                            _stream(stream)), "ikv_q4_load")
 
 
 def ikv_q4_append_token(shape, cache, q4, k_new, v_new, ema, init_mean, slot, stream=None) -> None:
-    _check(_lib.ikv_q4_append_token(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(q4), _p(k_new), _p(v_new),
-                                    _p(ema), init_mean, _p(slot), _stream(stream)), "ikv_q4_append_token")
+    _check(_lib.ikv_q4_append_token(shape, cache, q4, _p(k_new), _p(v_new), _p(ema), init_mean, _p(slot),
+                                    _stream(stream)), "ikv_q4_append_token")
 
 
 def ikv_q4_attend_score(shape, cache, q4, layer, q, out, score, ema, alpha, ws, ws_bytes, stream=None) -> None:
-    _check(_lib.ikv_q4_attend_score(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(q4), layer, _p(q), _p(out),
-                                    _p(score), _p(ema), alpha, _p(ws), ws_bytes, _stream(stream)),
-           "ikv_q4_attend_score")
+    _check(_lib.ikv_q4_attend_score(shape, cache, q4, layer, _p(q), _p(out), _p(score), _p(ema), alpha, _p(ws),
+                                    ws_bytes, _stream(stream)), "ikv_q4_attend_score")
 
 
 def ikv_pages_of(refs, planes) -> ikv_pages:
@@ -304,30 +302,26 @@ def ikv_pages_of(refs, planes) -> ikv_pages:
 
 def ikv_pages_workspace_size(shape, cache, pages) -> int:
     n = SZ(0)
-    _check(_lib.ikv_pages_workspace_size(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(pages),
-                                         ctypes.byref(n)), "ikv_pages_workspace_size")
+    _check(_lib.ikv_pages_workspace_size(shape, cache, pages, ctypes.byref(n)), "ikv_pages_workspace_size")
     return n.value
 
 
 def ikv_pages_release(shape, cache, pages, extra, stream=None) -> None:
-    _check(_lib.ikv_pages_release(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(pages), extra,
-                                  _stream(stream)), "ikv_pages_release")
+    _check(_lib.ikv_pages_release(shape, cache, pages, extra, _stream(stream)), "ikv_pages_release")
 
 
 def ikv_pages_fork(shape, cache, pages, n, src, dst, ema, stream=None) -> None:
-    _check(_lib.ikv_pages_fork(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(pages), n, _p(src), _p(dst),
-                               _p(ema), _stream(stream)), "ikv_pages_fork")
+    _check(_lib.ikv_pages_fork(shape, cache, pages, n, _p(src), _p(dst), _p(ema), _stream(stream)), "ikv_pages_fork")
 
 
 def ikv_pages_writable(shape, cache, pages, first, count, max_count, lacking, ws, ws_bytes, stream=None) -> None:
-    _check(_lib.ikv_pages_writable(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(pages), _p(first), _p(count),
-                                   max_count, _p(lacking), _p(ws), ws_bytes, _stream(stream)), "ikv_pages_writable")
+    _check(_lib.ikv_pages_writable(shape, cache, pages, _p(first), _p(count), max_count, _p(lacking), _p(ws), ws_bytes,
+                                   _stream(stream)), "ikv_pages_writable")
 
 
 def ikv_pages_compact(shape, cache, pages, keep, keep_len, ema, lacking, ws, ws_bytes, stream=None) -> None:
-    _check(_lib.ikv_pages_compact(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(pages), _p(keep),
-                                  _p(keep_len), _p(ema), _p(lacking), _p(ws), ws_bytes, _stream(stream)),
-           "ikv_pages_compact")
+    _check(_lib.ikv_pages_compact(shape, cache, pages, _p(keep), _p(keep_len), _p(ema), _p(lacking), _p(ws), ws_bytes,
+                                  _stream(stream)), "ikv_pages_compact")
 
 
 def raw_status(fn_name: str, *args) -> int:
