@@ -118,7 +118,7 @@ struct Segment {
     int pairs;          // the unit's pairs that are the CTA's
     int seg0, segs;     // the CTA of the unit's first segment, the unit's segments
 };
-// Where a CTA's run starts and how long it is; every thread of the CTA, each takes some sequences.
+// Where a CTA's run starts and how long it is.
 struct Run {
     int b, before;      // its first sequence, and the length (of one KV head) in front of that; b < 0: none
     int per;            // length of a run
@@ -126,14 +126,63 @@ struct Run {
     __device__ __forceinline__ int length(int pairs) const {
         return pairs == 0 ? 0 : whole ? whole : pairs + kSwitch;
     }
+    // n sequences with slots, of `total` pairs, low to top each
+    __device__ __forceinline__ void deal(int total, int n, int low, int top, int kvh, int ctas) {
+        const int units = n * kvh;
+        // (a unit of kMaxSplits - 2 whole runs at most: it may begin and end inside two more)
+        const int least = (top + kMaxSplits - 3) / (kMaxSplits - 2);
+        per = max(max((total * kvh + units * kSwitch + ctas - 1) / ctas, least), 1);
+        whole = 0;
+        if (top == low && units <= ctas) {
+            // units of one length, cut evenly, each into runs of its own, if that makes them no longer
+            const int each_unit = ctas / units, cut = max((top + each_unit - 1) / each_unit, least);
+            // (a few pairs: as many for every warp)
+            const int even = cut > 2 * kWarps ? cut : (cut + kWarps - 1) / kWarps * kWarps;
+            if (even <= per + kSwitch) {
+                per = even;
+                whole = (top + even - 1) / even * even;
+            }
+        }
+    }
+    // whether the CTA's run starts in a sequence of that length, `base` in front of it
+    __device__ __forceinline__ bool starts_in(int base, int len, int kvh) const {
+        const int64_t x = (int64_t)blockIdx.x * per;
+        return x >= base * kvh && x < (base + len) * kvh;
+    }
 };
-__device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
+// Up to 32 sequences: each warp for itself, a sequence a lane, with no barrier.  sp: the span of the first.
+__device__ __forceinline__ Run run_of_few(const Q4AttendArgs &a, Span &sp) {
+    const int lane = threadIdx.x & 31;
+    Span mine{0, 0, 0, 0, 0};
+    if (lane < a.batch) mine = span_of(a, lane);
+    Run run;
+    run.deal(__reduce_add_sync(0xffffffffu, mine.pairs), __popc(__ballot_sync(0xffffffffu, mine.pairs > 0)),
+             __reduce_min_sync(0xffffffffu, mine.pairs > 0 ? mine.pairs : INT_MAX),
+             __reduce_max_sync(0xffffffffu, mine.pairs), a.pv.kv_heads, (int)gridDim.x);
+    const int len = run.length(mine.pairs);
+    int end = len;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, end, d);
+        if (lane >= d) end += y;
+    }
+    run.b = __ffs(__ballot_sync(0xffffffffu, run.starts_in(end - len, len, a.pv.kv_heads))) - 1;
+    run.before = __shfl_sync(0xffffffffu, end - len, max(run.b, 0));
+    sp.L = __shfl_sync(0xffffffffu, mine.L, max(run.b, 0));
+    sp.S = __shfl_sync(0xffffffffu, mine.S, max(run.b, 0));
+    sp.tile0 = __shfl_sync(0xffffffffu, mine.tile0, max(run.b, 0));
+    sp.tiles = __shfl_sync(0xffffffffu, mine.tiles, max(run.b, 0));
+    sp.pairs = __shfl_sync(0xffffffffu, mine.pairs, max(run.b, 0));
+    return run;
+}
+// Any number: every thread of the CTA takes some sequences.
+__device__ __forceinline__ Run run_of(const Q4AttendArgs &a, Span &sp) {
     __shared__ int sums[kWarps], counts[kWarps], tops[kWarps], lows[kWarps], found[2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int each = (a.batch + kThreads - 1) / kThreads, b0 = threadIdx.x * each, b1 = min(b0 + each, a.batch);
-    int mine = 0, n_mine = 0, top = 0, low = INT_MAX, pairs = 0;
+    int mine = 0, n_mine = 0, top = 0, low = INT_MAX;
     for (int b = b0; b < b1; ++b) {
-        pairs = span_of(a, b).pairs;
+        const int pairs = span_of(a, b).pairs;
         mine += pairs;
         n_mine += pairs > 0;
         top = max(top, pairs);
@@ -170,27 +219,12 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
         top = max(top, tops[w]);
         low = min(low, lows[w]);
     }
-    const int kvh = a.pv.kv_heads, ctas = (int)gridDim.x, units = n * kvh;
-    // (a unit of kMaxSplits - 2 whole runs at most: it may begin and end inside two more)
-    const int least = (top + kMaxSplits - 3) / (kMaxSplits - 2);
     Run run;
-    run.per = max(max((total * kvh + units * kSwitch + ctas - 1) / ctas, least), 1);
-    run.whole = 0;
-    if (top == low && units <= ctas) {
-        // units of one length, cut evenly, each into runs of its own, if that makes them no longer
-        const int each_unit = ctas / units, cut = max((top + each_unit - 1) / each_unit, least);
-        // (a few pairs: as many for every warp)
-        const int even = cut > 2 * kWarps ? cut : (cut + kWarps - 1) / kWarps * kWarps;
-        if (even <= run.per + kSwitch) {
-            run.per = even;
-            run.whole = (top + even - 1) / even * even;
-        }
-    }
+    run.deal(total, n, low, top, a.pv.kv_heads, (int)gridDim.x);
     base = run.whole ? n_base * run.whole : base + n_base * kSwitch;
-    const int64_t x = (int64_t)blockIdx.x * run.per;
     for (int b = b0; b < b1; ++b) {
-        const int len = run.length(each == 1 ? pairs : span_of(a, b).pairs);
-        if (x >= base * kvh && x < (base + len) * kvh) {
+        const int len = run.length(span_of(a, b).pairs);
+        if (run.starts_in(base, len, a.pv.kv_heads)) {
             found[0] = b;
             found[1] = base;
         }
@@ -199,6 +233,7 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a) {
     __syncthreads();
     run.b = found[0];
     run.before = found[1];
+    if (run.b >= 0) sp = span_of(a, run.b);
     return run;
 }
 
@@ -239,7 +274,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
     const Tile<D> *ring = reinterpret_cast<const Tile<D> *>(smem) + warp * (kStages * kPair);
     pdl_wait();
     const int kvh = a.pv.kv_heads, G = a.q_heads / kvh;
-    const Run run = run_of(a);
+    Span sp;
+    const Run run = a.batch <= 32 ? run_of_few(a, sp) : run_of(a, sp);
     if (run.b < 0) return;  // past the last run
 
     // where a lane's pieces of a tile go: K's rows permuted, V's pieces swizzled
@@ -257,7 +293,6 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
 
     // the segment at hand
     int before = run.before, left = run.per;
-    Span sp = span_of(a, run.b);
     Segment sg;
     const int32_t *pos = nullptr;
     int first = 0, last = 0, mine = 0;  // its tiles [first, last) of the sequence, this warp's pairs of them
