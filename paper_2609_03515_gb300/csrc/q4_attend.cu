@@ -300,11 +300,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
         sg.b = b;
         sg.kv = kv;
         sg.pairs = min(sp.pairs - pair, left);
-        const int unit0 = before * kvh + kv * run.length(sp.pairs);
-        sg.seg0 = unit0 / run.per;
-        sg.segs = (unit0 + sp.pairs - 1) / run.per - sg.seg0 + 1;
         left -= run.length(sp.pairs) - pair;
-        if (threadIdx.x == 0 && pair == 0) a.segs[b * kvh + kv] = sg.segs;
         pos = a.pos ? a.pos + (int64_t)(a.rows_per_seq == 1 ? b : b * a.rows_per_seq + kv) * a.cap : nullptr;
         first = pair * kPair;
         last = min(first + sg.pairs * kPair, sp.tiles);
@@ -380,6 +376,13 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
     }
     prologue();
     while (true) {
+    // the unit's segments: the runs that its pairs lie in
+    {
+        const int unit0 = before * kvh + sg.kv * run.length(sp.pairs);
+        sg.seg0 = unit0 / run.per;
+        sg.segs = (unit0 + sp.pairs - 1) / run.per - sg.seg0 + 1;
+        if (threadIdx.x == 0 && first == 0) a.segs[sg.b * kvh + sg.kv] = sg.segs;
+    }
     const int L = sp.L, S = sp.S, tile0 = sp.tile0;
     const int64_t head0 = (int64_t)sg.b * a.q_heads + (int64_t)sg.kv * G;
 
