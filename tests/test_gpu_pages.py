@@ -383,3 +383,43 @@ def test_nothing_to_do():
     ikv.ikv_pages_compact(shape, cache, pages, keep, kl, None, lacking, ws, ws.numel())
     assert int(lacking) == 0 and ikv.ikv_device_status() == 0
     assert not c.block_table.any() and c.refs.tolist() == [1, 0, 0, 0, 0, 0] and not c.len.any()
+
+
+@pytest.mark.parametrize("kind,ps,nb", [("bf16", 16, 5), ("q4", 48, 300)])
+def test_workspace_and_other_pages_stay_as_they_are(kind, ps, nb):
+    """A pattern behind the workspace, and the contents of every page that a call does not hand out."""
+    c = make(kind, nb, ps, 64, 2, 0, [0] * nb, pool=4 * nb, cap=2 * ps, layers=2)
+    m, rng = Model(c), random.Random(nb)
+    shape, cache, pages = c.shape(), c.cache(c.cap), c.pages()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    n = ikv.ikv_pages_workspace_size(shape, cache, pages)
+    ws = torch.full((n + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+
+    def untouched(call):
+        before, free = [t.clone() for t in c.planes()], c.refs == 0
+        call()
+        same = ~(free & (c.refs > 0))
+        for t, was in zip(c.planes(), before):
+            assert torch.equal(t[:, same], was[:, same])
+        assert bool((ws[n:] == 0x5A).all()) and ikv.ikv_device_status() == 0
+
+    want = {b: (0, ps + 1) for b in range(0, nb, 2)}
+    m.writable(want)
+    untouched(lambda: ikv.ikv_pages_writable(shape, cache, pages, None, i32([ps + 1 if b in want else 0 for b in range(nb)]),
+                                             ps + 1, None, ws, n))
+    m.write(want, rng)
+    pairs = [(b - 1, b) for b in range(1, nb, 2)]
+    m.fork(pairs)
+    untouched(lambda: ikv.ikv_pages_fork(shape, cache, pages, len(pairs), i32([s for s, _ in pairs]), i32([d for _, d in pairs]),
+                                         c.ema))
+    m.writable({b: (ps + 1, 1) for b in range(nb)})
+    untouched(lambda: ikv.ikv_pages_writable(shape, cache, pages, None, None, 1, None, ws, n))
+    m.compare()
+    keep = {b: [[0, 1] + list(range(3, ps + 1))] for b in range(0, nb, 3)}
+    kp = torch.zeros(c.rows, c.cap, dtype=torch.int32)
+    for b, k in keep.items():
+        kp[b, :len(k[0])] = torch.tensor(k[0], dtype=torch.int32)
+    assert m.compact(keep) == 0
+    kp, kl = kp.cuda(), i32([len(keep[b][0]) if b in keep else -1 for b in range(nb)])
+    untouched(lambda: ikv.ikv_pages_compact(shape, cache, pages, kp, kl, c.ema, None, ws, n))
+    m.compare()

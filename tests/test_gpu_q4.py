@@ -415,3 +415,29 @@ def test_many_sequences(lens, kvh, G, gran):
     ikv.ikv_q4_attend_score(c.shape(), cch, c.q4(), 0, q, out, score, None, 0.0, ws, n)
     assert ikv.ikv_device_status() == 0
     check(c, 0, q, out, score, False, torch.ones_like(c.pos, dtype=torch.bool))
+
+
+@pytest.mark.parametrize("lens,kvh,G,d,dtype", [([3000], 1, 8, 128, ikv.IKV_F32), ([40, 900, 0, 17], 4, 7, 128, ikv.IKV_BF16),
+                                                ([250] * 40, 2, 1, 64, ikv.IKV_BF16)])
+def test_nothing_written_outside_the_buffers(lens, kvh, G, d, dtype):
+    """Patterns behind the workspace, around the outputs and in the pools stay as they were."""
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    c = make(lens, kvh, G, d, 16, dtype, layers=1)
+    noise(c, gen)
+    x = torch.randn(1, len(lens), max(lens), kvh, d, generator=gen, device="cuda").to(TORCH[dtype])
+    ikv.ikv_q4_store(c.shape(), c.cache(max(lens)), c.q4(), 0, 1, x, x, c.dense_rows(x), torch.zeros_like(c.len), c.len, max(lens))
+    pools = [t.clone() for t in c.planes()]
+    n = ikv.ikv_attend_workspace_size(c.shape(), c.cache(max(lens)))
+    ws = torch.full((n + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+    q = torch.randn(len(lens), G * kvh, d, generator=gen, device="cuda").to(TORCH[dtype])
+    out = torch.full((len(lens) + 2, G * kvh, d), 5.0, dtype=TORCH[dtype], device="cuda")
+    score = torch.full((c.rows + 2, c.cap), 5.0, device="cuda")
+    ema = torch.full((c.rows + 2, c.cap), 5.0, device="cuda")
+    ikv.ikv_q4_attend_score(c.shape(), c.cache(max(lens)), c.q4(), 0, q, out[1:-1], score[1:-1], ema[1:-1], 0.5, ws, n)
+    assert ikv.ikv_device_status() == 0
+    assert bool((ws[n:] == 0x5A).all())
+    for t in (out, score, ema):
+        assert bool((t[0] == 5.0).all()) and bool((t[-1] == 5.0).all())
+    for t, was in zip(c.planes(), pools):
+        assert torch.equal(t.view(torch.uint8), was.view(torch.uint8))
+    check(c, 0, q, out[1:-1], score[1:-1], False, torch.ones_like(c.pos, dtype=torch.bool))
