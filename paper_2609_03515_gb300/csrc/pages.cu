@@ -302,10 +302,21 @@ __global__ void __launch_bounds__(kCopyThreads) writable_copy_kernel(const Pages
     }
 }
 
+// A table entry from a sequence's first page made anew on: its old page is given back, its new one taken.
+__device__ __forceinline__ void commit_entry(const PagesArgs &a, const PagesWs &w, int b, int lp) {
+    int32_t *entry = a.table + (int64_t)b * a.max_pages + lp;
+    const int e = *entry, begin = w.begin[b], base = w.base[b];
+    const int to = lp - begin < w.base[b + 1] - base ? w.free_ids[base + lp - begin] : 0;
+    if (e > 0 && e < a.num_pages) atomicSub(a.refs + e, 1);
+    if (to) a.refs[to] = 1;
+    if (e != to) *entry = to;
+}
+
 // One CTA: where each sequence's first moved slot lies, the pages it makes anew, the free pages for
 // them.  keep[j] >= j rises with j, so the slots that stay are a prefix: a warp looks for its end.
 __global__ void __launch_bounds__(kPlanThreads)
-compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int32_t *lacking) {
+compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int32_t *lacking,
+                    int32_t *old) {
     pdl_wait();
     __shared__ int32_t need_s[kPlanThreads];
     int32_t *needs = a.batch <= kPlanThreads ? need_s : w.base;  // pages that a sequence makes anew
@@ -353,9 +364,20 @@ compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
     if (threadIdx.x == 0) {
         w.total[0] = have == total ? total : 0;
         w.total[1] = have == total;
-        w.total[2] = 0;  // arrivals of the copies
         if (lacking) *lacking = total - have;
         if (have < total) atomicOr(&g_pages_error, 64u);
+    }
+    if (!old || have < total) return;
+    // few entries: the tables change here, and the copies look up the old ones in `old`
+    const int entries = a.batch * a.max_pages;
+    for (int i = threadIdx.x; i < entries; i += kPlanThreads) {
+        const int b = i / a.max_pages, lp = i - b * a.max_pages;
+        old[i] = a.table[i];
+        if (lp >= w.begin[b]) commit_entry(a, w, b, lp);  // (none of a sequence left alone)
+    }
+    for (int b = threadIdx.x; b < a.batch; b += kPlanThreads) {
+        const int n = keep_len[(int64_t)b * a.rows_per_seq];
+        if (n >= 0) a.len[b] = min(n, a.cap);
     }
 }
 
@@ -398,32 +420,6 @@ __device__ __forceinline__ void gather_plane(unsigned char *plane, int rb, const
             if (to[u]) *to[u] = x[u];
     }
 }
-// A sequence's table, its pages' counts and its length, once its rows are copied.
-__device__ __forceinline__ void commit_sequence(const PagesArgs &a, const PagesWs &w, const int32_t *keep_len, int b) {
-    constexpr int U = 4;
-    const int n = keep_len[(int64_t)b * a.rows_per_seq];
-    if (n < 0) return;
-    const int begin = w.begin[b], base = w.base[b], made = w.base[b + 1] - base;
-    int32_t *table = a.table + (int64_t)b * a.max_pages;
-    for (int lp0 = begin + threadIdx.x; lp0 < a.max_pages; lp0 += U * kCopyThreads) {
-        int e[U], to[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int lp = lp0 + u * kCopyThreads;
-            e[u] = lp < a.max_pages ? table[lp] : 0;
-            to[u] = lp < a.max_pages && lp - begin < made ? w.free_ids[base + lp - begin] : 0;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int lp = lp0 + u * kCopyThreads;
-            if (e[u] > 0 && e[u] < a.num_pages) atomicSub(a.refs + e[u], 1);
-            if (to[u]) a.refs[to[u]] = 1;
-            if (lp < a.max_pages && e[u] != to[u]) table[lp] = to[u];
-        }
-    }
-    if (threadIdx.x == 0) a.len[b] = min(n, a.cap);
-}
-
 // Row x of pos, then of ema, then of vnorm, gathered in place: keep[j] >= j, so a run of slots is read
 // before it is written, and no later run is read from it.
 __device__ __forceinline__ void gather_in_place(const PagesArgs &a, const int32_t *keep, const int32_t *keep_len, int64_t x) {
@@ -462,24 +458,22 @@ __device__ __forceinline__ void gather_in_place(const PagesArgs &a, const int32_
         }
     }
 }
-template <bool COMMIT>
 __global__ void __launch_bounds__(kCopyThreads, 4)
-compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, int pages_at_once,
-                    int n_rows) {
+compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, const int32_t *old,
+                    int pages_at_once, int n_rows) {
     pdl_wait();
     __shared__ RowMove moves[kRowsAtOnce];
     if (!w.total[1]) return;  // too few pages
-    const bool gathers = (int)blockIdx.x < n_rows;  // beside the copies
-    if (gathers) {
+    if ((int)blockIdx.x < n_rows) {  // beside the copies
         gather_in_place(a, keep, keep_len, blockIdx.x);
-        if (!COMMIT) return;
+        return;
     }
     const int jobs = w.total[0];
     // heads that share their moves: all, or with a keep row for each KV head one
     const int heads = a.rows_per_seq == 1 ? a.kv_heads : 1;
     const int groups = (jobs + pages_at_once - 1) / pages_at_once, parts = a.kv_heads / heads;
     const int64_t items = (int64_t)groups * a.layers * parts;
-    for (int64_t it = gathers ? items : (int)blockIdx.x - n_rows; it < items; it += (int)gridDim.x - n_rows) {
+    for (int64_t it = (int)blockIdx.x - n_rows; it < items; it += (int)gridDim.x - n_rows) {
         const int g0 = (int)(it % parts);
         const int l = (int)(it / parts % a.layers), job0 = (int)(it / parts / a.layers) * pages_at_once;
         const int pages = min(pages_at_once, jobs - job0);
@@ -501,7 +495,7 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
                 if (j >= 0 && j < min(keep_len[r], a.cap)) {
                     const int64_t from = (int64_t)S + keep[r * a.cap + j];
                     const int fp = (int)(from / a.page_size);
-                    const int page = from >= 0 && fp < a.max_pages ? a.table[(int64_t)b * a.max_pages + fp] : -1;
+                    const int page = from >= 0 && fp < a.max_pages ? old[(int64_t)b * a.max_pages + fp] : -1;
                     if (page >= 0 && page < a.num_pages) {
                         m.src = (((int64_t)l * a.num_pages + page) * a.kv_heads + g0) * a.page_size + from % a.page_size;
                         m.dst = (((int64_t)l * a.num_pages + w.free_ids[job]) * a.kv_heads + g0) * a.page_size + q0 + q;
@@ -520,20 +514,15 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
             }
         }
     }
-    if constexpr (COMMIT) {
-        __shared__ int last;
-        __syncthreads();
-        if (threadIdx.x == 0) last = arrive_acq_rel(w.total + 2) == (int)gridDim.x - 1;
-        __syncthreads();
-        if (last)
-            for (int b = 0; b < a.batch; ++b) commit_sequence(a, w, keep_len, b);
-    }
 }
 
-// After the copies of many sequences: a CTA a sequence.
+// After the copies, where the plan left the tables to it: a CTA a sequence.
 __global__ void __launch_bounds__(kCopyThreads) compact_commit_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep_len) {
     pdl_wait();
-    if (w.total[1]) commit_sequence(a, w, keep_len, blockIdx.x);
+    const int b = blockIdx.x, n = keep_len[(int64_t)b * a.rows_per_seq];
+    if (!w.total[1] || n < 0) return;
+    for (int lp = w.begin[b] + threadIdx.x; lp < a.max_pages; lp += kCopyThreads) commit_entry(a, w, b, lp);
+    if (threadIdx.x == 0) a.len[b] = min(n, a.cap);
 }
 
 }  // namespace
@@ -593,7 +582,9 @@ cudaError_t launch_pages_writable(const PagesArgs &a, const PagesWs &w, const in
 
 cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int32_t *keep, const int32_t *keep_len,
                                  int32_t *lacking, int sms, cudaStream_t st) {
-    cudaError_t e = launch_k(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, w, keep, keep_len, lacking);
+    // up to 8192 entries the plan writes the tables; a launch after the copies for it takes longer
+    int32_t *old = (int64_t)a.batch * a.max_pages <= 8192 ? w.jobs : nullptr;
+    cudaError_t e = launch_k(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, w, keep, keep_len, lacking, old);
     note_launch();
     if (e != cudaSuccess) return e;
     const int at_once = a.page_size < kRowsAtOnce ? kRowsAtOnce / a.page_size : 1;
@@ -601,19 +592,10 @@ cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int
     const int64_t ctas = items < 8 * (int64_t)sms ? items : 8 * (int64_t)sms;
     const int64_t rows = 2 * (int64_t)a.batch * a.rows_per_seq + (a.vnorm ? (int64_t)a.layers * a.batch * a.kv_heads : 0);
     if (rows + ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    // Little to move: the last CTA of the copies writes the tables.  It saves a launch (3 us of a case of
-    // a few sequences), but costs registers that the copies of a large cache want (first eviction
-    // of a 32k prompt: 160 us against 153).
-    int64_t most = (int64_t)a.batch * a.max_pages;
-    const bool few_entries = most <= 2048;
-    most *= (int64_t)a.page_size * a.kv_heads * a.layers;
-    int64_t bytes = 0;
-    for (int i = 0; i < a.n_planes; ++i) bytes += most * a.row_bytes[i];
-    const bool commit = few_entries && bytes <= (int64_t)128 << 20;
-    e = launch_k(commit ? compact_copy_kernel<true> : compact_copy_kernel<false>, dim3((unsigned)(rows + ctas)), dim3(kCopyThreads),
-                 0, st, a, w, keep, keep_len, at_once, (int)rows);
+    e = launch_k(compact_copy_kernel, dim3((unsigned)(rows + ctas)), dim3(kCopyThreads), 0, st, a, w, keep, keep_len,
+                 (const int32_t *)(old ? old : a.table), at_once, (int)rows);
     note_launch();
-    if (e != cudaSuccess || commit) return e;
+    if (e != cudaSuccess || old) return e;
     e = launch_k(compact_commit_kernel, dim3((unsigned)a.batch), dim3(kCopyThreads), 0, st, a, w, keep_len);
     note_launch();
     return e;

@@ -97,10 +97,10 @@ struct PagesArgs {
 };
 // scratch of one call: what its kernels hand to one another
 struct PagesWs {
-    int32_t *total;                   // [4]: jobs, whether there were pages enough, arrivals, -
+    int32_t *total;                   // [4]: jobs, whether there were pages enough, -, -
     int32_t *free_ids;                // [batch * max_pages] the free pages that the call takes, ascending
     int32_t *count, *last;            // [num_pages] writers of a shared page, the last of them
-    int32_t *jobs;                    // [batch * max_pages][4]
+    int32_t *jobs;                    // [batch * max_pages][4]; a compaction's old table entries
     int32_t *begin, *base;            // [batch + 1] first page made anew, jobs of the sequences before
 };
 size_t pages_ws(int32_t batch, int32_t max_pages, int32_t num_pages, void *ws, PagesWs *w);

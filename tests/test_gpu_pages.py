@@ -423,3 +423,30 @@ def test_workspace_and_other_pages_stay_as_they_are(kind, ps, nb):
     kp, kl = kp.cuda(), i32([len(keep[b][0]) if b in keep else -1 for b in range(nb)])
     untouched(lambda: ikv.ikv_pages_compact(shape, cache, pages, kp, kl, c.ema, None, ws, n))
     m.compare()
+
+
+def test_compaction_of_many_table_entries():
+    """Block tables too long for the plan to write: sequences compacted, cut, emptied and left alone."""
+    nb, ps = 90, 7
+    c = make("f32", nb, ps, 64, 1, 0, [b % 9 for b in range(nb)], pool=900, cap=700, layers=1)
+    assert nb * c.max_pages > 8192
+    m, rng = Model(c), random.Random(8)
+    ws = c.pages_workspace()
+    shape, cache, pages = c.shape(), c.cache(c.cap), c.pages()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    lens = {b: (0, 10 + (11 * b) % 25) for b in range(nb)}
+    m.writable(lens)
+    ikv.ikv_pages_writable(shape, cache, pages, None, i32([n for _, n in lens.values()]), 40, None, ws, ws.numel())
+    m.compare()
+    m.write(lens, rng)
+    keep, kp, kl = {}, torch.zeros(nb, c.cap, dtype=torch.int32), []
+    for b in range(nb):
+        n = [m.len[b], 0, 5, m.len[b] - 3, None][b % 5]
+        kl.append(-1 if n is None else n)
+        if n is not None:
+            keep[b] = [list(range(n)) if b % 10 < 5 else sorted(rng.sample(range(m.len[b]), n))]
+            kp[b, :n] = torch.tensor(keep[b][0], dtype=torch.int32)
+    assert m.compact(keep) == 0
+    ikv.ikv_pages_compact(shape, cache, pages, kp.cuda(), i32(kl), c.ema, None, ws, ws.numel())
+    m.compare()
+    assert ikv.ikv_device_status() == 0
