@@ -114,7 +114,9 @@ __device__ __forceinline__ void copy_words(T *dst, const T *src, int64_t n, int6
     }
 }
 
-// CTAs (part, fork): the parent's table entries and counts, then its rows of pos, ema and vnorm.
+// CTAs (part, fork): part 0 the parent's table entries and counts, the others its rows of pos and vnorm,
+// and of ema.  Apart, because one CTA after another of them waits for memory: 30 forks of 8k slots with
+// release and writable 52.2 us, 53.9 when every CTA did a share of each.
 __global__ void __launch_bounds__(kRowThreads) fork_kernel(const PagesArgs a, const int32_t *src, const int32_t *dst) {
     pdl_wait();
     const int i = blockIdx.y, s = src[i], d = dst[i];
@@ -122,20 +124,36 @@ __global__ void __launch_bounds__(kRowThreads) fork_kernel(const PagesArgs a, co
         if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(&g_pages_error, 128u);
         return;
     }
-    const int64_t at = (int64_t)blockIdx.x * kRowThreads + threadIdx.x, step = (int64_t)gridDim.x * kRowThreads;
-    for (int64_t p = at; p < a.max_pages; p += step) {
-        const int e = a.table[(int64_t)s * a.max_pages + p];
-        a.table[(int64_t)d * a.max_pages + p] = e;
-        if (e > 0 && e < a.num_pages) atomicAdd(a.refs + e, 1);
+    if (blockIdx.x == 0) {
+        constexpr int U = 4;
+        const int32_t *from = a.table + (int64_t)s * a.max_pages;
+        int32_t *to = a.table + (int64_t)d * a.max_pages;
+        for (int p0 = threadIdx.x; p0 < a.max_pages; p0 += U * kRowThreads) {
+            int e[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) e[u] = p0 + u * kRowThreads < a.max_pages ? from[p0 + u * kRowThreads] : 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (p0 + u * kRowThreads < a.max_pages) to[p0 + u * kRowThreads] = e[u];
+                if (e[u] > 0 && e[u] < a.num_pages) atomicAdd(a.refs + e[u], 1);
+            }
+        }
+        if (threadIdx.x == 0) {
+            a.len[d] = a.len[s];
+            if (a.next_pos) a.next_pos[d] = a.next_pos[s];
+            if (a.start) a.start[d] = a.start[s];
+        }
+        return;
     }
-    if (at == 0) {
-        a.len[d] = a.len[s];
-        if (a.next_pos) a.next_pos[d] = a.next_pos[s];
-        if (a.start) a.start[d] = a.start[s];
-    }
+    // half of the other CTAs take pos and vnorm, half ema
+    const int parts = (gridDim.x - 1) / 2, part = (blockIdx.x - 1) % parts;
+    const int64_t at = (int64_t)part * kRowThreads + threadIdx.x, step = (int64_t)parts * kRowThreads;
     const int64_t n = (int64_t)a.rows_per_seq * a.cap;
+    if ((int)blockIdx.x > parts) {
+        if (a.ema) copy_words(a.ema + d * n, a.ema + s * n, n, at, step);
+        return;
+    }
     if (a.pos) copy_words(a.pos + d * n, a.pos + s * n, n, at, step);
-    if (a.ema) copy_words(a.ema + d * n, a.ema + s * n, n, at, step);
     if (a.vnorm) {
         const int64_t m = (int64_t)a.kv_heads * a.cap;
         for (int l = 0; l < a.layers; ++l)
@@ -557,8 +575,8 @@ cudaError_t launch_pages_release(const PagesArgs &a, int32_t extra, cudaStream_t
 cudaError_t launch_pages_fork(const PagesArgs &a, int32_t n, const int32_t *src, const int32_t *dst, cudaStream_t st) {
     const int64_t words = (int64_t)a.rows_per_seq * a.cap;
     const int64_t parts = (words + 8 * kRowThreads - 1) / (8 * kRowThreads);
-    const cudaError_t e = launch_k(fork_kernel, dim3((unsigned)(parts < 64 ? parts : 64), (unsigned)n), dim3(kRowThreads), 0,
-                                   st, a, src, dst);
+    const cudaError_t e = launch_k(fork_kernel, dim3((unsigned)(1 + 2 * (parts < 64 ? parts : 64)), (unsigned)n), dim3(kRowThreads),
+                                   0, st, a, src, dst);
     note_launch();
     return e;
 }
