@@ -214,7 +214,7 @@ int64_t ikv_launch_count(void);
  * attention kernel ran out (the kernel abandoned its work and returned);
  * bit 1: a split longer than the kernel's TMEM budget reached the device;
  * bit 2: an append found no free slot (start + len = cap) and was dropped, or
- * ikv_pages_writable was asked for slots past a sequence's slot space;
+ * ikv_pages_writable or ikv_pages_compact was asked for slots past a sequence's slot space;
  * bit 3: per-layer eviction, a sequence's next_pos reached cache->pos_cap (the token
  * was dropped); bit 4: a rank-trace set exceeded 16384 tokens (not traced);
  * bit 5: rows of ikv_q4_store or ikv_q4_load lay outside a sequence's slot space (left alone);
@@ -573,7 +573,8 @@ ikv_status ikv_pages_writable(const ikv_shape *shape, ikv_cache *cache, const ik
  * front of the first slot that moves stay as they are, shared or not; the survivors behind it are
  * gathered into free pages, and the old pages are given back (also when only the end was cut off,
  * which copies nothing).  start stays.  A sequence with keep_len < 0 is left alone.  keep and keep_len
- * as ikv_select_budget produces them; the rows of one sequence keep the same number.
+ * as ikv_select_budget produces them; the rows of one sequence keep the same number.  A keep_len past
+ * the slot space (start[b] + keep_len > cap) is cut to it and sets bit 2.
  *  lacking as in ikv_pages_writable: too few free pages leave everything as it was. */
 ikv_status ikv_pages_compact(const ikv_shape *shape, ikv_cache *cache, const ikv_pages *pages, const int32_t *keep,
                              const int32_t *keep_len, float *ema, int32_t *lacking, void *ws, size_t ws_bytes,

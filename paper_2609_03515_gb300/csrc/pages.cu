@@ -16,7 +16,10 @@ constexpr int kPlanThreads = 1024;
 constexpr int kCopyThreads = 256;
 constexpr int kRowThreads = 256;
 
-__device__ __forceinline__ int start_of(const PagesArgs &a, int b) { return a.start ? a.start[b] : 0; }
+// (within the slot space, whatever the array holds: table entries are found from it)
+__device__ __forceinline__ int start_of(const PagesArgs &a, int b) { return a.start ? min(max(a.start[b], 0), a.cap) : 0; }
+// slots that a sequence keeps in a compaction: no more than lie behind its start
+__device__ __forceinline__ int kept_of(const PagesArgs &a, int b, int keep_len) { return min(keep_len, a.cap - start_of(a, b)); }
 
 // Exclusive prefix sum of x over the CTA (kPlanThreads threads), and the total.
 __device__ __forceinline__ int block_scan(int x, int *total) {
@@ -343,7 +346,8 @@ compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
     const int lane = threadIdx.x & 31;
     for (int b = threadIdx.x >> 5; b < a.batch; b += kPlanThreads / 32) {
         const int64_t r0 = (int64_t)b * a.rows_per_seq;
-        const int n = min(keep_len[r0], a.cap);
+        const int asked = keep_len[r0], n = kept_of(a, b, asked);
+        if (n < asked && lane == 0) atomicOr(&g_pages_error, 4u);
         int begin = a.max_pages;  // a sequence that is left alone
         if (n >= 0) {
             int f = n;
@@ -394,8 +398,8 @@ compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
         if (lp >= w.begin[b]) commit_entry(a, w, b, lp);  // (none of a sequence left alone)
     }
     for (int b = threadIdx.x; b < a.batch; b += kPlanThreads) {
-        const int n = keep_len[(int64_t)b * a.rows_per_seq];
-        if (n >= 0) a.len[b] = min(n, a.cap);
+        const int n = kept_of(a, b, keep_len[(int64_t)b * a.rows_per_seq]);
+        if (n >= 0) a.len[b] = n;
     }
 }
 
@@ -510,7 +514,7 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
                 const int64_t r = a.rows_per_seq == 1 ? b : (int64_t)b * a.rows_per_seq + g0;
                 const int64_t j = (int64_t)(w.begin[b] + job - w.base[b]) * a.page_size + q0 + q - S;
                 RowMove m{-1, 0};
-                if (j >= 0 && j < min(keep_len[r], a.cap)) {
+                if (j >= 0 && j < min(keep_len[r], a.cap - S)) {
                     const int64_t from = (int64_t)S + keep[r * a.cap + j];
                     const int fp = (int)(from / a.page_size);
                     const int page = from >= 0 && fp < a.max_pages ? old[(int64_t)b * a.max_pages + fp] : -1;
@@ -537,10 +541,10 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
 // After the copies, where the plan left the tables to it: a CTA a sequence.
 __global__ void __launch_bounds__(kCopyThreads) compact_commit_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep_len) {
     pdl_wait();
-    const int b = blockIdx.x, n = keep_len[(int64_t)b * a.rows_per_seq];
+    const int b = blockIdx.x, n = kept_of(a, b, keep_len[(int64_t)b * a.rows_per_seq]);
     if (!w.total[1] || n < 0) return;
     for (int lp = w.begin[b] + threadIdx.x; lp < a.max_pages; lp += kCopyThreads) commit_entry(a, w, b, lp);
-    if (threadIdx.x == 0) a.len[b] = min(n, a.cap);
+    if (threadIdx.x == 0) a.len[b] = n;
 }
 
 }  // namespace

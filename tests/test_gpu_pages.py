@@ -450,3 +450,19 @@ def test_compaction_of_many_table_entries():
     ikv.ikv_pages_compact(shape, cache, pages, kp.cuda(), i32(kl), c.ema, None, ws, ws.numel())
     m.compare()
     assert ikv.ikv_device_status() == 0
+
+
+def test_compaction_past_the_slot_space():
+    """A keep_len that does not fit behind its start is cut to what does, and says so."""
+    c = make("bf16", 2, 16, 64, 1, 0, [8, 0], pool=20, cap=64)
+    ws = c.pages_workspace()
+    shape, cache, pages = c.shape(), c.cache(c.cap), c.pages()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    ikv.ikv_pages_writable(shape, cache, pages, None, i32([56, 30]), 56, None, ws, ws.numel())
+    c.len.copy_(i32([56, 30]))
+    table, refs = c.block_table.clone(), c.refs.clone()
+    keep = torch.arange(64, dtype=torch.int32, device="cuda").repeat(2, 1)
+    ikv.ikv_pages_compact(shape, cache, pages, keep, i32([64, 30]), c.ema, None, ws, ws.numel())
+    assert ikv.ikv_device_status() == 4
+    assert c.len.tolist() == [56, 30]
+    assert torch.equal(table, c.block_table) and torch.equal(refs, c.refs)
