@@ -604,7 +604,8 @@ cudaError_t launch_pages_writable(const PagesArgs &a, const PagesWs &w, const in
 
 cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int32_t *keep, const int32_t *keep_len,
                                  int32_t *lacking, int sms, cudaStream_t st) {
-    // up to 8192 entries the plan writes the tables; a launch after the copies for it takes longer
+    // up to 8192 entries the plan's one CTA writes the tables (a 32k prompt of 512 entries: 149.5 us, 152 with
+    // a launch behind the copies), in at most 8 rounds; above that a CTA a sequence does
     int32_t *old = (int64_t)a.batch * a.max_pages <= 8192 ? w.jobs : nullptr;
     cudaError_t e = launch_k(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, w, keep, keep_len, lacking, old);
     note_launch();

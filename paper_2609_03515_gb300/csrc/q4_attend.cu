@@ -14,7 +14,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kPair = 2;              // tiles of an iteration
 constexpr int kStages = 2;            // pairs of tiles a warp has in flight or in use
 // CTAs an SM holds: at 4, 128 channels lack the registers that 3 leave (32 x 16k, 28 / 4 heads: 56.3 us
-// against 52.6); 64 channels of bf16 queries have them (16 / 4 heads: 33.7 against 35.5)
+// where 3 took 52.6); 64 channels of bf16 queries have them (16 / 4 heads: 33.7 against 35.5)
 constexpr int ctas_per_sm(int head_dim, int elem_bytes) { return head_dim == 64 && elem_bytes == 2 ? 4 : 3; }
 constexpr int kSwitch = 12;           // what going from one unit to the next costs a CTA, in pairs of tiles
 constexpr float kMaxSlack = 6.f;      // log2: how far a logit may lie above the running reference
@@ -150,7 +150,8 @@ struct Run {
         return x >= base * kvh && x < (base + len) * kvh;
     }
 };
-// Up to 32 sequences: each warp for itself, a sequence a lane, with no barrier.  sp: the span of the first.
+// Up to 32 sequences: each warp for itself, a sequence a lane, with no barrier (1 x 3277 slots: 10.3 ->
+// 9.7 us).  sp: the span of the first.
 __device__ __forceinline__ Run run_of_few(const Q4AttendArgs &a, Span &sp) {
     const int lane = threadIdx.x & 31;
     Span mine{0, 0, 0, 0, 0};
@@ -258,9 +259,9 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a, Span &sp) {
 // Memory allows a tile of 128 channels 99 cycles of an SM.  It takes about 250 instructions (224
 // DUAL), 64 of them conversions of codes that fill the ALU pipe for 32 cycles; 12 warps issue some
 // 2.3 a cycle, which hides most of them.  32 sequences of 12k to 16k, 28 / 4 heads: 264 MB in
-// 52.6 us with the merge (5.0 TB/s), of which waiting for the tiles alone takes 47.8; one of 32k,
-// 32 / 8 heads, 38 MB in 12 us before its scores: lengths, table and first tiles are 4 of them,
-// the join 1.5.  A third stage is slower (54.5 us), a fourth CTA of 128 registers too (56.3).
+// 52.2 us with the merge (5.1 TB/s), of which waiting for the tiles alone takes 47.8; one of 32k,
+// 32 / 8 heads, 38 MB in 12 us, 17.6 with its scores: lengths, table and first tiles are 4 of them,
+// the join 1.5.  A third stage was slower (54.5 us where two took 52.6).
 template <int D, typename T, bool SCORE, bool DUAL>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend_kernel(const Q4AttendArgs a) {
     constexpr int Y = D / kQ4Group;        // groups of a row
