@@ -526,7 +526,8 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
  * changes them only through these calls, which hand out the lowest free pages first, in the
  * order of sequences and slots.  They write cache->block_table.  All are asynchronous and may be
  * captured in a graph.
- * The planes are the arrays paged alike: K and V, and for a 4-bit cache both scale pools.
+ * The planes are the arrays paged alike: K and V, and for a 4-bit cache both scale pools.  A pool of
+ * more than 0x7fff0000 pages is refused (IKV_ERR_SHAPE).
  * Writes into a page that several sequences hold reach them all: call ikv_pages_writable for the
  * slots that ikv_q4_store, ikv_append_token, ikv_step or ikv_compact_kv are about to write.
  * ------------------------------------------------------------------------- */

@@ -57,6 +57,7 @@ ikv_status check_pages(const ikv_shape *s, const ikv_cache *c, const ikv_pages *
     if (e) return e;
     if ((e = check_cache(s, c, need_pos))) return e;
     if (!p || !p->refs) return report(IKV_ERR_ARG, "pages or its refs is NULL");
+    if (c->num_pages > 0x7fff0000) return report(IKV_ERR_SHAPE, "too many pages");  // (the search counts past them)
     if (p->n_planes < 1 || p->n_planes > kMaxPlanes) return report(IKV_ERR_SHAPE, "n_planes outside [1, %d]", kMaxPlanes);
     for (int i = 0; i < p->n_planes; ++i) {
         if (!p->plane[i]) return report(IKV_ERR_ARG, "plane %d is NULL", i);

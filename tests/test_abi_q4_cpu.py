@@ -149,3 +149,9 @@ def test_page_calls_check_their_arguments():
         assert status(name, s, c, p, *args, A, ctypes.c_size_t(n - 1), None) == ikv.IKV_ERR_WORKSPACE
         assert status(name, s, c, p, *args, A + 8, big, None) == ikv.IKV_ERR_ALIGN
     assert status("ikv_pages_compact", s, c, p, None, A, None, None, A, big, None) == ikv.IKV_ERR_ARG
+
+
+def test_page_calls_refuse_pools_they_cannot_count():
+    c, p = cache(num_pages=0x7fffffff), pages()
+    assert status("ikv_pages_release", shape(), c, p, 0, None) == ikv.IKV_ERR_SHAPE
+    assert status("ikv_pages_workspace_size", shape(), c, p, ctypes.byref(ikv.SZ(0))) == ikv.IKV_ERR_SHAPE
