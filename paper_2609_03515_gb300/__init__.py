@@ -230,6 +230,8 @@ class Q4Cache(DecodeCache):
         [layers][tokens][kv_heads][head_dim] with the first row of every sequence in row0; any
         strides but the last."""
         st = k.stride()
+        if st[-1] != 1:
+            raise ValueError("the channels of a row must be contiguous")
         if row0 is not None:
             return ikv.ikv_rows(st[0], 0, st[1], st[2], row0.data_ptr())
         return ikv.ikv_rows(st[0], st[1], st[2], st[3], None)

@@ -238,6 +238,7 @@ ikv_status ikv_pages_fork(const ikv_shape *shape, ikv_cache *cache, const ikv_pa
     PagesArgs a{};
     const ikv_status e = check_pages(shape, cache, pages, false, &a);
     if (e) return e;
+    if (cache->pos_cap > 0) return report(IKV_ERR_UNSUPPORTED, "pos and ema laid out for per-layer eviction");
     if (n < 0 || n > shape->batch || n > 65535) return report(IKV_ERR_SHAPE, "n %d outside [0, batch]", n);
     if (n == 0) return IKV_OK;
     if (!src || !dst) return report(IKV_ERR_ARG, "src/dst is NULL");
@@ -269,6 +270,7 @@ ikv_status ikv_pages_compact(const ikv_shape *shape, ikv_cache *cache, const ikv
     PagesWs w;
     ikv_status e = check_pages(shape, cache, pages, false, &a);
     if (e) return e;
+    if (cache->pos_cap > 0) return report(IKV_ERR_UNSUPPORTED, "pos and ema laid out for per-layer eviction");
     if (!keep || !keep_len) return report(IKV_ERR_ARG, "keep/keep_len is NULL");
     if ((e = check_pages_ws(a, ws, ws_bytes, &w))) return e;
     a.ema = ema;

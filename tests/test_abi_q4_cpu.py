@@ -2,8 +2,9 @@
 import ctypes
 
 import pytest
+import torch
 
-from paper_2609_03515_gb300 import ikv
+from paper_2609_03515_gb300 import Q4Cache, ikv
 
 A = 64  # an address on a 16-byte boundary, never read
 
@@ -155,3 +156,17 @@ def test_page_calls_refuse_pools_they_cannot_count():
     c, p = cache(num_pages=0x7fffffff), pages()
     assert status("ikv_pages_release", shape(), c, p, 0, None) == ikv.IKV_ERR_SHAPE
     assert status("ikv_pages_workspace_size", shape(), c, p, ctypes.byref(ikv.SZ(0))) == ikv.IKV_ERR_SHAPE
+
+
+def test_forks_and_compactions_refuse_the_layout_of_per_layer_eviction():
+    s, c, p, big = shape(), cache(pos_cap=128), pages(), ctypes.c_size_t(1 << 30)
+    assert status("ikv_pages_fork", s, c, p, 1, A, A, A, None) == ikv.IKV_ERR_UNSUPPORTED
+    assert status("ikv_pages_compact", s, c, p, A, A, A, None, A, big, None) == ikv.IKV_ERR_UNSUPPORTED
+
+
+def test_dense_rows_with_strided_channels_are_refused():
+    c = Q4Cache(2, 1, 2, 2, 64, 64, device="cpu", page_size=16)
+    x = torch.zeros(1, 2, 8, 2, 64)
+    assert c.dense_rows(x.transpose(1, 2)).seq == x.stride(2)
+    with pytest.raises(ValueError):
+        c.dense_rows(x.transpose(3, 4))
