@@ -1,4 +1,5 @@
 // Decode attention over a cache held in 4 bits.
+#include <algorithm>
 #include <cfloat>
 #include <climits>
 #include <cstddef>
@@ -777,8 +778,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
 
 // The rest of a call: outputs of units of several segments (or of none: 0), Eq. 1's scores and Eq. 4.
 //
-// The first CTAs take a utility row's tokens, kFinishThreads / HS of them each, HS threads a token
-// that share the row's heads; the others merge a head's outputs (MANY: each a CTA, its warps a part of
+// The first CTAs take a utility row's tokens: kFinishThreads / HS of them each, HS threads a token
+// that share the row's heads, or blocks of V kFinishThreads, V tokens a thread, every row_ctas-th of the row; the others merge a head's outputs (MANY: each a CTA, its warps a part of
 // the segments each; else a head a warp).  A head's log-sum-exp comes from
 // its segments' (reference, sum) pairs, so no pass of its own has to gather it.
 constexpr int kFinishThreads = 512;
@@ -870,9 +871,33 @@ __device__ __forceinline__ void merge_any(const Q4FinishArgs &a, int x, float *r
                       static_cast<T *>(a.out) + (int64_t)hh * 32 * E, (float *)nullptr);
 }
 
-template <int HS, bool MANY>
-__global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4FinishArgs a) {
-    constexpr int kTok = kFinishThreads / HS, kAhead = 8, kWarpsF = kFinishThreads / 32, kHeads = 2;
+// A thread's V tokens.
+template <int V>
+struct Floats {
+    alignas(V * sizeof(float)) float x[V];
+    __device__ __forceinline__ void fill(float f) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = f;
+    }
+    __device__ __forceinline__ void load(const float *p) {
+        if (V == 4) *reinterpret_cast<float4 *>(x) = __ldcg(reinterpret_cast<const float4 *>(p));
+        else x[0] = __ldcg(p);
+    }
+    __device__ __forceinline__ void store(float *p, int n) const {  // n of them
+        if (V == 4 && n >= V) {
+            *reinterpret_cast<float4 *>(p) = *reinterpret_cast<const float4 *>(x);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v < n) p[v] = x[v];
+        }
+    }
+};
+
+template <int HS, bool MANY, int V>
+__global__ void __launch_bounds__(kFinishThreads, V == 1 ? 0 : 2) q4_finish_kernel(const Q4FinishArgs a) {
+    static_assert(HS == 1 || V == 1, "a thread's tokens are its own");
+    constexpr int kTok = kFinishThreads / HS * V, kAhead = V == 4 ? 4 : 8, kWarpsF = kFinishThreads / 32, kHeads = 2;
     extern __shared__ float lse[];  // [heads of a row]
     __shared__ float part[HS > 1 ? kFinishThreads : 1];
     __shared__ float room[kWarpsF * 128];  // of those that merge
@@ -892,22 +917,27 @@ __global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4Finis
         return;
     }
     const int r = blockIdx.x / a.row_ctas, b = r / a.rows_per_seq, block = blockIdx.x % a.row_ctas;
-    const int token = block * kTok + (threadIdx.x & (kTok - 1)), hs = threadIdx.x / kTok;
+    int token = block * kTok + (threadIdx.x & (kFinishThreads / HS - 1)) * V;
+    const int hs = threadIdx.x / (kFinishThreads / HS);
     const int h0 = a.rows_per_seq == 1 ? 0 : r % a.rows_per_seq * G;
     const int nh = a.rows_per_seq == 1 ? a.q_heads : G;
     const int64_t head0 = (int64_t)b * a.q_heads + h0;
     // whatever has an address goes out before anything is waited for
     const int L = a.len[b];
-    float z[kAhead], was = 0.f;
+    Floats<V> z[kAhead], was;
     const int64_t next = (int64_t)HS * a.lstride;  // from one of the thread's heads to its next
-    const float *zp = a.logits + (head0 + hs) * a.lstride + min(token, a.lstride - 1);
     const int mine = (nh - hs + HS - 1) / HS;      // the thread's heads: hs, hs + HS, ...
+    const float *zp = a.logits + (head0 + hs) * a.lstride + min(token, a.lstride - V);
     auto load = [&](int j0) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) z[j] = j0 + j < mine ? __ldcg(zp + (j0 + j) * next) : -INFINITY;
+        for (int j = 0; j < kAhead; ++j) {
+            if (j0 + j < mine) z[j].load(zp + (j0 + j) * next);
+            else z[j].fill(-INFINITY);
+        }
     };
     load(0);
-    if (a.ema && hs == 0 && token < a.cap) was = a.ema[(int64_t)r * a.cap + token];
+    was.fill(0.f);
+    if (a.ema && hs == 0 && token < a.cap) was.load(a.ema + (int64_t)r * a.cap + token);
     if (block * kTok >= L) return;  // (a sequence without slots has no segment count either)
     if (!MANY) {  // few segments: a head a thread
         for (int h = threadIdx.x; h < nh; h += kFinishThreads) {
@@ -980,24 +1010,38 @@ __global__ void __launch_bounds__(kFinishThreads) q4_finish_kernel(const Q4Finis
         }
     }
     __syncthreads();
-    float acc = 0.f;
-    for (int j0 = 0; j0 < mine; j0 += kAhead) {
-        if (j0) load(j0);
+    while (true) {
+        Floats<V> s;
+        s.fill(0.f);
+        for (int j0 = 0; j0 < mine; j0 += kAhead) {
+            if (j0) load(j0);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) acc += exp2_fast(z[j] - lse[min((j0 + j) * HS + hs, nh - 1)]);  // (past the last: 0)
-    }
-    if (HS > 1) {
-        part[threadIdx.x] = acc;
-        __syncthreads();
-        if (hs > 0) return;
+            for (int j = 0; j < kAhead; ++j)
 #pragma unroll
-        for (int k = 1; k < HS; ++k) acc += part[threadIdx.x + k * kTok];
+                for (int v = 0; v < V; ++v) s.x[v] += exp2_fast(z[j].x[v] - lse[min((j0 + j) * HS + hs, nh - 1)]);  // (past the last: 0)
+        }
+        if (HS > 1) {
+            part[threadIdx.x] = s.x[0];
+            __syncthreads();
+            if (hs > 0) return;
+#pragma unroll
+            for (int k = 1; k < HS; ++k) s.x[0] += part[threadIdx.x + k * kTok];
+        }
+        const int64_t to = (int64_t)r * a.cap + token;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            s.x[v] *= 1.f / (float)nh;
+            was.x[v] = a.alpha * was.x[v] + (1.f - a.alpha) * s.x[v];
+        }
+        if (a.score) s.store(a.score + to, L - token);
+        if (a.ema) was.store(a.ema + to, L - token);
+        if (V == 1) return;  // (a block a CTA)
+        token += a.row_ctas * kTok;
+        if (token >= L) return;
+        zp += a.row_ctas * kTok;
+        load(0);
+        if (a.ema) was.load(a.ema + (int64_t)r * a.cap + token);
     }
-    if (token >= L) return;
-    const float s = acc * (1.f / (float)nh);
-    const int64_t to = (int64_t)r * a.cap + token;
-    if (a.score) a.score[to] = s;
-    if (a.ema) a.ema[to] = a.alpha * was + (1.f - a.alpha) * s;
 }
 
 template <int D, typename T>
@@ -1014,15 +1058,16 @@ cudaError_t launch_t(const Q4AttendArgs &a, int ctas, cudaStream_t st) {
     return e;
 }
 
-template <int HS, bool MANY>
-cudaError_t launch_finish_t(Q4FinishArgs a, int64_t rows, int32_t max_len, cudaStream_t st) {
-    constexpr int tok = kFinishThreads / HS, heads = MANY ? 1 : kFinishThreads / 32;
-    a.row_ctas = (max_len + tok - 1) / tok;
+template <int HS, bool MANY, int V>
+cudaError_t launch_finish_t(Q4FinishArgs a, int64_t rows, int32_t max_len, int sms, cudaStream_t st) {
+    constexpr int tok = kFinishThreads / HS * V, heads = MANY ? 1 : kFinishThreads / 32;
+    const int blocks = (max_len + tok - 1) / tok;
+    a.row_ctas = V == 1 ? blocks : (int)std::min((int64_t)blocks, std::max(2 * (int64_t)sms / rows, (int64_t)1));
     const int64_t tokens = rows * a.row_ctas, merges = ((int64_t)a.batch * a.q_heads + heads - 1) / heads;
     if (tokens + merges > 0x7fffffff) return cudaErrorInvalidConfiguration;
     a.token_ctas = (int32_t)tokens;
     const int nh = a.rows_per_seq > 1 ? a.q_heads / a.kv_heads : a.q_heads;
-    const cudaError_t e = launch_k(q4_finish_kernel<HS, MANY>, dim3((unsigned)(tokens + merges)), dim3(kFinishThreads),
+    const cudaError_t e = launch_k(q4_finish_kernel<HS, MANY, V>, dim3((unsigned)(tokens + merges)), dim3(kFinishThreads),
                                    sizeof(float) * nh, st, a);
     note_launch();
     return e;
@@ -1031,10 +1076,16 @@ template <bool MANY>
 cudaError_t launch_finish(const Q4FinishArgs &a, int32_t max_len, int sms, cudaStream_t st) {
     const int64_t rows = a.score || a.ema ? (int64_t)a.batch * a.rows_per_seq : 0;
     // as many threads a token as it takes to give every SM a CTA
-    if (rows * ((max_len + kFinishThreads - 1) / kFinishThreads) >= sms) return launch_finish_t<1, MANY>(a, rows, max_len, st);
+    // as many tokens as four a thread take half of the SMs for: each CTA then gathers its row's log-sum-exps once
+    // for several blocks of them (32 x 12k to 16k, 4 rows a sequence, 28 heads: 92 -> 66 us with the attention;
+    // 32 ragged sequences of 4k to 8k, 32 heads: 59.4 -> 57.5; 16 of them are slower so)
+    const bool aligned = (reinterpret_cast<uintptr_t>(a.score) | reinterpret_cast<uintptr_t>(a.ema)) % 16 == 0;
+    if (aligned && rows > 0 && 2 * rows * ((max_len + 4 * kFinishThreads - 1) / (4 * kFinishThreads)) >= sms)
+        return launch_finish_t<1, MANY, 4>(a, rows, max_len, sms, st);
+    if (rows * ((max_len + kFinishThreads - 1) / kFinishThreads) >= sms) return launch_finish_t<1, MANY, 1>(a, rows, max_len, sms, st);
     if (rows * ((max_len + kFinishThreads / 4 - 1) / (kFinishThreads / 4)) >= sms)
-        return launch_finish_t<4, MANY>(a, rows, max_len, st);
-    return launch_finish_t<8, MANY>(a, rows, max_len, st);
+        return launch_finish_t<4, MANY, 1>(a, rows, max_len, sms, st);
+    return launch_finish_t<8, MANY, 1>(a, rows, max_len, sms, st);
 }
 
 }  // namespace

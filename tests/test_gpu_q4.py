@@ -441,3 +441,47 @@ def test_nothing_written_outside_the_buffers(lens, kvh, G, d, dtype):
     for t, was in zip(c.planes(), pools):
         assert torch.equal(t.view(torch.uint8), was.view(torch.uint8))
     check(c, 0, q, out[1:-1], score[1:-1], False, torch.ones_like(c.pos, dtype=torch.bool))
+
+
+@pytest.mark.parametrize("kvh,G,gran,dtype", [(2, 4, 1, ikv.IKV_BF16), (2, 2, 0, ikv.IKV_F32), (1, 7, 0, ikv.IKV_BF16)])
+@pytest.mark.parametrize("nb", [80, 160])
+def test_scores_of_many_tokens(kvh, G, gran, dtype, nb):
+    """Score passes whose threads take four tokens, one block of them or several, against one token a thread."""
+    gen = torch.Generator(device="cuda").manual_seed(nb + G)
+    d = 64
+    lens = [(37 * i) % 90 for i in range(nb)]
+    lens[3], lens[nb // 2], lens[nb - 1] = 4601, 2049, 4095
+    c = make(lens, kvh, G, d, 16, dtype, starts=[(3 * i) % 19 for i in range(nb)], layers=1, gran=gran, room=20)
+    noise(c, gen)
+    dt = torch.float32 if dtype == ikv.IKV_F32 else torch.bfloat16
+    x = torch.randn(1, nb, max(lens), kvh, d, generator=gen, device="cuda").to(dt)
+    ikv.ikv_q4_store(c.shape(), c.cache(max(lens)), c.q4(), 0, 1, x, x.flip(2), c.dense_rows(x), torch.zeros_like(c.len), c.len,
+                     max(lens))
+    live = torch.rand(c.pos.shape, generator=gen, device="cuda") > 0.3
+    c.pos.copy_(torch.where(live, c.pos, -1 - c.pos))
+    q = (2.0 * torch.randn(nb, G * kvh, d, generator=gen, device="cuda")).to(dt)
+    cch = c.cache(max(lens), dead_slots=True)
+    n = ikv.ikv_attend_workspace_size(c.shape(), cch)
+    ws = torch.full((n,), 0xAB, dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, 9.0)
+    was = torch.rand(c.rows, c.cap, generator=gen, device="cuda")
+    got = []
+    for shift in (0, 1):  # the second lies off the 16-byte boundaries
+        score = torch.full((c.rows * c.cap + 4,), -7.0, device="cuda")
+        ema = torch.zeros(c.rows * c.cap + 4, device="cuda")
+        inner = slice(shift, shift + c.rows * c.cap)
+        ema[inner] = was.flatten()
+        ikv.ikv_q4_attend_score(c.shape(), cch, c.q4(), 0, q, out, score[inner], ema[inner], 0.75, ws, n)
+        assert ikv.ikv_device_status() == 0
+        outside = torch.ones_like(score, dtype=torch.bool)
+        outside[inner] = False
+        assert bool((score[outside] == -7.0).all()) and bool((ema[outside] == 0.0).all())
+        got.append((score[inner].view(c.rows, c.cap), ema[inner].view(c.rows, c.cap)))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    score, ema = got[0]
+    check(c, 0, q, out, score, True, live)
+    inside = torch.arange(c.cap, device="cuda") < c.len.repeat_interleave(c.rows // nb)[:, None]
+    assert bool((score[~inside] == -7.0).all()) and torch.equal(ema[~inside], was[~inside])
+    # (two products and a sum, each rounded)
+    want = 0.75 * was.double() + 0.25 * score.double()
+    assert bool(((ema.double() - want).abs() <= want * 2.0 ** -22)[inside].all())
