@@ -529,7 +529,7 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
  * The planes are the arrays paged alike: K and V, and for a 4-bit cache both scale pools.  A pool of
  * more than 0x7fff0000 pages is refused (IKV_ERR_SHAPE).  ikv_pages_fork and ikv_pages_compact move rows
  * of pos and ema as "Utility rows" lays them out for the other modes, and refuse pos_cap > 0
- * (IKV_ERR_UNSUPPORTED).
+ * (IKV_ERR_UNSUPPORTED).  None of them goes by max_len.
  * Writes into a page that several sequences hold reach them all: call ikv_pages_writable for the
  * slots that ikv_q4_store, ikv_append_token, ikv_step or ikv_compact_kv are about to write.
  * ------------------------------------------------------------------------- */

@@ -55,7 +55,10 @@ ikv_status check_pages(const ikv_shape *s, const ikv_cache *c, const ikv_pages *
     clear_error();
     ikv_status e = check_shape(s);
     if (e) return e;
-    if ((e = check_cache(s, c, need_pos))) return e;
+    if (!c) return report(IKV_ERR_ARG, "cache is NULL");
+    ikv_cache same = *c;  // (no page call goes by max_len, so a bound past the slot space is one too)
+    if (c->max_len > 0) same.max_len = 0;
+    if ((e = check_cache(s, &same, need_pos))) return e;
     if (!p || !p->refs) return report(IKV_ERR_ARG, "pages or its refs is NULL");
     if (c->num_pages > 0x7fff0000) return report(IKV_ERR_SHAPE, "too many pages");  // (the search counts past them)
     if (p->n_planes < 1 || p->n_planes > kMaxPlanes) return report(IKV_ERR_SHAPE, "n_planes outside [1, %d]", kMaxPlanes);

@@ -170,3 +170,11 @@ def test_dense_rows_with_strided_channels_are_refused():
     assert c.dense_rows(x.transpose(1, 2)).seq == x.stride(2)
     with pytest.raises(ValueError):
         c.dense_rows(x.transpose(3, 4))
+
+
+def test_page_calls_do_not_go_by_max_len():
+    s, p = shape(), pages()
+    n = ikv.ikv_pages_workspace_size(s, cache(), p)
+    assert ikv.ikv_pages_workspace_size(s, cache(max_len=1000), p) == n  # a bound past the slot space
+    assert status("ikv_pages_release", s, cache(max_len=-1), p, 0, None) == ikv.IKV_ERR_SHAPE
+    assert status("ikv_pages_release", s, None, p, 0, None) == ikv.IKV_ERR_ARG
