@@ -179,6 +179,7 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
     const int64_t R = (int64_t)a.batch * span;
     FreePages pages{a.refs, a.num_pages};
     pages.load(0);
+    if (threadIdx.x == 0) w.total[2] = 0;  // rows of the longest copy
     // the entry of request i, or -1: page lp of sequence b
     auto request = [&](int64_t i, int *b, int *lp) -> int {
         if (i >= R) return -1;
@@ -206,7 +207,9 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
         const int64_t S = start_of(a, b), p0 = (int64_t)lp * a.page_size;
         const int r0 = (int)min(max(S - p0, (int64_t)0), (int64_t)a.page_size);
         const int r1 = (int)min(max(S + a.len[b] - p0, (int64_t)0), (int64_t)a.page_size);
-        *reinterpret_cast<int4 *>(w.jobs + 4 * (int64_t)rank) = make_int4(e, to, r0, e > 0 ? max(r1 - r0, 0) : 0);
+        const int rows = e > 0 ? max(r1 - r0, 0) : 0;
+        *reinterpret_cast<int4 *>(w.jobs + 4 * (int64_t)rank) = make_int4(e, to, r0, rows);
+        if (rows > 0) atomicMax(w.total + 2, rows);
     };
     auto report_total = [&](int total, int have) {
         if (threadIdx.x == 0) {
@@ -288,28 +291,33 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
     }
 }
 
-// Copies of jobs x layers x planes x KV heads: a run of rows each.  Bound by memory: 30 copies of
-// two pages of an 8k prompt, 32 layers (187 MB written, the pages read from L2) in 38 us.
-template <typename V>
+// Copies of jobs x layers x planes x KV heads: a run of rows each, by a CTA, or where all are short by a
+// warp.  Bound by memory: 30 copies of two pages of an 8k prompt, 32 layers (187 MB written, the pages
+// read from L2) in 38 us.
+// The short ones are new samples' first tokens: 42 copies of a token, 32 layers of 4 heads, in 14.3 us
+// with the fork, 29.4 by CTAs.
+constexpr int kWarpRun = 2048;  // bytes: up to four vectors a lane
+template <typename V, int THREADS>
 __device__ __forceinline__ void copy_run(unsigned char *dst, const unsigned char *src, int n) {
     constexpr int U = 4;
     const V *s = reinterpret_cast<const V *>(src);
     V *d = reinterpret_cast<V *>(dst);
     n /= (int)sizeof(V);
-    for (int i0 = threadIdx.x; i0 < n; i0 += kCopyThreads * U) {
+    for (int i0 = threadIdx.x % THREADS; i0 < n; i0 += THREADS * U) {
         V x[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i0 + u * kCopyThreads < n) x[u] = s[i0 + u * kCopyThreads];
+            if (i0 + u * THREADS < n) x[u] = s[i0 + u * THREADS];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i0 + u * kCopyThreads < n) d[i0 + u * kCopyThreads] = x[u];
+            if (i0 + u * THREADS < n) d[i0 + u * THREADS] = x[u];
     }
 }
-__global__ void __launch_bounds__(kCopyThreads) writable_copy_kernel(const PagesArgs a, const PagesWs w) {
-    pdl_wait();
-    const int64_t per = (int64_t)a.layers * a.n_planes * a.kv_heads, items = (int64_t)w.total[0] * per;
-    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
+template <int THREADS>  // of an item
+__device__ __forceinline__ void copy_items(const PagesArgs &a, const PagesWs &w, int jobs) {
+    constexpr int kTeams = kCopyThreads / THREADS;
+    const int64_t per = (int64_t)a.layers * a.n_planes * a.kv_heads, items = jobs * per;
+    for (int64_t i = (int64_t)blockIdx.x * kTeams + threadIdx.x / THREADS; i < items; i += (int64_t)gridDim.x * kTeams) {
         const int4 job = *reinterpret_cast<const int4 *>(w.jobs + 4 * (i / per));
         if (job.w <= 0) continue;
         const int x = (int)(i % per), g = x % a.kv_heads, y = x / a.kv_heads, pl = y % a.n_planes, l = y / a.n_planes;
@@ -318,9 +326,17 @@ __global__ void __launch_bounds__(kCopyThreads) writable_copy_kernel(const Pages
         unsigned char *d = a.plane[pl] + row(job.y);
         const unsigned char *s = a.plane[pl] + row(job.x);
         const int n = job.w * (int)rb;
-        if (rb % 16 == 0) copy_run<uint4>(d, s, n);
-        else copy_run<uint32_t>(d, s, n);
+        if (rb % 16 == 0) copy_run<uint4, THREADS>(d, s, n);
+        else copy_run<uint32_t, THREADS>(d, s, n);
     }
+}
+__global__ void __launch_bounds__(kCopyThreads) writable_copy_kernel(const PagesArgs a, const PagesWs w) {
+    pdl_wait();
+    int rb = 0;
+    for (int pl = 0; pl < a.n_planes; ++pl) rb = max(rb, a.row_bytes[pl]);
+    const int4 total = *reinterpret_cast<const int4 *>(w.total);
+    if ((int64_t)total.z * rb <= kWarpRun) copy_items<32>(a, w, total.x);
+    else copy_items<kCopyThreads>(a, w, total.x);
 }
 
 // A table entry from a sequence's first page made anew on: its old page is given back, its new one taken.
@@ -405,11 +421,13 @@ compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
 
 // Rows of new pages: slot j comes from slot keep[j] of the old pages.  CTAs take items of one layer
 // and as many new pages as make about kRowsAtOnce rows (small pages would leave most threads
-// idle); where a row comes from and goes to is looked up once for all planes, and heads that keep the
+// idle), or of fewer pages and heads where that leaves too few items for the CTAs that run at once (11
+// sequences cut to ~18 slots of 8 heads, 28 layers: 35.5 -> 16.7 us with the plan); where a row comes from and goes to is looked up once for all planes, and heads that keep the
 // same.  Bound by memory: a thread has kAhead vectors in flight.  A tenth of a 32k prompt, 32 layers
 // (859 MB moved in rows of 256 bytes) in 140 us, 6.1 TB/s; rows of 64 and 8 bytes (16 sequences in 4
 // bits, 337 MB) in 70.
 constexpr int kRowsAtOnce = 128;
+constexpr int kItemBytes = 16384;  // of a plane, at least: kAhead vectors a thread (with less, items of 16 KB cut to 4: 14.5 -> 18.0)
 struct RowMove {
     int64_t src, dst;  // rows of a plane, of the item's first head; src < 0: not moved
 };
@@ -464,14 +482,20 @@ __device__ __forceinline__ void gather_in_place(const PagesArgs &a, const int32_
     }
     const int n = min(keep_len[r], a.cap);
     const int32_t *k = keep + r * a.cap;
-    for (int j0 = 0; j0 < n; j0 += kCopyThreads * U) {
-        uint32_t v[U];
+    int from[U];  // a run ahead of the values: one trip to memory a run, not two (32768 slots: 22.3 -> 12.9 us)
+    auto load_keep = [&](int j0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = j0 + u * kCopyThreads + threadIdx.x;
-            const int from = j < n ? k[j] : 0;
-            v[u] = from >= 0 && from < a.cap ? row[from] : 0u;
+            from[u] = j < n ? k[j] : 0;
         }
+    };
+    load_keep(0);
+    for (int j0 = 0; j0 < n; j0 += kCopyThreads * U) {
+        uint32_t v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = from[u] >= 0 && from[u] < a.cap ? row[from[u]] : 0u;
+        load_keep(j0 + kCopyThreads * U);
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -482,7 +506,7 @@ __device__ __forceinline__ void gather_in_place(const PagesArgs &a, const int32_
 }
 __global__ void __launch_bounds__(kCopyThreads, 4)
 compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, const int32_t *old,
-                    int pages_at_once, int n_rows) {
+                    int pages_at_once, float units_a_job, int least_units, int n_rows) {
     pdl_wait();
     __shared__ RowMove moves[kRowsAtOnce];
     if (!w.total[1]) return;  // too few pages
@@ -490,13 +514,22 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
         gather_in_place(a, keep, keep_len, blockIdx.x);
         return;
     }
-    const int jobs = w.total[0];
+    const int jobs = w.total[0], ctas = (int)gridDim.x - n_rows;
     // heads that share their moves: all, or with a keep row for each KV head one
-    const int heads = a.rows_per_seq == 1 ? a.kv_heads : 1;
-    const int groups = (jobs + pages_at_once - 1) / pages_at_once, parts = a.kv_heads / heads;
+    int share = a.rows_per_seq == 1 ? a.kv_heads : 1, parts = a.kv_heads / share;
+    // fewer pages and heads an item, where there would be too few items for the CTAs that run at once
+    const int units = max((int)((float)jobs * units_a_job), least_units);
+    if (units < pages_at_once * share) {
+        pages_at_once = max(units / share, 1);
+        if (units < share) {
+            share = units;
+            parts = (a.kv_heads + share - 1) / share;
+        }
+    }
+    const int groups = (jobs + pages_at_once - 1) / pages_at_once;
     const int64_t items = (int64_t)groups * a.layers * parts;
-    for (int64_t it = (int)blockIdx.x - n_rows; it < items; it += (int)gridDim.x - n_rows) {
-        const int g0 = (int)(it % parts);
+    for (int64_t it = (int)blockIdx.x - n_rows; it < items; it += ctas) {
+        const int g0 = (int)(it % parts) * share, heads = min(share, a.kv_heads - g0);
         const int l = (int)(it / parts % a.layers), job0 = (int)(it / parts / a.layers) * pages_at_once;
         const int pages = min(pages_at_once, jobs - job0);
         for (int q0 = 0; q0 < a.page_size; q0 += kRowsAtOnce) {  // (pages longer than that: one of them, in parts)
@@ -615,8 +648,10 @@ cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int
     const int64_t ctas = items < 8 * (int64_t)sms ? items : 8 * (int64_t)sms;
     const int64_t rows = 2 * (int64_t)a.batch * a.rows_per_seq + (a.vnorm ? (int64_t)a.layers * a.batch * a.kv_heads : 0);
     if (rows + ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    const float units_a_job = 2.f * a.layers * a.kv_heads / (float)ctas;
+    const int least = kItemBytes / (a.page_size * a.row_bytes[0]);
     e = launch_k(compact_copy_kernel, dim3((unsigned)(rows + ctas)), dim3(kCopyThreads), 0, st, a, w, keep, keep_len,
-                 (const int32_t *)(old ? old : a.table), at_once, (int)rows);
+                 (const int32_t *)(old ? old : a.table), at_once, units_a_job, least > 1 ? least : 1, (int)rows);
     note_launch();
     if (e != cudaSuccess || old) return e;
     e = launch_k(compact_commit_kernel, dim3((unsigned)a.batch), dim3(kCopyThreads), 0, st, a, w, keep_len);

@@ -466,3 +466,31 @@ def test_compaction_past_the_slot_space():
     assert ikv.ikv_device_status() == 4
     assert c.len.tolist() == [56, 30]
     assert torch.equal(table, c.block_table) and torch.equal(refs, c.refs)
+
+
+@pytest.mark.parametrize("kind,ps,d,kvh,norms", [("bf16", 64, 128, 3, False), ("f32", 64, 128, 5, True), ("f32", 33, 128, 7, False),
+                                                 ("q4", 128, 128, 8, False)])
+def test_compactions_cut_into_some_of_the_heads(kind, ps, d, kvh, norms):
+    """Rows long enough that few pages are moved in items of fewer heads than share their moves."""
+    test_random_life_of_a_pool(kind, ps, d, kvh, 0, norms, 2)
+
+
+def test_copies_of_a_row_and_of_many():
+    """Writable pages whose copies are all short (a warp's each), and one long among them."""
+    for longest in (1, 16, 17, 64):
+        c = make("bf16", 4, 64, 64, 2, 0, [0, 0, 0, 0], pool=12, cap=128)
+        m, rng = Model(c), random.Random(longest)
+        ws = c.pages_workspace()
+        shape, cache, pages = c.shape(), c.cache(c.cap), c.pages()
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        first = {0: (0, 1), 1: (0, longest)}
+        m.writable(first)
+        ikv.ikv_pages_writable(shape, cache, pages, i32([0, 0, -1, -1]), i32([1, longest, 0, 0]), 64, None, ws, ws.numel())
+        m.write(first, rng)
+        m.fork([(0, 2), (1, 3)])
+        ikv.ikv_pages_fork(shape, cache, pages, 2, i32([0, 1]), i32([2, 3]), c.ema)
+        n = min(longest, 63)  # the page's last slot at the latest
+        m.writable({2: (1, 1), 3: (n, 1)})
+        ikv.ikv_pages_writable(shape, cache, pages, i32([-1, -1, 1, n]), None, 1, None, ws, ws.numel())
+        m.compare()
+        assert ikv.ikv_device_status() == 0
