@@ -422,7 +422,8 @@ compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
 // Rows of new pages: slot j comes from slot keep[j] of the old pages.  CTAs take items of one layer
 // and as many new pages as make about kRowsAtOnce rows (small pages would leave most threads
 // idle), or of fewer pages and heads where that leaves too few items for the CTAs that run at once (11
-// sequences cut to ~18 slots of 8 heads, 28 layers: 35.5 -> 16.7 us with the plan); where a row comes from and goes to is looked up once for all planes, and heads that keep the
+// sequences cut to ~18 slots of 8 heads, 28 layers: 37.7 -> 16.0 us with the plan; a tenth of a 32k prompt,
+// one layer: 43 -> 17); where a row comes from and goes to is looked up once for all planes, and heads that keep the
 // same.  Bound by memory: a thread has kAhead vectors in flight.  A tenth of a 32k prompt, 32 layers
 // (859 MB moved in rows of 256 bytes) in 140 us, 6.1 TB/s; rows of 64 and 8 bytes (16 sequences in 4
 // bits, 337 MB) in 70.
@@ -517,14 +518,13 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
     const int jobs = w.total[0], ctas = (int)gridDim.x - n_rows;
     // heads that share their moves: all, or with a keep row for each KV head one
     int share = a.rows_per_seq == 1 ? a.kv_heads : 1, parts = a.kv_heads / share;
-    // fewer pages and heads an item, where there would be too few items for the CTAs that run at once
+    // fewer pages and heads an item, where there would be fewer items than a quarter of the CTAs (two an SM)
+    // (halves: powers of two stay so, which gather_plane divides by)
     const int units = max((int)((float)jobs * units_a_job), least_units);
-    if (units < pages_at_once * share) {
-        pages_at_once = max(units / share, 1);
-        if (units < share) {
-            share = units;
-            parts = (a.kv_heads + share - 1) / share;
-        }
+    while (pages_at_once > 1 && pages_at_once * share > units) pages_at_once = (pages_at_once + 1) >> 1;
+    if (share > units) {
+        while (share > units) share = (share + 1) >> 1;
+        parts = (a.kv_heads + share - 1) / share;
     }
     const int groups = (jobs + pages_at_once - 1) / pages_at_once;
     const int64_t items = (int64_t)groups * a.layers * parts;
@@ -648,7 +648,7 @@ cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int
     const int64_t ctas = items < 8 * (int64_t)sms ? items : 8 * (int64_t)sms;
     const int64_t rows = 2 * (int64_t)a.batch * a.rows_per_seq + (a.vnorm ? (int64_t)a.layers * a.batch * a.kv_heads : 0);
     if (rows + ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    const float units_a_job = 2.f * a.layers * a.kv_heads / (float)ctas;
+    const float units_a_job = 4.f * a.layers * a.kv_heads / (float)ctas;
     const int least = kItemBytes / (a.page_size * a.row_bytes[0]);
     e = launch_k(compact_copy_kernel, dim3((unsigned)(rows + ctas)), dim3(kCopyThreads), 0, st, a, w, keep, keep_len,
                  (const int32_t *)(old ? old : a.table), at_once, units_a_job, least > 1 ? least : 1, (int)rows);
