@@ -52,7 +52,7 @@ __device__ __forceinline__ void finish_split(const AttendArgs &a, float *obuf, f
             acc += obuf[(w * G + h) * D + e] * f;
         }
         if (ns_active == 1) {
-            store_as(static_cast<T *>(a.out) + (hrow + h) * D + e, sum > 0.f ? acc / sum : 0.f);
+            store_as(static_cast<T *>(a.out) + (hrow + h) * D + e, over_sum(acc, sum));
             if (e == 0) a.lse2[lrow + h] = sum > 0.f ? M + log2f(sum) : -INFINITY;
         } else {
             const int64_t at = pbase + (int64_t)h * a.n_splits + s;

@@ -706,11 +706,12 @@ __global__ void __launch_bounds__(kThreads, 2)
                 fence_before_sync();
                 mbar_arrive(o_free);
                 // fold the pass into the running (max, sum, output); a pass whose rows are
-                // all dead (mx = -inf, sum = 0, O = 0) leaves them unchanged
+                // all dead (mx = -inf, sum = 0, O = 0) leaves them unchanged, one whose logits are
+                // all NaN (mx = -inf, sum = NaN) makes them NaN
 #pragma unroll
                 for (int h = 0; h < G; ++h) {
                     const float mn = fmaxf(M[h], mx[h]);
-                    if (mn != -INFINITY) {
+                    if (mn != -INFINITY || sum[h] != 0.f) {
                         const float a_old = exp2f(M[h] - mn), a_new = exp2f(mx[h] - mn);
                         acc[h] = acc[h] * a_old + o[h] * a_new;
                         W[h] = W[h] * a_old + sum[h] * a_new;
@@ -734,7 +735,7 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll
                 for (int h = 0; h < G; ++h)
                     a.out[(((int64_t)li * a.batch + b) * H + (int64_t)g * G + h) * kD + tid] =
-                        __float2bfloat16_rn(W[h] > 0.f ? acc[h] / W[h] : 0.f);
+                        __float2bfloat16_rn(over_sum(acc[h], W[h]));
                 if (tid < G) {
                     float mm = -INFINITY, ss = 0.f;
 #pragma unroll

@@ -19,6 +19,10 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
+// An output over its sum of weights.  That is 0 only where no slot is live; a NaN one (of a NaN logit)
+// has to leave NaN.
+__device__ __forceinline__ float over_sum(float acc, float sum) { return sum == 0.f ? 0.f : acc / sum; }
+
 // ml: the head's n <= kMaxSplits (max, sum) pairs, po: its partial outputs [n][32 E]; out gets
 // their merged output (32 E values), lse2 (or null) the log2-sum-exp.  wq: kMaxSplits floats
 // of shared memory of the calling warp.  The (max, sum) pairs give each partial's weight, then
@@ -75,7 +79,7 @@ __device__ __forceinline__ void merge_head(const float2 *ml, const float *po, in
         }
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) store_as(out + lane * E + e, W > 0.f ? acc[e] / W : 0.f);
+    for (int e = 0; e < E; ++e) store_as(out + lane * E + e, over_sum(acc[e], W));
     if (lse2 && lane == 0) *lse2 = W > 0.f ? M + log2f(W) : -INFINITY;
     __syncwarp();
 }
