@@ -18,8 +18,11 @@ constexpr int kStages = 2;            // pairs of tiles a warp has in flight or 
 // where 3 took 52.6); 64 channels of bf16 queries have them (16 / 4 heads: 33.7 against 35.5)
 constexpr int ctas_per_sm(int head_dim, int elem_bytes) { return head_dim == 64 && elem_bytes == 2 ? 4 : 3; }
 constexpr int kSwitch = 12;           // what going from one unit to the next costs a CTA, in pairs of tiles
-constexpr float kMaxSlack = 6.f;      // log2: how far a logit may lie above the running reference
-constexpr float kScaleRoom = 256.f;   // how far a V scale may grow, normalised, before it is renormalised
+constexpr float kMaxSlack = 7.f;      // log2: how far a logit may lie above the running reference
+constexpr float kScaleRoom = 256.f;   // a V scale's most, normalised, before its group is normalised again (a weight's: 2^15)
+// powers of two that V scales are multiplied by: the first of a group brings its smallest (2^-123) to 2^3 and
+// its inverse is a normal number; the largest scale takes 2^-120
+constexpr int kNormFirst = 126;
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 // The cache is read once: it goes out of L2 before the logits and partials, which are read again.
@@ -75,6 +78,26 @@ constexpr float kLowUp = 2048.f;
 __device__ __forceinline__ uint32_t shrink(uint32_t x) {
     const __half2 h = __hmul2(*reinterpret_cast<const __half2 *>(&x), __float2half2_rn(1.f / kLowUp));
     return *reinterpret_cast<const uint32_t *>(&h);
+}
+// 2^e for whole e <= 127: exact, 0 below 2^-126 (and for a NaN)
+__device__ __forceinline__ float pow2(float e) { return __int_as_float(((int)fmaxf(e, -127.f) + 127) << 23); }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {  // (of a number and NaN: the number)
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// A group's power of two, in the half of norm that starts at bit `at`: such that its largest scale, in the
+// same half of most, comes to 2^4 .. 2^5.  Returns what its outputs so far are multiplied by (0 where
+// they are nothing beside the new ones).
+__device__ __forceinline__ float renorm(uint32_t &norm, uint32_t most, int at) {
+    const int was = norm >> (at + 7) & 255, e = 127 + 4 + 127 - (int)min(most >> (at + 7) & 255u, 251u);
+    norm = (norm & ~(0xffffu << at)) | (uint32_t)e << (at + 7);
+    return pow2((float)(e - was));
 }
 __device__ __forceinline__ float bf16_lo(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
@@ -248,10 +271,14 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a, Span &sp) {
 // (bf16 queries: exact down to 2^-22 of the largest; fp32 queries: two terms).
 // O^T = V^T P^T: the rows are channels, the depth the 16 tokens; V's scales, which differ from
 // token to token, multiply the probabilities instead, once for each group of channels, in fp32
-// before they are rounded to fp16 (fp32 outputs: two terms).  Normalised by a power of two
-// that follows the largest scale seen, they stay within fp16's range.
-// The softmax runs on a reference that is at most 2^6 below the largest logit, so the sums are
-// rescaled a few times a sequence and no tile waits for a maximum across lanes.
+// before they are rounded to fp16 (fp32 outputs: two terms, 2^-22 of a weight; bf16 outputs: one, 2^-11
+// of each, at most an eighth of what the output's own rounding does).  Each group of channels has a power of
+// two that follows its largest scale seen and that its scales are multiplied by (exactly, two
+// groups an instruction), so the weights stay within fp16's range however large or small V is,
+// and a group of small channels beside one of large loses nothing.
+// The softmax runs on a whole number of log2 units as its reference, at most 2^7 below the largest
+// logit: the sums are rescaled a few times a sequence, exactly, and no tile waits for a
+// maximum across lanes.  Weights and their sums know nothing of V's scales.
 // DUAL (groups of four heads or fewer): a pair of tiles shares the columns, the first's logits in
 // columns 0 to 3 and the second's in 4 to 7, each with an operand that is zero in the other's
 // columns; logits, weights and scales then take half the instructions, and a head's two columns
@@ -462,8 +489,9 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
     float ref[2] = {-FLT_MAX, -FLT_MAX}, sum[2] = {0.f, 0.f};
-    // weights carry 2^norm_e, so that V scales times it stay within kScaleRoom while they are <= room
-    float norm_e = 0.f, room = -1.f;
+    uint32_t norm[Y / 2];  // bf16: what the scales of groups 2 y and 2 y + 1 are multiplied by
+#pragma unroll
+    for (int y = 0; y < Y / 2; ++y) norm[y] = (uint32_t)(kNormFirst + 127) * 0x00800080u;
 
     const int tok0 = perm_of_row(g);  // tokens of rows g and g + 8: tok0, tok0 + 8
     // One pair of tiles; MASK: some of its slots are not the sequence's, or dead.  A lane's columns
@@ -534,7 +562,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
                     if (lg1) lg[j + a.lstride] = z[v][2 * r + 1] * post[1];
                 }
             }
-        // ---- V scales of rows g and g + 8 (0 where the slot is none of the sequence's, whatever it holds)
+        // ---- V scales of rows g and g + 8 (0 where the slot is none of the sequence's, whatever it holds),
+        // normalised
+        auto scale_of = [&](int v, int r, int y) -> uint32_t {
+            const uint32_t w = reinterpret_cast<const uint32_t *>(tiles[v + my_tile].vs + (tok0 + 8 * r) * Tile<D>::kScaleRow)[y];
+            return in[v][r] ? w : 0u;
+        };
         uint32_t sv[NZ][2][Y / 2];
         float big = 0.f;
 #pragma unroll
@@ -543,25 +576,23 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
             for (int r = 0; r < 2; ++r)
 #pragma unroll
                 for (int y = 0; y < Y / 2; ++y) {
-                    const uint32_t w =
-                        reinterpret_cast<const uint32_t *>(tiles[v + my_tile].vs + (tok0 + 8 * r) * Tile<D>::kScaleRow)[y];
-                    sv[v][r][y] = in[v][r] ? w : 0u;
+                    sv[v][r][y] = mul_bf16x2(scale_of(v, r, y), norm[y]);
                     big = max3(big, bf16_lo(sv[v][r][y]), bf16_hi(sv[v][r][y]));
                 }
-        // ---- running reference of the logits, norm of the scales; a weight is 2^(logit - less)
-        float less[2] = {ref[0] - norm_e, ref[1] - norm_e}, d[NZ][4], over = -FLT_MAX;
+        // ---- running reference of the logits, norms of the scales; a weight is 2^(logit - ref)
+        float d[NZ][4], over = -FLT_MAX;
         auto weigh = [&]() {
 #pragma unroll
             for (int v = 0; v < NZ; ++v)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) d[v][e] = fmaf(z[v][e], post[e & 1], -less[e & 1]);
+                for (int e = 0; e < 4; ++e) d[v][e] = fmaf(z[v][e], post[e & 1], -ref[e & 1]);
         };
         weigh();
 #pragma unroll
         for (int v = 0; v < NZ; ++v)
 #pragma unroll
             for (int c = 0; c < 2; ++c) over = max3(over, d[v][c], d[v][2 + c]);
-        if (__any_sync(0xffffffffu, over > kMaxSlack + norm_e || big > room)) {
+        if (__any_sync(0xffffffffu, over > kMaxSlack || big > kScaleRoom)) {
             float f[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
@@ -570,33 +601,36 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
                 for (int v = 0; v < NZ; ++v) m = max3(m, z[v][c], z[v][2 + c]);
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-                m = fmaxf(ref[c], m * post[c]);
-                f[c] = exp2_fast(ref[c] - m);
+                m = fmaxf(ref[c], floorf(m * post[c]));
+                f[c] = pow2(ref[c] - m);
                 ref[c] = m;
-            }
-#pragma unroll
-            for (int x = 1; x < 32; x <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, x));
-            if (big > room) {
-                // (2^104: a weight of 2^6 and a sum of 2^16 of them stay finite)
-                const float e = big > 0.f ? (float)(4 - max(ilogbf(big), -100)) : norm_e;
-                // (nothing summed before the first)
-                const float up = room < 0.f ? 1.f : ldexpf(1.f, (int)(e - norm_e));
-                f[0] *= up;
-                f[1] *= up;
-                norm_e = e;
-                room = big > 0.f ? kScaleRoom * ldexpf(1.f, -(int)e) : 0.f;
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
                 sum[c] *= f[c];
-                less[c] = ref[c] - norm_e;
-#pragma unroll
-                for (int j = 0; j < 2 * Y; ++j) {
-                    o[j][c] *= f[c];
-                    o[j][2 + c] *= f[c];
-                }
             }
             weigh();
+#pragma unroll
+            for (int y = 0; y < Y / 2; ++y) {
+                uint32_t m = 0u;  // the largest scales of two groups
+#pragma unroll
+                for (int v = 0; v < NZ; ++v)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) m = max_bf16x2(m, scale_of(v, r, y));
+#pragma unroll
+                for (int x = 1; x < 32; x <<= 1) m = max_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, x));
+                const uint32_t most = mul_bf16x2(m, norm[y]);
+                float up[2] = {1.f, 1.f};
+                if (bf16_lo(most) > kScaleRoom) up[0] = renorm(norm[y], m, 0);
+                if (bf16_hi(most) > kScaleRoom) up[1] = renorm(norm[y], m, 16);
+#pragma unroll
+                for (int yy = 0; yy < 2; ++yy)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[2 * (2 * y + yy) + h][e] *= f[e & 1] * up[yy];
+#pragma unroll
+                for (int v = 0; v < NZ; ++v)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) sv[v][r][y] = mul_bf16x2(scale_of(v, r, y), norm[y]);
+            }
         }
         float p[NZ][4];
 #pragma unroll
@@ -718,19 +752,22 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], d);
     __syncthreads();  // every ring is done with
-    const float back = ldexpf(1.f, -(int)norm_e);
-    if (g == 0) {
-        ml[warp * 8 + 2 * t] = make_float2(ref[0], sum[0] * back);
-        ml[warp * 8 + 2 * t + 1] = make_float2(ref[1], sum[1] * back);
-    }
+    // Sums are brought into [1/2, 1) by the reference, which stays a whole number: outputs are then no
+    // larger than the largest value, whatever the number of tokens.
 #pragma unroll
-    for (int y = 0; y < Y; ++y)
+    for (int c = 0; c < 2; ++c) {
+        const int bits = __float_as_int(sum[c]) >> 23, up = bits > 0 && bits < 255 ? bits - 126 : 0;
+        const float down = pow2((float)-up);
+        if (g == 0) ml[warp * 8 + 2 * t + c] = make_float2(ref[c] + (float)up, sum[c] * down);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int y = 0; y < Y; ++y) {
+            const float back = __uint_as_float((254u - (norm[y >> 1] >> (16 * (y & 1) + 7) & 255u)) << 23);
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+            for (int h = 0; h < 2; ++h)
                 *reinterpret_cast<float2 *>(po + (warp * 8 + 2 * t + c) * D + 32 * y + 4 * g + 2 * h) =
-                    make_float2(o[2 * y + h][c] * back, o[2 * y + h][2 + c] * back);
+                    make_float2(o[2 * y + h][c] * down * back, o[2 * y + h][2 + c] * down * back);
+        }
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < G * (D / 4); i += kThreads) {
         const int h = i / (D / 4), e = i % (D / 4) * 4;
@@ -740,13 +777,16 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
         float m = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kParts; ++w) m = fmaxf(m, ml[part(w)].x);
-        const float base = m == -INFINITY ? 0.f : m;
+        // (so far above the largest that neither the sum over the warps here nor the one over the
+        // segments later passes the largest value)
+        const float base = m == -INFINITY ? 0.f : m + (sg.segs == 1 ? 3.f : 10.f);
+        static_assert(kParts <= 8 && kMaxSplits <= 128, "2^3 and 2^7 of them");
         float l = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kParts; ++w) {
             const float2 y = ml[part(w)];
-            const float f = exp2f(y.x - base);
+            const float f = pow2(y.x - base);
             const float4 v = *reinterpret_cast<const float4 *>(po + part(w) * D + e);
             l += f * y.y;
             x.x += f * v.x;
@@ -762,11 +802,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
             store_as(dst + 1, x.y * inv);
             store_as(dst + 2, x.z * inv);
             store_as(dst + 3, x.w * inv);
-            if (e == 0) a.lse2[head] = l == 0.f ? -INFINITY : m + log2f(l);
+            if (e == 0) a.lse2[head] = l == 0.f ? -INFINITY : base + log2f(l);
         } else {
             const int64_t to = head * kMaxSplits + ((int)blockIdx.x - sg.seg0);
             *reinterpret_cast<float4 *>(a.part_o + to * D + e) = x;
-            if (e == 0) reinterpret_cast<float2 *>(a.part_ml)[to] = make_float2(m, l);
+            if (e == 0) reinterpret_cast<float2 *>(a.part_ml)[to] = make_float2(m == -INFINITY ? m : base, l);
         }
     }
     // ---- the run goes on in the next unit
