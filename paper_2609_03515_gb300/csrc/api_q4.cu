@@ -156,7 +156,7 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     if (!q || !out) return report(IKV_ERR_ARG, "q/out is NULL");
     if (!aligned16(q) || !aligned16(out)) return report(IKV_ERR_ALIGN, "q/out must be 16-byte aligned");
     if (ema && !(alpha >= 0.f && alpha <= 1.f)) return report(IKV_ERR_ARG, "alpha must be in [0, 1]");
-    if (shape->q_heads > 8192) return report(IKV_ERR_UNSUPPORTED, "more than 8192 query heads");
+    if (shape->q_heads > kMaxQ4Heads) return report(IKV_ERR_UNSUPPORTED, "more than %d query heads", kMaxQ4Heads);
     const bool want_score = score || ema;
     const AttendWs w = attend_ws(shape, cap_of(cache), 1, want_score);
     if (!ws || ws_bytes < w.end) return report(IKV_ERR_WORKSPACE, "workspace needs %zu bytes", w.end);
@@ -178,10 +178,10 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     a.cap = cap_of(cache);
     a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)shape->head_dim));
     a.logits = want_score ? at<float>(ws, w.logits) : nullptr;
+    a.post = at<float>(ws, w.lse2);  // (the same size)
     a.lstride = logit_stride(a.cap);
     a.part_ml = at<float>(ws, w.part_ml);
     a.part_o = at<float>(ws, w.part_o);
-    a.lse2 = at<float>(ws, w.lse2);
     a.segs = at<int32_t>(ws, w.arrivals);
     // (the kernels count the sequences' pairs of tiles in 32 bits, with some to spare for each unit)
     if ((int64_t)shape->batch * shape->kv_heads * (a.cap / 32 + 64) > 0x30000000)
@@ -204,8 +204,8 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     f.bf16 = shape->dtype == IKV_BF16;
     f.segs = a.segs;
     f.logits = a.logits;
+    f.post = a.post;
     f.lstride = a.lstride;
-    f.lse2 = a.lse2;
     f.part_ml = a.part_ml;
     f.part_o = a.part_o;
     f.out = out;

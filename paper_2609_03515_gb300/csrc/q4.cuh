@@ -10,6 +10,7 @@ namespace ikv {
 // largest magnitude; a code is a sign and one of the magnitudes 0, .5, 1, 1.5, 2, 3, 4, 6 of s
 // (the E2M1 numbers, which the GPU converts two at a time).
 constexpr int kQ4Group = 32;
+constexpr int kMaxQ4Heads = 8192;  // query heads
 constexpr int kQ4Tile = 16;  // page sizes are multiples of it: the rows of one mma tile lie in one page
 
 // the two codes in byte i of w, as fp16 (exact)
@@ -58,10 +59,12 @@ struct Q4AttendArgs {
     void *out;                        // the same
     int32_t batch, q_heads, layer, rows_per_seq, cap;
     float scale_log2;
-    float *logits;                    // [batch][q_heads][lstride] log2-domain logits, or null
+    float *logits;                    // [batch][q_heads][lstride] logits; post of their head times them is
+                                      // log2 of the weights.  Or null
+    float *post;                      // [batch][q_heads] (of sequences that have a slot)
     int32_t lstride;
-    float *part_ml, *part_o;          // [batch][q_heads][kMaxSplits][2], [..][D]: units of several segments
-    float *lse2;                      // [batch][q_heads]: units of one segment
+    float *part_ml, *part_o;          // [batch][q_heads][kMaxSplits][2], [..][D]: reference and sum of each
+                                      // segment, and outputs of units of several
     int32_t *segs;                    // [batch][kv_heads] segments of a unit (of sequences that have a slot)
 };
 // CTAs of an attention launch at lengths up to max_len
@@ -73,7 +76,7 @@ struct Q4FinishArgs {
     int32_t batch, q_heads, kv_heads, rows_per_seq, cap, head_dim, bf16;
     const float *logits;
     int32_t lstride;
-    const float *lse2, *part_ml, *part_o;
+    const float *post, *part_ml, *part_o;
     const int32_t *segs;
     void *out;
     float alpha;

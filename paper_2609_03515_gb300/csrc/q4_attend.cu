@@ -262,7 +262,7 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a, Span &sp) {
     return run;
 }
 
-// softmax(q K^T / sqrt d) V for a CTA's segments, and the log2-domain logits of their slots.
+// softmax(q K^T / sqrt d) V for a CTA's segments, and the logits of their slots, over a.post.
 //
 // S^T = K q^T: the tile's 16 tokens are the rows of an mma, its 8 columns the heads of the
 // group (a group of 8 or fewer), 16 channels its depth.  A group of 32 channels is two of them
@@ -474,6 +474,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
                 }
             }
         const float mine = a.scale_log2 * ldexpf(1.f, e - 7);
+        if (SCORE && first == 0 && threadIdx.x < 32 && t == 0 && g < G && (!DUAL || g < 4)) a.post[head0 + g] = mine;
         post[0] = __shfl_sync(0xffffffffu, mine, 8 * t);
         post[1] = __shfl_sync(0xffffffffu, mine, 8 * t + 4);
     }
@@ -558,8 +559,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
                 for (int c = 0; c < 2; ++c)
                     if (!in[v][r]) z[v][2 * r + c] = -INFINITY;
                 if (SCORE && have) {
-                    if (lg0) lg[j] = z[v][2 * r] * post[0];
-                    if (lg1) lg[j + a.lstride] = z[v][2 * r + 1] * post[1];
+                    if (lg0) lg[j] = z[v][2 * r];
+                    if (lg1) lg[j + a.lstride] = z[v][2 * r + 1];
                 }
             }
         // ---- V scales of rows g and g + 8 (0 where the slot is none of the sequence's, whatever it holds),
@@ -794,7 +795,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
             x.z += f * v.z;
             x.w += f * v.w;
         }
-        const int64_t head = head0 + h;
+        const int64_t head = head0 + h, to = head * kMaxSplits + ((int)blockIdx.x - sg.seg0);
         if (sg.segs == 1) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
             T *dst = static_cast<T *>(a.out) + head * D + e;
@@ -802,12 +803,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
             store_as(dst + 1, x.y * inv);
             store_as(dst + 2, x.z * inv);
             store_as(dst + 3, x.w * inv);
-            if (e == 0) a.lse2[head] = l == 0.f ? -INFINITY : base + log2f(l);
         } else {
-            const int64_t to = head * kMaxSplits + ((int)blockIdx.x - sg.seg0);
             *reinterpret_cast<float4 *>(a.part_o + to * D + e) = x;
-            if (e == 0) reinterpret_cast<float2 *>(a.part_ml)[to] = make_float2(m == -INFINITY ? m : base, l);
         }
+        if (e == 0) reinterpret_cast<float2 *>(a.part_ml)[to] = make_float2(m == -INFINITY ? m : base, l);
     }
     // ---- the run goes on in the next unit
     if (!enter_next(sg.b, sg.kv)) return;
@@ -820,8 +819,9 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
 //
 // The first CTAs take a utility row's tokens: kFinishThreads / HS of them each, HS threads a token
 // that share the row's heads, or blocks of V kFinishThreads, V tokens a thread, every row_ctas-th of the row; the others merge a head's outputs (MANY: each a CTA, its warps a part of
-// the segments each; else a head a warp).  A head's log-sum-exp comes from
-// its segments' (reference, sum) pairs, so no pass of its own has to gather it.
+// the segments each; else a head a warp).  A head's reference and sum come from
+// its segments' pairs of them, so no pass of its own has to gather them; a probability is
+// 2^(logit - reference) / sum, with the logit's factor applied here, as in the sum, without another rounding.
 constexpr int kFinishThreads = 512;
 
 // One CTA merges one head's segments: every warp sums some of them, 32 E channels wide.
@@ -938,7 +938,7 @@ template <int HS, bool MANY, int V>
 __global__ void __launch_bounds__(kFinishThreads, V == 1 ? 0 : 2) q4_finish_kernel(const Q4FinishArgs a) {
     static_assert(HS == 1 || V == 1, "a thread's tokens are its own");
     constexpr int kTok = kFinishThreads / HS * V, kAhead = V == 4 ? 4 : 8, kWarpsF = kFinishThreads / 32, kHeads = 2;
-    extern __shared__ float lse[];  // [heads of a row]
+    extern __shared__ float4 whole[];  // [heads of a row] the logits' factor, reference, 1 / sum, -
     __shared__ float part[HS > 1 ? kFinishThreads : 1];
     __shared__ float room[kWarpsF * 128];  // of those that merge
     static_assert(kMaxSplits <= 128, "a warp's weights");
@@ -979,36 +979,37 @@ __global__ void __launch_bounds__(kFinishThreads, V == 1 ? 0 : 2) q4_finish_kern
     was.fill(0.f);
     if (a.ema && hs == 0 && token < a.cap) was.load(a.ema + (int64_t)r * a.cap + token);
     if (block * kTok >= L) return;  // (a sequence without slots has no segment count either)
+    // the sum brought into [1, 2) by the reference, which is a whole number; no live slot: probabilities 0
+    auto norm_of = [&](float post, float m, float w) {
+        const int bits = __float_as_int(w) >> 23, up = bits > 0 && bits < 255 ? bits - 127 : 0;
+        return make_float4(post, m == -INFINITY ? 0.f : m + (float)up, w == 0.f ? 0.f : 1.f / (w * pow2((float)-up)), 0.f);
+    };
     if (!MANY) {  // few segments: a head a thread
         for (int h = threadIdx.x; h < nh; h += kFinishThreads) {
             constexpr int kFew = 4;
             const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (head0 + h) * kMaxSplits;
             const int n = __ldcg(a.segs + (head0 + h) / G);
-            const float one = __ldcg(a.lse2 + head0 + h);
+            const float post = __ldcg(a.post + head0 + h);
             float2 y[kFew];
 #pragma unroll
             for (int k = 0; k < kFew; ++k) y[k] = __ldcg(ml + k);
-            float x = one;
-            if (n != 1) {
-                float m = -INFINITY, w = 0.f;
+            float m = -INFINITY, w = 0.f;
 #pragma unroll
-                for (int k = 0; k < kFew; ++k) m = k < n ? fmaxf(m, y[k].x) : m;
-                for (int k = kFew; k < n; ++k) m = fmaxf(m, __ldcg(&ml[k].x));
-                const float base = m == -INFINITY ? 0.f : m;
+            for (int k = 0; k < kFew; ++k) m = k < n ? fmaxf(m, y[k].x) : m;
+            for (int k = kFew; k < n; ++k) m = fmaxf(m, __ldcg(&ml[k].x));
+            const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
-                for (int k = 0; k < kFew; ++k) w += k < n ? y[k].y * exp2f(y[k].x - base) : 0.f;
-                for (int k = kFew; k < n; ++k) {
-                    const float2 v = __ldcg(ml + k);
-                    w += v.y * exp2f(v.x - base);
-                }
-                x = w == 0.f ? -INFINITY : m + log2f(w);
+            for (int k = 0; k < kFew; ++k) w += k < n ? y[k].y * pow2(y[k].x - base) : 0.f;
+            for (int k = kFew; k < n; ++k) {
+                const float2 v = __ldcg(ml + k);
+                w += v.y * pow2(v.x - base);
             }
-            lse[h] = x == -INFINITY ? INFINITY : x;  // no live slot: probabilities 0
+            whole[h] = norm_of(post, m, w);
         }
     }
     for (int hb = warp; MANY && hb < nh; hb += kHeads * kWarpsF) {
         int n[kHeads];
-        float one[kHeads];
+        float post[kHeads];
         constexpr int PL = 2;  // pairs a lane loads before it knows how many there are
         float2 y[kHeads][PL];
 #pragma unroll
@@ -1016,7 +1017,7 @@ __global__ void __launch_bounds__(kFinishThreads, V == 1 ? 0 : 2) q4_finish_kern
             const int h = hb + j * kWarpsF;
             const bool have = h < nh;
             n[j] = have ? __ldcg(a.segs + (head0 + h) / G) : 0;
-            one[j] = have ? __ldcg(a.lse2 + head0 + h) : 0.f;
+            post[j] = have ? __ldcg(a.post + head0 + h) : 0.f;
 #pragma unroll
             for (int k = 0; k < PL; ++k)
                 y[j][k] = have ? __ldcg(reinterpret_cast<const float2 *>(a.part_ml) + (head0 + h) * kMaxSplits + lane + 32 * k)
@@ -1027,26 +1028,22 @@ __global__ void __launch_bounds__(kFinishThreads, V == 1 ? 0 : 2) q4_finish_kern
             const int h = hb + j * kWarpsF;
             if (h >= nh) break;
             const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (head0 + h) * kMaxSplits;
-            float x = one[j];
-            if (n[j] != 1) {
-                float m = -INFINITY, w = 0.f;
+            float m = -INFINITY, w = 0.f;
 #pragma unroll
-                for (int k = 0; k < PL; ++k)
-                    if (lane + 32 * k < n[j]) m = fmaxf(m, y[j][k].x);
-                for (int k = 32 * PL + lane; k < n[j]; k += 32) m = fmaxf(m, __ldcg(&ml[k].x));
-                m = warp_max(m);
-                const float base = m == -INFINITY ? 0.f : m;
+            for (int k = 0; k < PL; ++k)
+                if (lane + 32 * k < n[j]) m = fmaxf(m, y[j][k].x);
+            for (int k = 32 * PL + lane; k < n[j]; k += 32) m = fmaxf(m, __ldcg(&ml[k].x));
+            m = warp_max(m);
+            const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
-                for (int k = 0; k < PL; ++k)
-                    if (lane + 32 * k < n[j]) w += y[j][k].y * exp2f(y[j][k].x - base);
-                for (int k = 32 * PL + lane; k < n[j]; k += 32) {
-                    const float2 v = __ldcg(ml + k);
-                    w += v.y * exp2f(v.x - base);
-                }
-                w = warp_sum(w);
-                x = w == 0.f ? -INFINITY : m + log2f(w);
+            for (int k = 0; k < PL; ++k)
+                if (lane + 32 * k < n[j]) w += y[j][k].y * pow2(y[j][k].x - base);
+            for (int k = 32 * PL + lane; k < n[j]; k += 32) {
+                const float2 v = __ldcg(ml + k);
+                w += v.y * pow2(v.x - base);
             }
-            if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;
+            w = warp_sum(w);
+            if (lane == 0) whole[h] = norm_of(post[j], m, w);
         }
     }
     __syncthreads();
@@ -1056,9 +1053,11 @@ __global__ void __launch_bounds__(kFinishThreads, V == 1 ? 0 : 2) q4_finish_kern
         for (int j0 = 0; j0 < mine; j0 += kAhead) {
             if (j0) load(j0);
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j)
+            for (int j = 0; j < kAhead; ++j) {
+                const float4 n = whole[min((j0 + j) * HS + hs, nh - 1)];  // (past the last: 0)
 #pragma unroll
-                for (int v = 0; v < V; ++v) s.x[v] += exp2_fast(z[j].x[v] - lse[min((j0 + j) * HS + hs, nh - 1)]);  // (past the last: 0)
+                for (int v = 0; v < V; ++v) s.x[v] = fmaf(exp2_fast(fmaf(z[j].x[v], n.x, -n.y)), n.z, s.x[v]);
+            }
         }
         if (HS > 1) {
             part[threadIdx.x] = s.x[0];
@@ -1070,8 +1069,9 @@ __global__ void __launch_bounds__(kFinishThreads, V == 1 ? 0 : 2) q4_finish_kern
         const int64_t to = (int64_t)r * a.cap + token;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            s.x[v] *= 1.f / (float)nh;
-            was.x[v] = a.alpha * was.x[v] + (1.f - a.alpha) * s.x[v];
+            // (each rounding named: every variant of the kernel gives the same bits)
+            s.x[v] = __fmul_rn(s.x[v], 1.f / (float)nh);
+            was.x[v] = __fmaf_rn(a.alpha, was.x[v], __fmul_rn(1.f - a.alpha, s.x[v]));
         }
         if (a.score) s.store(a.score + to, L - token);
         if (a.ema) was.store(a.ema + to, L - token);
@@ -1107,8 +1107,14 @@ cudaError_t launch_finish_t(Q4FinishArgs a, int64_t rows, int32_t max_len, int s
     if (tokens + merges > 0x7fffffff) return cudaErrorInvalidConfiguration;
     a.token_ctas = (int32_t)tokens;
     const int nh = a.rows_per_seq > 1 ? a.q_heads / a.kv_heads : a.q_heads;
-    const cudaError_t e = launch_k(q4_finish_kernel<HS, MANY, V>, dim3((unsigned)(tokens + merges)), dim3(kFinishThreads),
-                                   sizeof(float) * nh, st, a);
+    const int smem = (int)sizeof(float4) * nh;
+    constexpr int kDefault = 32 << 10;  // with the kernel's own arrays within 48 KB
+    cudaError_t e = cudaSuccess;
+    if (smem > kDefault)
+        e = cudaFuncSetAttribute(q4_finish_kernel<HS, MANY, V>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)sizeof(float4) * kMaxQ4Heads);
+    if (e != cudaSuccess) return e;
+    e = launch_k(q4_finish_kernel<HS, MANY, V>, dim3((unsigned)(tokens + merges)), dim3(kFinishThreads), smem, st, a);
     note_launch();
     return e;
 }

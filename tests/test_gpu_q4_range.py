@@ -125,3 +125,35 @@ def test_largest_values_do_not_overflow(dtype, lens):
     out, _ = attend(c, q, max(lens))
     # (6 s of a scale s = 2^123 exactly; sums of equal terms: 2^-18)
     assert bool(((out.double() / (1.5 * 2.0 ** 125) - 1).abs() <= 2.0 ** -18).all())
+
+
+@pytest.mark.parametrize("dtype", [ikv.IKV_F32, ikv.IKV_BF16])
+@pytest.mark.parametrize("n", [1, 2, 60, 700, 3000])
+def test_equal_keys_score_alike(dtype, n):
+    """Tokens whose keys are alike get 1 / n each, however large their logits: the sum of the weights and a
+    token's probability go by the same logit, so its roundings cancel and two exponentials (2^-22
+    each) and the sum (at most 2^4 terms a lane, 2^-21) remain."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    nb, kvh, G, d = 24, 1, 1, 64
+    c = make([n] * nb, kvh, G, d, 64, dtype, layers=1)
+    k = torch.randn(1, nb, 1, kvh, d, generator=gen, device="cuda")
+    q = torch.randn(nb, G * kvh, d, generator=gen, device="cuda")
+    q = (q * torch.linspace(0.1, 12, nb, device="cuda").view(-1, 1, 1) + 3.0 * k[0, :, 0].repeat_interleave(G, 1)).to(TORCH[dtype])
+    k = k.expand(-1, -1, n, -1, -1).to(TORCH[dtype]).contiguous()
+    v = torch.randn(k.shape, generator=gen, device="cuda").to(TORCH[dtype])
+    ikv.ikv_q4_store(c.shape(), c.cache(n), c.q4(), 0, 1, k, v, c.dense_rows(k), torch.zeros_like(c.len), c.len, n)
+    _, score = attend(c, q, n)
+    err = (score[:, :n].double() * n - 1).abs()
+    assert bool((err <= 2.0 ** -20).all()), float(err.max())
+
+
+def test_many_query_heads():
+    """As many heads as a row's references and sums take more than 48 KB of shared memory for."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    kvh, G, d = 600, 8, 64
+    c = make([70], kvh, G, d, 16, ikv.IKV_BF16, layers=1, room=2)
+    k = torch.randn(1, 1, 70, kvh, d, generator=gen, device="cuda").to(torch.bfloat16)
+    q = torch.randn(1, G * kvh, d, generator=gen, device="cuda").to(torch.bfloat16)
+    ikv.ikv_q4_store(c.shape(), c.cache(70), c.q4(), 0, 1, k, k.flip(2).contiguous(), c.dense_rows(k), torch.zeros_like(c.len), c.len, 70)
+    out, score = attend(c, q, 70)
+    check(c, q, out, score)
