@@ -125,6 +125,11 @@ typedef struct {
     int32_t pos_cap;             /* per-layer eviction: token positions the position-indexed state
                                     holds (ema is [batch][pos_cap]; every next_pos[b] must stay below
                                     it); sizes the step workspace.  0 otherwise. */
+    int32_t code_bits;           /* what a row of k and v is: 0 = head_dim values of shape->dtype; 4 = a row
+                                    held in 4 bits, which the calls that read or write values (attention,
+                                    steps, ikv_append_token, ikv_compact_kv, ikv_value_norms, and the sizes
+                                    of their workspaces) refuse with IKV_ERR_UNSUPPORTED.  The ikv_q4_*
+                                    calls take either. */
 } ikv_cache;
 
 /* Optional per-kernel CUDA events recorded on the call's stream by ikv_step
@@ -457,7 +462,9 @@ ikv_status ikv_step_end(const ikv_shape *shape, const ikv_params *params, ikv_ca
  * multiple of 16.  Everything else of ikv_cache keeps its meaning (block table, start, len,
  * pos, dead slots), so ikv_select_budget, ikv_ema_update and the ikv_pages_* calls serve such a
  * cache as they are; shape->dtype is the type of q, out and of the dense rows.  cache->vnorm
- * is not used.
+ * is not used.  Set cache->code_bits = 4: the calls for dense rows, which would take a row for four or
+ * eight times as long and run past the pools, then refuse the cache.  Nothing compacts such a cache in
+ * place: to evict from it, draw its pages from a pool (ikv_pages_compact).
  *
  * Each row is cut into groups of 32 channels.  With a the largest magnitude of a group:
  *   scale s = the smallest bf16 number with 6 s >= a; 0 if a < 2^-120 (the group reads as

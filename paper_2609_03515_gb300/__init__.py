@@ -109,6 +109,8 @@ class DecodeCache:
                       if value_norms else None)
         self.max_len = 0
 
+    code_bits = 0  # ikv_cache.code_bits: rows of dtype
+
     def _alloc_pools(self, shp, device) -> None:
         self.k = torch.zeros(shp + (self.head_dim,), dtype=self.torch_dtype, device=device)
         self.v = torch.zeros(shp + (self.head_dim,), dtype=self.torch_dtype, device=device)
@@ -134,7 +136,7 @@ class DecodeCache:
         return ikv.ikv_cache(self.k.data_ptr(), self.v.data_ptr(), self.block_table.data_ptr(), self.num_pages,
                              self.page_size, self.max_pages, self.len.data_ptr(), self.pos.data_ptr(),
                              self.next_pos.data_ptr(), ml, self.start.data_ptr(), 1 if dead_slots else 0,
-                             self.vnorm.data_ptr() if self.vnorm is not None else None, self.pos_cap)
+                             self.vnorm.data_ptr() if self.vnorm is not None else None, self.pos_cap, self.code_bits)
 
     @property
     def rows_per_seq(self) -> int:
@@ -211,7 +213,10 @@ class DecodeCache:
 class Q4Cache(DecodeCache):
     """A DecodeCache held in 4 bits (include/ikv.h, "Caches held in 4 bits"): k and v are code pools
     [layers][num_pages][kv_heads][page_size][head_dim / 2], k_scale and v_scale their scales; dtype is
-    the type of q, out and of the rows that ikv_q4_store takes."""
+    the type of q, out and of the rows that ikv_q4_store takes.  The calls for dense rows refuse it; to
+    evict from it, give it pool_pages (ikv_pages_compact)."""
+
+    code_bits = 4
 
     def _alloc_pools(self, shp, device) -> None:
         self.k = torch.zeros(shp + (self.head_dim // 2,), dtype=torch.uint8, device=device)

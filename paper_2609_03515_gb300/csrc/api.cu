@@ -78,7 +78,16 @@ ikv_status check_cache(const ikv_shape *s, const ikv_cache *c, bool need_pos) {
     const int64_t cap = (int64_t)c->page_size * c->max_pages;
     if (cap > (int64_t)(1 << 30)) return fail(IKV_ERR_SHAPE, "cap too large");
     if (c->max_len < 0 || c->max_len > cap) return fail(IKV_ERR_SHAPE, "max_len %d outside [0, cap=%lld]", c->max_len, (long long)cap);
+    if (c->code_bits != 0 && c->code_bits != 4) return fail(IKV_ERR_ARG, "code_bits must be 0 or 4");
     (void)s;
+    return IKV_OK;
+}
+
+// check_cache for the calls that take k and v for rows of shape->dtype
+ikv_status check_dense(const ikv_shape *s, const ikv_cache *c, bool need_pos) {
+    const ikv_status e = check_cache(s, c, need_pos);
+    if (e) return e;
+    if (c->code_bits) return fail(IKV_ERR_UNSUPPORTED, "the cache is held in %d bits", c->code_bits);
     return IKV_OK;
 }
 
@@ -474,7 +483,7 @@ ikv_status ikv_decode_attend_score(const ikv_shape *shape, const ikv_cache *cach
     g_err[0] = 0;
     ikv_status e = check_shape(shape);
     if (e) return e;
-    if ((e = check_cache(shape, cache, false))) return e;
+    if ((e = check_dense(shape, cache, false))) return e;
     if (layer < 0 || layer >= shape->layers) return fail(IKV_ERR_ARG, "layer %d out of range", layer);
     if (!q || !out) return fail(IKV_ERR_ARG, "q/out is NULL");
     if (!aligned16(q) || !aligned16(out)) return fail(IKV_ERR_ALIGN, "q/out must be 16-byte aligned");
@@ -525,7 +534,7 @@ ikv_status ikv_value_norms(const ikv_shape *shape, const ikv_cache *cache, cudaS
     g_err[0] = 0;
     ikv_status e = check_shape(shape);
     if (e) return e;
-    if ((e = check_cache(shape, cache, false))) return e;
+    if ((e = check_dense(shape, cache, false))) return e;
     if (!cache->vnorm) return fail(IKV_ERR_ARG, "cache->vnorm is NULL");
     IKV_TRY_CUDA(launch_value_norms(cache->v, view_of(shape, cache), cache->len, shape->batch, shape->layers,
                                     cap_of(cache), shape->dtype, cache->vnorm, stream),
@@ -570,7 +579,7 @@ ikv_status ikv_compact_workspace_size(const ikv_shape *shape, const ikv_cache *c
     g_err[0] = 0;
     ikv_status e = check_shape(shape);
     if (e) return e;
-    if ((e = check_cache(shape, cache, false))) return e;
+    if ((e = check_dense(shape, cache, false))) return e;
     if (!bytes) return fail(IKV_ERR_ARG, "bytes is NULL");
     if (mode != IKV_COMPACT_STABLE && mode != IKV_COMPACT_HOLEFILL && mode != IKV_COMPACT_STABLE_SHORT)
         return fail(IKV_ERR_ARG, "unknown compact mode %d", mode);
@@ -621,7 +630,7 @@ ikv_status ikv_compact_kv(const ikv_shape *shape, ikv_cache *cache, const int32_
     g_err[0] = 0;
     ikv_status e = check_shape(shape);
     if (e) return e;
-    if ((e = check_cache(shape, cache, true))) return e;
+    if ((e = check_dense(shape, cache, true))) return e;
     if (!keep || !keep_len) return fail(IKV_ERR_ARG, "keep/keep_len is NULL");
     size_t need = 0;
     if ((e = ikv_compact_workspace_size(shape, cache, mode, &need))) return e;
@@ -674,7 +683,7 @@ ikv_status ikv_append_token(const ikv_shape *shape, ikv_cache *cache, const void
     g_err[0] = 0;
     ikv_status e = check_shape(shape);
     if (e) return e;
-    if ((e = check_cache(shape, cache, true))) return e;
+    if ((e = check_dense(shape, cache, true))) return e;
     if (!k_new || !v_new) return fail(IKV_ERR_ARG, "k_new/v_new is NULL");
     if (!aligned16(k_new) || !aligned16(v_new)) return fail(IKV_ERR_ALIGN, "k_new/v_new must be 16-byte aligned");
     if (cache->max_len + 1 > cap_of(cache)) return fail(IKV_ERR_SHAPE, "no free slot: max_len + 1 > cap");
@@ -700,7 +709,7 @@ static ikv_status prepare_step(const ikv_shape *shape, const ikv_params *p, cons
                                int32_t t, void *ws, size_t ws_bytes, StepCtx *cx) {
     ikv_status e = check_shape(shape);
     if (e) return e;
-    if ((e = check_cache(shape, cache, true))) return e;
+    if ((e = check_dense(shape, cache, true))) return e;
     if (!p) return fail(IKV_ERR_ARG, "params is NULL");
     if (!ema || !p->budget) return fail(IKV_ERR_ARG, "ema/budget is NULL");
     if (t < 1) return fail(IKV_ERR_ARG, "t is 1-based (got %d)", t);
@@ -894,7 +903,7 @@ ikv_status ikv_step_workspace_size(const ikv_shape *shape, const ikv_cache *cach
     g_err[0] = 0;
     ikv_status e = check_shape(shape);
     if (e) return e;
-    if ((e = check_cache(shape, cache, false))) return e;
+    if ((e = check_dense(shape, cache, false))) return e;
     if (!bytes) return fail(IKV_ERR_ARG, "bytes is NULL");
     *bytes = step_ws(shape, cap_of(cache), cache->pos_cap).end;
     return IKV_OK;
