@@ -11,6 +11,8 @@ The calls of include/ikv.h in the order a server makes them:
            the books, then in each layer ikv_q4_store and ikv_q4_attend_score, which folds
            the layer's score into the utility; every `every` steps the cache is cut back;
   end      ikv_pages_release.
+A pool that runs short loses nothing: ikv_q4_append_token and ikv_q4_store leave out a sequence whose
+slots ikv_pages_writable did not grant, and the loop finds the error bit at its next cut.
 The model is a stand-in of random weights: a layer projects its input to q, k and v and adds the
 attention's output back.
 """
@@ -61,6 +63,7 @@ class Sampler:
         c.budget.fill_(budget)
         i32 = {"dtype": torch.int32, "device": "cuda"}
         self.slot = torch.full((batch,), -1, **i32)
+        self.lacking = torch.zeros(1, **i32)
         self.keep, self.keep_len = torch.zeros(c.rows, c.cap, **i32), torch.zeros(c.rows, **i32)
         self.shape, self.q4, self.pages = c.shape(), c.q4(), c.pages()
         self.cache = c.cache(c.cap - 1)
@@ -74,8 +77,10 @@ class Sampler:
         c, n = self.c, x.shape[0]
         only = torch.full((self.batch,), -1, dtype=torch.int32, device="cuda")
         only[b] = 0
-        ikv.ikv_pages_writable(self.shape, self.cache, self.pages, only, None, n, None, self.pages_ws,
+        ikv.ikv_pages_writable(self.shape, self.cache, self.pages, only, None, n, self.lacking, self.pages_ws,
                                self.pages_ws.numel())
+        if int(self.lacking):
+            raise RuntimeError("the prompt needs %d more pages than are free" % int(self.lacking))
         for layer in range(self.model.layers):
             _, k, v = self.model.qkv(layer, x)
             rows = ikv.ikv_rows(0, 0, k.stride(0), k.stride(1), None)
@@ -97,10 +102,8 @@ class Sampler:
         first = torch.where(live, c.len, -1)
         ikv.ikv_pages_writable(self.shape, self.cache, self.pages, first, None, 1, None, self.pages_ws,
                                self.pages_ws.numel())
+        # (sequences without a prompt were granted nothing and stay empty)
         ikv.ikv_q4_append_token(self.shape, self.cache, self.q4, None, None, c.ema, 0, self.slot)
-        # (sequences without a prompt stay empty)
-        c.len.masked_fill_(~live, 0)
-        self.slot.masked_fill_(~live, -1)
         for layer in range(m.layers):
             q, k, v = m.qkv(layer, x)
             rows = ikv.ikv_rows(0, k.stride(0), k.stride(0), k.stride(1), None)
@@ -110,6 +113,9 @@ class Sampler:
             x = m.after(layer, x, self.out)
         self.t += 1
         if cut or self.t % self.every == 0:
+            status = ikv.ikv_device_status()
+            if status:
+                raise RuntimeError("tokens were left out: device status %d" % status)
             ikv.ikv_select_budget(c.rows, c.cap, c.ema, c.len, 1, c.budget, None, self.keep, self.keep_len)
             ikv.ikv_pages_compact(self.shape, self.cache, self.pages, self.keep, self.keep_len, c.ema, None, self.pages_ws,
                                   self.pages_ws.numel())

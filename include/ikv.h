@@ -130,6 +130,12 @@ typedef struct {
                                     steps, ikv_append_token, ikv_compact_kv, ikv_value_norms, and the sizes
                                     of their workspaces) refuse with IKV_ERR_UNSUPPORTED.  The ikv_q4_*
                                     calls take either. */
+    int32_t *writable;           /* page pools: [batch][2] (device), or NULL: the slots [first, end) that
+                                    the last ikv_pages_writable found or made each sequence's own, see
+                                    there.  When set, ikv_append_token, ikv_q4_append_token and
+                                    ikv_q4_store leave out a sequence whose slots lie outside them;
+                                    ikv_step* and ikv_compact_kv do not go by them and refuse
+                                    (IKV_ERR_UNSUPPORTED). */
 } ikv_cache;
 
 /* Optional per-kernel CUDA events recorded on the call's stream by ikv_step
@@ -385,6 +391,7 @@ ikv_status ikv_compact_kv(const ikv_shape *shape, ikv_cache *cache, const int32_
  * of its row (init_mean == 1, Appendix "New token insertion during non-refresh
  * steps"; dead slots excluded when cache->dead_slots).  Then len[b] += 1 and
  * next_pos[b] += 1.
+ * A sequence whose slot len[b] cache->writable does not name is left as it is.
  * Fails with IKV_ERR_SHAPE (host) if max_len + 1 > cap.
  * ------------------------------------------------------------------------- */
 ikv_status ikv_append_token(const ikv_shape *shape, ikv_cache *cache, const void *k_new, const void *v_new,
@@ -496,7 +503,7 @@ typedef struct {
  *    newest slots, len[b] - n .. len[b] - 1 with n = min(count[b], len[b]).
  *  count: [batch] (device) rows of each sequence, cut to max_count; NULL: max_count each.
  * A sequence whose rows would reach past its slot space is left alone and sets bit 5 of the
- * device error word.  The pages of the slots are written in place: a page that several
+ * device error word; ikv_q4_store also leaves alone one whose slots cache->writable does not name.  The pages of the slots are written in place: a page that several
  * sequences share is made the writer's own first (ikv_pages_writable). */
 ikv_status ikv_q4_store(const ikv_shape *shape, const ikv_cache *cache, const ikv_q4 *q4, int32_t layer0,
                         int32_t n_layers, const void *k, const void *v, const ikv_rows *rows, const int32_t *first,
@@ -506,7 +513,8 @@ ikv_status ikv_q4_load(const ikv_shape *shape, const ikv_cache *cache, const ikv
                        const int32_t *count, int32_t max_count, cudaStream_t stream);
 
 /* ikv_append_token for a 4-bit cache: the same books (position, utility, len, next_pos), and
- * slot[b] (device [batch], written) receives the new token's slot, -1 where there was no room.
+ * slot[b] (device [batch], written) receives the new token's slot, -1 where there was no room or
+ * cache->writable does not name it (the sequence is then as it was).
  * k_new / v_new ([layers][batch][kv_heads][head_dim], dtype) are stored there in every layer; both
  * may be NULL for a model that has a layer's rows only when it gets there: it then calls
  * ikv_q4_store(layer0 = l, n_layers = 1, first = slot, count = NULL, max_count = 1) in each layer. */
@@ -572,8 +580,15 @@ ikv_status ikv_pages_fork(const ikv_shape *shape, ikv_cache *cache, const ikv_pa
  *  first: [batch] (device), < 0: sequence left out; NULL: len[b], the slots behind the last.
  *  count: [batch] (device), cut to max_count; NULL: max_count each.
  *  lacking: (device, or NULL) receives 0, or how many more free pages the call would have needed:
- *    then bit 6 of the device error word is set and nothing is changed.
- * A sequence whose slots would pass its slot space is left out and sets bit 2. */
+ *    then bit 6 of the device error word is set and no page changes hands.
+ * A sequence whose slots would pass its slot space is left out and sets bit 2.
+ * Behind a shortage, calls that are already enqueued would write into page 0 or into pages that others
+ * hold: either the host reads `lacking` before it enqueues them, or cache->writable is given.  Each
+ * sequence that was asked about (first >= 0, count > 0) then gets writable[b] = {first[b], first[b] + count[b]} if
+ * every page of these slots is its own now (also of one that had all of its pages while others
+ * lacked theirs), else {0, 0}, and the stores and appends behind leave it out.  The other sequences keep
+ * theirs.  The caller starts with zeros; ikv_pages_fork (both sequences), ikv_pages_compact and an
+ * ikv_pages_release that takes a page put {0, 0} there. */
 ikv_status ikv_pages_writable(const ikv_shape *shape, ikv_cache *cache, const ikv_pages *pages, const int32_t *first,
                               const int32_t *count, int32_t max_count, int32_t *lacking, void *ws, size_t ws_bytes,
                               cudaStream_t stream);

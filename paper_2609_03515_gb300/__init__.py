@@ -61,7 +61,8 @@ class DecodeCache:
                  and pos_state [batch][pos_cap] is the utility by token position
     budget:      [batch] int32
     With pool_pages, sequences own no page at first: pool_pages pages (numbers 1 ..) are handed out by
-    the ikv_pages_* calls, refs [num_pages] counts their holders, and block_table entries of 0 mean none.
+    the ikv_pages_* calls, refs [num_pages] counts their holders, block_table entries of 0 mean none, and
+    writable [batch][2] names the slots that ikv_pages_writable made each sequence's own.
     """
 
     def __init__(self, batch: int, layers: int, q_heads: int, kv_heads: int, head_dim: int, cap_tokens: int,
@@ -78,8 +79,9 @@ class DecodeCache:
         self._alloc_pools((layers, self.num_pages, kv_heads, page_size), device)
         # pages handed out as sequences grow (ikv_pages_*): no sequence holds one yet, and page 0
         # stands for none; otherwise every sequence owns max_pages pages for good
-        self.refs = None
+        self.refs = self.writable = None
         if pool_pages is not None:
+            self.writable = torch.zeros((batch, 2), dtype=torch.int32, device=device)
             self.refs = torch.zeros(self.num_pages, dtype=torch.int32, device=device)
             self.refs[0] = 1
         pages = torch.arange(self.num_pages, dtype=torch.int32)
@@ -131,12 +133,18 @@ class DecodeCache:
         return ikv.ikv_shape(self.batch, self.layers, self.q_heads, self.kv_heads, self.head_dim, self.dtype,
                              self.granularity)
 
-    def cache(self, max_len: Optional[int] = None, dead_slots: bool = False) -> ikv.ikv_cache:
+    def cache(self, max_len: Optional[int] = None, dead_slots: bool = False,
+              granted: Optional[bool] = None) -> ikv.ikv_cache:
+        """granted: stores and appends go by what ikv_pages_writable granted (ikv_cache.writable; steps refuse
+        that).  None: a pool of 4-bit rows, which no step serves, does."""
+        if granted is None:
+            granted = self.code_bits == 4 and self.writable is not None
         ml = self.max_len if max_len is None else max_len
         return ikv.ikv_cache(self.k.data_ptr(), self.v.data_ptr(), self.block_table.data_ptr(), self.num_pages,
                              self.page_size, self.max_pages, self.len.data_ptr(), self.pos.data_ptr(),
                              self.next_pos.data_ptr(), ml, self.start.data_ptr(), 1 if dead_slots else 0,
-                             self.vnorm.data_ptr() if self.vnorm is not None else None, self.pos_cap, self.code_bits)
+                             self.vnorm.data_ptr() if self.vnorm is not None else None, self.pos_cap, self.code_bits,
+                             self.writable.data_ptr() if granted else None)
 
     @property
     def rows_per_seq(self) -> int:

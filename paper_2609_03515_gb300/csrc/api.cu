@@ -631,6 +631,7 @@ ikv_status ikv_compact_kv(const ikv_shape *shape, ikv_cache *cache, const int32_
     ikv_status e = check_shape(shape);
     if (e) return e;
     if ((e = check_dense(shape, cache, true))) return e;
+    if (cache->writable) return fail(IKV_ERR_UNSUPPORTED, "ikv_pages_compact compacts a pool's sequences");
     if (!keep || !keep_len) return fail(IKV_ERR_ARG, "keep/keep_len is NULL");
     size_t need = 0;
     if ((e = ikv_compact_workspace_size(shape, cache, mode, &need))) return e;
@@ -672,6 +673,7 @@ static ikv_status append_impl(const ikv_shape *shape, ikv_cache *cache, const vo
     a.done = done;
     a.vnorm = cache->vnorm;
     a.slot = slot;
+    a.writable = cache->writable;
     if (!counters_zeroed)
         IKV_TRY_CUDA(cudaMemsetAsync(done, 0, sizeof(int32_t) * shape->batch, stream), "cudaMemsetAsync");
     IKV_TRY_CUDA(launch_append(a, stream), "append launch");
@@ -710,6 +712,7 @@ static ikv_status prepare_step(const ikv_shape *shape, const ikv_params *p, cons
     ikv_status e = check_shape(shape);
     if (e) return e;
     if ((e = check_dense(shape, cache, true))) return e;
+    if (cache->writable) return fail(IKV_ERR_UNSUPPORTED, "a step does not go by cache->writable");
     if (!p) return fail(IKV_ERR_ARG, "params is NULL");
     if (!ema || !p->budget) return fail(IKV_ERR_ARG, "ema/budget is NULL");
     if (t < 1) return fail(IKV_ERR_ARG, "t is 1-based (got %d)", t);

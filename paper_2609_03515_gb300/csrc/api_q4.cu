@@ -40,6 +40,7 @@ ikv_status move_rows(const ikv_shape *s, const ikv_cache *c, const ikv_q4 *q, in
     a.len = c->len;
     a.first = first;
     a.count = count;
+    a.writable = c->writable;
     a.batch = s->batch;
     a.layer0 = layer0;
     a.n_layers = n_layers;
@@ -61,6 +62,7 @@ ikv_status check_pages(const ikv_shape *s, const ikv_cache *c, const ikv_pages *
     if (c->max_len > 0) same.max_len = 0;
     if ((e = check_cache(s, &same, need_pos))) return e;
     if (!p || !p->refs) return report(IKV_ERR_ARG, "pages or its refs is NULL");
+    if (reinterpret_cast<uintptr_t>(c->writable) % sizeof(int2)) return report(IKV_ERR_ALIGN, "cache->writable must be 8-byte aligned");
     if (c->num_pages > 0x7fff0000) return report(IKV_ERR_SHAPE, "too many pages");  // (the search counts past them)
     if (p->n_planes < 1 || p->n_planes > kMaxPlanes) return report(IKV_ERR_SHAPE, "n_planes outside [1, %d]", kMaxPlanes);
     for (int i = 0; i < p->n_planes; ++i) {
@@ -87,6 +89,7 @@ ikv_status check_pages(const ikv_shape *s, const ikv_cache *c, const ikv_pages *
     a->next_pos = c->next_pos;
     a->start = c->start;
     a->pos = c->pos;
+    a->writable = reinterpret_cast<int2 *>(c->writable);
     a->vnorm = c->vnorm;
     return IKV_OK;
 }
@@ -139,6 +142,7 @@ ikv_status ikv_q4_append_token(const ikv_shape *shape, ikv_cache *cache, const i
     a.init_mean = ema ? init_mean : 0;
     a.dead_slots = cache->dead_slots ? 1 : 0;
     a.slot = slot;
+    a.writable = cache->writable;
     PdlScope pdl;
     IKV_TRY_CUDA(launch_append(a, stream), "append launch");
     if (!k_new) return IKV_OK;

@@ -486,12 +486,14 @@ __global__ void __launch_bounds__(kCompThreads) append_kernel(const AppendArgs a
     const int b = blockIdx.y;
     const int L = a.len[b];
     const int S = a.pv.start_of(b);
+    const bool left_out = a.writable && (L < a.writable[2 * b] || L >= a.writable[2 * b + 1]);
+    const bool room = !left_out && S + L < a.cap;
     const int kvh = a.pv.kv_heads;
     const int nkv = a.layers * kvh;
     const int rowB = a.pv.head_dim * a.elem_bytes;
     const int CPR = rowB >> 4;
-    if (a.slot && blockIdx.x == 0 && tid == 0) a.slot[b] = S + L < a.cap ? L : -1;
-    if (S + L < a.cap && a.k_new) {
+    if (a.slot && blockIdx.x == 0 && tid == 0) a.slot[b] = room ? L : -1;
+    if (room && a.k_new) {
         unsigned char *kb = reinterpret_cast<unsigned char *>(a.k);
         unsigned char *vb = reinterpret_cast<unsigned char *>(a.v);
         const unsigned char *kn = reinterpret_cast<const unsigned char *>(a.k_new);
@@ -524,7 +526,7 @@ __global__ void __launch_bounds__(kCompThreads) append_kernel(const AppendArgs a
             }
         }
     }
-    if (S + L < a.cap) {
+    if (room) {
         if (blockIdx.x == 0) {
             const int np = a.next_pos[b];
             for (int rr = 0; rr < a.rows_per_seq; ++rr) {
@@ -553,10 +555,10 @@ __global__ void __launch_bounds__(kCompThreads) append_kernel(const AppendArgs a
     if (gridDim.x == 1) {
         // bookkeeping only (one CTA per sequence, which has read len[b] above): no arrival
         if (tid == 0) {
-            if (S + L < a.cap) {
+            if (room) {
                 a.len[b] = L + 1;
                 a.next_pos[b] = a.next_pos[b] + 1;
-            } else {
+            } else if (!left_out) {
                 atomicOr(&g_append_error, 1u);  // the token was not stored; ikv_device_status reports it
             }
         }
@@ -564,10 +566,10 @@ __global__ void __launch_bounds__(kCompThreads) append_kernel(const AppendArgs a
     }
     if (tid == 0) {
         if (arrive_acq_rel(&a.done[b]) == (int)gridDim.x - 1) {
-            if (S + L < a.cap) {
+            if (room) {
                 a.len[b] = L + 1;
                 a.next_pos[b] = a.next_pos[b] + 1;
-            } else {
+            } else if (!left_out) {
                 atomicOr(&g_append_error, 1u);  // the token was not stored; ikv_device_status reports it
             }
             a.done[b] = 0;

@@ -326,6 +326,7 @@ struct AppendArgs {
     // k_new == null makes launch_append do the bookkeeping only and record each sequence's
     // reserved logical slot (-1: no room) in slot[b]; the attention stores the rows
     int32_t *slot;
+    const int32_t *writable;    // [batch][2] slots that a sequence may write, or null: all
 };
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t st);
 

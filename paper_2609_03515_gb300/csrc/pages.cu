@@ -21,6 +21,11 @@ __device__ __forceinline__ int start_of(const PagesArgs &a, int b) { return a.st
 // slots that a sequence keeps in a compaction: no more than lie behind its start
 __device__ __forceinline__ int kept_of(const PagesArgs &a, int b, int keep_len) { return min(keep_len, a.cap - start_of(a, b)); }
 
+// A page of the sequence's went, or others hold it too: it has to ask again before it writes.
+__device__ __forceinline__ void forget_granted(const PagesArgs &a, int b) {
+    if (a.writable) a.writable[b] = make_int2(0, 0);
+}
+
 // Exclusive prefix sum of x over the CTA (kPlanThreads threads), and the total.
 __device__ __forceinline__ int block_scan(int x, int *total) {
     __shared__ int sums[32];
@@ -101,6 +106,7 @@ __global__ void __launch_bounds__(kRowThreads) release_kernel(const PagesArgs a,
     if (L > 0 && p0 + a.page_size > S && p0 < S + L + extra) return;
     a.table[i] = 0;
     atomicSub(a.refs + e, 1);
+    forget_granted(a, b);
 }
 
 template <typename T>
@@ -143,6 +149,8 @@ __global__ void __launch_bounds__(kRowThreads) fork_kernel(const PagesArgs a, co
         }
         if (threadIdx.x == 0) {
             a.len[d] = a.len[s];
+            forget_granted(a, s);
+            forget_granted(a, d);
             if (a.next_pos) a.next_pos[d] = a.next_pos[s];
             if (a.start) a.start[d] = a.start[s];
         }
@@ -180,21 +188,30 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
     FreePages pages{a.refs, a.num_pages};
     pages.load(0);
     if (threadIdx.x == 0) w.total[2] = 0;  // rows of the longest copy
-    // the entry of request i, or -1: page lp of sequence b
-    auto request = [&](int64_t i, int *b, int *lp) -> int {
-        if (i >= R) return -1;
+    // the slots that sequence b asks for: {first, count}, or {-, 0}
+    auto asked = [&](int b) -> int2 {
+        const int n = min(count ? count[b] : max_count, max_count), from = first ? first[b] : a.len[b];
+        return make_int2(from, from < 0 ? 0 : max(n, 0));
+    };
+    // request i: page lp of sequence b
+    auto page_of = [&](int64_t i, int *b, int *lp) -> bool {
+        if (i >= R) return false;
         *b = FEW ? (int)i / span : (int)(i / span);
-        const int x = (int)(i - (int64_t)*b * span);
-        const int n = min(count ? count[*b] : max_count, max_count);
-        const int from = first ? first[*b] : a.len[*b], S = start_of(a, *b);
-        if (n <= 0 || from < 0) return -1;
-        if ((int64_t)S + from + n > a.cap) {
+        const int x = (int)(i - (int64_t)*b * span), S = start_of(a, *b);
+        const int2 w = asked(*b);
+        if (w.y == 0) return false;
+        if ((int64_t)S + w.x + w.y > a.cap) {
             if (x == 0) atomicOr(&g_pages_error, 4u);
-            return -1;
+            return false;
         }
-        const int f = S + from, p = f / a.page_size + x;
-        if (p > (f + n - 1) / a.page_size) return -1;
+        const int f = S + w.x, p = f / a.page_size + x;
         *lp = p;
+        return p <= (f + w.y - 1) / a.page_size;
+    };
+    // its entry, or -1
+    auto request = [&](int64_t i, int *b, int *lp) -> int {
+        if (!page_of(i, b, lp)) return -1;
+        const int p = *lp;
         const int e = a.table[(int64_t)*b * a.max_pages + p];
         if (e >= 0 && e < a.num_pages) return e;
         atomicOr(&g_pages_error, 128u);
@@ -239,9 +256,10 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
         const int rank = block_scan(need ? 1 : 0, &total);
         const int have = pages.find(total, ids_s);
         report_total(total, have);
-        if (have < total || !need) return;
-        assign(b, lp, e, ids_s[rank], rank);
-        if (e > 0) atomicSub(a.refs + e, 1);  // (every count is read)
+        if (have == total && need) {
+            assign(b, lp, e, ids_s[rank], rank);
+            if (e > 0) atomicSub(a.refs + e, 1);  // (every count is read)
+        }
     } else {
         for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
             const int e = request(i, &b, &lp);
@@ -273,9 +291,8 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
         }
         const int have = pages.find(total, w.free_ids);
         report_total(total, have);
-        if (have < total) return;
         int done = 0;
-        for (int64_t i0 = 0; i0 < R; i0 += kPlanThreads) {
+        for (int64_t i0 = 0; have == total && i0 < R; i0 += kPlanThreads) {
             const bool need = needs(i0 + threadIdx.x, &b, &lp, &e);
             int n;
             const int rank = done + block_scan(need ? 1 : 0, &n);  // (its barriers: everybody has read the counts)
@@ -284,10 +301,22 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
         }
         __syncthreads();
         // the copied pages' holders go once no count is read any more
-        for (int64_t i = threadIdx.x; i < total; i += kPlanThreads) {
+        for (int64_t i = threadIdx.x; have == total && i < total; i += kPlanThreads) {
             const int e = w.jobs[4 * i];
             if (e > 0) atomicSub(a.refs + e, 1);
         }
+    }
+    if (!a.writable) return;
+    // granted: the slots whose pages are all the sequence's own, as tables and counts are now
+    for (int s = threadIdx.x; s < a.batch; s += kPlanThreads) {
+        const int2 x = asked(s);
+        if (x.y > 0) a.writable[s] = (int64_t)start_of(a, s) + x.x + x.y > a.cap ? make_int2(0, 0) : make_int2(x.x, x.x + x.y);
+    }
+    __syncthreads();
+    for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
+        if (!page_of(i, &b, &lp)) continue;
+        const int e = __ldcg(a.table + (int64_t)b * a.max_pages + lp);
+        if (e <= 0 || e >= a.num_pages || __ldcg(a.refs + e) != 1) forget_granted(a, b);
     }
 }
 
@@ -415,7 +444,9 @@ compact_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
     }
     for (int b = threadIdx.x; b < a.batch; b += kPlanThreads) {
         const int n = kept_of(a, b, keep_len[(int64_t)b * a.rows_per_seq]);
-        if (n >= 0) a.len[b] = n;
+        if (n < 0) continue;
+        a.len[b] = n;
+        forget_granted(a, b);
     }
 }
 
@@ -577,7 +608,10 @@ __global__ void __launch_bounds__(kCopyThreads) compact_commit_kernel(const Page
     const int b = blockIdx.x, n = kept_of(a, b, keep_len[(int64_t)b * a.rows_per_seq]);
     if (!w.total[1] || n < 0) return;
     for (int lp = w.begin[b] + threadIdx.x; lp < a.max_pages; lp += kCopyThreads) commit_entry(a, w, b, lp);
-    if (threadIdx.x == 0) a.len[b] = n;
+    if (threadIdx.x == 0) {
+        a.len[b] = n;
+        forget_granted(a, b);
+    }
 }
 
 }  // namespace

@@ -158,6 +158,7 @@ __global__ void __launch_bounds__(kMoveThreads, 3) q4_move_kernel(const Q4MoveAr
         if (threadIdx.x == 0) atomicOr(&g_q4_error, 32u);
         return;
     }
+    if (STORE && a.writable && (first < a.writable[2 * b] || first + n > a.writable[2 * b + 1])) return;
     const int rows = n * G;
     if (blk * RPP * ROWS >= rows) return;
     const int u = threadIdx.x & (kUnits - 1), r0 = blk * RPP * ROWS + threadIdx.x / kUnits;

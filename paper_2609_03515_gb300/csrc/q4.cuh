@@ -42,7 +42,8 @@ struct Q4MoveArgs {
     uint16_t *ks, *vs;                // scales: row of D / 32 bf16
     PagedView pv;
     Q4Rows rows;
-    const int32_t *len, *first, *count;  // [batch]; first null: the newest max_count slots; count null: max_count
+    const int32_t *len, *first, *count;  // [batch]; first null: the newest slots, up to count; count null: max_count
+    const int32_t *writable;          // [batch][2] slots that a store may write, or null: all
     int32_t batch, layer0, n_layers, max_count, cap;
     int32_t head_shift;               // log2(kv_heads), or -1
     int32_t blocks;                   // CTAs of one sequence's rows; set by the launcher
@@ -96,6 +97,7 @@ struct PagesArgs {
     int32_t *table;                   // [batch][max_pages], 0 = none
     int32_t num_pages, page_size, max_pages, kv_heads, layers, batch, rows_per_seq, cap;
     int32_t *len, *next_pos, *start, *pos;
+    int2 *writable;                   // [batch] slots granted, or null
     float *ema, *vnorm;
 };
 // scratch of one call: what its kernels hand to one another

@@ -38,7 +38,8 @@ class ikv_shape(ctypes.Structure):
 class ikv_cache(ctypes.Structure):
     _fields_ = [("k", P), ("v", P), ("block_table", P), ("num_pages", I32), ("page_size", I32), ("max_pages", I32),
                 ("len", P), ("pos", P), ("next_pos", P), ("max_len", I32), ("start", P), ("dead_slots", I32),
-                ("vnorm", P), ("pos_cap", I32), ("code_bits", I32)]
+                ("vnorm", P), ("pos_cap", I32), ("code_bits", I32),
+                ("writable", P)]
 
 
 class ikv_timing(ctypes.Structure):
