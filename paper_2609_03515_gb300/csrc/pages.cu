@@ -538,7 +538,7 @@ __device__ __forceinline__ void gather_in_place(const PagesArgs &a, const int32_
 }
 __global__ void __launch_bounds__(kCopyThreads, 4)
 compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, const int32_t *keep_len, const int32_t *old,
-                    int pages_at_once, float units_a_job, int least_units, int n_rows) {
+                    int pages_at_once, float units_a_job, int least_units, int most_units, int n_rows) {
     pdl_wait();
     __shared__ RowMove moves[kRowsAtOnce];
     if (!w.total[1]) return;  // too few pages
@@ -551,7 +551,8 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
     int share = a.rows_per_seq == 1 ? a.kv_heads : 1, parts = a.kv_heads / share;
     // fewer pages and heads an item, where there would be fewer items than a quarter of the CTAs (two an SM)
     // (halves: powers of two stay so, which gather_plane divides by)
-    const int units = max((int)((float)jobs * units_a_job), least_units);
+    // (and never so many that an item's vectors pass 32 bits: pages may hold 16 MB a head)
+    const int units = min(max((int)((float)jobs * units_a_job), least_units), most_units);
     while (pages_at_once > 1 && pages_at_once * share > units) pages_at_once = (pages_at_once + 1) >> 1;
     if (share > units) {
         while (share > units) share = (share + 1) >> 1;
@@ -684,8 +685,11 @@ cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int
     if (rows + ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
     const float units_a_job = 4.f * a.layers * a.kv_heads / (float)ctas;
     const int least = kItemBytes / (a.page_size * a.row_bytes[0]);
+    int widest = 0;
+    for (int pl = 0; pl < a.n_planes; ++pl) widest = a.row_bytes[pl] > widest ? a.row_bytes[pl] : widest;
+    const int64_t most = ((int64_t)1 << 30) / ((int64_t)a.page_size * widest);  // pages of a head: 1 GB; at least 64
     e = launch_k(compact_copy_kernel, dim3((unsigned)(rows + ctas)), dim3(kCopyThreads), 0, st, a, w, keep, keep_len,
-                 (const int32_t *)(old ? old : a.table), at_once, units_a_job, least > 1 ? least : 1, (int)rows);
+                 (const int32_t *)(old ? old : a.table), at_once, units_a_job, least > 1 ? least : 1, (int)most, (int)rows);
     note_launch();
     if (e != cudaSuccess || old) return e;
     e = launch_k(compact_commit_kernel, dim3((unsigned)a.batch), dim3(kCopyThreads), 0, st, a, w, keep_len);
