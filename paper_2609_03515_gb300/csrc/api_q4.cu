@@ -24,7 +24,8 @@ ikv_status move_rows(const ikv_shape *s, const ikv_cache *c, const ikv_q4 *q, in
     if (layer0 < 0 || n_layers < 0 || layer0 > s->layers - n_layers)
         return report(IKV_ERR_ARG, "layers [%d, %d + %d) out of range", layer0, layer0, n_layers);
     if (max_count < 0 || max_count > cap_of(c)) return report(IKV_ERR_SHAPE, "max_count %d outside [0, cap]", max_count);
-    if ((int64_t)max_count * s->kv_heads > 0x7fffffff) return report(IKV_ERR_SHAPE, "max_count * kv_heads too large");
+    if ((int64_t)max_count * s->kv_heads > 0x7fff0000)  // (the kernel counts a CTA's rows past them)
+        return report(IKV_ERR_SHAPE, "max_count * kv_heads too large");
     if (max_count == 0 || n_layers == 0) return IKV_OK;  // (whatever the rows of nothing are)
     if (!k || !v || !rows) return report(IKV_ERR_ARG, "k/v/rows is NULL");
     const int64_t unit = s->dtype == IKV_BF16 ? 8 : 4;  // elements of 16 bytes
