@@ -161,7 +161,7 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     if (!q || !out) return report(IKV_ERR_ARG, "q/out is NULL");
     if (!aligned16(q) || !aligned16(out)) return report(IKV_ERR_ALIGN, "q/out must be 16-byte aligned");
     if (ema && !(alpha >= 0.f && alpha <= 1.f)) return report(IKV_ERR_ARG, "alpha must be in [0, 1]");
-    if (shape->q_heads > kMaxQ4Heads) return report(IKV_ERR_UNSUPPORTED, "more than %d query heads", kMaxQ4Heads);
+    if (shape->q_heads > kMaxQ4Heads) return report(IKV_ERR_SHAPE, "more than %d query heads", kMaxQ4Heads);
     const bool want_score = score || ema;
     const AttendWs w = attend_ws(shape, cap_of(cache), 1, want_score);
     if (!ws || ws_bytes < w.end) return report(IKV_ERR_WORKSPACE, "workspace needs %zu bytes", w.end);
