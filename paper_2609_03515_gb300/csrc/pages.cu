@@ -21,6 +21,12 @@ __device__ __forceinline__ int start_of(const PagesArgs &a, int b) { return a.st
 // slots that a sequence keeps in a compaction: no more than lie behind its start
 __device__ __forceinline__ int kept_of(const PagesArgs &a, int b, int keep_len) { return min(keep_len, a.cap - start_of(a, b)); }
 
+// Whether a block table entry names a page; one that is neither a page nor 0 is reported.
+__device__ __forceinline__ bool holds_page(const PagesArgs &a, int entry) {
+    if (entry > 0 && entry < a.num_pages) return true;
+    if (entry != 0) atomicOr(&g_pages_error, 128u);
+    return false;
+}
 // A page of the sequence's went, or others hold it too: it has to ask again before it writes.
 __device__ __forceinline__ void forget_granted(const PagesArgs &a, int b) {
     if (a.writable) a.writable[b] = make_int2(0, 0);
@@ -100,7 +106,7 @@ __global__ void __launch_bounds__(kRowThreads) release_kernel(const PagesArgs a,
     const int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
     if (i >= (int64_t)a.batch * a.max_pages) return;
     const int e = a.table[i];
-    if (e <= 0 || e >= a.num_pages) return;
+    if (!holds_page(a, e)) return;
     const int b = (int)(i / a.max_pages), lp = (int)(i % a.max_pages);
     const int64_t S = start_of(a, b), L = a.len[b], p0 = (int64_t)lp * a.page_size;
     if (L > 0 && p0 + a.page_size > S && p0 < S + L + extra) return;
@@ -143,8 +149,9 @@ __global__ void __launch_bounds__(kRowThreads) fork_kernel(const PagesArgs a, co
             for (int u = 0; u < U; ++u) e[u] = p0 + u * kRowThreads < a.max_pages ? from[p0 + u * kRowThreads] : 0;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (p0 + u * kRowThreads < a.max_pages) to[p0 + u * kRowThreads] = e[u];
-                if (e[u] > 0 && e[u] < a.num_pages) atomicAdd(a.refs + e[u], 1);
+                const bool held = holds_page(a, e[u]);
+                if (p0 + u * kRowThreads < a.max_pages) to[p0 + u * kRowThreads] = held ? e[u] : 0;
+                if (held) atomicAdd(a.refs + e[u], 1);
             }
         }
         if (threadIdx.x == 0) {
@@ -373,7 +380,7 @@ __device__ __forceinline__ void commit_entry(const PagesArgs &a, const PagesWs &
     int32_t *entry = a.table + (int64_t)b * a.max_pages + lp;
     const int e = *entry, begin = w.begin[b], base = w.base[b];
     const int to = lp - begin < w.base[b + 1] - base ? w.free_ids[base + lp - begin] : 0;
-    if (e > 0 && e < a.num_pages) atomicSub(a.refs + e, 1);
+    if (holds_page(a, e)) atomicSub(a.refs + e, 1);
     if (to) a.refs[to] = 1;
     if (e != to) *entry = to;
 }
