@@ -230,7 +230,8 @@ int64_t ikv_launch_count(void);
  * was dropped); bit 4: a rank-trace set exceeded 16384 tokens (not traced);
  * bit 5: rows of ikv_q4_store or ikv_q4_load lay outside a sequence's slot space (left alone);
  * bit 6: ikv_pages_writable or ikv_pages_compact needed more pages than were free (nothing was
- * done); bit 7: a sequence number or a block table entry that a page call met was out of range. */
+ * done); bit 7: a sequence number or a block table entry that a page call met was out of range, or
+ * ikv_pages_compact was told to keep a slot without a page. */
 ikv_status ikv_device_status(uint32_t *flags);
 
 /* Test of the bounded waits (no counterpart in the paper): the next tensor-core attention
@@ -599,7 +600,8 @@ ikv_status ikv_pages_writable(const ikv_shape *shape, ikv_cache *cache, const ik
  * gathered into free pages, and the old pages are given back (also when only the end was cut off,
  * which copies nothing).  start stays.  A sequence with keep_len < 0 is left alone.  keep and keep_len
  * as ikv_select_budget produces them; the rows of one sequence keep the same number.  A keep_len past
- * the slot space (start[b] + keep_len > cap) is cut to it and sets bit 2.
+ * the slot space (start[b] + keep_len > cap) is cut to it and sets bit 2; a kept slot whose old page is none
+ * is not copied and sets bit 7.
  *  lacking as in ikv_pages_writable: too few free pages leave everything as it was. */
 ikv_status ikv_pages_compact(const ikv_shape *shape, ikv_cache *cache, const ikv_pages *pages, const int32_t *keep,
                              const int32_t *keep_len, float *ema, int32_t *lacking, void *ws, size_t ws_bytes,

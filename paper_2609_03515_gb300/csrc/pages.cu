@@ -590,7 +590,7 @@ compact_copy_kernel(const PagesArgs a, const PagesWs w, const int32_t *keep, con
                     const int64_t from = (int64_t)S + keep[r * a.cap + j];
                     const int fp = (int)(from / a.page_size);
                     const int page = from >= 0 && fp < a.max_pages ? old[(int64_t)b * a.max_pages + fp] : -1;
-                    if (page >= 0 && page < a.num_pages) {
+                    if (page > 0 && page < a.num_pages) {  // (0: a slot without a page holds nothing to keep)
                         m.src = (((int64_t)l * a.num_pages + page) * a.kv_heads + g0) * a.page_size + from % a.page_size;
                         m.dst = (((int64_t)l * a.num_pages + w.free_ids[job]) * a.kv_heads + g0) * a.page_size + q0 + q;
                     } else {
