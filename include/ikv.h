@@ -547,7 +547,9 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
  * of pos and ema as "Utility rows" lays them out for the other modes, and refuse pos_cap > 0
  * (IKV_ERR_UNSUPPORTED).  None of them goes by max_len.
  * Writes into a page that several sequences hold reach them all: call ikv_pages_writable for the
- * slots that ikv_q4_store, ikv_append_token, ikv_step or ikv_compact_kv are about to write.
+ * slots that ikv_q4_store, ikv_append_token, ikv_step or ikv_compact_kv are about to write.  An append
+ * writes slot len[b].  A step (whole or split) that may evict, and ikv_compact_kv, write any of the slots
+ * 0 .. len[b], in every compact_mode and at every max_holes: first[b] = 0, count[b] = len[b] + 1.
  * ------------------------------------------------------------------------- */
 enum { IKV_MAX_PLANES = 4 };
 typedef struct {
@@ -588,7 +590,7 @@ ikv_status ikv_pages_fork(const ikv_shape *shape, ikv_cache *cache, const ikv_pa
  * sequence that was asked about (first >= 0, count > 0) then gets writable[b] = {first[b], first[b] + count[b]} if
  * every page of these slots is its own now (also of one that had all of its pages while others
  * lacked theirs), else {0, 0}, and the stores and appends behind leave it out.  The other sequences keep
- * theirs.  The caller starts with zeros; ikv_pages_fork (both sequences), ikv_pages_compact and an
+ * theirs.  The caller starts with zeros and gives all page calls the same cache->writable; ikv_pages_fork (both sequences), ikv_pages_compact and an
  * ikv_pages_release that takes a page put {0, 0} there. */
 ikv_status ikv_pages_writable(const ikv_shape *shape, ikv_cache *cache, const ikv_pages *pages, const int32_t *first,
                               const int32_t *count, int32_t max_count, int32_t *lacking, void *ws, size_t ws_bytes,

@@ -136,7 +136,7 @@ class DecodeCache:
     def cache(self, max_len: Optional[int] = None, dead_slots: bool = False,
               granted: Optional[bool] = None) -> ikv.ikv_cache:
         """granted: stores and appends go by what ikv_pages_writable granted (ikv_cache.writable; steps refuse
-        that).  None: a pool of 4-bit rows, which no step serves, does."""
+        that); the page calls then get it too.  None: a pool of 4-bit rows, which no step serves, does."""
         if granted is None:
             granted = self.code_bits == 4 and self.writable is not None
         ml = self.max_len if max_len is None else max_len
