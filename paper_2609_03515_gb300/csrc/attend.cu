@@ -714,7 +714,7 @@ cudaError_t launch_attend(const AttendArgs &a, int dtype, int head_dim, int grou
 cudaError_t read_clear_attend_error(unsigned int *v) {
     unsigned int z = 0;
     cudaError_t e = cudaMemcpyFromSymbol(v, g_attend_error, sizeof(*v));
-    if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_attend_error, &z, sizeof(z));
+    if (e == cudaSuccess && *v) e = cudaMemcpyToSymbol(g_attend_error, &z, sizeof(z));
     return e;
 }
 

@@ -1040,7 +1040,7 @@ extern "C" ikv_status ikv_device_status(uint32_t *flags) {
     if (!flags) return ikv::report(IKV_ERR_ARG, "flags is NULL");
     unsigned int v = 0, z = 0;
     cudaError_t e = cudaMemcpyFromSymbol(&v, ikv::g_tc_error, sizeof(v));
-    if (e == cudaSuccess) e = cudaMemcpyToSymbol(ikv::g_tc_error, &z, sizeof(z));
+    if (e == cudaSuccess && v) e = cudaMemcpyToSymbol(ikv::g_tc_error, &z, sizeof(z));  // (and so for each word)
     unsigned int ap = 0, at = 0, lw = 0, tr = 0, q4 = 0, pg = 0;
     if (e == cudaSuccess) e = ikv::read_clear_attend_error(&at);
     if (e == cudaSuccess) e = ikv::read_clear_append_error(&ap);

@@ -624,7 +624,7 @@ cudaError_t launch_compact(const CompactArgs &a, int mode, int sms, cudaStream_t
 cudaError_t read_clear_append_error(unsigned int *v) {
     unsigned int z = 0;
     cudaError_t e = cudaMemcpyFromSymbol(v, g_append_error, sizeof(*v));
-    if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_append_error, &z, sizeof(z));
+    if (e == cudaSuccess && *v) e = cudaMemcpyToSymbol(g_append_error, &z, sizeof(z));
     return e;
 }
 

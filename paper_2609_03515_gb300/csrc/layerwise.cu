@@ -206,7 +206,7 @@ cudaError_t launch_layer_fold(const LayerArgs &a, int32_t max_len, int32_t max_p
 cudaError_t read_clear_layer_error(unsigned int *v) {
     unsigned int z = 0;
     cudaError_t e = cudaMemcpyFromSymbol(v, g_layer_error, sizeof(*v));
-    if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_layer_error, &z, sizeof(z));
+    if (e == cudaSuccess && *v) e = cudaMemcpyToSymbol(g_layer_error, &z, sizeof(z));
     return e;
 }
 

@@ -707,7 +707,7 @@ cudaError_t launch_pages_compact(const PagesArgs &a, const PagesWs &w, const int
 cudaError_t read_clear_pages_error(unsigned int *v) {
     unsigned int z = 0;
     cudaError_t e = cudaMemcpyFromSymbol(v, g_pages_error, sizeof(*v));
-    if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_pages_error, &z, sizeof(z));
+    if (e == cudaSuccess && *v) e = cudaMemcpyToSymbol(g_pages_error, &z, sizeof(z));
     return e;
 }
 

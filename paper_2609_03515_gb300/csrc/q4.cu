@@ -290,7 +290,7 @@ cudaError_t launch_q4_load(const Q4MoveArgs &a, int dtype, cudaStream_t st) { re
 cudaError_t read_clear_q4_error(unsigned int *v) {
     unsigned int z = 0;
     cudaError_t e = cudaMemcpyFromSymbol(v, g_q4_error, sizeof(*v));
-    if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_q4_error, &z, sizeof(z));
+    if (e == cudaSuccess && *v) e = cudaMemcpyToSymbol(g_q4_error, &z, sizeof(z));
     return e;
 }
 

@@ -147,7 +147,7 @@ cudaError_t launch_trace(const TraceArgs &a, cudaStream_t st) {
 cudaError_t read_clear_trace_error(unsigned int *v) {
     unsigned int z = 0;
     cudaError_t e = cudaMemcpyFromSymbol(v, g_trace_error, sizeof(*v));
-    if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_trace_error, &z, sizeof(z));
+    if (e == cudaSuccess && *v) e = cudaMemcpyToSymbol(g_trace_error, &z, sizeof(z));
     return e;
 }
 
