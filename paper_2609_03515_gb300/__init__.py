@@ -246,8 +246,8 @@ class Q4Cache(DecodeCache):
         if st[-1] != 1:
             raise ValueError("the channels of a row must be contiguous")
         if row0 is not None:
-            if row0.dtype != torch.int32 or row0.numel() != self.batch or not row0.is_contiguous():
-                raise ValueError("row0 must be contiguous int32 [batch]")
+            if row0.dtype != torch.int32 or row0.numel() < self.batch or not row0.is_contiguous():
+                raise ValueError("row0 must be contiguous int32, a number for each sequence")
             rows = ikv.ikv_rows(st[0], 0, st[1], st[2], row0.data_ptr())
             rows.row0_tensor = row0  # (the struct holds its address)
             return rows

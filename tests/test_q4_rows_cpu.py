@@ -27,3 +27,10 @@ def test_row_numbers_of_another_kind_are_refused(bad):
     c = Q4Cache(2, 1, 2, 2, 64, 64, device="cpu", page_size=16)
     with pytest.raises(ValueError):
         c.dense_rows(torch.zeros(1, 9, 2, 64), bad)
+
+
+def test_one_number_more_is_taken():
+    """First rows of all sequences and the end of the last, as packed prompts often come with."""
+    c = Q4Cache(2, 1, 2, 2, 64, 64, device="cpu", page_size=16)
+    row0 = torch.tensor([0, 5, 9], dtype=torch.int32)
+    assert c.dense_rows(torch.zeros(1, 9, 2, 64), row0).row0 == row0.data_ptr()
