@@ -526,7 +526,8 @@ ikv_status ikv_q4_append_token(const ikv_shape *shape, ikv_cache *cache, const i
  * that the codes stand for, score and ema as there, ws of ikv_attend_workspace_size() bytes.  A
  * sequence without a live slot gets out = 0.  Slots outside [0, len[b]) are never used, whatever
  * they hold.  A NaN group of a live V row makes its 32 channels NaN for that KV head's queries, one
- * of a live K row every channel.  Fails with IKV_ERR_SHAPE where batch * kv_heads * cap passes
+ * of a live K row every channel.  Logits are formed with q scaled up to 2^8: rows of K above 2^112 may
+ * overflow them, which leaves NaN.  Fails with IKV_ERR_SHAPE where batch * kv_heads * cap passes
  * 2.5e10 slots or the pool 6.8e10 rows, and above 8192 query heads. */
 ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, const ikv_q4 *q4, int32_t layer,
                                const void *q, void *out, float *score, float *ema, float alpha, void *ws,
@@ -572,7 +573,7 @@ ikv_status ikv_pages_release(const ikv_shape *shape, ikv_cache *cache, const ikv
 /* Sequence dst[i] continues from sequence src[i], i < n (both device [n]): it shares every page of
  * src[i], whose refs grow, and takes over len, next_pos, start, its rows of pos, of ema (or NULL) and of
  * vnorm.  No page is copied: ikv_pages_writable does that where a sequence first writes.  Each
- * dst[i] holds no page (ikv_pages_release at len 0), appears once and is no src. */
+ * dst[i] holds no page (ikv_pages_release at len 0), appears once and is no src.  n is at most 65535. */
 ikv_status ikv_pages_fork(const ikv_shape *shape, ikv_cache *cache, const ikv_pages *pages, int32_t n,
                           const int32_t *src, const int32_t *dst, float *ema, cudaStream_t stream);
 

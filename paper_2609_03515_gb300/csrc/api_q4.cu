@@ -199,7 +199,6 @@ ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, c
     IKV_TRY_CUDA(launch_q4_attend(a, shape->dtype, shape->head_dim, ctas, stream), "4-bit attend launch");
     Q4FinishArgs f{};
     f.len = cache->len;
-    f.start = cache->start;
     f.batch = shape->batch;
     f.q_heads = shape->q_heads;
     f.kv_heads = shape->kv_heads;

@@ -73,7 +73,7 @@ int32_t q4_attend_ctas(const ikv_shape *s, int32_t max_len, int sms);
 cudaError_t launch_q4_attend(const Q4AttendArgs &a, int dtype, int head_dim, int32_t ctas, cudaStream_t st);
 
 struct Q4FinishArgs {
-    const int32_t *len, *start;
+    const int32_t *len;
     int32_t batch, q_heads, kv_heads, rows_per_seq, cap, head_dim, bf16;
     const float *logits;
     int32_t lstride;
@@ -102,7 +102,8 @@ struct PagesArgs {
 };
 // scratch of one call: what its kernels hand to one another
 struct PagesWs {
-    int32_t *total;                   // [4]: jobs, whether there were pages enough, -, -
+    int32_t *total;                   // [4]: jobs; whether there were pages enough (compaction);
+                                      // rows of the longest copy (writable); -
     int32_t *free_ids;                // [batch * max_pages] the free pages that the call takes, ascending
     int32_t *count, *last;            // [num_pages] writers of a shared page, the last of them
     int32_t *jobs;                    // [batch * max_pages][4]; a compaction's old table entries

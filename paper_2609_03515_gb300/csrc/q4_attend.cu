@@ -268,7 +268,7 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a, Span &sp) {
 // group (a group of 8 or fewer), 16 channels its depth.  A group of 32 channels is two of them
 // and has one scale, so codes are converted to fp16 as they are (exact) and the scale
 // multiplies the group's fp32 sum.  q is scaled by a power of two to [2^7, 2^8) and held in fp16
-// (bf16 queries: exact down to 2^-22 of the largest; fp32 queries: two terms).
+// (bf16 queries: exact down to 2^-22 of the largest; fp32 queries: two terms, 2^-22 of each).
 // O^T = V^T P^T: the rows are channels, the depth the 16 tokens; V's scales, which differ from
 // token to token, multiply the probabilities instead, once for each group of channels, in fp32
 // before they are rounded to fp16 (fp32 outputs: two terms, 2^-22 of a weight; bf16 outputs: one, 2^-11
@@ -817,9 +817,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend
 
 // The rest of a call: outputs of units of several segments (or of none: 0), Eq. 1's scores and Eq. 4.
 //
-// The first CTAs take a utility row's tokens: kFinishThreads / HS of them each, HS threads a token
-// that share the row's heads, or blocks of V kFinishThreads, V tokens a thread, every row_ctas-th of the row; the others merge a head's outputs (MANY: each a CTA, its warps a part of
-// the segments each; else a head a warp).  A head's reference and sum come from
+// The first token_ctas CTAs take the utility rows' tokens, row_ctas of them a row: a block of
+// kFinishThreads / HS tokens each, with HS threads a token that share the row's heads, or (V = 4) every
+// row_ctas-th block of V kFinishThreads, with V tokens a thread.  The CTAs behind them merge the heads'
+// outputs: MANY, a CTA a head, each of whose warps sums a part of the segments; else a warp a head.  A head's reference and sum come from
 // its segments' pairs of them, so no pass of its own has to gather them; a probability is
 // 2^(logit - reference) / sum, with the logit's factor applied here, as in the sum, without another rounding.
 constexpr int kFinishThreads = 512;
@@ -1121,13 +1122,15 @@ cudaError_t launch_finish_t(Q4FinishArgs a, int64_t rows, int32_t max_len, int s
 template <bool MANY>
 cudaError_t launch_finish(const Q4FinishArgs &a, int32_t max_len, int sms, cudaStream_t st) {
     const int64_t rows = a.score || a.ema ? (int64_t)a.batch * a.rows_per_seq : 0;
-    // as many threads a token as it takes to give every SM a CTA
-    // as many tokens as four a thread take half of the SMs for: each CTA then gathers its row's log-sum-exps once
-    // for several blocks of them (32 x 12k to 16k, 4 rows a sequence, 28 heads: 92 -> 66 us with the attention;
-    // 32 ragged sequences of 4k to 8k, 32 heads: 59.4 -> 57.5; 16 of them are slower so)
+    // Four tokens a thread from as many tokens on as take half of the SMs then: a CTA gathers its row's references
+    // and sums once for several blocks of them.  us with the attention, one token a thread / four, batches of
+    // 4k to 8k: 32 heads, a row a sequence, 64 blocks of 2048 tokens 31.7 / 33.4, 80 37.6 / 39.0, 96 45.8 / 45.6, 128
+    // 56.8 / 55.7, 192 81.4 / 77.0; 16 heads, 64 17.5 / 17.6, 80 19.9 / 19.5, 192 34.7 / 30.8; 28 heads, a row for
+    // each of 4 KV heads, 64 12.9 / 12.5, 96 16.3 / 15.1, 256 27.8 / 21.7.
     const bool aligned = (reinterpret_cast<uintptr_t>(a.score) | reinterpret_cast<uintptr_t>(a.ema)) % 16 == 0;
     if (aligned && rows > 0 && 2 * rows * ((max_len + 4 * kFinishThreads - 1) / (4 * kFinishThreads)) >= sms)
         return launch_finish_t<1, MANY, 4>(a, rows, max_len, sms, st);
+    // else as many threads a token as it takes to give every SM a CTA
     if (rows * ((max_len + kFinishThreads - 1) / kFinishThreads) >= sms) return launch_finish_t<1, MANY, 1>(a, rows, max_len, sms, st);
     if (rows * ((max_len + kFinishThreads / 4 - 1) / (kFinishThreads / 4)) >= sms)
         return launch_finish_t<4, MANY, 1>(a, rows, max_len, sms, st);
@@ -1152,7 +1155,12 @@ cudaError_t launch_q4_attend(const Q4AttendArgs &a, int dtype, int head_dim, int
 }
 
 cudaError_t launch_q4_finish(const Q4FinishArgs &a, int32_t ctas, int32_t max_len, int sms, cudaStream_t st) {
-    // segments of a unit, if all are alike
+    // A CTA a head from a mean of 8 segments a unit on.  us with the attention, a warp a head / a CTA, without and with
+    // scores (8 KV heads, 32 heads): one sequence, 8 segments 7.7 / 7.4 and 8.1 / 7.8, 16 8.1 / 7.9 and 10.0 / 8.6,
+    // 57 18.4 / 15.9 and 26.5 / 18.0; two, 8 7.7 / 8.1 and 8.6 / 8.7, 28 22.9 / 21.3 and 34.0 / 27.6; four, 14 33.8 /
+    // 33.2 and 39.4 / 41.0; six, 9.5 45.7 / 45.7 and 55.0 / 56.6; eight, 7 21.1 / 21.3 and 25.2 / 28.3; sixteen, 3.6
+    // 34.9 / 37.6 and 39.1 / 44.0.  The host knows the mean alone: one long sequence among short ones
+    // (60000 and 15 of 300: 25.4 / 23.0 and 38.2 / 32.6) goes by a warp a head.
     return ctas > 8 * (int64_t)a.batch * a.kv_heads ? launch_finish<true>(a, max_len, sms, st)
                                                      : launch_finish<false>(a, max_len, sms, st);
 }
