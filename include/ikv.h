@@ -131,8 +131,7 @@ typedef struct {
                                     of their workspaces) refuse with IKV_ERR_UNSUPPORTED.  The ikv_q4_*
                                     calls take either. */
     int32_t *writable;           /* page pools: [batch][2] (device), or NULL: the slots [first, end) that
-                                    the last ikv_pages_writable found or made each sequence's own, see
-                                    there.  When set, ikv_append_token, ikv_q4_append_token and
+                                    ikv_pages_writable found or made each sequence's own, see there.  When set, ikv_append_token, ikv_q4_append_token and
                                     ikv_q4_store leave out a sequence whose slots lie outside them;
                                     ikv_step* and ikv_compact_kv do not go by them and refuse
                                     (IKV_ERR_UNSUPPORTED). */
@@ -231,7 +230,8 @@ int64_t ikv_launch_count(void);
  * bit 5: rows of ikv_q4_store or ikv_q4_load lay outside a sequence's slot space (left alone);
  * bit 6: ikv_pages_writable or ikv_pages_compact needed more pages than were free (nothing was
  * done); bit 7: a sequence number or a block table entry that a page call met was out of range, or
- * ikv_pages_compact was told to keep a slot without a page. */
+ * ikv_pages_compact was told to keep a slot without a page; bit 8: an append or ikv_q4_store left out a
+ * sequence that cache->writable grants other slots. */
 ikv_status ikv_device_status(uint32_t *flags);
 
 /* Test of the bounded waits (no counterpart in the paper): the next tensor-core attention
@@ -588,11 +588,13 @@ ikv_status ikv_pages_fork(const ikv_shape *shape, ikv_cache *cache, const ikv_pa
  * A sequence whose slots would pass its slot space is left out and sets bit 2.
  * Behind a shortage, calls that are already enqueued would write into page 0 or into pages that others
  * hold: either the host reads `lacking` before it enqueues them, or cache->writable is given.  Each
- * sequence that was asked about (first >= 0, count > 0) then gets writable[b] = {first[b], first[b] + count[b]} if
- * every page of these slots is its own now (also of one that had all of its pages while others
- * lacked theirs), else {0, 0}, and the stores and appends behind leave it out.  The other sequences keep
- * theirs.  The caller starts with zeros and gives all page calls the same cache->writable; ikv_pages_fork (both sequences), ikv_pages_compact and an
- * ikv_pages_release that takes a page put {0, 0} there. */
+ * sequence whose slots' pages are all its own then (one that had all of its pages gets there while others
+ * lack theirs) receives writable[b] = {first[b], first[b] + count[b]}, joined with what stood there if the two
+ * touch; the others keep what they have.  Stores and appends behind leave out a sequence whose slots
+ * lie outside, without a word where it holds {0, 0} (never granted any), else with bit 8 of the device
+ * error word.  The caller starts with zeros and gives all page calls the same cache->writable;
+ * ikv_pages_fork (both sequences), ikv_pages_compact and an ikv_pages_release that takes a page put
+ * {0, 0} there. */
 ikv_status ikv_pages_writable(const ikv_shape *shape, ikv_cache *cache, const ikv_pages *pages, const int32_t *first,
                               const int32_t *count, int32_t max_count, int32_t *lacking, void *ws, size_t ws_bytes,
                               cudaStream_t stream);

@@ -1049,6 +1049,6 @@ extern "C" ikv_status ikv_device_status(uint32_t *flags) {
     if (e == cudaSuccess) e = ikv::read_clear_q4_error(&q4);
     if (e == cudaSuccess) e = ikv::read_clear_pages_error(&pg);
     if (e != cudaSuccess) return ikv::report(IKV_ERR_CUDA, "ikv_device_status: %s", cudaGetErrorString(e));
-    *flags = v | at | (ap ? 4u : 0u) | lw | tr | q4 | pg;
+    *flags = v | at | (ap & 1u ? 4u : 0u) | (ap & 2u ? 256u : 0u) | lw | tr | q4 | pg;
     return IKV_OK;
 }

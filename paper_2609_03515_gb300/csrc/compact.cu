@@ -475,7 +475,8 @@ constexpr int kAppendRows = 8;
 
 }  // namespace
 
-__device__ unsigned int g_append_error = 0;  // bit 0: an append found no free slot (start + len = cap)
+// bit 0: an append found no free slot (start + len = cap); bit 1: one was left out, with slots granted elsewhere
+__device__ unsigned int g_append_error = 0;
 
 namespace {
 
@@ -486,7 +487,8 @@ __global__ void __launch_bounds__(kCompThreads) append_kernel(const AppendArgs a
     const int b = blockIdx.y;
     const int L = a.len[b];
     const int S = a.pv.start_of(b);
-    const bool left_out = a.writable && (L < a.writable[2 * b] || L >= a.writable[2 * b + 1]);
+    const int2 may = a.writable ? make_int2(a.writable[2 * b], a.writable[2 * b + 1]) : make_int2(L, L + 1);
+    const bool left_out = L < may.x || L >= may.y;
     const bool room = !left_out && S + L < a.cap;
     const int kvh = a.pv.kv_heads;
     const int nkv = a.layers * kvh;
@@ -558,8 +560,8 @@ __global__ void __launch_bounds__(kCompThreads) append_kernel(const AppendArgs a
             if (room) {
                 a.len[b] = L + 1;
                 a.next_pos[b] = a.next_pos[b] + 1;
-            } else if (!left_out) {
-                atomicOr(&g_append_error, 1u);  // the token was not stored; ikv_device_status reports it
+            } else if (!left_out || may.x < may.y) {
+                atomicOr(&g_append_error, left_out ? 2u : 1u);  // the token was not stored; ikv_device_status reports it
             }
         }
         return;
@@ -569,8 +571,8 @@ __global__ void __launch_bounds__(kCompThreads) append_kernel(const AppendArgs a
             if (room) {
                 a.len[b] = L + 1;
                 a.next_pos[b] = a.next_pos[b] + 1;
-            } else if (!left_out) {
-                atomicOr(&g_append_error, 1u);  // the token was not stored; ikv_device_status reports it
+            } else if (!left_out || may.x < may.y) {
+                atomicOr(&g_append_error, left_out ? 2u : 1u);  // the token was not stored; ikv_device_status reports it
             }
             a.done[b] = 0;
         }

@@ -374,7 +374,7 @@ struct TraceArgs {
 cudaError_t launch_trace_gather(const TraceArgs &a, int32_t max_len, cudaStream_t st);
 cudaError_t launch_trace(const TraceArgs &a, cudaStream_t st);
 cudaError_t read_clear_trace_error(unsigned int *v);
-// reads and clears the append kernel's device error word (bit 0: no free slot)
+// reads and clears the append kernel's device error word (bit 0: no free slot; bit 1: left out)
 cudaError_t read_clear_append_error(unsigned int *v);
 // the same of the 4-bit stores and loads (bit 5) and of the page calls (bits 2, 6, 7)
 cudaError_t read_clear_q4_error(unsigned int *v);

@@ -314,16 +314,25 @@ writable_plan_kernel(const PagesArgs a, const PagesWs w, const int32_t *first, c
         }
     }
     if (!a.writable) return;
-    // granted: the slots whose pages are all the sequence's own, as tables and counts are now
+    // granted: the slots whose pages are all the sequence's own, as tables and counts are now; with
+    // those that it had, if they touch
     for (int s = threadIdx.x; s < a.batch; s += kPlanThreads) {
         const int2 x = asked(s);
-        if (x.y > 0) a.writable[s] = (int64_t)start_of(a, s) + x.x + x.y > a.cap ? make_int2(0, 0) : make_int2(x.x, x.x + x.y);
+        w.begin[s] = x.y > 0 && (int64_t)start_of(a, s) + x.x + x.y <= a.cap;
     }
     __syncthreads();
     for (int64_t i = threadIdx.x; i < R; i += kPlanThreads) {
         if (!page_of(i, &b, &lp)) continue;
         const int e = __ldcg(a.table + (int64_t)b * a.max_pages + lp);
-        if (e <= 0 || e >= a.num_pages || __ldcg(a.refs + e) != 1) forget_granted(a, b);
+        if (e <= 0 || e >= a.num_pages || __ldcg(a.refs + e) != 1) w.begin[b] = 0;
+    }
+    __syncthreads();
+    for (int s = threadIdx.x; s < a.batch; s += kPlanThreads) {
+        if (!w.begin[s]) continue;
+        const int2 x = asked(s), had = a.writable[s];
+        int2 now = make_int2(x.x, x.x + x.y);
+        if (had.x < had.y && had.x <= now.y && now.x <= had.y) now = make_int2(min(had.x, now.x), max(had.y, now.y));
+        a.writable[s] = now;
     }
 }
 

@@ -3,7 +3,7 @@
 
 namespace ikv {
 
-__device__ unsigned int g_q4_error = 0;  // bit 5: rows outside a sequence's slot space
+__device__ unsigned int g_q4_error = 0;  // bit 5: rows outside a sequence's slot space; bit 8: outside those granted
 
 namespace {
 
@@ -158,7 +158,13 @@ __global__ void __launch_bounds__(kMoveThreads, 3) q4_move_kernel(const Q4MoveAr
         if (threadIdx.x == 0) atomicOr(&g_q4_error, 32u);
         return;
     }
-    if (STORE && a.writable && (first < a.writable[2 * b] || first + n > a.writable[2 * b + 1])) return;
+    if (STORE && a.writable) {
+        const int lo = a.writable[2 * b], hi = a.writable[2 * b + 1];
+        if (first < lo || first + n > hi) {
+            if (threadIdx.x == 0 && lo < hi) atomicOr(&g_q4_error, 256u);
+            return;
+        }
+    }
     const int rows = n * G;
     if (blk * RPP * ROWS >= rows) return;
     const int u = threadIdx.x & (kUnits - 1), r0 = blk * RPP * ROWS + threadIdx.x / kUnits;

@@ -4,6 +4,7 @@ import random
 
 import pytest
 import torch
+from test_gpu_q4 import quantise, values
 
 from paper_2609_03515_gb300 import DecodeCache, Q4Cache, ikv
 
@@ -49,7 +50,7 @@ def test_a_shortage_leaves_the_rest_alone(kind):
     # three copies and a page behind the last sequence's first: two are free
     ikv.ikv_pages_writable(shape, cache, pages, None, None, 1, lacking, ws, ws.numel())
     assert int(lacking) == 2 and ikv.ikv_device_status() == 64
-    assert c.writable.tolist() == [[0, 0]] * 4 + [[7, 8], [0, 0]]
+    assert c.writable.tolist() == [[0, 0]] * 4 + [[0, 8], [0, 16]]
     held, books = [t.clone() for t in c.planes()], [t.clone() for t in (c.pos, c.ema, c.next_pos, c.block_table, c.refs)]
     x = torch.randn(2, 6, 2, 64, generator=gen, device="cuda").to(torch.bfloat16)
     append(kind, c, x, slot)
@@ -58,7 +59,7 @@ def test_a_shortage_leaves_the_rest_alone(kind):
         # a store that goes by its own list of slots
         rows = c.dense_rows(x.unsqueeze(2))
         ikv.ikv_q4_store(shape, cache, c.q4(), 0, 2, x, x, rows, i32([5, 5, 5, 5, 8, 16]), None, 1)
-    assert ikv.ikv_device_status() == 0
+    assert ikv.ikv_device_status() == 256
     assert c.len.tolist() == [5, 5, 5, 5, 8, 16]
     own = int(c.block_table[4, 0])
     for t, was in zip(c.planes(), held):
@@ -70,15 +71,15 @@ def test_a_shortage_leaves_the_rest_alone(kind):
         assert torch.equal(t, was) if t.shape[0] != 6 else torch.equal(t[rest], was[rest])
     # pages come back: the same calls go through
     ikv.ikv_pages_writable(shape, cache, pages, i32([-1, 5, 5, -1, -1, -1]), None, 1, lacking, ws, ws.numel())
-    assert int(lacking) == 0 and c.writable.tolist() == [[0, 0], [5, 6], [5, 6], [0, 0], [7, 8], [0, 0]]
+    assert int(lacking) == 0 and c.writable.tolist() == [[0, 0], [5, 6], [5, 6], [0, 0], [0, 8], [0, 16]]
     append(kind, c, x, slot)
-    assert ikv.ikv_device_status() == 0 and c.len.tolist() == [5, 6, 6, 5, 8, 16]
+    assert ikv.ikv_device_status() == 256 and c.len.tolist() == [5, 6, 6, 5, 8, 16]
 
 
 @pytest.mark.parametrize("ps,nb,most,pool,scarce", [(16, 6, 20, 12, True), (32, 5, 3, 6, False), (48, 300, 60, 200, True)])
 def test_grants_follow_the_pages(ps, nb, most, pool, scarce):
-    """Random lives: after every call a sequence's grant is what it was last given, while all of its pages
-    are its own; forks, compactions and releases take it back."""
+    """Random lives: a sequence's grant is what it was last given, with what touched it before, and all of its
+    pages are the sequence's own; forks, compactions and releases take it back."""
     rng = random.Random(ps)
     starts = [rng.choice([0, 0, 2 * ps + 1]) for _ in range(nb)]
     c = make("q4", nb, pool, cap=5 * ps, ps=ps, starts=starts)
@@ -103,8 +104,11 @@ def test_grants_follow_the_pages(ps, nb, most, pool, scarce):
                 s = starts[b] + first[b]
                 own = s + n <= c.cap and all(table[b][p] and refs[table[b][p]] == 1
                                              for p in range(s // c.page_size, (s + n - 1) // c.page_size + 1))
-                want[b] = [first[b], first[b] + n] if own else [0, 0]
                 if own:
+                    lo, hi = first[b], first[b] + n
+                    if want[b][0] < want[b][1] and want[b][0] <= hi and lo <= want[b][1]:
+                        lo, hi = min(lo, want[b][0]), max(hi, want[b][1])
+                    want[b] = [lo, hi]
                     lens[b] = max(lens[b], first[b] + n)
             c.len.copy_(i32(lens))
         elif what == "fork":
@@ -129,6 +133,10 @@ def test_grants_follow_the_pages(ps, nb, most, pool, scarce):
             after = c.block_table.tolist()
             want = [w if x == y else [0, 0] for w, x, y in zip(want, table, after)]
         assert c.writable.tolist() == want
+        table, refs = c.block_table.tolist(), c.refs.tolist()
+        for b, (lo, hi) in enumerate(want):
+            for p in range((starts[b] + lo) // ps, (starts[b] + hi - 1) // ps + 1) if lo < hi else ():
+                assert table[b][p] > 0 and refs[table[b][p]] == 1
     assert short or not scarce
 
 
@@ -155,14 +163,36 @@ def test_one_token_each_in_a_graph():
     assert c.len.tolist() == [16, 16, 16] and ikv.ikv_device_status() == 0
     g.replay()  # three pages are wanted, one is free: none is handed out
     torch.cuda.synchronize()
-    assert c.len.tolist() == [16, 16, 16] and ikv.ikv_device_status() == 64 and int((c.refs[1:] > 0).sum()) == 3
+    assert c.len.tolist() == [16, 16, 16] and ikv.ikv_device_status() == 64 + 256 and int((c.refs[1:] > 0).sum()) == 3
     c.len[1] = 0
     ikv.ikv_pages_release(shape, cache, pages, 0)
     g.replay()  # now two are, for the two that go on; the third starts anew and takes none
     torch.cuda.synchronize()
-    assert ikv.ikv_device_status() == 64 and c.len.tolist() == [16, 0, 16]
+    assert ikv.ikv_device_status() == 64 + 256 and c.len.tolist() == [16, 0, 16]
     c.len[2] = 0
     ikv.ikv_pages_release(shape, cache, pages, 0)
     g.replay()
     torch.cuda.synchronize()
     assert ikv.ikv_device_status() == 0 and c.len.tolist() == [17, 1, 1]
+
+
+def test_chunks_are_granted_together():
+    """A prompt in two pieces, both granted before either is stored; a piece that touches neither is refused."""
+    c = make("q4", 1, 6)
+    shape, cache, pages, ws = c.shape(), c.cache(c.cap - 1), c.pages(), c.pages_workspace()
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(2, 1, 40, 2, 64, generator=gen, device="cuda").to(torch.bfloat16)
+    for first, n in ((0, 20), (20, 20)):
+        ikv.ikv_pages_writable(shape, cache, pages, i32([first]), None, n, None, ws, ws.numel())
+    assert c.writable.tolist() == [[0, 40]]
+    for first, n in ((0, 20), (20, 20)):
+        part = x[:, :, first:first + n]
+        ikv.ikv_q4_store(shape, cache, c.q4(), 0, 2, part, part, c.dense_rows(part), i32([first]), None, n)
+    assert ikv.ikv_device_status() == 0
+    back, other = torch.zeros_like(x), torch.zeros_like(x)
+    ikv.ikv_q4_load(shape, cache, c.q4(), 0, 2, back, other, c.dense_rows(back), i32([0]), None, 40)
+    want = values(*quantise(x)).to(torch.bfloat16)
+    assert torch.equal(back, want) and torch.equal(other, want)
+    held = [t.clone() for t in c.planes()]
+    ikv.ikv_q4_store(shape, cache, c.q4(), 0, 2, x, x, c.dense_rows(x), i32([30]), None, 20)  # 30 .. 49
+    assert ikv.ikv_device_status() == 256 and all(torch.equal(t, was) for t, was in zip(c.planes(), held))
