@@ -284,11 +284,11 @@ __device__ __forceinline__ Run run_of(const Q4AttendArgs &a, Span &sp) {
 // columns; logits, weights and scales then take half the instructions, and a head's two columns
 // are joined like two warps (16 ragged sequences of 4k to 8k, 32 / 8 heads: 39.0 -> 36.7 us).
 //
-// Memory allows a tile of 128 channels 99 cycles of an SM.  It takes about 250 instructions (224
+// Memory allows a tile of 128 channels 99 cycles of an SM.  It takes about 265 instructions (229
 // DUAL), 64 of them conversions of codes that fill the ALU pipe for 32 cycles; 12 warps issue some
-// 2.3 a cycle, which hides most of them.  32 sequences of 12k to 16k, 28 / 4 heads: 264 MB in
-// 52.2 us with the merge (5.1 TB/s), of which waiting for the tiles alone takes 47.8; one of 32k,
-// 32 / 8 heads, 38 MB in 12 us, 17.6 with its scores: lengths, table and first tiles are 4 of them,
+// 2.2 a cycle, which hides most of them.  32 sequences of 12k to 16k, 28 / 4 heads: 264 MB in
+// 53.0 us with the merge (5.0 TB/s), of which waiting for the tiles alone takes 47.8; one of 32k,
+// 32 / 8 heads, 38 MB in 12 us, 17.8 with its scores: lengths, table and first tiles are 4 of them,
 // the join 1.5.  A third stage was slower (54.5 us where two took 52.6).
 template <int D, typename T, bool SCORE, bool DUAL>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, sizeof(T))) q4_attend_kernel(const Q4AttendArgs a) {
