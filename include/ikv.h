@@ -527,7 +527,7 @@ ikv_status ikv_q4_append_token(const ikv_shape *shape, ikv_cache *cache, const i
  * sequence without a live slot gets out = 0.  Slots outside [0, len[b]) are never used, whatever
  * they hold.  A NaN group of a live V row makes its 32 channels NaN for that KV head's queries, one
  * of a live K row every channel.  Logits are formed with q scaled up to 2^8: rows of K above 2^112 may
- * overflow them, which leaves NaN.  Fails with IKV_ERR_SHAPE where batch * kv_heads * cap passes
+ * overflow them, which leaves NaN or zeros.  Fails with IKV_ERR_SHAPE where batch * kv_heads * cap passes
  * 2.5e10 slots or the pool 6.8e10 rows, and above 8192 query heads. */
 ikv_status ikv_q4_attend_score(const ikv_shape *shape, const ikv_cache *cache, const ikv_q4 *q4, int32_t layer,
                                const void *q, void *out, float *score, float *ema, float alpha, void *ws,
