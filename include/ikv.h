@@ -612,6 +612,73 @@ ikv_status ikv_pages_compact(const ikv_shape *shape, ikv_cache *cache, const ikv
                              const int32_t *keep_len, float *ema, int32_t *lacking, void *ws, size_t ws_bytes,
                              cudaStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Decode attention of sequences that share a prefix
+ *
+ * Sequences that continue from one prompt (ikv_pages_fork) hold the same rows in their first
+ * slots.  ikv_decode_attend_score reads those rows once for each sequence; ikv_prefix_attend_score
+ * reads them once for all sequences of a group.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    int32_t n_groups;            /* 0: no sequence shares anything */
+    const int32_t *first;        /* [n_groups + 1] (device): group i is member[first[i]] .. member[first[i + 1] - 1] */
+    const int32_t *member;       /* [first[n_groups]] (device): sequence numbers; each sequence at most once */
+    const int32_t *len;          /* [n_groups] (device): slots 0 .. len[i] - 1 of the members hold the same rows */
+} ikv_prefix;
+
+/* ikv_decode_attend_score with the groups' prefixes computed once: the same q, out, score, ema,
+ * granularity and dead slots, and the same results up to the order of the sums.
+ *  - K and V of slots 0 .. P - 1 of a group's members are read from the first member's pages, with
+ *    P = min(len[i], the members' lengths); what the other members' tables hold there is not looked
+ *    at (shared pages and copies serve alike).  Each member's liveness (pos) is its own.
+ *  - Sequences in no group, and slots behind the prefix, are read from their own pages.
+ *  - A sequence without a live slot gets out = 0.  Slots outside a sequence are never used, whatever
+ *    they hold, and a row that a query does not see (dead, or another sequence's) never reaches its
+ *    output, NaN and infinities included.
+ *  - A member that is no sequence number, or that an earlier entry names already, is left out, and so
+ *    are entries behind the first `batch` ones: bit 7 of the device error word.
+ * No page size is excluded; bf16 rows in pages of a multiple of 8 slots take the tensor cores.
+ * Dense caches only (IKV_ERR_UNSUPPORTED for code_bits = 4).  Goes by len[], not by cache->max_len.
+ *  ws: at least ikv_prefix_workspace_size() bytes. */
+ikv_status ikv_prefix_workspace_size(const ikv_shape *shape, const ikv_cache *cache, const ikv_prefix *prefix,
+                                     size_t *bytes);
+ikv_status ikv_prefix_attend_score(const ikv_shape *shape, const ikv_cache *cache, const ikv_prefix *prefix,
+                                   int32_t layer, const void *q, void *out, float *score, float *ema, float alpha,
+                                   void *ws, size_t ws_bytes, cudaStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention of the newest tokens through a sliding window with sinks
+ *
+ * Causal attention of the newest count[b] tokens of every sequence over its cache, from one token
+ * (decode) to a whole prompt (prefill).  Their K and V rows are in the cache already: query i of
+ * sequence b sits at slot p = len[b] - count[b] + i.  It sees slot j if 0 <= j <= p and
+ * (j > p - window or j < sinks), and, with cache->dead_slots, if j is live:
+ *     out = softmax(q . K_j / sqrt(d)) V_j over the slots it sees, 0 if it sees none.
+ * The window counts slots, not positions.  Slots no query sees are not read.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    int32_t window;              /* slots a query sees up to its own, >= 1; 0: all of them */
+    int32_t sinks;               /* first slots of the sequence that every query sees, >= 0 */
+    const int32_t *row0;         /* [batch] (device) row of each sequence's first query in q and out; NULL: b * max_count */
+    const int32_t *count;        /* [batch] (device) query tokens, cut to [0, max_count]; NULL: max_count each */
+    int32_t max_count;           /* HOST-side upper bound on every count[b] */
+    int64_t q_stride, out_stride; /* elements from a token's row of q (of out) to the next, multiples of 16 bytes;
+                                    0: q_heads * head_dim */
+} ikv_window;
+
+/*  q: row r holds a token's q_heads * head_dim values (dtype) at r * q_stride; out likewise.  Rows of out
+ *  that belong to no query are left as they are; the sequences' rows must not overlap in out.
+ * A query in front of the first slot (count[b] > len[b]) sees nothing.  What a query does not see
+ * never reaches its output, NaN and infinities included.  Dense caches only (IKV_ERR_UNSUPPORTED for
+ * code_bits = 4); no page size is excluded, bf16 rows in pages of a multiple of 8 slots take the tensor
+ * cores.  Goes by len[], not by cache->max_len.  granularity matters for dead slots only.
+ * Fails with IKV_ERR_SHAPE where batch * max_count * q_heads passes 2^30.
+ *  ws: at least ikv_window_workspace_size() bytes. */
+ikv_status ikv_window_workspace_size(const ikv_shape *shape, const ikv_cache *cache, const ikv_window *window,
+                                     size_t *bytes);
+ikv_status ikv_window_attend(const ikv_shape *shape, const ikv_cache *cache, const ikv_window *window, int32_t layer,
+                             const void *q, void *out, void *ws, size_t ws_bytes, cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

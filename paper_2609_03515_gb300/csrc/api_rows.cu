@@ -1,0 +1,192 @@
+// C ABI of the shared-prefix decode and of the sliding window: argument checks, workspace, launches.
+#include <cmath>
+
+#include "rows.cuh"
+
+using namespace ikv;
+
+namespace {
+
+ikv_status check_rows(const ikv_shape *s, const ikv_cache *c) {
+    clear_error();
+    ikv_status e = check_shape(s);
+    if (e) return e;
+    if ((e = check_dense(s, c, false))) return e;
+    if (s->q_heads > 8192) return report(IKV_ERR_SHAPE, "more than 8192 query heads");
+    return IKV_OK;
+}
+
+ikv_status check_prefix(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p) {
+    const ikv_status e = check_rows(s, c);
+    if (e) return e;
+    if (!p) return report(IKV_ERR_ARG, "prefix is NULL");
+    if (p->n_groups < 0) return report(IKV_ERR_ARG, "n_groups must be >= 0");
+    if (p->n_groups > 0 && (!p->first || !p->member || !p->len))
+        return report(IKV_ERR_ARG, "prefix first/member/len is NULL");
+    if (p->n_groups > (1 << 20) || (int64_t)s->batch * s->q_heads > 1 << 28)
+        return report(IKV_ERR_SHAPE, "too many groups or query rows");
+    return IKV_OK;
+}
+
+ikv_status check_window(const ikv_shape *s, const ikv_cache *c, const ikv_window *w) {
+    const ikv_status e = check_rows(s, c);
+    if (e) return e;
+    if (!w) return report(IKV_ERR_ARG, "window is NULL");
+    if (w->window < 0 || w->sinks < 0) return report(IKV_ERR_ARG, "window and sinks must be >= 0");
+    if (w->max_count < 0) return report(IKV_ERR_ARG, "max_count must be >= 0");
+    if ((int64_t)s->batch * w->max_count > ((int64_t)1 << 30) / s->q_heads)
+        return report(IKV_ERR_SHAPE, "batch * max_count * q_heads too large");
+    const int64_t row = (int64_t)s->q_heads * s->head_dim, unit = s->dtype == IKV_BF16 ? 8 : 4;
+    for (const int64_t x : {w->q_stride, w->out_stride}) {
+        if (x == 0) continue;
+        if (x < row) return report(IKV_ERR_SHAPE, "a token's row holds %lld elements", (long long)row);
+        if (x % unit) return report(IKV_ERR_ALIGN, "rows of q and out must lie on 16-byte boundaries");
+    }
+    return IKV_OK;
+}
+
+// The arguments of a call but for its pointers to q and results, and its workspace: *bytes of it, at ws
+// if there is one.
+RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, const ikv_window *w, void *ws,
+                   size_t *bytes) {
+    RowsArgs a{};
+    a.k = c->k;
+    a.v = c->v;
+    a.pv = view_of(s, c);
+    a.len = c->len;
+    a.pos = c->dead_slots ? c->pos : nullptr;
+    a.rows_per_seq = rows_per_seq(s);
+    a.cap = cap_of(c);
+    a.batch = s->batch;
+    a.q_heads = s->q_heads;
+    a.group = s->q_heads / s->kv_heads;
+    a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)s->head_dim));
+    a.q_stride = a.out_stride = (int64_t)s->q_heads * s->head_dim;
+    a.ctas = sm_count() * rows_simt_ctas_per_sm(s->head_dim);
+    if (a.ctas > kRowsMaxCtas) a.ctas = kRowsMaxCtas;
+    const int most = kRowsSimt / a.group;
+    const int n = p ? s->batch : w->max_count;
+    a.unit_n = most;
+    a.rows_cap = (n < most ? n : most) * a.group;
+    int64_t units;
+    if (w) {
+        if (w->q_stride) a.q_stride = w->q_stride;
+        if (w->out_stride) a.out_stride = w->out_stride;
+        a.window = w->window > 0 && w->window < 1 << 30 ? w->window : 1 << 30;
+        a.sinks = w->sinks < 1 << 30 ? w->sinks : 1 << 30;
+        a.row0 = w->row0;
+        a.count = w->count;
+        a.max_count = w->max_count;
+        a.seq_units = (w->max_count + a.unit_n - 1) / a.unit_n;
+        units = (int64_t)s->batch * a.seq_units;
+    } else {
+        a.prefix = 1;
+        a.n_groups = p->n_groups;
+        a.first = p->first;
+        a.member = p->member;
+        a.group_len = p->len;
+        units = (int64_t)p->n_groups + s->batch / a.unit_n + s->batch;
+    }
+    size_t off = 0;
+    auto take = [&](auto *&x, size_t count) {
+        x = ws ? at<std::remove_reference_t<decltype(*x)>>(ws, off) : nullptr;
+        off = align256(off + count * sizeof(*x));
+    };
+    take(a.head, 1);
+    take(a.start, a.ctas);
+    take(a.units, units);
+    const size_t pre = p ? (size_t)(p->n_groups + s->batch / a.unit_n) * s->kv_heads + a.ctas : 2 * (size_t)a.ctas;
+    take(a.part_ml, pre * a.rows_cap);
+    take(a.part_o, pre * a.rows_cap * s->head_dim);
+    if (p) {
+        const size_t nb = s->batch, own = (nb * s->kv_heads + a.ctas) * a.group;
+        take(a.owner, nb);
+        take(a.vm, nb);
+        take(a.entry_group, nb);
+        take(a.group_p, p->n_groups);
+        take(a.group_lead, p->n_groups);
+        take(a.group_unit, p->n_groups);
+        take(a.seq, nb);
+        take(a.lse2, nb * s->q_heads);
+        take(a.own_ml, own);
+        take(a.own_o, own * s->head_dim);
+    }
+    *bytes = off;
+    return a;
+}
+
+ikv_status check_call(const ikv_shape *s, int32_t layer, const void *q, const void *out, const void *ws, size_t ws_bytes,
+                      size_t need) {
+    if (layer < 0 || layer >= s->layers) return report(IKV_ERR_ARG, "layer %d out of range", layer);
+    if (!q || !out) return report(IKV_ERR_ARG, "q/out is NULL");
+    if (!aligned16(q) || !aligned16(out)) return report(IKV_ERR_ALIGN, "q/out must be 16-byte aligned");
+    if (!ws || ws_bytes < need) return report(IKV_ERR_WORKSPACE, "workspace needs %zu bytes", need);
+    if (!aligned16(ws)) return report(IKV_ERR_ALIGN, "workspace must be 16-byte aligned");
+    return IKV_OK;
+}
+
+ikv_status attend(const RowsArgs &a, const ikv_shape *s, cudaStream_t st) {
+    IKV_TRY_CUDA(launch_rows_plan(a, st), "row plan launch");
+    IKV_TRY_CUDA(launch_rows_simt(a, s->dtype, s->head_dim, st), "row attention launch");
+    IKV_TRY_CUDA(launch_rows_merge(a, s->dtype, s->head_dim, st), "row merge launch");
+    return IKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ikv_status ikv_prefix_workspace_size(const ikv_shape *shape, const ikv_cache *cache, const ikv_prefix *prefix,
+                                     size_t *bytes) {
+    const ikv_status e = check_prefix(shape, cache, prefix);
+    if (e) return e;
+    if (!bytes) return report(IKV_ERR_ARG, "bytes is NULL");
+    rows_args(shape, cache, prefix, nullptr, nullptr, bytes);
+    return IKV_OK;
+}
+
+ikv_status ikv_prefix_attend_score(const ikv_shape *shape, const ikv_cache *cache, const ikv_prefix *prefix,
+                                   int32_t layer, const void *q, void *out, float *score, float *ema, float alpha,
+                                   void *ws, size_t ws_bytes, cudaStream_t stream) {
+    ikv_status e = check_prefix(shape, cache, prefix);
+    if (e) return e;
+    size_t need = 0;
+    RowsArgs a = rows_args(shape, cache, prefix, nullptr, ws, &need);
+    if ((e = check_call(shape, layer, q, out, ws, ws_bytes, need))) return e;
+    if (ema && !(alpha >= 0.f && alpha <= 1.f)) return report(IKV_ERR_ARG, "alpha must be in [0, 1]");
+    a.layer = layer;
+    a.q = q;
+    a.out = out;
+    PdlScope pdl;
+    if ((e = attend(a, shape, stream))) return e;
+    if (!score && !ema) return IKV_OK;
+    const RowsScoreArgs sc{alpha, score, ema, cache->max_len};
+    IKV_TRY_CUDA(launch_rows_score(a, sc, shape->dtype, shape->head_dim, stream), "row score launch");
+    return IKV_OK;
+}
+
+ikv_status ikv_window_workspace_size(const ikv_shape *shape, const ikv_cache *cache, const ikv_window *window,
+                                     size_t *bytes) {
+    const ikv_status e = check_window(shape, cache, window);
+    if (e) return e;
+    if (!bytes) return report(IKV_ERR_ARG, "bytes is NULL");
+    rows_args(shape, cache, nullptr, window, nullptr, bytes);
+    return IKV_OK;
+}
+
+ikv_status ikv_window_attend(const ikv_shape *shape, const ikv_cache *cache, const ikv_window *window, int32_t layer,
+                             const void *q, void *out, void *ws, size_t ws_bytes, cudaStream_t stream) {
+    ikv_status e = check_window(shape, cache, window);
+    if (e) return e;
+    size_t need = 0;
+    RowsArgs a = rows_args(shape, cache, nullptr, window, ws, &need);
+    if ((e = check_call(shape, layer, q, out, ws, ws_bytes, need))) return e;
+    if (window->max_count == 0) return IKV_OK;
+    a.layer = layer;
+    a.q = q;
+    a.out = out;
+    PdlScope pdl;
+    return attend(a, shape, stream);
+}
+
+}  // extern "C"

@@ -103,6 +103,7 @@ bool aligned16(const void *p);
 int sm_count();
 ikv_status check_shape(const ikv_shape *s);
 ikv_status check_cache(const ikv_shape *s, const ikv_cache *c, bool need_pos);
+ikv_status check_dense(const ikv_shape *s, const ikv_cache *c, bool need_pos);  // and not in 4 bits
 int rows_per_seq(const ikv_shape *s);
 int32_t cap_of(const ikv_cache *c);
 PagedView view_of(const ikv_shape *s, const ikv_cache *c);
@@ -379,6 +380,8 @@ cudaError_t read_clear_append_error(unsigned int *v);
 // the same of the 4-bit stores and loads (bit 5) and of the page calls (bits 2, 6, 7)
 cudaError_t read_clear_q4_error(unsigned int *v);
 cudaError_t read_clear_pages_error(unsigned int *v);
+// the same of the packed-row attentions (bits 0, 7)
+cudaError_t read_clear_rows_error(unsigned int *v);
 // the same of the kernels of attend.cu (bit 2)
 cudaError_t read_clear_attend_error(unsigned int *v);
 

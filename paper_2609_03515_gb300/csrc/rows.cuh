@@ -1,0 +1,179 @@
+// Attention of packed query rows over paged K/V: what the shared-prefix decode (ikv_prefix_*) and
+// the sliding window (ikv_window_*) have in common.
+//
+// A unit is a set of query rows that read the same slots of one sequence: consecutive query tokens of
+// a sequence (window), the members of a group over their prefix, or one sequence over its own slots
+// behind it (prefix).  Row r of a unit is query head g * G + r % G of its token or member r / G, for
+// each KV head g.  The slots that some row of a unit sees lie in at most two runs of 128-slot tiles:
+// the sinks' and the window's.
+//
+// The tiles of all (unit, KV head) pairs are laid out one behind another and cut into equal shares, one
+// for each CTA of the attention kernel, whatever the lengths are: a CTA takes the pairs, or parts of
+// them, of its share in turn.  A part leaves an unnormalised output and its (max, sum) in the workspace
+// for the merge kernel.  The plan kernel (one CTA) writes the units and where each share begins.
+#pragma once
+#include "ikv_internal.cuh"
+
+namespace ikv {
+
+constexpr int kRowsTile = 128;      // slots a tile
+constexpr int kRowsMaxCtas = 512;
+
+struct RowsUnit {                   // 64 bytes
+    int32_t b;                      // the sequence whose block table is read
+    int32_t m0;                     // window: first query token; prefix: first entry of the member list; -1: one
+                                    // sequence's own slots
+    int32_t n;                      // tokens or members
+    int32_t S0;                     // slots below are numbers in b's slot space: S0 is its slot 0
+    int32_t lo, hi;                 // every visible slot lies in [lo, hi)
+    int32_t p0;                     // window: slot of the first query token (may be below S0)
+    int32_t wlo, sh;                // some row sees the slots of [lo, sh) and of [wlo, hi), none sees others
+    int32_t t_a, n_a, t_w, nt;      // tile i of nt: t_a + i for i < n_a, t_w + i - n_a behind
+    int32_t row0;                   // window: row of query token 0 in q and out
+    int64_t cum;                    // tiles of all earlier units, for all KV heads
+};
+
+struct RowsHead {
+    int64_t total, per;             // tiles in all, tiles of a CTA's share
+    int32_t n_units, n_pre;         // n_pre: units of shared prefixes, in front of the others
+};
+struct RowsStart {                  // where a CTA's share begins, and its tiles
+    int32_t unit, g, j, n;
+};
+struct RowsSeq {                    // prefix: what sequence b's rows are made from
+    int32_t pre, entry;             // its group's unit that holds it (-1: none), its member number there
+    int32_t own;                    // its unit of own slots (-1: none)
+    int32_t len;                    // slots of its prefix
+};
+
+struct RowsArgs {
+    const void *k, *v;
+    PagedView pv;
+    int32_t layer;
+    const int32_t *len;             // [batch]
+    const int32_t *pos;             // [rows][cap], -1 at dead slots, or null
+    int32_t rows_per_seq, cap, batch, q_heads, group;
+    float scale_log2;               // log2(e) / sqrt(d)
+    const void *q;
+    void *out;
+    int64_t q_stride, out_stride;   // elements from a token's (sequence's) heads to the next
+    int32_t unit_n;                 // most tokens or members of a unit
+    // window
+    int32_t window, sinks;          // window in [1, 2^30], sinks in [0, 2^30]
+    const int32_t *row0, *count;
+    int32_t max_count, seq_units;   // seq_units: units of max_count tokens
+    // prefix
+    int32_t prefix;                 // nonzero: a shared-prefix call
+    int32_t n_groups;
+    const int32_t *first, *member, *group_len;
+    // workspace
+    RowsHead *head;
+    RowsStart *start;               // [ctas]
+    RowsUnit *units;
+    int32_t *owner;                 // prefix: [batch] first entry that names the sequence
+    int32_t *vm;                    // prefix: [batch] the entries, -1 where one is left out
+    int32_t *entry_group;           // prefix: [batch] the entries' groups
+    int32_t *group_p, *group_lead, *group_unit;  // prefix: [n_groups] slots shared, first member, first unit
+    RowsSeq *seq;                   // prefix: [batch]
+    float *lse2;                    // prefix: [batch][H] log2-sum-exp
+    // partial results: slot s holds rows_cap rows, part_ml [s][row] (max, sum) in the log2 domain,
+    // part_o [s][row][D].  Window: slot 2 c + 1 of CTA c for a pair that it begins, 2 c for one that it
+    // continues.  Prefix: pair number + CTA number, in regions of their own for the pairs of shared
+    // prefixes and for those of own slots (own_ml, own_o; G rows a slot).
+    int32_t rows_cap, ctas;
+    float2 *part_ml, *own_ml;
+    float *part_o, *own_o;
+};
+
+// Where the parts of pair (u, g) lie, CTA c's
+__device__ __forceinline__ int64_t rows_slot(const RowsArgs &a, const RowsHead &h, const RowsUnit &u, int unit, int g,
+                                             int c, bool begins) {
+    if (!a.prefix) return 2 * (int64_t)c + (begins ? 1 : 0);
+    return (int64_t)(u.m0 >= 0 ? unit : unit - h.n_pre) * a.pv.kv_heads + g + c;
+}
+
+// The tile of a unit
+__device__ __forceinline__ int rows_tile(const RowsUnit &u, int i) { return i < u.n_a ? u.t_a + i : u.t_w + i - u.n_a; }
+
+// The parts of a share, in turn
+struct RowsWalk {
+    int32_t unit, g, j, left;       // the next part begins at tile j of pair (unit, g)
+    __device__ __forceinline__ void begin(const RowsArgs &a, int cta) {
+        const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.start) + cta);
+        unit = s.x;
+        g = s.y;
+        j = s.z;
+        left = s.w;
+    }
+    // the part's tiles, given its unit
+    __device__ __forceinline__ int part(const RowsUnit &u) const { return min(u.nt - j, left); }
+    __device__ __forceinline__ void next(const RowsArgs &a, int n) {
+        left -= n;
+        j = 0;
+        if (++g == a.pv.kv_heads) {
+            g = 0;
+            ++unit;
+        }
+    }
+};
+__device__ __forceinline__ RowsUnit rows_unit(const RowsArgs &a, int unit) {
+    RowsUnit u;
+    const int4 *p = reinterpret_cast<const int4 *>(a.units + unit);
+    int4 *q = reinterpret_cast<int4 *>(&u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = __ldcg(p + i);
+    return u;
+}
+
+// What row r of a unit sees: slots s of [lo, hi] with s >= wlo or s < sh, live ones.  seq < 0: not a row.
+struct RowsRow {
+    int32_t seq;                    // its sequence
+    int32_t lo, hi, wlo, sh;
+    const int32_t *pos;             // its positions, by slot - S0, or null
+    int64_t q, out;                 // its elements in q and out
+};
+template <int D>
+__device__ __forceinline__ RowsRow rows_row(const RowsArgs &a, const RowsUnit &u, int g, int r) {
+    RowsRow w;
+    const int t = r / a.group, h = g * a.group + r % a.group;
+    w.lo = u.lo;
+    int64_t row;
+    if (!a.prefix) {
+        const int p = u.p0 + t;
+        w.seq = t < u.n ? u.b : -1;
+        w.hi = p;
+        w.wlo = max(u.lo, p - a.window + 1);
+        w.sh = u.S0 + a.sinks;
+        row = (int64_t)u.row0 + u.m0 + t;
+    } else {
+        w.seq = t >= u.n ? -1 : u.m0 >= 0 ? __ldcg(a.vm + u.m0 + t) : u.b;
+        w.hi = u.hi - 1;
+        w.wlo = w.sh = u.lo;
+        row = w.seq;
+    }
+    w.pos = a.pos && w.seq >= 0
+                ? a.pos + ((int64_t)w.seq * a.rows_per_seq + (a.rows_per_seq == 1 ? 0 : g)) * a.cap
+                : nullptr;
+    w.q = row * a.q_stride + (int64_t)h * D;
+    w.out = row * a.out_stride + (int64_t)h * D;
+    return w;
+}
+__device__ __forceinline__ bool rows_sees(const RowsRow &w, int S0, int s) {
+    return s >= w.lo && s <= w.hi && (s >= w.wlo || s < w.sh) && (!w.pos || __ldg(w.pos + (s - S0)) >= 0);
+}
+
+cudaError_t launch_rows_plan(const RowsArgs &a, cudaStream_t st);
+cudaError_t launch_rows_simt(const RowsArgs &a, int dtype, int head_dim, cudaStream_t st);
+cudaError_t launch_rows_merge(const RowsArgs &a, int dtype, int head_dim, cudaStream_t st);
+int rows_simt_ctas_per_sm(int head_dim);
+constexpr int kRowsSimt = 64;       // rows of a unit of the kernel without tensor cores
+
+// prefix: scores and utilities from K once more, with the log2-sum-exps known
+struct RowsScoreArgs {
+    float alpha;
+    float *score, *ema;             // [rows][cap] or null
+    int32_t max_len;
+};
+cudaError_t launch_rows_score(const RowsArgs &a, const RowsScoreArgs &s, int dtype, int head_dim, cudaStream_t st);
+
+}  // namespace ikv

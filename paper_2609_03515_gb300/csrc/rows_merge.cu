@@ -1,0 +1,235 @@
+// Merges the parts of packed-row attentions (rows.cuh): with (m_i, l_i, O_i) of each part of a row,
+//     M = max m_i, out = (sum 2^(m_i - M) O_i) / (sum 2^(m_i - M) l_i),
+// a warp a row.  Window: only the pairs that a share's border cuts have parts, and each border's CTA
+// finds its own.  Prefix: every row has parts, of its group's pair and of its own.
+#include "rows_redo.cuh"
+
+namespace ikv {
+namespace {
+
+constexpr int kMergeWarps = 4;
+
+// n parts: (max, sum) of part i at ml(i), output at o(i)
+template <int D, typename T, typename ML, typename O>
+__device__ __forceinline__ void merge_row(int n, ML ml, O o, float *wq, T *out, float *lse2) {
+    constexpr int E = D / 32, kAhead = 8;
+    const int lane = threadIdx.x & 31;
+    // (one part of each lane is in registers; more than 32 parts are read twice)
+    float2 x0 = make_float2(-INFINITY, 0.f);
+    if (lane < n) x0 = __ldcg(ml(lane));
+    float M = x0.x;
+    for (int i = lane + 32; i < n; i += 32) M = fmaxf(M, __ldcg(ml(i)).x);
+    M = warp_max(M);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float W = 0.f;
+    for (int i = lane; i < n; i += 32) {
+        const float2 x = i == lane ? x0 : __ldcg(ml(i));
+        const float f = exp2f(x.x - ref);
+        W += x.y * f;
+        wq[i] = f;
+    }
+    W = warp_sum(W);
+    __syncwarp();
+    float acc[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
+        float v[kAhead][E];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (i0 + i < n) {
+                const float *p = o(i0 + i) + lane * E;
+                if (E == 4) {
+                    const float4 y = __ldcg(reinterpret_cast<const float4 *>(p));
+                    v[i][0] = y.x;
+                    v[i][1] = y.y;
+                    v[i][E - 2] = y.z;
+                    v[i][E - 1] = y.w;
+                } else {
+                    const float2 y = __ldcg(reinterpret_cast<const float2 *>(p));
+                    v[i][0] = y.x;
+                    v[i][1] = y.y;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (i0 + i < n) {
+                const float f = wq[i0 + i];
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] += f * v[i][e];
+            }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) store_as(out + lane * E + e, over_sum(acc[e], W));
+    // (a NaN sum leaves a NaN, for the scores to be NaN too)
+    if (lse2 && lane == 0) *lse2 = W == 0.f ? -INFINITY : M + log2f(W);
+    __syncwarp();
+}
+
+// Grid: (CTAs of the attention, row blocks).  CTA c: the pair that the border in front of share c cuts,
+// if no earlier border cuts it.
+template <int D, typename T>
+__global__ void __launch_bounds__(kMergeWarps * 32) rows_merge_window_kernel(const RowsArgs a) {
+    pdl_wait();
+    __shared__ float wq[kMergeWarps][kRowsMaxCtas];
+    const int c = blockIdx.x, warp = threadIdx.x >> 5;
+    RowsWalk w;
+    w.begin(a, c);
+    if (w.left == 0 || w.j == 0) return;
+    const int64_t per = __ldcg(&a.head->per);
+    if (w.j > per) return;
+    const RowsUnit u = rows_unit(a, w.unit);
+    const int n = 1 + (int)((u.nt - w.j + per - 1) / per);  // parts: share c - 1's and those behind
+    const int rows = u.n * a.group;
+    for (int r = blockIdx.y * kMergeWarps + warp; r < rows; r += gridDim.y * kMergeWarps) {
+        const RowsRow row = rows_row<D>(a, u, w.g, r);
+        auto slot = [&](int i) { return i == 0 ? 2 * (int64_t)(c - 1) + 1 : 2 * (int64_t)(c + i - 1); };
+        merge_row<D, T>(
+            n, [&](int i) { return a.part_ml + slot(i) * a.rows_cap + r; },
+            [&](int i) { return a.part_o + (slot(i) * a.rows_cap + r) * D; }, wq[warp],
+            static_cast<T *>(a.out) + row.out, nullptr);
+    }
+}
+
+// A warp a (sequence, query head)
+template <int D, typename T>
+__global__ void __launch_bounds__(kMergeWarps * 32) rows_merge_prefix_kernel(const RowsArgs a) {
+    pdl_wait();
+    __shared__ float wq[kMergeWarps][2 * kRowsMaxCtas];
+    const int warp = threadIdx.x >> 5, hk = a.pv.kv_heads;
+    const int64_t at = (int64_t)blockIdx.x * kMergeWarps + warp;
+    if (at >= (int64_t)a.batch * a.q_heads) return;
+    const int b = (int)(at / a.q_heads), h = (int)(at % a.q_heads), g = h / a.group, x = h % a.group;
+    const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.seq) + b);
+    const int64_t per = __ldcg(&a.head->per);
+    const int n_pre = __ldcg(&a.head->n_pre);
+    int64_t slot_p = 0, slot_o = 0;
+    int np = 0, no = 0;
+    auto parts = [&](int unit, int64_t pair0, int64_t &slot) {  // of pair (unit, g); slot: its first part's
+        const int nt = __ldcg(&a.units[unit].nt);
+        const int64_t x0 = __ldcg(&a.units[unit].cum) + (int64_t)g * nt;
+        const int64_t c0 = x0 / per;
+        slot = pair0 + g + c0;
+        return (int)((x0 + nt - 1) / per - c0) + 1;
+    };
+    if (s.x >= 0) np = parts(s.x, (int64_t)s.x * hk, slot_p);
+    if (s.z >= 0) no = parts(s.z, (int64_t)(s.z - n_pre) * hk, slot_o);
+    const int rp = s.y * a.group + x;
+    merge_row<D, T>(
+        np + no,
+        [&](int i) {
+            return i < np ? a.part_ml + (slot_p + i) * a.rows_cap + rp : a.own_ml + (slot_o + i - np) * a.group + x;
+        },
+        [&](int i) {
+            return i < np ? a.part_o + ((slot_p + i) * a.rows_cap + rp) * D
+                          : a.own_o + ((slot_o + i - np) * a.group + x) * D;
+        },
+        wq[warp], static_cast<T *>(a.out) + at * D, a.lse2 + at);
+}
+
+template <int D, typename T>
+cudaError_t launch_merge(const RowsArgs &a, cudaStream_t st) {
+    if (a.prefix) {
+        const int64_t rows = (int64_t)a.batch * a.q_heads;
+        return launch_k(rows_merge_prefix_kernel<D, T>, dim3((unsigned)((rows + kMergeWarps - 1) / kMergeWarps)),
+                        dim3(kMergeWarps * 32), 0, st, a);
+    }
+    const int y = (a.rows_cap + 4 * kMergeWarps - 1) / (4 * kMergeWarps);  // four rows a warp
+    return launch_k(rows_merge_window_kernel<D, T>, dim3(a.ctas, y), dim3(kMergeWarps * 32), 0, st, a);
+}
+
+// Scores without tensor cores: K once more, with each row's log2-sum-exp,
+//     score = mean over the row's heads of 2^(q . k scale - lse2).
+// A CTA: 32 slots of a sequence, a lane a slot, the query heads of each KV head spread over its warps.
+constexpr int kScoreWarps = 8;
+template <int D, typename T>
+__global__ void __launch_bounds__(kScoreWarps * 32) rows_score_kernel(const RowsArgs a, const RowsScoreArgs sc) {
+    pdl_wait();
+    __shared__ float sK[32][D + 1], sQ[8][D], part[kScoreWarps][33];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rps = a.rows_per_seq, G = a.group, hk = a.pv.kv_heads;
+    for (int b = blockIdx.y; b < a.batch; b += gridDim.y) {
+        const int S0 = a.pv.start ? min(max(__ldg(a.pv.start + b), 0), a.cap) : 0;
+        const int L = min(max(__ldg(a.len + b), 0), a.cap - S0);
+        const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.seq) + b);
+        int lead = b, lead_s0 = S0;
+        if (s.x >= 0) {
+            lead = __ldcg(&a.units[s.x].b);
+            lead_s0 = __ldcg(&a.units[s.x].S0);
+        }
+        for (int j0 = blockIdx.x * 32; j0 < L; j0 += gridDim.x * 32) {
+            float sum = 0.f;
+            for (int g = 0; g < hk; ++g) {
+                __syncthreads();
+                for (int i = tid; i < 32 * D; i += kScoreWarps * 32) {
+                    const int r = i / D, c = i % D, j = j0 + r;
+                    float x = 0.f;
+                    if (j < L) {
+                        const bool shared = j < s.w;
+                        x = load_as_float(static_cast<const T *>(a.k) +
+                                          a.pv.row_phys(shared ? lead : b, a.layer, g, (shared ? lead_s0 : S0) + j) * D + c);
+                    }
+                    sK[r][c] = x;
+                }
+                for (int i = tid; i < G * D; i += kScoreWarps * 32)
+                    sQ[i / D][i % D] = load_as_float(static_cast<const T *>(a.q) + ((int64_t)b * a.q_heads + g * G) * D + i);
+                __syncthreads();
+                if (warp < G) {
+                    float z = 0.f;
+    #pragma unroll 8
+                    for (int c = 0; c < D; ++c) z += sQ[warp][c] * sK[lane][c];
+                    const float lse = __ldcg(a.lse2 + (int64_t)b * a.q_heads + g * G + warp);
+                    if (lse != -INFINITY) sum += exp2f(z * a.scale_log2 - lse);
+                }
+                if (rps > 1 || g == hk - 1) {
+                    part[warp][lane] = sum;
+                    sum = 0.f;
+                    __syncthreads();
+                    const int j = j0 + lane;
+                    if (warp == 0 && j < L) {
+                        float t = 0.f;
+    #pragma unroll
+                        for (int w = 0; w < kScoreWarps; ++w) t += part[w][lane];
+                        const int64_t at = ((int64_t)b * rps + (rps > 1 ? g : 0)) * a.cap + j;
+                        const bool live = !a.pos || __ldg(a.pos + at) >= 0;
+                        t = live ? t / (float)(rps > 1 ? G : a.q_heads) : 0.f;
+                        if (sc.score) sc.score[at] = t;
+                        if (sc.ema) sc.ema[at] = sc.alpha * sc.ema[at] + (1.f - sc.alpha) * t;
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <int D, typename T>
+cudaError_t launch_score(const RowsArgs &a, const RowsScoreArgs &s, cudaStream_t st) {
+    const int blocks = s.max_len > 32 ? (s.max_len + 31) / 32 : 1;
+    return launch_k(rows_score_kernel<D, T>, dim3(blocks, a.batch < 65535 ? a.batch : 65535), dim3(kScoreWarps * 32), 0,
+                    st, a, s);
+}
+
+}  // namespace
+
+cudaError_t launch_rows_merge(const RowsArgs &a, int dtype, int head_dim, cudaStream_t st) {
+    cudaError_t e;
+    if (dtype == IKV_BF16)
+        e = head_dim == 64 ? launch_merge<64, __nv_bfloat16>(a, st) : launch_merge<128, __nv_bfloat16>(a, st);
+    else
+        e = head_dim == 64 ? launch_merge<64, float>(a, st) : launch_merge<128, float>(a, st);
+    note_launch();
+    return e;
+}
+
+cudaError_t launch_rows_score(const RowsArgs &a, const RowsScoreArgs &s, int dtype, int head_dim, cudaStream_t st) {
+    cudaError_t e;
+    if (dtype == IKV_BF16)
+        e = head_dim == 64 ? launch_score<64, __nv_bfloat16>(a, s, st) : launch_score<128, __nv_bfloat16>(a, s, st);
+    else
+        e = head_dim == 64 ? launch_score<64, float>(a, s, st) : launch_score<128, float>(a, s, st);
+    note_launch();
+    return e;
+}
+
+}  // namespace ikv

@@ -74,6 +74,15 @@ class ikv_pages(ctypes.Structure):
     _fields_ = [("refs", P), ("n_planes", I32), ("plane", P * IKV_MAX_PLANES), ("row_bytes", I32 * IKV_MAX_PLANES)]
 
 
+class ikv_prefix(ctypes.Structure):
+    _fields_ = [("n_groups", I32), ("first", P), ("member", P), ("len", P)]
+
+
+class ikv_window(ctypes.Structure):
+    _fields_ = [("window", I32), ("sinks", I32), ("row0", P), ("count", P), ("max_count", I32),
+                ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
+
+
 class IKVError(RuntimeError):
     def __init__(self, status: int, where: str, msg: str):
         super().__init__(f"{where} failed with status {status}: {msg}")
@@ -86,6 +95,7 @@ def _load():
     lib = ctypes.CDLL(LIB_PATH)
     SP, CP, PP = ctypes.POINTER(ikv_shape), ctypes.POINTER(ikv_cache), ctypes.POINTER(ikv_params)
     QP, RP, GP = ctypes.POINTER(ikv_q4), ctypes.POINTER(ikv_rows), ctypes.POINTER(ikv_pages)
+    XP, WP = ctypes.POINTER(ikv_prefix), ctypes.POINTER(ikv_window)
     sigs = {
         "ikv_last_error": ([], ctypes.c_char_p),
         "ikv_launch_count": ([], ctypes.c_int64),
@@ -118,6 +128,10 @@ def _load():
         "ikv_pages_fork": ([SP, CP, GP, I32, P, P, P, P], I32),
         "ikv_pages_writable": ([SP, CP, GP, P, P, I32, P, P, SZ, P], I32),
         "ikv_pages_compact": ([SP, CP, GP, P, P, P, P, P, SZ, P], I32),
+        "ikv_prefix_workspace_size": ([SP, CP, XP, ctypes.POINTER(SZ)], I32),
+        "ikv_prefix_attend_score": ([SP, CP, XP, I32, P, P, P, P, F32, P, SZ, P], I32),
+        "ikv_window_workspace_size": ([SP, CP, WP, ctypes.POINTER(SZ)], I32),
+        "ikv_window_attend": ([SP, CP, WP, I32, P, P, P, SZ, P], I32),
     }
     for name, (args, res) in sigs.items():
         f = getattr(lib, name)
@@ -323,6 +337,28 @@ def ikv_pages_writable(shape, cache, pages, first, count, max_count, lacking, ws
 def ikv_pages_compact(shape, cache, pages, keep, keep_len, ema, lacking, ws, ws_bytes, stream=None) -> None:
     _check(_lib.ikv_pages_compact(shape, cache, pages, _p(keep), _p(keep_len), _p(ema), _p(lacking), _p(ws), ws_bytes,
                                   _stream(stream)), "ikv_pages_compact")
+
+
+def ikv_prefix_workspace_size(shape, cache, prefix) -> int:
+    n = SZ(0)
+    _check(_lib.ikv_prefix_workspace_size(shape, cache, prefix, ctypes.byref(n)), "ikv_prefix_workspace_size")
+    return n.value
+
+
+def ikv_prefix_attend_score(shape, cache, prefix, layer, q, out, score, ema, alpha, ws, ws_bytes, stream=None) -> None:
+    _check(_lib.ikv_prefix_attend_score(shape, cache, prefix, layer, _p(q), _p(out), _p(score), _p(ema), alpha, _p(ws),
+                                        ws_bytes, _stream(stream)), "ikv_prefix_attend_score")
+
+
+def ikv_window_workspace_size(shape, cache, window) -> int:
+    n = SZ(0)
+    _check(_lib.ikv_window_workspace_size(shape, cache, window, ctypes.byref(n)), "ikv_window_workspace_size")
+    return n.value
+
+
+def ikv_window_attend(shape, cache, window, layer, q, out, ws, ws_bytes, stream=None) -> None:
+    _check(_lib.ikv_window_attend(shape, cache, window, layer, _p(q), _p(out), _p(ws), ws_bytes, _stream(stream)),
+           "ikv_window_attend")
 
 
 def raw_status(fn_name: str, *args) -> int:
