@@ -62,10 +62,11 @@ RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, 
     a.group = s->q_heads / s->kv_heads;
     a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)s->head_dim));
     a.q_stride = a.out_stride = (int64_t)s->q_heads * s->head_dim;
-    a.ctas = sm_count() * rows_simt_ctas_per_sm(s->head_dim);
+    const bool tc = rows_tc_supported(s, c);
+    a.ctas = sm_count() * (tc ? 1 : rows_simt_ctas_per_sm(s->head_dim));
     if (a.ctas > kRowsMaxCtas) a.ctas = kRowsMaxCtas;
-    const int most = kRowsSimt / a.group;
     const int n = p ? s->batch : w->max_count;
+    const int most = tc ? 2 * (128 / a.group) : kRowsSimt / a.group;  // (tensor cores: two row tiles)
     a.unit_n = most;
     a.rows_cap = (n < most ? n : most) * a.group;
     int64_t units;
@@ -73,7 +74,7 @@ RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, 
         if (w->q_stride) a.q_stride = w->q_stride;
         if (w->out_stride) a.out_stride = w->out_stride;
         a.window = w->window > 0 && w->window < 1 << 30 ? w->window : 1 << 30;
-        a.sinks = w->sinks < 1 << 30 ? w->sinks : 1 << 30;
+        a.sinks = w->sinks < 1 << 30 ? w->sinks : (1 << 30) - 1;
         a.row0 = w->row0;
         a.count = w->count;
         a.max_count = w->max_count;
@@ -107,7 +108,7 @@ RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, 
         take(a.group_lead, p->n_groups);
         take(a.group_unit, p->n_groups);
         take(a.seq, nb);
-        take(a.lse2, nb * s->q_heads);
+        take(a.norm, nb * s->q_heads);
         take(a.own_ml, own);
         take(a.own_o, own * s->head_dim);
     }
@@ -125,9 +126,10 @@ ikv_status check_call(const ikv_shape *s, int32_t layer, const void *q, const vo
     return IKV_OK;
 }
 
-ikv_status attend(const RowsArgs &a, const ikv_shape *s, cudaStream_t st) {
+ikv_status attend(const RowsArgs &a, const ikv_shape *s, const ikv_cache *c, cudaStream_t st) {
     IKV_TRY_CUDA(launch_rows_plan(a, st), "row plan launch");
-    IKV_TRY_CUDA(launch_rows_simt(a, s->dtype, s->head_dim, st), "row attention launch");
+    IKV_TRY_CUDA(rows_tc_supported(s, c) ? launch_rows_tc(a, s->head_dim, st) : launch_rows_simt(a, s->dtype, s->head_dim, st),
+                 "row attention launch");
     IKV_TRY_CUDA(launch_rows_merge(a, s->dtype, s->head_dim, st), "row merge launch");
     return IKV_OK;
 }
@@ -158,7 +160,7 @@ ikv_status ikv_prefix_attend_score(const ikv_shape *shape, const ikv_cache *cach
     a.q = q;
     a.out = out;
     PdlScope pdl;
-    if ((e = attend(a, shape, stream))) return e;
+    if ((e = attend(a, shape, cache, stream))) return e;
     if (!score && !ema) return IKV_OK;
     const RowsScoreArgs sc{alpha, score, ema, cache->max_len};
     IKV_TRY_CUDA(launch_rows_score(a, sc, shape->dtype, shape->head_dim, stream), "row score launch");
@@ -186,7 +188,7 @@ ikv_status ikv_window_attend(const ikv_shape *shape, const ikv_cache *cache, con
     a.q = q;
     a.out = out;
     PdlScope pdl;
-    return attend(a, shape, stream);
+    return attend(a, shape, cache, stream);
 }
 
 }  // extern "C"

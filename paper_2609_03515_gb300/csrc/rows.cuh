@@ -59,7 +59,7 @@ struct RowsArgs {
     int64_t q_stride, out_stride;   // elements from a token's (sequence's) heads to the next
     int32_t unit_n;                 // most tokens or members of a unit
     // window
-    int32_t window, sinks;          // window in [1, 2^30], sinks in [0, 2^30]
+    int32_t window, sinks;          // window in [1, 2^30], sinks in [0, 2^30)
     const int32_t *row0, *count;
     int32_t max_count, seq_units;   // seq_units: units of max_count tokens
     // prefix
@@ -75,7 +75,9 @@ struct RowsArgs {
     int32_t *entry_group;           // prefix: [batch] the entries' groups
     int32_t *group_p, *group_lead, *group_unit;  // prefix: [n_groups] slots shared, first member, first unit
     RowsSeq *seq;                   // prefix: [batch]
-    float *lse2;                    // prefix: [batch][H] log2-sum-exp
+    float2 *norm;                   // prefix: [batch][H] the maximum M that a row's weights go by (log2 domain)
+                                    // and 1 over their sum.  (Not their log-sum-exp: at logits of 100 its
+                                    // rounding alone costs a weight 3e-6 of its value)
     // partial results: slot s holds rows_cap rows, part_ml [s][row] (max, sum) in the log2 domain,
     // part_o [s][row][D].  Window: slot 2 c + 1 of CTA c for a pair that it begins, 2 c for one that it
     // continues.  Prefix: pair number + CTA number, in regions of their own for the pairs of shared
@@ -164,11 +166,14 @@ __device__ __forceinline__ bool rows_sees(const RowsRow &w, int S0, int s) {
 
 cudaError_t launch_rows_plan(const RowsArgs &a, cudaStream_t st);
 cudaError_t launch_rows_simt(const RowsArgs &a, int dtype, int head_dim, cudaStream_t st);
+bool rows_tc_supported(const ikv_shape *s, const ikv_cache *c);
+cudaError_t launch_rows_tc(const RowsArgs &a, int head_dim, cudaStream_t st);
+cudaError_t read_clear_rows_tc_error(unsigned int *v);
 cudaError_t launch_rows_merge(const RowsArgs &a, int dtype, int head_dim, cudaStream_t st);
 int rows_simt_ctas_per_sm(int head_dim);
 constexpr int kRowsSimt = 64;       // rows of a unit of the kernel without tensor cores
 
-// prefix: scores and utilities from K once more, with the log2-sum-exps known
+// prefix: scores and utilities from K once more, with the rows' maxima and sums known
 struct RowsScoreArgs {
     float alpha;
     float *score, *ema;             // [rows][cap] or null

@@ -11,7 +11,7 @@ constexpr int kMergeWarps = 4;
 
 // n parts: (max, sum) of part i at ml(i), output at o(i)
 template <int D, typename T, typename ML, typename O>
-__device__ __forceinline__ void merge_row(int n, ML ml, O o, float *wq, T *out, float *lse2) {
+__device__ __forceinline__ void merge_row(int n, ML ml, O o, float *wq, T *out, float2 *norm) {
     constexpr int E = D / 32, kAhead = 8;
     const int lane = threadIdx.x & 31;
     // (one part of each lane is in registers; more than 32 parts are read twice)
@@ -63,7 +63,7 @@ __device__ __forceinline__ void merge_row(int n, ML ml, O o, float *wq, T *out, 
 #pragma unroll
     for (int e = 0; e < E; ++e) store_as(out + lane * E + e, over_sum(acc[e], W));
     // (a NaN sum leaves a NaN, for the scores to be NaN too)
-    if (lse2 && lane == 0) *lse2 = W == 0.f ? -INFINITY : M + log2f(W);
+    if (norm && lane == 0) *norm = make_float2(ref, W == 0.f ? 0.f : 1.f / W);
     __syncwarp();
 }
 
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) rows_merge_prefix_kernel(con
             return i < np ? a.part_o + ((slot_p + i) * a.rows_cap + rp) * D
                           : a.own_o + ((slot_o + i - np) * a.group + x) * D;
         },
-        wq[warp], static_cast<T *>(a.out) + at * D, a.lse2 + at);
+        wq[warp], static_cast<T *>(a.out) + at * D, a.norm + at);
 }
 
 template <int D, typename T>
@@ -139,8 +139,8 @@ cudaError_t launch_merge(const RowsArgs &a, cudaStream_t st) {
     return launch_k(rows_merge_window_kernel<D, T>, dim3(a.ctas, y), dim3(kMergeWarps * 32), 0, st, a);
 }
 
-// Scores without tensor cores: K once more, with each row's log2-sum-exp,
-//     score = mean over the row's heads of 2^(q . k scale - lse2).
+// Scores without tensor cores: K once more, with each row's maximum M and sum of weights W,
+//     score = mean over the row's heads of 2^(q . k scale - M) / W.
 // A CTA: 32 slots of a sequence, a lane a slot, the query heads of each KV head spread over its warps.
 constexpr int kScoreWarps = 8;
 template <int D, typename T>
@@ -179,8 +179,8 @@ __global__ void __launch_bounds__(kScoreWarps * 32) rows_score_kernel(const Rows
                     float z = 0.f;
     #pragma unroll 8
                     for (int c = 0; c < D; ++c) z += sQ[warp][c] * sK[lane][c];
-                    const float lse = __ldcg(a.lse2 + (int64_t)b * a.q_heads + g * G + warp);
-                    if (lse != -INFINITY) sum += exp2f(z * a.scale_log2 - lse);
+                    const float2 mw = __ldcg(a.norm + (int64_t)b * a.q_heads + g * G + warp);
+                    if (mw.y != 0.f) sum += exp2f(__fmaf_rn(z, a.scale_log2, -mw.x)) * mw.y;
                 }
                 if (rps > 1 || g == hk - 1) {
                     part[warp][lane] = sum;

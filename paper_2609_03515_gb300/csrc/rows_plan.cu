@@ -298,6 +298,9 @@ cudaError_t read_clear_rows_error(unsigned int *v) {
     unsigned int z = 0;
     cudaError_t e = cudaMemcpyFromSymbol(v, g_rows_error, sizeof(*v));
     if (e == cudaSuccess && *v) e = cudaMemcpyToSymbol(g_rows_error, &z, sizeof(z));
+    unsigned int tc = 0;
+    if (e == cudaSuccess) e = read_clear_rows_tc_error(&tc);
+    *v |= tc;
     return e;
 }
 

@@ -66,9 +66,9 @@ __device__ __noinline__ void rows_redo(const RowsArgs &a, const RowsUnit &u, int
             float z = 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) z += q[e] * load_as_float(static_cast<const T *>(a.k) + at + 32 * e);
-            z = warp_sum(z) * a.scale_log2;
-            const float mx = fmaxf(m, z), ref = mx == -INFINITY ? 0.f : mx;
-            const float f = exp2f(m - ref), p = exp2f(z - ref);
+            z = warp_sum(z);
+            const float mx = fmaxf(m, __fmul_rn(z, a.scale_log2)), ref = mx == -INFINITY ? 0.f : mx;
+            const float f = exp2f(m - ref), p = exp2f(__fmaf_rn(z, a.scale_log2, -ref));
             l = l * f + p;
             m = mx;
 #pragma unroll

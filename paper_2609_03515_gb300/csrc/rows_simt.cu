@@ -121,8 +121,8 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const bool see = row[i].seq >= 0 && rows_sees(row[i], u.S0, s0 + tx + 16 * j);
-                s[i][j] = see ? s[i][j] * a.scale_log2 : -INFINITY;
-                mx = fmaxf(mx, s[i][j]);
+                if (!see) s[i][j] = -INFINITY;
+                mx = fmaxf(mx, __fmul_rn(s[i][j], a.scale_log2));
             }
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -131,7 +131,8 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float p = exp2f(s[i][j] - ref);
+                // (the product unrounded: what the maximum is off by is common to all of the row's weights)
+                const float p = exp2f(__fmaf_rn(s[i][j], a.scale_log2, -ref));
                 sum += p;
                 sP[(ty * RPT + i) * (kStep + 4) + tx + 16 * j] = p;
             }

@@ -1,0 +1,555 @@
+// Packed-row attention on the tensor cores: bf16, pages of a multiple of 8 slots (sm_103a).
+//
+// S = Q K^T and O += P V with the rows in the M dimension of 128 x 128 tcgen05 products, so that one tile
+// of K and V serves up to 256 query rows: two row tiles, A and B, each with its scores and its output in
+// tensor memory (S 128 columns, O D columns) and a warpgroup of its own whose thread r holds row r.  A
+// thread turns its row of S into weights, 2^(S scale - m), and writes them as bf16 over S, from where the
+// second product takes them as its A operand; nothing of S or P passes through shared memory.  While one
+// warpgroup computes its weights, the tensor cores work for the other.
+//
+// A unit of at most 128 rows (decode) gives A and B every other tile of its slots instead; their outputs
+// are joined at the end.
+//
+// The running maximum m only moves when a row's weights would grow past 2^8, so that O is seldom
+// rescaled: weights and sum are relative to the same m, which cancels in O / l.  The sum takes the weights
+// in 32 bits; rounding them to bf16 for the product costs at most 2^-8 of sum p |V|.
+//
+// Warps: 0-3 and 4-7 the two row tiles, 8 TMA, 9 MMA, 10-11 load Q.  K and V tiles pass through a ring of
+// 32 KB (D = 64: 16 KB) stages in the order K0 K1 V0 K2 V1 .., which is the order of the products.  Boxes of
+// a tile that no row sees are fetched from behind the tensor's end, which fills zeros and reads nothing.
+// Every wait is bounded; on timeout the CTA sets the error word, drains what is in flight and returns.
+#include <cudaTypedefs.h>
+
+#include "rows_redo.cuh"
+#include "tc.cuh"
+
+namespace ikv {
+
+__device__ unsigned int g_rows_tc_error = 0;
+
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kAtom = 128 * 128;            // bytes of 64 channels of a 128-row tile (128-byte swizzle)
+constexpr uint64_t kLimitNs = 1000000000ull;
+constexpr float kSlack = 8.f;               // log2 of the largest weight before the maximum moves
+
+template <int D>
+struct Tc {
+    static constexpr int kStage = kAtom * (D / 64);
+    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr int kOffRing = 2 * kStage;  // (Q of A and B in front)
+    static constexpr int kOffEx = kOffRing + kStages * kStage;
+    static constexpr int kOffBar = kOffEx + 128 * 8;
+    static constexpr int kBars = 2 * kStages + 9;
+    static constexpr int kOffMisc = kOffBar + kBars * 8;
+    static constexpr int kSmem = kOffMisc + 16 + 1024;  // (to align by 1024)
+};
+
+struct TcMap {
+    int32_t rows_per_box, pool_rows;        // pool_rows: rows of the layer, a row behind the end
+};
+
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
+    if (mbar_test(bar, parity)) return true;
+    const uint64_t start = global_ns();
+    for (;;) {
+        if (mbar_try(bar, parity, 2000)) return true;
+        if (*abort) return false;
+        if (global_ns() - start > kLimitNs) break;
+    }
+    *abort = 1;
+    atomicOr(&g_rows_tc_error, 1u);
+    return false;
+}
+// of one's own copies or products, whatever the abort flag says
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
+    if (mbar_test(bar, parity)) return;
+    const uint64_t start = global_ns();
+    while (!mbar_try(bar, parity, 2000))
+        if (global_ns() - start > kLimitNs) {
+            atomicOr(&g_rows_tc_error, 1u);
+            return;
+        }
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+            dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+// bits of the slots a .. b of a tile that lie in its w-th 32
+__device__ __forceinline__ uint32_t range_bits(int a, int b, int w) {
+    const int lo = max(a - 32 * w, 0), hi = min(b - 32 * w, 31);
+    return lo > hi ? 0u : (0xffffffffu >> (31 - (hi - lo))) << lo;
+}
+// tiles of a share's load stream: load x of a part of n tiles
+__device__ __forceinline__ void load_of(int x, int n, int &tile, bool &is_v) {
+    is_v = x == 2 * n - 1 || (x > 0 && !(x & 1));
+    tile = x == 2 * n - 1 ? n - 1 : is_v ? (x - 2) / 2 : (x + 1) / 2;
+}
+__device__ __forceinline__ int load_k(int j) { return j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ int load_v(int j, int n) { return j < n - 1 ? 2 * j + 2 : 2 * n - 1; }
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    rows_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                   const __grid_constant__ RowsArgs a, const TcMap tm) {
+    using C = Tc<D>;
+    using T = __nv_bfloat16;
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    unsigned char *sm = smem_raw + (base - raw);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t bar0 = base + C::kOffBar;
+    auto kv_full = [&](int i) { return bar0 + 8u * i; };
+    auto kv_empty = [&](int i) { return bar0 + 8u * (C::kStages + i); };
+    const uint32_t q_full = bar0 + 8u * (2 * C::kStages), q_empty = q_full + 8;
+    auto s_full = [&](int x) { return q_full + 16u + 8u * x; };
+    auto p_full = [&](int x) { return q_full + 32u + 8u * x; };
+    auto o_full = [&](int x) { return q_full + 48u + 8u * x; };
+    const uint32_t mma_done = q_full + 64u;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + C::kOffMisc);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + C::kOffMisc + 4);
+    if (warp == 8 && lane == 0) {
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(kv_full(i), 1);
+            mbar_init(kv_empty(i), 1);
+        }
+        mbar_init(q_full, 64);
+        mbar_init(q_empty, 1);
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(s_full(x), 1);
+            mbar_init(p_full(x), 4);
+            mbar_init(o_full(x), 1);
+        }
+        mbar_init(mma_done, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot))
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_wait();
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    const int tile_rows = 128 / a.group * a.group;  // rows of a row tile
+    RowsWalk w;
+    w.begin(a, blockIdx.x);
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (warp == 8) {
+            // ---------------- K and V, a lane a box
+            int J = 0;
+            bool ok = true;
+            const int boxes = kRowsTile / tm.rows_per_box;
+            while (w.left > 0 && ok) {
+                const RowsUnit u = rows_unit(a, w.unit);
+                const int n = w.part(u);
+                for (int x = 0; x < 2 * n && ok; ++x, ++J) {
+                    int tile;
+                    bool is_v;
+                    load_of(x, n, tile, is_v);
+                    const int s0 = rows_tile(u, w.j + tile) * kRowsTile + lane * tm.rows_per_box, s1 = s0 + tm.rows_per_box;
+                    int row = tm.pool_rows;
+                    if (lane < boxes && s0 < u.hi && (s1 > u.wlo || (s0 < u.sh && s1 > u.lo))) {
+                        const int lp = a.pv.page_shift >= 0 ? s0 >> a.pv.page_shift : s0 / a.pv.page_size;
+                        const int page = __ldg(a.pv.block_table + (int64_t)u.b * a.pv.max_pages + lp);
+                        row = (page * a.pv.kv_heads + w.g) * a.pv.page_size + (s0 - lp * a.pv.page_size);
+                    }
+                    const int st = J % C::kStages;
+                    if (lane == 0) {
+                        if (J >= C::kStages) ok = bar_wait(kv_empty(st), (J / C::kStages - 1) & 1, abort_flag);
+                        if (ok) mbar_expect_tx(kv_full(st), C::kStage);
+                    }
+                    ok = __shfl_sync(0xffffffffu, ok, 0);
+                    if (ok && lane < boxes) {
+                        const uint32_t dst = base + C::kOffRing + st * C::kStage + lane * tm.rows_per_box * 128;
+#pragma unroll
+                        for (int c = 0; c < D / 64; ++c)
+                            tma_tile(dst + c * kAtom, is_v ? &tmV : &tmK, 64 * c, row, kv_full(st));
+                    }
+                    if (!ok) break;
+                }
+                w.next(a, n);
+            }
+            if (lane == 0)  // every copy has landed before the CTA ends
+                for (int i = J - 1; i >= 0 && i >= J - C::kStages; --i) bar_drain(kv_full(i % C::kStages), (i / C::kStages) & 1);
+            __syncwarp();
+        } else if (warp == 9) {
+            // ---------------- products
+            if (lane == 0) {
+                constexpr uint32_t id_qk = idesc_bf16(false, 128, 128), id_pv = idesc_bf16(false, 128, D, true);
+                int J = 0, seg = 0;
+                uint32_t np[2] = {0, 0};  // weights taken
+                bool ok = true;
+                while (w.left > 0 && ok) {
+                    const RowsUnit u = rows_unit(a, w.unit);
+                    const int n = w.part(u);
+                    const bool pair = u.n * a.group > tile_rows;
+                    auto qk = [&](int x, int j) {
+                        const int i = J + load_k(j), st = i % C::kStages;
+                        if (!bar_wait(kv_full(st), (i / C::kStages) & 1, abort_flag)) return false;
+                        fence_after_sync();
+                        const uint32_t q = base + (pair ? x * C::kStage : 0), k = base + C::kOffRing + st * C::kStage;
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) {
+                            const uint32_t off = (kk >> 2) * kAtom + (kk & 3) * 32;
+                            mma_bf16(tmem + 128 * x, sdesc(q + off, 16, 1024), sdesc(k + off, 16, 1024), id_qk, kk > 0);
+                        }
+                        if (!pair || x == 1) mma_commit(kv_empty(st));
+                        mma_commit(s_full(x));
+                        return true;
+                    };
+                    auto pv = [&](int x, int j, bool first) {
+                        const int i = J + load_v(j, n), st = i % C::kStages;
+                        if (!bar_wait(p_full(x), np[x] & 1, abort_flag)) return false;
+                        ++np[x];
+                        if (!bar_wait(kv_full(st), (i / C::kStages) & 1, abort_flag)) return false;
+                        fence_after_sync();
+                        const uint32_t v = base + C::kOffRing + st * C::kStage;
+#pragma unroll
+                        for (int kk = 0; kk < kRowsTile / 16; ++kk)  // V: channels contiguous, 8-slot groups 1 KB apart
+                            mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * kk, sdesc(v + kk * 2048, kAtom, 1024), id_pv,
+                                        !first || kk > 0);
+                        if (!pair || x == 1) mma_commit(kv_empty(st));
+                        mma_commit(o_full(x));
+                        return true;
+                    };
+                    ok = bar_wait(q_full, seg & 1, abort_flag);
+                    fence_after_sync();
+                    // P of a tile lies over its S: S of the next is issued behind the product that takes P
+                    if (pair) {
+                        ok = ok && qk(0, 0) && qk(1, 0);
+                        if (ok && n == 1) mma_commit(q_empty);
+                        for (int j = 0; j < n && ok; ++j) {
+                            ok = pv(0, j, j == 0) && (j + 1 == n || qk(0, j + 1)) && pv(1, j, j == 0) &&
+                                 (j + 1 == n || qk(1, j + 1));
+                            if (ok && j + 2 == n) mma_commit(q_empty);
+                        }
+                    } else {
+                        ok = ok && qk(0, 0) && (n == 1 || qk(1, 1));
+                        if (ok && n <= 2) mma_commit(q_empty);
+                        for (int j = 0; j < n && ok; ++j) {
+                            ok = pv(j & 1, j, j < 2) && (j + 2 >= n || qk(j & 1, j + 2));
+                            if (ok && j + 3 == n) mma_commit(q_empty);
+                        }
+                    }
+                    J += 2 * n;
+                    ++seg;
+                    w.next(a, n);
+                }
+                mma_commit(mma_done);  // also after an abort: no product may write TMEM when it is freed
+                bar_drain(mma_done, 0);
+            }
+            __syncwarp();
+        } else {
+            // ---------------- Q
+            const int t = tid - 320;
+            constexpr int CH = D / 8, RI = 64 / CH;  // 16-byte pieces of a row, rows an iteration
+            const int c = t % CH * 8;
+            int seg = 0;
+            bool ok = true;
+            while (w.left > 0 && ok) {
+                const RowsUnit u = rows_unit(a, w.unit);
+                const int n = w.part(u), rows = u.n * a.group;
+                if (seg > 0) ok = bar_wait(q_empty, (seg - 1) & 1, abort_flag);
+                if (ok) {
+#pragma unroll 4
+                    for (int r = t / CH; r < rows; r += RI) {
+                        const RowsRow row = rows_row<D>(a, u, w.g, r);
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (row.seq >= 0) v = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + row.q + c);
+                        const int x = r >= tile_rows ? 1 : 0;
+                        *reinterpret_cast<uint4 *>(sm + x * C::kStage + (c >> 6) * kAtom + sw128(r - x * tile_rows, c & 63)) = v;
+                    }
+                    fence_async_smem();
+                    mbar_arrive(q_full);
+                }
+                ++seg;
+                w.next(a, n);
+            }
+        }
+    } else {
+        // ---------------- weights and outputs: thread r of a warpgroup holds row r of its row tile
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        const int X = warp >> 2, wq = warp & 3, row_in = wq * 32 + lane;
+        const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+        const uint32_t tS = tmem + 128 * X + lane_off, tO = tmem + 256 + lane_off;
+        float2 *ex = reinterpret_cast<float2 *>(sm + C::kOffEx);
+        const int n_pre = __ldcg(&a.head->n_pre);
+        uint32_t ns = 0, np = 0;  // scores and weights so far
+        bool ok = true;
+        while (w.left > 0) {
+            const RowsUnit u = rows_unit(a, w.unit);
+            const int n = w.part(u), rows = u.n * a.group;
+            const bool pair = rows > tile_rows;
+            const int r = pair ? X * tile_rows + row_in : row_in;
+            const int mine = pair && X == 1 ? rows - tile_rows : min(rows, tile_rows);  // rows of this tile
+            RowsRow row = rows_row<D>(a, u, w.g, r);
+            if (row_in >= mine) row.seq = -1;
+            if (row.seq < 0) row.pos = nullptr;
+            const bool busy = wq * 32 < mine;
+            const int steps = pair ? n : X == 0 ? (n + 1) / 2 : n / 2;
+            float m = -INFINITY, l = 0.f;
+            for (int s = 0; s < steps; ++s) {
+                const int t0 = rows_tile(u, w.j + (pair ? s : 2 * s + X)) * kRowsTile;
+                const bool full = row.seq < 0 || (t0 >= row.lo && t0 + 127 <= row.hi &&
+                                                  (t0 >= row.wlo || t0 + 127 < row.sh));
+                const bool masked = __any_sync(0xffffffffu, !full || row.pos);
+                uint32_t see[4];
+                if (masked && busy) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        see[k] = row.seq < 0 ? 0u
+                                             : range_bits(max(row.lo, row.wlo) - t0, row.hi - t0, k) |
+                                                   range_bits(row.lo - t0, min(row.sh - 1, row.hi) - t0, k);
+                    if (a.pos) {
+                        // liveness, one sequence of the warp's rows at a time: a lane looks up every 32nd slot
+                        const int rw = pair ? X * tile_rows + wq * 32 : wq * 32;
+                        const bool many = a.prefix && u.m0 >= 0;
+                        const int m0 = many ? rw / a.group : 0, m1 = many ? min(rw + 31, rows - 1) / a.group : 0;
+                        for (int k = m0; k <= m1; ++k) {
+                            const int from = many ? max(k * a.group - rw, 0) : 0;
+                            const int32_t *pos = reinterpret_cast<const int32_t *>(
+                                __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row.pos), from));
+                            const bool me = !many || r / a.group == k;
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                const int slot = t0 + 32 * x + lane;
+                                const bool live = pos && slot >= u.lo && slot < u.hi && __ldg(pos + (slot - u.S0)) >= 0;
+                                const uint32_t bits = __ballot_sync(0xffffffffu, live);
+                                if (me) see[x] &= bits;
+                            }
+                        }
+                    }
+                }
+                if (ok) ok = bar_wait(s_full(X), ns & 1, abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                ++ns;
+                if (ok && busy) {
+                    fence_after_sync();
+                    uint32_t v[128];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) tmem_ld32(tS + 32 * k, v + 32 * k);
+                    tmem_wait_ld();
+                    if (masked) {
+#pragma unroll
+                        for (int k = 0; k < 128; ++k)
+                            if (!((see[k >> 5] >> (k & 31)) & 1u)) v[k] = 0xff800000u;
+                    }
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int k = 0; k < 128; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(v[k]));
+                    const float top = __fmul_rn(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), a.scale_log2);
+                    if (s == 0) {
+                        m = top;
+                    } else {
+                        const bool move = top > m + kSlack;
+                        if (__any_sync(0xffffffffu, move)) {
+                            const float f = move ? ex2(m - top) : 1.f;
+                            ok = bar_wait(o_full(X), (np - 1) & 1, abort_flag);
+                            ok = __all_sync(0xffffffffu, ok);
+                            fence_after_sync();
+                            if (ok) {
+#pragma unroll
+                                for (int k = 0; k < D; k += 32) {
+                                    uint32_t o[32];
+                                    tmem_ld32(tO + 128 * X + k, o);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                    tmem_st32(tO + 128 * X + k, o);
+                                }
+                            }
+                            l *= f;
+                            if (move) m = top;
+                        }
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint32_t p[64];
+#pragma unroll
+                    for (int k = 0; k < 64; ++k) {
+                        const float x = ex2(__fmaf_rn(__uint_as_float(v[2 * k]), a.scale_log2, -ref));
+                        const float y = ex2(__fmaf_rn(__uint_as_float(v[2 * k + 1]), a.scale_log2, -ref));
+                        sum[k & 3] += x + y;
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+                        p[k] = *reinterpret_cast<const uint32_t *>(&h);
+                    }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    tmem_st32(tS, p);
+                    tmem_st32(tS + 32, p + 32);
+                    tmem_wait_st();
+                }
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full(X));
+                ++np;
+            }
+            if (steps > 0) {
+                if (ok) ok = bar_wait(o_full(X), (np - 1) & 1, abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                fence_after_sync();
+            }
+            float f0 = 1.f, f1 = 0.f;
+            if (!pair) {  // B's output joins A's
+                if (X == 1) ex[row_in] = make_float2(m, l);
+                fence_before_sync();
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                fence_after_sync();
+                if (X == 0 && n > 1) {
+                    const float2 o = ex[row_in];
+                    const float mn = fmaxf(m, o.x), ref = mn == -INFINITY ? 0.f : mn;
+                    f0 = ex2(m - ref);
+                    f1 = ex2(o.x - ref);
+                    l = l * f0 + o.y * f1;
+                    m = mn;
+                }
+            }
+            if (ok && busy && (pair || X == 0)) {
+                const bool begins = w.j == 0, whole = begins && n == u.nt && !a.prefix;
+                RowsHead h;
+                h.n_pre = n_pre;
+                const int64_t slot = whole ? 0 : rows_slot(a, h, u, w.unit, w.g, blockIdx.x, begins);
+                const bool joined = !pair && n > 1;
+                const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+                bool bad = false;
+#pragma unroll
+                for (int k = 0; k < D; k += 32) {
+                    uint32_t o[32];
+                    float y[32];
+                    tmem_ld32(tO + 128 * X + k, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) y[i] = __uint_as_float(o[i]);
+                    if (joined) {
+                        tmem_ld32(tO + 128 + k, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) y[i] = y[i] * f0 + __uint_as_float(o[i]) * f1;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        bad |= !(fabsf(y[i]) < INFINITY);
+                        y[i] *= inv;
+                    }
+                    if (row.seq >= 0) {
+                        if (whole) {
+                            T *d = static_cast<T *>(a.out) + row.out + k;
+#pragma unroll
+                            for (int i = 0; i < 32; i += 8) {
+                                uint32_t q[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const __nv_bfloat162 b2 = __floats2bfloat162_rn(y[i + 2 * e], y[i + 2 * e + 1]);
+                                    q[e] = *reinterpret_cast<const uint32_t *>(&b2);
+                                }
+                                *reinterpret_cast<uint4 *>(d + i) = make_uint4(q[0], q[1], q[2], q[3]);
+                            }
+                        } else {
+                            float *d = rows_part_o<D>(a, u, slot, r) + k;
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4) store4(d + i, y[i], y[i + 1], y[i + 2], y[i + 3]);
+                        }
+                    }
+                }
+                if (row.seq >= 0 && !whole) rows_store_ml(a, u, slot, r, m, l);
+                // (see rows_redo: V rows that are not finite and that the row does not see)
+                unsigned redo = __ballot_sync(0xffffffffu, bad && row.seq >= 0 && !isnan(l));
+                while (redo) {
+                    const int i = __ffs(redo) - 1;
+                    redo &= redo - 1;
+                    rows_redo<D, T>(a, u, w.g, w.j, n, whole, slot, __shfl_sync(0xffffffffu, r, i));
+                }
+            }
+            if (!pair) {  // (B's output has been read)
+                fence_before_sync();
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                fence_after_sync();
+            }
+            w.next(a, n);
+        }
+    }
+    fence_before_sync();
+    __syncthreads();
+    if (warp == 9) {
+        fence_after_sync();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
+    static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+        cudaDriverEntryPointQueryResult q;
+        void *p = nullptr;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q);
+        return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p)
+                                                                    : nullptr;
+    }();
+    return fn;
+}
+
+bool layer_map(CUtensorMap *m, const void *rows0, int head_dim, uint64_t rows, int rows_per_box) {
+    const auto fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)head_dim, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)head_dim * 2};
+    const cuuint32_t box[2] = {64u, (cuuint32_t)rows_per_box}, es[2] = {1u, 1u};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(rows0), dims, strides, box, es,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch_tc(const RowsArgs &a, cudaStream_t st) {
+    TcMap t;
+    const uint64_t rows = (uint64_t)a.pv.num_pages * a.pv.kv_heads * a.pv.page_size;
+    t.pool_rows = (int32_t)rows;
+    // boxes as high as the page allows, at most 64 rows: they are also the grain in which the ends of
+    // what a unit sees are read
+    t.rows_per_box = 8;
+    while (t.rows_per_box < 64 && a.pv.page_size % (2 * t.rows_per_box) == 0) t.rows_per_box *= 2;
+    CUtensorMap mk, mv;
+    const size_t off = (size_t)a.layer * rows * D * 2;
+    if (!layer_map(&mk, static_cast<const char *>(a.k) + off, D, rows, t.rows_per_box) ||
+        !layer_map(&mv, static_cast<const char *>(a.v) + off, D, rows, t.rows_per_box))
+        return cudaErrorInvalidValue;
+    const cudaError_t e = cudaFuncSetAttribute(rows_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc<D>::kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_k(rows_tc_kernel<D>, dim3(a.ctas), dim3(kThreads), Tc<D>::kSmem, st, mk, mv, a, t);
+}
+
+}  // namespace
+
+// (a TMA coordinate is 32 bits, and one behind the last row has to be one too)
+bool rows_tc_supported(const ikv_shape *s, const ikv_cache *c) {
+    return s->dtype == IKV_BF16 && c->page_size % 8 == 0 &&
+           (uint64_t)c->num_pages * s->kv_heads * c->page_size < 0x7fffff00u;
+}
+
+cudaError_t launch_rows_tc(const RowsArgs &a, int head_dim, cudaStream_t st) {
+    const cudaError_t e = head_dim == 64 ? launch_tc<64>(a, st) : launch_tc<128>(a, st);
+    note_launch();
+    return e;
+}
+
+cudaError_t read_clear_rows_tc_error(unsigned int *v) {
+    unsigned int z = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(v, g_rows_tc_error, sizeof(*v));
+    if (e == cudaSuccess && *v) e = cudaMemcpyToSymbol(g_rows_tc_error, &z, sizeof(z));
+    return e;
+}
+
+}  // namespace ikv

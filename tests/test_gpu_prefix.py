@@ -92,19 +92,20 @@ def check(c, groups, plens, status=0, **kw):
 @pytest.mark.parametrize("dtype,page", [("bf16", 64), ("bf16", 20), ("f32", 16)])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("group", [1, 2, 4, 7, 8])
-@pytest.mark.parametrize("gran", ["seq", "kvhead"])
-def test_shapes(dtype, page, d, group, gran):
+@pytest.mark.parametrize("gran,hidden", [("seq", math.nan), ("kvhead", math.nan), ("seq", 9.0)])
+def test_shapes(dtype, page, d, group, gran, hidden):
     lens = [200, 180, 131, 150, 133, 1, 77]
-    c = Cache(lens, 2, group, d, dtype, page, seed=1, gran=gran, share=[(0, [3, 1], 130), (4, [2], 129)]).device()
+    c = Cache(lens, 2, group, d, dtype, page, seed=1, gran=gran, share=[(0, [3, 1], 130), (4, [2], 129)]).device(hidden)
     check(c, [[0, 3, 1], [4, 2]], [130, 129], ema=True)
 
 
 @pytest.mark.parametrize("dtype,page", [("bf16", 16), ("bf16", 24), ("bf16", 5), ("f32", 16)])
 @pytest.mark.parametrize("plen", [0, 1, 127, 128, 129, 255, 256, 300])
 @pytest.mark.parametrize("start", [0, 9, 128])
-def test_prefixes_end_anywhere(dtype, page, plen, start):
+@pytest.mark.parametrize("hidden", [math.nan, 9.0])
+def test_prefixes_end_anywhere(dtype, page, plen, start, hidden):
     lens = [300, 301, 300, 420]
-    c = Cache(lens, 1, 4, 128, dtype, page, seed=2, starts=[start] * 4, share=[(1, [0, 2, 3], plen)]).device()
+    c = Cache(lens, 1, 4, 128, dtype, page, seed=2, starts=[start] * 4, share=[(1, [0, 2, 3], plen)]).device(hidden)
     check(c, [[1, 0, 3, 2]], [plen])
     check(c, [[1, 0, 3, 2]], [plen], layer=0, score=False)
 
@@ -125,17 +126,18 @@ def test_group_sizes(dtype, group, members):
     lens = [190 + i % 5 for i in range(members)] + [40, 7]
     order = [(i * 7) % members for i in range(members)] if members % 7 else list(range(members))
     c = Cache(lens, 1, group, 64 if members > 100 else 128, dtype, 16, seed=4, layers=2,
-              share=[(order[0], order[1:], 188)]).device()
+              share=[(order[0], order[1:], 188)]).device(9.0)
     check(c, [order], [188], score=members < 50)
 
 
 @pytest.mark.parametrize("dtype,page", [("bf16", 64), ("bf16", 12), ("f32", 16)])
 @pytest.mark.parametrize("gran", ["seq", "kvhead"])
 @pytest.mark.parametrize("dead", [0.2, 0.95, 1.0])
-def test_dead_slots_are_each_members_own(dtype, page, gran, dead):
+@pytest.mark.parametrize("hidden", [math.nan, 9.0])
+def test_dead_slots_are_each_members_own(dtype, page, gran, dead, hidden):
     lens = [200, 260, 240, 300, 50]
     c = Cache(lens, 2, 4, 128, dtype, page, seed=5, dead=dead, gran=gran, starts=[0, 5, 0, 0, 70],
-              share=[(1, [0, 2], 170)]).device()
+              share=[(1, [0, 2], 170)]).device(hidden)
     check(c, [[1, 0, 2]], [170], ema=True)
 
 
@@ -214,7 +216,7 @@ def test_many_groups():
     """More groups and sequences than threads of a CTA."""
     n = 1100
     lens = [20 + i % 9 for i in range(2 * n)]
-    c = Cache(lens, 1, 1, 64, "bf16", 8, seed=11, layers=1, share=[(i, [i + n], 18) for i in range(n)]).device()
+    c = Cache(lens, 1, 1, 64, "bf16", 8, seed=11, layers=1, share=[(i, [i + n], 18) for i in range(n)]).device(9.0)
     check(c, [[i, i + n] for i in range(n)], [18] * n, layer=0)
 
 

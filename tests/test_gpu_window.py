@@ -63,27 +63,30 @@ def counts_of(lens, kind):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("group", [1, 2, 4, 7, 8])
 @pytest.mark.parametrize("kind", ["one", "few", "all"])
-def test_shapes(dtype, page, d, group, kind):
+@pytest.mark.parametrize("hidden", [math.nan, 9.0])
+def test_shapes(dtype, page, d, group, kind, hidden):
     lens = [300, 1, 129, 57]
-    c = Cache(lens, 2, group, d, dtype, page, seed=1).device()
+    c = Cache(lens, 2, group, d, dtype, page, seed=1).device(hidden)
     check(c, counts_of(lens, kind), 100, 3)
 
 
 @pytest.mark.parametrize("dtype,page", [("bf16", 16), ("bf16", 20), ("f32", 16)])
 @pytest.mark.parametrize("window", [0, 1, 2, 63, 64, 128, 129, 200, 5000, 2**31 - 1])
 @pytest.mark.parametrize("sinks", [0, 1, 4, 130, 2**31 - 1])
-def test_windows(dtype, page, window, sinks):
+@pytest.mark.parametrize("hidden", [math.nan, 9.0])
+def test_windows(dtype, page, window, sinks, hidden):
     lens = [401, 128, 6]
-    c = Cache(lens, 1, 4, 128, dtype, page, seed=2, starts=[0, 5, 77]).device()
+    c = Cache(lens, 1, 4, 128, dtype, page, seed=2, starts=[0, 5, 77]).device(hidden)
     for kind in ("one", "some", "all"):
         check(c, counts_of(lens, kind), window, sinks)
 
 
 @pytest.mark.parametrize("dtype,page", [("bf16", 8), ("bf16", 24), ("bf16", 128), ("bf16", 256), ("bf16", 1), ("f32", 5)])
 @pytest.mark.parametrize("start", [0, 1, 127, 130])
-def test_pages_and_starts(dtype, page, start):
+@pytest.mark.parametrize("hidden", [math.nan, 9.0])
+def test_pages_and_starts(dtype, page, start, hidden):
     lens = [260, 33, 512]
-    c = Cache(lens, 2, 2, 128, dtype, page, seed=3, starts=[start, 0, start + 3]).device()
+    c = Cache(lens, 2, 2, 128, dtype, page, seed=3, starts=[start, 0, start + 3]).device(hidden)
     check(c, [7, 33, 140], 90, 5)
     check(c, [1, 1, 1], 90, 5, layer=0)
 
@@ -91,14 +94,15 @@ def test_pages_and_starts(dtype, page, start):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("gran", ["seq", "kvhead"])
 @pytest.mark.parametrize("dead", [0.3, 0.97, 1.0])
-def test_dead_slots_are_not_seen(dtype, gran, dead):
+@pytest.mark.parametrize("hidden", [math.nan, 9.0])
+def test_dead_slots_are_not_seen(dtype, gran, dead, hidden):
     lens = [300, 40, 131]
     c = Cache(lens, 2, 4, 128, dtype, 16, seed=4, dead=dead, gran=gran, starts=[3, 0, 64])
-    if gran == "seq":  # dead rows hold NaN
+    if gran == "seq" and math.isnan(hidden):  # dead rows hold NaN
         for b in range(len(lens)):
             c.k[b][:, :, ~c.alive(b, 0)] = math.nan
             c.v[b][:, :, ~c.alive(b, 0)] = math.inf
-    c.device()
+    c.device(hidden)
     check(c, [300, 40, 131], 50, 4)
     check(c, [1, 1, 1], 50, 4)
     check(c, [9, 9, 9], 0, 0)
@@ -174,7 +178,7 @@ def test_null_rows_and_counts():
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_long_contexts_split_over_the_gpu(dtype):
     """One token and a chunk of 300 over 20000 slots: every share's border inside a pair."""
-    c = Cache([20000], 2, 4, 128, dtype, 64, seed=11, layers=1).device()
+    c = Cache([20000], 2, 4, 128, dtype, 64, seed=11, layers=1).device(9.0)
     for counts, window in (([1], 0), ([1], 9999), ([300], 0)):
         check(c, counts, window, 4, layer=0)
 
@@ -188,7 +192,7 @@ def test_many_short_sequences():
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_large_logits(dtype):
     """Logits of some hundred: the running maximum moves far, weights underflow."""
-    c = Cache([700], 1, 4, 128, dtype, 64, seed=13, spread=40.0).device()
+    c = Cache([700], 1, 4, 128, dtype, 64, seed=13, spread=40.0).device(9.0)
     check(c, [700], 0, 0)
     check(c, [2], 300, 5)
 
