@@ -47,9 +47,10 @@ __device__ __forceinline__ void rows_store_ml(const RowsArgs &a, const RowsUnit 
 // multiply rows of V that a row does not see by 0, which leaves NaN where those are not finite.  Rare,
 // so simple: a slot at a time.
 template <int D, typename T>
-__device__ __noinline__ void rows_redo(const RowsArgs &a, const RowsUnit &u, int g, int j0, int n, bool whole,
-                                       int64_t slot, int r) {
+__device__ __noinline__ void rows_redo(const RowsArgs &a, int unit, int g, int j0, int n, bool whole, int64_t slot,
+                                       int r) {
     constexpr int E = D / 32;
+    const RowsUnit u = rows_unit(a, unit);
     const int lane = threadIdx.x & 31;
     const RowsRow row = rows_row<D>(a, u, g, r);
     float q[E], acc[E], m = -INFINITY, l = 0.f;

@@ -186,7 +186,7 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
         }
         for (int half = 0; half < 2; ++half)
             if ((redo >> (16 * half)) & 0xffffu)
-                rows_redo<D, T>(a, u, g, j0, n, whole, slot, ((tid >> 5) * 2 + half) * RPT + i);
+                rows_redo<D, T>(a, unit, g, j0, n, whole, slot, ((tid >> 5) * 2 + half) * RPT + i);
     }
 }
 

@@ -77,6 +77,22 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// two at a time: x y + z, x + y
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(r)
+        : "l"(*reinterpret_cast<unsigned long long *>(&x)), "l"(*reinterpret_cast<unsigned long long *>(&y)),
+          "l"(*reinterpret_cast<unsigned long long *>(&z)));
+    return *reinterpret_cast<float2 *>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(r)
+        : "l"(*reinterpret_cast<unsigned long long *>(&x)), "l"(*reinterpret_cast<unsigned long long *>(&y)));
+    return *reinterpret_cast<float2 *>(&r);
+}
 __device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
@@ -266,14 +282,37 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int n = w.part(u), rows = u.n * a.group;
                 if (seg > 0) ok = bar_wait(q_empty, (seg - 1) & 1, abort_flag);
                 if (ok) {
-#pragma unroll 4
-                    for (int r = t / CH; r < rows; r += RI) {
-                        const RowsRow row = rows_row<D>(a, u, w.g, r);
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (row.seq >= 0) v = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + row.q + c);
-                        const int x = r >= tile_rows ? 1 : 0;
-                        *reinterpret_cast<uint4 *>(sm + x * C::kStage + (c >> 6) * kAtom + sw128(r - x * tile_rows, c & 63)) = v;
+                    // every piece by an asynchronous copy, all of them in flight: a load of 16 bytes at a
+                    // time a thread took 30 us for 256 rows
+                    const bool many = a.prefix && u.m0 >= 0;
+                    const int64_t row0 = a.prefix ? u.b : (int64_t)u.row0 + u.m0;
+                    const T *q = static_cast<const T *>(a.q) + (int64_t)w.g * a.group * D + c;
+                    int tok = (t / CH) / a.group, h = (t / CH) % a.group;
+                    int x = 0, r = t / CH;  // row tile, row in it
+                    for (int i = t / CH; i < rows; i += RI) {
+                        int64_t row = row0 + tok;
+                        bool real = true;
+                        if (many) {
+                            const int b = __ldg(a.vm + u.m0 + tok);
+                            real = b >= 0;
+                            row = real ? b : 0;
+                        }
+                        const uint32_t dst = base + x * C::kStage + (c >> 6) * kAtom + sw128(r, c & 63);
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst),
+                                     "l"(q + row * a.q_stride + (int64_t)h * D), "r"(real ? 16 : 0)
+                                     : "memory");
+                        h += RI;
+                        while (h >= a.group) {
+                            h -= a.group;
+                            ++tok;
+                        }
+                        r += RI;
+                        if (r >= tile_rows && x == 0) {
+                            r -= tile_rows;
+                            x = 1;
+                        }
                     }
+                    asm volatile("cp.async.wait_all;" ::: "memory");
                     fence_async_smem();
                     mbar_arrive(q_full);
                 }
@@ -340,18 +379,26 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ++ns;
                 if (ok && busy) {
                     fence_after_sync();
-                    uint32_t v[128];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) tmem_ld32(tS + 32 * k, v + 32 * k);
-                    tmem_wait_ld();
-                    if (masked) {
-#pragma unroll
-                        for (int k = 0; k < 128; ++k)
-                            if (!((see[k >> 5] >> (k & 31)) & 1u)) v[k] = 0xff800000u;
-                    }
+                    // S is read twice, 32 columns at a time, so that a row's 128 scores never are in registers
+                    // together (that spilled, and cost more than the second read)
                     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    uint32_t va[32], vb[32];
+                    tmem_ld32(tS, va);
 #pragma unroll
-                    for (int k = 0; k < 128; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(v[k]));
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t *v = c & 1 ? vb : va;
+                        tmem_wait_ld(v);
+                        if (c < 3) tmem_ld32(tS + 32 * (c + 1), c & 1 ? va : vb);
+                        if (masked) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (!((see[c] >> k) & 1u)) v[k] = 0xff800000u;
+                        }
+#pragma unroll
+                        for (int k = 0; k < 32; k += 2)
+                            mx[(k >> 1) & 3] = fmaxf(fmaxf(mx[(k >> 1) & 3], __uint_as_float(v[k])), __uint_as_float(v[k + 1]));
+                    }
+                    tmem_ld32(tS, va);  // (again)
                     const float top = __fmul_rn(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), a.scale_log2);
                     if (s == 0) {
                         m = top;
@@ -367,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 for (int k = 0; k < D; k += 32) {
                                     uint32_t o[32];
                                     tmem_ld32(tO + 128 * X + k, o);
-                                    tmem_wait_ld();
+                                    tmem_wait_ld(o);
 #pragma unroll
                                     for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
                                     tmem_st32(tO + 128 * X + k, o);
@@ -378,19 +425,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                     const float ref = m == -INFINITY ? 0.f : m;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                    uint32_t p[64];
+                    // weights of 32 slots take 16 columns: they never reach scores that are still to be read
+                    const float2 sc2 = make_float2(a.scale_log2, a.scale_log2), ref2 = make_float2(-ref, -ref);
+                    float2 sum[4] = {};
 #pragma unroll
-                    for (int k = 0; k < 64; ++k) {
-                        const float x = ex2(__fmaf_rn(__uint_as_float(v[2 * k]), a.scale_log2, -ref));
-                        const float y = ex2(__fmaf_rn(__uint_as_float(v[2 * k + 1]), a.scale_log2, -ref));
-                        sum[k & 3] += x + y;
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-                        p[k] = *reinterpret_cast<const uint32_t *>(&h);
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t *v = c & 1 ? vb : va;
+                        tmem_wait_ld(v);
+                        if (c < 3) tmem_ld32(tS + 32 * (c + 1), c & 1 ? va : vb);
+                        if (masked) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (!((see[c] >> k) & 1u)) v[k] = 0xff800000u;
+                        }
+                        uint32_t p[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            float2 x = fma2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), sc2, ref2);
+                            x.x = ex2(x.x);
+                            x.y = ex2(x.y);
+                            sum[k & 3] = add2(sum[k & 3], x);
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
+                            p[k] = *reinterpret_cast<const uint32_t *>(&h);
+                        }
+                        tmem_st16(tS + 16 * c, p);
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                    tmem_st32(tS, p);
-                    tmem_st32(tS + 32, p + 32);
+                    const float2 s01 = add2(sum[0], sum[1]), s23 = add2(sum[2], sum[3]);
+                    l += (s01.x + s01.y) + (s23.x + s23.y);
                     tmem_wait_st();
                 }
                 fence_before_sync();
@@ -431,12 +492,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     uint32_t o[32];
                     float y[32];
                     tmem_ld32(tO + 128 * X + k, o);
-                    tmem_wait_ld();
+                    tmem_wait_ld(o);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) y[i] = __uint_as_float(o[i]);
                     if (joined) {
                         tmem_ld32(tO + 128 + k, o);
-                        tmem_wait_ld();
+                        tmem_wait_ld(o);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) y[i] = y[i] * f0 + __uint_as_float(o[i]) * f1;
                     }
@@ -471,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 while (redo) {
                     const int i = __ffs(redo) - 1;
                     redo &= redo - 1;
-                    rows_redo<D, T>(a, u, w.g, w.j, n, whole, slot, __shfl_sync(0xffffffffu, r, i));
+                    rows_redo<D, T>(a, w.unit, w.g, w.j, n, whole, slot, __shfl_sync(0xffffffffu, r, i));
                 }
             }
             if (!pair) {  // (B's output has been read)
