@@ -79,7 +79,7 @@ struct RowsArgs {
                                     // and 1 over their sum.  (Not their log-sum-exp: at logits of 100 its
                                     // rounding alone costs a weight 3e-6 of its value)
     // partial results: slot s holds rows_cap rows, part_ml [s][row] (max, sum) in the log2 domain,
-    // part_o [s][row][D].  Window: slot 2 c + 1 of CTA c for a pair that it begins, 2 c for one that it
+    // part_o [s][D / 4][row][4] (a thread stores a row, so that a warp's stores are one piece).  Window: slot 2 c + 1 of CTA c for a pair that it begins, 2 c for one that it
     // continues.  Prefix: pair number + CTA number, in regions of their own for the pairs of shared
     // prefixes and for those of own slots (own_ml, own_o; G rows a slot).
     int32_t rows_cap, ctas;

@@ -1,79 +1,91 @@
 // Merges the parts of packed-row attentions (rows.cuh): with (m_i, l_i, O_i) of each part of a row,
-//     M = max m_i, out = (sum 2^(m_i - M) O_i) / (sum 2^(m_i - M) l_i),
-// a warp a row.  Window: only the pairs that a share's border cuts have parts, and each border's CTA
-// finds its own.  Prefix: every row has parts, of its group's pair and of its own.
+//     M = max m_i, out = (sum 2^(m_i - M) O_i) / (sum 2^(m_i - M) l_i).
+// A CTA merges up to 8 rows of one pair.  Window: only the pairs that a share's border cuts have parts, and
+// each border's CTA finds its own.  Prefix: every row has parts, of its group's pair and of its own.
+// Latency is what it costs: the first parts' outputs are loaded before their weights are known.
 #include "rows_redo.cuh"
 
 namespace ikv {
 namespace {
 
-constexpr int kMergeWarps = 4;
+constexpr int kMergeThreads = 128, kMergeRows = 8, kMergeAhead = 8;
 
-// n parts: (max, sum) of part i at ml(i), output at o(i)
-template <int D, typename T, typename ML, typename O>
-__device__ __forceinline__ void merge_row(int n, ML ml, O o, float *wq, T *out, float2 *norm) {
-    constexpr int E = D / 32, kAhead = 8;
-    const int lane = threadIdx.x & 31;
-    // (one part of each lane is in registers; more than 32 parts are read twice)
-    float2 x0 = make_float2(-INFINITY, 0.f);
-    if (lane < n) x0 = __ldcg(ml(lane));
-    float M = x0.x;
-    for (int i = lane + 32; i < n; i += 32) M = fmaxf(M, __ldcg(ml(i)).x);
-    M = warp_max(M);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float W = 0.f;
-    for (int i = lane; i < n; i += 32) {
-        const float2 x = i == lane ? x0 : __ldcg(ml(i));
-        const float f = exp2f(x.x - ref);
-        W += x.y * f;
-        wq[i] = f;
-    }
-    W = warp_sum(W);
-    __syncwarp();
-    float acc[E];
+// n parts of `rows` <= 8 rows: (max, sum) of part i of row r at ml(i)[r], its channels 4 c .. at o(i)[c * step(i)
+// + 4 r].  done(r, ref, W): row r's maximum and sum; out(r): its output.
+template <int D, typename T, typename ML, typename O, typename Step, typename Done, typename Out>
+__device__ __forceinline__ void merge_rows(int n, int rows, ML ml, O o, Step step, Done done, Out out) {
+    constexpr int kChunks = D / 4, kIter = kChunks * kMergeRows / kMergeThreads;
+    __shared__ float wq[kMergeRows][2 * kRowsMaxCtas], total[kMergeRows];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int row = tid % kMergeRows, chunk = tid / kMergeRows;
+    float4 early[kIter][kMergeAhead];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    for (int i0 = 0; i0 < n; i0 += kAhead) {
-        float v[kAhead][E];
+    for (int k = 0; k < kIter; ++k)
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (i0 + i < n) {
-                const float *p = o(i0 + i) + lane * E;
-                if (E == 4) {
-                    const float4 y = __ldcg(reinterpret_cast<const float4 *>(p));
-                    v[i][0] = y.x;
-                    v[i][1] = y.y;
-                    v[i][E - 2] = y.z;
-                    v[i][E - 1] = y.w;
-                } else {
-                    const float2 y = __ldcg(reinterpret_cast<const float2 *>(p));
-                    v[i][0] = y.x;
-                    v[i][1] = y.y;
-                }
-            }
+        for (int i = 0; i < kMergeAhead; ++i)
+            if (i < n && row < rows)
+                early[k][i] = __ldcg(reinterpret_cast<const float4 *>(
+                    o(i) + (int64_t)(chunk + k * (kChunks / kIter)) * step(i) + 4 * row));
+    for (int r = warp; r < rows; r += kMergeThreads / 32) {
+        float2 x0 = make_float2(-INFINITY, 0.f);
+        if (lane < n) x0 = __ldcg(ml(lane) + r);
+        float M = x0.x;
+        for (int i = lane + 32; i < n; i += 32) M = fmaxf(M, __ldcg(ml(i) + r).x);
+        M = warp_max(M);
+        const float ref = M == -INFINITY ? 0.f : M;
+        float W = 0.f;
+        for (int i = lane; i < n; i += 32) {
+            const float2 x = i == lane ? x0 : __ldcg(ml(i) + r);
+            const float f = exp2f(x.x - ref);
+            W += x.y * f;
+            wq[r][i] = f;
         }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            if (i0 + i < n) {
-                const float f = wq[i0 + i];
-#pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] += f * v[i][e];
-            }
+        W = warp_sum(W);
+        if (lane == 0) {
+            total[r] = W;
+            done(r, ref, W);
+        }
     }
+    __syncthreads();
+    if (row < rows) {
+        const float W = total[row];
+        T *dst = out(row);
 #pragma unroll
-    for (int e = 0; e < E; ++e) store_as(out + lane * E + e, over_sum(acc[e], W));
-    // (a NaN sum leaves a NaN, for the scores to be NaN too)
-    if (norm && lane == 0) *norm = make_float2(ref, W == 0.f ? 0.f : 1.f / W);
-    __syncwarp();
+        for (int k = 0; k < kIter; ++k) {
+            const int c = chunk + k * (kChunks / kIter);
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+            auto add = [&](int i, float4 v) {
+                const float f = wq[row][i];
+                acc[0] += f * v.x;
+                acc[1] += f * v.y;
+                acc[2] += f * v.z;
+                acc[3] += f * v.w;
+            };
+#pragma unroll
+            for (int i = 0; i < kMergeAhead; ++i)
+                if (i < n) add(i, early[k][i]);
+            for (int i0 = kMergeAhead; i0 < n; i0 += kMergeAhead) {
+                float4 v[kMergeAhead];
+#pragma unroll
+                for (int i = 0; i < kMergeAhead; ++i)
+                    if (i0 + i < n)
+                        v[i] = __ldcg(reinterpret_cast<const float4 *>(o(i0 + i) + (int64_t)c * step(i0 + i) + 4 * row));
+#pragma unroll
+                for (int i = 0; i < kMergeAhead; ++i)
+                    if (i0 + i < n) add(i0 + i, v[i]);
+            }
+            store4(dst + 4 * c, over_sum(acc[0], W), over_sum(acc[1], W), over_sum(acc[2], W), over_sum(acc[3], W));
+        }
+    }
+    __syncthreads();
 }
 
 // Grid: (CTAs of the attention, row blocks).  CTA c: the pair that the border in front of share c cuts,
 // if no earlier border cuts it.
 template <int D, typename T>
-__global__ void __launch_bounds__(kMergeWarps * 32) rows_merge_window_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(kMergeThreads) rows_merge_window_kernel(const RowsArgs a) {
     pdl_wait();
-    __shared__ float wq[kMergeWarps][kRowsMaxCtas];
-    const int c = blockIdx.x, warp = threadIdx.x >> 5;
+    const int c = blockIdx.x;
     RowsWalk w;
     w.begin(a, c);
     if (w.left == 0 || w.j == 0) return;
@@ -82,25 +94,21 @@ __global__ void __launch_bounds__(kMergeWarps * 32) rows_merge_window_kernel(con
     const RowsUnit u = rows_unit(a, w.unit);
     const int n = 1 + (int)((u.nt - w.j + per - 1) / per);  // parts: share c - 1's and those behind
     const int rows = u.n * a.group;
-    for (int r = blockIdx.y * kMergeWarps + warp; r < rows; r += gridDim.y * kMergeWarps) {
-        const RowsRow row = rows_row<D>(a, u, w.g, r);
-        auto slot = [&](int i) { return i == 0 ? 2 * (int64_t)(c - 1) + 1 : 2 * (int64_t)(c + i - 1); };
-        merge_row<D, T>(
-            n, [&](int i) { return a.part_ml + slot(i) * a.rows_cap + r; },
-            [&](int i) { return a.part_o + (slot(i) * a.rows_cap + r) * D; }, wq[warp],
-            static_cast<T *>(a.out) + row.out, nullptr);
+    auto slot = [&](int i) { return i == 0 ? 2 * (int64_t)(c - 1) + 1 : 2 * (int64_t)(c + i - 1); };
+    for (int r0 = blockIdx.y * kMergeRows; r0 < rows; r0 += gridDim.y * kMergeRows) {
+        merge_rows<D, T>(
+            n, min(kMergeRows, rows - r0), [&](int i) { return a.part_ml + slot(i) * a.rows_cap + r0; },
+            [&](int i) { return a.part_o + slot(i) * a.rows_cap * D + 4 * r0; }, [&](int) { return 4 * a.rows_cap; },
+            [](int, float, float) {},
+            [&](int r) { return static_cast<T *>(a.out) + rows_row<D>(a, u, w.g, r0 + r).out; });
     }
 }
 
-// A warp a (sequence, query head)
+// A CTA a (sequence, KV head)
 template <int D, typename T>
-__global__ void __launch_bounds__(kMergeWarps * 32) rows_merge_prefix_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(kMergeThreads) rows_merge_prefix_kernel(const RowsArgs a) {
     pdl_wait();
-    __shared__ float wq[kMergeWarps][2 * kRowsMaxCtas];
-    const int warp = threadIdx.x >> 5, hk = a.pv.kv_heads;
-    const int64_t at = (int64_t)blockIdx.x * kMergeWarps + warp;
-    if (at >= (int64_t)a.batch * a.q_heads) return;
-    const int b = (int)(at / a.q_heads), h = (int)(at % a.q_heads), g = h / a.group, x = h % a.group;
+    const int hk = a.pv.kv_heads, b = blockIdx.x / hk, g = blockIdx.x % hk;
     const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.seq) + b);
     const int64_t per = __ldcg(&a.head->per);
     const int n_pre = __ldcg(&a.head->n_pre);
@@ -115,28 +123,27 @@ __global__ void __launch_bounds__(kMergeWarps * 32) rows_merge_prefix_kernel(con
     };
     if (s.x >= 0) np = parts(s.x, (int64_t)s.x * hk, slot_p);
     if (s.z >= 0) no = parts(s.z, (int64_t)(s.z - n_pre) * hk, slot_o);
-    const int rp = s.y * a.group + x;
-    merge_row<D, T>(
-        np + no,
+    const int rp = s.y * a.group;  // the pre part's rows
+    const int64_t row0 = (int64_t)b * a.q_heads + g * a.group;
+    merge_rows<D, T>(
+        np + no, a.group,
+        [&](int i) { return i < np ? a.part_ml + (slot_p + i) * a.rows_cap + rp : a.own_ml + (slot_o + i - np) * a.group; },
         [&](int i) {
-            return i < np ? a.part_ml + (slot_p + i) * a.rows_cap + rp : a.own_ml + (slot_o + i - np) * a.group + x;
+            return i < np ? a.part_o + (slot_p + i) * a.rows_cap * D + 4 * rp : a.own_o + (slot_o + i - np) * a.group * D;
         },
-        [&](int i) {
-            return i < np ? a.part_o + ((slot_p + i) * a.rows_cap + rp) * D
-                          : a.own_o + ((slot_o + i - np) * a.group + x) * D;
-        },
-        wq[warp], static_cast<T *>(a.out) + at * D, a.norm + at);
+        [&](int i) { return 4 * (i < np ? a.rows_cap : a.group); },
+        // (a NaN sum leaves a NaN, for the scores to be NaN too)
+        [&](int r, float ref, float W) { a.norm[row0 + r] = make_float2(ref, W == 0.f ? 0.f : 1.f / W); },
+        [&](int r) { return static_cast<T *>(a.out) + (row0 + r) * D; });
 }
 
 template <int D, typename T>
 cudaError_t launch_merge(const RowsArgs &a, cudaStream_t st) {
-    if (a.prefix) {
-        const int64_t rows = (int64_t)a.batch * a.q_heads;
-        return launch_k(rows_merge_prefix_kernel<D, T>, dim3((unsigned)((rows + kMergeWarps - 1) / kMergeWarps)),
-                        dim3(kMergeWarps * 32), 0, st, a);
-    }
-    const int y = (a.rows_cap + 4 * kMergeWarps - 1) / (4 * kMergeWarps);  // four rows a warp
-    return launch_k(rows_merge_window_kernel<D, T>, dim3(a.ctas, y), dim3(kMergeWarps * 32), 0, st, a);
+    if (a.prefix)
+        return launch_k(rows_merge_prefix_kernel<D, T>, dim3((unsigned)(a.batch * a.pv.kv_heads)), dim3(kMergeThreads), 0,
+                        st, a);
+    const int y = (a.rows_cap + kMergeRows - 1) / kMergeRows;
+    return launch_k(rows_merge_window_kernel<D, T>, dim3(a.ctas, y), dim3(kMergeThreads), 0, st, a);
 }
 
 // Scores without tensor cores: K once more, with each row's maximum M and sum of weights W,

@@ -20,10 +20,13 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, float a, float b, float
     *reinterpret_cast<uint2 *>(p) = w;
 }
 
-// Partial row r of a slot
+// Channels 0 .. 3 of partial row r of a slot, and the distance to the next four
 template <int D>
 __device__ __forceinline__ float *rows_part_o(const RowsArgs &a, const RowsUnit &u, int64_t slot, int r) {
-    return a.prefix && u.m0 < 0 ? a.own_o + (slot * a.group + r) * D : a.part_o + (slot * a.rows_cap + r) * D;
+    return a.prefix && u.m0 < 0 ? a.own_o + slot * a.group * D + 4 * r : a.part_o + slot * a.rows_cap * D + 4 * r;
+}
+__device__ __forceinline__ int rows_part_step(const RowsArgs &a, const RowsUnit &u) {
+    return 4 * (a.prefix && u.m0 < 0 ? a.group : a.rows_cap);
 }
 __device__ __forceinline__ float2 *rows_part_ml(const RowsArgs &a, const RowsUnit &u, int64_t slot, int r) {
     return a.prefix && u.m0 < 0 ? a.own_ml + slot * a.group + r : a.part_ml + slot * a.rows_cap + r;
@@ -36,7 +39,7 @@ __device__ __forceinline__ void rows_store4(const RowsArgs &a, const RowsUnit &u
         store4(static_cast<T *>(a.out) + row.out + c, over_sum(x[0], l), over_sum(x[1], l), over_sum(x[2], l),
                over_sum(x[3], l));
     else
-        store4(rows_part_o<D>(a, u, slot, r) + c, x[0], x[1], x[2], x[3]);
+        store4(rows_part_o<D>(a, u, slot, r) + (int64_t)(c / 4) * rows_part_step(a, u), x[0], x[1], x[2], x[3]);
 }
 __device__ __forceinline__ void rows_store_ml(const RowsArgs &a, const RowsUnit &u, int64_t slot, int r, float m,
                                               float l) {
@@ -81,7 +84,10 @@ __device__ __noinline__ void rows_redo(const RowsArgs &a, int unit, int g, int j
         for (int e = 0; e < E; ++e) store_as(static_cast<T *>(a.out) + row.out + lane + 32 * e, over_sum(acc[e], l));
     } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) rows_part_o<D>(a, u, slot, r)[lane + 32 * e] = acc[e];
+        for (int e = 0; e < E; ++e) {
+            const int c = lane + 32 * e;
+            rows_part_o<D>(a, u, slot, r)[(int64_t)(c / 4) * rows_part_step(a, u) + c % 4] = acc[e];
+        }
         if (lane == 0) rows_store_ml(a, u, slot, r, m, l);
     }
 }

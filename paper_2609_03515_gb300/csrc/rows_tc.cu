@@ -41,7 +41,7 @@ struct Tc {
     static constexpr int kOffRing = 2 * kStage;  // (Q of A and B in front)
     static constexpr int kOffEx = kOffRing + kStages * kStage;
     static constexpr int kOffBar = kOffEx + 128 * 8;
-    static constexpr int kBars = 2 * kStages + 9;
+    static constexpr int kBars = 2 * kStages + 10;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
     static constexpr int kSmem = kOffMisc + 16 + 1024;  // (to align by 1024)
 };
@@ -61,6 +61,10 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     *abort = 1;
     atomicOr(&g_rows_tc_error, 1u);
     return false;
+}
+// by a converged warp, with one answer for all of it
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
+    return __all_sync(0xffffffffu, bar_wait(bar, parity, abort));
 }
 // of one's own copies or products, whatever the abort flag says
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
@@ -126,11 +130,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t bar0 = base + C::kOffBar;
     auto kv_full = [&](int i) { return bar0 + 8u * i; };
     auto kv_empty = [&](int i) { return bar0 + 8u * (C::kStages + i); };
-    const uint32_t q_full = bar0 + 8u * (2 * C::kStages), q_empty = q_full + 8;
-    auto s_full = [&](int x) { return q_full + 16u + 8u * x; };
-    auto p_full = [&](int x) { return q_full + 32u + 8u * x; };
-    auto o_full = [&](int x) { return q_full + 48u + 8u * x; };
-    const uint32_t mma_done = q_full + 64u;
+    const uint32_t bar1 = bar0 + 8u * (2 * C::kStages), q_empty = bar1, mma_done = bar1 + 8;
+    auto q_full = [&](int x) { return bar1 + 16u + 8u * x; };
+    auto s_full = [&](int x) { return bar1 + 32u + 8u * x; };
+    auto p_full = [&](int x) { return bar1 + 48u + 8u * x; };
+    auto o_full = [&](int x) { return bar1 + 64u + 8u * x; };
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + C::kOffMisc + 4);
     if (warp == 8 && lane == 0) {
@@ -138,9 +142,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(kv_full(i), 1);
             mbar_init(kv_empty(i), 1);
         }
-        mbar_init(q_full, 64);
         mbar_init(q_empty, 1);
         for (int x = 0; x < 2; ++x) {
+            mbar_init(q_full(x), 64);
             mbar_init(s_full(x), 1);
             mbar_init(p_full(x), 4);
             mbar_init(o_full(x), 1);
@@ -205,91 +209,116 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
         } else if (warp == 9) {
             // ---------------- products
-            if (lane == 0) {
-                constexpr uint32_t id_qk = idesc_bf16(false, 128, 128), id_pv = idesc_bf16(false, 128, D, true);
-                int J = 0, seg = 0;
-                uint32_t np[2] = {0, 0};  // weights taken
-                bool ok = true;
-                while (w.left > 0 && ok) {
-                    const RowsUnit u = rows_unit(a, w.unit);
-                    const int n = w.part(u);
-                    const bool pair = u.n * a.group > tile_rows;
-                    auto qk = [&](int x, int j) {
-                        const int i = J + load_k(j), st = i % C::kStages;
-                        if (!bar_wait(kv_full(st), (i / C::kStages) & 1, abort_flag)) return false;
-                        fence_after_sync();
-                        const uint32_t q = base + (pair ? x * C::kStage : 0), k = base + C::kOffRing + st * C::kStage;
+            // The warp stays converged and one lane issues: descriptors are then formed in uniform registers.
+            // (A lane alone in a branch formed them in its own and took 125 cycles a product instead of 64.)
+            constexpr uint32_t id_qk = idesc_bf16(false, 128, 128), id_pv = idesc_bf16(false, 128, D, true);
+            const bool leader = elect_one();
+            const uint64_t dq0 = sdesc(base, 16, 1024), dk0 = sdesc(base + C::kOffRing, 16, 1024),
+                           dv0 = sdesc(base + C::kOffRing, kAtom, 1024);
+            int st0 = 0;                   // stage and parity of the part's first load
+            uint32_t par0 = 0, seg = 0;
+            uint32_t np[2] = {0, 0};       // weights taken
+            bool ok = true;
+            while (w.left > 0 && ok) {
+                const RowsUnit u = rows_unit(a, w.unit);
+                const int n = __shfl_sync(0xffffffffu, w.part(u), 0);
+                const bool pair = __shfl_sync(0xffffffffu, u.n * a.group > tile_rows, 0);
+                auto stage_of = [&](int x, int &st, uint32_t &par) {
+                    const int i = st0 + x;
+                    st = i % C::kStages;
+                    par = (par0 + i / C::kStages) & 1;
+                };
+                auto qk = [&](int x, int j) {
+                    int st;
+                    uint32_t par;
+                    stage_of(load_k(j), st, par);
+                    if (!warp_wait(kv_full(st), par, abort_flag)) return false;
+                    fence_after_sync();
+                    const uint64_t dq = dq0 + (pair ? x * (C::kStage >> 4) : 0), dk = dk0 + st * (C::kStage >> 4);
+                    if (leader) {
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk) {
-                            const uint32_t off = (kk >> 2) * kAtom + (kk & 3) * 32;
-                            mma_bf16(tmem + 128 * x, sdesc(q + off, 16, 1024), sdesc(k + off, 16, 1024), id_qk, kk > 0);
+                            const uint32_t off = ((kk >> 2) * kAtom + (kk & 3) * 32) >> 4;
+                            mma_bf16(tmem + 128 * x, dq + off, dk + off, id_qk, kk > 0);
                         }
                         if (!pair || x == 1) mma_commit(kv_empty(st));
                         mma_commit(s_full(x));
-                        return true;
-                    };
-                    auto pv = [&](int x, int j, bool first) {
-                        const int i = J + load_v(j, n), st = i % C::kStages;
-                        if (!bar_wait(p_full(x), np[x] & 1, abort_flag)) return false;
-                        ++np[x];
-                        if (!bar_wait(kv_full(st), (i / C::kStages) & 1, abort_flag)) return false;
-                        fence_after_sync();
-                        const uint32_t v = base + C::kOffRing + st * C::kStage;
+                    }
+                    __syncwarp();
+                    return true;
+                };
+                auto pv = [&](int x, int j, bool first) {
+                    int st;
+                    uint32_t par;
+                    stage_of(load_v(j, n), st, par);
+                    if (!warp_wait(kv_full(st), par, abort_flag)) return false;
+                    if (!warp_wait(p_full(x), np[x] & 1, abort_flag)) return false;
+                    ++np[x];
+                    fence_after_sync();
+                    const uint64_t dv = dv0 + st * (C::kStage >> 4);
+                    if (leader) {
 #pragma unroll
                         for (int kk = 0; kk < kRowsTile / 16; ++kk)  // V: channels contiguous, 8-slot groups 1 KB apart
-                            mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * kk, sdesc(v + kk * 2048, kAtom, 1024), id_pv,
+                            mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * kk, dv + kk * (2048 >> 4), id_pv,
                                         !first || kk > 0);
                         if (!pair || x == 1) mma_commit(kv_empty(st));
                         mma_commit(o_full(x));
-                        return true;
-                    };
-                    ok = bar_wait(q_full, seg & 1, abort_flag);
-                    fence_after_sync();
-                    // P of a tile lies over its S: S of the next is issued behind the product that takes P
-                    if (pair) {
-                        ok = ok && qk(0, 0) && qk(1, 0);
-                        if (ok && n == 1) mma_commit(q_empty);
-                        for (int j = 0; j < n && ok; ++j) {
-                            ok = pv(0, j, j == 0) && (j + 1 == n || qk(0, j + 1)) && pv(1, j, j == 0) &&
-                                 (j + 1 == n || qk(1, j + 1));
-                            if (ok && j + 2 == n) mma_commit(q_empty);
-                        }
-                    } else {
-                        ok = ok && qk(0, 0) && (n == 1 || qk(1, 1));
-                        if (ok && n <= 2) mma_commit(q_empty);
-                        for (int j = 0; j < n && ok; ++j) {
-                            ok = pv(j & 1, j, j < 2) && (j + 2 >= n || qk(j & 1, j + 2));
-                            if (ok && j + 3 == n) mma_commit(q_empty);
-                        }
                     }
-                    J += 2 * n;
-                    ++seg;
-                    w.next(a, n);
+                    __syncwarp();
+                    return true;
+                };
+                auto q_done = [&] {
+                    if (leader) mma_commit(q_empty);
+                    __syncwarp();
+                };
+                ok = warp_wait(q_full(0), seg & 1, abort_flag);
+                // P of a tile lies over its S: S of the next is issued behind the product that takes P
+                if (pair) {
+                    ok = ok && qk(0, 0) && warp_wait(q_full(1), seg & 1, abort_flag) && qk(1, 0);
+                    if (ok && n == 1) q_done();
+                    for (int j = 0; j < n && ok; ++j) {
+                        ok = pv(0, j, j == 0) && (j + 1 == n || qk(0, j + 1)) && pv(1, j, j == 0) &&
+                             (j + 1 == n || qk(1, j + 1));
+                        if (ok && j + 2 == n) q_done();
+                    }
+                } else {
+                    ok = ok && warp_wait(q_full(1), seg & 1, abort_flag) && qk(0, 0) && (n == 1 || qk(1, 1));
+                    if (ok && n <= 2) q_done();
+                    for (int j = 0; j < n && ok; ++j) {
+                        ok = pv(j & 1, j, j < 2) && (j + 2 >= n || qk(j & 1, j + 2));
+                        if (ok && j + 3 == n) q_done();
+                    }
                 }
-                mma_commit(mma_done);  // also after an abort: no product may write TMEM when it is freed
-                bar_drain(mma_done, 0);
+                st0 += 2 * n;
+                par0 = (par0 + st0 / C::kStages) & 1;
+                st0 %= C::kStages;
+                ++seg;
+                w.next(a, n);
             }
+            if (leader) mma_commit(mma_done);  // also after an abort: no product may write TMEM when it is freed
             __syncwarp();
+            bar_drain(mma_done, 0);
         } else {
             // ---------------- Q
             const int t = tid - 320;
-            constexpr int CH = D / 8, RI = 64 / CH;  // 16-byte pieces of a row, rows an iteration
-            const int c = t % CH * 8;
-            int seg = 0;
+            // Every piece by an asynchronous copy, all of them in flight: four lanes a row, 16 rows an iteration.
+            // A's rows are handed over first.
+            constexpr int CH = D / 8;      // 16-byte pieces of a row
+            const int c = t & 3;
+            uint32_t seg = 0;
             bool ok = true;
             while (w.left > 0 && ok) {
                 const RowsUnit u = rows_unit(a, w.unit);
                 const int n = w.part(u), rows = u.n * a.group;
+                const bool many = a.prefix && u.m0 >= 0;
+                const int64_t row0 = a.prefix ? u.b : (int64_t)u.row0 + u.m0;
+                const T *q = static_cast<const T *>(a.q) + (int64_t)w.g * a.group * D + 8 * c;
                 if (seg > 0) ok = bar_wait(q_empty, (seg - 1) & 1, abort_flag);
-                if (ok) {
-                    // every piece by an asynchronous copy, all of them in flight: a load of 16 bytes at a
-                    // time a thread took 30 us for 256 rows
-                    const bool many = a.prefix && u.m0 >= 0;
-                    const int64_t row0 = a.prefix ? u.b : (int64_t)u.row0 + u.m0;
-                    const T *q = static_cast<const T *>(a.q) + (int64_t)w.g * a.group * D + c;
-                    int tok = (t / CH) / a.group, h = (t / CH) % a.group;
-                    int x = 0, r = t / CH;  // row tile, row in it
-                    for (int i = t / CH; i < rows; i += RI) {
+                for (int x = 0; x < 2 && ok; ++x) {
+                    const int first = x * tile_rows, end = min(rows - first, tile_rows);
+                    int tok = (first + t / 4) / a.group, h = (first + t / 4) % a.group;
+#pragma unroll 2
+                    for (int r = t / 4; r < end; r += 16) {
                         int64_t row = row0 + tok;
                         bool real = true;
                         if (many) {
@@ -297,24 +326,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                             real = b >= 0;
                             row = real ? b : 0;
                         }
-                        const uint32_t dst = base + x * C::kStage + (c >> 6) * kAtom + sw128(r, c & 63);
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst),
-                                     "l"(q + row * a.q_stride + (int64_t)h * D), "r"(real ? 16 : 0)
-                                     : "memory");
-                        h += RI;
-                        while (h >= a.group) {
+                        const T *src = q + row * a.q_stride + (int64_t)h * D;
+                        const uint32_t dst = base + x * C::kStage + r * 128;
+#pragma unroll
+                        for (int i = 0; i < CH / 4; ++i)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                             dst + (i >> 1) * kAtom + ((((c + 4 * i) ^ r) & 7) << 4)),
+                                         "l"(src + 32 * i), "r"(real ? 16 : 0)
+                                         : "memory");
+                        h += 16 % a.group;
+                        tok += 16 / a.group;
+                        if (h >= a.group) {
                             h -= a.group;
                             ++tok;
                         }
-                        r += RI;
-                        if (r >= tile_rows && x == 0) {
-                            r -= tile_rows;
-                            x = 1;
-                        }
                     }
-                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                }
+                if (ok) {
+                    asm volatile("cp.async.wait_group 1;" ::: "memory");
                     fence_async_smem();
-                    mbar_arrive(q_full);
+                    mbar_arrive(q_full(0));
+                    asm volatile("cp.async.wait_group 0;" ::: "memory");
+                    fence_async_smem();
+                    mbar_arrive(q_full(1));
                 }
                 ++seg;
                 w.next(a, n);
@@ -520,9 +555,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 *reinterpret_cast<uint4 *>(d + i) = make_uint4(q[0], q[1], q[2], q[3]);
                             }
                         } else {
-                            float *d = rows_part_o<D>(a, u, slot, r) + k;
+                            const int step = rows_part_step(a, u);
+                            float *d = rows_part_o<D>(a, u, slot, r) + (int64_t)(k / 4) * step;
 #pragma unroll
-                            for (int i = 0; i < 32; i += 4) store4(d + i, y[i], y[i + 1], y[i + 2], y[i + 3]);
+                            for (int i = 0; i < 32; i += 4) store4(d + (i / 4) * step, y[i], y[i + 1], y[i + 2], y[i + 3]);
                         }
                     }
                 }
