@@ -30,15 +30,19 @@ struct RowsUnit {                   // 64 bytes
     int32_t wlo, sh;                // some row sees the slots of [lo, sh) and of [wlo, hi), none sees others
     int32_t t_a, n_a, t_w, nt;      // tile i of nt: t_a + i for i < n_a, t_w + i - n_a behind
     int32_t row0;                   // window: row of query token 0 in q and out
-    int64_t cum;                    // tiles of all earlier units, for all KV heads
+    int64_t cum;                    // cost of all earlier units, for all KV heads
 };
 
+// Cost is counted in tiles; a pair costs kRowsExtra besides its own, for its first products, which nothing
+// overlaps, and its output.
+constexpr int kRowsExtra = 2;
+
 struct RowsHead {
-    int64_t total, per;             // tiles in all, tiles of a CTA's share
+    int64_t total, per;             // cost in all, of a CTA's share
     int32_t n_units, n_pre;         // n_pre: units of shared prefixes, in front of the others
 };
-struct RowsStart {                  // where a CTA's share begins, and its tiles
-    int32_t unit, g, j, n;
+struct RowsStart {                  // where a CTA's share begins (at cost `at` of pair (unit, g)), and its cost
+    int32_t unit, g, at, n;
 };
 struct RowsSeq {                    // prefix: what sequence b's rows are made from
     int32_t pre, entry;             // its group's unit that holds it (-1: none), its member number there
@@ -97,21 +101,26 @@ __device__ __forceinline__ int64_t rows_slot(const RowsArgs &a, const RowsHead &
 // The tile of a unit
 __device__ __forceinline__ int rows_tile(const RowsUnit &u, int i) { return i < u.n_a ? u.t_a + i : u.t_w + i - u.n_a; }
 
-// The parts of a share, in turn
+// The parts of a share, in turn.  The first kRowsExtra of a pair's cost lie in front of its tiles; a border
+// in them cuts nothing.
 struct RowsWalk {
     int32_t unit, g, j, left;       // the next part begins at tile j of pair (unit, g)
+    int32_t skip;                   // cost in front of tile j that is this share's
     __device__ __forceinline__ void begin(const RowsArgs &a, int cta) {
         const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.start) + cta);
         unit = s.x;
         g = s.y;
-        j = s.z;
+        j = max(s.z - kRowsExtra, 0);
+        skip = max(kRowsExtra - s.z, 0);
         left = s.w;
     }
-    // the part's tiles, given its unit
-    __device__ __forceinline__ int part(const RowsUnit &u) const { return min(u.nt - j, left); }
-    __device__ __forceinline__ void next(const RowsArgs &a, int n) {
-        left -= n;
+    // whether there is a part, and its tiles, given its unit's
+    __device__ __forceinline__ bool more() const { return left > skip; }
+    __device__ __forceinline__ int part(int nt) const { return min(nt - j, left - skip); }
+    __device__ __forceinline__ void next(const RowsArgs &a, int nt, int n) {
+        left -= skip + n;
         j = 0;
+        skip = kRowsExtra;
         if (++g == a.pv.kv_heads) {
             g = 0;
             ++unit;

@@ -74,6 +74,10 @@ __device__ __forceinline__ void whole_run(RowsUnit &u, int lo, int hi) {
     u.row0 = 0;
 }
 
+__device__ __forceinline__ int64_t cost(const RowsUnit &u, int kv_heads) {
+    return u.nt > 0 ? (int64_t)(u.nt + kRowsExtra) * kv_heads : 0;
+}
+
 __device__ __forceinline__ void store_unit(const RowsArgs &a, int at, const RowsUnit &u) {
     int4 *d = reinterpret_cast<int4 *>(a.units + at);
     const int4 *s = reinterpret_cast<const int4 *>(&u);
@@ -88,7 +92,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
     __shared__ int32_t small_tab[6 * kPlanSmall];
     const int tid = threadIdx.x, nthr = blockDim.x, hk = a.pv.kv_heads;
     int units = 0, n_pre = 0;
-    int64_t tiles = 0;
+    int64_t tiles = 0;  // (their cost)
     if (!a.prefix) {
         const int64_t all = (int64_t)a.batch * a.seq_units;
         for (int64_t i0 = 0; i0 < all; i0 += nthr) {
@@ -121,7 +125,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
                 }
             }
             int at;
-            scan(sc, u.nt > 0 ? 1 : 0, (int64_t)u.nt * hk, units, tiles, at, u.cum);
+            scan(sc, u.nt > 0 ? 1 : 0, cost(u, hk), units, tiles, at, u.cum);
             if (u.nt > 0) {
                 store_unit(a, at, u);
                 if (at < kPlanCum) cums[at] = u.cum;
@@ -208,12 +212,12 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
             }
             int at;
             int64_t cum;
-            scan(sc, n, (int64_t)n * u.nt * hk, units, tiles, at, cum);
+            scan(sc, n, n * cost(u, hk), units, tiles, at, cum);
             if (i < n_groups) gunit[i] = at;
             for (int k = 0; k < n; ++k) {
                 u.m0 = e0 + k * a.unit_n;
                 u.n = min(a.unit_n, e1 - u.m0);
-                u.cum = cum + (int64_t)k * u.nt * hk;
+                u.cum = cum + k * cost(u, hk);
                 store_unit(a, at + k, u);
                 if (at + k < kPlanCum) cums[at + k] = u.cum;
             }
@@ -242,7 +246,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
                 whole_run(u, u.S0 + s.len, u.S0 + clamp_len(a, b, u.S0));
             }
             int at;
-            scan(sc, u.nt > 0 ? 1 : 0, (int64_t)u.nt * hk, units, tiles, at, u.cum);
+            scan(sc, u.nt > 0 ? 1 : 0, cost(u, hk), units, tiles, at, u.cum);
             if (u.nt > 0) {
                 store_unit(a, at, u);
                 if (at < kPlanCum) cums[at] = u.cum;
@@ -272,11 +276,11 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
                 else
                     hi = mid;
             }
-            const int nt = __ldcg(&a.units[lo].nt);
+            const int each = __ldcg(&a.units[lo].nt) + kRowsExtra;
             const int64_t r = x - (lo < kPlanCum ? cums[lo] : __ldcg(&a.units[lo].cum));
             s.unit = lo;
-            s.g = (int32_t)(r / nt);
-            s.j = (int32_t)(r % nt);
+            s.g = (int32_t)(r / each);
+            s.at = (int32_t)(r % each);
             s.n = (int32_t)min(per, tiles - x);
         }
         *reinterpret_cast<int4 *>(a.start + c) = *reinterpret_cast<int4 *>(&s);

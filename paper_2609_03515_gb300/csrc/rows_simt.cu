@@ -202,14 +202,14 @@ __global__ void __launch_bounds__(kSimtThreads) rows_simt_kernel(const RowsArgs 
     head.n_pre = __ldcg(&a.head->n_pre);
     RowsWalk w;
     w.begin(a, blockIdx.x);
-    while (w.left > 0) {
+    while (w.more()) {
         const RowsUnit u = rows_unit(a, w.unit);
-        const int n = w.part(u);
+        const int n = w.part(u.nt);
         if (u.n * a.group <= 16)
             simt_part<D, T, 1>(a, head, u, w.unit, w.g, w.j, n, sQ, sK, sV, sP);
         else
             simt_part<D, T, 4>(a, head, u, w.unit, w.g, w.j, n, sQ, sK, sV, sP);
-        w.next(a, n);
+        w.next(a, u.nt, n);
     }
 }
 

@@ -37,11 +37,12 @@ constexpr float kSlack = 8.f;               // log2 of the largest weight before
 template <int D>
 struct Tc {
     static constexpr int kStage = kAtom * (D / 64);
-    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr int kStages = D == 128 ? 4 : 8;
     static constexpr int kOffRing = 2 * kStage;  // (Q of A and B in front)
-    static constexpr int kOffEx = kOffRing + kStages * kStage;
+    static constexpr int kOffOut = kOffRing + kStages * kStage;  // a warp: 64 channels of its 32 rows
+    static constexpr int kOffEx = kOffOut + 8 * 4096;
     static constexpr int kOffBar = kOffEx + 128 * 8;
-    static constexpr int kBars = 2 * kStages + 10;
+    static constexpr int kBars = 2 * kStages + 12;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
     static constexpr int kSmem = kOffMisc + 16 + 1024;  // (to align by 1024)
 };
@@ -50,8 +51,9 @@ struct TcMap {
     int32_t rows_per_box, pool_rows;        // pool_rows: rows of the layer, a row behind the end
 };
 
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
-    if (mbar_test(bar, parity)) return true;
+// Bounded: false where the phase does not complete in time (which also raises the CTA's abort flag and the
+// error word), or once another warp has given up.
+__device__ __forceinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *abort) {
     const uint64_t start = global_ns();
     for (;;) {
         if (mbar_try(bar, parity, 2000)) return true;
@@ -62,9 +64,13 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     atomicOr(&g_rows_tc_error, 1u);
     return false;
 }
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
+    return mbar_try(bar, parity, 2000) || bar_wait_long(bar, parity, abort);
+}
 // by a converged warp, with one answer for all of it
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
-    return __all_sync(0xffffffffu, bar_wait(bar, parity, abort));
+    if (__all_sync(0xffffffffu, mbar_try(bar, parity, 2000))) return true;
+    return __all_sync(0xffffffffu, bar_wait_long(bar, parity, abort));
 }
 // of one's own copies or products, whatever the abort flag says
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
@@ -114,8 +120,6 @@ __device__ __forceinline__ void load_of(int x, int n, int &tile, bool &is_v) {
     is_v = x == 2 * n - 1 || (x > 0 && !(x & 1));
     tile = x == 2 * n - 1 ? n - 1 : is_v ? (x - 2) / 2 : (x + 1) / 2;
 }
-__device__ __forceinline__ int load_k(int j) { return j == 0 ? 0 : 2 * j - 1; }
-__device__ __forceinline__ int load_v(int j, int n) { return j < n - 1 ? 2 * j + 2 : 2 * n - 1; }
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -135,6 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto s_full = [&](int x) { return bar1 + 32u + 8u * x; };
     auto p_full = [&](int x) { return bar1 + 48u + 8u * x; };
     auto o_full = [&](int x) { return bar1 + 64u + 8u * x; };
+    auto p_half = [&](int x) { return bar1 + 80u + 8u * x; };
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + C::kOffMisc + 4);
     if (warp == 8 && lane == 0) {
@@ -147,6 +152,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(q_full(x), 64);
             mbar_init(s_full(x), 1);
             mbar_init(p_full(x), 4);
+            mbar_init(p_half(x), 4);
             mbar_init(o_full(x), 1);
         }
         mbar_init(mma_done, 1);
@@ -168,15 +174,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     w.begin(a, blockIdx.x);
 
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 8) {
             // ---------------- K and V, a lane a box
             int J = 0;
             bool ok = true;
             const int boxes = kRowsTile / tm.rows_per_box;
-            while (w.left > 0 && ok) {
+            while (w.more() && ok) {
                 const RowsUnit u = rows_unit(a, w.unit);
-                const int n = w.part(u);
+                const int n = w.part(u.nt);
                 for (int x = 0; x < 2 * n && ok; ++x, ++J) {
                     int tile;
                     bool is_v;
@@ -202,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     if (!ok) break;
                 }
-                w.next(a, n);
+                w.next(a, u.nt, n);
             }
             if (lane == 0)  // every copy has landed before the CTA ends
                 for (int i = J - 1; i >= 0 && i >= J - C::kStages; --i) bar_drain(kv_full(i % C::kStages), (i / C::kStages) & 1);
@@ -215,54 +221,59 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool leader = elect_one();
             const uint64_t dq0 = sdesc(base, 16, 1024), dk0 = sdesc(base + C::kOffRing, 16, 1024),
                            dv0 = sdesc(base + C::kOffRing, kAtom, 1024);
-            int st0 = 0;                   // stage and parity of the part's first load
-            uint32_t par0 = 0, seg = 0;
-            uint32_t np[2] = {0, 0};       // weights taken
+            struct Stage {
+                int i;
+                uint32_t par;
+            } at{0, 0};                    // the next load to be used
+            auto take = [&] {
+                const Stage s = at;
+                if (++at.i == C::kStages) at = Stage{0, at.par ^ 1};
+                return s;
+            };
+            uint32_t seg = 0, np[2] = {0, 0};  // weights taken
             bool ok = true;
-            while (w.left > 0 && ok) {
-                const RowsUnit u = rows_unit(a, w.unit);
-                const int n = __shfl_sync(0xffffffffu, w.part(u), 0);
-                const bool pair = __shfl_sync(0xffffffffu, u.n * a.group > tile_rows, 0);
-                auto stage_of = [&](int x, int &st, uint32_t &par) {
-                    const int i = st0 + x;
-                    st = i % C::kStages;
-                    par = (par0 + i / C::kStages) & 1;
-                };
-                auto qk = [&](int x, int j) {
-                    int st;
-                    uint32_t par;
-                    stage_of(load_k(j), st, par);
-                    if (!warp_wait(kv_full(st), par, abort_flag)) return false;
+            while (w.more() && ok) {
+                const RowsUnit *up = a.units + w.unit;
+                const int n = __shfl_sync(0xffffffffu, w.part(up->nt), 0);
+                const bool pair = __shfl_sync(0xffffffffu, up->n * a.group > tile_rows, 0);
+                auto there = [&](Stage s) { return warp_wait(kv_full(s.i), s.par, abort_flag); };
+                // S of row tile x; (free: K's stage is done with then)
+                auto qk = [&](int x, Stage k, bool free) {
                     fence_after_sync();
-                    const uint64_t dq = dq0 + (pair ? x * (C::kStage >> 4) : 0), dk = dk0 + st * (C::kStage >> 4);
+                    const uint64_t dq = dq0 + (pair ? x * (C::kStage >> 4) : 0), dk = dk0 + k.i * (C::kStage >> 4);
                     if (leader) {
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk) {
                             const uint32_t off = ((kk >> 2) * kAtom + (kk & 3) * 32) >> 4;
                             mma_bf16(tmem + 128 * x, dq + off, dk + off, id_qk, kk > 0);
                         }
-                        if (!pair || x == 1) mma_commit(kv_empty(st));
                         mma_commit(s_full(x));
+                        if (free) mma_commit(kv_empty(k.i));
                     }
                     __syncwarp();
-                    return true;
                 };
-                auto pv = [&](int x, int j, bool first) {
-                    int st;
-                    uint32_t par;
-                    stage_of(load_v(j, n), st, par);
-                    if (!warp_wait(kv_full(st), par, abort_flag)) return false;
+                // O of row tile x, the first half of the slots as soon as their weights are there
+                auto pv = [&](int x, Stage v, bool first, bool free) {
+                    if (!warp_wait(p_half(x), np[x] & 1, abort_flag)) return false;
+                    fence_after_sync();
+                    const uint64_t dv = dv0 + v.i * (C::kStage >> 4);
+                    auto product = [&](int kk) {  // V: channels contiguous, 8-slot groups 1 KB apart
+                        mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * kk, dv + kk * (2048 >> 4), id_pv,
+                                    !first || kk > 0);
+                    };
+                    if (leader) {
+#pragma unroll
+                        for (int kk = 0; kk < kRowsTile / 32; ++kk) product(kk);
+                    }
+                    __syncwarp();
                     if (!warp_wait(p_full(x), np[x] & 1, abort_flag)) return false;
                     ++np[x];
                     fence_after_sync();
-                    const uint64_t dv = dv0 + st * (C::kStage >> 4);
                     if (leader) {
 #pragma unroll
-                        for (int kk = 0; kk < kRowsTile / 16; ++kk)  // V: channels contiguous, 8-slot groups 1 KB apart
-                            mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * kk, dv + kk * (2048 >> 4), id_pv,
-                                        !first || kk > 0);
-                        if (!pair || x == 1) mma_commit(kv_empty(st));
+                        for (int kk = kRowsTile / 32; kk < kRowsTile / 16; ++kk) product(kk);
                         mma_commit(o_full(x));
+                        if (free) mma_commit(kv_empty(v.i));
                     }
                     __syncwarp();
                     return true;
@@ -271,29 +282,49 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (leader) mma_commit(q_empty);
                     __syncwarp();
                 };
-                ok = warp_wait(q_full(0), seg & 1, abort_flag);
                 // P of a tile lies over its S: S of the next is issued behind the product that takes P
+                Stage k = take();
+                ok = warp_wait(q_full(0), seg & 1, abort_flag) && there(k);
+                if (!ok) break;
+                qk(0, k, !pair);
+                ok = warp_wait(q_full(1), seg & 1, abort_flag);
+                if (!ok) break;
                 if (pair) {
-                    ok = ok && qk(0, 0) && warp_wait(q_full(1), seg & 1, abort_flag) && qk(1, 0);
-                    if (ok && n == 1) q_done();
-                    for (int j = 0; j < n && ok; ++j) {
-                        ok = pv(0, j, j == 0) && (j + 1 == n || qk(0, j + 1)) && pv(1, j, j == 0) &&
-                             (j + 1 == n || qk(1, j + 1));
-                        if (ok && j + 2 == n) q_done();
+                    qk(1, k, true);
+                    if (n == 1) q_done();
+                    for (int j = 0; j < n; ++j) {
+                        const bool more = j + 1 < n;
+                        if (more) k = take();
+                        const Stage v = take();
+                        ok = (!more || there(k)) && there(v) && pv(0, v, j == 0, false);
+                        if (!ok) break;
+                        if (more) qk(0, k, false);
+                        ok = pv(1, v, j == 0, true);
+                        if (!ok) break;
+                        if (more) qk(1, k, true);
+                        if (j + 2 == n) q_done();
                     }
                 } else {
-                    ok = ok && warp_wait(q_full(1), seg & 1, abort_flag) && qk(0, 0) && (n == 1 || qk(1, 1));
-                    if (ok && n <= 2) q_done();
-                    for (int j = 0; j < n && ok; ++j) {
-                        ok = pv(j & 1, j, j < 2) && (j + 2 >= n || qk(j & 1, j + 2));
-                        if (ok && j + 3 == n) q_done();
+                    if (n > 1) {
+                        k = take();
+                        if (!(ok = there(k))) break;
+                        qk(1, k, true);
+                    }
+                    if (n <= 2) q_done();
+                    for (int j = 0; j < n; ++j) {
+                        const Stage v = take();
+                        ok = there(v) && pv(j & 1, v, j < 2, true);
+                        if (!ok) break;
+                        if (j + 2 < n) {
+                            k = take();
+                            if (!(ok = there(k))) break;
+                            qk(j & 1, k, true);
+                            if (j + 3 == n) q_done();
+                        }
                     }
                 }
-                st0 += 2 * n;
-                par0 = (par0 + st0 / C::kStages) & 1;
-                st0 %= C::kStages;
                 ++seg;
-                w.next(a, n);
+                w.next(a, up->nt, n);
             }
             if (leader) mma_commit(mma_done);  // also after an abort: no product may write TMEM when it is freed
             __syncwarp();
@@ -307,9 +338,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int c = t & 3;
             uint32_t seg = 0;
             bool ok = true;
-            while (w.left > 0 && ok) {
+            while (w.more() && ok) {
                 const RowsUnit u = rows_unit(a, w.unit);
-                const int n = w.part(u), rows = u.n * a.group;
+                const int n = w.part(u.nt), rows = u.n * a.group;
                 const bool many = a.prefix && u.m0 >= 0;
                 const int64_t row0 = a.prefix ? u.b : (int64_t)u.row0 + u.m0;
                 const T *q = static_cast<const T *>(a.q) + (int64_t)w.g * a.group * D + 8 * c;
@@ -352,12 +383,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mbar_arrive(q_full(1));
                 }
                 ++seg;
-                w.next(a, n);
+                w.next(a, u.nt, n);
             }
         }
     } else {
         // ---------------- weights and outputs: thread r of a warpgroup holds row r of its row tile
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int X = warp >> 2, wq = warp & 3, row_in = wq * 32 + lane;
         const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
         const uint32_t tS = tmem + 128 * X + lane_off, tO = tmem + 256 + lane_off;
@@ -365,46 +396,58 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int n_pre = __ldcg(&a.head->n_pre);
         uint32_t ns = 0, np = 0;  // scores and weights so far
         bool ok = true;
-        while (w.left > 0) {
-            const RowsUnit u = rows_unit(a, w.unit);
-            const int n = w.part(u), rows = u.n * a.group;
-            const bool pair = rows > tile_rows;
-            const int r = pair ? X * tile_rows + row_in : row_in;
-            const int mine = pair && X == 1 ? rows - tile_rows : min(rows, tile_rows);  // rows of this tile
-            RowsRow row = rows_row<D>(a, u, w.g, r);
-            if (row_in >= mine) row.seq = -1;
-            if (row.seq < 0) row.pos = nullptr;
-            const bool busy = wq * 32 < mine;
-            const int steps = pair ? n : X == 0 ? (n + 1) / 2 : n / 2;
+        while (w.more()) {
+            // (the unit is looked up where it is needed: kept, it would push scores out of the registers)
+            const RowsUnit *up = a.units + w.unit;
+            int n, r, seq, hi, wlo, steps;
+            bool pair, busy;
+            {
+                const RowsUnit u = rows_unit(a, w.unit);
+                n = w.part(u.nt);
+                const int rows = u.n * a.group;
+                pair = rows > tile_rows;
+                r = pair ? X * tile_rows + row_in : row_in;
+                const int mine = pair && X == 1 ? rows - tile_rows : min(rows, tile_rows);  // rows of this tile
+                const RowsRow row = rows_row<D>(a, u, w.g, r);
+                seq = row_in < mine ? row.seq : -1;
+                hi = row.hi;
+                wlo = row.wlo;
+                busy = wq * 32 < mine;
+                steps = pair ? n : X == 0 ? (n + 1) / 2 : n / 2;
+            }
             float m = -INFINITY, l = 0.f;
             for (int s = 0; s < steps; ++s) {
-                const int t0 = rows_tile(u, w.j + (pair ? s : 2 * s + X)) * kRowsTile;
-                const bool full = row.seq < 0 || (t0 >= row.lo && t0 + 127 <= row.hi &&
-                                                  (t0 >= row.wlo || t0 + 127 < row.sh));
-                const bool masked = __any_sync(0xffffffffu, !full || row.pos);
                 uint32_t see[4];
-                if (masked && busy) {
+                bool masked;
+                {
+                    const int j = w.j + (pair ? s : 2 * s + X), n_a = up->n_a;
+                    const int t0 = (j < n_a ? up->t_a + j : up->t_w + j - n_a) * kRowsTile;
+                    const int lo = up->lo, S0 = up->S0, sh = a.prefix ? lo : S0 + a.sinks;
+                    const bool full = seq < 0 || (t0 >= lo && t0 + 127 <= hi && (t0 >= wlo || t0 + 127 < sh));
+                    masked = __any_sync(0xffffffffu, !full) || a.pos;
+                    if (masked && busy) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        see[k] = row.seq < 0 ? 0u
-                                             : range_bits(max(row.lo, row.wlo) - t0, row.hi - t0, k) |
-                                                   range_bits(row.lo - t0, min(row.sh - 1, row.hi) - t0, k);
-                    if (a.pos) {
-                        // liveness, one sequence of the warp's rows at a time: a lane looks up every 32nd slot
-                        const int rw = pair ? X * tile_rows + wq * 32 : wq * 32;
-                        const bool many = a.prefix && u.m0 >= 0;
-                        const int m0 = many ? rw / a.group : 0, m1 = many ? min(rw + 31, rows - 1) / a.group : 0;
-                        for (int k = m0; k <= m1; ++k) {
-                            const int from = many ? max(k * a.group - rw, 0) : 0;
-                            const int32_t *pos = reinterpret_cast<const int32_t *>(
-                                __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row.pos), from));
-                            const bool me = !many || r / a.group == k;
+                        for (int k = 0; k < 4; ++k)
+                            see[k] = seq < 0 ? 0u
+                                             : range_bits(max(lo, wlo) - t0, hi - t0, k) |
+                                                   range_bits(lo - t0, min(sh - 1, hi) - t0, k);
+                        if (a.pos) {
+                            // liveness, one sequence of the warp's rows at a time: a lane looks up every 32nd slot
+                            const int rw = r - lane, rows = up->n * a.group, end = up->hi;
+                            const bool many = a.prefix && up->m0 >= 0;
+                            const int m0 = many ? rw / a.group : 0, m1 = many ? min(rw + 31, rows - 1) / a.group : 0;
+                            for (int k = m0; k <= m1; ++k) {
+                                const int who = __shfl_sync(0xffffffffu, seq, many ? max(k * a.group - rw, 0) : 0);
+                                const int32_t *pos =
+                                    a.pos + ((int64_t)max(who, 0) * a.rows_per_seq + (a.rows_per_seq == 1 ? 0 : w.g)) * a.cap;
+                                const bool me = !many || r / a.group == k;
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                const int slot = t0 + 32 * x + lane;
-                                const bool live = pos && slot >= u.lo && slot < u.hi && __ldg(pos + (slot - u.S0)) >= 0;
-                                const uint32_t bits = __ballot_sync(0xffffffffu, live);
-                                if (me) see[x] &= bits;
+                                for (int x = 0; x < 4; ++x) {
+                                    const int slot = t0 + 32 * x + lane;
+                                    const bool live = who >= 0 && slot >= lo && slot < end && __ldg(pos + (slot - S0)) >= 0;
+                                    const uint32_t bits = __ballot_sync(0xffffffffu, live);
+                                    if (me) see[x] &= bits;
+                                }
                             }
                         }
                     }
@@ -414,26 +457,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ++ns;
                 if (ok && busy) {
                     fence_after_sync();
-                    // S is read twice, 32 columns at a time, so that a row's 128 scores never are in registers
-                    // together (that spilled, and cost more than the second read)
+                    uint32_t v[128];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, v + 32 * c);
                     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    uint32_t va[32], vb[32];
-                    tmem_ld32(tS, va);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t *v = c & 1 ? vb : va;
-                        tmem_wait_ld(v);
-                        if (c < 3) tmem_ld32(tS + 32 * (c + 1), c & 1 ? va : vb);
-                        if (masked) {
+                    for (int c = 0; c < 4; ++c) tmem_wait_ld(v + 32 * c);
+                    if (masked) {
 #pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                if (!((see[c] >> k) & 1u)) v[k] = 0xff800000u;
-                        }
-#pragma unroll
-                        for (int k = 0; k < 32; k += 2)
-                            mx[(k >> 1) & 3] = fmaxf(fmaxf(mx[(k >> 1) & 3], __uint_as_float(v[k])), __uint_as_float(v[k + 1]));
+                        for (int k = 0; k < 128; ++k)
+                            if (!((see[k >> 5] >> (k & 31)) & 1u)) v[k] = 0xff800000u;
                     }
-                    tmem_ld32(tS, va);  // (again)
+#pragma unroll
+                    for (int k = 0; k < 128; k += 2)
+                        mx[(k >> 1) & 3] = fmaxf(fmaxf(mx[(k >> 1) & 3], __uint_as_float(v[k])), __uint_as_float(v[k + 1]));
                     const float top = __fmul_rn(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), a.scale_log2);
                     if (s == 0) {
                         m = top;
@@ -460,40 +497,40 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                     const float ref = m == -INFINITY ? 0.f : m;
-                    // weights of 32 slots take 16 columns: they never reach scores that are still to be read
                     const float2 sc2 = make_float2(a.scale_log2, a.scale_log2), ref2 = make_float2(-ref, -ref);
                     float2 sum[4] = {};
+                    // (in place: the weights of slots 2 k and 2 k + 1 take register k)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        uint32_t *v = c & 1 ? vb : va;
-                        tmem_wait_ld(v);
-                        if (c < 3) tmem_ld32(tS + 32 * (c + 1), c & 1 ? va : vb);
-                        if (masked) {
 #pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                if (!((see[c] >> k) & 1u)) v[k] = 0xff800000u;
-                        }
-                        uint32_t p[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
+                        for (int k = 16 * c; k < 16 * c + 16; ++k) {
                             float2 x = fma2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), sc2, ref2);
                             x.x = ex2(x.x);
                             x.y = ex2(x.y);
                             sum[k & 3] = add2(sum[k & 3], x);
                             const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
-                            p[k] = *reinterpret_cast<const uint32_t *>(&h);
+                            v[k] = *reinterpret_cast<const uint32_t *>(&h);
                         }
-                        tmem_st16(tS + 16 * c, p);
+                        tmem_st16(tS + 16 * c, v + 16 * c);
+                        if (c == 1) {  // the first 64 slots' weights go ahead
+                            tmem_wait_st();
+                            fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(p_half(X));
+                        }
                     }
                     const float2 s01 = add2(sum[0], sum[1]), s23 = add2(sum[2], sum[3]);
                     l += (s01.x + s01.y) + (s23.x + s23.y);
                     tmem_wait_st();
+                } else if (lane == 0) {
+                    mbar_arrive(p_half(X));
                 }
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full(X));
                 ++np;
             }
+            const RowsUnit u = rows_unit(a, w.unit);
             if (steps > 0) {
                 if (ok) ok = bar_wait(o_full(X), (np - 1) & 1, abort_flag);
                 ok = __all_sync(0xffffffffu, ok);
@@ -515,6 +552,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             if (ok && busy && (pair || X == 0)) {
+                RowsRow row = rows_row<D>(a, u, w.g, r);
+                row.seq = seq;
                 const bool begins = w.j == 0, whole = begins && n == u.nt && !a.prefix;
                 RowsHead h;
                 h.n_pre = n_pre;
@@ -522,12 +561,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool joined = !pair && n > 1;
                 const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
                 bool bad = false;
-#pragma unroll
+                unsigned char *stage = sm + C::kOffOut + warp * 4096;
+#pragma unroll 1
                 for (int k = 0; k < D; k += 32) {
                     uint32_t o[32];
-                    float y[32];
                     tmem_ld32(tO + 128 * X + k, o);
                     tmem_wait_ld(o);
+                    float y[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) y[i] = __uint_as_float(o[i]);
                     if (joined) {
@@ -541,29 +581,41 @@ __global__ void __launch_bounds__(kThreads, 1)
                         bad |= !(fabsf(y[i]) < INFINITY);
                         y[i] *= inv;
                     }
-                    if (row.seq >= 0) {
-                        if (whole) {
-                            T *d = static_cast<T *>(a.out) + row.out + k;
+                    if (whole) {
+                        // 64 channels of 32 rows at a time through shared memory: eight lanes store a row's 128
+                        // bytes, where a lane a row would touch 32 lines with every store
+                        if (k % 64 == 0) __syncwarp();
 #pragma unroll
-                            for (int i = 0; i < 32; i += 8) {
-                                uint32_t q[4];
+                        for (int i = 0; i < 32; i += 8) {
+                            uint32_t q[4];
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const __nv_bfloat162 b2 = __floats2bfloat162_rn(y[i + 2 * e], y[i + 2 * e + 1]);
-                                    q[e] = *reinterpret_cast<const uint32_t *>(&b2);
-                                }
-                                *reinterpret_cast<uint4 *>(d + i) = make_uint4(q[0], q[1], q[2], q[3]);
+                            for (int e = 0; e < 4; ++e) {
+                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(y[i + 2 * e], y[i + 2 * e + 1]);
+                                q[e] = *reinterpret_cast<const uint32_t *>(&b2);
                             }
-                        } else {
-                            const int step = rows_part_step(a, u);
-                            float *d = rows_part_o<D>(a, u, slot, r) + (int64_t)(k / 4) * step;
-#pragma unroll
-                            for (int i = 0; i < 32; i += 4) store4(d + (i / 4) * step, y[i], y[i + 1], y[i + 2], y[i + 3]);
+                            *reinterpret_cast<uint4 *>(stage + sw128(lane, k % 64 + i)) = make_uint4(q[0], q[1], q[2], q[3]);
                         }
+                        if (k % 64 == 32) {
+                            __syncwarp();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const int rr = 4 * i + lane / 8, c = lane % 8 * 8;
+                                const int64_t at = __shfl_sync(0xffffffffu, row.out, rr);
+                                if (__shfl_sync(0xffffffffu, row.seq, rr) >= 0)
+                                    *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + at + k - 32 + c) =
+                                        *reinterpret_cast<const uint4 *>(stage + sw128(rr, c));
+                            }
+                        }
+                    } else if (row.seq >= 0) {
+                        const int step = rows_part_step(a, u);
+                        float *d = rows_part_o<D>(a, u, slot, r) + (int64_t)(k / 4) * step;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) store4(d + (i / 4) * step, y[i], y[i + 1], y[i + 2], y[i + 3]);
                     }
                 }
                 if (row.seq >= 0 && !whole) rows_store_ml(a, u, slot, r, m, l);
                 // (see rows_redo: V rows that are not finite and that the row does not see)
+                __syncwarp();  // (it stores over what another lane did)
                 unsigned redo = __ballot_sync(0xffffffffu, bad && row.seq >= 0 && !isnan(l));
                 while (redo) {
                     const int i = __ffs(redo) - 1;
@@ -576,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 fence_after_sync();
             }
-            w.next(a, n);
+            w.next(a, u.nt, n);
         }
     }
     fence_before_sync();
