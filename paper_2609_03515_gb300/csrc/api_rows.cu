@@ -47,8 +47,9 @@ ikv_status check_window(const ikv_shape *s, const ikv_cache *c, const ikv_window
 
 // The arguments of a call but for its pointers to q and results, and its workspace: *bytes of it, at ws
 // if there is one.
+// (score: the call's score pass needs its own; sizes are with it)
 RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, const ikv_window *w, void *ws,
-                   size_t *bytes) {
+                   size_t *bytes, bool score = true) {
     RowsArgs a{};
     a.k = c->k;
     a.v = c->v;
@@ -68,6 +69,7 @@ RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, 
     const int n = p ? s->batch : w->max_count;
     const int most = tc ? 2 * (128 / a.group) : kRowsSimt / a.group;  // (tensor cores: two row tiles)
     a.unit_n = most;
+    a.tile_n = tc ? 128 / a.group : most;
     a.rows_cap = (n < most ? n : most) * a.group;
     int64_t units;
     if (w) {
@@ -96,6 +98,21 @@ RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, 
     take(a.head, 1);
     take(a.start, a.ctas);
     take(a.units, units);
+    if (a.pos) {
+        a.live_words = (a.cap + 31) / 32;
+        take(a.live, (size_t)a.batch * a.rows_per_seq * a.live_words);
+    }
+    if (tc && p) {
+        // (64 columns a thread: an item's members, half of them each, are 2 (64 / G))
+        a.item_n = 2 * (64 / a.group);
+        a.item_subs = a.rows_per_seq > 1 ? s->kv_heads : 1;
+        take(a.items, a.ctas);
+        take(a.icum, units);
+        if (!score) {
+            a.items = nullptr;
+            a.icum = nullptr;
+        }
+    }
     const size_t pre = p ? (size_t)(p->n_groups + s->batch / a.unit_n) * s->kv_heads + a.ctas : 2 * (size_t)a.ctas;
     take(a.part_ml, pre * a.rows_cap);
     take(a.part_o, pre * a.rows_cap * s->head_dim);
@@ -153,7 +170,7 @@ ikv_status ikv_prefix_attend_score(const ikv_shape *shape, const ikv_cache *cach
     ikv_status e = check_prefix(shape, cache, prefix);
     if (e) return e;
     size_t need = 0;
-    RowsArgs a = rows_args(shape, cache, prefix, nullptr, ws, &need);
+    RowsArgs a = rows_args(shape, cache, prefix, nullptr, ws, &need, score || ema);
     if ((e = check_call(shape, layer, q, out, ws, ws_bytes, need))) return e;
     if (ema && !(alpha >= 0.f && alpha <= 1.f)) return report(IKV_ERR_ARG, "alpha must be in [0, 1]");
     a.layer = layer;
@@ -163,7 +180,9 @@ ikv_status ikv_prefix_attend_score(const ikv_shape *shape, const ikv_cache *cach
     if ((e = attend(a, shape, cache, stream))) return e;
     if (!score && !ema) return IKV_OK;
     const RowsScoreArgs sc{alpha, score, ema, cache->max_len};
-    IKV_TRY_CUDA(launch_rows_score(a, sc, shape->dtype, shape->head_dim, stream), "row score launch");
+    IKV_TRY_CUDA(a.items ? launch_rows_score_tc(a, sc, shape->head_dim, stream)
+                         : launch_rows_score(a, sc, shape->dtype, shape->head_dim, stream),
+                 "row score launch");
     return IKV_OK;
 }
 

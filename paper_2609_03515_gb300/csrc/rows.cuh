@@ -33,9 +33,9 @@ struct RowsUnit {                   // 64 bytes
     int64_t cum;                    // cost of all earlier units, for all KV heads
 };
 
-// Cost is counted in tiles; a pair costs kRowsExtra besides its own, for its first products, which nothing
-// overlaps, and its output.
-constexpr int kRowsExtra = 2;
+// Cost is counted in tiles.  Besides its own a pair costs one or two for its first products, which nothing
+// overlaps, and its output: two where its rows fill two row tiles of the tensor-core kernel.
+constexpr int kRowsOne = 1, kRowsTwo = 2;
 
 struct RowsHead {
     int64_t total, per;             // cost in all, of a CTA's share
@@ -43,6 +43,11 @@ struct RowsHead {
 };
 struct RowsStart {                  // where a CTA's share begins (at cost `at` of pair (unit, g)), and its cost
     int32_t unit, g, at, n;
+};
+// The score pass on the tensor cores: an item is a tile of a unit for up to 128 of its rows, and, with a utility
+// row a KV head, one of those; item sub * nt + j of a unit is tile j of its sub-th such set.
+struct RowsItems {                  // where a CTA's begin, and how many it has
+    int32_t unit, sub, j, n;
 };
 struct RowsSeq {                    // prefix: what sequence b's rows are made from
     int32_t pre, entry;             // its group's unit that holds it (-1: none), its member number there
@@ -56,12 +61,14 @@ struct RowsArgs {
     int32_t layer;
     const int32_t *len;             // [batch]
     const int32_t *pos;             // [rows][cap], -1 at dead slots, or null
+    uint32_t *live;                 // with pos: [rows][live_words] workspace, bit j of a row: slot j is live
+    int32_t live_words;
     int32_t rows_per_seq, cap, batch, q_heads, group;
     float scale_log2;               // log2(e) / sqrt(d)
     const void *q;
     void *out;
     int64_t q_stride, out_stride;   // elements from a token's (sequence's) heads to the next
-    int32_t unit_n;                 // most tokens or members of a unit
+    int32_t unit_n, tile_n;         // most tokens or members of a unit, of a row tile of it
     // window
     int32_t window, sinks;          // window in [1, 2^30], sinks in [0, 2^30)
     const int32_t *row0, *count;
@@ -73,6 +80,10 @@ struct RowsArgs {
     // workspace
     RowsHead *head;
     RowsStart *start;               // [ctas]
+    RowsItems *items;               // [ctas] of the tensor-core score pass, or null
+    int64_t *icum;                  // with items: items of all earlier units
+    int32_t item_n, item_subs;      // members of an item, and how many times its tiles are gone through (1, or the KV
+                                    // heads)
     RowsUnit *units;
     int32_t *owner;                 // prefix: [batch] first entry that names the sequence
     int32_t *vm;                    // prefix: [batch] the entries, -1 where one is left out
@@ -101,26 +112,27 @@ __device__ __forceinline__ int64_t rows_slot(const RowsArgs &a, const RowsHead &
 // The tile of a unit
 __device__ __forceinline__ int rows_tile(const RowsUnit &u, int i) { return i < u.n_a ? u.t_a + i : u.t_w + i - u.n_a; }
 
-// The parts of a share, in turn.  The first kRowsExtra of a pair's cost lie in front of its tiles; a border
-// in them cuts nothing.
+__device__ __forceinline__ int rows_extra(const RowsArgs &a, int n) { return n > a.tile_n ? kRowsTwo : kRowsOne; }
+
+// The parts of a share, in turn.  A pair's extra cost lies in front of its tiles; a border in it cuts nothing.
 struct RowsWalk {
-    int32_t unit, g, j, left;       // the next part begins at tile j of pair (unit, g)
-    int32_t skip;                   // cost in front of tile j that is this share's
+    int32_t unit, g, at, left;      // the share goes on at cost `at` of pair (unit, g)
     __device__ __forceinline__ void begin(const RowsArgs &a, int cta) {
         const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.start) + cta);
         unit = s.x;
         g = s.y;
-        j = max(s.z - kRowsExtra, 0);
-        skip = max(kRowsExtra - s.z, 0);
+        at = s.z;
         left = s.w;
     }
-    // whether there is a part, and its tiles, given its unit's
-    __device__ __forceinline__ bool more() const { return left > skip; }
-    __device__ __forceinline__ int part(int nt) const { return min(nt - j, left - skip); }
-    __device__ __forceinline__ void next(const RowsArgs &a, int nt, int n) {
-        left -= skip + n;
-        j = 0;
-        skip = kRowsExtra;
+    // The next part: from tile j, n tiles (none: the share is done), of a unit of nt tiles and un tokens
+    __device__ __forceinline__ int first(const RowsArgs &a, int un) const { return max(at - rows_extra(a, un), 0); }
+    __device__ __forceinline__ int part(const RowsArgs &a, int nt, int un) const {
+        const int e = rows_extra(a, un);
+        return min(nt - max(at - e, 0), left - max(e - at, 0));
+    }
+    __device__ __forceinline__ void next(const RowsArgs &a, int nt, int un) {
+        left -= nt + rows_extra(a, un) - at;
+        at = 0;
         if (++g == a.pv.kv_heads) {
             g = 0;
             ++unit;
@@ -180,6 +192,9 @@ cudaError_t launch_rows_tc(const RowsArgs &a, int head_dim, cudaStream_t st);
 cudaError_t read_clear_rows_tc_error(unsigned int *v);
 cudaError_t launch_rows_merge(const RowsArgs &a, int dtype, int head_dim, cudaStream_t st);
 int rows_simt_ctas_per_sm(int head_dim);
+// the score pass on the tensor cores
+cudaError_t launch_rows_score_tc(const RowsArgs &a, const struct RowsScoreArgs &s, int head_dim, cudaStream_t st);
+cudaError_t read_clear_rows_score_error(unsigned int *v);
 constexpr int kRowsSimt = 64;       // rows of a unit of the kernel without tensor cores
 
 // prefix: scores and utilities from K once more, with the rows' maxima and sums known

@@ -88,11 +88,12 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_window_kernel(const 
     const int c = blockIdx.x;
     RowsWalk w;
     w.begin(a, c);
-    if (w.left == 0 || w.j == 0) return;
+    if (w.left == 0 || w.at == 0) return;
     const int64_t per = __ldcg(&a.head->per);
-    if (w.j > per) return;  // (the share in front of this one begins behind the pair's first tile)
     const RowsUnit u = rows_unit(a, w.unit);
-    const int n = 1 + (int)((u.nt - w.j + per - 1) / per);  // parts: share c - 1's and those behind
+    const int j = w.first(a, u.n);
+    if (j == 0 || j > per) return;  // (beyond: the share in front of this one begins behind the pair's first tile)
+    const int n = 1 + (int)((u.nt - j + per - 1) / per);  // parts: share c - 1's and those behind
     const int rows = u.n * a.group;
     auto slot = [&](int i) { return i == 0 ? 2 * (int64_t)(c - 1) + 1 : 2 * (int64_t)(c + i - 1); };
     for (int r0 = blockIdx.y * kMergeRows; r0 < rows; r0 += gridDim.y * kMergeRows) {
@@ -115,8 +116,8 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_prefix_kernel(const 
     int64_t slot_p = 0, slot_o = 0;
     int np = 0, no = 0;
     auto parts = [&](int unit, int64_t pair0, int64_t &slot) {  // of pair (unit, g); slot: its first part's
-        const int nt = __ldcg(&a.units[unit].nt);
-        const int64_t x0 = __ldcg(&a.units[unit].cum) + (int64_t)g * (nt + kRowsExtra) + kRowsExtra;
+        const int nt = __ldcg(&a.units[unit].nt), e = rows_extra(a, __ldcg(&a.units[unit].n));
+        const int64_t x0 = __ldcg(&a.units[unit].cum) + (int64_t)g * (nt + e) + e;
         const int64_t c0 = x0 / per;
         slot = pair0 + g + c0;
         return (int)((x0 + nt - 1) / per - c0) + 1;

@@ -14,46 +14,33 @@ constexpr int kPlanCum = 1024;      // units whose offsets stay in shared memory
 
 constexpr int kPlanSmall = 1024;    // sequences and groups whose tables stay there
 
-struct Scan {
-    int64_t sum[kPlanThreads / 32];
-    int32_t cnt[kPlanThreads / 32];
+struct Sums {
+    int32_t n;                      // units
+    int64_t cost, items;            // of the attention, of the score pass
+    __device__ __forceinline__ Sums operator+(const Sums &o) const { return {n + o.n, cost + o.cost, items + o.items}; }
 };
 
-// Exclusive sums of (n, tiles) over the CTA's threads; the totals are added to the carries.
-__device__ __forceinline__ void scan(Scan &sc, int n, int64_t tiles, int &n_carry, int64_t &t_carry, int &n_at,
-                                     int64_t &t_at) {
+// Exclusive sums over the CTA's threads, on top of `carry`, which the totals are added to.
+__device__ __forceinline__ Sums scan(Sums *sc, const Sums &x, Sums &carry) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    int a = n;
-    int64_t b = tiles;
+    Sums a = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, a, o);
-        const int64_t y = __shfl_up_sync(0xffffffffu, b, o);
-        if (lane >= o) {
-            a += x;
-            b += y;
-        }
+        const Sums y{__shfl_up_sync(0xffffffffu, a.n, o), __shfl_up_sync(0xffffffffu, a.cost, o),
+                     __shfl_up_sync(0xffffffffu, a.items, o)};
+        if (lane >= o) a = a + y;
     }
-    if (lane == 31) {
-        sc.cnt[warp] = a;
-        sc.sum[warp] = b;
-    }
+    if (lane == 31) sc[warp] = a;
     __syncthreads();
-    int na = 0, nall = 0;
-    int64_t ta = 0, tall = 0;
+    Sums before{0, 0, 0}, all{0, 0, 0};
     for (int w = 0; w < warps; ++w) {
-        if (w == warp) {
-            na = nall;
-            ta = tall;
-        }
-        nall += sc.cnt[w];
-        tall += sc.sum[w];
+        if (w == warp) before = all;
+        all = all + sc[w];
     }
     __syncthreads();
-    n_at = n_carry + na + a - n;
-    t_at = t_carry + ta + b - tiles;
-    n_carry += nall;
-    t_carry += tall;
+    const Sums at = carry + before;
+    carry = carry + all;
+    return {at.n + a.n - x.n, at.cost + a.cost - x.cost, at.items + a.items - x.items};
 }
 
 __device__ __forceinline__ int clamp_start(const RowsArgs &a, int b) {
@@ -74,8 +61,13 @@ __device__ __forceinline__ void whole_run(RowsUnit &u, int lo, int hi) {
     u.row0 = 0;
 }
 
-__device__ __forceinline__ int64_t cost(const RowsUnit &u, int kv_heads) {
-    return u.nt > 0 ? (int64_t)(u.nt + kRowsExtra) * kv_heads : 0;
+__device__ __forceinline__ int64_t cost(const RowsArgs &a, const RowsUnit &u) {
+    return u.nt > 0 ? (int64_t)(u.nt + rows_extra(a, u.n)) * a.pv.kv_heads : 0;
+}
+
+// tiles of the score pass: each for every `item_n` members (and, with a utility row a KV head, for each of those)
+__device__ __forceinline__ int64_t items(const RowsArgs &a, const RowsUnit &u) {
+    return a.items && u.nt > 0 ? (int64_t)u.nt * a.item_subs * ((u.n + a.item_n - 1) / a.item_n) : 0;
 }
 
 __device__ __forceinline__ void store_unit(const RowsArgs &a, int at, const RowsUnit &u) {
@@ -85,14 +77,50 @@ __device__ __forceinline__ void store_unit(const RowsArgs &a, int at, const Rows
     for (int i = 0; i < 4; ++i) d[i] = s[i];
 }
 
+// CTAs behind the first: the live slots of every utility row as bits, 1024 slots a warp at a time
+__device__ __forceinline__ void live_bits(const RowsArgs &a) {
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int chunks = (a.live_words + 31) / 32;
+    const int64_t all = (int64_t)a.batch * a.rows_per_seq * chunks;
+    for (int64_t i = (int64_t)(blockIdx.x - 1) * warps + (threadIdx.x >> 5); i < all; i += (int64_t)(gridDim.x - 1) * warps) {
+        const int64_t row = i / chunks;
+        const int w0 = (int)(i % chunks) * 32, b = (int)(row / a.rows_per_seq);
+        const int len = clamp_len(a, b, clamp_start(a, b));
+        if (w0 * 32 >= len) continue;
+        const int32_t *pos = a.pos + row * a.cap + w0 * 32;
+        const int n = min(len - w0 * 32, 1024);
+        uint32_t mine = 0;
+#pragma unroll 8
+        for (int w = 0; w < 32; ++w) {
+            const int j = 32 * w + lane;
+            const uint32_t bits = __ballot_sync(0xffffffffu, j < n && __ldg(pos + j) >= 0);
+            if (w == lane) mine = bits;
+        }
+        if (w0 + lane < a.live_words) a.live[row * a.live_words + w0 + lane] = mine;
+    }
+}
+
 __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs a) {
     pdl_wait();
-    __shared__ Scan sc;
-    __shared__ int64_t cums[kPlanCum];
+    if (blockIdx.x > 0) {
+        live_bits(a);
+        return;
+    }
+    __shared__ Sums sc[kPlanThreads / 32];
+    __shared__ int64_t cums[kPlanCum], icums[kPlanCum];
     __shared__ int32_t small_tab[6 * kPlanSmall];
-    const int tid = threadIdx.x, nthr = blockDim.x, hk = a.pv.kv_heads;
-    int units = 0, n_pre = 0;
-    int64_t tiles = 0;  // (their cost)
+    const int tid = threadIdx.x, nthr = blockDim.x;
+    int n_pre = 0;
+    Sums sum{0, 0, 0};
+    auto put = [&](RowsUnit u, const Sums &at) {  // unit number at.n
+        u.cum = at.cost;
+        store_unit(a, at.n, u);
+        if (a.icum) a.icum[at.n] = at.items;
+        if (at.n < kPlanCum) {
+            cums[at.n] = at.cost;
+            icums[at.n] = at.items;
+        }
+    };
     if (!a.prefix) {
         const int64_t all = (int64_t)a.batch * a.seq_units;
         for (int64_t i0 = 0; i0 < all; i0 += nthr) {
@@ -124,12 +152,8 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
                     }
                 }
             }
-            int at;
-            scan(sc, u.nt > 0 ? 1 : 0, cost(u, hk), units, tiles, at, u.cum);
-            if (u.nt > 0) {
-                store_unit(a, at, u);
-                if (at < kPlanCum) cums[at] = u.cum;
-            }
+            const Sums at = scan(sc, {u.nt > 0 ? 1 : 0, cost(a, u), 0}, sum);
+            if (u.nt > 0) put(u, at);
         }
     } else {
         // (small batches keep the tables in shared memory: the chain of their look-ups is the time)
@@ -208,21 +232,24 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
                 n = (e1 - e0 + a.unit_n - 1) / a.unit_n;
                 u.b = glead[i];
                 u.S0 = clamp_start(a, u.b);
+                u.n = min(a.unit_n, e1 - e0);
                 whole_run(u, u.S0, u.S0 + gp[i]);
             }
-            int at;
-            int64_t cum;
-            scan(sc, n, n * cost(u, hk), units, tiles, at, cum);
-            if (i < n_groups) gunit[i] = at;
+            // (all but a group's last unit are full)
+            const int most = u.n, rest = n > 0 ? e1 - e0 - (n - 1) * most : 0;
+            RowsUnit last = u;
+            last.n = rest;
+            Sums at = scan(sc, {n, n > 0 ? (n - 1) * cost(a, u) + cost(a, last) : 0,
+                                n > 0 ? (n - 1) * items(a, u) + items(a, last) : 0}, sum);
+            if (i < n_groups) gunit[i] = at.n;
             for (int k = 0; k < n; ++k) {
-                u.m0 = e0 + k * a.unit_n;
-                u.n = min(a.unit_n, e1 - u.m0);
-                u.cum = cum + k * cost(u, hk);
-                store_unit(a, at + k, u);
-                if (at + k < kPlanCum) cums[at + k] = u.cum;
+                u.m0 = e0 + k * most;
+                u.n = k == n - 1 ? rest : most;
+                put(u, at);
+                at = at + Sums{1, cost(a, u), items(a, u)};
             }
         }
-        n_pre = units;
+        n_pre = sum.n;
         __syncthreads();
         for (int b0 = 0; b0 < a.batch; b0 += nthr) {
             const int b = b0 + tid;
@@ -245,45 +272,61 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
                 u.S0 = clamp_start(a, b);
                 whole_run(u, u.S0 + s.len, u.S0 + clamp_len(a, b, u.S0));
             }
-            int at;
-            scan(sc, u.nt > 0 ? 1 : 0, cost(u, hk), units, tiles, at, u.cum);
+            const Sums at = scan(sc, {u.nt > 0 ? 1 : 0, cost(a, u), items(a, u)}, sum);
             if (u.nt > 0) {
-                store_unit(a, at, u);
-                if (at < kPlanCum) cums[at] = u.cum;
-                s.own = at;
+                put(u, at);
+                s.own = at.n;
             }
             if (b < a.batch) *reinterpret_cast<int4 *>(a.seq + b) = *reinterpret_cast<int4 *>(&s);
         }
     }
     __syncthreads();
-    int64_t per = (tiles + a.ctas - 1) / a.ctas;
+    int64_t per = (sum.cost + a.ctas - 1) / a.ctas;
     if (per < 1) per = 1;
     if (tid == 0) {
-        a.head->total = tiles;
+        a.head->total = sum.cost;
         a.head->per = per;
-        a.head->n_units = units;
+        a.head->n_units = sum.n;
         a.head->n_pre = n_pre;
     }
+    // the last unit that begins at or before x
+    auto find = [&](const int64_t *small, auto big, int64_t x) {
+        int lo = 0, hi = sum.n;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if ((mid < kPlanCum ? small[mid] : big(mid)) <= x)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        return lo;
+    };
     for (int c = tid; c < a.ctas; c += nthr) {
         RowsStart s{0, 0, 0, 0};
         const int64_t x = (int64_t)c * per;
-        if (x < tiles) {
-            int lo = 0, hi = units;  // the last unit that begins at or before x
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                if ((mid < kPlanCum ? cums[mid] : __ldcg(&a.units[mid].cum)) <= x)
-                    lo = mid;
-                else
-                    hi = mid;
-            }
-            const int each = __ldcg(&a.units[lo].nt) + kRowsExtra;
-            const int64_t r = x - (lo < kPlanCum ? cums[lo] : __ldcg(&a.units[lo].cum));
-            s.unit = lo;
+        if (x < sum.cost) {
+            auto big = [&](int i) { return __ldcg(&a.units[i].cum); };
+            s.unit = find(cums, big, x);
+            const int each = __ldcg(&a.units[s.unit].nt) + rows_extra(a, __ldcg(&a.units[s.unit].n));
+            const int64_t r = x - (s.unit < kPlanCum ? cums[s.unit] : big(s.unit));
             s.g = (int32_t)(r / each);
             s.at = (int32_t)(r % each);
-            s.n = (int32_t)min(per, tiles - x);
+            s.n = (int32_t)min(per, sum.cost - x);
         }
         *reinterpret_cast<int4 *>(a.start + c) = *reinterpret_cast<int4 *>(&s);
+        if (!a.items) continue;
+        RowsItems t{0, 0, 0, 0};
+        const int64_t many = (sum.items + a.ctas - 1) / a.ctas, y = c * many;
+        if (y < sum.items) {
+            auto big = [&](int i) { return __ldcg(a.icum + i); };
+            t.unit = find(icums, big, y);
+            const int nt = __ldcg(&a.units[t.unit].nt);
+            const int64_t r = y - (t.unit < kPlanCum ? icums[t.unit] : big(t.unit));
+            t.sub = (int32_t)(r / nt);
+            t.j = (int32_t)(r % nt);
+            t.n = (int32_t)min(many, sum.items - y);
+        }
+        *reinterpret_cast<int4 *>(a.items + c) = *reinterpret_cast<int4 *>(&t);
     }
 }
 
@@ -293,7 +336,13 @@ cudaError_t launch_rows_plan(const RowsArgs &a, cudaStream_t st) {
     const int64_t most = a.prefix ? (int64_t)(a.batch > a.n_groups ? a.batch : a.n_groups) : (int64_t)a.batch * a.seq_units;
     int threads = 128;
     while (threads < kPlanThreads && threads < most) threads *= 2;
-    const cudaError_t e = launch_k(rows_plan_kernel, dim3(1), dim3(threads), 0, st, a);
+    int ctas = 1;
+    if (a.live) {
+        const int64_t warps = (int64_t)a.batch * a.rows_per_seq * ((a.live_words + 31) / 32);
+        const int64_t n = (warps + threads / 32 - 1) / (threads / 32);
+        ctas += (int)(n < 4 * a.ctas ? n : 4 * a.ctas);
+    }
+    const cudaError_t e = launch_k(rows_plan_kernel, dim3(ctas), dim3(threads), 0, st, a);
     note_launch();
     return e;
 }
@@ -302,9 +351,10 @@ cudaError_t read_clear_rows_error(unsigned int *v) {
     unsigned int z = 0;
     cudaError_t e = cudaMemcpyFromSymbol(v, g_rows_error, sizeof(*v));
     if (e == cudaSuccess && *v) e = cudaMemcpyToSymbol(g_rows_error, &z, sizeof(z));
-    unsigned int tc = 0;
+    unsigned int tc = 0, sc = 0;
     if (e == cudaSuccess) e = read_clear_rows_tc_error(&tc);
-    *v |= tc;
+    if (e == cudaSuccess) e = read_clear_rows_score_error(&sc);
+    *v |= tc | sc;
     return e;
 }
 

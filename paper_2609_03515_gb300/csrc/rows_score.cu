@@ -1,0 +1,312 @@
+// The score pass of the shared-prefix decode on the tensor cores (bf16): K is read once more, with each row's
+// maximum M and sum of weights W known from the merge,
+//     score[b][j] = mean over the row's heads of 2^(q . k_j scale - M) / W.
+// The scores' own products are the attention's bit for bit, so what W is off by is common to numerator and sum.
+// Writing the logits instead costs 8 bytes a (row, slot), more than K from 32 rows on.
+//
+// S^T = K Q^T with the 128 slots of a tile in the M dimension: a thread holds a slot, and the query heads that
+// it averages over are columns of its TMEM lane, so the sum over heads needs no exchange and has a fixed order.
+// An item is a tile for up to 128 rows; averaging over all heads goes through the KV heads in turn with the sums
+// of up to 64 members (16 at G = 4) in a thread's registers.
+//
+// Warps: 0-3 columns 0-63, 4-7 columns 64-127 of S^T; 8 TMA (K), 9 MMA, 10-11 Q.  K and Q pass through a ring of
+// three stages, S^T through two halves of tensor memory.
+#include "rows_tc.cuh"
+
+namespace ikv {
+namespace {
+
+constexpr int kThreads = 384;
+
+template <int D>
+struct Sc {
+    static constexpr int kTile = kAtom * (D / 64);  // bytes of K, of Q
+    static constexpr int kStages = 3;
+    static constexpr int kOffNorm = kStages * 2 * kTile;  // (M, 1 / W) of a stage's rows
+    static constexpr int kOffBar = kOffNorm + kStages * 128 * 8;
+    static constexpr int kBars = 3 * kStages + 5;
+    static constexpr int kOffMisc = kOffBar + kBars * 8;
+    static constexpr int kSmem = kOffMisc + 16 + 1024;
+};
+
+struct Item {
+    RowsUnit u;
+    int m0, n, t0, g0, gs;  // members, first slot, KV heads
+};
+
+// A CTA's items, in turn
+struct Items {
+    int unit, sub, j, left;
+    __device__ __forceinline__ void begin(const RowsArgs &a) {
+        const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.items) + blockIdx.x);
+        unit = s.x;
+        sub = s.y;
+        j = s.z;
+        left = s.w;
+    }
+    __device__ __forceinline__ Item item(const RowsArgs &a) const {
+        Item t;
+        t.u = rows_unit(a, unit);
+        t.m0 = sub / a.item_subs * a.item_n;
+        t.n = min(a.item_n, t.u.n - t.m0);
+        t.t0 = rows_tile(t.u, j) * kRowsTile;
+        t.g0 = a.item_subs > 1 ? sub % a.item_subs : 0;
+        t.gs = a.item_subs > 1 ? 1 : a.pv.kv_heads;
+        return t;
+    }
+    __device__ __forceinline__ void next(const RowsArgs &a, const RowsUnit &u) {
+        --left;
+        if (++j < u.nt) return;
+        j = 0;
+        if (++sub < a.item_subs * ((u.n + a.item_n - 1) / a.item_n)) return;
+        sub = 0;
+        ++unit;
+    }
+};
+
+__device__ __forceinline__ int member_of(const RowsArgs &a, const RowsUnit &u, int m) {
+    return u.m0 >= 0 ? __ldcg(a.vm + u.m0 + m) : u.b;
+}
+
+template <int D, int G>
+__global__ void __launch_bounds__(kThreads, 1)
+    rows_score_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ RowsArgs a, const TcMap tm,
+                         const RowsScoreArgs sc) {
+    using C = Sc<D>;
+    using T = __nv_bfloat16;
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    unsigned char *sm = smem_raw + (base - raw);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t bar0 = base + C::kOffBar;
+    auto k_full = [&](int i) { return bar0 + 8u * i; };
+    auto q_full = [&](int i) { return bar0 + 8u * (C::kStages + i); };
+    auto empty = [&](int i) { return bar0 + 8u * (2 * C::kStages + i); };  // K's, Q's and the norms' stage
+    const uint32_t bar1 = bar0 + 8u * (3 * C::kStages);
+    auto s_full = [&](int x) { return bar1 + 8u * x; };
+    auto s_empty = [&](int x) { return bar1 + 16u + 8u * x; };
+    const uint32_t mma_done = bar1 + 32u;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + C::kOffMisc);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + C::kOffMisc + 4);
+    if (warp == 8 && lane == 0) {
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(k_full(i), 1);
+            mbar_init(q_full(i), 64);
+            mbar_init(empty(i), 256 + 1);  // the products and every thread that reads norms
+        }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(s_full(x), 1);
+            mbar_init(s_empty(x), 256);
+        }
+        mbar_init(mma_done, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 256;" ::"r"(smem_u32(tmem_slot))
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_wait();
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    Items w;
+    w.begin(a);
+    int J = 0;  // (item, KV head) products so far: stage J % kStages, half J % 2 of tensor memory
+    if (warp == 8) {
+        // ---------------- K
+        bool ok = true;
+        const int boxes = kRowsTile / tm.rows_per_box;
+        for (; w.left > 0 && ok;) {
+            const Item t = w.item(a);
+            const int s0 = t.t0 + lane * tm.rows_per_box;
+            const bool need = lane < boxes && s0 < t.u.hi && s0 + tm.rows_per_box > t.u.lo;
+            int row = need ? pool_row(a, t.u.b, t.g0, s0) : tm.pool_rows;
+            for (int g = 0; g < t.gs && ok; ++g, ++J) {
+                const int st = J % C::kStages;
+                if (lane == 0) {
+                    if (J >= C::kStages) ok = bar_wait(empty(st), (J / C::kStages - 1) & 1, abort_flag);
+                    if (ok) mbar_expect_tx(k_full(st), C::kTile);
+                }
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                if (!ok) break;
+                if (lane < boxes) tma_rows(base + st * 2 * C::kTile + lane * tm.rows_per_box * (2 * D), &tmK, row, k_full(st));
+                if (need) row += a.pv.page_size;  // (the next KV head's)
+            }
+            w.next(a, t.u);
+        }
+        if (lane == 0)
+            for (int i = J - 1; i >= 0 && i >= J - C::kStages; --i) bar_drain(k_full(i % C::kStages), (i / C::kStages) & 1);
+        __syncwarp();
+    } else if (warp == 9) {
+        // ---------------- products
+        const bool leader = elect_one();
+        bool ok = true;
+        const uint64_t dk0 = sdesc(base, 16, 16 * D), dq0 = sdesc(base + C::kTile, 16, 1024);
+        for (; w.left > 0 && ok;) {
+            const Item t = w.item(a);
+            const int half = 64 / G;
+            const int cols = __shfl_sync(0xffffffffu, t.n > half ? 64 + ((t.n - half) * G + 15) / 16 * 16 : (t.n * G + 15) / 16 * 16, 0), gs = __shfl_sync(0xffffffffu, t.gs, 0);
+            const uint32_t id = idesc_bf16(false, 128, cols);
+            for (int g = 0; g < gs && ok; ++g, ++J) {
+                const int st = J % C::kStages, x = J & 1;
+                ok = warp_wait(k_full(st), (J / C::kStages) & 1, abort_flag) &&
+                     warp_wait(q_full(st), (J / C::kStages) & 1, abort_flag) &&
+                     (J < 2 || warp_wait(s_empty(x), (J / 2 - 1) & 1, abort_flag));
+                if (!ok) break;
+                fence_after_sync();
+                const uint64_t dk = dk0 + st * (2 * C::kTile >> 4), dq = dq0 + st * (2 * C::kTile >> 4);
+                if (leader) {
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t c = (kk & 3) * 32;
+                        mma_bf16(tmem + 128 * x, dk + (((kk >> 2) * kBlock + c) >> 4), dq + (((kk >> 2) * kAtom + c) >> 4), id,
+                                 kk > 0);
+                    }
+                    mma_commit(s_full(x));
+                    mma_commit(empty(st));
+                }
+                __syncwarp();
+            }
+            w.next(a, t.u);
+        }
+        if (leader) mma_commit(mma_done);
+        __syncwarp();
+        bar_drain(mma_done, 0);
+    } else if (warp >= 10) {
+        // ---------------- Q, four lanes a row, and the rows' norms
+        const int th = tid - 320, c = th & 3;
+        bool ok = true;
+        for (; w.left > 0 && ok;) {
+            const Item t = w.item(a);
+            const int rows = t.n * G;
+            for (int g = 0; g < t.gs && ok; ++g, ++J) {
+                const int st = J % C::kStages;
+                if (J >= C::kStages) ok = bar_wait(empty(st), (J / C::kStages - 1) & 1, abort_flag);
+                if (!ok) break;
+                const uint32_t dst0 = base + st * 2 * C::kTile + C::kTile;
+                float2 *norm = reinterpret_cast<float2 *>(sm + C::kOffNorm) + st * 128;
+#pragma unroll 2
+                for (int i0 = th / 4; i0 < rows; i0 += 16) {
+                    const int b = member_of(a, t.u, t.m0 + i0 / G);
+                    const int64_t row = (int64_t)max(b, 0) * a.q_heads + (t.g0 + g) * G + i0 % G;
+                    const int r = i0 < 64 / G * G ? i0 : i0 - 64 / G * G + 64;  // its column of S^T
+                    const T *src = static_cast<const T *>(a.q) + row * D + 8 * c;
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                         dst0 + (i >> 1) * kAtom + r * 128 + ((((c + 4 * i) ^ r) & 7) << 4)),
+                                     "l"(src + 32 * i), "r"(b >= 0 ? 16 : 0)
+                                     : "memory");
+                    if (c == 0) norm[r] = b >= 0 ? __ldcg(a.norm + row) : make_float2(0.f, 0.f);
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                fence_async_smem();
+                mbar_arrive(q_full(st));
+            }
+            w.next(a, t.u);
+        }
+    } else {
+        // ---------------- weights: a thread a slot, half of the columns
+        constexpr int kMembers = 64 / G;  // of a thread's 64 columns; G = 7 uses 63
+        const int half = warp >> 2;
+        const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+        const int rps = a.rows_per_seq;
+        bool ok = true;
+        for (; w.left > 0;) {
+            const Item t = w.item(a);
+            const int slot = t.t0 + (warp & 3) * 32 + lane, m1 = half * kMembers;
+            const int mine = min(max(t.n - m1, 0), kMembers);  // members of this half
+            float sum[kMembers];
+#pragma unroll
+            for (int m = 0; m < kMembers; ++m) sum[m] = 0.f;
+            for (int g = 0; g < t.gs; ++g, ++J) {
+                const int st = J % C::kStages, x = J & 1;
+                if (ok) ok = bar_wait(q_full(st), (J / C::kStages) & 1, abort_flag);  // (the norms)
+                if (ok) ok = bar_wait(s_full(x), (J / 2) & 1, abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                fence_after_sync();
+                const float2 *norm = reinterpret_cast<const float2 *>(sm + C::kOffNorm) + st * 128 + 64 * half;
+                if (ok && mine > 0) {
+                    uint32_t v[64];
+                    const uint32_t at = tmem + 128 * x + lane_off + 64 * half;
+                    tmem_ld32(at, v);
+                    if (mine * G > 32) tmem_ld32(at + 32, v + 32);
+                    tmem_wait_ld(v);
+                    if (mine * G > 32) tmem_wait_ld(v + 32);
+#pragma unroll
+                    for (int m = 0; m < kMembers; ++m)
+                        if (m < mine) {
+#pragma unroll
+                            for (int h = 0; h < G; ++h) {
+                                const float2 mw = norm[m * G + h];
+                                sum[m] += ex2(__fmaf_rn(__uint_as_float(v[m * G + h]), a.scale_log2, -mw.x)) * mw.y;
+                            }
+                        }
+                }
+                fence_before_sync();
+                mbar_arrive(s_empty(x));
+                mbar_arrive(empty(st));
+            }
+            if (ok && slot >= t.u.lo && slot < t.u.hi) {
+                const int j = slot - t.u.S0;
+                const float inv = 1.f / (float)(t.gs > 1 || rps == 1 ? a.q_heads : G);
+#pragma unroll
+                for (int m = 0; m < kMembers; ++m)
+                    if (m < mine) {
+                        const int b = member_of(a, t.u, t.m0 + m1 + m);
+                        if (b >= 0) {
+                            const int64_t r = (int64_t)b * rps + (rps > 1 ? t.g0 : 0);
+                            const bool live = !a.live || (__ldcg(a.live + r * a.live_words + (j >> 5)) >> (j & 31)) & 1u;
+                            const float s = live ? sum[m] * inv : 0.f;
+                            if (sc.score) sc.score[r * a.cap + j] = s;
+                            if (sc.ema) sc.ema[r * a.cap + j] = sc.alpha * sc.ema[r * a.cap + j] + (1.f - sc.alpha) * s;
+                        }
+                    }
+            }
+            w.next(a, t.u);
+        }
+    }
+    fence_before_sync();
+    __syncthreads();
+    if (warp == 9) {
+        fence_after_sync();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 256;" ::"r"(tmem) : "memory");
+    }
+}
+
+template <int D, int G>
+cudaError_t launch_dg(const RowsArgs &a, const RowsScoreArgs &s, cudaStream_t st) {
+    TcMap t;
+    CUtensorMap mk;
+    if (!layer_map(&mk, a.k, a, D, &t)) return cudaErrorInvalidValue;
+    const cudaError_t e =
+        cudaFuncSetAttribute(rows_score_tc_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sc<D>::kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_k(rows_score_tc_kernel<D, G>, dim3(a.ctas), dim3(kThreads), Sc<D>::kSmem, st, mk, a, t, s);
+}
+template <int D>
+cudaError_t launch_d(const RowsArgs &a, const RowsScoreArgs &s, cudaStream_t st) {
+    switch (a.group) {
+        case 1: return launch_dg<D, 1>(a, s, st);
+        case 2: return launch_dg<D, 2>(a, s, st);
+        case 4: return launch_dg<D, 4>(a, s, st);
+        case 7: return launch_dg<D, 7>(a, s, st);
+        case 8: return launch_dg<D, 8>(a, s, st);
+        default: return cudaErrorInvalidValue;
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_rows_score_tc(const RowsArgs &a, const RowsScoreArgs &s, int head_dim, cudaStream_t st) {
+    const cudaError_t e = head_dim == 64 ? launch_d<64>(a, s, st) : launch_d<128>(a, s, st);
+    note_launch();
+    return e;
+}
+
+cudaError_t read_clear_rows_score_error(unsigned int *v) { return read_clear_timeout(v); }
+
+}  // namespace ikv

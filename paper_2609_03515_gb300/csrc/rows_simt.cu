@@ -202,14 +202,15 @@ __global__ void __launch_bounds__(kSimtThreads) rows_simt_kernel(const RowsArgs 
     head.n_pre = __ldcg(&a.head->n_pre);
     RowsWalk w;
     w.begin(a, blockIdx.x);
-    while (w.more()) {
+    while (w.left > 0) {
         const RowsUnit u = rows_unit(a, w.unit);
-        const int n = w.part(u.nt);
+        const int n = w.part(a, u.nt, u.n), j0 = w.first(a, u.n);
+        if (n <= 0) break;
         if (u.n * a.group <= 16)
-            simt_part<D, T, 1>(a, head, u, w.unit, w.g, w.j, n, sQ, sK, sV, sP);
+            simt_part<D, T, 1>(a, head, u, w.unit, w.g, j0, n, sQ, sK, sV, sP);
         else
-            simt_part<D, T, 4>(a, head, u, w.unit, w.g, w.j, n, sQ, sK, sV, sP);
-        w.next(a, u.nt, n);
+            simt_part<D, T, 4>(a, head, u, w.unit, w.g, j0, n, sQ, sK, sV, sP);
+        w.next(a, u.nt, u.n);
     }
 }
 

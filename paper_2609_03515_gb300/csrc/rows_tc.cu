@@ -18,20 +18,13 @@
 // 32 KB (D = 64: 16 KB) stages in the order K0 K1 V0 K2 V1 .., which is the order of the products.  Boxes of
 // a tile that no row sees are fetched from behind the tensor's end, which fills zeros and reads nothing.
 // Every wait is bounded; on timeout the CTA sets the error word, drains what is in flight and returns.
-#include <cudaTypedefs.h>
-
-#include "rows_redo.cuh"
-#include "tc.cuh"
+#include "rows_tc.cuh"
 
 namespace ikv {
-
-__device__ unsigned int g_rows_tc_error = 0;
 
 namespace {
 
 constexpr int kThreads = 384;
-constexpr int kAtom = 128 * 128;            // bytes of 64 channels of a 128-row tile (128-byte swizzle)
-constexpr uint64_t kLimitNs = 1000000000ull;
 constexpr float kSlack = 8.f;               // log2 of the largest weight before the maximum moves
 
 template <int D>
@@ -47,69 +40,6 @@ struct Tc {
     static constexpr int kSmem = kOffMisc + 16 + 1024;  // (to align by 1024)
 };
 
-struct TcMap {
-    int32_t rows_per_box, pool_rows;        // pool_rows: rows of the layer, a row behind the end
-};
-
-// Bounded: false where the phase does not complete in time (which also raises the CTA's abort flag and the
-// error word), or once another warp has given up.
-__device__ __forceinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *abort) {
-    const uint64_t start = global_ns();
-    for (;;) {
-        if (mbar_try(bar, parity, 2000)) return true;
-        if (*abort) return false;
-        if (global_ns() - start > kLimitNs) break;
-    }
-    *abort = 1;
-    atomicOr(&g_rows_tc_error, 1u);
-    return false;
-}
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
-    return mbar_try(bar, parity, 2000) || bar_wait_long(bar, parity, abort);
-}
-// by a converged warp, with one answer for all of it
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
-    if (__all_sync(0xffffffffu, mbar_try(bar, parity, 2000))) return true;
-    return __all_sync(0xffffffffu, bar_wait_long(bar, parity, abort));
-}
-// of one's own copies or products, whatever the abort flag says
-__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
-    if (mbar_test(bar, parity)) return;
-    const uint64_t start = global_ns();
-    while (!mbar_try(bar, parity, 2000))
-        if (global_ns() - start > kLimitNs) {
-            atomicOr(&g_rows_tc_error, 1u);
-            return;
-        }
-}
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// two at a time: x y + z, x + y
-__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
-    unsigned long long r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(r)
-        : "l"(*reinterpret_cast<unsigned long long *>(&x)), "l"(*reinterpret_cast<unsigned long long *>(&y)),
-          "l"(*reinterpret_cast<unsigned long long *>(&z)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-__device__ __forceinline__ float2 add2(float2 x, float2 y) {
-    unsigned long long r;
-    asm("add.rn.f32x2 %0, %1, %2;"
-        : "=l"(r)
-        : "l"(*reinterpret_cast<unsigned long long *>(&x)), "l"(*reinterpret_cast<unsigned long long *>(&y)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-__device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-            dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-        : "memory");
-}
 // bits of the slots a .. b of a tile that lie in its w-th 32
 __device__ __forceinline__ uint32_t range_bits(int a, int b, int w) {
     const int lo = max(a - 32 * w, 0), hi = min(b - 32 * w, 31);
@@ -180,19 +110,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             int J = 0;
             bool ok = true;
             const int boxes = kRowsTile / tm.rows_per_box;
-            while (w.more() && ok) {
+            while (w.left > 0 && ok) {
                 const RowsUnit u = rows_unit(a, w.unit);
-                const int n = w.part(u.nt);
+                const int n = w.part(a, u.nt, u.n), j0 = w.first(a, u.n);
+                if (n <= 0) break;
                 for (int x = 0; x < 2 * n && ok; ++x, ++J) {
                     int tile;
                     bool is_v;
                     load_of(x, n, tile, is_v);
-                    const int s0 = rows_tile(u, w.j + tile) * kRowsTile + lane * tm.rows_per_box, s1 = s0 + tm.rows_per_box;
+                    const int s0 = rows_tile(u, j0 + tile) * kRowsTile + lane * tm.rows_per_box, s1 = s0 + tm.rows_per_box;
                     int row = tm.pool_rows;
                     if (lane < boxes && s0 < u.hi && (s1 > u.wlo || (s0 < u.sh && s1 > u.lo))) {
-                        const int lp = a.pv.page_shift >= 0 ? s0 >> a.pv.page_shift : s0 / a.pv.page_size;
-                        const int page = __ldg(a.pv.block_table + (int64_t)u.b * a.pv.max_pages + lp);
-                        row = (page * a.pv.kv_heads + w.g) * a.pv.page_size + (s0 - lp * a.pv.page_size);
+                        row = pool_row(a, u.b, w.g, s0);
                     }
                     const int st = J % C::kStages;
                     if (lane == 0) {
@@ -200,15 +129,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (ok) mbar_expect_tx(kv_full(st), C::kStage);
                     }
                     ok = __shfl_sync(0xffffffffu, ok, 0);
-                    if (ok && lane < boxes) {
-                        const uint32_t dst = base + C::kOffRing + st * C::kStage + lane * tm.rows_per_box * 128;
-#pragma unroll
-                        for (int c = 0; c < D / 64; ++c)
-                            tma_tile(dst + c * kAtom, is_v ? &tmV : &tmK, 64 * c, row, kv_full(st));
-                    }
+                    if (ok && lane < boxes)
+                        tma_rows(base + C::kOffRing + st * C::kStage + lane * tm.rows_per_box * (2 * D), is_v ? &tmV : &tmK, row,
+                                 kv_full(st));
                     if (!ok) break;
                 }
-                w.next(a, u.nt, n);
+                w.next(a, u.nt, u.n);
             }
             if (lane == 0)  // every copy has landed before the CTA ends
                 for (int i = J - 1; i >= 0 && i >= J - C::kStages; --i) bar_drain(kv_full(i % C::kStages), (i / C::kStages) & 1);
@@ -219,8 +145,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             // (A lane alone in a branch formed them in its own and took 125 cycles a product instead of 64.)
             constexpr uint32_t id_qk = idesc_bf16(false, 128, 128), id_pv = idesc_bf16(false, 128, D, true);
             const bool leader = elect_one();
-            const uint64_t dq0 = sdesc(base, 16, 1024), dk0 = sdesc(base + C::kOffRing, 16, 1024),
-                           dv0 = sdesc(base + C::kOffRing, kAtom, 1024);
+            const uint64_t dq0 = sdesc(base, 16, 1024), dk0 = sdesc(base + C::kOffRing, 16, 16 * D),
+                           dv0 = sdesc(base + C::kOffRing, kBlock, 16 * D);
             struct Stage {
                 int i;
                 uint32_t par;
@@ -232,9 +158,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             uint32_t seg = 0, np[2] = {0, 0};  // weights taken
             bool ok = true;
-            while (w.more() && ok) {
+            while (w.left > 0 && ok) {
                 const RowsUnit *up = a.units + w.unit;
-                const int n = __shfl_sync(0xffffffffu, w.part(up->nt), 0);
+                const int n = __shfl_sync(0xffffffffu, w.part(a, up->nt, up->n), 0);
+                if (n <= 0) break;
                 const bool pair = __shfl_sync(0xffffffffu, up->n * a.group > tile_rows, 0);
                 auto there = [&](Stage s) { return warp_wait(kv_full(s.i), s.par, abort_flag); };
                 // S of row tile x; (free: K's stage is done with then)
@@ -244,8 +171,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (leader) {
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk) {
-                            const uint32_t off = ((kk >> 2) * kAtom + (kk & 3) * 32) >> 4;
-                            mma_bf16(tmem + 128 * x, dq + off, dk + off, id_qk, kk > 0);
+                            const uint32_t c = (kk & 3) * 32;
+                            mma_bf16(tmem + 128 * x, dq + (((kk >> 2) * kAtom + c) >> 4),
+                                     dk + (((kk >> 2) * kBlock + c) >> 4), id_qk, kk > 0);
                         }
                         mma_commit(s_full(x));
                         if (free) mma_commit(kv_empty(k.i));
@@ -257,8 +185,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (!warp_wait(p_half(x), np[x] & 1, abort_flag)) return false;
                     fence_after_sync();
                     const uint64_t dv = dv0 + v.i * (C::kStage >> 4);
-                    auto product = [&](int kk) {  // V: channels contiguous, 8-slot groups 1 KB apart
-                        mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * kk, dv + kk * (2048 >> 4), id_pv,
+                    auto product = [&](int kk) {  // V: channels contiguous, 64 of them 1 KB apart
+                        mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * kk, dv + kk * (32 * D >> 4), id_pv,
                                     !first || kk > 0);
                     };
                     if (leader) {
@@ -324,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
                 ++seg;
-                w.next(a, up->nt, n);
+                w.next(a, up->nt, up->n);
             }
             if (leader) mma_commit(mma_done);  // also after an abort: no product may write TMEM when it is freed
             __syncwarp();
@@ -338,9 +266,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int c = t & 3;
             uint32_t seg = 0;
             bool ok = true;
-            while (w.more() && ok) {
+            while (w.left > 0 && ok) {
                 const RowsUnit u = rows_unit(a, w.unit);
-                const int n = w.part(u.nt), rows = u.n * a.group;
+                const int rows = u.n * a.group;
+                if (w.part(a, u.nt, u.n) <= 0) break;
                 const bool many = a.prefix && u.m0 >= 0;
                 const int64_t row0 = a.prefix ? u.b : (int64_t)u.row0 + u.m0;
                 const T *q = static_cast<const T *>(a.q) + (int64_t)w.g * a.group * D + 8 * c;
@@ -383,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mbar_arrive(q_full(1));
                 }
                 ++seg;
-                w.next(a, u.nt, n);
+                w.next(a, u.nt, u.n);
             }
         }
     } else {
@@ -396,14 +325,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int n_pre = __ldcg(&a.head->n_pre);
         uint32_t ns = 0, np = 0;  // scores and weights so far
         bool ok = true;
-        while (w.more()) {
+        while (w.left > 0) {
             // (the unit is looked up where it is needed: kept, it would push scores out of the registers)
             const RowsUnit *up = a.units + w.unit;
-            int n, r, seq, hi, wlo, steps;
+            int n, j0, r, seq, hi, wlo, steps;
             bool pair, busy;
             {
                 const RowsUnit u = rows_unit(a, w.unit);
-                n = w.part(u.nt);
+                n = w.part(a, u.nt, u.n);
+                if (n <= 0) break;
+                j0 = w.first(a, u.n);
                 const int rows = u.n * a.group;
                 pair = rows > tile_rows;
                 r = pair ? X * tile_rows + row_in : row_in;
@@ -420,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t see[4];
                 bool masked;
                 {
-                    const int j = w.j + (pair ? s : 2 * s + X), n_a = up->n_a;
+                    const int j = j0 + (pair ? s : 2 * s + X), n_a = up->n_a;
                     const int t0 = (j < n_a ? up->t_a + j : up->t_w + j - n_a) * kRowsTile;
                     const int lo = up->lo, S0 = up->S0, sh = a.prefix ? lo : S0 + a.sinks;
                     const bool full = seq < 0 || (t0 >= lo && t0 + 127 <= hi && (t0 >= wlo || t0 + 127 < sh));
@@ -431,23 +362,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                             see[k] = seq < 0 ? 0u
                                              : range_bits(max(lo, wlo) - t0, hi - t0, k) |
                                                    range_bits(lo - t0, min(sh - 1, hi) - t0, k);
-                        if (a.pos) {
-                            // liveness, one sequence of the warp's rows at a time: a lane looks up every 32nd slot
-                            const int rw = r - lane, rows = up->n * a.group, end = up->hi;
-                            const bool many = a.prefix && up->m0 >= 0;
-                            const int m0 = many ? rw / a.group : 0, m1 = many ? min(rw + 31, rows - 1) / a.group : 0;
-                            for (int k = m0; k <= m1; ++k) {
-                                const int who = __shfl_sync(0xffffffffu, seq, many ? max(k * a.group - rw, 0) : 0);
-                                const int32_t *pos =
-                                    a.pos + ((int64_t)max(who, 0) * a.rows_per_seq + (a.rows_per_seq == 1 ? 0 : w.g)) * a.cap;
-                                const bool me = !many || r / a.group == k;
+                        if (a.pos && seq >= 0) {  // the row's own live slots, by slot - S0
+                            const int64_t rr = (int64_t)seq * a.rows_per_seq + (a.rows_per_seq == 1 ? 0 : w.g);
+                            const uint32_t *bits = a.live + rr * a.live_words;
+                            const int x0 = (t0 - S0) >> 5, sh0 = (t0 - S0) & 31;
+                            uint32_t lo_w = x0 >= 0 && x0 < a.live_words ? __ldcg(bits + x0) : 0u;
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) {
-                                    const int slot = t0 + 32 * x + lane;
-                                    const bool live = who >= 0 && slot >= lo && slot < end && __ldg(pos + (slot - S0)) >= 0;
-                                    const uint32_t bits = __ballot_sync(0xffffffffu, live);
-                                    if (me) see[x] &= bits;
-                                }
+                            for (int x = 0; x < 4; ++x) {
+                                const int k = x0 + x + 1;
+                                const uint32_t hi_w = k >= 0 && k < a.live_words ? __ldcg(bits + k) : 0u;
+                                see[x] &= __funnelshift_r(lo_w, hi_w, sh0);
+                                lo_w = hi_w;
                             }
                         }
                     }
@@ -554,13 +479,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (ok && busy && (pair || X == 0)) {
                 RowsRow row = rows_row<D>(a, u, w.g, r);
                 row.seq = seq;
-                const bool begins = w.j == 0, whole = begins && n == u.nt && !a.prefix;
+                const bool begins = j0 == 0, whole = begins && n == u.nt && !a.prefix;
                 RowsHead h;
                 h.n_pre = n_pre;
                 const int64_t slot = whole ? 0 : rows_slot(a, h, u, w.unit, w.g, blockIdx.x, begins);
                 const bool joined = !pair && n > 1;
                 const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-                bool bad = false;
+                float probe = 0.f;  // NaN once a value is not finite
                 unsigned char *stage = sm + C::kOffOut + warp * 4096;
 #pragma unroll 1
                 for (int k = 0; k < D; k += 32) {
@@ -578,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        bad |= !(fabsf(y[i]) < INFINITY);
+                        probe = __fmaf_rn(y[i], 0.f, probe);
                         y[i] *= inv;
                     }
                     if (whole) {
@@ -597,14 +522,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         if (k % 64 == 32) {
                             __syncwarp();
+                            uint4 x[8];
+                            int64_t at[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
-                                const int rr = 4 * i + lane / 8, c = lane % 8 * 8;
-                                const int64_t at = __shfl_sync(0xffffffffu, row.out, rr);
-                                if (__shfl_sync(0xffffffffu, row.seq, rr) >= 0)
-                                    *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + at + k - 32 + c) =
-                                        *reinterpret_cast<const uint4 *>(stage + sw128(rr, c));
+                                const int rr = 4 * i + lane / 8;
+                                x[i] = *reinterpret_cast<const uint4 *>(stage + sw128(rr, lane % 8 * 8));
+                                at[i] = __shfl_sync(0xffffffffu, row.seq >= 0 ? row.out : -1, rr);
                             }
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                if (at[i] >= 0)
+                                    *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + at[i] + k - 32 + lane % 8 * 8) = x[i];
                         }
                     } else if (row.seq >= 0) {
                         const int step = rows_part_step(a, u);
@@ -616,11 +545,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (row.seq >= 0 && !whole) rows_store_ml(a, u, slot, r, m, l);
                 // (see rows_redo: V rows that are not finite and that the row does not see)
                 __syncwarp();  // (it stores over what another lane did)
-                unsigned redo = __ballot_sync(0xffffffffu, bad && row.seq >= 0 && !isnan(l));
+                unsigned redo = __ballot_sync(0xffffffffu, isnan(probe) && row.seq >= 0 && !isnan(l));
                 while (redo) {
                     const int i = __ffs(redo) - 1;
                     redo &= redo - 1;
-                    rows_redo<D, T>(a, w.unit, w.g, w.j, n, whole, slot, __shfl_sync(0xffffffffu, r, i));
+                    rows_redo<D, T>(a, w.unit, w.g, j0, n, whole, slot, __shfl_sync(0xffffffffu, r, i));
                 }
             }
             if (!pair) {  // (B's output has been read)
@@ -628,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 fence_after_sync();
             }
-            w.next(a, u.nt, n);
+            w.next(a, u.nt, u.n);
         }
     }
     fence_before_sync();
@@ -639,42 +568,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
-    static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
-        cudaDriverEntryPointQueryResult q;
-        void *p = nullptr;
-        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q);
-        return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p)
-                                                                    : nullptr;
-    }();
-    return fn;
-}
-
-bool layer_map(CUtensorMap *m, const void *rows0, int head_dim, uint64_t rows, int rows_per_box) {
-    const auto fn = encode_fn();
-    if (!fn) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)head_dim, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)head_dim * 2};
-    const cuuint32_t box[2] = {64u, (cuuint32_t)rows_per_box}, es[2] = {1u, 1u};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(rows0), dims, strides, box, es,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int D>
 cudaError_t launch_tc(const RowsArgs &a, cudaStream_t st) {
     TcMap t;
-    const uint64_t rows = (uint64_t)a.pv.num_pages * a.pv.kv_heads * a.pv.page_size;
-    t.pool_rows = (int32_t)rows;
-    // boxes as high as the page allows, at most 64 rows: they are also the grain in which the ends of
-    // what a unit sees are read
-    t.rows_per_box = 8;
-    while (t.rows_per_box < 64 && a.pv.page_size % (2 * t.rows_per_box) == 0) t.rows_per_box *= 2;
     CUtensorMap mk, mv;
-    const size_t off = (size_t)a.layer * rows * D * 2;
-    if (!layer_map(&mk, static_cast<const char *>(a.k) + off, D, rows, t.rows_per_box) ||
-        !layer_map(&mv, static_cast<const char *>(a.v) + off, D, rows, t.rows_per_box))
-        return cudaErrorInvalidValue;
+    if (!layer_map(&mk, a.k, a, D, &t) || !layer_map(&mv, a.v, a, D, &t)) return cudaErrorInvalidValue;
     const cudaError_t e = cudaFuncSetAttribute(rows_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc<D>::kSmem);
     if (e != cudaSuccess) return e;
     return launch_k(rows_tc_kernel<D>, dim3(a.ctas), dim3(kThreads), Tc<D>::kSmem, st, mk, mv, a, t);
@@ -694,11 +592,6 @@ cudaError_t launch_rows_tc(const RowsArgs &a, int head_dim, cudaStream_t st) {
     return e;
 }
 
-cudaError_t read_clear_rows_tc_error(unsigned int *v) {
-    unsigned int z = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(v, g_rows_tc_error, sizeof(*v));
-    if (e == cudaSuccess && *v) e = cudaMemcpyToSymbol(g_rows_tc_error, &z, sizeof(z));
-    return e;
-}
+cudaError_t read_clear_rows_tc_error(unsigned int *v) { return read_clear_timeout(v); }
 
 }  // namespace ikv
