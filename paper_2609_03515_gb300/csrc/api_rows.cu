@@ -88,6 +88,9 @@ RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, 
         a.first = p->first;
         a.member = p->member;
         a.group_len = p->len;
+        // (64 units, each with at most cap / 128 + 2 tiles and 2 more, and twice that many items)
+        a.small = s->batch <= 32 && p->n_groups <= 32 &&
+                  (int64_t)(a.cap / kRowsTile + 4) * s->kv_heads * 64 * 4 < (int64_t)1 << 31;
         units = (int64_t)p->n_groups + s->batch / a.unit_n + s->batch;
     }
     size_t off = 0;

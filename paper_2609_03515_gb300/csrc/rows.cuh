@@ -37,9 +37,10 @@ struct RowsUnit {                   // 64 bytes
 // overlaps, and its output: two where its rows fill two row tiles of the tensor-core kernel.
 constexpr int kRowsOne = 1, kRowsTwo = 2;
 
-struct RowsHead {
+struct alignas(16) RowsHead {
     int64_t total, per;             // cost in all, of a CTA's share
     int32_t n_units, n_pre;         // n_pre: units of shared prefixes, in front of the others
+    int32_t pad[2];
 };
 struct RowsStart {                  // where a CTA's share begins (at cost `at` of pair (unit, g)), and its cost
     int32_t unit, g, at, n;
@@ -75,6 +76,7 @@ struct RowsArgs {
     int32_t max_count, seq_units;   // seq_units: units of max_count tokens
     // prefix
     int32_t prefix;                 // nonzero: a shared-prefix call
+    int32_t small;                  // nonzero: a plan of at most 32 sequences and groups, whose sums fit 32 bits
     int32_t n_groups;
     const int32_t *first, *member, *group_len;
     // workspace

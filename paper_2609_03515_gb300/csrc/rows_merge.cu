@@ -10,12 +10,24 @@ namespace {
 
 constexpr int kMergeThreads = 128, kMergeRows = 8, kMergeAhead = 8;
 
+__device__ __forceinline__ RowsHead rows_head(const RowsArgs &a) {
+    RowsHead h;
+    const int4 x = __ldcg(reinterpret_cast<const int4 *>(a.head)), y = __ldcg(reinterpret_cast<const int4 *>(a.head) + 1);
+    reinterpret_cast<int4 *>(&h)[0] = x;
+    reinterpret_cast<int4 *>(&h)[1] = y;
+    return h;
+}
+// (a division of 64 bits takes longer than a look-up in memory)
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t y) {
+    return (x | y) >> 31 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
+}
+
 // n parts of `rows` <= 8 rows: (max, sum) of part i of row r at ml(i)[r], its channels 4 c .. at o(i)[c * step(i)
 // + 4 r].  done(r, ref, W): row r's maximum and sum; out(r): its output.
 template <int D, typename T, typename ML, typename O, typename Step, typename Done, typename Out>
 __device__ __forceinline__ void merge_rows(int n, int rows, ML ml, O o, Step step, Done done, Out out) {
     constexpr int kChunks = D / 4, kIter = kChunks * kMergeRows / kMergeThreads;
-    __shared__ float wq[kMergeRows][2 * kRowsMaxCtas], total[kMergeRows];
+    __shared__ float wq[kMergeRows][32], top[kMergeRows], total[kMergeRows];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int row = tid % kMergeRows, chunk = tid / kMergeRows;
     float4 early[kIter][kMergeAhead];
@@ -38,24 +50,25 @@ __device__ __forceinline__ void merge_rows(int n, int rows, ML ml, O o, Step ste
             const float2 x = i == lane ? x0 : __ldcg(ml(i) + r);
             const float f = exp2f(x.x - ref);
             W += x.y * f;
-            wq[r][i] = f;
+            if (i == lane) wq[r][i] = f;
         }
         W = warp_sum(W);
         if (lane == 0) {
             total[r] = W;
+            top[r] = ref;
             done(r, ref, W);
         }
     }
     __syncthreads();
     if (row < rows) {
-        const float W = total[row];
+        const float W = total[row], ref = top[row];
         T *dst = out(row);
 #pragma unroll
         for (int k = 0; k < kIter; ++k) {
             const int c = chunk + k * (kChunks / kIter);
             float acc[4] = {0.f, 0.f, 0.f, 0.f};
             auto add = [&](int i, float4 v) {
-                const float f = wq[row][i];
+                const float f = i < 32 ? wq[row][i] : exp2f(__ldcg(ml(i) + row).x - ref);
                 acc[0] += f * v.x;
                 acc[1] += f * v.y;
                 acc[2] += f * v.z;
@@ -93,7 +106,7 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_window_kernel(const 
     const RowsUnit u = rows_unit(a, w.unit);
     const int j = w.first(a, u.n);
     if (j == 0 || j > per) return;  // (beyond: the share in front of this one begins behind the pair's first tile)
-    const int n = 1 + (int)((u.nt - j + per - 1) / per);  // parts: share c - 1's and those behind
+    const int n = 1 + (int)divide(u.nt - j + per - 1, per);  // parts: share c - 1's and those behind
     const int rows = u.n * a.group;
     auto slot = [&](int i) { return i == 0 ? 2 * (int64_t)(c - 1) + 1 : 2 * (int64_t)(c + i - 1); };
     for (int r0 = blockIdx.y * kMergeRows; r0 < rows; r0 += gridDim.y * kMergeRows) {
@@ -111,19 +124,21 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_prefix_kernel(const 
     pdl_wait();
     const int hk = a.pv.kv_heads, b = blockIdx.x / hk, g = blockIdx.x % hk;
     const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.seq) + b);
-    const int64_t per = __ldcg(&a.head->per);
-    const int n_pre = __ldcg(&a.head->n_pre);
+    const RowsHead head = rows_head(a);
+    RowsUnit pre, own;
+    if (s.x >= 0) pre = rows_unit(a, s.x);
+    if (s.z >= 0) own = rows_unit(a, s.z);
     int64_t slot_p = 0, slot_o = 0;
     int np = 0, no = 0;
-    auto parts = [&](int unit, int64_t pair0, int64_t &slot) {  // of pair (unit, g); slot: its first part's
-        const int nt = __ldcg(&a.units[unit].nt), e = rows_extra(a, __ldcg(&a.units[unit].n));
-        const int64_t x0 = __ldcg(&a.units[unit].cum) + (int64_t)g * (nt + e) + e;
-        const int64_t c0 = x0 / per;
+    auto parts = [&](const RowsUnit &u, int64_t pair0, int64_t &slot) {  // of pair (u, g); slot: its first part's
+        const int e = rows_extra(a, u.n);
+        const int64_t x0 = u.cum + (int64_t)g * (u.nt + e) + e;
+        const int64_t c0 = divide(x0, head.per);
         slot = pair0 + g + c0;
-        return (int)((x0 + nt - 1) / per - c0) + 1;
+        return (int)(divide(x0 + u.nt - 1, head.per) - c0) + 1;
     };
-    if (s.x >= 0) np = parts(s.x, (int64_t)s.x * hk, slot_p);
-    if (s.z >= 0) no = parts(s.z, (int64_t)(s.z - n_pre) * hk, slot_o);
+    if (s.x >= 0) np = parts(pre, (int64_t)s.x * hk, slot_p);
+    if (s.z >= 0) no = parts(own, (int64_t)(s.z - head.n_pre) * hk, slot_o);
     const int rp = s.y * a.group;  // the pre part's rows
     const int64_t row0 = (int64_t)b * a.q_heads + g * a.group;
     merge_rows<D, T>(

@@ -12,12 +12,17 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanCum = 1024;      // units whose offsets stay in shared memory for the search
 
-constexpr int kPlanSmall = 1024;    // sequences and groups whose tables stay there
+constexpr int kPlanSmall = 512;     // sequences and groups whose tables stay there
 
 struct Sums {
     int32_t n;                      // units
     int64_t cost, items;            // of the attention, of the score pass
     __device__ __forceinline__ Sums operator+(const Sums &o) const { return {n + o.n, cost + o.cost, items + o.items}; }
+};
+// the same in 32 bits, for plans that fit
+struct Sums32 {
+    int32_t n, cost, items;
+    __device__ __forceinline__ Sums32 operator+(const Sums32 &o) const { return {n + o.n, cost + o.cost, items + o.items}; }
 };
 
 // Exclusive sums over the CTA's threads, on top of `carry`, which the totals are added to.
@@ -100,6 +105,118 @@ __device__ __forceinline__ void live_bits(const RowsArgs &a) {
     }
 }
 
+// Exclusive sums over a warp, on top of `carry`
+__device__ __forceinline__ Sums32 warp_scan(const Sums32 &x, Sums32 &carry) {
+    const int lane = threadIdx.x & 31;
+    Sums32 s = x;
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+        const Sums32 y{__shfl_up_sync(0xffffffffu, s.n, o), __shfl_up_sync(0xffffffffu, s.cost, o),
+                       __shfl_up_sync(0xffffffffu, s.items, o)};
+        if (lane >= o) s = s + y;
+    }
+    const Sums32 at{carry.n + s.n - x.n, carry.cost + s.cost - x.cost, carry.items + s.items - x.items};
+    carry = carry + Sums32{__shfl_sync(0xffffffffu, s.n, 31), __shfl_sync(0xffffffffu, s.cost, 31),
+                           __shfl_sync(0xffffffffu, s.items, 31)};
+    return at;
+}
+
+// The prefix plan of at most 32 sequences and groups, by one warp without a barrier (the general one costs some
+// 4 us more, all of them waits).  tab: 64 words of shared memory.
+template <typename Put>
+__device__ __forceinline__ void small_plan(const RowsArgs &a, Put put, Sums32 &sum, int &n_pre, int32_t *tab) {
+    constexpr unsigned kAll = 0xffffffffu;
+    const int lane = threadIdx.x & 31;
+    int f0 = 0x7fffffff, f1 = 0x7fffffff, glen = 0, S0 = 0, L = 0;
+    if (lane < a.n_groups) {
+        f0 = __ldg(a.first + lane);
+        f1 = __ldg(a.first + lane + 1);
+        glen = max(__ldg(a.group_len + lane), 0);
+    }
+    if (lane < a.batch) {
+        S0 = clamp_start(a, lane);
+        L = clamp_len(a, lane, S0);
+    }
+    int n_groups = a.n_groups;
+    if (__any_sync(kAll, lane < n_groups && (f0 < 0 || f0 > f1))) n_groups = 0;  // the groups' entries would overlap
+    const int raw = n_groups > 0 ? __shfl_sync(kAll, f1, n_groups - 1) : 0;
+    const int entries = min(raw, a.batch), entry0 = n_groups > 0 ? __shfl_sync(kAll, f0, 0) : 0;
+    bool wrong = (n_groups != a.n_groups || raw > a.batch) && lane == 0;
+    // lane: entry
+    const bool entry = lane >= entry0 && lane < entries;
+    int b = entry ? __ldg(a.member + lane) : -1;
+    const unsigned same = __match_any_sync(kAll, entry && b >= 0 && b < a.batch ? b : -1 - lane);
+    if (entry && !(b >= 0 && b < a.batch && __ffs(same) - 1 == lane)) {  // it counts if it is the first that names it
+        wrong = true;
+        b = -1;
+    }
+    if (__any_sync(kAll, wrong) && lane == 0) atomicOr(&g_rows_error, 128u);
+    if (entry) a.vm[lane] = b;
+    int gi = 0;  // its group: the last that begins at or before it
+#pragma unroll 1
+    for (int o = 16; o > 0; o >>= 1) {
+        const int f = __shfl_sync(kAll, f0, min(gi + o, 31));
+        if (gi + o < n_groups && f <= lane) gi += o;
+    }
+    const bool counts = entry && b >= 0;
+    const unsigned mates = __match_any_sync(kAll, counts ? gi : -1 - lane);
+    const int my_len = __shfl_sync(kAll, L, max(b, 0)), my_S0 = __shfl_sync(kAll, S0, max(b, 0));
+    int p = min((int)__reduce_min_sync(mates, (unsigned)my_len), __shfl_sync(kAll, glen, gi));
+    if (!counts || __popc(mates) < 2) p = 0;  // (one alone: nothing to share)
+    const int e0 = __shfl_sync(kAll, f0, gi), e1 = min(__shfl_sync(kAll, f1, gi), entries);
+    RowsUnit u{};
+    int n = 0;
+    if (p > 0 && __ffs(mates) - 1 == lane) {  // the first member makes the group's units
+        u.b = b;
+        u.S0 = my_S0;
+        n = (e1 - e0 + a.unit_n - 1) / a.unit_n;
+        u.n = min(a.unit_n, e1 - e0);
+        whole_run(u, u.S0, u.S0 + p);
+    }
+    const int rest = n > 0 ? e1 - e0 - (n - 1) * u.n : 0, most = u.n;
+    RowsUnit last = u;
+    last.n = rest;
+    Sums32 at = warp_scan({n, n > 0 ? (n - 1) * (int)cost(a, u) + (int)cost(a, last) : 0,
+                           n > 0 ? (n - 1) * (int)items(a, u) + (int)items(a, last) : 0}, sum);
+    const int unit0 = __shfl_sync(kAll, at.n, __ffs(mates) - 1);
+    for (int k = 0; k < n; ++k) {
+        u.m0 = e0 + k * most;
+        u.n = k == n - 1 ? rest : most;
+        put(u, {at.n, at.cost, at.items});
+        at = at + Sums32{1, (int)cost(a, u), (int)items(a, u)};
+    }
+    n_pre = sum.n;
+    // lane: sequence
+    tab[lane] = -1;
+    __syncwarp();
+    if (counts && p > 0) {
+        const int k = lane - e0;
+        tab[b] = (unit0 + k / a.unit_n) | (k % a.unit_n) << 16;
+        tab[32 + b] = p;
+    }
+    __syncwarp();
+    RowsSeq s{-1, 0, -1, 0};
+    if (tab[lane] >= 0) {
+        s.pre = tab[lane] & 0xffff;
+        s.entry = tab[lane] >> 16;
+        s.len = tab[32 + lane];
+    }
+    u = RowsUnit{};
+    if (lane < a.batch) {
+        u.b = lane;
+        u.m0 = -1;
+        u.n = 1;
+        u.S0 = S0;
+        whole_run(u, S0 + s.len, S0 + L);
+    }
+    const Sums32 own = warp_scan({u.nt > 0 ? 1 : 0, (int)cost(a, u), (int)items(a, u)}, sum);
+    if (u.nt > 0) {
+        put(u, {own.n, own.cost, own.items});
+        s.own = own.n;
+    }
+    if (lane < a.batch) *reinterpret_cast<int4 *>(a.seq + lane) = *reinterpret_cast<int4 *>(&s);
+}
+
 __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs a) {
     pdl_wait();
     if (blockIdx.x > 0) {
@@ -108,7 +225,10 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
     }
     __shared__ Sums sc[kPlanThreads / 32];
     __shared__ int64_t cums[kPlanCum], icums[kPlanCum];
+    __shared__ int2 sizes[kPlanCum];  // tiles, cost of a pair
     __shared__ int32_t small_tab[6 * kPlanSmall];
+    __shared__ int32_t bcast;
+    __shared__ Sums bcast_sum;
     const int tid = threadIdx.x, nthr = blockDim.x;
     int n_pre = 0;
     Sums sum{0, 0, 0};
@@ -119,6 +239,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
         if (at.n < kPlanCum) {
             cums[at.n] = at.cost;
             icums[at.n] = at.items;
+            sizes[at.n] = make_int2(u.nt, u.nt + rows_extra(a, u.n));
         }
     };
     if (!a.prefix) {
@@ -155,6 +276,19 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
             const Sums at = scan(sc, {u.nt > 0 ? 1 : 0, cost(a, u), 0}, sum);
             if (u.nt > 0) put(u, at);
         }
+    } else if (a.small) {
+        // one warp: a lane a group, then an entry, then a sequence
+        if (tid < 32) {
+            Sums32 x{0, 0, 0};
+            small_plan(a, put, x, n_pre, small_tab);
+            if (tid == 0) {
+                bcast = n_pre;
+                bcast_sum = {x.n, x.cost, x.items};
+            }
+        }
+        __syncthreads();
+        n_pre = bcast;
+        sum = bcast_sum;
     } else {
         // (small batches keep the tables in shared memory: the chain of their look-ups is the time)
         int32_t *owner = a.owner, *vm = a.vm, *group = a.entry_group;
@@ -281,7 +415,8 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
         }
     }
     __syncthreads();
-    int64_t per = (sum.cost + a.ctas - 1) / a.ctas;
+    auto share = [&](int64_t x) { return x >> 31 ? (x + a.ctas - 1) / a.ctas : (int64_t)(((uint32_t)x + a.ctas - 1) / (uint32_t)a.ctas); };
+    int64_t per = share(sum.cost);
     if (per < 1) per = 1;
     if (tid == 0) {
         a.head->total = sum.cost;
@@ -289,11 +424,28 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
         a.head->n_units = sum.n;
         a.head->n_pre = n_pre;
     }
+    auto size = [&](int i) {
+        return i < kPlanCum ? sizes[i]
+                            : make_int2(__ldcg(&a.units[i].nt), __ldcg(&a.units[i].nt) + rows_extra(a, __ldcg(&a.units[i].n)));
+    };
+    auto divide = [](int64_t x, int y) { return x >> 31 ? (int32_t)(x / y) : (int32_t)((uint32_t)x / (uint32_t)y); };
     // the last unit that begins at or before x
     auto find = [&](const int64_t *small, auto big, int64_t x) {
         int lo = 0, hi = sum.n;
+        if (hi <= kPlanCum) {  // (no look-ups in memory)
+#pragma unroll 1
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (small[mid] <= x)
+                    lo = mid;
+                else
+                    hi = mid;
+            }
+            return lo;
+        }
+#pragma unroll 1
         while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
+            const int mid = (lo + hi) >> 1;
             if ((mid < kPlanCum ? small[mid] : big(mid)) <= x)
                 lo = mid;
             else
@@ -307,23 +459,23 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
         if (x < sum.cost) {
             auto big = [&](int i) { return __ldcg(&a.units[i].cum); };
             s.unit = find(cums, big, x);
-            const int each = __ldcg(&a.units[s.unit].nt) + rows_extra(a, __ldcg(&a.units[s.unit].n));
+            const int each = size(s.unit).y;
             const int64_t r = x - (s.unit < kPlanCum ? cums[s.unit] : big(s.unit));
-            s.g = (int32_t)(r / each);
-            s.at = (int32_t)(r % each);
+            s.g = divide(r, each);
+            s.at = (int32_t)(r - (int64_t)s.g * each);
             s.n = (int32_t)min(per, sum.cost - x);
         }
         *reinterpret_cast<int4 *>(a.start + c) = *reinterpret_cast<int4 *>(&s);
         if (!a.items) continue;
         RowsItems t{0, 0, 0, 0};
-        const int64_t many = (sum.items + a.ctas - 1) / a.ctas, y = c * many;
+        const int64_t many = share(sum.items), y = c * many;
         if (y < sum.items) {
             auto big = [&](int i) { return __ldcg(a.icum + i); };
             t.unit = find(icums, big, y);
-            const int nt = __ldcg(&a.units[t.unit].nt);
+            const int nt = size(t.unit).x;
             const int64_t r = y - (t.unit < kPlanCum ? icums[t.unit] : big(t.unit));
-            t.sub = (int32_t)(r / nt);
-            t.j = (int32_t)(r % nt);
+            t.sub = divide(r, nt);
+            t.j = (int32_t)(r - (int64_t)t.sub * nt);
             t.n = (int32_t)min(many, sum.items - y);
         }
         *reinterpret_cast<int4 *>(a.items + c) = *reinterpret_cast<int4 *>(&t);
@@ -334,7 +486,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
 
 cudaError_t launch_rows_plan(const RowsArgs &a, cudaStream_t st) {
     const int64_t most = a.prefix ? (int64_t)(a.batch > a.n_groups ? a.batch : a.n_groups) : (int64_t)a.batch * a.seq_units;
-    int threads = 128;
+    int threads = 256;  // (of which each finds where a share begins)
     while (threads < kPlanThreads && threads < most) threads *= 2;
     int ctas = 1;
     if (a.live) {

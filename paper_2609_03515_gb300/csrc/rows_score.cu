@@ -156,6 +156,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                      warp_wait(q_full(st), (J / C::kStages) & 1, abort_flag) &&
                      (J < 2 || warp_wait(s_empty(x), (J / 2 - 1) & 1, abort_flag));
                 if (!ok) break;
+                fence_async_smem();  // (Q came by plain copies)
                 fence_after_sync();
                 const uint64_t dk = dk0 + st * (2 * C::kTile >> 4), dq = dq0 + st * (2 * C::kTile >> 4);
                 if (leader) {
@@ -176,38 +177,49 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         bar_drain(mma_done, 0);
     } else if (warp >= 10) {
-        // ---------------- Q, four lanes a row, and the rows' norms
+        // ---------------- Q, four lanes a row, and the rows' norms.  The copies report to the stage's barrier
+        // themselves, so that the next stage's go out at once: waiting for each took 2 us a product.
         const int th = tid - 320, c = th & 3;
+        constexpr int kHalf = 64 / G, kRows = 8;  // rows a thread: th / 4 + 16 i
         bool ok = true;
         for (; w.left > 0 && ok;) {
             const Item t = w.item(a);
             const int rows = t.n * G;
+            int64_t row[kRows];
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int x = th / 4 + 16 * i, b = x < rows ? member_of(a, t.u, t.m0 + x / G) : -1;
+                row[i] = b >= 0 ? (int64_t)b * a.q_heads + t.g0 * G + x % G : -1;
+            }
             for (int g = 0; g < t.gs && ok; ++g, ++J) {
                 const int st = J % C::kStages;
                 if (J >= C::kStages) ok = bar_wait(empty(st), (J / C::kStages - 1) & 1, abort_flag);
                 if (!ok) break;
-                const uint32_t dst0 = base + st * 2 * C::kTile + C::kTile;
-                float2 *norm = reinterpret_cast<float2 *>(sm + C::kOffNorm) + st * 128;
-#pragma unroll 2
-                for (int i0 = th / 4; i0 < rows; i0 += 16) {
-                    const int b = member_of(a, t.u, t.m0 + i0 / G);
-                    const int64_t row = (int64_t)max(b, 0) * a.q_heads + (t.g0 + g) * G + i0 % G;
-                    const int r = i0 < 64 / G * G ? i0 : i0 - 64 / G * G + 64;  // its column of S^T
-                    const T *src = static_cast<const T *>(a.q) + row * D + 8 * c;
+                const uint32_t dst0 = base + st * 2 * C::kTile + C::kTile, norm = base + C::kOffNorm + st * 128 * 8;
 #pragma unroll
-                    for (int i = 0; i < D / 32; ++i)
+                for (int i = 0; i < kRows; ++i) {
+                    const int x = th / 4 + 16 * i;
+                    if (x >= rows) break;
+                    const int r = x < kHalf * G ? x : x - kHalf * G + 64;  // its column of S^T
+                    const bool real = row[i] >= 0;
+                    const int64_t at = real ? row[i] + g * G : 0;
+                    const T *src = static_cast<const T *>(a.q) + at * D + 8 * c;
+#pragma unroll
+                    for (int k = 0; k < D / 32; ++k)
                         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                         dst0 + (i >> 1) * kAtom + r * 128 + ((((c + 4 * i) ^ r) & 7) << 4)),
-                                     "l"(src + 32 * i), "r"(b >= 0 ? 16 : 0)
+                                         dst0 + (k >> 1) * kAtom + r * 128 + ((((c + 4 * k) ^ r) & 7) << 4)),
+                                     "l"(src + 32 * k), "r"(real ? 16 : 0)
                                      : "memory");
-                    if (c == 0) norm[r] = b >= 0 ? __ldcg(a.norm + row) : make_float2(0.f, 0.f);
+                    if (c == 0)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(norm + 8 * r), "l"(a.norm + at),
+                                     "r"(real ? 8 : 0)
+                                     : "memory");
                 }
-                asm volatile("cp.async.wait_all;" ::: "memory");
-                fence_async_smem();
-                mbar_arrive(q_full(st));
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(q_full(st)) : "memory");
             }
             w.next(a, t.u);
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
         // ---------------- weights: a thread a slot, half of the columns
         constexpr int kMembers = 64 / G;  // of a thread's 64 columns; G = 7 uses 63
@@ -219,6 +231,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Item t = w.item(a);
             const int slot = t.t0 + (warp & 3) * 32 + lane, m1 = half * kMembers;
             const int mine = min(max(t.n - m1, 0), kMembers);  // members of this half
+            // (looked up ahead, a lane a member, and so are their slots' liveness and old utilities below: between the
+            // stores each would wait for memory by itself)
+            int who[(kMembers + 31) / 32];
+#pragma unroll
+            for (int k = 0; k < (kMembers + 31) / 32; ++k)
+                who[k] = lane + 32 * k < mine ? member_of(a, t.u, t.m0 + m1 + lane + 32 * k) : -1;
             float sum[kMembers];
 #pragma unroll
             for (int m = 0; m < kMembers; ++m) sum[m] = 0.f;
@@ -250,20 +268,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mbar_arrive(s_empty(x));
                 mbar_arrive(empty(st));
             }
-            if (ok && slot >= t.u.lo && slot < t.u.hi) {
-                const int j = slot - t.u.S0;
-                const float inv = 1.f / (float)(t.gs > 1 || rps == 1 ? a.q_heads : G);
+            const bool inside = ok && slot >= t.u.lo && slot < t.u.hi;
+            const int j = slot - t.u.S0;
+            const float inv = 1.f / (float)(rps == 1 ? a.q_heads : G);
+            constexpr int kTogether = kMembers < 8 ? kMembers : 8;
 #pragma unroll
-                for (int m = 0; m < kMembers; ++m)
-                    if (m < mine) {
-                        const int b = member_of(a, t.u, t.m0 + m1 + m);
-                        if (b >= 0) {
-                            const int64_t r = (int64_t)b * rps + (rps > 1 ? t.g0 : 0);
-                            const bool live = !a.live || (__ldcg(a.live + r * a.live_words + (j >> 5)) >> (j & 31)) & 1u;
-                            const float s = live ? sum[m] * inv : 0.f;
-                            if (sc.score) sc.score[r * a.cap + j] = s;
-                            if (sc.ema) sc.ema[r * a.cap + j] = sc.alpha * sc.ema[r * a.cap + j] + (1.f - sc.alpha) * s;
-                        }
+            for (int m0 = 0; m0 < kMembers; m0 += kTogether) {
+                int64_t at[kTogether];
+                float old[kTogether];
+                uint32_t live[kTogether];
+#pragma unroll
+                for (int k = 0; k < kTogether; ++k) {
+                    const int m = m0 + k;
+                    at[k] = -1;
+                    if (m >= kMembers || m >= mine) continue;
+                    const int b = __shfl_sync(0xffffffffu, who[m / 32], m % 32);
+                    const int64_t r = (int64_t)b * rps + (rps > 1 ? t.g0 : 0);
+                    if (b < 0 || !inside) continue;
+                    at[k] = r * a.cap + j;
+                    live[k] = a.live ? __ldcg(a.live + r * a.live_words + (j >> 5)) >> (j & 31) : 1u;
+                    if (sc.ema) old[k] = sc.ema[at[k]];
+                }
+#pragma unroll
+                for (int k = 0; k < kTogether; ++k)
+                    if (m0 + k < kMembers && at[k] >= 0) {
+                        const float s = live[k] & 1u ? sum[m0 + k < kMembers ? m0 + k : 0] * inv : 0.f;
+                        if (sc.score) sc.score[at[k]] = s;
+                        if (sc.ema) sc.ema[at[k]] = sc.alpha * old[k] + (1.f - sc.alpha) * s;
                     }
             }
             w.next(a, t.u);
