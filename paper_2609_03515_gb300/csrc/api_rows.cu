@@ -108,7 +108,9 @@ RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, 
     if (tc && p) {
         // (64 columns a thread: an item's members, half of them each, are 2 (64 / G))
         a.item_n = 2 * (64 / a.group);
-        a.item_subs = a.rows_per_seq > 1 ? s->kv_heads : 1;
+        // a utility row a KV head: an item each while there are few, else one for all of them, which looks up its
+        // unit and members once
+        a.item_subs = a.rows_per_seq > 1 && (int64_t)s->batch * (c->max_len / kRowsTile + 1) < 4 * a.ctas ? s->kv_heads : 1;
         take(a.items, a.ctas);
         take(a.icum, units);
         if (!score) {

@@ -8,7 +8,7 @@
 namespace ikv {
 namespace {
 
-constexpr int kMergeThreads = 128, kMergeRows = 8, kMergeAhead = 8;
+constexpr int kMergeRows = 8, kMergeAhead = 8;
 
 __device__ __forceinline__ RowsHead rows_head(const RowsArgs &a) {
     RowsHead h;
@@ -22,73 +22,79 @@ __device__ __forceinline__ int64_t divide(int64_t x, int64_t y) {
     return (x | y) >> 31 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
 }
 
-// n parts of `rows` <= 8 rows: (max, sum) of part i of row r at ml(i)[r], its channels 4 c .. at o(i)[c * step(i)
-// + 4 r].  done(r, ref, W): row r's maximum and sum; out(r): its output.
-template <int D, typename T, typename ML, typename O, typename Step, typename Done, typename Out>
-__device__ __forceinline__ void merge_rows(int n, int rows, ML ml, O o, Step step, Done done, Out out) {
-    constexpr int kChunks = D / 4, kIter = kChunks * kMergeRows / kMergeThreads;
-    __shared__ float wq[kMergeRows][32], top[kMergeRows], total[kMergeRows];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+// n parts that lie one behind another: (max, sum) of row r of part i at ml[i * sm + r], channels 4 c .. of it at
+// o[i * so + c * step + 4 r]
+struct Run {
+    const float2 *ml;
+    const float *o;
+    int n, sm, so, step;
+    __device__ __forceinline__ float2 sum(int i, int r) const { return __ldcg(ml + (int64_t)i * sm + r); }
+    __device__ __forceinline__ float4 out(int i, int r, int c) const {
+        return __ldcg(reinterpret_cast<const float4 *>(o + (int64_t)i * so + (c * step + 4 * r)));
+    }
+};
+
+// The parts of x, then those of y, of up to 8 rows: a thread four channels of a row (2 D threads).
+// done(r, M, 1 / W): row r's maximum and sum, out(r): its output.
+template <int D, typename T, typename Done, typename Out>
+__device__ __forceinline__ void merge_rows(const Run &x, const Run &y, int rows, Done done, Out out) {
+    __shared__ float wq[kMergeRows][32], top[kMergeRows], inverse[kMergeRows];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n = x.n + y.n;
     const int row = tid % kMergeRows, chunk = tid / kMergeRows;
-    float4 early[kIter][kMergeAhead];
+    auto part = [&](int i) { return i < x.n ? x.out(i, row, chunk) : y.out(i - x.n, row, chunk); };
+    float4 early[kMergeAhead];
+    const int ahead = row < rows ? min(n, kMergeAhead) : 0;
 #pragma unroll
-    for (int k = 0; k < kIter; ++k)
-#pragma unroll
-        for (int i = 0; i < kMergeAhead; ++i)
-            if (i < n && row < rows)
-                early[k][i] = __ldcg(reinterpret_cast<const float4 *>(
-                    o(i) + (int64_t)(chunk + k * (kChunks / kIter)) * step(i) + 4 * row));
-    for (int r = warp; r < rows; r += kMergeThreads / 32) {
-        float2 x0 = make_float2(-INFINITY, 0.f);
-        if (lane < n) x0 = __ldcg(ml(lane) + r);
-        float M = x0.x;
-        for (int i = lane + 32; i < n; i += 32) M = fmaxf(M, __ldcg(ml(i) + r).x);
+    for (int i = 0; i < kMergeAhead; ++i)
+        if (i < ahead) early[i] = part(i);
+    auto sums = [&](int i, int r) { return i < x.n ? x.sum(i, r) : y.sum(i - x.n, r); };
+    for (int r = warp; r < rows; r += 2 * D / 32) {
+        float2 s0 = make_float2(-INFINITY, 0.f);
+        if (lane < n) s0 = sums(lane, r);
+        float M = s0.x;
+        for (int i = lane + 32; i < n; i += 32) M = fmaxf(M, sums(i, r).x);
         M = warp_max(M);
         const float ref = M == -INFINITY ? 0.f : M;
-        float W = 0.f;
-        for (int i = lane; i < n; i += 32) {
-            const float2 x = i == lane ? x0 : __ldcg(ml(i) + r);
-            const float f = exp2f(x.x - ref);
-            W += x.y * f;
-            if (i == lane) wq[r][i] = f;
+        const float f = exp2f(s0.x - ref);
+        float W = s0.y * f;
+        wq[r][lane] = f;
+        for (int i = lane + 32; i < n; i += 32) {
+            const float2 s = sums(i, r);
+            W += s.y * exp2f(s.x - ref);
         }
         W = warp_sum(W);
         if (lane == 0) {
-            total[r] = W;
+            const float inv = W == 0.f ? 0.f : 1.f / W;  // (a NaN sum leaves NaN)
+            inverse[r] = inv;
             top[r] = ref;
-            done(r, ref, W);
+            done(r, ref, inv);
         }
     }
     __syncthreads();
     if (row < rows) {
-        const float W = total[row], ref = top[row];
-        T *dst = out(row);
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        auto add = [&](float f, float4 v) {
+            acc[0] += f * v.x;
+            acc[1] += f * v.y;
+            acc[2] += f * v.z;
+            acc[3] += f * v.w;
+        };
 #pragma unroll
-        for (int k = 0; k < kIter; ++k) {
-            const int c = chunk + k * (kChunks / kIter);
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
-            auto add = [&](int i, float4 v) {
-                const float f = i < 32 ? wq[row][i] : exp2f(__ldcg(ml(i) + row).x - ref);
-                acc[0] += f * v.x;
-                acc[1] += f * v.y;
-                acc[2] += f * v.z;
-                acc[3] += f * v.w;
-            };
+        for (int i = 0; i < kMergeAhead; ++i)
+            if (i < ahead) add(wq[row][i], early[i]);
+        for (int i0 = kMergeAhead; i0 < n; i0 += kMergeAhead) {
+            float4 v[kMergeAhead];
 #pragma unroll
             for (int i = 0; i < kMergeAhead; ++i)
-                if (i < n) add(i, early[k][i]);
-            for (int i0 = kMergeAhead; i0 < n; i0 += kMergeAhead) {
-                float4 v[kMergeAhead];
+                if (i0 + i < n) v[i] = part(i0 + i);
 #pragma unroll
-                for (int i = 0; i < kMergeAhead; ++i)
-                    if (i0 + i < n)
-                        v[i] = __ldcg(reinterpret_cast<const float4 *>(o(i0 + i) + (int64_t)c * step(i0 + i) + 4 * row));
-#pragma unroll
-                for (int i = 0; i < kMergeAhead; ++i)
-                    if (i0 + i < n) add(i0 + i, v[i]);
-            }
-            store4(dst + 4 * c, over_sum(acc[0], W), over_sum(acc[1], W), over_sum(acc[2], W), over_sum(acc[3], W));
+            for (int i = 0; i < kMergeAhead; ++i)
+                if (i0 + i < n) add(i0 + i < 32 ? wq[row][i0 + i] : exp2f(sums(i0 + i, row).x - top[row]), v[i]);
         }
+        const float inv = inverse[row];
+        // (an infinite output times 1 / W stays what it is; a sum of weights of 0 leaves 0)
+        if (inv == 0.f) acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+        store4(out(row) + 4 * chunk, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
     }
     __syncthreads();
 }
@@ -96,7 +102,7 @@ __device__ __forceinline__ void merge_rows(int n, int rows, ML ml, O o, Step ste
 // Grid: (CTAs of the attention, row blocks).  CTA c: the pair that the border in front of share c cuts,
 // if no earlier border cuts it.
 template <int D, typename T>
-__global__ void __launch_bounds__(kMergeThreads) rows_merge_window_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(2 * D) rows_merge_window_kernel(const RowsArgs a) {
     pdl_wait();
     const int c = blockIdx.x;
     RowsWalk w;
@@ -108,19 +114,20 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_window_kernel(const 
     if (j == 0 || j > per) return;  // (beyond: the share in front of this one begins behind the pair's first tile)
     const int n = 1 + (int)divide(u.nt - j + per - 1, per);  // parts: share c - 1's and those behind
     const int rows = u.n * a.group;
-    auto slot = [&](int i) { return i == 0 ? 2 * (int64_t)(c - 1) + 1 : 2 * (int64_t)(c + i - 1); };
+    const int so = a.rows_cap * D;
     for (int r0 = blockIdx.y * kMergeRows; r0 < rows; r0 += gridDim.y * kMergeRows) {
-        merge_rows<D, T>(
-            n, min(kMergeRows, rows - r0), [&](int i) { return a.part_ml + slot(i) * a.rows_cap + r0; },
-            [&](int i) { return a.part_o + slot(i) * a.rows_cap * D + 4 * r0; }, [&](int) { return 4 * a.rows_cap; },
-            [](int, float, float) {},
-            [&](int r) { return static_cast<T *>(a.out) + rows_row<D>(a, u, w.g, r0 + r).out; });
+        auto run = [&](int slot, int parts) {
+            return Run{a.part_ml + (int64_t)slot * a.rows_cap + r0, a.part_o + (int64_t)slot * so + 4 * r0, parts,
+                       2 * a.rows_cap, 2 * so, 4 * a.rows_cap};
+        };
+        merge_rows<D, T>(run(2 * (c - 1) + 1, 1), run(2 * c, n - 1), min(kMergeRows, rows - r0), [](int, float, float) {},
+                         [&](int r) { return static_cast<T *>(a.out) + rows_row<D>(a, u, w.g, r0 + r).out; });
     }
 }
 
 // A CTA a (sequence, KV head)
 template <int D, typename T>
-__global__ void __launch_bounds__(kMergeThreads) rows_merge_prefix_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(2 * D) rows_merge_prefix_kernel(const RowsArgs a) {
     pdl_wait();
     const int hk = a.pv.kv_heads, b = blockIdx.x / hk, g = blockIdx.x % hk;
     const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.seq) + b);
@@ -139,27 +146,22 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_prefix_kernel(const 
     };
     if (s.x >= 0) np = parts(pre, (int64_t)s.x * hk, slot_p);
     if (s.z >= 0) no = parts(own, (int64_t)(s.z - head.n_pre) * hk, slot_o);
-    const int rp = s.y * a.group;  // the pre part's rows
+    const int rp = s.y * a.group, so = a.rows_cap * D, sw = a.group * D;  // rp: the pre part's rows
     const int64_t row0 = (int64_t)b * a.q_heads + g * a.group;
     merge_rows<D, T>(
-        np + no, a.group,
-        [&](int i) { return i < np ? a.part_ml + (slot_p + i) * a.rows_cap + rp : a.own_ml + (slot_o + i - np) * a.group; },
-        [&](int i) {
-            return i < np ? a.part_o + (slot_p + i) * a.rows_cap * D + 4 * rp : a.own_o + (slot_o + i - np) * a.group * D;
-        },
-        [&](int i) { return 4 * (i < np ? a.rows_cap : a.group); },
-        // (a NaN sum leaves a NaN, for the scores to be NaN too)
-        [&](int r, float ref, float W) { a.norm[row0 + r] = make_float2(ref, W == 0.f ? 0.f : 1.f / W); },
+        Run{a.part_ml + slot_p * a.rows_cap + rp, a.part_o + slot_p * so + 4 * rp, np, a.rows_cap, so, 4 * a.rows_cap},
+        Run{a.own_ml + slot_o * a.group, a.own_o + slot_o * sw, no, a.group, sw, 4 * a.group}, a.group,
+        [&](int r, float ref, float inv) { a.norm[row0 + r] = make_float2(ref, inv); },
         [&](int r) { return static_cast<T *>(a.out) + (row0 + r) * D; });
 }
 
 template <int D, typename T>
 cudaError_t launch_merge(const RowsArgs &a, cudaStream_t st) {
     if (a.prefix)
-        return launch_k(rows_merge_prefix_kernel<D, T>, dim3((unsigned)(a.batch * a.pv.kv_heads)), dim3(kMergeThreads), 0,
+        return launch_k(rows_merge_prefix_kernel<D, T>, dim3((unsigned)(a.batch * a.pv.kv_heads)), dim3(2 * D), 0,
                         st, a);
     const int y = (a.rows_cap + kMergeRows - 1) / kMergeRows;
-    return launch_k(rows_merge_window_kernel<D, T>, dim3(a.ctas, y), dim3(kMergeThreads), 0, st, a);
+    return launch_k(rows_merge_window_kernel<D, T>, dim3(a.ctas, y), dim3(2 * D), 0, st, a);
 }
 
 // Scores without tensor cores: K once more, with each row's maximum M and sum of weights W,

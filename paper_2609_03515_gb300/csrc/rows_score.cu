@@ -22,9 +22,10 @@ template <int D>
 struct Sc {
     static constexpr int kTile = kAtom * (D / 64);  // bytes of K, of Q
     static constexpr int kStages = 3;
-    static constexpr int kOffNorm = kStages * 2 * kTile;  // (M, 1 / W) of a stage's rows
-    static constexpr int kOffBar = kOffNorm + kStages * 128 * 8;
-    static constexpr int kBars = 3 * kStages + 5;
+    static constexpr int kOffNorm = kStages * 2 * kTile;  // (M, 1 / W) of a product's rows
+    static constexpr int kNorms = 8;  // Q may be three products ahead of the products, and they two ahead of the weights
+    static constexpr int kOffBar = kOffNorm + kNorms * 128 * 8;
+    static constexpr int kBars = 3 * kStages + 5 + kNorms;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
     static constexpr int kSmem = kOffMisc + 16 + 1024;
 };
@@ -81,23 +82,25 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t bar0 = base + C::kOffBar;
     auto k_full = [&](int i) { return bar0 + 8u * i; };
     auto q_full = [&](int i) { return bar0 + 8u * (C::kStages + i); };
-    auto empty = [&](int i) { return bar0 + 8u * (2 * C::kStages + i); };  // K's, Q's and the norms' stage
+    auto empty = [&](int i) { return bar0 + 8u * (2 * C::kStages + i); };  // K's and Q's stage
     const uint32_t bar1 = bar0 + 8u * (3 * C::kStages);
     auto s_full = [&](int x) { return bar1 + 8u * x; };
     auto s_empty = [&](int x) { return bar1 + 16u + 8u * x; };
     const uint32_t mma_done = bar1 + 32u;
+    auto n_full = [&](int i) { return bar1 + 40u + 8u * i; };  // a product's norms
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + C::kOffMisc + 4);
     if (warp == 8 && lane == 0) {
         for (int i = 0; i < C::kStages; ++i) {
             mbar_init(k_full(i), 1);
             mbar_init(q_full(i), 64);
-            mbar_init(empty(i), 256 + 1);  // the products and every thread that reads norms
+            mbar_init(empty(i), 1);
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(s_full(x), 1);
             mbar_init(s_empty(x), 256);
         }
+        for (int i = 0; i < C::kNorms; ++i) mbar_init(n_full(i), 64);
         mbar_init(mma_done, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -195,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int st = J % C::kStages;
                 if (J >= C::kStages) ok = bar_wait(empty(st), (J / C::kStages - 1) & 1, abort_flag);
                 if (!ok) break;
-                const uint32_t dst0 = base + st * 2 * C::kTile + C::kTile, norm = base + C::kOffNorm + st * 128 * 8;
+                const uint32_t dst0 = base + st * 2 * C::kTile + C::kTile, norm = base + C::kOffNorm + J % C::kNorms * 128 * 8;
 #pragma unroll
                 for (int i = 0; i < kRows; ++i) {
                     const int x = th / 4 + 16 * i;
@@ -216,6 +219,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                      : "memory");
                 }
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(q_full(st)) : "memory");
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(n_full(J % C::kNorms)) : "memory");
             }
             w.next(a, t.u);
         }
@@ -223,6 +227,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
         // ---------------- weights: a thread a slot, half of the columns
         constexpr int kMembers = 64 / G;  // of a thread's 64 columns; G = 7 uses 63
+        constexpr int kBlockM = kMembers < 8 ? kMembers : 8;
         const int half = warp >> 2;
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
         const int rps = a.rows_per_seq;
@@ -237,16 +242,32 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int k = 0; k < (kMembers + 31) / 32; ++k)
                 who[k] = lane + 32 * k < mine ? member_of(a, t.u, t.m0 + m1 + lane + 32 * k) : -1;
+            const bool inside = ok && slot >= t.u.lo && slot < t.u.hi;
+            const int j = slot - t.u.S0;
+            const float inv = 1.f / (float)(rps == 1 ? a.q_heads : G);
             float sum[kMembers];
 #pragma unroll
             for (int m = 0; m < kMembers; ++m) sum[m] = 0.f;
             for (int g = 0; g < t.gs; ++g, ++J) {
-                const int st = J % C::kStages, x = J & 1;
-                if (ok) ok = bar_wait(q_full(st), (J / C::kStages) & 1, abort_flag);  // (the norms)
+                const int x = J & 1;
+                const bool out = rps > 1 || g == t.gs - 1;  // the sums are complete behind this product
+                uint64_t dead = 0;
+                if (out && a.live) {
+#pragma unroll
+                    for (int m = 0; m < kMembers; ++m) {
+                        const int b = __shfl_sync(0xffffffffu, who[m / 32], m % 32);
+                        if (inside && b >= 0 &&
+                            !((__ldcg(a.live + ((int64_t)b * rps + (rps > 1 ? t.g0 + g : 0)) * a.live_words + (j >> 5)) >> (j & 31)) & 1u))
+                            dead |= 1ull << m;
+                        if (m % kBlockM == kBlockM - 1 && m + 1 >= mine) break;
+                    }
+                }
+                // (not Q's stage, which may be full again by now)
+                if (ok) ok = bar_wait(n_full(J % C::kNorms), (J / C::kNorms) & 1, abort_flag);
                 if (ok) ok = bar_wait(s_full(x), (J / 2) & 1, abort_flag);
                 ok = __all_sync(0xffffffffu, ok);
                 fence_after_sync();
-                const float2 *norm = reinterpret_cast<const float2 *>(sm + C::kOffNorm) + st * 128 + 64 * half;
+                const float2 *norm = reinterpret_cast<const float2 *>(sm + C::kOffNorm) + J % C::kNorms * 128 + 64 * half;
                 if (ok && mine > 0) {
                     uint32_t v[64];
                     const uint32_t at = tmem + 128 * x + lane_off + 64 * half;
@@ -254,48 +275,52 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (mine * G > 32) tmem_ld32(at + 32, v + 32);
                     tmem_wait_ld(v);
                     if (mine * G > 32) tmem_wait_ld(v + 32);
+                    // (a block of members at once, those that are not there too: a branch for each would put their
+                    // look-ups and exponentials one behind another)
 #pragma unroll
-                    for (int m = 0; m < kMembers; ++m)
-                        if (m < mine) {
+                    for (int m0 = 0; m0 < kMembers; m0 += kBlockM)
+                        if (m0 < mine) {
 #pragma unroll
-                            for (int h = 0; h < G; ++h) {
-                                const float2 mw = norm[m * G + h];
-                                sum[m] += ex2(__fmaf_rn(__uint_as_float(v[m * G + h]), a.scale_log2, -mw.x)) * mw.y;
+                            for (int m = m0; m < m0 + kBlockM && m < kMembers; ++m) {
+                                float w4 = 0.f;
+#pragma unroll
+                                for (int h = 0; h < G; ++h) {
+                                    const float2 mw = norm[m * G + h];
+                                    w4 = __fmaf_rn(ex2(__fmaf_rn(__uint_as_float(v[m * G + h]), a.scale_log2, -mw.x)), mw.y, w4);
+                                }
+                                sum[m] += w4;
                             }
                         }
                 }
                 fence_before_sync();
                 mbar_arrive(s_empty(x));
-                mbar_arrive(empty(st));
-            }
-            const bool inside = ok && slot >= t.u.lo && slot < t.u.hi;
-            const int j = slot - t.u.S0;
-            const float inv = 1.f / (float)(rps == 1 ? a.q_heads : G);
-            constexpr int kTogether = kMembers < 8 ? kMembers : 8;
+                if (out) {
 #pragma unroll
-            for (int m0 = 0; m0 < kMembers; m0 += kTogether) {
-                int64_t at[kTogether];
-                float old[kTogether];
-                uint32_t live[kTogether];
+                    for (int m0 = 0; m0 < kMembers; m0 += kBlockM) {
+                        if (m0 >= mine) continue;
+                        int64_t at[kBlockM];
+                        float old[kBlockM];
 #pragma unroll
-                for (int k = 0; k < kTogether; ++k) {
-                    const int m = m0 + k;
-                    at[k] = -1;
-                    if (m >= kMembers || m >= mine) continue;
-                    const int b = __shfl_sync(0xffffffffu, who[m / 32], m % 32);
-                    const int64_t r = (int64_t)b * rps + (rps > 1 ? t.g0 : 0);
-                    if (b < 0 || !inside) continue;
-                    at[k] = r * a.cap + j;
-                    live[k] = a.live ? __ldcg(a.live + r * a.live_words + (j >> 5)) >> (j & 31) : 1u;
-                    if (sc.ema) old[k] = sc.ema[at[k]];
-                }
+                        for (int k = 0; k < kBlockM; ++k) {
+                            const int m = m0 + k < kMembers ? m0 + k : 0;
+                            const int b = __shfl_sync(0xffffffffu, who[m / 32], m % 32);  // (-1 where m >= mine)
+                            at[k] = m0 + k < kMembers && b >= 0 && inside
+                                        ? ((int64_t)b * rps + (rps > 1 ? t.g0 + g : 0)) * a.cap + j
+                                        : -1;
+                            if (sc.ema && at[k] >= 0) old[k] = sc.ema[at[k]];
+                        }
 #pragma unroll
-                for (int k = 0; k < kTogether; ++k)
-                    if (m0 + k < kMembers && at[k] >= 0) {
-                        const float s = live[k] & 1u ? sum[m0 + k < kMembers ? m0 + k : 0] * inv : 0.f;
-                        if (sc.score) sc.score[at[k]] = s;
-                        if (sc.ema) sc.ema[at[k]] = sc.alpha * old[k] + (1.f - sc.alpha) * s;
+                        for (int k = 0; k < kBlockM; ++k) {
+                            const int m = m0 + k < kMembers ? m0 + k : 0;
+                            if (at[k] >= 0) {
+                                const float s = (dead >> m) & 1ull ? 0.f : sum[m] * inv;
+                                if (sc.score) sc.score[at[k]] = s;
+                                if (sc.ema) sc.ema[at[k]] = sc.alpha * old[k] + (1.f - sc.alpha) * s;
+                            }
+                            if (m0 + k < kMembers) sum[m] = 0.f;
+                        }
                     }
+                }
             }
             w.next(a, t.u);
         }
