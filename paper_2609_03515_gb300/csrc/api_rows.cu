@@ -68,8 +68,8 @@ RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, 
     if (a.ctas > kRowsMaxCtas) a.ctas = kRowsMaxCtas;
     const int n = p ? s->batch : w->max_count;
     const int most = tc ? 2 * (128 / a.group) : kRowsSimt / a.group;  // (tensor cores: two row tiles)
-    a.unit_n = most;
     a.tile_n = tc ? 128 / a.group : most;
+    a.unit_n = n <= a.tile_n ? a.tile_n : most;
     a.rows_cap = (n < most ? n : most) * a.group;
     int64_t units;
     if (w) {

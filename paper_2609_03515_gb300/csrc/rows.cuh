@@ -33,9 +33,14 @@ struct RowsUnit {                   // 64 bytes
     int64_t cum;                    // cost of all earlier units, for all KV heads
 };
 
-// Cost is counted in tiles.  Besides its own a pair costs one or two for its first products, which nothing
-// overlaps, and its output: two where its rows fill two row tiles of the tensor-core kernel.
-constexpr int kRowsOne = 1, kRowsTwo = 2;
+// What a tile of a pair (unit, KV head) costs, and what the pair costs besides, for its first products, which
+// nothing overlaps, and its output.  In the tensor-core kernel a tile took 1.0 to 1.4 us with one row tile and 1.4 to
+// 1.6 with two, a pair besides 2.2 to 3.4 and 4.5 to 5.5.  (Shares of tiles alone: a window of 2k over 8k tokens
+// 290 us a call instead of 223, the CTA with the shortest pairs 40% behind the others.)
+struct RowsCost {
+    int32_t tile, extra;
+};
+constexpr int kTileOne = 3, kExtraOne = 6, kTileTwo = 4, kExtraTwo = 12;
 
 struct alignas(16) RowsHead {
     int64_t total, per;             // cost in all, of a CTA's share
@@ -114,33 +119,6 @@ __device__ __forceinline__ int64_t rows_slot(const RowsArgs &a, const RowsHead &
 // The tile of a unit
 __device__ __forceinline__ int rows_tile(const RowsUnit &u, int i) { return i < u.n_a ? u.t_a + i : u.t_w + i - u.n_a; }
 
-__device__ __forceinline__ int rows_extra(const RowsArgs &a, int n) { return n > a.tile_n ? kRowsTwo : kRowsOne; }
-
-// The parts of a share, in turn.  A pair's extra cost lies in front of its tiles; a border in it cuts nothing.
-struct RowsWalk {
-    int32_t unit, g, at, left;      // the share goes on at cost `at` of pair (unit, g)
-    __device__ __forceinline__ void begin(const RowsArgs &a, int cta) {
-        const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.start) + cta);
-        unit = s.x;
-        g = s.y;
-        at = s.z;
-        left = s.w;
-    }
-    // The next part: from tile j, n tiles (none: the share is done), of a unit of nt tiles and un tokens
-    __device__ __forceinline__ int first(const RowsArgs &a, int un) const { return max(at - rows_extra(a, un), 0); }
-    __device__ __forceinline__ int part(const RowsArgs &a, int nt, int un) const {
-        const int e = rows_extra(a, un);
-        return min(nt - max(at - e, 0), left - max(e - at, 0));
-    }
-    __device__ __forceinline__ void next(const RowsArgs &a, int nt, int un) {
-        left -= nt + rows_extra(a, un) - at;
-        at = 0;
-        if (++g == a.pv.kv_heads) {
-            g = 0;
-            ++unit;
-        }
-    }
-};
 __device__ __forceinline__ RowsUnit rows_unit(const RowsArgs &a, int unit) {
     RowsUnit u;
     const int4 *p = reinterpret_cast<const int4 *>(a.units + unit);
@@ -150,6 +128,39 @@ __device__ __forceinline__ RowsUnit rows_unit(const RowsArgs &a, int unit) {
     return u;
 }
 
+__device__ __forceinline__ RowsCost rows_cost(const RowsArgs &a, int n) { return n > a.tile_n ? RowsCost{kTileTwo, kExtraTwo} : RowsCost{kTileOne, kExtraOne}; }
+__device__ __forceinline__ int64_t pair_cost(const RowsCost &c, int nt) { return c.extra + (int64_t)c.tile * nt; }
+// The first tile of a pair that begins at its cost `at` or behind: a border there cuts in front of it
+__device__ __forceinline__ int tile_at(const RowsCost &c, int64_t at) {
+    return at <= c.extra ? 0 : (int)((uint32_t)(at - c.extra + c.tile - 1) / (uint32_t)c.tile);
+}
+
+// The parts of a share, in turn: while (left > 0) { part(); next(); }
+struct RowsWalk {
+    int32_t unit, g;                // the share goes on at cost `at` of pair (unit, g)
+    int32_t at, left;
+    __device__ __forceinline__ void begin(const int4 &s) {
+        unit = s.x;
+        g = s.y;
+        at = s.z;
+        left = s.w;
+    }
+    // the share's tiles of the pair: n (or none) from j0 on
+    __device__ __forceinline__ int part(const RowsArgs &a, const RowsUnit &u, int &j0) const {
+        const RowsCost c = rows_cost(a, u.n);
+        j0 = tile_at(c, at);
+        const int64_t end = (int64_t)at + left;
+        return (end >= pair_cost(c, u.nt) ? u.nt : min(tile_at(c, end), u.nt)) - min(j0, u.nt);
+    }
+    __device__ __forceinline__ void next(const RowsArgs &a, const RowsUnit &u) {
+        left = (int32_t)max(left - (pair_cost(rows_cost(a, u.n), u.nt) - at), (int64_t)0);
+        at = 0;
+        if (++g == a.pv.kv_heads) {
+            g = 0;
+            ++unit;
+        }
+    }
+};
 // What row r of a unit sees: slots s of [lo, hi] with s >= wlo or s < sh, live ones.  seq < 0: not a row.
 struct RowsRow {
     int32_t seq;                    // its sequence

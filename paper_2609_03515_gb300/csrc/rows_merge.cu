@@ -8,7 +8,7 @@
 namespace ikv {
 namespace {
 
-constexpr int kMergeRows = 8, kMergeAhead = 8;
+constexpr int kMergeRows = 8;
 
 __device__ __forceinline__ RowsHead rows_head(const RowsArgs &a) {
     RowsHead h;
@@ -34,85 +34,72 @@ struct Run {
     }
 };
 
-// The parts of x, then those of y, of up to 8 rows: a thread four channels of a row (2 D threads).
-// done(r, M, 1 / W): row r's maximum and sum, out(r): its output.
-template <int D, typename T, typename Done, typename Out>
+// The parts of x, then those of y, of up to 8 rows: a thread four channels of a row (2 D threads), kAhead parts at a
+// time.  Every thread looks up its row's maxima and sums itself, so that they come with the outputs and nothing is
+// exchanged.  done(r, M, 1 / W): row r's maximum and sum, out(r): its output.
+template <int D, typename T, int kAhead, typename Done, typename Out>
 __device__ __forceinline__ void merge_rows(const Run &x, const Run &y, int rows, Done done, Out out) {
-    __shared__ float wq[kMergeRows][32], top[kMergeRows], inverse[kMergeRows];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n = x.n + y.n;
-    const int row = tid % kMergeRows, chunk = tid / kMergeRows;
-    auto part = [&](int i) { return i < x.n ? x.out(i, row, chunk) : y.out(i - x.n, row, chunk); };
-    float4 early[kMergeAhead];
-    const int ahead = row < rows ? min(n, kMergeAhead) : 0;
+    const int row = threadIdx.x % kMergeRows, chunk = threadIdx.x / kMergeRows, n = x.n + y.n;
+    if (row >= rows) return;
+    float M = -INFINITY, W = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
+        float2 s[kAhead];
+        float4 v[kAhead];
 #pragma unroll
-    for (int i = 0; i < kMergeAhead; ++i)
-        if (i < ahead) early[i] = part(i);
-    auto sums = [&](int i, int r) { return i < x.n ? x.sum(i, r) : y.sum(i - x.n, r); };
-    for (int r = warp; r < rows; r += 2 * D / 32) {
-        float2 s0 = make_float2(-INFINITY, 0.f);
-        if (lane < n) s0 = sums(lane, r);
-        float M = s0.x;
-        for (int i = lane + 32; i < n; i += 32) M = fmaxf(M, sums(i, r).x);
-        M = warp_max(M);
-        const float ref = M == -INFINITY ? 0.f : M;
-        const float f = exp2f(s0.x - ref);
-        float W = s0.y * f;
-        wq[r][lane] = f;
-        for (int i = lane + 32; i < n; i += 32) {
-            const float2 s = sums(i, r);
-            W += s.y * exp2f(s.x - ref);
+        for (int i = 0; i < kAhead; ++i) {
+            s[i] = make_float2(-INFINITY, 0.f);
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i0 + i < n) {
+                const bool in_x = i0 + i < x.n;
+                const Run &z = in_x ? x : y;
+                const int k = in_x ? i0 + i : i0 + i - x.n;
+                s[i] = z.sum(k, row);
+                v[i] = z.out(k, row, chunk);
+            }
         }
-        W = warp_sum(W);
-        if (lane == 0) {
-            const float inv = W == 0.f ? 0.f : 1.f / W;  // (a NaN sum leaves NaN)
-            inverse[r] = inv;
-            top[r] = ref;
-            done(r, ref, inv);
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) top = fmaxf(top, s[i].x);
+        const float ref = top == -INFINITY ? 0.f : top, f = exp2f(M - ref);
+        M = top;
+        W *= f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] *= f;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const float w = exp2f(s[i].x - ref);
+            W += s[i].y * w;
+            acc[0] += v[i].x * w;
+            acc[1] += v[i].y * w;
+            acc[2] += v[i].z * w;
+            acc[3] += v[i].w * w;
         }
     }
-    __syncthreads();
-    if (row < rows) {
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
-        auto add = [&](float f, float4 v) {
-            acc[0] += f * v.x;
-            acc[1] += f * v.y;
-            acc[2] += f * v.z;
-            acc[3] += f * v.w;
-        };
-#pragma unroll
-        for (int i = 0; i < kMergeAhead; ++i)
-            if (i < ahead) add(wq[row][i], early[i]);
-        for (int i0 = kMergeAhead; i0 < n; i0 += kMergeAhead) {
-            float4 v[kMergeAhead];
-#pragma unroll
-            for (int i = 0; i < kMergeAhead; ++i)
-                if (i0 + i < n) v[i] = part(i0 + i);
-#pragma unroll
-            for (int i = 0; i < kMergeAhead; ++i)
-                if (i0 + i < n) add(i0 + i < 32 ? wq[row][i0 + i] : exp2f(sums(i0 + i, row).x - top[row]), v[i]);
-        }
-        const float inv = inverse[row];
-        // (an infinite output times 1 / W stays what it is; a sum of weights of 0 leaves 0)
-        if (inv == 0.f) acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
-        store4(out(row) + 4 * chunk, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-    }
-    __syncthreads();
+    const float inv = W == 0.f ? 0.f : 1.f / W;  // (a NaN sum leaves NaN)
+    if (inv == 0.f) acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+    store4(out(row) + 4 * chunk, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    if (chunk == 0) done(row, M == -INFINITY ? 0.f : M, inv);
 }
 
 // Grid: (CTAs of the attention, row blocks).  CTA c: the pair that the border in front of share c cuts,
 // if no earlier border cuts it.
-template <int D, typename T>
-__global__ void __launch_bounds__(2 * D) rows_merge_window_kernel(const RowsArgs a) {
+// kAhead: parts in flight.  2 for prompts, whose pairs have rarely more and many rows (37 us after a prompt of 8k with
+// 8, for want of resident CTAs, 20 with 2), 8 for few rows, split over many shares.
+template <int D, typename T, int kAhead>
+__global__ void __launch_bounds__(2 * D, (kAhead == 2 ? 1280 : 768) / (2 * D)) rows_merge_window_kernel(const RowsArgs a) {
     pdl_wait();
     const int c = blockIdx.x;
     RowsWalk w;
-    w.begin(a, c);
+    w.begin(__ldcg(reinterpret_cast<const int4 *>(a.start + c)));
     if (w.left == 0 || w.at == 0) return;
     const int64_t per = __ldcg(&a.head->per);
     const RowsUnit u = rows_unit(a, w.unit);
-    const int j = w.first(a, u.n);
-    if (j == 0 || j > per) return;  // (beyond: the share in front of this one begins behind the pair's first tile)
-    const int n = 1 + (int)divide(u.nt - j + per - 1, per);  // parts: share c - 1's and those behind
+    const RowsCost cost = rows_cost(a, u.n);
+    const int j = tile_at(cost, w.at);
+    // no tile in front of the border or none behind it, or an earlier border cuts the pair too
+    if (j == 0 || j >= u.nt || tile_at(cost, w.at - per) > 0) return;
+    // parts: share c - 1's, and those up to the share that the last tile begins in
+    const int n = 2 + (int)divide(cost.extra + (int64_t)(u.nt - 1) * cost.tile - w.at, per);
     const int rows = u.n * a.group;
     const int so = a.rows_cap * D;
     for (int r0 = blockIdx.y * kMergeRows; r0 < rows; r0 += gridDim.y * kMergeRows) {
@@ -120,14 +107,14 @@ __global__ void __launch_bounds__(2 * D) rows_merge_window_kernel(const RowsArgs
             return Run{a.part_ml + (int64_t)slot * a.rows_cap + r0, a.part_o + (int64_t)slot * so + 4 * r0, parts,
                        2 * a.rows_cap, 2 * so, 4 * a.rows_cap};
         };
-        merge_rows<D, T>(run(2 * (c - 1) + 1, 1), run(2 * c, n - 1), min(kMergeRows, rows - r0), [](int, float, float) {},
+        merge_rows<D, T, kAhead>(run(2 * (c - 1) + 1, 1), run(2 * c, n - 1), min(kMergeRows, rows - r0), [](int, float, float) {},
                          [&](int r) { return static_cast<T *>(a.out) + rows_row<D>(a, u, w.g, r0 + r).out; });
     }
 }
 
 // A CTA a (sequence, KV head)
 template <int D, typename T>
-__global__ void __launch_bounds__(2 * D) rows_merge_prefix_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(2 * D, 768 / (2 * D)) rows_merge_prefix_kernel(const RowsArgs a) {
     pdl_wait();
     const int hk = a.pv.kv_heads, b = blockIdx.x / hk, g = blockIdx.x % hk;
     const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.seq) + b);
@@ -138,17 +125,17 @@ __global__ void __launch_bounds__(2 * D) rows_merge_prefix_kernel(const RowsArgs
     int64_t slot_p = 0, slot_o = 0;
     int np = 0, no = 0;
     auto parts = [&](const RowsUnit &u, int64_t pair0, int64_t &slot) {  // of pair (u, g); slot: its first part's
-        const int e = rows_extra(a, u.n);
-        const int64_t x0 = u.cum + (int64_t)g * (u.nt + e) + e;
+        const RowsCost c = rows_cost(a, u.n);
+        const int64_t x0 = u.cum + g * pair_cost(c, u.nt) + c.extra;
         const int64_t c0 = divide(x0, head.per);
         slot = pair0 + g + c0;
-        return (int)(divide(x0 + u.nt - 1, head.per) - c0) + 1;
+        return (int)(divide(x0 + (int64_t)(u.nt - 1) * c.tile, head.per) - c0) + 1;
     };
     if (s.x >= 0) np = parts(pre, (int64_t)s.x * hk, slot_p);
     if (s.z >= 0) no = parts(own, (int64_t)(s.z - head.n_pre) * hk, slot_o);
     const int rp = s.y * a.group, so = a.rows_cap * D, sw = a.group * D;  // rp: the pre part's rows
     const int64_t row0 = (int64_t)b * a.q_heads + g * a.group;
-    merge_rows<D, T>(
+    merge_rows<D, T, 8>(
         Run{a.part_ml + slot_p * a.rows_cap + rp, a.part_o + slot_p * so + 4 * rp, np, a.rows_cap, so, 4 * a.rows_cap},
         Run{a.own_ml + slot_o * a.group, a.own_o + slot_o * sw, no, a.group, sw, 4 * a.group}, a.group,
         [&](int r, float ref, float inv) { a.norm[row0 + r] = make_float2(ref, inv); },
@@ -161,7 +148,8 @@ cudaError_t launch_merge(const RowsArgs &a, cudaStream_t st) {
         return launch_k(rows_merge_prefix_kernel<D, T>, dim3((unsigned)(a.batch * a.pv.kv_heads)), dim3(2 * D), 0,
                         st, a);
     const int y = (a.rows_cap + kMergeRows - 1) / kMergeRows;
-    return launch_k(rows_merge_window_kernel<D, T>, dim3(a.ctas, y), dim3(2 * D), 0, st, a);
+    return a.rows_cap > 64 ? launch_k(rows_merge_window_kernel<D, T, 2>, dim3(a.ctas, y), dim3(2 * D), 0, st, a)
+                           : launch_k(rows_merge_window_kernel<D, T, 8>, dim3(a.ctas, y), dim3(2 * D), 0, st, a);
 }
 
 // Scores without tensor cores: K once more, with each row's maximum M and sum of weights W,

@@ -67,7 +67,7 @@ __device__ __forceinline__ void whole_run(RowsUnit &u, int lo, int hi) {
 }
 
 __device__ __forceinline__ int64_t cost(const RowsArgs &a, const RowsUnit &u) {
-    return u.nt > 0 ? (int64_t)(u.nt + rows_extra(a, u.n)) * a.pv.kv_heads : 0;
+    return u.nt > 0 ? pair_cost(rows_cost(a, u.n), u.nt) * a.pv.kv_heads : 0;
 }
 
 // tiles of the score pass: each for every `item_n` members (and, with a utility row a KV head, for each of those)
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
         if (at.n < kPlanCum) {
             cums[at.n] = at.cost;
             icums[at.n] = at.items;
-            sizes[at.n] = make_int2(u.nt, u.nt + rows_extra(a, u.n));
+            sizes[at.n] = make_int2(u.nt, (int)pair_cost(rows_cost(a, u.n), u.nt));
         }
     };
     if (!a.prefix) {
@@ -416,8 +416,8 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
     }
     __syncthreads();
     auto share = [&](int64_t x) { return x >> 31 ? (x + a.ctas - 1) / a.ctas : (int64_t)(((uint32_t)x + a.ctas - 1) / (uint32_t)a.ctas); };
-    int64_t per = share(sum.cost);
-    if (per < 1) per = 1;
+    // (a share has at least a tile's cost: none that lies in a pair's tiles is empty)
+    const int64_t per = max(share(sum.cost), (int64_t)(a.unit_n > a.tile_n ? kTileTwo : kTileOne));
     if (tid == 0) {
         a.head->total = sum.cost;
         a.head->per = per;
@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
     }
     auto size = [&](int i) {
         return i < kPlanCum ? sizes[i]
-                            : make_int2(__ldcg(&a.units[i].nt), __ldcg(&a.units[i].nt) + rows_extra(a, __ldcg(&a.units[i].n)));
+                            : make_int2(__ldcg(&a.units[i].nt), (int)pair_cost(rows_cost(a, __ldcg(&a.units[i].n)), __ldcg(&a.units[i].nt)));
     };
     auto divide = [](int64_t x, int y) { return x >> 31 ? (int32_t)(x / y) : (int32_t)((uint32_t)x / (uint32_t)y); };
     // the last unit that begins at or before x
@@ -454,7 +454,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
         return lo;
     };
     for (int c = tid; c < a.ctas; c += nthr) {
-        RowsStart s{0, 0, 0, 0};
+        RowsStart s{};
         const int64_t x = (int64_t)c * per;
         if (x < sum.cost) {
             auto big = [&](int i) { return __ldcg(&a.units[i].cum); };

@@ -191,7 +191,7 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
 }
 
 template <int D, typename T>
-__global__ void __launch_bounds__(kSimtThreads) rows_simt_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(kSimtThreads, D == 64 ? 2 : 1) rows_simt_kernel(const RowsArgs a) {
     pdl_wait();
     extern __shared__ __align__(16) unsigned char smem[];
     float *sQ = reinterpret_cast<float *>(smem);
@@ -201,16 +201,18 @@ __global__ void __launch_bounds__(kSimtThreads) rows_simt_kernel(const RowsArgs 
     RowsHead head;
     head.n_pre = __ldcg(&a.head->n_pre);
     RowsWalk w;
-    w.begin(a, blockIdx.x);
+    w.begin(__ldcg(reinterpret_cast<const int4 *>(a.start + blockIdx.x)));
     while (w.left > 0) {
         const RowsUnit u = rows_unit(a, w.unit);
-        const int n = w.part(a, u.nt, u.n), j0 = w.first(a, u.n);
-        if (n <= 0) break;
-        if (u.n * a.group <= 16)
-            simt_part<D, T, 1>(a, head, u, w.unit, w.g, j0, n, sQ, sK, sV, sP);
-        else
-            simt_part<D, T, 4>(a, head, u, w.unit, w.g, j0, n, sQ, sK, sV, sP);
-        w.next(a, u.nt, u.n);
+        int j0;
+        const int n = w.part(a, u, j0);
+        if (n > 0) {
+            if (u.n * a.group <= 16)
+                simt_part<D, T, 1>(a, head, u, w.unit, w.g, j0, n, sQ, sK, sV, sP);
+            else
+                simt_part<D, T, 4>(a, head, u, w.unit, w.g, j0, n, sQ, sK, sV, sP);
+        }
+        w.next(a, u);
     }
 }
 

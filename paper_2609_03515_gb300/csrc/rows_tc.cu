@@ -14,7 +14,8 @@
 // rescaled: weights and sum are relative to the same m, which cancels in O / l.  The sum takes the weights
 // in 32 bits; rounding them to bf16 for the product costs at most 2^-8 of sum p |V|.
 //
-// Warps: 0-3 and 4-7 the two row tiles, 8 TMA, 9 MMA, 10-11 load Q.  K and V tiles pass through a ring of
+// Warps: 0-3 and 4-7 the two row tiles, 8 TMA, 9 MMA, 10-11 Q; 11 also finds the parts of the share, ahead of the
+// others.  K and V tiles pass through a ring of
 // 32 KB (D = 64: 16 KB) stages in the order K0 K1 V0 K2 V1 .., which is the order of the products.  Boxes of
 // a tile that no row sees are fetched from behind the tensor's end, which fills zeros and reads nothing.
 // Every wait is bounded; on timeout the CTA sets the error word, drains what is in flight and returns.
@@ -27,15 +28,23 @@ namespace {
 constexpr int kThreads = 384;
 constexpr float kSlack = 8.f;               // log2 of the largest weight before the maximum moves
 
+// A part of the CTA's share, for all warps: n tiles from j0 on of pair (unit, g); n = 0 behind the last
+struct alignas(16) Part {
+    RowsUnit u;
+    int32_t unit, g, j0, n;
+};
+constexpr int kParts = 4;                   // of them in shared memory, most of them ahead
+
 template <int D>
 struct Tc {
     static constexpr int kStage = kAtom * (D / 64);
     static constexpr int kStages = D == 128 ? 4 : 8;
     static constexpr int kOffRing = 2 * kStage;  // (Q of A and B in front)
-    static constexpr int kOffOut = kOffRing + kStages * kStage;  // a warp: 64 channels of its 32 rows
-    static constexpr int kOffEx = kOffOut + 8 * 4096;
-    static constexpr int kOffBar = kOffEx + 128 * 8;
-    static constexpr int kBars = 2 * kStages + 12;
+    static constexpr int kOffOut = kOffRing + kStages * kStage;  // a warp: 32 channels of its 32 rows
+    static constexpr int kOffEx = kOffOut + 8 * 2048;
+    static constexpr int kOffPart = kOffEx + 2 * 128 * 8 + 128 * 4;
+    static constexpr int kOffBar = kOffPart + kParts * sizeof(Part);
+    static constexpr int kBars = 2 * kStages + 13 + 2 * kParts;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
     static constexpr int kSmem = kOffMisc + 16 + 1024;  // (to align by 1024)
 };
@@ -70,6 +79,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto p_full = [&](int x) { return bar1 + 48u + 8u * x; };
     auto o_full = [&](int x) { return bar1 + 64u + 8u * x; };
     auto p_half = [&](int x) { return bar1 + 80u + 8u * x; };
+    auto part_full = [&](int i) { return bar1 + 96u + 8u * i; };
+    auto part_empty = [&](int i) { return bar1 + 96u + 8u * (kParts + i); };
+    const uint32_t joined = bar1 + 96u + 16u * kParts;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + C::kOffMisc + 4);
     if (warp == 8 && lane == 0) {
@@ -85,6 +97,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(p_half(x), 4);
             mbar_init(o_full(x), 1);
         }
+        for (int i = 0; i < kParts; ++i) {
+            mbar_init(part_full(i), 1);
+            mbar_init(part_empty(i), 12);  // every warp
+        }
+        mbar_init(joined, 8);
         mbar_init(mma_done, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -100,8 +117,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_after_sync();
     const uint32_t tmem = *tmem_slot;
     const int tile_rows = 128 / a.group * a.group;  // rows of a row tile
-    RowsWalk w;
-    w.begin(a, blockIdx.x);
+    // the parts, which warp 11 finds ahead of the others; part number seg, until release()
+    uint32_t seg = 0;
+    const Part *const parts = reinterpret_cast<const Part *>(sm + C::kOffPart);
+    auto part_at = [&] { return parts + seg % kParts; };
+    auto part_wait = [&] { return warp_wait(part_full(seg % kParts), seg / kParts & 1, abort_flag) && part_at()->n > 0; };
+    auto release = [&] {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(part_empty(seg % kParts));
+        ++seg;
+    };
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -110,10 +135,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             int J = 0;
             bool ok = true;
             const int boxes = kRowsTile / tm.rows_per_box;
-            while (w.left > 0 && ok) {
-                const RowsUnit u = rows_unit(a, w.unit);
-                const int n = w.part(a, u.nt, u.n), j0 = w.first(a, u.n);
-                if (n <= 0) break;
+            while (ok && part_wait()) {
+                const Part p = *part_at();
+                const RowsUnit &u = p.u;
+                const int n = p.n, j0 = p.j0;
                 for (int x = 0; x < 2 * n && ok; ++x, ++J) {
                     int tile;
                     bool is_v;
@@ -121,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int s0 = rows_tile(u, j0 + tile) * kRowsTile + lane * tm.rows_per_box, s1 = s0 + tm.rows_per_box;
                     int row = tm.pool_rows;
                     if (lane < boxes && s0 < u.hi && (s1 > u.wlo || (s0 < u.sh && s1 > u.lo))) {
-                        row = pool_row(a, u.b, w.g, s0);
+                        row = pool_row(a, u.b, p.g, s0);
                     }
                     const int st = J % C::kStages;
                     if (lane == 0) {
@@ -134,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                  kv_full(st));
                     if (!ok) break;
                 }
-                w.next(a, u.nt, u.n);
+                release();
             }
             if (lane == 0)  // every copy has landed before the CTA ends
                 for (int i = J - 1; i >= 0 && i >= J - C::kStages; --i) bar_drain(kv_full(i % C::kStages), (i / C::kStages) & 1);
@@ -156,13 +181,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (++at.i == C::kStages) at = Stage{0, at.par ^ 1};
                 return s;
             };
-            uint32_t seg = 0, np[2] = {0, 0};  // weights taken
+            uint32_t np[2] = {0, 0};       // weights taken
             bool ok = true;
-            while (w.left > 0 && ok) {
-                const RowsUnit *up = a.units + w.unit;
-                const int n = __shfl_sync(0xffffffffu, w.part(a, up->nt, up->n), 0);
-                if (n <= 0) break;
-                const bool pair = __shfl_sync(0xffffffffu, up->n * a.group > tile_rows, 0);
+            while (ok && part_wait()) {
+                const int n = __shfl_sync(0xffffffffu, part_at()->n, 0);
+                const bool pair = __shfl_sync(0xffffffffu, part_at()->u.n * a.group > tile_rows, 0);
                 auto there = [&](Stage s) { return warp_wait(kv_full(s.i), s.par, abort_flag); };
                 // S of row tile x; (free: K's stage is done with then)
                 auto qk = [&](int x, Stage k, bool free) {
@@ -251,29 +274,48 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                 }
-                ++seg;
-                w.next(a, up->nt, up->n);
+                release();
             }
             if (leader) mma_commit(mma_done);  // also after an abort: no product may write TMEM when it is freed
             __syncwarp();
             bar_drain(mma_done, 0);
         } else {
-            // ---------------- Q
-            const int t = tid - 320;
+            // ---------------- Q; warp 11 also finds the parts, three ahead
+            RowsWalk w;
+            w.begin(__ldcg(reinterpret_cast<const int4 *>(a.start + blockIdx.x)));
+            uint32_t found = 0;
+            bool ok = true, more = warp == 11;
+            auto find = [&] {
+                Part p;
+                p.n = 0;
+                while (w.left > 0 && p.n == 0) {
+                    p.u = rows_unit(a, w.unit);
+                    p.n = w.part(a, p.u, p.j0);
+                    p.unit = w.unit;
+                    p.g = w.g;
+                    w.next(a, p.u);
+                }
+                more = p.n > 0;
+                const uint32_t i = found % kParts;
+                if (found >= kParts) ok = warp_wait(part_empty(i), found / kParts - 1 & 1, abort_flag);
+                if (ok && lane == 0) {
+                    const_cast<Part *>(parts)[i] = p;
+                    mbar_arrive(part_full(i));
+                }
+                ++found;
+            };
+            if (more) find();
             // Every piece by an asynchronous copy, all of them in flight: four lanes a row, 16 rows an iteration.
             // A's rows are handed over first.
             constexpr int CH = D / 8;      // 16-byte pieces of a row
-            const int c = t & 3;
-            uint32_t seg = 0;
-            bool ok = true;
-            while (w.left > 0 && ok) {
-                const RowsUnit u = rows_unit(a, w.unit);
+            const int t = tid - 320, c = t & 3;
+            while (ok && part_wait()) {
+                const RowsUnit u = part_at()->u;
                 const int rows = u.n * a.group;
-                if (w.part(a, u.nt, u.n) <= 0) break;
                 const bool many = a.prefix && u.m0 >= 0;
                 const int64_t row0 = a.prefix ? u.b : (int64_t)u.row0 + u.m0;
-                const T *q = static_cast<const T *>(a.q) + (int64_t)w.g * a.group * D + 8 * c;
-                if (seg > 0) ok = bar_wait(q_empty, (seg - 1) & 1, abort_flag);
+                const T *q = static_cast<const T *>(a.q) + (int64_t)part_at()->g * a.group * D + 8 * c;
+                if (seg > 0) ok = warp_wait(q_empty, (seg - 1) & 1, abort_flag);
                 for (int x = 0; x < 2 && ok; ++x) {
                     const int first = x * tile_rows, end = min(rows - first, tile_rows);
                     int tok = (first + t / 4) / a.group, h = (first + t / 4) % a.group;
@@ -303,6 +345,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     asm volatile("cp.async.commit_group;" ::: "memory");
                 }
+                // (while the copies are on their way)
+                for (int i = seg == 0 ? 2 : 1; i > 0 && more && ok; --i) find();
                 if (ok) {
                     asm volatile("cp.async.wait_group 1;" ::: "memory");
                     fence_async_smem();
@@ -311,8 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     fence_async_smem();
                     mbar_arrive(q_full(1));
                 }
-                ++seg;
-                w.next(a, u.nt, u.n);
+                release();
             }
         }
     } else {
@@ -321,25 +364,32 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int X = warp >> 2, wq = warp & 3, row_in = wq * 32 + lane;
         const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
         const uint32_t tS = tmem + 128 * X + lane_off, tO = tmem + 256 + lane_off;
-        float2 *ex = reinterpret_cast<float2 *>(sm + C::kOffEx);
+        float2 *ex = reinterpret_cast<float2 *>(sm + C::kOffEx);  // [2][128] (m, l) of A's and B's rows
+        float *found = reinterpret_cast<float *>(ex + 256);        // [128] B's probes
         const int n_pre = __ldcg(&a.head->n_pre);
-        uint32_t ns = 0, np = 0;  // scores and weights so far
+        uint32_t ns = 0, np = 0, nj = 0;  // scores, weights and meetings so far
         bool ok = true;
-        while (w.left > 0) {
-            // (the unit is looked up where it is needed: kept, it would push scores out of the registers)
-            const RowsUnit *up = a.units + w.unit;
-            int n, j0, r, seq, hi, wlo, steps;
+        auto meet = [&] {  // A's and B's warps (a bounded wait, as every other: a warp may have given up)
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(joined);
+            ok = warp_wait(joined, nj++ & 1, abort_flag) && ok;
+            fence_after_sync();
+        };
+        while (part_wait()) {
+            // (the part's fields are read from shared memory where they are needed: kept, they would push scores out of
+            // the registers)
+            const volatile Part *vp = part_at();
+            int n, r, seq, hi, wlo, steps;
             bool pair, busy;
             {
-                const RowsUnit u = rows_unit(a, w.unit);
-                n = w.part(a, u.nt, u.n);
-                if (n <= 0) break;
-                j0 = w.first(a, u.n);
-                const int rows = u.n * a.group;
+                const Part *p = part_at();
+                n = p->n;
+                const int rows = p->u.n * a.group;
                 pair = rows > tile_rows;
                 r = pair ? X * tile_rows + row_in : row_in;
                 const int mine = pair && X == 1 ? rows - tile_rows : min(rows, tile_rows);  // rows of this tile
-                const RowsRow row = rows_row<D>(a, u, w.g, r);
+                const RowsRow row = rows_row<D>(a, p->u, p->g, r);
                 seq = row_in < mine ? row.seq : -1;
                 hi = row.hi;
                 wlo = row.wlo;
@@ -351,9 +401,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t see[4];
                 bool masked;
                 {
-                    const int j = j0 + (pair ? s : 2 * s + X), n_a = up->n_a;
-                    const int t0 = (j < n_a ? up->t_a + j : up->t_w + j - n_a) * kRowsTile;
-                    const int lo = up->lo, S0 = up->S0, sh = a.prefix ? lo : S0 + a.sinks;
+                    const int j = vp->j0 + (pair ? s : 2 * s + X), n_a = vp->u.n_a;
+                    const int t0 = (j < n_a ? vp->u.t_a + j : vp->u.t_w + j - n_a) * kRowsTile;
+                    const int lo = vp->u.lo, S0 = vp->u.S0, sh = a.prefix ? lo : S0 + a.sinks;
                     const bool full = seq < 0 || (t0 >= lo && t0 + 127 <= hi && (t0 >= wlo || t0 + 127 < sh));
                     masked = __any_sync(0xffffffffu, !full) || a.pos;
                     if (masked && busy) {
@@ -363,7 +413,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                              : range_bits(max(lo, wlo) - t0, hi - t0, k) |
                                                    range_bits(lo - t0, min(sh - 1, hi) - t0, k);
                         if (a.pos && seq >= 0) {  // the row's own live slots, by slot - S0
-                            const int64_t rr = (int64_t)seq * a.rows_per_seq + (a.rows_per_seq == 1 ? 0 : w.g);
+                            const int64_t rr = (int64_t)seq * a.rows_per_seq + (a.rows_per_seq == 1 ? 0 : vp->g);
                             const uint32_t *bits = a.live + rr * a.live_words;
                             const int x0 = (t0 - S0) >> 5, sh0 = (t0 - S0) & 31;
                             uint32_t lo_w = x0 >= 0 && x0 < a.live_words ? __ldcg(bits + x0) : 0u;
@@ -455,109 +505,130 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (lane == 0) mbar_arrive(p_full(X));
                 ++np;
             }
-            const RowsUnit u = rows_unit(a, w.unit);
             if (steps > 0) {
                 if (ok) ok = bar_wait(o_full(X), (np - 1) & 1, abort_flag);
                 ok = __all_sync(0xffffffffu, ok);
                 fence_after_sync();
             }
+            // One row tile: A and B join what they have of each row, half of the channels each
             float f0 = 1.f, f1 = 0.f;
-            if (!pair) {  // B's output joins A's
-                if (X == 1) ex[row_in] = make_float2(m, l);
-                fence_before_sync();
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                fence_after_sync();
-                if (X == 0 && n > 1) {
-                    const float2 o = ex[row_in];
-                    const float mn = fmaxf(m, o.x), ref = mn == -INFINITY ? 0.f : mn;
-                    f0 = ex2(m - ref);
-                    f1 = ex2(o.x - ref);
-                    l = l * f0 + o.y * f1;
-                    m = mn;
+            if (!pair) {
+                ex[X * 128 + row_in] = make_float2(m, l);
+                meet();
+                if (n > 1) {
+                    const float2 p0 = ex[row_in], p1 = ex[128 + row_in];
+                    m = fmaxf(p0.x, p1.x);
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    f0 = ex2(p0.x - ref);
+                    f1 = ex2(p1.x - ref);
+                    l = p0.y * f0 + p1.y * f1;
+                } else {
+                    const float2 p0 = ex[row_in];
+                    m = p0.x;
+                    l = p0.y;
                 }
             }
-            if (ok && busy && (pair || X == 0)) {
-                RowsRow row = rows_row<D>(a, u, w.g, r);
-                row.seq = seq;
-                const bool begins = j0 == 0, whole = begins && n == u.nt && !a.prefix;
-                RowsHead h;
-                h.n_pre = n_pre;
-                const int64_t slot = whole ? 0 : rows_slot(a, h, u, w.unit, w.g, blockIdx.x, begins);
-                const bool joined = !pair && n > 1;
+            float probe = 0.f;  // NaN once a value is not finite
+            const Part *p = part_at();
+            const bool begins = p->j0 == 0, whole = begins && n == p->u.nt && !a.prefix;
+            RowsRow row = rows_row<D>(a, p->u, p->g, r);
+            row.seq = seq;
+            RowsHead h;
+            h.n_pre = n_pre;
+            const int64_t slot = whole ? 0 : rows_slot(a, h, p->u, p->unit, p->g, blockIdx.x, begins);
+            if (ok && busy) {
                 const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-                float probe = 0.f;  // NaN once a value is not finite
-                unsigned char *stage = sm + C::kOffOut + warp * 4096;
-#pragma unroll 1
-                for (int k = 0; k < D; k += 32) {
-                    uint32_t o[32];
-                    tmem_ld32(tO + 128 * X + k, o);
-                    tmem_wait_ld(o);
-                    float y[32];
+                const int k0 = pair || X == 0 ? 0 : D / 2;
+                unsigned char *stage = sm + C::kOffOut + warp * 2048;
+                const int step = rows_part_step(a, p->u);
+                float *part = rows_part_o<D>(a, p->u, slot, r) + (int64_t)(k0 / 4) * step;
+                T *to[4];  // where this lane stores pieces of rows lane / 4 + 8 i
+                if (whole) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) y[i] = __uint_as_float(o[i]);
-                    if (joined) {
-                        tmem_ld32(tO + 128 + k, o);
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t at = __shfl_sync(0xffffffffu, row.seq >= 0 ? row.out : -1, 8 * i + lane / 4);
+                        to[i] = at >= 0 ? static_cast<T *>(a.out) + at + k0 + lane % 4 * 8 : nullptr;
+                    }
+                }
+                const float2 zero2 = make_float2(0.f, 0.f), inv2 = make_float2(inv, inv);
+                float2 look = zero2;
+                auto pair_of = [](const uint32_t *v, int i) {
+                    return make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+                };
+                const int chunks = pair ? D / 32 : D / 64;
+#pragma unroll 1
+                for (int c = 0; c < chunks; ++c) {  // channels k0 + 32 c ..
+                    uint32_t v[32];
+                    tmem_ld32(tO + (pair ? 128 * X : 0) + k0 + 32 * c, v);
+                    if (!pair && n > 1) {
+                        uint32_t o[32];
+                        tmem_ld32(tO + 128 + k0 + 32 * c, o);
+                        tmem_wait_ld(v);
                         tmem_wait_ld(o);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) y[i] = y[i] * f0 + __uint_as_float(o[i]) * f1;
+                        for (int i = 0; i < 16; ++i) {
+                            const float2 z = fma2(pair_of(o, i), make_float2(f1, f1), fma2(pair_of(v, i), make_float2(f0, f0), zero2));
+                            v[2 * i] = __float_as_uint(z.x);
+                            v[2 * i + 1] = __float_as_uint(z.y);
+                        }
                     }
+                    tmem_wait_ld(v);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        probe = __fmaf_rn(y[i], 0.f, probe);
-                        y[i] *= inv;
-                    }
+                    for (int i = 0; i < 16; ++i) look = fma2(pair_of(v, i), zero2, look);
                     if (whole) {
-                        // 64 channels of 32 rows at a time through shared memory: eight lanes store a row's 128
-                        // bytes, where a lane a row would touch 32 lines with every store
-                        if (k % 64 == 0) __syncwarp();
+                        // 32 channels of 32 rows at a time through shared memory: four lanes store 64 bytes of a row,
+                        // where a lane a row would touch 32 lines with every store
+                        __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
+                        for (int i = 0; i < 4; ++i) {
                             uint32_t q[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(y[i + 2 * e], y[i + 2 * e + 1]);
+                                const float2 z = fma2(pair_of(v, 4 * i + e), inv2, zero2);
+                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(z.x, z.y);
                                 q[e] = *reinterpret_cast<const uint32_t *>(&b2);
                             }
-                            *reinterpret_cast<uint4 *>(stage + sw128(lane, k % 64 + i)) = make_uint4(q[0], q[1], q[2], q[3]);
+                            *reinterpret_cast<uint4 *>(stage + lane * 64 + (((i ^ (lane >> 1)) & 3) << 4)) =
+                                make_uint4(q[0], q[1], q[2], q[3]);
                         }
-                        if (k % 64 == 32) {
-                            __syncwarp();
-                            uint4 x[8];
-                            int64_t at[8];
+                        __syncwarp();
+                        uint4 x[4];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const int rr = 4 * i + lane / 8;
-                                x[i] = *reinterpret_cast<const uint4 *>(stage + sw128(rr, lane % 8 * 8));
-                                at[i] = __shfl_sync(0xffffffffu, row.seq >= 0 ? row.out : -1, rr);
-                            }
-#pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                if (at[i] >= 0)
-                                    *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + at[i] + k - 32 + lane % 8 * 8) = x[i];
+                        for (int i = 0; i < 4; ++i) {
+                            const int rr = 8 * i + lane / 4;
+                            x[i] = *reinterpret_cast<const uint4 *>(stage + rr * 64 + (((lane ^ (rr >> 1)) & 3) << 4));
                         }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (to[i]) *reinterpret_cast<uint4 *>(to[i] + 32 * c) = x[i];
                     } else if (row.seq >= 0) {
-                        const int step = rows_part_step(a, u);
-                        float *d = rows_part_o<D>(a, u, slot, r) + (int64_t)(k / 4) * step;
+                        float *d = part + (int64_t)(8 * c) * step;
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) store4(d + (i / 4) * step, y[i], y[i + 1], y[i + 2], y[i + 3]);
+                        for (int i = 0; i < 8; ++i)
+                            *reinterpret_cast<uint4 *>(d + i * step) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                     }
                 }
-                if (row.seq >= 0 && !whole) rows_store_ml(a, u, slot, r, m, l);
+                probe = look.x + look.y;
+                if (row.seq >= 0 && !whole && (pair || X == 0)) rows_store_ml(a, p->u, slot, r, m, l);
+            }
+            if (!pair) {
+                // both outputs have been read, and ex: B's findings go to A
+                meet();
+                if (X == 1) found[row_in] = probe;
+                meet();
+                if (X == 0) probe += found[row_in];
+            }
+            if (ok && busy && (pair || X == 0)) {
                 // (see rows_redo: V rows that are not finite and that the row does not see)
-                __syncwarp();  // (it stores over what another lane did)
-                unsigned redo = __ballot_sync(0xffffffffu, isnan(probe) && row.seq >= 0 && !isnan(l));
+                __syncwarp();  // (it stores over what other lanes did)
+                unsigned redo = __ballot_sync(0xffffffffu, isnan(probe) && seq >= 0 && !isnan(l));
                 while (redo) {
                     const int i = __ffs(redo) - 1;
                     redo &= redo - 1;
-                    rows_redo<D, T>(a, w.unit, w.g, j0, n, whole, slot, __shfl_sync(0xffffffffu, r, i));
+                    rows_redo<D, T>(a, p->unit, p->g, p->j0, n, whole, slot, __shfl_sync(0xffffffffu, r, i));
                 }
             }
-            if (!pair) {  // (B's output has been read)
-                fence_before_sync();
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                fence_after_sync();
-            }
-            w.next(a, u.nt, u.n);
+            release();
         }
     }
     fence_before_sync();
