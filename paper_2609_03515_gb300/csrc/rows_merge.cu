@@ -154,14 +154,22 @@ cudaError_t launch_merge(const RowsArgs &a, cudaStream_t st) {
 
 // Scores without tensor cores: K once more, with each row's maximum M and sum of weights W,
 //     score = mean over the row's heads of 2^(q . k scale - M) / W.
-// A CTA: 32 slots of a sequence, a lane a slot, the query heads of each KV head spread over its warps.
+// A CTA: 32 slots of a sequence, a lane a slot, a warp every eighth KV head with all of its query heads.  Each lane
+// reads its own row of K, whose lines the first-level cache holds until they are used up; no warp waits for another
+// until the sums of the heads meet, in a fixed order.
 constexpr int kScoreWarps = 8;
-template <int D, typename T>
+__device__ __forceinline__ float4 load_four(const float *p) { return __ldg(reinterpret_cast<const float4 *>(p)); }
+__device__ __forceinline__ float4 load_four(const __nv_bfloat16 *p) {
+    const uint2 x = __ldg(reinterpret_cast<const uint2 *>(p));
+    return make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
+                       __uint_as_float(x.y & 0xffff0000u));
+}
+template <int D, typename T, int G>
 __global__ void __launch_bounds__(kScoreWarps * 32) rows_score_kernel(const RowsArgs a, const RowsScoreArgs sc) {
     pdl_wait();
-    __shared__ float sK[32][D + 1], sQ[8][D], part[kScoreWarps][33];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int rps = a.rows_per_seq, G = a.group, hk = a.pv.kv_heads;
+    __shared__ float part[kScoreWarps][33];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rps = a.rows_per_seq, hk = a.pv.kv_heads;
     for (int b = blockIdx.y; b < a.batch; b += gridDim.y) {
         const int S0 = a.pv.start ? min(max(__ldg(a.pv.start + b), 0), a.cap) : 0;
         const int L = min(max(__ldg(a.len + b), 0), a.cap - S0);
@@ -172,45 +180,53 @@ __global__ void __launch_bounds__(kScoreWarps * 32) rows_score_kernel(const Rows
             lead_s0 = __ldcg(&a.units[s.x].S0);
         }
         for (int j0 = blockIdx.x * 32; j0 < L; j0 += gridDim.x * 32) {
+            const int j = j0 + lane;
+            const bool inside = j < L, shared = j < s.w;
+            auto put = [&](int row, float t) {
+                const int64_t at = ((int64_t)b * rps + row) * a.cap + j;
+                if (a.pos && __ldg(a.pos + at) < 0) t = 0.f;
+                if (sc.score) sc.score[at] = t;
+                if (sc.ema) sc.ema[at] = sc.alpha * sc.ema[at] + (1.f - sc.alpha) * t;
+            };
             float sum = 0.f;
-            for (int g = 0; g < hk; ++g) {
-                __syncthreads();
-                for (int i = tid; i < 32 * D; i += kScoreWarps * 32) {
-                    const int r = i / D, c = i % D, j = j0 + r;
-                    float x = 0.f;
-                    if (j < L) {
-                        const bool shared = j < s.w;
-                        x = load_as_float(static_cast<const T *>(a.k) +
-                                          a.pv.row_phys(shared ? lead : b, a.layer, g, (shared ? lead_s0 : S0) + j) * D + c);
+            for (int g = warp; g < hk; g += kScoreWarps) {
+                const T *k = static_cast<const T *>(a.k) +
+                             (inside ? a.pv.row_phys(shared ? lead : b, a.layer, g, (shared ? lead_s0 : S0) + j) : 0) * D;
+                const int64_t row = (int64_t)b * a.q_heads + g * G;
+                const T *q = static_cast<const T *>(a.q) + row * D;
+                float2 z[G];
+#pragma unroll
+                for (int h = 0; h < G; ++h) z[h] = make_float2(0.f, 0.f);
+#pragma unroll 8
+                for (int c = 0; c < D; c += 4) {
+                    const float4 x = load_four(k + c);
+#pragma unroll
+                    for (int h = 0; h < G; ++h) {
+                        const float4 y = load_four(q + h * D + c);
+                        z[h] = fma2(make_float2(x.x, x.y), make_float2(y.x, y.y), z[h]);
+                        z[h] = fma2(make_float2(x.z, x.w), make_float2(y.z, y.w), z[h]);
                     }
-                    sK[r][c] = x;
                 }
-                for (int i = tid; i < G * D; i += kScoreWarps * 32)
-                    sQ[i / D][i % D] = load_as_float(static_cast<const T *>(a.q) + ((int64_t)b * a.q_heads + g * G) * D + i);
-                __syncthreads();
-                if (warp < G) {
-                    float z = 0.f;
-    #pragma unroll 8
-                    for (int c = 0; c < D; ++c) z += sQ[warp][c] * sK[lane][c];
-                    const float2 mw = __ldcg(a.norm + (int64_t)b * a.q_heads + g * G + warp);
-                    if (mw.y != 0.f) sum += exp2f(__fmaf_rn(z, a.scale_log2, -mw.x)) * mw.y;
+#pragma unroll
+                for (int h = 0; h < G; ++h) {
+                    const float2 mw = __ldcg(a.norm + row + h);
+                    if (mw.y != 0.f) sum += exp2f(__fmaf_rn(z[h].x + z[h].y, a.scale_log2, -mw.x)) * mw.y;
                 }
-                if (rps > 1 || g == hk - 1) {
-                    part[warp][lane] = sum;
+                if (rps > 1) {
+                    if (inside) put(g, sum * (1.f / G));
                     sum = 0.f;
-                    __syncthreads();
-                    const int j = j0 + lane;
-                    if (warp == 0 && j < L) {
-                        float t = 0.f;
-    #pragma unroll
-                        for (int w = 0; w < kScoreWarps; ++w) t += part[w][lane];
-                        const int64_t at = ((int64_t)b * rps + (rps > 1 ? g : 0)) * a.cap + j;
-                        const bool live = !a.pos || __ldg(a.pos + at) >= 0;
-                        t = live ? t / (float)(rps > 1 ? G : a.q_heads) : 0.f;
-                        if (sc.score) sc.score[at] = t;
-                        if (sc.ema) sc.ema[at] = sc.alpha * sc.ema[at] + (1.f - sc.alpha) * t;
-                    }
                 }
+            }
+            if (rps == 1) {
+                part[warp][lane] = sum;
+                __syncthreads();
+                if (warp == 0 && inside) {
+                    float t = 0.f;
+#pragma unroll
+                    for (int w = 0; w < kScoreWarps; ++w) t += part[w][lane];
+                    put(0, t / (float)a.q_heads);
+                }
+                __syncthreads();
             }
         }
     }
@@ -219,8 +235,15 @@ __global__ void __launch_bounds__(kScoreWarps * 32) rows_score_kernel(const Rows
 template <int D, typename T>
 cudaError_t launch_score(const RowsArgs &a, const RowsScoreArgs &s, cudaStream_t st) {
     const int blocks = s.max_len > 32 ? (s.max_len + 31) / 32 : 1;
-    return launch_k(rows_score_kernel<D, T>, dim3(blocks, a.batch < 65535 ? a.batch : 65535), dim3(kScoreWarps * 32), 0,
-                    st, a, s);
+    const dim3 grid(blocks, a.batch < 65535 ? a.batch : 65535), block(kScoreWarps * 32);
+    switch (a.group) {
+        case 1: return launch_k(rows_score_kernel<D, T, 1>, grid, block, 0, st, a, s);
+        case 2: return launch_k(rows_score_kernel<D, T, 2>, grid, block, 0, st, a, s);
+        case 4: return launch_k(rows_score_kernel<D, T, 4>, grid, block, 0, st, a, s);
+        case 7: return launch_k(rows_score_kernel<D, T, 7>, grid, block, 0, st, a, s);
+        case 8: return launch_k(rows_score_kernel<D, T, 8>, grid, block, 0, st, a, s);
+        default: return cudaErrorInvalidValue;
+    }
 }
 
 }  // namespace

@@ -6,6 +6,23 @@
 namespace ikv {
 namespace {
 
+// two at a time: x y + z, x + y
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(r)
+        : "l"(*reinterpret_cast<unsigned long long *>(&x)), "l"(*reinterpret_cast<unsigned long long *>(&y)),
+          "l"(*reinterpret_cast<unsigned long long *>(&z)));
+    return *reinterpret_cast<float2 *>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(r)
+        : "l"(*reinterpret_cast<unsigned long long *>(&x)), "l"(*reinterpret_cast<unsigned long long *>(&y)));
+    return *reinterpret_cast<float2 *>(&r);
+}
+
 __device__ __forceinline__ float load_as_float(const float *p) { return __ldg(p); }
 __device__ __forceinline__ float load_as_float(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
 

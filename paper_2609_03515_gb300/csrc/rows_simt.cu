@@ -36,10 +36,10 @@ __device__ __forceinline__ void cp16(void *dst, const void *src, bool real) {
 }
 
 __device__ __forceinline__ void fma4(float *acc, float p, float4 v) {
-    acc[0] += p * v.x;
-    acc[1] += p * v.y;
-    acc[2] += p * v.z;
-    acc[3] += p * v.w;
+    const float2 pp = make_float2(p, p);
+    float2 *a = reinterpret_cast<float2 *>(acc);
+    a[0] = fma2(pp, make_float2(v.x, v.y), a[0]);
+    a[1] = fma2(pp, make_float2(v.z, v.w), a[1]);
 }
 
 // One part: tiles [j0, j0 + n) of pair (unit, g).  (whole: its rows' outputs are final)
@@ -49,12 +49,15 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
     constexpr int RS = row_stride<D, T>(), NC = D / 16, CH = D * (int)sizeof(T) / 16;
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, lane = tid & 31;
     const int rows = u.n * a.group;
-    RowsRow row[RPT];
+    int seq[RPT], hi[RPT], wlo[RPT];  // of its rows (the rest of a RowsRow again where it is needed)
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
-        row[i] = rows_row<D>(a, u, g, ty * RPT + i);
-        if (ty * RPT + i >= rows) row[i].seq = -1;
+        const RowsRow w = rows_row<D>(a, u, g, ty * RPT + i);
+        seq[i] = ty * RPT + i < rows ? w.seq : -1;
+        hi[i] = w.hi;
+        wlo[i] = w.wlo;
     }
+    const int sh = a.prefix ? u.lo : u.S0 + a.sinks;
     __syncthreads();  // (the last part's shared memory has been read)
     for (int i = tid; i < 16 * RPT * (D / 4); i += kSimtThreads) {
         const int r = i / (D / 4), c = i % (D / 4) * 4;
@@ -65,8 +68,15 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
     }
     const int steps = n * (kRowsTile / kStep);
     auto first_slot = [&](int i) { return rows_tile(u, j0 + i / 2) * kRowsTile + (i & 1) * kStep; };
-    auto fetch = [&](int i) {
-        T *k = sK + (i & 1) * kStep * RS, *v = sV + (i & 1) * kStep * RS;
+    auto step_from = [&](int i) {  // the first from i on with a slot that some row sees
+        for (; i < steps; ++i) {
+            const int s = first_slot(i);
+            if (s < u.hi && (s + kStep > u.wlo || (s < u.sh && s + kStep > u.lo))) break;
+        }
+        return i;
+    };
+    auto fetch = [&](int i, int buf) {
+        T *k = sK + buf * kStep * RS, *v = sV + buf * kStep * RS;
         const int s0 = first_slot(i);
         for (int x = tid; x < kStep * CH; x += kSimtThreads) {
             const int r = x / CH, c = x % CH * (16 / (int)sizeof(T)), s = s0 + r;
@@ -78,7 +88,8 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    float m[RPT], l[RPT], acc[RPT][NC];
+    float m[RPT], l[RPT];
+    alignas(8) float acc[RPT][NC];
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
         m[i] = -INFINITY;
@@ -86,22 +97,25 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
 #pragma unroll
         for (int c = 0; c < NC; ++c) acc[i][c] = 0.f;
     }
-    fetch(0);
-    for (int st = 0; st < steps; ++st) {
-        if (st + 1 < steps) {
-            fetch(st + 1);
+    int st = step_from(0), buf = 0;
+    if (st < steps) fetch(st, 0);
+    for (int ahead; st < steps; st = ahead, buf ^= 1) {
+        ahead = step_from(st + 1);
+        if (ahead < steps) {
+            fetch(ahead, buf ^ 1);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
         } else {
             asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
         __syncthreads();
-        const T *k = sK + (st & 1) * kStep * RS, *v = sV + (st & 1) * kStep * RS;
+        const T *k = sK + buf * kStep * RS, *v = sV + buf * kStep * RS;
         const int s0 = first_slot(st);
-        float s[RPT][4];
+        // (sums of even and of odd channels: two products an instruction)
+        float2 s2[RPT][4];
 #pragma unroll
         for (int i = 0; i < RPT; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+            for (int j = 0; j < 4; ++j) s2[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 4
         for (int c = 0; c < D; c += 4) {
             float4 kk[4];
@@ -111,19 +125,35 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
             for (int i = 0; i < RPT; ++i) {
                 const float4 q = load4(sQ + (ty * RPT + i) * (D + 4) + c);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    s[i][j] += q.x * kk[j].x + q.y * kk[j].y + q.z * kk[j].z + q.w * kk[j].w;
+                for (int j = 0; j < 4; ++j) {
+                    s2[i][j] = fma2(make_float2(q.x, q.y), make_float2(kk[j].x, kk[j].y), s2[i][j]);
+                    s2[i][j] = fma2(make_float2(q.z, q.w), make_float2(kk[j].z, kk[j].w), s2[i][j]);
+                }
             }
         }
+        float s[RPT][4];
+#pragma unroll
+        for (int i = 0; i < RPT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[i][j] = s2[i][j].x + s2[i][j].y;
 #pragma unroll
         for (int i = 0; i < RPT; ++i) {
             float mx = m[i];
+            if (seq[i] < 0 || a.pos || s0 < u.lo || s0 + kStep - 1 > hi[i] || (s0 < wlo[i] && s0 + kStep > sh)) {
+                RowsRow w;
+                w.lo = u.lo;
+                w.hi = hi[i];
+                w.wlo = wlo[i];
+                w.sh = sh;
+                w.pos = a.pos && seq[i] >= 0
+                            ? a.pos + ((int64_t)seq[i] * a.rows_per_seq + (a.rows_per_seq == 1 ? 0 : g)) * a.cap
+                            : nullptr;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool see = row[i].seq >= 0 && rows_sees(row[i], u.S0, s0 + tx + 16 * j);
-                if (!see) s[i][j] = -INFINITY;
-                mx = fmaxf(mx, __fmul_rn(s[i][j], a.scale_log2));
+                for (int j = 0; j < 4; ++j)
+                    if (seq[i] < 0 || !rows_sees(w, u.S0, s0 + tx + 16 * j)) s[i][j] = -INFINITY;
             }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, __fmul_rn(s[i][j], a.scale_log2));
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
             const float ref = mx == -INFINITY ? 0.f : mx;  // no slot so far: nothing to scale
@@ -175,13 +205,14 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
         bool bad = false;
 #pragma unroll
         for (int c = 0; c < NC; ++c) bad |= !(fabsf(acc[i][c]) < INFINITY);
-        bad = bad && row[i].seq >= 0 && !isnan(l[i]);
+        bad = bad && seq[i] >= 0 && !isnan(l[i]);
         const unsigned redo = __ballot_sync(0xffffffffu, bad);
         const bool again = (redo >> (lane & 16)) & 0xffffu;
-        if (row[i].seq >= 0 && !again) {
+        if (seq[i] >= 0 && !again) {
+            const RowsRow w = rows_row<D>(a, u, g, r);
 #pragma unroll
             for (int kc = 0; kc < D / 64; ++kc)
-                rows_store4<D, T>(a, u, row[i], whole, slot, r, 4 * tx + 64 * kc, acc[i] + 4 * kc, l[i]);
+                rows_store4<D, T>(a, u, w, whole, slot, r, 4 * tx + 64 * kc, acc[i] + 4 * kc, l[i]);
             if (!whole && tx == 0) rows_store_ml(a, u, slot, r, m[i], l[i]);
         }
         for (int half = 0; half < 2; ++half)

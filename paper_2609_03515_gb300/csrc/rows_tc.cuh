@@ -60,23 +60,6 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// two at a time: x y + z, x + y
-__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
-    unsigned long long r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(r)
-        : "l"(*reinterpret_cast<unsigned long long *>(&x)), "l"(*reinterpret_cast<unsigned long long *>(&y)),
-          "l"(*reinterpret_cast<unsigned long long *>(&z)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-__device__ __forceinline__ float2 add2(float2 x, float2 y) {
-    unsigned long long r;
-    asm("add.rn.f32x2 %0, %1, %2;"
-        : "=l"(r)
-        : "l"(*reinterpret_cast<unsigned long long *>(&x)), "l"(*reinterpret_cast<unsigned long long *>(&y)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-
 // The row of a layer's pool that holds slot s of sequence b, KV head g
 __device__ __forceinline__ int pool_row(const RowsArgs &a, int b, int g, int s) {
     const int lp = a.pv.page_shift >= 0 ? s >> a.pv.page_shift : s / a.pv.page_size;
