@@ -6,6 +6,11 @@
 namespace ikv {
 namespace {
 
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // two at a time: x y + z, x + y
 __device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
     unsigned long long r;
@@ -47,16 +52,6 @@ __device__ __forceinline__ int rows_part_step(const RowsArgs &a, const RowsUnit 
 }
 __device__ __forceinline__ float2 *rows_part_ml(const RowsArgs &a, const RowsUnit &u, int64_t slot, int r) {
     return a.prefix && u.m0 < 0 ? a.own_ml + slot * a.group + r : a.part_ml + slot * a.rows_cap + r;
-}
-// Channels c .. c + 3 of row r: its output, or its unnormalised part
-template <int D, typename T>
-__device__ __forceinline__ void rows_store4(const RowsArgs &a, const RowsUnit &u, const RowsRow &row, bool whole,
-                                            int64_t slot, int r, int c, const float *x, float l) {
-    if (whole)
-        store4(static_cast<T *>(a.out) + row.out + c, over_sum(x[0], l), over_sum(x[1], l), over_sum(x[2], l),
-               over_sum(x[3], l));
-    else
-        store4(rows_part_o<D>(a, u, slot, r) + (int64_t)(c / 4) * rows_part_step(a, u), x[0], x[1], x[2], x[3]);
 }
 __device__ __forceinline__ void rows_store_ml(const RowsArgs &a, const RowsUnit &u, int64_t slot, int r, float m,
                                               float l) {

@@ -3,9 +3,10 @@
 //     S = Q K^T, m' = max(m, max_j S_j), p_j = 2^(S_j - m'), l' = l 2^(m - m') + sum p, O' = O 2^(m - m') + p V
 // in fp32 on the FMA units, 64 slots of K and V a step, copied asynchronously a step ahead.
 //
-// A CTA of 256 threads holds 64 rows (16 where a part has no more): thread (ty, tx) has rows RPT ty ..,
-// slots tx + 16 j of S and channels 4 tx + 64 k .. of O, so that a row's 16 threads share a half-warp: its
-// maximum and its weights never leave the warp.
+// A CTA of 8 warps holds 64 rows (16 where a part has no more): a warp 8 (2) of them, lane x of it slots x and x + 32
+// of S and channels 2 x, 2 x + 1 (+ 64) of O.  What a warp reads of Q and P is then the same for all lanes, and what it
+// reads of K and V is used for 8 rows.  (Shared memory sets the pace: half-warps of 4 rows took 1.5 times as many of
+// its cycles, warps of 16 rows 0.75 times, but left too few warps to fill it.)
 #include "merge.cuh"
 #include "rows.cuh"
 #include "rows_redo.cuh"
@@ -14,7 +15,7 @@ namespace ikv {
 namespace {
 
 constexpr int kStep = 64;           // slots of K and V a step
-constexpr int kSimtThreads = 256;
+constexpr int kSimtThreads = 256, kSimtWarps = 8;
 
 template <int D, typename T>
 __host__ __device__ constexpr int row_stride() { return D + 16 / (int)sizeof(T); }  // elements: 16 bytes of padding a row
@@ -35,36 +36,26 @@ __device__ __forceinline__ void cp16(void *dst, const void *src, bool real) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
 
-__device__ __forceinline__ void fma4(float *acc, float p, float4 v) {
-    const float2 pp = make_float2(p, p);
-    float2 *a = reinterpret_cast<float2 *>(acc);
-    a[0] = fma2(pp, make_float2(v.x, v.y), a[0]);
-    a[1] = fma2(pp, make_float2(v.z, v.w), a[1]);
+__device__ __forceinline__ float2 load2(const float *p) { return *reinterpret_cast<const float2 *>(p); }
+__device__ __forceinline__ float2 load2(const __nv_bfloat16 *p) {
+    const uint32_t x = *reinterpret_cast<const uint32_t *>(p);
+    return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
 }
 
 // One part: tiles [j0, j0 + n) of pair (unit, g).  (whole: its rows' outputs are final)
 template <int D, typename T, int RPT>
 __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUnit &u, int unit, int g, int j0, int n,
-                          float *sQ, T *sK, T *sV, float *sP) {
-    constexpr int RS = row_stride<D, T>(), NC = D / 16, CH = D * (int)sizeof(T) / 16;
-    const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, lane = tid & 31;
+                          float *sQ, T *sK, T *sV, float *sP, int4 *sRow) {
+    constexpr int RS = row_stride<D, T>(), NC = D / 64, CH = D * (int)sizeof(T) / 16, QS = D + 4, PS = kStep + 4;
+    const int tid = threadIdx.x, lane = tid & 31, r0 = (tid >> 5) * RPT;
     const int rows = u.n * a.group;
-    int seq[RPT], hi[RPT], wlo[RPT];  // of its rows (the rest of a RowsRow again where it is needed)
-#pragma unroll
-    for (int i = 0; i < RPT; ++i) {
-        const RowsRow w = rows_row<D>(a, u, g, ty * RPT + i);
-        seq[i] = ty * RPT + i < rows ? w.seq : -1;
-        hi[i] = w.hi;
-        wlo[i] = w.wlo;
-    }
     const int sh = a.prefix ? u.lo : u.S0 + a.sinks;
+    // the slots that every row sees: [lo, all_hi], without [sh, all_wlo)
+    const int all_hi = a.prefix ? u.hi - 1 : u.p0, all_wlo = a.prefix ? u.lo : max(u.lo, u.p0 + u.n - a.window);
     __syncthreads();  // (the last part's shared memory has been read)
-    for (int i = tid; i < 16 * RPT * (D / 4); i += kSimtThreads) {
-        const int r = i / (D / 4), c = i % (D / 4) * 4;
-        const RowsRow w = rows_row<D>(a, u, g, r);
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r < rows && w.seq >= 0) x = load4(static_cast<const T *>(a.q) + w.q + c);
-        *reinterpret_cast<float4 *>(sQ + r * (D + 4) + c) = x;
+    if (tid < kSimtWarps * RPT) {  // (sequence, last slot, first of the window) of each row
+        const RowsRow w = rows_row<D>(a, u, g, tid);
+        sRow[tid] = make_int4(tid < rows ? w.seq : -1, w.hi, w.wlo, 0);
     }
     const int steps = n * (kRowsTile / kStep);
     auto first_slot = [&](int i) { return rows_tile(u, j0 + i / 2) * kRowsTile + (i & 1) * kStep; };
@@ -78,6 +69,7 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
     auto fetch = [&](int i, int buf) {
         T *k = sK + buf * kStep * RS, *v = sV + buf * kStep * RS;
         const int s0 = first_slot(i);
+#pragma unroll 4
         for (int x = tid; x < kStep * CH; x += kSimtThreads) {
             const int r = x / CH, c = x % CH * (16 / (int)sizeof(T)), s = s0 + r;
             // (slots that no row sees are zeros)
@@ -88,17 +80,24 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    float m[RPT], l[RPT];
-    alignas(8) float acc[RPT][NC];
+    int st = step_from(0), buf = 0;
+    if (st < steps) fetch(st, 0);
+    for (int i = tid; i < kSimtWarps * RPT * (D / 4); i += kSimtThreads) {
+        const int r = i / (D / 4), c = i % (D / 4) * 4;
+        const RowsRow w = rows_row<D>(a, u, g, r);
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < rows && w.seq >= 0) x = load4(static_cast<const T *>(a.q) + w.q + c);
+        *reinterpret_cast<float4 *>(sQ + r * QS + c) = x;
+    }
+    float m[RPT], l[RPT];  // l: of the lane's own slots
+    float2 acc[RPT][NC];
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
         m[i] = -INFINITY;
         l[i] = 0.f;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) acc[i][c] = 0.f;
+        for (int c = 0; c < NC; ++c) acc[i][c] = make_float2(0.f, 0.f);
     }
-    int st = step_from(0), buf = 0;
-    if (st < steps) fetch(st, 0);
     for (int ahead; st < steps; st = ahead, buf ^= 1) {
         ahead = step_from(st + 1);
         if (ahead < steps) {
@@ -110,86 +109,72 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
         __syncthreads();
         const T *k = sK + buf * kStep * RS, *v = sV + buf * kStep * RS;
         const int s0 = first_slot(st);
+        const bool masked = a.pos || s0 < u.lo || s0 + kStep - 1 > all_hi || (s0 < all_wlo && s0 + kStep > sh);
         // (sums of even and of odd channels: two products an instruction)
-        float2 s2[RPT][4];
+        float2 s2[RPT][2];
 #pragma unroll
-        for (int i = 0; i < RPT; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s2[i][j] = make_float2(0.f, 0.f);
-#pragma unroll 4
+        for (int i = 0; i < RPT; ++i) s2[i][0] = s2[i][1] = make_float2(0.f, 0.f);
+#pragma unroll 2
         for (int c = 0; c < D; c += 4) {
-            float4 kk[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) kk[j] = load4(k + (tx + 16 * j) * RS + c);
+            const float4 k0 = load4(k + lane * RS + c), k1 = load4(k + (lane + 32) * RS + c);
 #pragma unroll
             for (int i = 0; i < RPT; ++i) {
-                const float4 q = load4(sQ + (ty * RPT + i) * (D + 4) + c);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s2[i][j] = fma2(make_float2(q.x, q.y), make_float2(kk[j].x, kk[j].y), s2[i][j]);
-                    s2[i][j] = fma2(make_float2(q.z, q.w), make_float2(kk[j].z, kk[j].w), s2[i][j]);
-                }
+                const float4 q = load4(sQ + (r0 + i) * QS + c);
+                s2[i][0] = fma2(make_float2(q.x, q.y), make_float2(k0.x, k0.y), s2[i][0]);
+                s2[i][1] = fma2(make_float2(q.x, q.y), make_float2(k1.x, k1.y), s2[i][1]);
+                s2[i][0] = fma2(make_float2(q.z, q.w), make_float2(k0.z, k0.w), s2[i][0]);
+                s2[i][1] = fma2(make_float2(q.z, q.w), make_float2(k1.z, k1.w), s2[i][1]);
             }
         }
-        float s[RPT][4];
-#pragma unroll
-        for (int i = 0; i < RPT; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[i][j] = s2[i][j].x + s2[i][j].y;
 #pragma unroll
         for (int i = 0; i < RPT; ++i) {
-            float mx = m[i];
-            if (seq[i] < 0 || a.pos || s0 < u.lo || s0 + kStep - 1 > hi[i] || (s0 < wlo[i] && s0 + kStep > sh)) {
+            float z0 = s2[i][0].x + s2[i][0].y, z1 = s2[i][1].x + s2[i][1].y;
+            if (masked) {
+                const int4 x = sRow[r0 + i];
                 RowsRow w;
                 w.lo = u.lo;
-                w.hi = hi[i];
-                w.wlo = wlo[i];
+                w.hi = x.y;
+                w.wlo = x.z;
                 w.sh = sh;
-                w.pos = a.pos && seq[i] >= 0
-                            ? a.pos + ((int64_t)seq[i] * a.rows_per_seq + (a.rows_per_seq == 1 ? 0 : g)) * a.cap
+                w.pos = a.pos && x.x >= 0
+                            ? a.pos + ((int64_t)x.x * a.rows_per_seq + (a.rows_per_seq == 1 ? 0 : g)) * a.cap
                             : nullptr;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (seq[i] < 0 || !rows_sees(w, u.S0, s0 + tx + 16 * j)) s[i][j] = -INFINITY;
+                if (x.x < 0 || !rows_sees(w, u.S0, s0 + lane)) z0 = -INFINITY;
+                if (x.x < 0 || !rows_sees(w, u.S0, s0 + lane + 32)) z1 = -INFINITY;
             }
+            // The maximum only moves where a weight would grow past 2^8: a vote in place of a reduction.  (The
+            // products unrounded: what the maximum is off by is common to all of the row's weights.)
+            const float z = __fmul_rn(fmaxf(z0, z1), a.scale_log2);
+            if (__any_sync(0xffffffffu, z > m[i] + 8.f)) {
+                const float top = fmaxf(m[i], warp_max(z)), f = ex2(m[i] - top);
+                l[i] *= f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, __fmul_rn(s[i][j], a.scale_log2));
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            const float ref = mx == -INFINITY ? 0.f : mx;  // no slot so far: nothing to scale
-            const float f = exp2f(m[i] - ref);
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                // (the product unrounded: what the maximum is off by is common to all of the row's weights)
-                const float p = exp2f(__fmaf_rn(s[i][j], a.scale_log2, -ref));
-                sum += p;
-                sP[(ty * RPT + i) * (kStep + 4) + tx + 16 * j] = p;
+                for (int c = 0; c < NC; ++c) acc[i][c] = fma2(acc[i][c], make_float2(f, f), make_float2(0.f, 0.f));
+                m[i] = top;
             }
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            l[i] = l[i] * f + sum;
-            m[i] = mx;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) acc[i][c] *= f;
+            const float ref = m[i] == -INFINITY ? 0.f : m[i];  // no slot so far: nothing to scale
+            const float p0 = ex2(__fmaf_rn(z0, a.scale_log2, -ref)), p1 = ex2(__fmaf_rn(z1, a.scale_log2, -ref));
+            sP[(r0 + i) * PS + lane] = p0;
+            sP[(r0 + i) * PS + lane + 32] = p1;
+            l[i] += p0 + p1;
         }
-        __syncwarp();  // (a row's weights are written and read by one half-warp)
+        __syncwarp();  // (a row's weights are written and read by one warp)
 #pragma unroll 2
         for (int x = 0; x < kStep; x += 4) {
-            float4 p[RPT];
+            float2 w[4][NC];
 #pragma unroll
-            for (int i = 0; i < RPT; ++i) p[i] = load4(sP + (ty * RPT + i) * (kStep + 4) + x);
+            for (int y = 0; y < 4; ++y)
 #pragma unroll
-            for (int kc = 0; kc < D / 64; ++kc) {
-                float4 w[4];
+                for (int c = 0; c < NC; ++c) w[y][c] = load2(v + (x + y) * RS + 2 * lane + 64 * c);
 #pragma unroll
-                for (int y = 0; y < 4; ++y) w[y] = load4(v + (x + y) * RS + 4 * tx + 64 * kc);
+            for (int i = 0; i < RPT; ++i) {
+                const float4 p = load4(sP + (r0 + i) * PS + x);
 #pragma unroll
-                for (int i = 0; i < RPT; ++i) {
-                    fma4(acc[i] + 4 * kc, p[i].x, w[0]);
-                    fma4(acc[i] + 4 * kc, p[i].y, w[1]);
-                    fma4(acc[i] + 4 * kc, p[i].z, w[2]);
-                    fma4(acc[i] + 4 * kc, p[i].w, w[3]);
+                for (int c = 0; c < NC; ++c) {
+                    acc[i][c] = fma2(make_float2(p.x, p.x), w[0][c], acc[i][c]);
+                    acc[i][c] = fma2(make_float2(p.y, p.y), w[1][c], acc[i][c]);
+                    acc[i][c] = fma2(make_float2(p.z, p.z), w[2][c], acc[i][c]);
+                    acc[i][c] = fma2(make_float2(p.w, p.w), w[3][c], acc[i][c]);
                 }
             }
         }
@@ -201,23 +186,31 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
     const int64_t slot = whole ? 0 : rows_slot(a, head, u, unit, g, blockIdx.x, begins);
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
-        const int r = ty * RPT + i;
+        const int r = r0 + i;
+        if (sRow[r].x < 0) continue;  // (the warp's)
+        const float sum = warp_sum(l[i]);
         bool bad = false;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) bad |= !(fabsf(acc[i][c]) < INFINITY);
-        bad = bad && seq[i] >= 0 && !isnan(l[i]);
-        const unsigned redo = __ballot_sync(0xffffffffu, bad);
-        const bool again = (redo >> (lane & 16)) & 0xffffu;
-        if (seq[i] >= 0 && !again) {
-            const RowsRow w = rows_row<D>(a, u, g, r);
-#pragma unroll
-            for (int kc = 0; kc < D / 64; ++kc)
-                rows_store4<D, T>(a, u, w, whole, slot, r, 4 * tx + 64 * kc, acc[i] + 4 * kc, l[i]);
-            if (!whole && tx == 0) rows_store_ml(a, u, slot, r, m[i], l[i]);
+        for (int c = 0; c < NC; ++c) bad |= !(fabsf(acc[i][c].x) < INFINITY) || !(fabsf(acc[i][c].y) < INFINITY);
+        if (__any_sync(0xffffffffu, bad) && !isnan(sum)) {
+            rows_redo<D, T>(a, unit, g, j0, n, whole, slot, r);
+            continue;
         }
-        for (int half = 0; half < 2; ++half)
-            if ((redo >> (16 * half)) & 0xffffu)
-                rows_redo<D, T>(a, unit, g, j0, n, whole, slot, ((tid >> 5) * 2 + half) * RPT + i);
+        if (whole) {
+            T *to = static_cast<T *>(a.out) + rows_row<D>(a, u, g, r).out + 2 * lane;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                store_as(to + 64 * c, over_sum(acc[i][c].x, sum));
+                store_as(to + 64 * c + 1, over_sum(acc[i][c].y, sum));
+            }
+        } else {
+            const int step = rows_part_step(a, u);
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                *reinterpret_cast<float2 *>(rows_part_o<D>(a, u, slot, r) + (int64_t)(lane / 2 + 16 * c) * step +
+                                            lane % 2 * 2) = acc[i][c];
+            if (lane == 0) rows_store_ml(a, u, slot, r, m[i], sum);
+        }
     }
 }
 
@@ -229,6 +222,7 @@ __global__ void __launch_bounds__(kSimtThreads, D == 64 ? 2 : 1) rows_simt_kerne
     T *sK = reinterpret_cast<T *>(sQ + kRowsSimt * (D + 4));
     T *sV = sK + 2 * kStep * row_stride<D, T>();
     float *sP = reinterpret_cast<float *>(sV + 2 * kStep * row_stride<D, T>());
+    __shared__ int4 sRow[kRowsSimt];
     RowsHead head;
     head.n_pre = __ldcg(&a.head->n_pre);
     RowsWalk w;
@@ -239,9 +233,9 @@ __global__ void __launch_bounds__(kSimtThreads, D == 64 ? 2 : 1) rows_simt_kerne
         const int n = w.part(a, u, j0);
         if (n > 0) {
             if (u.n * a.group <= 16)
-                simt_part<D, T, 1>(a, head, u, w.unit, w.g, j0, n, sQ, sK, sV, sP);
+                simt_part<D, T, 2>(a, head, u, w.unit, w.g, j0, n, sQ, sK, sV, sP, sRow);
             else
-                simt_part<D, T, 4>(a, head, u, w.unit, w.g, j0, n, sQ, sK, sV, sP);
+                simt_part<D, T, 8>(a, head, u, w.unit, w.g, j0, n, sQ, sK, sV, sP, sRow);
         }
         w.next(a, u);
     }

@@ -55,11 +55,6 @@ __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
             return;
         }
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 // The row of a layer's pool that holds slot s of sequence b, KV head g
 __device__ __forceinline__ int pool_row(const RowsArgs &a, int b, int g, int s) {
     const int lp = a.pv.page_shift >= 0 ? s >> a.pv.page_shift : s / a.pv.page_size;
