@@ -82,17 +82,18 @@ RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, 
         a.max_count = w->max_count;
         a.seq_units = (w->max_count + a.unit_n - 1) / a.unit_n;
         units = (int64_t)s->batch * a.seq_units;
+        a.small = units <= 32;
     } else {
         a.prefix = 1;
         a.n_groups = p->n_groups;
         a.first = p->first;
         a.member = p->member;
         a.group_len = p->len;
-        // (64 units, each with at most cap / 128 + 2 tiles and 2 more, and twice that many items)
-        a.small = s->batch <= 32 && p->n_groups <= 32 &&
-                  (int64_t)(a.cap / kRowsTile + 4) * s->kv_heads * 64 * 4 < (int64_t)1 << 31;
+        a.small = s->batch <= 32 && p->n_groups <= 32 && s->batch <= a.unit_n;
         units = (int64_t)p->n_groups + s->batch / a.unit_n + s->batch;
     }
+    // (64 units, each with at most cap / 128 + 2 tiles of cost 4 and 12 more, and twice that many items)
+    a.small = a.small && (int64_t)(a.cap / kRowsTile + 8) * s->kv_heads * 64 * 4 < (int64_t)1 << 31;
     size_t off = 0;
     auto take = [&](auto *&x, size_t count) {
         x = ws ? at<std::remove_reference_t<decltype(*x)>>(ws, off) : nullptr;

@@ -81,7 +81,6 @@ struct RowsArgs {
     int32_t max_count, seq_units;   // seq_units: units of max_count tokens
     // prefix
     int32_t prefix;                 // nonzero: a shared-prefix call
-    int32_t small;                  // nonzero: a plan of at most 32 sequences and groups, whose sums fit 32 bits
     int32_t n_groups;
     const int32_t *first, *member, *group_len;
     // workspace
@@ -105,6 +104,7 @@ struct RowsArgs {
     // continues.  Prefix: pair number + CTA number, in regions of their own for the pairs of shared
     // prefixes and for those of own slots (own_ml, own_o; G rows a slot).
     int32_t rows_cap, ctas;
+    int32_t small;                  // nonzero: a plan for one warp (at most 32 sequences, groups, units), in 32 bits
     float2 *part_ml, *own_ml;
     float *part_o, *own_o;
 };

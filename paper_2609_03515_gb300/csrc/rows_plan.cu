@@ -66,13 +66,43 @@ __device__ __forceinline__ void whole_run(RowsUnit &u, int lo, int hi) {
     u.row0 = 0;
 }
 
+// Query tokens [t0, t0 + unit_n) of a sequence (window); nt = 0 where there are none
+__device__ __forceinline__ RowsUnit window_unit(const RowsArgs &a, uint32_t i) {
+    RowsUnit u{};
+    const int b = (int)(i / (uint32_t)a.seq_units), t0 = (int)(i - (uint32_t)b * a.seq_units) * a.unit_n;
+    const int c = a.count ? min(max(__ldg(a.count + b), 0), a.max_count) : a.max_count;
+    u.S0 = clamp_start(a, b);
+    const int len = clamp_len(a, b, u.S0);
+    u.row0 = a.row0 ? __ldg(a.row0 + b) : b * a.max_count;
+    if (t0 >= c) return u;
+    u.b = b;
+    u.m0 = t0;
+    u.n = min(a.unit_n, c - t0);
+    u.lo = u.S0;
+    u.p0 = u.S0 + len - c + t0;
+    u.hi = u.p0 + u.n;  // the last query's slot and those before
+    if (u.hi > u.S0) {
+        u.wlo = max(u.S0, u.p0 - a.window + 1);
+        u.sh = min(u.S0 + a.sinks, u.hi);
+        u.t_w = u.wlo / kRowsTile;
+        u.t_a = u.S0 / kRowsTile;
+        u.n_a = u.sh > u.S0 ? max(0, min((u.sh - 1) / kRowsTile + 1, u.t_w) - u.t_a) : 0;
+        u.nt = u.n_a + (u.hi - 1) / kRowsTile - u.t_w + 1;
+    } else {  // no query sees a slot: a tile without one makes the zeros
+        u.hi = u.wlo = u.sh = u.S0;
+        u.t_w = u.S0 / kRowsTile;
+        u.nt = 1;
+    }
+    return u;
+}
+
 __device__ __forceinline__ int64_t cost(const RowsArgs &a, const RowsUnit &u) {
     return u.nt > 0 ? pair_cost(rows_cost(a, u.n), u.nt) * a.pv.kv_heads : 0;
 }
 
-// tiles of the score pass: each for every `item_n` members (and, with a utility row a KV head, for each of those)
+// tiles of the score pass: each for every `item_n` members, at least half of a unit's most (and, with a utility row a KV head, for each of those)
 __device__ __forceinline__ int64_t items(const RowsArgs &a, const RowsUnit &u) {
-    return a.items && u.nt > 0 ? (int64_t)u.nt * a.item_subs * ((u.n + a.item_n - 1) / a.item_n) : 0;
+    return a.items && u.nt > 0 ? (int64_t)u.nt * a.item_subs * (u.n > a.item_n ? 2 : 1) : 0;
 }
 
 __device__ __forceinline__ void store_unit(const RowsArgs &a, int at, const RowsUnit &u) {
@@ -121,8 +151,8 @@ __device__ __forceinline__ Sums32 warp_scan(const Sums32 &x, Sums32 &carry) {
     return at;
 }
 
-// The prefix plan of at most 32 sequences and groups, by one warp without a barrier (the general one costs some
-// 4 us more, all of them waits).  tab: 64 words of shared memory.
+// The prefix plan of at most 32 sequences and groups, each group one unit, by one warp without a barrier.  (Its time is
+// that of the instructions on their way from memory, executed once each: it is kept short.)  tab: 64 words of shared memory.
 template <typename Put>
 __device__ __forceinline__ void small_plan(const RowsArgs &a, Put put, Sums32 &sum, int &n_pre, int32_t *tab) {
     constexpr unsigned kAll = 0xffffffffu;
@@ -165,33 +195,22 @@ __device__ __forceinline__ void small_plan(const RowsArgs &a, Put put, Sums32 &s
     if (!counts || __popc(mates) < 2) p = 0;  // (one alone: nothing to share)
     const int e0 = __shfl_sync(kAll, f0, gi), e1 = min(__shfl_sync(kAll, f1, gi), entries);
     RowsUnit u{};
-    int n = 0;
-    if (p > 0 && __ffs(mates) - 1 == lane) {  // the first member makes the group's units
+    if (p > 0 && __ffs(mates) - 1 == lane) {  // the first member makes the group's unit
         u.b = b;
+        u.m0 = e0;
+        u.n = e1 - e0;
         u.S0 = my_S0;
-        n = (e1 - e0 + a.unit_n - 1) / a.unit_n;
-        u.n = min(a.unit_n, e1 - e0);
         whole_run(u, u.S0, u.S0 + p);
     }
-    const int rest = n > 0 ? e1 - e0 - (n - 1) * u.n : 0, most = u.n;
-    RowsUnit last = u;
-    last.n = rest;
-    Sums32 at = warp_scan({n, n > 0 ? (n - 1) * (int)cost(a, u) + (int)cost(a, last) : 0,
-                           n > 0 ? (n - 1) * (int)items(a, u) + (int)items(a, last) : 0}, sum);
+    const Sums32 at = warp_scan({u.nt > 0 ? 1 : 0, (int)cost(a, u), (int)items(a, u)}, sum);
     const int unit0 = __shfl_sync(kAll, at.n, __ffs(mates) - 1);
-    for (int k = 0; k < n; ++k) {
-        u.m0 = e0 + k * most;
-        u.n = k == n - 1 ? rest : most;
-        put(u, {at.n, at.cost, at.items});
-        at = at + Sums32{1, (int)cost(a, u), (int)items(a, u)};
-    }
+    if (u.nt > 0) put(u, {at.n, at.cost, at.items});
     n_pre = sum.n;
     // lane: sequence
     tab[lane] = -1;
     __syncwarp();
     if (counts && p > 0) {
-        const int k = lane - e0;
-        tab[b] = (unit0 + k / a.unit_n) | (k % a.unit_n) << 16;
+        tab[b] = unit0 | (lane - e0) << 16;
         tab[32 + b] = p;
     }
     __syncwarp();
@@ -242,45 +261,17 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
             sizes[at.n] = make_int2(u.nt, (int)pair_cost(rows_cost(a, u.n), u.nt));
         }
     };
-    if (!a.prefix) {
-        const int64_t all = (int64_t)a.batch * a.seq_units;
-        for (int64_t i0 = 0; i0 < all; i0 += nthr) {
-            const int64_t i = i0 + tid;
-            RowsUnit u{};
-            if (i < all) {
-                const int b = (int)(i / a.seq_units), t0 = (int)(i % a.seq_units) * a.unit_n;
-                const int c = a.count ? min(max(__ldg(a.count + b), 0), a.max_count) : a.max_count;
-                if (t0 < c) {
-                    u.b = b;
-                    u.m0 = t0;
-                    u.n = min(a.unit_n, c - t0);
-                    u.S0 = clamp_start(a, b);
-                    u.lo = u.S0;
-                    u.row0 = a.row0 ? __ldg(a.row0 + b) : b * a.max_count;
-                    u.p0 = u.S0 + clamp_len(a, b, u.S0) - c + t0;
-                    u.hi = u.p0 + u.n;  // the last query's slot and those before
-                    if (u.hi > u.S0) {
-                        u.wlo = max(u.S0, u.p0 - a.window + 1);
-                        u.sh = min(u.S0 + a.sinks, u.hi);
-                        u.t_w = u.wlo / kRowsTile;
-                        u.t_a = u.S0 / kRowsTile;
-                        u.n_a = u.sh > u.S0 ? max(0, min((u.sh - 1) / kRowsTile + 1, u.t_w) - u.t_a) : 0;
-                        u.nt = u.n_a + (u.hi - 1) / kRowsTile - u.t_w + 1;
-                    } else {  // no query sees a slot: a tile without one makes the zeros
-                        u.hi = u.wlo = u.sh = u.S0;
-                        u.t_w = u.S0 / kRowsTile;
-                        u.nt = 1;
-                    }
-                }
-            }
-            const Sums at = scan(sc, {u.nt > 0 ? 1 : 0, cost(a, u), 0}, sum);
-            if (u.nt > 0) put(u, at);
-        }
-    } else if (a.small) {
-        // one warp: a lane a group, then an entry, then a sequence
+    if (a.small) {
         if (tid < 32) {
             Sums32 x{0, 0, 0};
-            small_plan(a, put, x, n_pre, small_tab);
+            if (a.prefix) {
+                small_plan(a, put, x, n_pre, small_tab);
+            } else {
+                RowsUnit u{};
+                if (tid < a.batch * a.seq_units) u = window_unit(a, tid);
+                const Sums32 at = warp_scan({u.nt > 0 ? 1 : 0, (int)cost(a, u), 0}, x);
+                if (u.nt > 0) put(u, {at.n, at.cost, 0});
+            }
             if (tid == 0) {
                 bcast = n_pre;
                 bcast_sum = {x.n, x.cost, x.items};
@@ -289,6 +280,14 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
         __syncthreads();
         n_pre = bcast;
         sum = bcast_sum;
+    } else if (!a.prefix) {
+        const uint32_t all = (uint32_t)a.batch * a.seq_units;  // (at most 2^30)
+        for (uint32_t i0 = 0; i0 < all; i0 += nthr) {
+            RowsUnit u{};
+            if (i0 + tid < all) u = window_unit(a, i0 + tid);
+            const Sums at = scan(sc, {u.nt > 0 ? 1 : 0, cost(a, u), 0}, sum);
+            if (u.nt > 0) put(u, at);
+        }
     } else {
         // (small batches keep the tables in shared memory: the chain of their look-ups is the time)
         int32_t *owner = a.owner, *vm = a.vm, *group = a.entry_group;
