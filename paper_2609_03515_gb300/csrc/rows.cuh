@@ -12,6 +12,8 @@
 // them, of its share in turn.  A part leaves an unnormalised output and its (max, sum) in the workspace
 // for the merge kernel.  The plan kernel (one CTA) writes the units and where each share begins.
 #pragma once
+#include <atomic>
+
 #include "ikv_internal.cuh"
 
 namespace ikv {
@@ -28,7 +30,8 @@ struct RowsUnit {                   // 64 bytes
     int32_t lo, hi;                 // every visible slot lies in [lo, hi)
     int32_t p0;                     // window: slot of the first query token (may be below S0)
     int32_t wlo, sh;                // some row sees the slots of [lo, sh) and of [wlo, hi), none sees others
-    int32_t t_a, n_a, t_w, nt;      // tile i of nt: t_a + i for i < n_a, t_w + i - n_a behind
+    int32_t open;                   // nonzero: hi is behind the sequence's last slot, the slots there may hold anything
+    int32_t n_a, t_w, nt;           // tile i of nt: lo / 128 + i for i < n_a, t_w + i - n_a behind
     int32_t row0;                   // window: row of query token 0 in q and out
     int64_t cum;                    // cost of all earlier units, for all KV heads
 };
@@ -117,7 +120,7 @@ __device__ __forceinline__ int64_t rows_slot(const RowsArgs &a, const RowsHead &
 }
 
 // The tile of a unit
-__device__ __forceinline__ int rows_tile(const RowsUnit &u, int i) { return i < u.n_a ? u.t_a + i : u.t_w + i - u.n_a; }
+__device__ __forceinline__ int rows_tile(const RowsUnit &u, int i) { return i < u.n_a ? (u.lo >> 7) + i : u.t_w + i - u.n_a; }
 
 __device__ __forceinline__ RowsUnit rows_unit(const RowsArgs &a, int unit) {
     RowsUnit u;
@@ -196,6 +199,18 @@ __device__ __forceinline__ RowsRow rows_row(const RowsArgs &a, const RowsUnit &u
 }
 __device__ __forceinline__ bool rows_sees(const RowsRow &w, int S0, int s) {
     return s >= w.lo && s <= w.hi && (s >= w.wlo || s < w.sh) && (!w.pos || __ldg(w.pos + (s - S0)) >= 0);
+}
+
+// cudaFuncSetAttribute(kernel, MaxDynamicSharedMemorySize, bytes), once a device (`done`: a bit each)
+template <typename Kernel>
+cudaError_t allow_smem(Kernel kernel, size_t bytes, std::atomic<uint64_t> &done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && (done.load(std::memory_order_relaxed) >> dev) & 1u) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+    return e;
 }
 
 cudaError_t launch_rows_plan(const RowsArgs &a, cudaStream_t st);

@@ -60,7 +60,7 @@ __device__ __forceinline__ void whole_run(RowsUnit &u, int lo, int hi) {
     u.lo = u.wlo = u.sh = lo;
     u.hi = hi;
     u.p0 = 0;
-    u.t_a = u.n_a = 0;
+    u.open = u.n_a = 0;
     u.t_w = lo / kRowsTile;
     u.nt = hi > lo ? (hi - 1) / kRowsTile - u.t_w + 1 : 0;
     u.row0 = 0;
@@ -85,8 +85,8 @@ __device__ __forceinline__ RowsUnit window_unit(const RowsArgs &a, uint32_t i) {
         u.wlo = max(u.S0, u.p0 - a.window + 1);
         u.sh = min(u.S0 + a.sinks, u.hi);
         u.t_w = u.wlo / kRowsTile;
-        u.t_a = u.S0 / kRowsTile;
-        u.n_a = u.sh > u.S0 ? max(0, min((u.sh - 1) / kRowsTile + 1, u.t_w) - u.t_a) : 0;
+        u.open = u.m0 + u.n == c;
+        u.n_a = u.sh > u.S0 ? max(0, min((u.sh - 1) / kRowsTile + 1, u.t_w) - u.S0 / kRowsTile) : 0;
         u.nt = u.n_a + (u.hi - 1) / kRowsTile - u.t_w + 1;
     } else {  // no query sees a slot: a tile without one makes the zeros
         u.hi = u.wlo = u.sh = u.S0;
@@ -227,6 +227,7 @@ __device__ __forceinline__ void small_plan(const RowsArgs &a, Put put, Sums32 &s
         u.n = 1;
         u.S0 = S0;
         whole_run(u, S0 + s.len, S0 + L);
+        u.open = 1;
     }
     const Sums32 own = warp_scan({u.nt > 0 ? 1 : 0, (int)cost(a, u), (int)items(a, u)}, sum);
     if (u.nt > 0) {
@@ -404,6 +405,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
                 u.n = 1;
                 u.S0 = clamp_start(a, b);
                 whole_run(u, u.S0 + s.len, u.S0 + clamp_len(a, b, u.S0));
+                u.open = 1;
             }
             const Sums at = scan(sc, {u.nt > 0 ? 1 : 0, cost(a, u), items(a, u)}, sum);
             if (u.nt > 0) {

@@ -338,8 +338,8 @@ cudaError_t launch_dg(const RowsArgs &a, const RowsScoreArgs &s, cudaStream_t st
     TcMap t;
     CUtensorMap mk;
     if (!layer_map(&mk, a.k, a, D, &t)) return cudaErrorInvalidValue;
-    const cudaError_t e =
-        cudaFuncSetAttribute(rows_score_tc_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sc<D>::kSmem);
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_smem(rows_score_tc_kernel<D, G>, Sc<D>::kSmem, done);
     if (e != cudaSuccess) return e;
     return launch_k(rows_score_tc_kernel<D, G>, dim3(a.ctas), dim3(kThreads), Sc<D>::kSmem, st, mk, a, t, s);
 }

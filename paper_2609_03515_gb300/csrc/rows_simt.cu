@@ -244,7 +244,8 @@ __global__ void __launch_bounds__(kSimtThreads, D == 64 ? 2 : 1) rows_simt_kerne
 template <int D, typename T>
 cudaError_t launch_simt(const RowsArgs &a, cudaStream_t st) {
     constexpr size_t bytes = simt_smem<D, T>();
-    const cudaError_t e = cudaFuncSetAttribute(rows_simt_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_smem(rows_simt_kernel<D, T>, bytes, done);
     if (e != cudaSuccess) return e;
     return launch_k(rows_simt_kernel<D, T>, dim3(a.ctas), dim3(kSimtThreads), bytes, st, a);
 }

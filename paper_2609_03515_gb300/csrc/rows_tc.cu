@@ -63,6 +63,7 @@ __device__ __forceinline__ void load_of(int x, int n, int &tile, bool &is_v) {
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     rows_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                   const __grid_constant__ CUtensorMap tmK8, const __grid_constant__ CUtensorMap tmV8,
                    const __grid_constant__ RowsArgs a, const TcMap tm) {
     using C = Tc<D>;
     using T = __nv_bfloat16;
@@ -138,25 +139,31 @@ __global__ void __launch_bounds__(kThreads, 1)
             while (ok && part_wait()) {
                 const Part p = *part_at();
                 const RowsUnit &u = p.u;
-                const int n = p.n, j0 = p.j0;
+                const int n = p.n, j0 = p.j0, ragged = u.open && (u.hi & (tm.rows_per_box - 1)) ? u.hi : 0x7fffffff;
                 for (int x = 0; x < 2 * n && ok; ++x, ++J) {
                     int tile;
                     bool is_v;
                     load_of(x, n, tile, is_v);
-                    const int s0 = rows_tile(u, j0 + tile) * kRowsTile + lane * tm.rows_per_box, s1 = s0 + tm.rows_per_box;
+                    const int t0 = rows_tile(u, j0 + tile) * kRowsTile, s0 = t0 + lane * tm.rows_per_box, s1 = s0 + tm.rows_per_box;
                     int row = tm.pool_rows;
-                    if (lane < boxes && s0 < u.hi && (s1 > u.wlo || (s0 < u.sh && s1 > u.lo))) {
-                        row = pool_row(a, u.b, p.g, s0);
-                    }
+                    if (lane < boxes && s0 < u.hi && (s1 > u.wlo || (s0 < u.sh && s1 > u.lo))) row = pool_row(a, u.b, p.g, s0);
+                    // the box that the sequence ends in comes 8 rows at a time, and not those behind its end
+                    const int last = t0 + kRowsTile > ragged ? (u.hi - t0) >> tm.box_shift : -1;
+                    const int last_row = last >= 0 ? __shfl_sync(0xffffffffu, row, last) : 0;
                     const int st = J % C::kStages;
                     if (lane == 0) {
                         if (J >= C::kStages) ok = bar_wait(kv_empty(st), (J / C::kStages - 1) & 1, abort_flag);
                         if (ok) mbar_expect_tx(kv_full(st), C::kStage);
                     }
                     ok = __shfl_sync(0xffffffffu, ok, 0);
-                    if (ok && lane < boxes)
-                        tma_rows(base + C::kOffRing + st * C::kStage + lane * tm.rows_per_box * (2 * D), is_v ? &tmV : &tmK, row,
-                                 kv_full(st));
+                    const uint32_t dst = base + C::kOffRing + st * C::kStage;
+                    if (ok && lane < boxes && lane != last)
+                        tma_rows(dst + lane * tm.rows_per_box * (2 * D), is_v ? &tmV : &tmK, row, kv_full(st));
+                    if (ok && last >= 0 && lane < tm.rows_per_box / 8) {
+                        const int s = last * tm.rows_per_box + 8 * lane;
+                        tma_rows(dst + s * (2 * D), is_v ? &tmV8 : &tmK8,
+                                 t0 + s < u.hi && last_row < tm.pool_rows ? last_row + 8 * lane : tm.pool_rows, kv_full(st));
+                    }
                     if (!ok) break;
                 }
                 release();
@@ -186,6 +193,22 @@ __global__ void __launch_bounds__(kThreads, 1)
             while (ok && part_wait()) {
                 const int n = __shfl_sync(0xffffffffu, part_at()->n, 0);
                 const bool pair = __shfl_sync(0xffffffffu, part_at()->u.n * a.group > tile_rows, 0);
+                // Slots behind a sequence's last may hold anything (a pool that was never written), and 0 * NaN would send
+                // every row of the part into rows_redo: their rows of V, at most 7, become zeros
+                const int hi = part_at()->j0 + n == part_at()->u.nt && part_at()->u.open ? part_at()->u.hi : 0;
+                auto clean = [&](Stage v) {
+                    if (hi % 8 == 0) return;
+                    const int r0 = hi % kRowsTile, r = r0 / 8 * 8 + lane / 4;
+                    unsigned char *row = sm + C::kOffRing + v.i * C::kStage + (r >> 3) * (16 * D) + (r & 7) * 128;
+                    if (r >= r0) {
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i)  // 16-byte pieces lane % 4, + 4 ..
+                            *reinterpret_cast<uint4 *>(row + (i >> 1) * kBlock + ((lane & 3) + 4 * (i & 1)) * 16) =
+                                make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_smem();
+                    __syncwarp();
+                };
                 auto there = [&](Stage s) { return warp_wait(kv_full(s.i), s.par, abort_flag); };
                 // S of row tile x; (free: K's stage is done with then)
                 auto qk = [&](int x, Stage k, bool free) {
@@ -247,7 +270,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const bool more = j + 1 < n;
                         if (more) k = take();
                         const Stage v = take();
-                        ok = (!more || there(k)) && there(v) && pv(0, v, j == 0, false);
+                        ok = (!more || there(k)) && there(v);
+                        if (!ok) break;
+                        if (!more) clean(v);
+                        ok = pv(0, v, j == 0, false);
                         if (!ok) break;
                         if (more) qk(0, k, false);
                         ok = pv(1, v, j == 0, true);
@@ -264,7 +290,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (n <= 2) q_done();
                     for (int j = 0; j < n; ++j) {
                         const Stage v = take();
-                        ok = there(v) && pv(j & 1, v, j < 2, true);
+                        ok = there(v);
+                        if (!ok) break;
+                        if (j + 1 == n) clean(v);
+                        ok = pv(j & 1, v, j < 2, true);
                         if (!ok) break;
                         if (j + 2 < n) {
                             k = take();
@@ -402,8 +431,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 bool masked;
                 {
                     const int j = vp->j0 + (pair ? s : 2 * s + X), n_a = vp->u.n_a;
-                    const int t0 = (j < n_a ? vp->u.t_a + j : vp->u.t_w + j - n_a) * kRowsTile;
-                    const int lo = vp->u.lo, S0 = vp->u.S0, sh = a.prefix ? lo : S0 + a.sinks;
+                    const int lo = vp->u.lo, t0 = (j < n_a ? (lo >> 7) + j : vp->u.t_w + j - n_a) * kRowsTile;
+                    const int S0 = vp->u.S0, sh = a.prefix ? lo : S0 + a.sinks;
                     const bool full = seq < 0 || (t0 >= lo && t0 + 127 <= hi && (t0 >= wlo || t0 + 127 < sh));
                     masked = __any_sync(0xffffffffu, !full) || a.pos;
                     if (masked && busy) {
@@ -642,11 +671,14 @@ __global__ void __launch_bounds__(kThreads, 1)
 template <int D>
 cudaError_t launch_tc(const RowsArgs &a, cudaStream_t st) {
     TcMap t;
-    CUtensorMap mk, mv;
-    if (!layer_map(&mk, a.k, a, D, &t) || !layer_map(&mv, a.v, a, D, &t)) return cudaErrorInvalidValue;
-    const cudaError_t e = cudaFuncSetAttribute(rows_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc<D>::kSmem);
+    CUtensorMap mk, mv, mk8, mv8;
+    if (!layer_map(&mk8, a.k, a, D, &t, 8) || !layer_map(&mv8, a.v, a, D, &t, 8) || !layer_map(&mk, a.k, a, D, &t) ||
+        !layer_map(&mv, a.v, a, D, &t))
+        return cudaErrorInvalidValue;
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_smem(rows_tc_kernel<D>, Tc<D>::kSmem, done);
     if (e != cudaSuccess) return e;
-    return launch_k(rows_tc_kernel<D>, dim3(a.ctas), dim3(kThreads), Tc<D>::kSmem, st, mk, mv, a, t);
+    return launch_k(rows_tc_kernel<D>, dim3(a.ctas), dim3(kThreads), Tc<D>::kSmem, st, mk, mv, mk8, mv8, a, t);
 }
 
 }  // namespace

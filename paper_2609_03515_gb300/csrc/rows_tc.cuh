@@ -21,7 +21,8 @@ constexpr uint64_t kLimitNs = 1000000000ull;
 __device__ unsigned int g_tc_timeout = 0;   // (each file's own)
 
 struct TcMap {
-    int32_t rows_per_box, pool_rows;        // pool_rows: rows of the layer, a row behind the end
+    int32_t rows_per_box, box_shift;        // a power of two
+    int32_t pool_rows;                      // rows of the layer: a row behind the end
 };
 
 // Bounded: false where the phase does not complete in time (which also raises the CTA's abort flag and the
@@ -82,15 +83,15 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
 }
 
 // A layer's rows as [groups of 8][64-channel blocks][8 rows][64 channels]
-bool layer_map(CUtensorMap *m, const void *pool, const RowsArgs &a, int head_dim, TcMap *t) {
+bool layer_map(CUtensorMap *m, const void *pool, const RowsArgs &a, int head_dim, TcMap *t, int most = 64) {
     const auto fn = encode_fn();
     if (!fn) return false;
     const uint64_t rows = (uint64_t)a.pv.num_pages * a.pv.kv_heads * a.pv.page_size, row = (uint64_t)head_dim * 2;
     t->pool_rows = (int32_t)rows;
-    // boxes as high as the page allows, at most 64 rows: they are also the grain in which the ends of
-    // what a unit sees are read
+    // boxes as high as the page allows, at most `most` rows: they are also the grain in which what a unit sees is read
     t->rows_per_box = 8;
-    while (t->rows_per_box < 64 && a.pv.page_size % (2 * t->rows_per_box) == 0) t->rows_per_box *= 2;
+    while (t->rows_per_box < most && a.pv.page_size % (2 * t->rows_per_box) == 0) t->rows_per_box *= 2;
+    t->box_shift = __builtin_ctz((unsigned)t->rows_per_box);
     const cuuint64_t dims[4] = {64, 8, (cuuint64_t)head_dim / 64, rows / 8}, strides[3] = {row, 128, 8 * row};
     const cuuint32_t box[4] = {64, 8, (cuuint32_t)head_dim / 64, (cuuint32_t)t->rows_per_box / 8}, es[4] = {1, 1, 1, 1};
     const void *rows0 = static_cast<const char *>(pool) + (size_t)a.layer * rows * row;
