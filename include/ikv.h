@@ -220,7 +220,7 @@ const char *ikv_last_error(void);
 int64_t ikv_launch_count(void);
 
 /* Device-side error word of the current device, then cleared (synchronises
- * the device).  0 = no error.  Bit 0: a bounded wait inside the tensor-core
+ * the device).  0 = no error.  Bit 0: a bounded wait inside a tensor-core
  * attention kernel ran out (the kernel abandoned its work and returned);
  * bit 1: a split longer than the kernel's TMEM budget reached the device;
  * bit 2: an append found no free slot (start + len = cap) and was dropped, or
@@ -229,8 +229,8 @@ int64_t ikv_launch_count(void);
  * was dropped); bit 4: a rank-trace set exceeded 16384 tokens (not traced);
  * bit 5: rows of ikv_q4_store or ikv_q4_load lay outside a sequence's slot space (left alone);
  * bit 6: ikv_pages_writable or ikv_pages_compact needed more pages than were free (nothing was
- * done); bit 7: a sequence number or a block table entry that a page call met was out of range, or
- * ikv_pages_compact was told to keep a slot without a page; bit 8: an append or ikv_q4_store left out a
+ * done); bit 7: a sequence number or a block table entry that a page call met, or a member of ikv_prefix,
+ * was out of range or there twice, or ikv_pages_compact was told to keep a slot without a page; bit 8: an append or ikv_q4_store left out a
  * sequence that cache->writable grants other slots. */
 ikv_status ikv_device_status(uint32_t *flags);
 
@@ -636,9 +636,12 @@ typedef struct {
  *    they hold, and a row that a query does not see (dead, or another sequence's) never reaches its
  *    output, NaN and infinities included.
  *  - A member that is no sequence number, or that an earlier entry names already, is left out, and so
- *    are entries behind the first `batch` ones: bit 7 of the device error word.
- * No page size is excluded; bf16 rows in pages of a multiple of 8 slots take the tensor cores.
- * Dense caches only (IKV_ERR_UNSUPPORTED for code_bits = 4).  Goes by len[], not by cache->max_len.
+ *    are entries behind the first `batch` ones; where first[] does not ascend from 0 or more, no group is
+ *    used: bit 7 of the device error word.
+ * No page size is excluded; bf16 rows in pages of a multiple of 8 slots take the tensor cores (up to 2^25
+ * slots a sequence).  Dense caches only (IKV_ERR_UNSUPPORTED for code_bits = 4).  Goes by len[];
+ * cache->max_len only sizes launches.  May be captured in a graph: lengths, groups and starts are read when it runs.
+ * Fails with IKV_ERR_SHAPE where batch * q_heads passes 2^28 or n_groups 2^20, and above 8192 query heads.
  *  ws: at least ikv_prefix_workspace_size() bytes. */
 ikv_status ikv_prefix_workspace_size(const ikv_shape *shape, const ikv_cache *cache, const ikv_prefix *prefix,
                                      size_t *bytes);
@@ -671,8 +674,9 @@ typedef struct {
  * A query in front of the first slot (count[b] > len[b]) sees nothing.  What a query does not see
  * never reaches its output, NaN and infinities included.  Dense caches only (IKV_ERR_UNSUPPORTED for
  * code_bits = 4); no page size is excluded, bf16 rows in pages of a multiple of 8 slots take the tensor
- * cores.  Goes by len[], not by cache->max_len.  granularity matters for dead slots only.
- * Fails with IKV_ERR_SHAPE where batch * max_count * q_heads passes 2^30.
+ * cores (up to 2^25 slots a sequence).  Goes by len[], not by cache->max_len.  granularity matters for dead
+ * slots only.  May be captured in a graph: lengths, counts, rows and starts are read when it runs.
+ * Fails with IKV_ERR_SHAPE where batch * max_count * q_heads passes 2^30, and above 8192 query heads.
  *  ws: at least ikv_window_workspace_size() bytes. */
 ikv_status ikv_window_workspace_size(const ikv_shape *shape, const ikv_cache *cache, const ikv_window *window,
                                      size_t *bytes);

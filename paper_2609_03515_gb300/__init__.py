@@ -191,6 +191,44 @@ class DecodeCache:
         n = ikv.ikv_step_workspace_size(self.shape(), self.cache(self.cap - 1))
         return torch.zeros(n, dtype=torch.uint8, device=self.k.device)
 
+    # ---- attention over a shared prefix, and through a window --------------
+    def prefix(self, groups: Sequence[Sequence[int]], lengths: Sequence[int]) -> ikv.ikv_prefix:
+        """The groups of ikv_prefix_attend_score: the sequences of each, the one whose pages are read first, and
+        the slots they share.  The struct keeps its device tensors (first, member and length_tensor, which may be
+        rewritten as the lengths change)."""
+        if len(groups) != len(lengths):
+            raise ValueError("a length for each group")
+        member = [b for g in groups for b in g]
+        if len(set(member)) != len(member) or any(not 0 <= b < self.batch for b in member):
+            raise ValueError("each sequence belongs to one group at most")
+        first = [0]
+        for g in groups:
+            first.append(first[-1] + len(g))
+        t = [torch.tensor(list(x) or [0], dtype=torch.int32, device=self.k.device) for x in (first, member, lengths)]
+        p = ikv.ikv_prefix(len(groups), *[x.data_ptr() for x in t])
+        p.first_tensor, p.member_tensor, p.length_tensor = t  # (the struct holds their addresses)
+        return p
+
+    def prefix_workspace(self, prefix: ikv.ikv_prefix) -> torch.Tensor:
+        n = ikv.ikv_prefix_workspace_size(self.shape(), self.cache(), prefix)
+        return torch.empty(n, dtype=torch.uint8, device=self.k.device)
+
+    def window(self, window: int, sinks: int, counts: Sequence[int], q_stride: int = 0,
+               out_stride: int = 0) -> ikv.ikv_window:
+        """What ikv_window_attend is asked for, with the queries of all sequences packed one behind another:
+        counts[b] of sequence b.  The struct keeps its device tensors."""
+        if len(counts) != self.batch or any(n < 0 for n in counts):
+            raise ValueError("a number of queries for each sequence")
+        row0 = [sum(counts[:b]) for b in range(self.batch)]
+        t = [torch.tensor(x, dtype=torch.int32, device=self.k.device) for x in (row0, list(counts))]
+        w = ikv.ikv_window(window, sinks, t[0].data_ptr(), t[1].data_ptr(), max(counts), q_stride, out_stride)
+        w.row0_tensor, w.count_tensor = t  # (the struct holds their addresses)
+        return w
+
+    def window_workspace(self, window: ikv.ikv_window) -> torch.Tensor:
+        n = ikv.ikv_window_workspace_size(self.shape(), self.cache(), window)
+        return torch.empty(n, dtype=torch.uint8, device=self.k.device)
+
     def params(self, alpha: float, refresh_period: int = 1, score_free: bool = False,
                compact_mode: int = ikv.IKV_COMPACT_STABLE, refresh_init: int = ikv.IKV_INIT_ZERO,
                layer_eligible: Optional[Sequence[int]] = None, max_holes: int = 0,

@@ -16,6 +16,14 @@ ikv_status check_rows(const ikv_shape *s, const ikv_cache *c) {
     return IKV_OK;
 }
 
+// (a CTA's share of a call's cost is counted in 32 bits: `units` sets of query rows over up to cap slots)
+ikv_status check_cost(const ikv_shape *s, const ikv_cache *c, int64_t units) {
+    const int64_t pairs = units * s->kv_heads, tiles = cap_of(c) / kRowsTile + 4;
+    if (pairs / sm_count() > ((int64_t)1 << 31) / (kTileTwo * tiles + kExtraTwo) - 1)
+        return report(IKV_ERR_SHAPE, "too many query rows over too long a slot space");
+    return IKV_OK;
+}
+
 ikv_status check_prefix(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p) {
     const ikv_status e = check_rows(s, c);
     if (e) return e;
@@ -25,7 +33,7 @@ ikv_status check_prefix(const ikv_shape *s, const ikv_cache *c, const ikv_prefix
         return report(IKV_ERR_ARG, "prefix first/member/len is NULL");
     if (p->n_groups > (1 << 20) || (int64_t)s->batch * s->q_heads > 1 << 28)
         return report(IKV_ERR_SHAPE, "too many groups or query rows");
-    return IKV_OK;
+    return check_cost(s, c, 2 * (int64_t)s->batch + p->n_groups);
 }
 
 ikv_status check_window(const ikv_shape *s, const ikv_cache *c, const ikv_window *w) {
@@ -42,7 +50,8 @@ ikv_status check_window(const ikv_shape *s, const ikv_cache *c, const ikv_window
         if (x < row) return report(IKV_ERR_SHAPE, "a token's row holds %lld elements", (long long)row);
         if (x % unit) return report(IKV_ERR_ALIGN, "rows of q and out must lie on 16-byte boundaries");
     }
-    return IKV_OK;
+    // (16 query rows a unit at least but for its last)
+    return check_cost(s, c, (int64_t)s->batch * (w->max_count / (16 / (s->q_heads / s->kv_heads)) + 1));
 }
 
 // The arguments of a call but for its pointers to q and results, and its workspace: *bytes of it, at ws

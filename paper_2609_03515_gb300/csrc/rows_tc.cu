@@ -683,9 +683,10 @@ cudaError_t launch_tc(const RowsArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-// (a TMA coordinate is 32 bits, and one behind the last row has to be one too)
+// (A TMA coordinate is 32 bits, and one behind the last row has to be one too.  A pair of 2^18 tiles takes half a
+// second, and the waits for one last a second at most.)
 bool rows_tc_supported(const ikv_shape *s, const ikv_cache *c) {
-    return s->dtype == IKV_BF16 && c->page_size % 8 == 0 &&
+    return s->dtype == IKV_BF16 && c->page_size % 8 == 0 && cap_of(c) <= 1 << 25 &&
            (uint64_t)c->num_pages * s->kv_heads * c->page_size < 0x7fffff00u;
 }
 

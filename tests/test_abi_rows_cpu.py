@@ -84,6 +84,10 @@ def test_window_arguments(lib):
         (dict(out_stride=1025), lib.IKV_ERR_ALIGN),
     ]:
         assert _window(lib, **kw) == want, (kw, lib.ikv_last_error())
+    # more work than a CTA's share can be counted for
+    huge = _cache(lib, page_size=64, max_pages=1 << 23)
+    assert _window(lib, cache=huge, shape=_shape(lib, batch=64), max_count=4096) == lib.IKV_ERR_SHAPE
+    assert _prefix(lib, cache=huge, shape=_shape(lib, batch=1 << 20)) == lib.IKV_ERR_SHAPE
     n = lib.SZ(0)
     w = lib.ikv_window(0, 0, None, None, 1, 0, 0)
     assert lib.raw_status("ikv_window_workspace_size", _shape(lib), _cache(lib), None, ctypes.byref(n)) == lib.IKV_ERR_ARG
