@@ -21,7 +21,7 @@ namespace ikv {
 constexpr int kRowsTile = 128;      // slots a tile
 constexpr int kRowsMaxCtas = 512;
 
-struct RowsUnit {                   // 64 bytes
+struct alignas(16) RowsUnit {                   // 64 bytes
     int32_t b;                      // the sequence whose block table is read
     int32_t m0;                     // window: first query token; prefix: first entry of the member list; -1: one
                                     // sequence's own slots
@@ -50,15 +50,15 @@ struct alignas(16) RowsHead {
     int32_t n_units, n_pre;         // n_pre: units of shared prefixes, in front of the others
     int32_t pad[2];
 };
-struct RowsStart {                  // where a CTA's share begins (at cost `at` of pair (unit, g)), and its cost
+struct alignas(16) RowsStart {                  // where a CTA's share begins (at cost `at` of pair (unit, g)), and its cost
     int32_t unit, g, at, n;
 };
 // The score pass on the tensor cores: an item is a tile of a unit for up to 128 of its rows, and, with a utility
 // row a KV head, one of those; item sub * nt + j of a unit is tile j of its sub-th such set.
-struct RowsItems {                  // where a CTA's begin, and how many it has
+struct alignas(16) RowsItems {                  // where a CTA's begin, and how many it has
     int32_t unit, sub, j, n;
 };
-struct RowsSeq {                    // prefix: what sequence b's rows are made from
+struct alignas(16) RowsSeq {                    // prefix: what sequence b's rows are made from
     int32_t pre, entry;             // its group's unit that holds it (-1: none), its member number there
     int32_t own;                    // its unit of own slots (-1: none)
     int32_t len;                    // slots of its prefix

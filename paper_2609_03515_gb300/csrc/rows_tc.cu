@@ -44,7 +44,7 @@ struct Tc {
     static constexpr int kOffEx = kOffOut + 8 * 2048;
     static constexpr int kOffPart = kOffEx + 2 * 128 * 8 + 128 * 4;
     static constexpr int kOffBar = kOffPart + kParts * sizeof(Part);
-    static constexpr int kBars = 2 * kStages + 13 + 2 * kParts;
+    static constexpr int kBars = 2 * kStages + 11 + 2 * kParts;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
     static constexpr int kSmem = kOffMisc + 16 + 1024;  // (to align by 1024)
 };
@@ -79,10 +79,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto s_full = [&](int x) { return bar1 + 32u + 8u * x; };
     auto p_full = [&](int x) { return bar1 + 48u + 8u * x; };
     auto o_full = [&](int x) { return bar1 + 64u + 8u * x; };
-    auto p_half = [&](int x) { return bar1 + 80u + 8u * x; };
-    auto part_full = [&](int i) { return bar1 + 96u + 8u * i; };
-    auto part_empty = [&](int i) { return bar1 + 96u + 8u * (kParts + i); };
-    const uint32_t joined = bar1 + 96u + 16u * kParts;
+    auto part_full = [&](int i) { return bar1 + 80u + 8u * i; };
+    auto part_empty = [&](int i) { return bar1 + 80u + 8u * (kParts + i); };
+    const uint32_t joined = bar1 + 80u + 16u * kParts;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + C::kOffMisc + 4);
     if (warp == 8 && lane == 0) {
@@ -95,7 +94,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(q_full(x), 64);
             mbar_init(s_full(x), 1);
             mbar_init(p_full(x), 4);
-            mbar_init(p_half(x), 4);
             mbar_init(o_full(x), 1);
         }
         for (int i = 0; i < kParts; ++i) {
@@ -226,26 +224,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     __syncwarp();
                 };
-                // O of row tile x, the first half of the slots as soon as their weights are there
+                // O of row tile x
                 auto pv = [&](int x, Stage v, bool first, bool free) {
-                    if (!warp_wait(p_half(x), np[x] & 1, abort_flag)) return false;
-                    fence_after_sync();
-                    const uint64_t dv = dv0 + v.i * (C::kStage >> 4);
-                    auto product = [&](int kk) {  // V: channels contiguous, 64 of them 1 KB apart
-                        mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * kk, dv + kk * (32 * D >> 4), id_pv,
-                                    !first || kk > 0);
-                    };
-                    if (leader) {
-#pragma unroll
-                        for (int kk = 0; kk < kRowsTile / 32; ++kk) product(kk);
-                    }
-                    __syncwarp();
                     if (!warp_wait(p_full(x), np[x] & 1, abort_flag)) return false;
                     ++np[x];
                     fence_after_sync();
+                    const uint64_t dv = dv0 + v.i * (C::kStage >> 4);
                     if (leader) {
 #pragma unroll
-                        for (int kk = kRowsTile / 32; kk < kRowsTile / 16; ++kk) product(kk);
+                        for (int kk = 0; kk < kRowsTile / 16; ++kk)  // V: channels contiguous, 64 of them 1 KB apart
+                            mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * kk, dv + kk * (32 * D >> 4), id_pv,
+                                        !first || kk > 0);
                         mma_commit(o_full(x));
                         if (free) mma_commit(kv_empty(v.i));
                     }
@@ -516,23 +505,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                             v[k] = *reinterpret_cast<const uint32_t *>(&h);
                         }
                         tmem_st16(tS + 16 * c, v + 16 * c);
-                        if (c == 1) {  // the first 64 slots' weights go ahead
-                            tmem_wait_st();
-                            fence_before_sync();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(p_half(X));
-                        }
                     }
                     const float2 s01 = add2(sum[0], sum[1]), s23 = add2(sum[2], sum[3]);
                     l += (s01.x + s01.y) + (s23.x + s23.y);
                     tmem_wait_st();
-                } else if (lane == 0) {
-                    mbar_arrive(p_half(X));
                 }
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full(X));
                 ++np;
+            }
+            // where the results go (while the last product is under way)
+            const Part *p = part_at();
+            const bool begins = p->j0 == 0, whole = begins && n == p->u.nt && !a.prefix;
+            RowsHead h;
+            h.n_pre = n_pre;
+            const int64_t slot = whole ? 0 : rows_slot(a, h, p->u, p->unit, p->g, blockIdx.x, begins);
+            const int k0 = pair || X == 0 ? 0 : D / 2, step = rows_part_step(a, p->u);
+            unsigned char *stage = sm + C::kOffOut + warp * 2048;
+            T *to[4];  // of a whole pair: where this lane stores pieces of rows lane / 4 + 8 i
+            float *part = rows_part_o<D>(a, p->u, slot, r) + (int64_t)(k0 / 4) * step;
+            if (whole) {
+                const int64_t mine = seq >= 0 ? rows_row<D>(a, p->u, p->g, r).out : -1;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t at = __shfl_sync(0xffffffffu, mine, 8 * i + lane / 4);
+                    to[i] = at >= 0 ? static_cast<T *>(a.out) + at + k0 + lane % 4 * 8 : nullptr;
+                }
             }
             if (steps > 0) {
                 if (ok) ok = bar_wait(o_full(X), (np - 1) & 1, abort_flag);
@@ -558,50 +557,32 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             float probe = 0.f;  // NaN once a value is not finite
-            const Part *p = part_at();
-            const bool begins = p->j0 == 0, whole = begins && n == p->u.nt && !a.prefix;
-            RowsRow row = rows_row<D>(a, p->u, p->g, r);
-            row.seq = seq;
-            RowsHead h;
-            h.n_pre = n_pre;
-            const int64_t slot = whole ? 0 : rows_slot(a, h, p->u, p->unit, p->g, blockIdx.x, begins);
             if (ok && busy) {
                 const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-                const int k0 = pair || X == 0 ? 0 : D / 2;
-                unsigned char *stage = sm + C::kOffOut + warp * 2048;
-                const int step = rows_part_step(a, p->u);
-                float *part = rows_part_o<D>(a, p->u, slot, r) + (int64_t)(k0 / 4) * step;
-                T *to[4];  // where this lane stores pieces of rows lane / 4 + 8 i
-                if (whole) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int64_t at = __shfl_sync(0xffffffffu, row.seq >= 0 ? row.out : -1, 8 * i + lane / 4);
-                        to[i] = at >= 0 ? static_cast<T *>(a.out) + at + k0 + lane % 4 * 8 : nullptr;
-                    }
-                }
                 const float2 zero2 = make_float2(0.f, 0.f), inv2 = make_float2(inv, inv);
                 float2 look = zero2;
                 auto pair_of = [](const uint32_t *v, int i) {
                     return make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
                 };
                 const int chunks = pair ? D / 32 : D / 64;
+                // v: the chunk at hand; w: B's part of it, or A's (B's) next, on its way meanwhile
+                uint32_t v[32], w[32];
+                const bool both = !pair && n > 1;
+                const uint32_t from = tO + (pair ? 128 * X : 0) + k0, then = both ? tO + 128 + k0 : from + 32;
+                tmem_ld32(from, v);
+                tmem_ld32(then, w);  // (within O in any case)
+                tmem_wait_ld(v);
 #pragma unroll 1
                 for (int c = 0; c < chunks; ++c) {  // channels k0 + 32 c ..
-                    uint32_t v[32];
-                    tmem_ld32(tO + (pair ? 128 * X : 0) + k0 + 32 * c, v);
-                    if (!pair && n > 1) {
-                        uint32_t o[32];
-                        tmem_ld32(tO + 128 + k0 + 32 * c, o);
-                        tmem_wait_ld(v);
-                        tmem_wait_ld(o);
+                    if (both) {
+                        tmem_wait_ld(w);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float2 z = fma2(pair_of(o, i), make_float2(f1, f1), fma2(pair_of(v, i), make_float2(f0, f0), zero2));
+                            const float2 z = fma2(pair_of(w, i), make_float2(f1, f1), fma2(pair_of(v, i), make_float2(f0, f0), zero2));
                             v[2 * i] = __float_as_uint(z.x);
                             v[2 * i + 1] = __float_as_uint(z.y);
                         }
                     }
-                    tmem_wait_ld(v);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) look = fma2(pair_of(v, i), zero2, look);
                     if (whole) {
@@ -630,15 +611,27 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             if (to[i]) *reinterpret_cast<uint4 *>(to[i] + 32 * c) = x[i];
-                    } else if (row.seq >= 0) {
+                    } else if (seq >= 0) {
                         float *d = part + (int64_t)(8 * c) * step;
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
                             *reinterpret_cast<uint4 *>(d + i * step) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                     }
+                    if (c + 1 == chunks) break;
+                    if (both) {
+                        tmem_ld32(from + 32 * (c + 1), v);
+                        tmem_ld32(then + 32 * (c + 1), w);
+                        tmem_wait_ld(v);
+                    } else {
+                        tmem_wait_ld(w);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = w[i];
+                        if (c + 2 < chunks) tmem_ld32(from + 32 * (c + 2), w);
+                    }
                 }
+                tmem_wait_ld(w);
                 probe = look.x + look.y;
-                if (row.seq >= 0 && !whole && (pair || X == 0)) rows_store_ml(a, p->u, slot, r, m, l);
+                if (seq >= 0 && !whole && (pair || X == 0)) rows_store_ml(a, p->u, slot, r, m, l);
             }
             if (!pair) {
                 // both outputs have been read, and ex: B's findings go to A
