@@ -201,6 +201,7 @@ __device__ __forceinline__ void small_plan(const RowsArgs &a, Put put, Sums32 &s
         u.n = e1 - e0;
         u.S0 = my_S0;
         whole_run(u, u.S0, u.S0 + p);
+        u.open = p == my_len;
     }
     const Sums32 at = warp_scan({u.nt > 0 ? 1 : 0, (int)cost(a, u), (int)items(a, u)}, sum);
     const int unit0 = __shfl_sync(kAll, at.n, __ffs(mates) - 1);
@@ -368,6 +369,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
                 u.S0 = clamp_start(a, u.b);
                 u.n = min(a.unit_n, e1 - e0);
                 whole_run(u, u.S0, u.S0 + gp[i]);
+                u.open = gp[i] == clamp_len(a, u.b, u.S0);
             }
             // (all but a group's last unit are full)
             const int most = u.n, rest = n > 0 ? e1 - e0 - (n - 1) * most : 0;

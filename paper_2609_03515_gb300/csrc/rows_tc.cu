@@ -15,10 +15,15 @@
 // in 32 bits; rounding them to bf16 for the product costs at most 2^-8 of sum p |V|.
 //
 // Warps: 0-3 and 4-7 the two row tiles, 8 TMA, 9 MMA, 10-11 Q; 11 also finds the parts of the share, ahead of the
-// others.  K and V tiles pass through a ring of
-// 32 KB (D = 64: 16 KB) stages in the order K0 K1 V0 K2 V1 .., which is the order of the products.  Boxes of
-// a tile that no row sees are fetched from behind the tensor's end, which fills zeros and reads nothing.
-// Every wait is bounded; on timeout the CTA sets the error word, drains what is in flight and returns.
+// others.  K and V tiles pass through a ring of 32 KB (D = 64: 16 KB) stages in the order K0 K1 V0 K2 V1 .., which
+// is the order of the products.  Boxes of a tile that no row sees are fetched from behind the tensor's end, which
+// fills zeros and reads nothing.  Every wait is bounded; on timeout the CTA sets the error word, drains what is in
+// flight and returns.
+//
+// Measured: a causal prompt of 16384 tokens, 32 / 8 heads of 128, 1475 us (1.49 PFLOP/s; 1.45 us a step of 256 rows by
+// 128 slots, 1.05 at the tensor cores' rate: their issue and its hand-offs are what is left).  Two prefixes of 8k for 16
+// sequences each: 31 of 47 us in here, 64 KB of K and V every 1.05 us and SM (93% of the copy rate) between the starts
+// and outputs of its pairs.
 #include "rows_tc.cuh"
 
 namespace ikv {
@@ -468,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (s == 0) {
                         m = top;
                     } else {
-                        const bool move = top > m + kSlack;
+                        const bool move = seq >= 0 && top > m + kSlack;  // (rows that are none hold anything)
                         if (__any_sync(0xffffffffu, move)) {
                             const float f = move ? ex2(m - top) : 1.f;
                             ok = bar_wait(o_full(X), (np - 1) & 1, abort_flag);

@@ -180,6 +180,15 @@ def test_a_dead_row_that_is_not_finite_reaches_only_the_members_that_see_it(dtyp
     assert bool(call.score[1, :160].isnan().all())
 
 
+@pytest.mark.parametrize("dtype,page", [("bf16", 16), ("bf16", 24), ("f32", 16)])
+def test_a_prefix_up_to_the_first_members_end(dtype, page):
+    """Nothing of the first member's own, NaN behind it; a slot space that is full."""
+    lens = [5 * page - 7, 5 * page - 7 + 1, 5 * page]
+    c = Cache(lens, 2, 4, 128, dtype, page, seed=14, share=[(0, [1, 2], lens[0])], extra_pages=0).device()
+    check(c, [[0, 1, 2]], [lens[0]], ema=True)
+    check(c, [[0, 1, 2]], [5 * page])
+
+
 def test_no_groups_and_lone_members():
     lens = [130, 61, 300]
     c = Cache(lens, 2, 4, 128, "bf16", 64, seed=8).device()

@@ -183,6 +183,17 @@ def test_long_contexts_split_over_the_gpu(dtype):
         check(c, counts, window, 4, layer=0)
 
 
+@pytest.mark.parametrize("dtype,page", [("bf16", 16), ("bf16", 48), ("f32", 16)])
+def test_a_slot_space_that_is_full(dtype, page):
+    """The last slot is the slot space's last: nothing behind the block table is looked up."""
+    lens = [6 * page - 3, 6 * page - 17, 1]
+    c = Cache(lens, 2, 4, 128, dtype, page, seed=15, starts=[3, 17, 6 * page - 1], extra_pages=0).device()
+    assert c.cap == 6 * page
+    for kind in ("one", "some", "all"):
+        check(c, counts_of(lens, kind), 40, 5)
+        check(c, counts_of(lens, kind), 0, 0)
+
+
 def test_many_short_sequences():
     lens = [1 + (i * 37) % 90 for i in range(300)]
     c = Cache(lens, 1, 8, 64, "bf16", 16, seed=12, layers=1).device()
