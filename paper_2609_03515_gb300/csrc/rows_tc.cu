@@ -569,27 +569,31 @@ __global__ void __launch_bounds__(kThreads, 1)
                 auto pair_of = [](const uint32_t *v, int i) {
                     return make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
                 };
-                const int chunks = pair ? D / 32 : D / 64;
-                // v: the chunk at hand; w: B's part of it, or A's (B's) next, on its way meanwhile
-                uint32_t v[32], w[32];
+                // all of it on its way at once: beside running products a look into tensor memory takes some 1000 cycles
+                constexpr int kHalf = D / 64;  // chunks of 32 channels of half a row
                 const bool both = !pair && n > 1;
-                const uint32_t from = tO + (pair ? 128 * X : 0) + k0, then = both ? tO + 128 + k0 : from + 32;
-                tmem_ld32(from, v);
-                tmem_ld32(then, w);  // (within O in any case)
-                tmem_wait_ld(v);
-#pragma unroll 1
-                for (int c = 0; c < chunks; ++c) {  // channels k0 + 32 c ..
-                    if (both) {
-                        tmem_wait_ld(w);
+                const int chunks = pair ? 2 * kHalf : kHalf;
+                const uint32_t from = tO + (pair ? 128 * X : 0) + k0, then = both ? tO + 128 + k0 : from + 32 * kHalf;
+                uint32_t v[64 * kHalf];  // the row, or A's and B's parts of half of it
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float2 z = fma2(pair_of(w, i), make_float2(f1, f1), fma2(pair_of(v, i), make_float2(f0, f0), zero2));
-                            v[2 * i] = __float_as_uint(z.x);
-                            v[2 * i + 1] = __float_as_uint(z.y);
-                        }
+                for (int c = 0; c < kHalf; ++c) tmem_ld32(from + 32 * c, v + 32 * c);
+#pragma unroll
+                for (int c = 0; c < kHalf; ++c) tmem_ld32(then + 32 * c, v + 32 * (kHalf + c));
+#pragma unroll
+                for (int c = 0; c < 2 * kHalf; ++c) tmem_wait_ld(v + 32 * c);
+                if (both) {
+#pragma unroll
+                    for (int i = 0; i < 16 * kHalf; ++i) {
+                        const float2 z = fma2(pair_of(v + 32 * kHalf, i), make_float2(f1, f1), fma2(pair_of(v, i), make_float2(f0, f0), zero2));
+                        v[2 * i] = __float_as_uint(z.x);
+                        v[2 * i + 1] = __float_as_uint(z.y);
                     }
+                }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) look = fma2(pair_of(v, i), zero2, look);
+                for (int c = 0; c < 2 * kHalf; ++c) {  // channels k0 + 32 c ..
+                    if (c >= chunks) break;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) look = fma2(pair_of(v + 32 * c, i), zero2, look);
                     if (whole) {
                         // 32 channels of 32 rows at a time through shared memory: four lanes store 64 bytes of a row,
                         // where a lane a row would touch 32 lines with every store
@@ -599,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             uint32_t q[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const float2 z = fma2(pair_of(v, 4 * i + e), inv2, zero2);
+                                const float2 z = fma2(pair_of(v + 32 * c, 4 * i + e), inv2, zero2);
                                 const __nv_bfloat162 b2 = __floats2bfloat162_rn(z.x, z.y);
                                 q[e] = *reinterpret_cast<const uint32_t *>(&b2);
                             }
@@ -620,21 +624,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                         float *d = part + (int64_t)(8 * c) * step;
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            *reinterpret_cast<uint4 *>(d + i * step) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                    }
-                    if (c + 1 == chunks) break;
-                    if (both) {
-                        tmem_ld32(from + 32 * (c + 1), v);
-                        tmem_ld32(then + 32 * (c + 1), w);
-                        tmem_wait_ld(v);
-                    } else {
-                        tmem_wait_ld(w);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = w[i];
-                        if (c + 2 < chunks) tmem_ld32(from + 32 * (c + 2), w);
+                            *reinterpret_cast<uint4 *>(d + i * step) = make_uint4(v[32 * c + 4 * i], v[32 * c + 4 * i + 1], v[32 * c + 4 * i + 2], v[32 * c + 4 * i + 3]);
                     }
                 }
-                tmem_wait_ld(w);
                 probe = look.x + look.y;
                 if (seq >= 0 && !whole && (pair || X == 0)) rows_store_ml(a, p->u, slot, r, m, l);
             }
