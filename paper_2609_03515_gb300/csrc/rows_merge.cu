@@ -2,7 +2,8 @@
 //     M = max m_i, out = (sum 2^(m_i - M) O_i) / (sum 2^(m_i - M) l_i).
 // A CTA merges up to 8 rows of one pair.  Window: only the pairs that a share's border cuts have parts, and
 // each border's CTA finds its own.  Prefix: every row has parts, of its group's pair and of its own.
-// Latency is what it costs: the first parts' outputs are loaded before their weights are known.
+// Latency is what it costs, 3 us for a few parts a row: the first parts' outputs are loaded before their weights are
+// known, and every thread looks its row's weights up itself.
 #include "rows_redo.cuh"
 
 namespace ikv {

@@ -22,7 +22,7 @@
 //
 // Measured: a causal prompt of 16384 tokens, 32 / 8 heads of 128, 1475 us (1.49 PFLOP/s; 1.45 us a step of 256 rows by
 // 128 slots, 1.05 at the tensor cores' rate: their issue and its hand-offs are what is left).  Two prefixes of 8k for 16
-// sequences each: 31 of 47 us in here, 64 KB of K and V every 1.05 us and SM (93% of the copy rate) between the starts
+// sequences each: 31 of 48 us in here, 64 KB of K and V every 1.05 us and SM (93% of the copy rate) between the starts
 // and outputs of its pairs.
 #include "rows_tc.cuh"
 
