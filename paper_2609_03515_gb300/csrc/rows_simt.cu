@@ -58,10 +58,13 @@ __device__ void simt_part(const RowsArgs &a, const RowsHead &head, const RowsUni
     // the slots that every row sees: [lo, all_hi], without [sh, all_wlo)
     const int all_hi = a.prefix ? u.hi - 1 : u.p0, all_wlo = a.prefix ? u.lo : max(u.lo, u.p0 + u.n - a.window);
     __syncthreads();  // (the last part's shared memory has been read)
-    if (tid < kSimtWarps * RPT) {  // (sequence, last slot, first of the window) of each row
-        const RowsRow w = rows_row<D>(a, u, g, tid);
-        sRow[tid] = make_int4(tid < rows ? w.seq : -1, w.hi, w.wlo, 0);
+    if (lane < RPT) {  // (sequence, last slot, first of the window) of each row, by the warp that reads it: a unit
+                       // that sees no slot has no step, and no other barrier
+        const int r = r0 + lane;
+        const RowsRow w = rows_row<D>(a, u, g, r);
+        sRow[r] = make_int4(r < rows ? w.seq : -1, w.hi, w.wlo, 0);
     }
+    __syncwarp();
     const int steps = n * (kRowsTile / kStep);
     auto first_slot = [&](int i) { return rows_tile(u, j0 + i / 2) * kRowsTile + (i & 1) * kStep; };
     auto step_from = [&](int i) {  // the first from i on with a slot that some row sees
