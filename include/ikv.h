@@ -635,6 +635,8 @@ typedef struct {
  *  - A sequence without a live slot gets out = 0.  Slots outside a sequence are never used, whatever
  *    they hold, and a row that a query does not see (dead, or another sequence's) never reaches its
  *    output, NaN and infinities included.
+ *  - Where a bounded wait ran out (bit 0 of the device error word) out is undefined; score and ema hold
+ *    what they held before if it was the attention's.
  *  - A member that is no sequence number, or that an earlier entry names already, is left out, and so
  *    are entries behind the first `batch` ones; where first[] does not ascend from 0 or more, no group is
  *    used: bit 7 of the device error word.

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "ikv.h"
 
 namespace ikv {
@@ -384,5 +386,8 @@ cudaError_t read_clear_pages_error(unsigned int *v);
 cudaError_t read_clear_rows_error(unsigned int *v);
 // the same of the kernels of attend.cu (bit 2)
 cudaError_t read_clear_attend_error(unsigned int *v);
+
+// nonzero: the next launch of a tensor-core attention is a test of its bounded waits
+extern std::atomic<int> g_stall_next;
 
 }  // namespace ikv

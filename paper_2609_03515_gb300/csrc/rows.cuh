@@ -48,7 +48,8 @@ constexpr int kTileOne = 3, kExtraOne = 6, kTileTwo = 4, kExtraTwo = 12;
 struct alignas(16) RowsHead {
     int64_t total, per;             // cost in all, of a CTA's share
     int32_t n_units, n_pre;         // n_pre: units of shared prefixes, in front of the others
-    int32_t pad[2];
+    int32_t failed;                 // nonzero: a wait of the attention ran out, parts are missing
+    int32_t pad;
 };
 struct alignas(16) RowsStart {                  // where a CTA's share begins (at cost `at` of pair (unit, g)), and its cost
     int32_t unit, g, at, n;

@@ -93,7 +93,9 @@ __global__ void __launch_bounds__(2 * D, (kAhead == 2 ? 1280 : 768) / (2 * D)) r
     RowsWalk w;
     w.begin(__ldcg(reinterpret_cast<const int4 *>(a.start + c)));
     if (w.left == 0 || w.at == 0) return;
-    const int64_t per = __ldcg(&a.head->per);
+    const RowsHead head = rows_head(a);
+    if (head.failed) return;
+    const int64_t per = head.per;
     const RowsUnit u = rows_unit(a, w.unit);
     const RowsCost cost = rows_cost(a, u.n);
     const int j = tile_at(cost, w.at);
@@ -120,6 +122,7 @@ __global__ void __launch_bounds__(2 * D, 768 / (2 * D)) rows_merge_prefix_kernel
     const int hk = a.pv.kv_heads, b = blockIdx.x / hk, g = blockIdx.x % hk;
     const int4 s = __ldcg(reinterpret_cast<const int4 *>(a.seq) + b);
     const RowsHead head = rows_head(a);
+    if (head.failed) return;
     RowsUnit pre, own;
     if (s.x >= 0) pre = rows_unit(a, s.x);
     if (s.z >= 0) own = rows_unit(a, s.z);

@@ -427,6 +427,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
         a.head->per = per;
         a.head->n_units = sum.n;
         a.head->n_pre = n_pre;
+        a.head->failed = 0;
     }
     auto size = [&](int i) {
         return i < kPlanCum ? sizes[i]

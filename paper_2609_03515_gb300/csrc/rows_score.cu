@@ -120,6 +120,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tmem = *tmem_slot;
     Items w;
     w.begin(a);
+    if (__ldcg(&a.head->failed)) w.left = 0;  // no norms
     int J = 0;  // (item, KV head) products so far: stage J % kStages, half J % 2 of tensor memory
     if (warp == 8) {
         // ---------------- K

@@ -49,7 +49,7 @@ struct Tc {
     static constexpr int kOffEx = kOffOut + 8 * 2048;
     static constexpr int kOffPart = kOffEx + 2 * 128 * 8 + 128 * 4;
     static constexpr int kOffBar = kOffPart + kParts * sizeof(Part);
-    static constexpr int kBars = 2 * kStages + 11 + 2 * kParts;
+    static constexpr int kBars = 2 * kStages + 12 + 2 * kParts;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
     static constexpr int kSmem = kOffMisc + 16 + 1024;  // (to align by 1024)
 };
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto o_full = [&](int x) { return bar1 + 64u + 8u * x; };
     auto part_full = [&](int i) { return bar1 + 80u + 8u * i; };
     auto part_empty = [&](int i) { return bar1 + 80u + 8u * (kParts + i); };
-    const uint32_t joined = bar1 + 80u + 16u * kParts;
+    const uint32_t joined = bar1 + 80u + 16u * kParts, stall_bar = joined + 8;  // (nothing arrives at the latter)
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + C::kOffMisc + 4);
     if (warp == 8 && lane == 0) {
@@ -106,6 +106,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(part_empty(i), 12);  // every warp
         }
         mbar_init(joined, 8);
+        mbar_init(stall_bar, 1);
         mbar_init(mma_done, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -193,6 +194,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             uint32_t np[2] = {0, 0};       // weights taken
             bool ok = true;
+            if (tm.stall) ok = __all_sync(0xffffffffu, bar_wait_long(stall_bar, 0, abort_flag, kStallNs));  // runs out
             while (ok && part_wait()) {
                 const int n = __shfl_sync(0xffffffffu, part_at()->n, 0);
                 const bool pair = __shfl_sync(0xffffffffu, part_at()->u.n * a.group > tile_rows, 0);
@@ -652,6 +654,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     fence_before_sync();
     __syncthreads();
+    if (tid == 0 && *abort_flag) a.head->failed = 1;  // (the merge and the scores have nothing to go by)
     if (warp == 9) {
         fence_after_sync();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
@@ -665,6 +668,7 @@ cudaError_t launch_tc(const RowsArgs &a, cudaStream_t st) {
     if (!layer_map(&mk8, a.k, a, D, &t, 8) || !layer_map(&mv8, a.v, a, D, &t, 8) || !layer_map(&mk, a.k, a, D, &t) ||
         !layer_map(&mv, a.v, a, D, &t))
         return cudaErrorInvalidValue;
+    t.stall = g_stall_next.exchange(0);
     static std::atomic<uint64_t> done{0};
     const cudaError_t e = allow_smem(rows_tc_kernel<D>, Tc<D>::kSmem, done);
     if (e != cudaSuccess) return e;

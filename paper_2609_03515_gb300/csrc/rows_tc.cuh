@@ -17,22 +17,25 @@ namespace {
 constexpr int kAtom = 128 * 128;            // bytes of 64 channels of 128 query rows
 constexpr int kBlock = 1024;                // bytes of 64 channels of 8 slots
 constexpr uint64_t kLimitNs = 1000000000ull;
+constexpr uint64_t kStallNs = 10000ull;     // of the wait that a test makes run out
 
 __device__ unsigned int g_tc_timeout = 0;   // (each file's own)
 
 struct TcMap {
     int32_t rows_per_box, box_shift;        // a power of two
     int32_t pool_rows;                      // rows of the layer: a row behind the end
+    int32_t stall;                          // nonzero: the products wait for what never comes (a test's launch)
 };
 
 // Bounded: false where the phase does not complete in time (which also raises the CTA's abort flag and the
 // error word), or once another warp has given up.
-__device__ __forceinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *abort) {
+__device__ __forceinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *abort,
+                                              uint64_t limit = kLimitNs) {
     const uint64_t start = global_ns();
     for (;;) {
         if (mbar_try(bar, parity, 2000)) return true;
         if (*abort) return false;
-        if (global_ns() - start > kLimitNs) break;
+        if (global_ns() - start > limit) break;
     }
     *abort = 1;
     atomicOr(&g_tc_timeout, 1u);
