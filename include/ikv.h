@@ -242,6 +242,11 @@ ikv_status ikv_device_status(uint32_t *flags);
  * Host only; launches nothing. */
 ikv_status ikv_test_stall_next_attention(void);
 
+/* The same for the next score pass of ikv_prefix_attend_score on the tensor cores: its wait, in every CTA's
+ * second product, runs out.  out is as ever; scores and utilities that the pass had not finished by then are
+ * left as they were. */
+ikv_status ikv_test_stall_next_score(void);
+
 /* Which decode-attention kernel ikv_decode_attend_score and ikv_step launch for
  * this shape and cache (all layers, cache->max_len):
  * IKV_PATH_TENSOR_CORE -- TMA-staged K/V tiles, tcgen05 QK^T and PV with TMEM
@@ -635,8 +640,8 @@ typedef struct {
  *  - A sequence without a live slot gets out = 0.  Slots outside a sequence are never used, whatever
  *    they hold, and a row that a query does not see (dead, or another sequence's) never reaches its
  *    output, NaN and infinities included.
- *  - Where a bounded wait ran out (bit 0 of the device error word) out is undefined; score and ema hold
- *    what they held before if it was the attention's.
+ *  - Where a bounded wait ran out (bit 0 of the device error word) out is undefined; score and ema hold whole
+ *    results or what they held before, and before in all places if it was the attention's.
  *  - A member that is no sequence number, or that an earlier entry names already, is left out, and so
  *    are entries behind the first `batch` ones; where first[] does not ascend from 0 or more, no group is
  *    used: bit 7 of the device error word.

@@ -855,7 +855,7 @@ int tc_passes(int64_t units, int n_chunks, int sms, bool gsum) {
     return n_chunks;
 }
 
-std::atomic<int> g_stall_next{0};
+std::atomic<int> g_stall_next{0}, g_stall_next_score{0};
 
 cudaError_t launch_attend_tc(const AttendArgs &a, const TcOutputs &o, int group, int sms, cudaStream_t st) {
     const int rpb = a.pv.page_size >= kTile ? kTile : a.pv.page_size;
@@ -922,6 +922,11 @@ cudaError_t launch_attend_tc(const AttendArgs &a, const TcOutputs &o, int group,
 
 extern "C" ikv_status ikv_test_stall_next_attention(void) {
     ikv::g_stall_next.store(1);
+    return IKV_OK;
+}
+
+extern "C" ikv_status ikv_test_stall_next_score(void) {
+    ikv::g_stall_next_score.store(1);
     return IKV_OK;
 }
 

@@ -387,7 +387,8 @@ cudaError_t read_clear_rows_error(unsigned int *v);
 // the same of the kernels of attend.cu (bit 2)
 cudaError_t read_clear_attend_error(unsigned int *v);
 
-// nonzero: the next launch of a tensor-core attention is a test of its bounded waits
-extern std::atomic<int> g_stall_next;
+// nonzero: the next launch of a tensor-core attention, of the packed rows' score pass on the tensor cores, is a
+// test of its bounded waits
+extern std::atomic<int> g_stall_next, g_stall_next_score;
 
 }  // namespace ikv

@@ -28,7 +28,7 @@ struct Sc {
     static constexpr int kOffNorm = kStages * 2 * kTile;  // (M, 1 / W) of a product's rows
     static constexpr int kNorms = 8;  // Q may be three products ahead of the products, and they two ahead of the weights
     static constexpr int kOffBar = kOffNorm + kNorms * 128 * 8;
-    static constexpr int kBars = 3 * kStages + 5 + kNorms;
+    static constexpr int kBars = 3 * kStages + 6 + kNorms;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
     static constexpr int kSmem = kOffMisc + 16 + 1024;
 };
@@ -91,6 +91,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto s_empty = [&](int x) { return bar1 + 16u + 8u * x; };
     const uint32_t mma_done = bar1 + 32u;
     auto n_full = [&](int i) { return bar1 + 40u + 8u * i; };  // a product's norms
+    const uint32_t stall_bar = n_full(C::kNorms);  // nothing arrives here
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + C::kOffMisc + 4);
     if (warp == 8 && lane == 0) {
@@ -105,6 +106,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int i = 0; i < C::kNorms; ++i) mbar_init(n_full(i), 64);
         mbar_init(mma_done, 1);
+        mbar_init(stall_bar, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -162,6 +164,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ok = warp_wait(k_full(st), (J / C::kStages) & 1, abort_flag) &&
                      warp_wait(q_full(st), (J / C::kStages) & 1, abort_flag) &&
                      (J < 2 || warp_wait(s_empty(x), (J / 2 - 1) & 1, abort_flag));
+                if (tm.stall && J == 1)  // runs out, within an item that averages over KV heads
+                    ok = __all_sync(0xffffffffu, bar_wait_long(stall_bar, 0, abort_flag, kStallNs));
                 if (!ok) break;
                 fence_async_smem();  // (Q came by plain copies)
                 fence_after_sync();
@@ -298,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 fence_before_sync();
                 mbar_arrive(s_empty(x));
-                if (out) {
+                if (out && ok) {  // (after a wait that ran out the sums are not whole: score and ema stay as they are)
 #pragma unroll
                     for (int m0 = 0; m0 < kMembers; m0 += kBlockM) {
                         if (m0 >= mine) continue;
@@ -342,6 +346,7 @@ cudaError_t launch_dg(const RowsArgs &a, const RowsScoreArgs &s, cudaStream_t st
     TcMap t;
     CUtensorMap mk;
     if (!layer_map(&mk, a.k, a, D, &t)) return cudaErrorInvalidValue;
+    t.stall = g_stall_next_score.exchange(0);
     static std::atomic<uint64_t> done{0};
     const cudaError_t e = allow_smem(rows_score_tc_kernel<D, G>, Sc<D>::kSmem, done);
     if (e != cudaSuccess) return e;

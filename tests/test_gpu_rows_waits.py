@@ -48,6 +48,24 @@ def test_prefix_attention_that_gives_up_leaves_scores_and_utilities(d):
     right(call)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_score_pass_that_gives_up_stores_no_partial_sums(d):
+    """It stops between the KV heads of an item: sums over the first alone must not be stored."""
+    call = make(d)
+    ikv.ikv_test_stall_next_score()
+    call.run()
+    torch.cuda.synchronize()
+    assert ikv.ikv_device_status() == 1
+    assert ikv.ikv_device_status() == 0
+    same(call)
+    out, tol, _, _ = reference(call)
+    assert bool(((call.out.cpu().double() - out).abs() <= tol).all())
+    call.run()
+    torch.cuda.synchronize()
+    assert ikv.ikv_device_status() == 0
+    right(call)
+
+
 def test_window_that_gives_up_reports_it_and_the_next_call_is_right():
     c = Cache([700, 33], 2, 4, 128, "bf16", 16, seed=22, layers=1).device()
     q = torch.randn(733, c.h * c.d, generator=torch.Generator().manual_seed(3)).to(DT["bf16"]).cuda()
