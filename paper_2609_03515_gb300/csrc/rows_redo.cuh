@@ -58,37 +58,61 @@ __device__ __forceinline__ void rows_store_ml(const RowsArgs &a, const RowsUnit 
     *rows_part_ml(a, u, slot, r) = make_float2(m, l);
 }
 
+// Four values of a row
+__device__ __forceinline__ float4 load4_as_float(const float *p) { return __ldg(reinterpret_cast<const float4 *>(p)); }
+__device__ __forceinline__ float4 load4_as_float(const __nv_bfloat16 *p) {
+    const uint2 x = __ldg(reinterpret_cast<const uint2 *>(p));
+    return make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
+                       __uint_as_float(x.y & 0xffff0000u));
+}
+
 // Row r of a part by one warp, over the slots that it sees and no others: the products of a whole tile
-// multiply rows of V that a row does not see by 0, which leaves NaN where those are not finite.  Rare,
-// so simple: a slot at a time.
+// multiply rows of V that a row does not see by 0, which leaves NaN where those are not finite.  32 slots at a
+// time, a lane a slot for the scores, a lane D / 32 channels for the output.
 template <int D, typename T>
 __device__ __noinline__ void rows_redo(const RowsArgs &a, int unit, int g, int j0, int n, bool whole, int64_t slot,
                                        int r) {
     constexpr int E = D / 32;
+    constexpr unsigned kAll = 0xffffffffu;
     const RowsUnit u = rows_unit(a, unit);
     const int lane = threadIdx.x & 31;
     const RowsRow row = rows_row<D>(a, u, g, r);
-    float q[E], acc[E], m = -INFINITY, l = 0.f;
+    const T *q = static_cast<const T *>(a.q) + row.q;
+    float acc[E], m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        q[e] = load_as_float(static_cast<const T *>(a.q) + row.q + lane + 32 * e);
-        acc[e] = 0.f;
-    }
-    for (int j = j0; j < j0 + n; ++j) {
-        const int t0 = rows_tile(u, j) * kRowsTile;
-        for (int s = t0; s < t0 + kRowsTile; ++s) {
-            if (!rows_sees(row, u.S0, s)) continue;
-            const int64_t at = a.pv.row_phys(u.b, a.layer, g, s) * D + lane;
-            float z = 0.f;
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    for (int i = 4 * j0; i < 4 * (j0 + n); ++i) {
+        const int s = rows_tile(u, i / 4) * kRowsTile + i % 4 * 32 + lane;
+        const bool sees = rows_sees(row, u.S0, s);
+        const unsigned all = __ballot_sync(kAll, sees);
+        if (!all) continue;
+        const int64_t at = sees ? a.pv.row_phys(u.b, a.layer, g, s) * D : 0;
+        float z = -INFINITY;
+        if (sees) {
+            const T *k = static_cast<const T *>(a.k) + at;
+            float2 z2 = make_float2(0.f, 0.f);
+#pragma unroll 8
+            for (int c = 0; c < D; c += 4) {
+                const float4 x = load4_as_float(k + c), y = load4_as_float(q + c);
+                z2 = fma2(make_float2(x.x, x.y), make_float2(y.x, y.y), z2);
+                z2 = fma2(make_float2(x.z, x.w), make_float2(y.z, y.w), z2);
+            }
+            z = z2.x + z2.y;
+        }
+        const float mx = fmaxf(m, warp_max(__fmul_rn(z, a.scale_log2))), ref = mx == -INFINITY ? 0.f : mx;
+        const float f = exp2f(m - ref), p = sees ? exp2f(__fmaf_rn(z, a.scale_log2, -ref)) : 0.f;
+        l = l * f + warp_sum(p);
+        m = mx;
 #pragma unroll
-            for (int e = 0; e < E; ++e) z += q[e] * load_as_float(static_cast<const T *>(a.k) + at + 32 * e);
-            z = warp_sum(z);
-            const float mx = fmaxf(m, __fmul_rn(z, a.scale_log2)), ref = mx == -INFINITY ? 0.f : mx;
-            const float f = exp2f(m - ref), p = exp2f(__fmaf_rn(z, a.scale_log2, -ref));
-            l = l * f + p;
-            m = mx;
+        for (int e = 0; e < E; ++e) acc[e] *= f;
+#pragma unroll 8
+        for (int x = 0; x < 32; ++x) {
+            const float w = __shfl_sync(kAll, p, x);
+            const T *v = static_cast<const T *>(a.v) + __shfl_sync(kAll, at, x) + lane;
+            if ((all >> x) & 1u) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = acc[e] * f + p * load_as_float(static_cast<const T *>(a.v) + at + 32 * e);
+                for (int e = 0; e < E; ++e) acc[e] += w * load_as_float(v + 32 * e);
+            }
         }
     }
     if (whole) {

@@ -14,6 +14,9 @@
 // rescaled: weights and sum are relative to the same m, which cancels in O / l.  The sum takes the weights
 // in 32 bits; rounding them to bf16 for the product costs at most 2^-8 of sum p |V|.
 //
+// A row that met a row of V which it does not see and which is not finite (0 * inf) is computed again behind the CTA's
+// last part, where no warp waits for another any more: it may take as long as the row's slots do.
+//
 // Warps: 0-3 and 4-7 the two row tiles, 8 TMA, 9 MMA, 10-11 Q; 11 also finds the parts of the share, ahead of the
 // others.  K and V tiles pass through a ring of 32 KB (D = 64: 16 KB) stages in the order K0 K1 V0 K2 V1 .., which
 // is the order of the products.  Boxes of a tile that no row sees are fetched from behind the tensor's end, which
@@ -65,6 +68,72 @@ __device__ __forceinline__ void load_of(int x, int n, int &tile, bool &is_v) {
     tile = x == 2 * n - 1 ? n - 1 : is_v ? (x - 2) / 2 : (x + 1) / 2;
 }
 
+// Whether a row that the CTA has stored holds NaN or infinities though its sum is a number.  (A whole pair's sums are
+// not kept.)
+template <int D>
+__device__ __forceinline__ bool row_suspect(const RowsArgs &a, const RowsUnit &u, const RowsRow &row, bool whole, int64_t slot,
+                                            int r) {
+    const int lane = threadIdx.x & 31;
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) {
+        const int c = lane + 32 * e;
+        const float x = whole ? __bfloat162float(static_cast<const __nv_bfloat16 *>(a.out)[row.out + c])
+                              : __ldcg(rows_part_o<D>(a, u, slot, r) + (int64_t)(c / 4) * rows_part_step(a, u) + c % 4);
+        bad |= !(fabsf(x) < INFINITY);
+    }
+    return __any_sync(0xffffffffu, bad) && (whole || !isnan(__ldcg(rows_part_ml(a, u, slot, r)).y));
+}
+// Whether among the part's tiles lies a row of V that is not finite and that the row does not see.  (In a box that was
+// copied: elsewhere there need not be a page.  What was cleared of such a box counts too, and costs time alone.)
+template <int D>
+__device__ __forceinline__ bool row_misled(const RowsArgs &a, const TcMap &tm, const RowsUnit &u, const RowsRow &row, int g, int j0,
+                                           int n) {
+    const int lane = threadIdx.x & 31;
+    for (int i = 4 * j0; i < 4 * (j0 + n); ++i) {
+        const int s = rows_tile(u, i / 4) * kRowsTile + i % 4 * 32 + lane, s0 = s & -tm.rows_per_box, s1 = s0 + tm.rows_per_box;
+        bool look = s0 < u.hi && (s1 > u.wlo || (s0 < u.sh && s1 > u.lo)) && !rows_sees(row, u.S0, s);
+        int64_t at = 0;
+        if (look) {
+            const int row8 = pool_row(a, u.b, g, s);
+            look = row8 >= 0 && row8 < tm.pool_rows;
+            at = ((int64_t)a.layer * tm.pool_rows + row8) * D;
+        }
+        unsigned all = __ballot_sync(0xffffffffu, look);
+        while (all) {
+            const int x = __ffs(all) - 1;
+            all &= all - 1;
+            const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v) + __shfl_sync(0xffffffffu, at, x) + lane;
+            bool bad = false;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) bad |= !(fabsf(__bfloat162float(v[32 * e])) < INFINITY);
+            if (__any_sync(0xffffffffu, bad)) return true;
+        }
+    }
+    return false;
+}
+// The CTA's share once more, a warp of `warps` a row: the rows that have to be computed again
+template <int D>
+__device__ __noinline__ void redo_share(const RowsArgs &a, const TcMap &tm, int n_pre, int warp, int warps) {
+    RowsHead h;
+    h.n_pre = n_pre;
+    RowsWalk w;
+    w.begin(__ldcg(reinterpret_cast<const int4 *>(a.start + blockIdx.x)));
+    while (w.left > 0) {
+        const RowsUnit u = rows_unit(a, w.unit);
+        int j0;
+        const int n = w.part(a, u, j0);
+        const bool begins = j0 == 0, whole = begins && n == u.nt && !a.prefix;
+        const int64_t slot = whole || n <= 0 ? 0 : rows_slot(a, h, u, w.unit, w.g, blockIdx.x, begins);
+        for (int r = warp; n > 0 && r < u.n * a.group; r += warps) {
+            const RowsRow row = rows_row<D>(a, u, w.g, r);
+            if (row.seq >= 0 && row_suspect<D>(a, u, row, whole, slot, r) && row_misled<D>(a, tm, u, row, w.g, j0, n))
+                rows_redo<D, __nv_bfloat16>(a, w.unit, w.g, j0, n, whole, slot, r);
+        }
+        w.next(a, u);
+    }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     rows_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -89,6 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t joined = bar1 + 80u + 16u * kParts, stall_bar = joined + 8;  // (nothing arrives at the latter)
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + C::kOffMisc + 4);
+    volatile int *redo_flag = abort_flag + 1;   // some row's output is not finite though its sum is
     if (warp == 8 && lane == 0) {
         for (int i = 0; i < C::kStages; ++i) {
             mbar_init(kv_full(i), 1);
@@ -109,6 +179,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(stall_bar, 1);
         mbar_init(mma_done, 1);
         *abort_flag = 0;
+        *redo_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) {
@@ -640,17 +711,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (X == 0) probe += found[row_in];
             }
             if (ok && busy && (pair || X == 0)) {
-                // (see rows_redo: V rows that are not finite and that the row does not see)
-                __syncwarp();  // (it stores over what other lanes did)
-                unsigned redo = __ballot_sync(0xffffffffu, isnan(probe) && seq >= 0 && !isnan(l));
-                while (redo) {
-                    const int i = __ffs(redo) - 1;
-                    redo &= redo - 1;
-                    rows_redo<D, T>(a, p->unit, p->g, p->j0, n, whole, slot, __shfl_sync(0xffffffffu, r, i));
-                }
+                // (perhaps for V rows that are not finite and that the row does not see)
+                if (isnan(probe) && seq >= 0 && !isnan(l)) *redo_flag = 1;
             }
             release();
         }
+        // every part of the share is stored: nothing waits for these warps but the end of the CTA
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (*redo_flag && !*abort_flag) redo_share<D>(a, tm, n_pre, warp, 8);
     }
     fence_before_sync();
     __syncthreads();
