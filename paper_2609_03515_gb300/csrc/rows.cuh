@@ -30,7 +30,8 @@ struct alignas(16) RowsUnit {                   // 64 bytes
     int32_t lo, hi;                 // every visible slot lies in [lo, hi)
     int32_t p0;                     // window: slot of the first query token (may be below S0)
     int32_t wlo, sh;                // some row sees the slots of [lo, sh) and of [wlo, hi), none sees others
-    int32_t open;                   // nonzero: hi is behind the sequence's last slot, the slots there may hold anything
+    int32_t open;                   // nonzero: a copy of up to 64 slots that ends at hi or behind it may reach behind the
+                                    // sequence's last slot, where anything may lie
     int32_t n_a, t_w, nt;           // tile i of nt: lo / 128 + i for i < n_a, t_w + i - n_a behind
     int32_t row0;                   // window: row of query token 0 in q and out
     int64_t cum;                    // cost of all earlier units, for all KV heads

@@ -56,6 +56,9 @@ __device__ __forceinline__ int clamp_len(const RowsArgs &a, int b, int S0) {
     return min(max(__ldg(a.len + b), 0), a.cap - S0);
 }
 
+// RowsUnit::open of a unit that ends at slot hi of a sequence that ends at `end`
+__device__ __forceinline__ int32_t is_open(int hi, int end) { return ((hi + 63) & ~63) > end; }
+
 // a run of slots [lo, hi) seen by every row of a unit
 __device__ __forceinline__ void whole_run(RowsUnit &u, int lo, int hi) {
     u.lo = u.wlo = u.sh = lo;
@@ -86,7 +89,7 @@ __device__ __forceinline__ RowsUnit window_unit(const RowsArgs &a, uint32_t i) {
         u.wlo = max(u.S0, u.p0 - a.window + 1);
         u.sh = min(u.S0 + a.sinks, u.hi);
         u.t_w = u.wlo / kRowsTile;
-        u.open = u.m0 + u.n == c;
+        u.open = is_open(u.hi, u.S0 + len);
         u.n_a = u.sh > u.S0 ? max(0, min((u.sh - 1) / kRowsTile + 1, u.t_w) - u.S0 / kRowsTile) : 0;
         u.nt = u.n_a + (u.hi - 1) / kRowsTile - u.t_w + 1;
     } else {  // no query sees a slot: a tile without one makes the zeros
@@ -202,7 +205,7 @@ __device__ __forceinline__ void small_plan(const RowsArgs &a, Put put, Sums32 &s
         u.n = e1 - e0;
         u.S0 = my_S0;
         whole_run(u, u.S0, u.S0 + p);
-        u.open = p == my_len;
+        u.open = is_open(u.hi, u.S0 + my_len);
     }
     const Sums32 at = warp_scan({u.nt > 0 ? 1 : 0, (int)cost(a, u), (int)items(a, u)}, sum);
     const int unit0 = __shfl_sync(kAll, at.n, __ffs(mates) - 1);
@@ -370,7 +373,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
                 u.S0 = clamp_start(a, u.b);
                 u.n = min(a.unit_n, e1 - e0);
                 whole_run(u, u.S0, u.S0 + gp[i]);
-                u.open = gp[i] == clamp_len(a, u.b, u.S0);
+                u.open = is_open(u.hi, u.S0 + clamp_len(a, u.b, u.S0));
             }
             // (all but a group's last unit are full)
             const int most = u.n, rest = n > 0 ? e1 - e0 - (n - 1) * most : 0;

@@ -92,7 +92,7 @@ __device__ __forceinline__ bool row_misled(const RowsArgs &a, const TcMap &tm, c
     const int lane = threadIdx.x & 31;
     for (int i = 4 * j0; i < 4 * (j0 + n); ++i) {
         const int s = rows_tile(u, i / 4) * kRowsTile + i % 4 * 32 + lane, s0 = s & -tm.rows_per_box, s1 = s0 + tm.rows_per_box;
-        bool look = s0 < u.hi && (s1 > u.wlo || (s0 < u.sh && s1 > u.lo)) && !rows_sees(row, u.S0, s);
+        bool look = s >= u.lo && s0 < u.hi && (s1 > u.wlo || s0 < u.sh) && !rows_sees(row, u.S0, s);
         int64_t at = 0;
         if (look) {
             const int row8 = pool_row(a, u.b, g, s);
@@ -223,8 +223,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     int row = tm.pool_rows;
                     if (lane < boxes && s0 < u.hi && (s1 > u.wlo || (s0 < u.sh && s1 > u.lo))) row = pool_row(a, u.b, p.g, s0);
                     // the box that the sequence ends in comes 8 rows at a time, and not those behind its end
+                    // (V's box that the unit's slots begin in likewise, and not those in front)
                     const int last = t0 + kRowsTile > ragged ? (u.hi - t0) >> tm.box_shift : -1;
-                    const int last_row = last >= 0 ? __shfl_sync(0xffffffffu, row, last) : 0;
+                    const int first = is_v && (u.lo & -kRowsTile) == t0 && (u.lo & (tm.rows_per_box - 1)) ? (u.lo - t0) >> tm.box_shift : -1;
                     const int st = J % C::kStages;
                     if (lane == 0) {
                         if (J >= C::kStages) ok = bar_wait(kv_empty(st), (J / C::kStages - 1) & 1, abort_flag);
@@ -232,12 +233,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     ok = __shfl_sync(0xffffffffu, ok, 0);
                     const uint32_t dst = base + C::kOffRing + st * C::kStage;
-                    if (ok && lane < boxes && lane != last)
+                    if (ok && lane < boxes && lane != last && lane != first)
                         tma_rows(dst + lane * tm.rows_per_box * (2 * D), is_v ? &tmV : &tmK, row, kv_full(st));
-                    if (ok && last >= 0 && lane < tm.rows_per_box / 8) {
-                        const int s = last * tm.rows_per_box + 8 * lane;
-                        tma_rows(dst + s * (2 * D), is_v ? &tmV8 : &tmK8,
-                                 t0 + s < u.hi && last_row < tm.pool_rows ? last_row + 8 * lane : tm.pool_rows, kv_full(st));
+                    if (ok && (last >= 0 || first >= 0)) {
+                        const int edge = lane < 8 ? last : lane < 16 && first != last ? first : -1;  // rows 8 (lane % 8) of it
+                        const int from = __shfl_sync(0xffffffffu, row, max(edge, 0));
+                        const int s = edge * tm.rows_per_box + 8 * (lane % 8);
+                        const bool real = t0 + s < u.hi && t0 + s + 8 > u.lo && from < tm.pool_rows;
+                        if (edge >= 0 && lane % 8 < tm.rows_per_box / 8)
+                            tma_rows(dst + s * (2 * D), is_v ? &tmV8 : &tmK8, real ? from + 8 * (lane % 8) : tm.pool_rows, kv_full(st));
                     }
                     if (!ok) break;
                 }
@@ -269,14 +273,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             while (ok && part_wait()) {
                 const int n = __shfl_sync(0xffffffffu, part_at()->n, 0);
                 const bool pair = __shfl_sync(0xffffffffu, part_at()->u.n * a.group > tile_rows, 0);
-                // Slots behind a sequence's last may hold anything (a pool that was never written), and 0 * NaN would send
-                // every row of the part into rows_redo: their rows of V, at most 7, become zeros
+                // Slots behind a sequence's last, and those in front of a unit's first (of a page that begins earlier, of a
+                // prefix that is read elsewhere), may hold anything, a pool that was never written, and 0 * NaN would have
+                // every row of the part computed again: their rows of V, at most 7 at either end, become zeros.  (1.3 % of
+                // two prefixes of 8k, 0.7 % of prompts)
                 const int hi = part_at()->j0 + n == part_at()->u.nt && part_at()->u.open ? part_at()->u.hi : 0;
-                auto clean = [&](Stage v) {
-                    if (hi % 8 == 0) return;
-                    const int r0 = hi % kRowsTile, r = r0 / 8 * 8 + lane / 4;
+                const int lo = part_at()->j0 == 0 && rows_tile(part_at()->u, 0) == part_at()->u.lo >> 7 ? part_at()->u.lo : 0;
+                // rows of V behind or in front of slot `end`, in its group of 8
+                auto clean = [&](Stage v, int end, bool behind) {
+                    if (end % 8 == 0) return;
+                    const int r0 = end % kRowsTile, r = r0 / 8 * 8 + lane / 4;
                     unsigned char *row = sm + C::kOffRing + v.i * C::kStage + (r >> 3) * (16 * D) + (r & 7) * 128;
-                    if (r >= r0) {
+                    if (behind == (r >= r0)) {
 #pragma unroll
                         for (int i = 0; i < D / 32; ++i)  // 16-byte pieces lane % 4, + 4 ..
                             *reinterpret_cast<uint4 *>(row + (i >> 1) * kBlock + ((lane & 3) + 4 * (i & 1)) * 16) =
@@ -339,7 +347,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const Stage v = take();
                         ok = (!more || there(k)) && there(v);
                         if (!ok) break;
-                        if (!more) clean(v);
+                        if (j == 0) clean(v, lo, false);
+                        if (!more) clean(v, hi, true);
                         ok = pv(0, v, j == 0, false);
                         if (!ok) break;
                         if (more) qk(0, k, false);
@@ -359,7 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const Stage v = take();
                         ok = there(v);
                         if (!ok) break;
-                        if (j + 1 == n) clean(v);
+                        if (j == 0) clean(v, lo, false);
+                        if (j + 1 == n) clean(v, hi, true);
                         ok = pv(j & 1, v, j < 2, true);
                         if (!ok) break;
                         if (j + 2 < n) {
