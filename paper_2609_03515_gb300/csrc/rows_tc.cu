@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         int64_t row = row0 + tok;
                         bool real = true;
                         if (many) {
-                            const int b = __ldg(a.vm + u.m0 + tok);
+                            const int b = __ldcg(a.vm + u.m0 + tok);
                             real = b >= 0;
                             row = real ? b : 0;
                         }
