@@ -463,6 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 release();
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");  // (after an abort some may be on their way)
         }
     } else {
         // ---------------- weights and outputs: thread r of a warpgroup holds row r of its row tile
