@@ -111,7 +111,7 @@ RowsArgs rows_args(const ikv_shape *s, const ikv_cache *c, const ikv_prefix *p, 
     take(a.head, 1);
     take(a.start, a.ctas);
     take(a.units, units);
-    if (a.pos) {
+    if (a.pos && tc) {  // (the kernels without tensor cores read the positions themselves)
         a.live_words = (a.cap + 31) / 32;
         take(a.live, (size_t)a.batch * a.rows_per_seq * a.live_words);
     }

@@ -47,10 +47,9 @@ struct RowsCost {
 constexpr int kTileOne = 3, kExtraOne = 6, kTileTwo = 4, kExtraTwo = 12;
 
 struct alignas(16) RowsHead {
-    int64_t total, per;             // cost in all, of a CTA's share
-    int32_t n_units, n_pre;         // n_pre: units of shared prefixes, in front of the others
+    int64_t per;                    // cost of a CTA's share
+    int32_t n_pre;                  // units of shared prefixes, in front of the others
     int32_t failed;                 // nonzero: a wait of the attention ran out, parts are missing
-    int32_t pad;
 };
 struct alignas(16) RowsStart {                  // where a CTA's share begins (at cost `at` of pair (unit, g)), and its cost
     int32_t unit, g, at, n;
@@ -72,7 +71,8 @@ struct RowsArgs {
     int32_t layer;
     const int32_t *len;             // [batch]
     const int32_t *pos;             // [rows][cap], -1 at dead slots, or null
-    uint32_t *live;                 // with pos: [rows][live_words] workspace, bit j of a row: slot j is live
+    uint32_t *live;                 // with pos, on the tensor cores: [rows][live_words] workspace, bit j of a row: slot
+                                    // j is live
     int32_t live_words;
     int32_t rows_per_seq, cap, batch, q_heads, group;
     float scale_log2;               // log2(e) / sqrt(d)

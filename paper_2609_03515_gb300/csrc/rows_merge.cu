@@ -13,9 +13,7 @@ constexpr int kMergeRows = 8;
 
 __device__ __forceinline__ RowsHead rows_head(const RowsArgs &a) {
     RowsHead h;
-    const int4 x = __ldcg(reinterpret_cast<const int4 *>(a.head)), y = __ldcg(reinterpret_cast<const int4 *>(a.head) + 1);
-    reinterpret_cast<int4 *>(&h)[0] = x;
-    reinterpret_cast<int4 *>(&h)[1] = y;
+    *reinterpret_cast<int4 *>(&h) = __ldcg(reinterpret_cast<const int4 *>(a.head));
     return h;
 }
 // (a division of 64 bits takes longer than a look-up in memory)

@@ -426,9 +426,7 @@ __global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(const RowsArgs 
     // (a share has at least a tile's cost: none that lies in a pair's tiles is empty)
     const int64_t per = max(share(sum.cost), (int64_t)(a.unit_n > a.tile_n ? kTileTwo : kTileOne));
     if (tid == 0) {
-        a.head->total = sum.cost;
         a.head->per = per;
-        a.head->n_units = sum.n;
         a.head->n_pre = n_pre;
         a.head->failed = 0;
     }
