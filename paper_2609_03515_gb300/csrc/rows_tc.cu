@@ -414,39 +414,44 @@ __global__ void __launch_bounds__(kThreads, 1)
             // Every piece by an asynchronous copy, all of them in flight: four lanes a row, 16 rows an iteration.
             // A's rows are handed over first.
             constexpr int CH = D / 8;      // 16-byte pieces of a row
+            constexpr int kAtOnce = 2;    // rows of a thread
             const int t = tid - 320, c = t & 3;
             while (ok && part_wait()) {
                 const RowsUnit u = part_at()->u;
                 const int rows = u.n * a.group;
                 const bool many = a.prefix && u.m0 >= 0;
-                const int64_t row0 = a.prefix ? u.b : (int64_t)u.row0 + u.m0;
+                const int64_t row0 = many ? 0 : a.prefix ? u.b : (int64_t)u.row0 + u.m0;
                 const T *q = static_cast<const T *>(a.q) + (int64_t)part_at()->g * a.group * D + 8 * c;
                 if (seg > 0) ok = warp_wait(q_empty, (seg - 1) & 1, abort_flag);
                 for (int x = 0; x < 2 && ok; ++x) {
                     const int first = x * tile_rows, end = min(rows - first, tile_rows);
                     int tok = (first + t / 4) / a.group, h = (first + t / 4) % a.group;
-#pragma unroll 2
-                    for (int r = t / 4; r < end; r += 16) {
-                        int64_t row = row0 + tok;
-                        bool real = true;
-                        if (many) {
-                            const int b = __ldcg(a.vm + u.m0 + tok);
-                            real = b >= 0;
-                            row = real ? b : 0;
-                        }
-                        const T *src = q + row * a.q_stride + (int64_t)h * D;
-                        const uint32_t dst = base + x * C::kStage + r * 128;
+                    for (int r0 = t / 4; r0 < end; r0 += 16 * kAtOnce) {
+                        int who[kAtOnce], head[kAtOnce];  // (members are looked up ahead of the copies)
 #pragma unroll
-                        for (int i = 0; i < CH / 4; ++i)
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                             dst + (i >> 1) * kAtom + ((((c + 4 * i) ^ r) & 7) << 4)),
-                                         "l"(src + 32 * i), "r"(real ? 16 : 0)
-                                         : "memory");
-                        h += 16 % a.group;
-                        tok += 16 / a.group;
-                        if (h >= a.group) {
-                            h -= a.group;
-                            ++tok;
+                        for (int k = 0; k < kAtOnce; ++k) {
+                            who[k] = many && r0 + 16 * k < end ? a.vm[u.m0 + tok] : tok;
+                            head[k] = h;
+                            h += 16 % a.group;
+                            tok += 16 / a.group;
+                            if (h >= a.group) {
+                                h -= a.group;
+                                ++tok;
+                            }
+                        }
+#pragma unroll
+                        for (int k = 0; k < kAtOnce; ++k) {
+                            const int r = r0 + 16 * k;
+                            if (r >= end) break;
+                            const bool real = who[k] >= 0;
+                            const T *src = q + (row0 + (real ? who[k] : 0)) * a.q_stride + (int64_t)head[k] * D;
+                            const uint32_t dst = base + x * C::kStage + r * 128;
+#pragma unroll
+                            for (int i = 0; i < CH / 4; ++i)
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                                 dst + (i >> 1) * kAtom + ((((c + 4 * i) ^ r) & 7) << 4)),
+                                             "l"(src + 32 * i), "r"(real ? 16 : 0)
+                                             : "memory");
                         }
                     }
                     asm volatile("cp.async.commit_group;" ::: "memory");
