@@ -622,7 +622,7 @@ ikv_status ikv_pages_compact(const ikv_shape *shape, ikv_cache *cache, const ikv
  *
  * Sequences that continue from one prompt (ikv_pages_fork) hold the same rows in their first
  * slots.  ikv_decode_attend_score reads those rows once for each sequence; ikv_prefix_attend_score
- * reads them once for all sequences of a group.
+ * computes with them for all sequences of a group at once.
  * ------------------------------------------------------------------------- */
 typedef struct {
     int32_t n_groups;            /* 0: no sequence shares anything */
@@ -632,14 +632,16 @@ typedef struct {
 } ikv_prefix;
 
 /* ikv_decode_attend_score with the groups' prefixes computed once: the same q, out, score, ema,
- * granularity and dead slots, and the same results up to the order of the sums.
+ * granularity and dead slots, and the same results up to the order of the sums and, with bf16 caches, the rounding
+ * of the weights to bf16 for the product with V (at most 2^-8 of sum w |V|; the two calls round them against
+ * different maxima).  Scores without tensor cores (fp32, other pages) read K of the prefix once a member.
  *  - K and V of slots 0 .. P - 1 of a group's members are read from the first member's pages, with
  *    P = min(len[i], the members' lengths); what the other members' tables hold there is not looked
  *    at (shared pages and copies serve alike).  Each member's liveness (pos) is its own.
  *  - Sequences in no group, and slots behind the prefix, are read from their own pages.
  *  - A sequence without a live slot gets out = 0.  Slots outside a sequence are never used, whatever
  *    they hold, and a row that a query does not see (dead, or another sequence's) never reaches its
- *    output, NaN and infinities included.
+ *    output, NaN and infinities included.  q and out must not overlap.
  *  - Where a bounded wait ran out (bit 0 of the device error word) out is undefined; score and ema hold whole
  *    results or what they held before, and before in all places if it was the attention's.
  *  - A member that is no sequence number, or that an earlier entry names already, is left out, and so
@@ -677,7 +679,7 @@ typedef struct {
 } ikv_window;
 
 /*  q: row r holds a token's q_heads * head_dim values (dtype) at r * q_stride; out likewise.  Rows of out
- *  that belong to no query are left as they are; the sequences' rows must not overlap in out.
+ *  that belong to no query are left as they are; the sequences' rows must not overlap in out, nor q and out.
  * A query in front of the first slot (count[b] > len[b]) sees nothing.  What a query does not see
  * never reaches its output, NaN and infinities included.  Dense caches only (IKV_ERR_UNSUPPORTED for
  * code_bits = 4); no page size is excluded, bf16 rows in pages of a multiple of 8 slots take the tensor

@@ -40,7 +40,9 @@ struct alignas(16) RowsUnit {                   // 64 bytes
 // What a tile of a pair (unit, KV head) costs, and what the pair costs besides, for its first products, which
 // nothing overlaps, and its output.  In the tensor-core kernel a tile took 1.0 to 1.4 us with one row tile and 1.4 to
 // 1.6 with two, a pair besides 2.2 to 3.4 and 4.5 to 5.5.  (Shares of tiles alone: a window of 2k over 8k tokens
-// 290 us a call instead of 223, the CTA with the shortest pairs 40% behind the others.)
+// 290 us a call instead of 223, the CTA with the shortest pairs 40% behind the others.)  A pair's constant is at the low
+// end of what it took, and a part that continues a cut pair pays a start and an output that nothing counts: in three
+// decode batches the last CTA, with the most short pairs, ends 31, 46 and 48% behind the mean.
 struct RowsCost {
     int32_t tile, extra;
 };

@@ -83,7 +83,9 @@ __device__ __forceinline__ void merge_rows(const Run &x, const Run &y, int rows,
 // Grid: (CTAs of the attention, row blocks).  CTA c: the pair that the border in front of share c cuts,
 // if no earlier border cuts it.
 // kAhead: parts in flight.  2 for prompts, whose pairs have rarely more and many rows (37 us after a prompt of 8k with
-// 8, for want of resident CTAs, 20 with 2), 8 for few rows, split over many shares.
+// 8, for want of resident CTAs, 20 with 2), 8 for few rows, split over many shares.  A call of 4 sequences with 4k slots,
+// by tokens a sequence at 32 / 8 heads, 2 / 8 in flight: 1 token 24.9 / 23.9 us, 16 (64 rows) 31.5 / 30.6, 64 (256 rows,
+// one unit) 54.2 / 52.8, 256 (four units) 81.8 / 88.9.
 template <int D, typename T, int kAhead>
 __global__ void __launch_bounds__(2 * D, (kAhead == 2 ? 1280 : 768) / (2 * D)) rows_merge_window_kernel(const RowsArgs a) {
     pdl_wait();
@@ -154,7 +156,7 @@ cudaError_t launch_merge(const RowsArgs &a, cudaStream_t st) {
                            : launch_k(rows_merge_window_kernel<D, T, 8>, dim3(a.ctas, y), dim3(2 * D), 0, st, a);
 }
 
-// Scores without tensor cores: K once more, with each row's maximum M and sum of weights W,
+// Scores without tensor cores: K once more, a shared prefix's once a member, with each row's maximum M and sum of weights W,
 //     score = mean over the row's heads of 2^(q . k scale - M) / W.
 // A CTA: 32 slots of a sequence, a lane a slot, a warp every eighth KV head with all of its query heads.  Each lane
 // reads its own row of K, whose lines the first-level cache holds until they are used up; no warp waits for another

@@ -13,7 +13,7 @@
 // three stages, S^T through two halves of tensor memory.
 //
 // Measured: two prefixes of 8k for 16 sequences each, 32 / 8 heads of 128, mean over all 32: 23 us, of
-// which K's 82 MB out of HBM take 12; 305 items for 152 SMs leave a third round to one of them.
+// which K's 82 MB out of HBM take 12; 305 items are dealt to 152 CTAs by threes, so that 50 have none.
 #include "rows_tc.cuh"
 
 namespace ikv {

@@ -23,10 +23,10 @@
 // fills zeros and reads nothing.  Every wait is bounded; on timeout the CTA sets the error word, drains what is in
 // flight and returns.
 //
-// Measured: a causal prompt of 16384 tokens, 32 / 8 heads of 128, 1475 us (1.49 PFLOP/s; 1.45 us a step of 256 rows by
-// 128 slots, 1.05 at the tensor cores' rate: their issue and its hand-offs are what is left).  Two prefixes of 8k for 16
-// sequences each: 31 of 48 us in here, 64 KB of K and V every 1.05 us and SM (93% of the copy rate) between the starts
-// and outputs of its pairs.
+// Measured: a causal prompt of 16384 tokens, 32 / 8 heads of 128, 1462 us (1.50 PFLOP/s), 869 steps of 256 rows by 128
+// slots a CTA: 1.68 us a step with all that is besides, 1.36 at the rate that the library's large products reach.  Two
+// prefixes of 8k for 16 sequences each: 31 of 49 us in here, 154 MB of K and V at 73% of the copy rate, the starts and
+// outputs of 256 short pairs among them.
 #include "rows_tc.cuh"
 
 namespace ikv {
@@ -275,10 +275,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool pair = __shfl_sync(0xffffffffu, part_at()->u.n * a.group > tile_rows, 0);
                 // Slots behind a sequence's last, and those in front of a unit's first (of a page that begins earlier, of a
                 // prefix that is read elsewhere), may hold anything, a pool that was never written, and 0 * NaN would have
-                // every row of the part computed again: their rows of V, at most 7 at either end, become zeros.  (1.3 % of
-                // two prefixes of 8k, 0.7 % of prompts)
-                const int hi = part_at()->j0 + n == part_at()->u.nt && part_at()->u.open ? part_at()->u.hi : 0;
-                const int lo = part_at()->j0 == 0 && rows_tile(part_at()->u, 0) == part_at()->u.lo >> 7 ? part_at()->u.lo : 0;
+                // every row of the part computed again: their rows of V, at most 7 at either end, become zeros.  (Those in
+                // front cost two prefixes of 8k 0.8 us of 49, a small call 0.3 of 18.5.)
+                const Part *p = part_at();
+                const int hi = __shfl_sync(0xffffffffu, p->j0 + n == p->u.nt && p->u.open ? p->u.hi : 0, 0);
+                const int lo = __shfl_sync(0xffffffffu, p->j0 == 0 && rows_tile(p->u, 0) == p->u.lo >> 7 ? p->u.lo : 0, 0);
                 // rows of V behind or in front of slot `end`, in its group of 8
                 auto clean = [&](Stage v, int end, bool behind) {
                     if (end % 8 == 0) return;
